@@ -52,7 +52,8 @@ typedef enum {
   HILO_E_SHAPE = 2,     /* grid not even/positive, dim != heads*head_dim, size limits (below) */
   HILO_E_DTYPE = 3,     /* dtype unknown, or head_dim unsupported for the dtype               */
   HILO_E_PARAM = 4,     /* selection mode or token set unknown, tau not finite, keep out of   */
-                        /* [0, NB], dilate_r negative, n_blocks negative                      */
+                        /* [0, NB], dilate_r negative, n_blocks negative; an operator's flag,  */
+                        /* constant or alignment (below)                                      */
   HILO_E_WORKSPACE = 5, /* workspace smaller than hilo_workspace_bytes()                      */
   HILO_E_DEVICE = 6     /* a HIP launch failed, or no GPU                                     */
 } hilo_status;
@@ -352,6 +353,140 @@ hilo_status hilo_attention_core_fp8(const hilo_shape *shape, const void *qkv8,
 #define HILO_ATTN_SCRATCH_BYTES ((size_t)72 * 1024 * 1024)
 hilo_status hilo_attention_core_noalloc(const hilo_shape *shape, const void *qkv,
                                         const int32_t *cu_seqlens, void *out, void *stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * Operators of a block with rotary positions, norms on both sides of each half, and int8
+ * projections.  They work on the same packed rows as the block calls, without a hilo_shape:
+ *   rows        rows of the buffers (their capacity, below 2^28)
+ *   batch, text_len, cu_seqlens
+ *               as everywhere: sample s is rows [cu_seqlens[s], cu_seqlens[s+1]), its last text_len
+ *               rows are text (stream 1), the others image rows (stream 0); cu_seqlens [batch + 1]
+ *               is device memory, starts at 0, does not decrease and ends at most at `rows`; every
+ *               sample has at least text_len rows.  A sample, or its image rows, may be empty.
+ * Rows at or behind cu_seqlens[batch] are neither read nor written.  `dtype` (HILO_F32, HILO_BF16) is
+ * the type of every tensor called "dtype" below.  Pointers are aligned to 16 bytes, tensors of bf16
+ * and of 8-bit codes that are read or written 8 bytes at a time to 8 (HILO_E_PARAM otherwise),
+ * unless an entry says that any alignment will do.  rows == 0 enqueues nothing.
+ * --------------------------------------------------------------------------------------------- */
+
+/* Rotary positions with several axes (time, height, width, ...) on the heads of packed rows.  The
+ * first 2 n columns of a head (n = sum of pairs[a], 1 <= n <= head_dim / 2) turn, the others pass
+ * through.  Pair j belongs to axis a when it is one of the pairs[a] pairs behind those of the axes
+ * before, as its i-th; with t = pos[row][a] * w
+ *   (u, v) -> (u cos t - v sin t, v cos t + u sin t)
+ *   w = base[a]^(-i / pairs[a]), or with ONE_SPECTRUM base[0]^(-j / n)
+ * (u, v) are columns j and j + n of the head, or with ADJACENT 2 j and 2 j + 1.  Angles are formed and
+ * reduced in 64 bits, their cosines and sines rounded to float32, the turn made in float32 and rounded
+ * to dtype once.  Limits: 1 <= axes <= 4; heads > 0; head_dim even, 2 .. 256 (HILO_E_SHAPE); flags known,
+ * base finite and positive, pairs not negative (HILO_E_PARAM).                                  */
+typedef enum { HILO_ROPE_ADJACENT = 1, HILO_ROPE_ONE_SPECTRUM = 2 } hilo_rope_flags;
+typedef struct {
+  int32_t heads, head_dim, axes, flags;
+  int32_t pairs[4];
+  double base[4];
+} hilo_rotary;
+
+/* x [rows][ldx] dtype: heads * head_dim columns from x on, ldx >= heads * head_dim values between rows
+ * (the q and k columns of a packed projection: heads = 2 * heads of the block, ldx = 3 * dim); out
+ * [rows][ldo] dtype alike; out == x with ldo == ldx turns in place, any other overlap of the two is
+ * not supported.  pos [rows][axes] float32, finite.  rows_end: device pointer to the number of rows in
+ * use (cu_seqlens + batch), or NULL for `rows`.  backward != 0 turns by -t: the gradient of x from
+ * that of out (in place too).  Any alignment will do; 16 bytes is the fastest.                  */
+hilo_status hilo_rope(int32_t dtype, const hilo_rotary *rotary, const void *x, int64_t ldx, const float *pos,
+                      int64_t rows, const int32_t *rows_end, int32_t backward, void *out, int64_t ldo,
+                      void *stream);
+
+/* Positions (time, height, width) of a compressed sequence's tokens, for hilo_rope with three axes:
+ * image i of its sample, then a fine patch's row and column on the grid, or the centre of a pooled
+ * block (row 2 bi + 0.5, column 2 bj + 0.5); text row t gets text_pos [text_len][3] float32 (t-th row),
+ * or zeros where text_pos is NULL.  fine_idx, pool_idx, counts, cu_seqlens, seg_off as hilo_select
+ * leaves them; pos [T_max][3] float32, rows past cu_seqlens[batch] untouched.                   */
+hilo_status hilo_token_positions(const hilo_shape *shape, const int32_t *fine_idx, const int32_t *pool_idx,
+                                 const int32_t *counts, const int32_t *cu_seqlens, const int32_t *seg_off,
+                                 const float *text_pos, float *pos, void *stream);
+
+/* Norms before and after a block, fused with the block's gate and residual scale.  Per row, with the
+ * vectors of its sample and stream and the gains of its stream:
+ *   x_out = residual_scale * x + gate * (norm(y) * post_gain)         y: what the block made of its input
+ *   h     = norm(x_out) * pre_gain * (1 + scale) + shift              h: the next block's input
+ * norm(v) = (v - mean) / sqrt(mean((v - mean)^2) + eps) for LAYER, v / sqrt(mean(v^2) + eps) for RMS, over
+ * the dim values of the row, in float32.  gate, shift, scale: float32, the vector of (sample s, stream
+ * k) at (2 s + k) * mod_stride (in the modulation [batch][2][6][dim]: mod_stride = 6 * dim, gate = mod +
+ * 2 * dim, ...); NULL: 1, 0, 0.  post_gain, pre_gain: float32 [dim] by stream (image, text); NULL: 1.
+ * kind unknown, eps negative or not finite, residual_scale not finite, mod_stride no multiple of 4
+ * or (where it is used) less than dim: HILO_E_PARAM.                                            */
+typedef enum { HILO_NORM_LAYER = 0, HILO_NORM_RMS = 1 } hilo_norm_kind;
+typedef struct {
+  int32_t kind;
+  float eps, residual_scale;
+  int64_t mod_stride;
+  const float *gate, *shift, *scale;
+  const float *post_gain[2], *pre_gain[2];
+} hilo_norms;
+
+/* y [rows][dim] dtype, x and x_out [rows][dim] float32 (x_out == x: in place); h [rows][dim] dtype, or with
+ * h_scale [rows] float32 int8 codes and row scales as hilo_quantize_rows_i8 forms them from the float32
+ * values.  y NULL: no norm after a block, h from x itself (x_out must be NULL too); h NULL: no norm
+ * before the next; not both (HILO_E_NULL).  stats [rows][4] float32 or NULL: mean and 1 / deviation of y
+ * and of x_out (0 where a norm is left out, mean 0 for RMS), for the backward pass.
+ * 4 <= dim <= 8192, dim % 4 == 0 (HILO_E_SHAPE); h as codes needs dim % 16 == 0 for hilo_linear_i8.    */
+hilo_status hilo_norm_residual(int32_t dtype, const hilo_norms *norms, const void *y, const float *x,
+                               float *x_out, void *h, float *h_scale, float *stats, int64_t rows, int32_t dim,
+                               int32_t batch, int32_t text_len, const int32_t *cu_seqlens, void *stream);
+
+/* Gradients of the vectors: gate, shift, scale float32 at (2 s + k) * mod_stride like the vectors, sums over
+ * the rows of (sample s, stream k), zero where it has none; the gains' by stream, sums over the rows of
+ * all samples -- the same pointer for both streams: over both (for a gain that both share).  Any NULL.  */
+typedef struct {
+  int64_t mod_stride;
+  float *gate, *shift, *scale;
+  float *post_gain[2], *pre_gain[2];
+} hilo_norm_grads;
+
+/* The backward pass of hilo_norm_residual: dx_out [rows][dim] float32, the gradient that reaches x_out from
+ * elsewhere (NULL: none); dh [rows][dim] dtype (NULL: the forward pass had no h); y and x_out as there
+ * (y NULL: it had none; then dx is the gradient of x without the residual scale), stats what it left.
+ * dx [rows][dim] float32 (dx == dx_out: in place), dy [rows][dim] dtype with y (dy == dh or y: in place).
+ * grads NULL: none.  workspace: ws_bytes >= hilo_norm_residual_workspace_bytes(rows, batch, dim) of device
+ * scratch where grads is given, contents undefined after; calls that may overlap, two captured
+ * graphs among them, need one each.  Sums are taken in a fixed order: equal inputs give equal bits.      */
+hilo_status hilo_norm_residual_backward(int32_t dtype, const hilo_norms *norms, const float *dx_out,
+                                        const void *dh, const void *y, const float *x_out, const float *stats,
+                                        float *dx, void *dy, const hilo_norm_grads *grads, int64_t rows,
+                                        int32_t dim, int32_t batch, int32_t text_len, const int32_t *cu_seqlens,
+                                        void *workspace, size_t ws_bytes, void *stream);
+size_t hilo_norm_residual_workspace_bytes(int64_t rows, int32_t batch, int32_t dim); /* 0 if invalid */
+
+/* Per-row int8 quantisation of x [rows][cols] dtype (every step one float32 operation):
+ *   amax = max |x|;  inv = 127 / amax;  code = round-to-nearest-even(clamp(x * inv, -127, 127));
+ *   scale = amax / 127
+ * rows with amax < 2^-120 get codes and scale 0; a row that holds an infinity or a NaN gets a scale that is
+ * not finite.  codes [rows][cols] int8, scale [rows] float32.  cols > 0, cols % 16 == 0, cols <= 65536.
+ * For weights once (a row per output channel) and for activations (a row per token).  limit: device
+ * pointer to the number of rows in use, or NULL for `rows`.                                     */
+hilo_status hilo_quantize_rows_i8(int32_t dtype, const void *x, int64_t rows, int64_t cols, const int32_t *limit,
+                                  int8_t *codes, float *scale, void *stream);
+
+/* Matrix product in 8-bit integers with scales for each token and each output channel:
+ *   acc[m][n] = sum_k a[m][k] * w[n][k]  (int32, exact)
+ *   out[m][n] = act(acc[m][n] * (a_scale[m] * s[n]) + b[n])
+ * act: none, or GELU_tanh as in hilo_mlp.  w: image and text stream's weights (stream 1 is not looked at when
+ * text_len is 0).  x [rows][in_dim]: int8 codes with x_scale [rows] float32, or with x_scale NULL dtype,
+ * quantised as hilo_quantize_rows_i8 does within the call.  out [rows][out_dim] dtype.
+ * in_dim % 16 == 0, 16 .. 65536; out_dim % 4 == 0, 4 .. 2^24; act unknown: HILO_E_PARAM.
+ * workspace: ws_bytes >= hilo_linear_i8_workspace_bytes(rows, in_dim) of device scratch, contents undefined
+ * after; calls that may overlap, two captured graphs among them, need one each.                 */
+typedef enum { HILO_ACT_NONE = 0, HILO_ACT_GELU = 1 } hilo_act;
+typedef struct {
+  const int8_t *w; /* [out_dim][in_dim] codes */
+  const float *s;  /* [out_dim] scales        */
+  const void *b;   /* [out_dim] dtype or NULL */
+} hilo_linear_w_i8;
+hilo_status hilo_linear_i8(int32_t dtype, const hilo_linear_w_i8 w[2], const void *x, const float *x_scale,
+                           void *out, int64_t rows, int32_t in_dim, int32_t out_dim, int32_t act, int32_t batch,
+                           int32_t text_len, const int32_t *cu_seqlens, void *workspace, size_t ws_bytes,
+                           void *stream);
+size_t hilo_linear_i8_workspace_bytes(int64_t rows, int32_t in_dim); /* 0 if invalid */
 
 size_t hilo_workspace_bytes(const hilo_shape *shape); /* 0 if the shape is invalid */
 /* T_max = batch * (images * (N + N/4) + text_len): the most rows any token set can produce

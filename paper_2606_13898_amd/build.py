@@ -15,7 +15,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libhilo.so")
-SOURCES = ["select.hip", "pack.hip", "gemm.hip", "attention.hip", "abi.hip"]
+SOURCES = ["select.hip", "pack.hip", "gemm.hip", "attention.hip", "rope.hip", "norm.hip", "linear.hip", "abi.hip"]
 ARCH = "gfx950"
 # Per-source flags.  attention.hip: its maxima see only finite scores and -inf masks, and without
 # NaN semantics fmaxf needs no quieting of each MFMA result before the comparison

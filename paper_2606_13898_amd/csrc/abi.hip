@@ -15,12 +15,14 @@ namespace {
 
 enum Kind {
   K_SCORE, K_SELECT, K_LAYOUT, K_COMPRESS, K_NORM_ATTN, K_GEMM_QKV, K_ATTN_CORE, K_GEMM_O,
-  K_NORM_MLP, K_GEMM_FC1, K_GEMM_FC2, K_DECOMPRESS, K_QUANT_ATTN, K_QUANT_MLP, K_COUNT
+  K_NORM_MLP, K_GEMM_FC1, K_GEMM_FC2, K_DECOMPRESS, K_QUANT_ATTN, K_QUANT_MLP,
+  K_ROPE, K_POSITIONS, K_NORM_RESIDUAL, K_NORM_RESIDUAL_BACK, K_QUANT_I8, K_LINEAR_I8, K_COUNT
 };
 const char *kKindNames[K_COUNT] = {"score", "select", "layout", "compress", "rownorm_attn",
                                    "gemm_qkv", "attention_core", "gemm_o", "rownorm_mlp",
                                    "gemm_fc1", "gemm_fc2", "decompress", "quantize_attn",
-                                   "quantize_mlp"};
+                                   "quantize_mlp", "rope", "token_positions", "norm_residual",
+                                   "norm_residual_backward", "quantize_i8", "linear_i8"};
 
 struct ProfRec {
   int kind;
@@ -172,7 +174,7 @@ const char *hilo_status_str(int32_t st) {
     case HILO_E_NULL: return "required pointer is NULL";
     case HILO_E_SHAPE: return "invalid or unsupported shape";
     case HILO_E_DTYPE: return "unsupported dtype or head_dim";
-    case HILO_E_PARAM: return "invalid selection parameter";
+    case HILO_E_PARAM: return "invalid parameter or misaligned pointer";
     case HILO_E_WORKSPACE: return "workspace too small";
     case HILO_E_DEVICE: return "HIP launch failed or no GPU";
     default: return "unknown status";
@@ -743,6 +745,256 @@ hilo_status hilo_blocks(const hilo_shape *s, float *z, const int32_t *cu_seqlens
     if ((e = enqueue_mlp(s, z, cu_seqlens, mlp_w + 2 * l, nullptr, ml, workspace, st)) != HILO_OK) return e;
   }
   return HILO_OK;
+}
+
+}  // extern "C"
+
+// --------------------------------------------------------------- rotary, sandwich norms, int8 products
+
+namespace {
+
+bool aligned(const void *p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
+
+hilo_status check_dtype(int32_t dtype) { return dtype == HILO_F32 || dtype == HILO_BF16 ? HILO_OK : HILO_E_DTYPE; }
+
+hilo_status check_rows(int64_t rows, int32_t batch, int32_t text_len) {
+  if (rows < 0 || rows >= (1LL << 28) || batch <= 0 || text_len < 0) return HILO_E_SHAPE;
+  return (long long)batch * text_len <= rows && batch < (1 << 20) ? HILO_OK : HILO_E_SHAPE;
+}
+
+hilo_status check_norms(int32_t dtype, const hilo_norms *n, int32_t dim) {
+  hilo_status e = check_dtype(dtype);
+  if (e != HILO_OK) return e;
+  if (!n) return HILO_E_NULL;
+  if (dim < 4 || dim > 8192 || dim % 4 != 0) return HILO_E_SHAPE;
+  if (n->kind != HILO_NORM_LAYER && n->kind != HILO_NORM_RMS) return HILO_E_PARAM;
+  if (!std::isfinite(n->eps) || n->eps < 0.f || !std::isfinite(n->residual_scale)) return HILO_E_PARAM;
+  if ((n->gate || n->shift || n->scale) && (n->mod_stride % 4 != 0 || n->mod_stride < dim)) return HILO_E_PARAM;
+  const void *v[7] = {n->gate, n->shift, n->scale, n->post_gain[0], n->post_gain[1], n->pre_gain[0], n->pre_gain[1]};
+  for (const void *q : v)
+    if (!aligned(q, 16)) return HILO_E_PARAM;
+  return HILO_OK;
+}
+
+// 8 bytes of bf16 or 16 of float32 at a time
+size_t vec_align(int32_t dtype) { return dtype == HILO_BF16 ? 8 : 16; }
+
+}  // namespace
+
+extern "C" {
+
+hilo_status hilo_rope(int32_t dtype, const hilo_rotary *r, const void *x, int64_t ldx, const float *pos,
+                      int64_t rows, const int32_t *rows_end, int32_t backward, void *out, int64_t ldo, void *stream) {
+  hilo_status e = check_dtype(dtype);
+  if (e != HILO_OK) return e;
+  if (!r) return HILO_E_NULL;
+  if (r->axes < 1 || r->axes > 4 || r->heads <= 0 || r->head_dim < 2 || r->head_dim > 2 * kRopeMaxPairs || r->head_dim % 2)
+    return HILO_E_SHAPE;
+  if (r->flags & ~(HILO_ROPE_ADJACENT | HILO_ROPE_ONE_SPECTRUM)) return HILO_E_PARAM;
+  long long n = 0;
+  for (int a = 0; a < r->axes; ++a) {
+    if (r->pairs[a] < 0 || !std::isfinite(r->base[a]) || !(r->base[a] > 0.0)) return HILO_E_PARAM;
+    n += r->pairs[a];
+  }
+  const long long width = (long long)r->heads * r->head_dim;
+  if (n < 1 || 2 * n > r->head_dim || width > (1 << 24)) return HILO_E_SHAPE;
+  if (rows < 0 || rows >= (1LL << 28) || ldx < width || ldo < width || ldx >= (1LL << 31) || ldo >= (1LL << 31)) return HILO_E_SHAPE;
+  if (!x || !pos || !out) return HILO_E_NULL;
+  const size_t es = dtype == HILO_BF16 ? 2 : 4;
+  if (!aligned(x, es) || !aligned(out, es) || !aligned(pos, 4) || (x == out && ldx != ldo)) return HILO_E_PARAM;
+  if (rows == 0) return HILO_OK;
+  if (!have_device()) return HILO_E_DEVICE;
+  RopeProblem p{};
+  p.x = x; p.ldx = ldx;
+  p.out = out; p.ldo = ldo;
+  p.pos = pos;
+  p.rows_end = rows_end;
+  p.rows = int(rows);
+  p.heads = r->heads; p.hd = r->head_dim; p.axes = r->axes; p.n = int(n);
+  p.adjacent = (r->flags & HILO_ROPE_ADJACENT) != 0;
+  p.backward = backward != 0;
+  // frequencies in turns: a geometric series by one power and products (off by less than 128 roundings of 64 bits)
+  const bool one = (r->flags & HILO_ROPE_ONE_SPECTRUM) != 0;
+  constexpr double kTurn = 1.0 / 6.283185307179586476925;
+  double w = kTurn, step = one ? std::pow(r->base[0], -1.0 / double(n)) : 1.0;
+  int j = 0;
+  for (int a = 0; a < 4; ++a) {
+    p.first[a] = j;
+    if (a >= r->axes || r->pairs[a] == 0) continue;
+    if (!one) {
+      w = kTurn;
+      step = std::pow(r->base[a], -1.0 / double(r->pairs[a]));
+    }
+    for (int i = 0; i < r->pairs[a]; ++i, w *= step) p.freq[j++] = w;
+  }
+  hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  return dev_status(timed(K_ROPE, st, [&] { return launch_rope(dtype == HILO_BF16, p, st); }));
+}
+
+hilo_status hilo_token_positions(const hilo_shape *s, const int32_t *fine_idx, const int32_t *pool_idx,
+                                 const int32_t *counts, const int32_t *cu_seqlens, const int32_t *seg_off,
+                                 const float *text_pos, float *pos, void *stream) {
+  hilo_status e = check_grid(s);
+  if (e != HILO_OK) return e;
+  if (!fine_idx || !pool_idx || !counts || !cu_seqlens || !seg_off || !pos) return HILO_E_NULL;
+  if (!have_device()) return HILO_E_DEVICE;
+  hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  return dev_status(timed(K_POSITIONS, st, [&] {
+    return launch_token_positions(fine_idx, pool_idx, counts, cu_seqlens, seg_off, text_pos, pos, s->batch, s->images,
+                                  s->grid_h, s->grid_w, s->text_len, st);
+  }));
+}
+
+hilo_status hilo_norm_residual(int32_t dtype, const hilo_norms *n, const void *y, const float *x, float *x_out,
+                               void *h, float *h_scale, float *stats, int64_t rows, int32_t dim, int32_t batch,
+                               int32_t text_len, const int32_t *cu_seqlens, void *stream) {
+  hilo_status e = check_norms(dtype, n, dim);
+  if (e != HILO_OK || (e = check_rows(rows, batch, text_len)) != HILO_OK) return e;
+  if (!x || !cu_seqlens || (!y && !h) || (y != nullptr) != (x_out != nullptr) || (h_scale && !h)) return HILO_E_NULL;
+  if (!aligned(x, 16) || !aligned(x_out, 16) || !aligned(y, vec_align(dtype)) || !aligned(stats, 16) ||
+      !aligned(h, h_scale ? 4 : vec_align(dtype)) || !aligned(h_scale, 4))
+    return HILO_E_PARAM;
+  if (rows == 0) return HILO_OK;
+  if (!have_device()) return HILO_E_DEVICE;
+  NormProblem p{};
+  p.cu = cu_seqlens;
+  p.B = batch; p.L = text_len; p.D = dim; p.rows = int(rows);
+  p.rms = n->kind == HILO_NORM_RMS;
+  p.eps = n->eps;
+  p.alpha = n->residual_scale;
+  p.gate = n->gate; p.shift = n->shift; p.scale = n->scale;
+  p.mod_stride = n->mod_stride;
+  for (int k = 0; k < 2; ++k) {
+    p.post[k] = n->post_gain[k];
+    p.pre[k] = n->pre_gain[k];
+  }
+  p.y = y; p.x = x; p.x_out = x_out;
+  p.h = h; p.h_scale = h_scale;
+  p.stats = stats;
+  hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  return dev_status(timed(K_NORM_RESIDUAL, st, [&] { return launch_norm_residual(dtype == HILO_BF16, p, st); }));
+}
+
+size_t hilo_norm_residual_workspace_bytes(int64_t rows, int32_t batch, int32_t dim) {
+  if (check_rows(rows, batch, 0) != HILO_OK || dim < 4 || dim > 8192 || dim % 4 != 0) return 0;
+  return align256(norm_back_bytes(int(rows), batch, dim));
+}
+
+hilo_status hilo_norm_residual_backward(int32_t dtype, const hilo_norms *n, const float *dx_out, const void *dh,
+                                        const void *y, const float *x_out, const float *stats, float *dx, void *dy,
+                                        const hilo_norm_grads *g, int64_t rows, int32_t dim, int32_t batch,
+                                        int32_t text_len, const int32_t *cu_seqlens, void *workspace, size_t ws_bytes,
+                                        void *stream) {
+  hilo_status e = check_norms(dtype, n, dim);
+  if (e != HILO_OK || (e = check_rows(rows, batch, text_len)) != HILO_OK) return e;
+  if (!stats || !dx || !cu_seqlens || (!y && !dh) || (dh && !x_out) || (y != nullptr) != (dy != nullptr) || (g && !workspace))
+    return HILO_E_NULL;
+  if (!aligned(dx_out, 16) || !aligned(dh, vec_align(dtype)) || !aligned(y, vec_align(dtype)) || !aligned(x_out, 16) ||
+      !aligned(stats, 16) || !aligned(dx, 16) || !aligned(dy, vec_align(dtype)) || !aligned(workspace, 16))
+    return HILO_E_PARAM;
+  if (g) {
+    if ((g->gate || g->shift || g->scale) && (g->mod_stride % 4 != 0 || g->mod_stride < dim)) return HILO_E_PARAM;
+    const void *v[7] = {g->gate, g->shift, g->scale, g->post_gain[0], g->post_gain[1], g->pre_gain[0], g->pre_gain[1]};
+    for (const void *q : v)
+      if (!aligned(q, 16)) return HILO_E_PARAM;
+    if (ws_bytes < hilo_norm_residual_workspace_bytes(rows, batch, dim)) return HILO_E_WORKSPACE;
+  }
+  if (rows == 0 && !g) return HILO_OK;
+  if (!have_device()) return HILO_E_DEVICE;
+  NormBackProblem p{};
+  p.cu = cu_seqlens;
+  p.B = batch; p.L = text_len; p.D = dim; p.rows = int(rows);
+  p.rms = n->kind == HILO_NORM_RMS;
+  p.alpha = y ? n->residual_scale : 1.f;
+  p.gate = n->gate; p.scale = n->scale;
+  p.mod_stride = n->mod_stride;
+  for (int k = 0; k < 2; ++k) {
+    p.post[k] = n->post_gain[k];
+    p.pre[k] = n->pre_gain[k];
+  }
+  p.dx_out = dx_out; p.dh = dh; p.y = y; p.x_out = x_out; p.stats = stats;
+  p.dx = dx; p.dy = dy;
+  if (g) {
+    p.dgate = g->gate; p.dshift = g->shift; p.dscale = g->scale;
+    p.dmod_stride = g->mod_stride;
+    for (int k = 0; k < 2; ++k) {
+      p.dpost[k] = g->post_gain[k];
+      p.dpre[k] = g->pre_gain[k];
+    }
+    p.part = reinterpret_cast<float *>(workspace);
+  }
+  hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  return dev_status(timed(K_NORM_RESIDUAL_BACK, st, [&] { return launch_norm_residual_back(dtype == HILO_BF16, p, st); }));
+}
+
+hilo_status hilo_quantize_rows_i8(int32_t dtype, const void *x, int64_t rows, int64_t cols, const int32_t *limit,
+                                  int8_t *codes, float *scale, void *stream) {
+  hilo_status e = check_dtype(dtype);
+  if (e != HILO_OK) return e;
+  if (rows < 0 || rows >= (1LL << 28) || cols <= 0 || cols % 16 != 0 || cols > 65536) return HILO_E_SHAPE;
+  if (!x || !codes || !scale) return HILO_E_NULL;
+  if (!aligned(x, 16) || !aligned(codes, 8) || !aligned(scale, 4)) return HILO_E_PARAM;
+  if (rows == 0) return HILO_OK;
+  if (!have_device()) return HILO_E_DEVICE;
+  hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  return dev_status(timed(K_QUANT_I8, st, [&] {
+    return launch_quantize_rows_i8(dtype == HILO_BF16, x, int(rows), int(cols), codes, scale, limit, st);
+  }));
+}
+
+// Workspace: the codes and scales of float rows, then the partial tiles.
+size_t hilo_linear_i8_workspace_bytes(int64_t rows, int32_t in_dim) {
+  if (check_rows(rows, 1, 0) != HILO_OK || in_dim < 16 || in_dim > 65536 || in_dim % 16 != 0) return 0;
+  return align256(size_t(rows) * in_dim) + align256(size_t(rows) * sizeof(float)) + linear_i8_part_bytes(rows) + 256;
+}
+
+hilo_status hilo_linear_i8(int32_t dtype, const hilo_linear_w_i8 w[2], const void *x, const float *x_scale, void *out,
+                           int64_t rows, int32_t in_dim, int32_t out_dim, int32_t act, int32_t batch, int32_t text_len,
+                           const int32_t *cu_seqlens, void *workspace, size_t ws_bytes, void *stream) {
+  hilo_status e = check_dtype(dtype);
+  if (e != HILO_OK || (e = check_rows(rows, batch, text_len)) != HILO_OK) return e;
+  if (in_dim < 16 || in_dim > 65536 || in_dim % 16 != 0 || out_dim < 4 || out_dim > (1 << 24) || out_dim % 4 != 0)
+    return HILO_E_SHAPE;
+  if (act != HILO_ACT_NONE && act != HILO_ACT_GELU) return HILO_E_PARAM;
+  if (!w || !x || !out || !cu_seqlens || !workspace) return HILO_E_NULL;
+  const int streams = text_len > 0 ? 2 : 1;
+  for (int k = 0; k < streams; ++k) {
+    if (!w[k].w || !w[k].s) return HILO_E_NULL;
+    if (!aligned(w[k].w, 16) || !aligned(w[k].s, 16) || !aligned(w[k].b, vec_align(dtype))) return HILO_E_PARAM;
+  }
+  if (!aligned(x, 16) || !aligned(x_scale, 4) || !aligned(out, vec_align(dtype)) || !aligned(workspace, 256)) return HILO_E_PARAM;
+  if (ws_bytes < hilo_linear_i8_workspace_bytes(rows, in_dim)) return HILO_E_WORKSPACE;
+  if (rows == 0) return HILO_OK;
+  if (!have_device()) return HILO_E_DEVICE;
+  hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  char *ws = reinterpret_cast<char *>(workspace);
+  int8_t *codes = reinterpret_cast<int8_t *>(ws);
+  float *scales = reinterpret_cast<float *>(ws + align256(size_t(rows) * in_dim));
+  GemmProblem p{};
+  p.A = x;
+  p.a_scale = x_scale;
+  if (!x_scale) {
+    const hipError_t he = timed(K_QUANT_I8, st, [&] {
+      return launch_quantize_rows_i8(dtype == HILO_BF16, x, int(rows), in_dim, codes, scales, cu_seqlens + batch, st);
+    });
+    if (he != hipSuccess) return HILO_E_DEVICE;
+    p.A = codes;
+    p.a_scale = scales;
+  }
+  p.lda = in_dim;
+  p.N = out_dim; p.K = in_dim;
+  p.out = out; p.ldo = out_dim;
+  p.cu = cu_seqlens;
+  p.B = batch; p.L = text_len;
+  p.max_img_rows = int(rows);
+  for (int k = 0; k < 2; ++k) {
+    const hilo_linear_w_i8 &v = w[k < streams ? k : 0];
+    p.W[k] = v.w;
+    p.w_scale[k] = v.s;
+    p.bias[k] = v.b;
+  }
+  p.part = reinterpret_cast<float *>(ws + align256(size_t(rows) * in_dim) + align256(size_t(rows) * sizeof(float)));
+  return dev_status(timed(K_LINEAR_I8, st, [&] { return launch_linear_i8(dtype == HILO_BF16, act == HILO_ACT_GELU, p, st); }));
 }
 
 hilo_status hilo_profile_enable(int32_t on) {

@@ -95,6 +95,25 @@ HILO_DEV int pow2_exponent(float amax) {
 // 2^-k for k in [-127, 127] as a float (always a normal number for the k above)
 HILO_DEV float pow2_inverse(int k) { return __uint_as_float(uint32_t(127 - k) << 23); }
 
+HILO_DEV uint32_t wave_max_u32(uint32_t v) {
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) v = max(v, uint32_t(__shfl_xor(int(v), off, 64)));
+  return v;
+}
+
+// int8 codes of a row with a float32 scale.  The row's largest magnitude is taken on the bits of |x|: they order as the
+// values do, infinity above every number and NaN above that, so a row that holds either gets a scale that is not
+// finite and nothing formed from it passes for a number.  Rows below 2^-120, whose inverse would overflow, count as 0.
+HILO_DEV uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7fffffffu; }
+HILO_DEV float i8_inverse(uint32_t top) {
+  return top < 0x03800000u || top >= 0x7f800000u ? 0.f : __fdiv_rn(127.0f, __uint_as_float(top));
+}
+HILO_DEV float i8_scale(uint32_t top) { return top < 0x03800000u ? 0.f : __fdiv_rn(__uint_as_float(top), 127.0f); }
+HILO_DEV uint32_t i8_code(float v) { return uint32_t(int(rintf(fminf(fmaxf(v, -127.f), 127.f)))) & 0xffu; }
+HILO_DEV uint32_t i8x4(float a, float b, float c, float d) {
+  return i8_code(a) | (i8_code(b) << 8) | (i8_code(c) << 16) | (i8_code(d) << 24);
+}
+
 // Sample boundary i of the packed sequence.  The boundaries do not change while a kernel runs, so
 // they are read through the constant address space: the compiler then uses scalar loads with their
 // own wait, where a vector load inside a pipelined loop is followed by a wait for every global load

@@ -16,23 +16,9 @@
 
 #include "common.h"
 #include "kernels.h"
+#include "tiles.h"
 
 namespace hilo {
-
-// tanh-approximated GELU, 0.5 u (1 + tanh(y)) with y = sqrt(2/pi) (u + 0.044715 u^3), evaluated
-// through the identity 0.5 (1 + tanh(y)) = 1 / (1 + exp(-2y)): one hardware exp2 and one
-// reciprocal (about one ulp each) instead of a full tanh.  Very negative u gives exp2 -> inf and
-// the result -0; very positive u gives exp2 -> 0 and the result u.
-HILO_DEV float gelu_tanh(float u) {
-  constexpr float c = -2.0f * 0.7978845608028654f * 1.4426950408889634f;  // -2 sqrt(2/pi) log2(e)
-  const float t = c * u * (1.0f + 0.044715f * u * u);
-  return u * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(t));
-}
-
-// Row range of a row tile; tiles of a sample are [image tiles][text tiles].
-struct TileRows {
-  int s, sigma, row0, nrows;
-};
 
 template <int EPI, bool BF16OUT>
 HILO_DEV void epilogue4(const GemmProblem &p, const TileRows &tr, int m, int n, const float *acc) {
@@ -83,37 +69,6 @@ HILO_DEV void epilogue4(const GemmProblem &p, const TileRows &tr, int m, int n, 
 // the wave's 1 KiB destination (the destination base is uniform, held in M0).
 HILO_DEV void g2lds16(const void *g, void *lds_wave_base) {
   __builtin_amdgcn_global_load_lds(g, (__attribute__((address_space(3))) void *)lds_wave_base, 16, 0, 0);
-}
-
-// Active row tiles of the ragged problem: per sample, ceil(image rows / BM) image tiles then
-// ceil(L / BM) text tiles.  Only the device knows the row counts, so every workgroup walks the
-// (few) segments itself.
-HILO_DEV int row_tiles_total(const GemmProblem &p, int BM) {
-  int R = 0;
-  for (int s = 0; s < p.B; ++s) {
-    const int nimg = cu_at(p.cu, s + 1) - p.L - cu_at(p.cu, s);
-    R += (nimg + BM - 1) / BM + (p.L + BM - 1) / BM;
-  }
-  return R;
-}
-
-HILO_DEV TileRows decode_row_tile(const GemmProblem &p, int BM, int r) {
-  TileRows tr{0, 0, 0, 0};
-  for (int s = 0; s < p.B; ++s) {
-    const int lo = cu_at(p.cu, s), hi = cu_at(p.cu, s + 1), ts = hi - p.L;
-    const int ti = (ts - lo + BM - 1) / BM, tt = (p.L + BM - 1) / BM;
-    if (r < ti) {
-      tr = TileRows{s, 0, lo + r * BM, min(BM, ts - (lo + r * BM))};
-      break;
-    }
-    r -= ti;
-    if (r < tt) {
-      tr = TileRows{s, 1, ts + r * BM, min(BM, hi - (ts + r * BM))};
-      break;
-    }
-    r -= tt;
-  }
-  return tr;
 }
 
 // Schedule of the projections over P = kGemmWorkgroups persistent workgroups (one per CU; a constant, so
@@ -385,16 +340,7 @@ struct SkTile {
   }
 };
 
-// Values that are the same on every lane, restated as such (the compiler otherwise keeps some of
-// the stream-K bookkeeping in VGPRs and branches on it with exec masks).
-HILO_DEV int uni(int v) { return __builtin_amdgcn_readfirstlane(v); }
-HILO_DEV float *uni(float *ptr) {
-  const uint64_t v = reinterpret_cast<uint64_t>(ptr);
-  const uint32_t lo = __builtin_amdgcn_readfirstlane(uint32_t(v)), hi = __builtin_amdgcn_readfirstlane(uint32_t(v >> 32));
-  return reinterpret_cast<float *>((uint64_t(hi) << 32) | lo);
-}
 HILO_DEV SkItem uni(const SkItem &x) { return SkItem{uni(x.t), uni(x.kb), uni(x.ke), uni(x.slot), uni(int(x.valid)) != 0}; }
-HILO_DEV TileRows uni(const TileRows &x) { return TileRows{uni(x.s), uni(x.sigma), uni(x.row0), uni(x.nrows)}; }
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));

@@ -117,4 +117,81 @@ hipError_t launch_attention(bool bf16, const void *qkv, const int *cu, void *out
 // never more than kAttnPartBytes.
 size_t attention_part_bytes(bool bf16, int hd);
 
+// Rotary positions: rows [rows][ldx] of `heads` heads of hd values each; rows at or behind *rows_end (device,
+// may be null) are left alone.  The first 2 n columns of a head turn: pair j is columns (j, j + n), or (2 j, 2 j + 1)
+// if adjacent, its axis the largest a with first[a] <= j, its angle pos[row][axis] * freq[j] turns.
+constexpr int kRopeMaxPairs = 128;
+constexpr int kRopeTable = 1024;  // (row, pair) cosines and sines a workgroup holds
+struct RopeProblem {
+  const void *x;
+  long long ldx;
+  void *out;
+  long long ldo;
+  const float *pos;
+  const int *rows_end;
+  int rows, heads, hd, axes, n;
+  int first[4];  // first pair of each axis (n behind the last axis)
+  int adjacent, backward;
+  int units_head, block_rows, block_heads;  // set by the launcher
+  double freq[kRopeMaxPairs];
+};
+hipError_t launch_rope(bool bf16, RopeProblem p, hipStream_t st);
+hipError_t launch_token_positions(const int *fine_idx, const int *pool_idx, const int *counts, const int *cu,
+                                  const int *seg, const float *text_pos, float *pos, int B, int I, int H, int W, int L,
+                                  hipStream_t st);
+
+// Norms before and after a block (norm.hip).  Device pointers; gate, shift, scale: row (2 s + stream) at mod_stride
+// values each; gains per stream.  Any of gate, shift, scale and the gains may be null.
+struct NormProblem {
+  const int *cu;
+  int B, L, D, rows;
+  int rms;
+  float eps, alpha;
+  const float *gate, *shift, *scale;
+  long long mod_stride;
+  const float *post[2], *pre[2];
+  const void *y;        // [rows][D] dtype, or null: no norm after the block
+  const float *x;       // [rows][D]
+  float *x_out;         // [rows][D], null with y
+  void *h;              // [rows][D] dtype, int8 codes with h_scale, or null: no norm before the next block
+  float *h_scale;       // [rows]
+  float *stats;         // [rows][4]: mean and 1 / deviation of y, of x_out; may be null
+};
+hipError_t launch_norm_residual(bool bf16, const NormProblem &p, hipStream_t st);
+
+// Its backward pass.
+struct NormBackProblem {
+  const int *cu;
+  int B, L, D, rows;
+  int rms;
+  float alpha;
+  const float *gate, *scale;
+  long long mod_stride;
+  const float *post[2], *pre[2];
+  const float *dx_out;   // [rows][D] or null
+  const void *dh;        // [rows][D] dtype or null
+  const void *y;         // [rows][D] dtype or null
+  const float *x_out;    // [rows][D]
+  const float *stats;    // [rows][4]
+  float *dx;             // [rows][D]
+  void *dy;              // [rows][D] dtype (with y)
+  float *dgate, *dshift, *dscale;  // rows (2 s + stream), dmod_stride values each; may be null
+  long long dmod_stride;
+  float *dpost[2], *dpre[2];       // per stream; the two the same: their sum
+  float *part;           // norm_back_bytes
+  int P;                 // workers, set by the launcher
+};
+size_t norm_back_bytes(int rows, int B, int D);
+hipError_t launch_norm_residual_back(bool bf16, NormBackProblem p, hipStream_t st);
+
+// int8 products (linear.hip, gemm.hip).  Rows of x as int8 codes with a float32 scale each; limit: a device pointer to
+// the number of rows, or null.
+hipError_t launch_quantize_rows_i8(bool bf16, const void *x, int rows, int cols, int8_t *codes, float *scale,
+                                   const int *limit, hipStream_t st);
+// A [rows][K] codes with a_scale, W[s] [N][K] codes with w_scale[s], bias[s] dtype or null; out [rows][N] dtype.
+// max_img_rows: the buffers' rows.  K % 16 == 0, N % 4 == 0.
+hipError_t launch_linear_i8(bool bf16, bool gelu, const GemmProblem &p, hipStream_t st);
+// Bytes of partial tiles that launch_linear_i8 needs for buffers of `rows` rows.
+size_t linear_i8_part_bytes(long long rows);
+
 }  // namespace hilo

@@ -19,6 +19,9 @@ LIB_PATH = os.path.join(_PKG, "libhilo.so")
 F32, BF16 = 0, 1
 THRESHOLD, TOPK = 0, 1
 PARTITION, OVERLAP, DROP = 0, 1, 2  # hilo_token_set
+ROPE_ADJACENT, ROPE_ONE_SPECTRUM = 1, 2  # hilo_rope_flags
+NORM_LAYER, NORM_RMS = 0, 1  # hilo_norm_kind
+ACT_NONE, ACT_GELU = 0, 1  # hilo_act
 DTYPES = {"f32": F32, "bf16": BF16}
 TORCH_DTYPES = {F32: torch.float32, BF16: torch.bfloat16}
 
@@ -49,6 +52,26 @@ class hilo_attn_w_fp8(ctypes.Structure):
 
 class hilo_mlp_w_fp8(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("w1", "s1", "b1", "w2", "s2", "b2")]
+
+
+class hilo_rotary(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("heads", "head_dim", "axes", "flags")] + [
+        ("pairs", ctypes.c_int32 * 4), ("base", ctypes.c_double * 4)]
+
+
+class hilo_norms(ctypes.Structure):
+    _fields_ = [("kind", ctypes.c_int32), ("eps", ctypes.c_float), ("residual_scale", ctypes.c_float),
+                ("mod_stride", ctypes.c_int64), ("gate", ctypes.c_void_p), ("shift", ctypes.c_void_p),
+                ("scale", ctypes.c_void_p), ("post_gain", ctypes.c_void_p * 2), ("pre_gain", ctypes.c_void_p * 2)]
+
+
+class hilo_norm_grads(ctypes.Structure):
+    _fields_ = [("mod_stride", ctypes.c_int64), ("gate", ctypes.c_void_p), ("shift", ctypes.c_void_p),
+                ("scale", ctypes.c_void_p), ("post_gain", ctypes.c_void_p * 2), ("pre_gain", ctypes.c_void_p * 2)]
+
+
+class hilo_linear_w_i8(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("w", "s", "b")]
 
 
 _lib = None
@@ -88,6 +111,19 @@ _SIG = {
     "hilo_attention_core": [ctypes.POINTER(hilo_shape), _P, _P, _P, _P, ctypes.c_size_t, _P],
     "hilo_attention_core_noalloc": [ctypes.POINTER(hilo_shape), _P, _P, _P, _P],
     "hilo_attention_core_fp8": [ctypes.POINTER(hilo_shape), _P, _P, _P, _P, ctypes.c_size_t, _P],
+    "hilo_rope": [ctypes.c_int32, ctypes.POINTER(hilo_rotary), _P, ctypes.c_int64, _P, ctypes.c_int64, _P,
+                  ctypes.c_int32, _P, ctypes.c_int64, _P],
+    "hilo_token_positions": [ctypes.POINTER(hilo_shape), _P, _P, _P, _P, _P, _P, _P, _P],
+    "hilo_norm_residual": [ctypes.c_int32, ctypes.POINTER(hilo_norms), _P, _P, _P, _P, _P, _P, ctypes.c_int64,
+                           ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, _P, _P],
+    "hilo_norm_residual_backward": [ctypes.c_int32, ctypes.POINTER(hilo_norms), _P, _P, _P, _P, _P, _P, _P,
+                                    ctypes.POINTER(hilo_norm_grads), ctypes.c_int64, ctypes.c_int32, ctypes.c_int32,
+                                    ctypes.c_int32, _P, _P, ctypes.c_size_t, _P],
+    "hilo_norm_residual_workspace_bytes": [ctypes.c_int64, ctypes.c_int32, ctypes.c_int32],
+    "hilo_quantize_rows_i8": [ctypes.c_int32, _P, ctypes.c_int64, ctypes.c_int64, _P, _P, _P, _P],
+    "hilo_linear_i8": [ctypes.c_int32, ctypes.POINTER(hilo_linear_w_i8), _P, _P, _P, ctypes.c_int64, ctypes.c_int32,
+                       ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, _P, _P, ctypes.c_size_t, _P],
+    "hilo_linear_i8_workspace_bytes": [ctypes.c_int64, ctypes.c_int32],
     "hilo_workspace_bytes": [ctypes.POINTER(hilo_shape)],
     "hilo_workspace_bytes_fp8": [ctypes.POINTER(hilo_shape)],
     "hilo_max_tokens": [ctypes.POINTER(hilo_shape)],
@@ -100,6 +136,7 @@ _SIG = {
     "hilo_profile_name": [ctypes.c_int32],
 }
 _RES = {"hilo_workspace_bytes": ctypes.c_size_t, "hilo_workspace_bytes_fp8": ctypes.c_size_t, "hilo_max_tokens": ctypes.c_int64,
+        "hilo_norm_residual_workspace_bytes": ctypes.c_size_t, "hilo_linear_i8_workspace_bytes": ctypes.c_size_t,
         "hilo_status_str": ctypes.c_char_p, "hilo_profile_name": ctypes.c_char_p}
 
 
@@ -367,6 +404,278 @@ def hilo_attention_core_fp8(shape, qkv8, cu_seqlens, out, workspace, stream=None
 def hilo_attention_core_noalloc(shape, qkv, cu_seqlens, out, stream=None):
     _check("hilo_attention_core_noalloc", lib().hilo_attention_core_noalloc(
         ctypes.byref(shape), _ptr(qkv), _ptr(cu_seqlens), _ptr(out), _stream(stream)))
+
+
+# ---------------------------------------------------- rotary positions, sandwich norms, int8 products
+#
+# These calls check what the library cannot see: types, shapes, layouts and devices of the tensors.  They run on the
+# current stream of the tensors' device, or on `stream`, which has to be one of that device.
+
+_FLOATS = {torch.float32: F32, torch.bfloat16: BF16}
+
+
+def _float_code(t: torch.Tensor) -> int:
+    code = _FLOATS.get(t.dtype)
+    if code is None:
+        raise ValueError(f"float32 or bfloat16 expected, not {t.dtype}")
+    return code
+
+
+def _arg(t: Optional[torch.Tensor], dtype: torch.dtype, shape, dev: int, what: str) -> Optional[int]:
+    """The pointer of a contiguous tensor of this type and shape on device `dev`, or None."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.shape != shape:
+        raise ValueError(f"{what}: expected {dtype} {tuple(shape)}, not {t.dtype} {tuple(t.shape)}")
+    if t.get_device() != dev:
+        raise ValueError(f"{what}: on {t.device}, other tensors on device {dev}")
+    if not t.is_contiguous():
+        raise ValueError(f"{what}: libhilo takes contiguous tensors only")
+    return t.data_ptr()
+
+
+def _on_device(t: torch.Tensor) -> int:
+    dev = t.get_device()
+    if dev < 0:
+        raise ValueError("libhilo takes device tensors only")
+    return dev
+
+
+def _launch(fn, dev: int, stream, *args):
+    """fn(*args, stream) with `dev` as the current device."""
+    if dev != torch.cuda.current_device():
+        with torch.cuda.device(dev):
+            return _launch(fn, dev, stream, *args)
+    st = getattr(lib(), fn)(*args, torch.cuda.current_stream(dev).cuda_stream if stream is None else _stream(stream))
+    if st != 0:
+        raise HiloError(fn, st)
+
+
+def _packed(cu: torch.Tensor, dev: int):
+    if cu.dtype is not torch.int32 or cu.dim() != 1 or cu.numel() < 2 or not cu.is_contiguous():
+        raise ValueError("cu_seqlens: expected int32 [batch + 1]")
+    if cu.get_device() != dev:
+        raise ValueError(f"cu_seqlens: on {cu.device}, other tensors on device {dev}")
+    return cu.numel() - 1, cu.data_ptr()
+
+
+def rotary(heads: int, head_dim: int, pairs: Sequence[int], base=10000.0, flags: int = 0) -> hilo_rotary:
+    """What hilo_rope turns: pairs of every axis, base one number or one per axis, flags ROPE_*."""
+    axes = len(pairs)
+    if not 1 <= axes <= 4:
+        raise ValueError("1 to 4 axes")
+    bases = [float(base)] * axes if isinstance(base, (int, float)) else [float(b) for b in base]
+    if len(bases) != axes:
+        raise ValueError("one base, or one per axis")
+    return hilo_rotary(heads, head_dim, axes, flags, (ctypes.c_int32 * 4)(*pairs), (ctypes.c_double * 4)(*bases))
+
+
+def hilo_rope(r: hilo_rotary, x: torch.Tensor, pos: torch.Tensor, out: torch.Tensor, cu: Optional[torch.Tensor] = None,
+              backward: bool = False, stream=None):
+    """out = the heads of x turned by their rows' positions (backward: by minus them).  x, out: [rows][heads *
+    head_dim], any row stride (a view of the packed projection will do), out may be x; pos [rows][axes] float32; cu:
+    the boundaries, whose last one bounds the rows."""
+    dev, dtype = _on_device(x), _float_code(x)
+    if x.dim() != 2 or x.shape[1] != r.heads * r.head_dim or out.shape != x.shape or out.dtype is not x.dtype:
+        raise ValueError(f"x and out: expected [rows][{r.heads * r.head_dim}] of one type")
+    rows = x.shape[0]
+    if rows and (x.stride(1) != 1 or out.stride(1) != 1):
+        raise ValueError("x and out: the last index is contiguous")
+    if out.get_device() != dev:
+        raise ValueError("x and out: on one device")
+    ldx, ldo = (x.stride(0), out.stride(0)) if rows > 1 else (x.shape[1], x.shape[1])
+    end = None
+    if cu is not None:
+        b, end = _packed(cu, dev)
+        end += 4 * b
+    _launch("hilo_rope", dev, stream, dtype, ctypes.byref(r), x.data_ptr(), ldx,
+            _arg(pos, torch.float32, (rows, r.axes), dev, "pos"), rows, end, 1 if backward else 0, out.data_ptr(), ldo)
+
+
+def hilo_token_positions(shape, fine_idx, pool_idx, counts, cu_seqlens, seg_off, text_pos, pos, stream=None):
+    _check("hilo_token_positions", lib().hilo_token_positions(
+        ctypes.byref(shape), _ptr(fine_idx), _ptr(pool_idx), _ptr(counts), _ptr(cu_seqlens), _ptr(seg_off),
+        _ptr(text_pos), _ptr(pos), _stream(stream)))
+
+
+def _vectors(h, vectors: dict, gains: dict):
+    """Fills the pointers of a hilo_norms or hilo_norm_grads; keeps the tensors and what they are on it."""
+    h.batch = h.dim = h.dev = None
+    h.kept = [vectors, gains]
+    for name, v in vectors.items():
+        if v is None:
+            continue
+        if v.dtype is not torch.float32 or v.dim() != 3 or v.shape[1] != 2 or (v.numel() and v.stride(2) != 1):
+            raise ValueError(f"{name}: expected float32 [batch][2][dim]")
+        stride = v.stride(1)
+        if v.shape[0] > 1 and v.stride(0) != 2 * stride:
+            raise ValueError(f"{name}: its (sample, stream) vectors have to be evenly spaced")
+        if h.batch is not None and (tuple(v.shape), v.stride(1)) != ((h.batch, 2, h.dim), h.mod_stride):
+            raise ValueError("gate, shift and scale: one shape and one spacing")
+        h.batch, h.dim, h.mod_stride = v.shape[0], v.shape[2], stride
+        _same_device(h, v, name)
+        setattr(h, name, v.data_ptr())
+    for name, pair in gains.items():
+        if pair is None:
+            continue
+        for k in range(2):
+            g = pair[k]
+            if g is None:
+                continue
+            if g.dtype is not torch.float32 or g.dim() != 1 or not g.is_contiguous() or h.dim not in (None, g.numel()):
+                raise ValueError(f"{name}: expected float32 [dim] for the image and the text stream")
+            h.dim = g.numel()
+            _same_device(h, g, name)
+            getattr(h, name)[k] = g.data_ptr()
+    return h
+
+
+def _same_device(h, t, name):
+    if h.dev is None:
+        h.dev = _on_device(t)
+    if t.get_device() != h.dev:
+        raise ValueError(f"{name}: on {t.device}, other tensors on device {h.dev}")
+
+
+def norms(kind: int = NORM_LAYER, eps: float = 1e-6, residual_scale: float = 1.0, *, gate=None, shift=None, scale=None,
+          post_gain=None, pre_gain=None) -> hilo_norms:
+    """The norms on both sides of a block: gate, shift, scale float32 [batch][2][dim] (views of one modulation tensor
+    will do: mod[:, :, 2] of [batch][2][6][dim]), gains a pair of float32 [dim] (image, text stream).  Keeps the
+    tensors alive; their values are read by each call."""
+    return _vectors(hilo_norms(kind, eps, residual_scale), {"gate": gate, "shift": shift, "scale": scale},
+                    {"post_gain": post_gain, "pre_gain": pre_gain})
+
+
+def norm_grads(*, gate=None, shift=None, scale=None, post_gain=None, pre_gain=None) -> hilo_norm_grads:
+    """Where hilo_norm_residual_backward leaves the gradients of the vectors: shapes as in norms()."""
+    return _vectors(hilo_norm_grads(), {"gate": gate, "shift": shift, "scale": scale},
+                    {"post_gain": post_gain, "pre_gain": pre_gain})
+
+
+def _norm_rows(n, like: torch.Tensor, cu: torch.Tensor, others=()):
+    if like.dim() != 2:
+        raise ValueError("expected [rows][dim] tensors")
+    dev, dim = _on_device(like), like.shape[1]
+    batch, cu_ptr = _packed(cu, dev)
+    for h in (n, *others):
+        if h is not None and (h.dim not in (None, dim) or h.batch not in (None, batch) or h.dev not in (None, dev)):
+            raise ValueError(f"vectors for dim {h.dim}, batch {h.batch} on device {h.dev}; rows have dim {dim}, batch "
+                             f"{batch} on device {dev}")
+    return dev, dim, batch, cu_ptr
+
+
+def hilo_norm_residual(n: hilo_norms, y, x, x_out, h, cu, text_len: int = 0, *, h_scale=None, stats=None, stream=None):
+    """x_out = residual_scale x + gate norm(y), h = norm(x_out) (1 + scale) + shift; y and x_out, or h, may be None.
+    h int8 with h_scale [rows]: codes and row scales.  stats [rows][4] float32: for the backward pass."""
+    dev, dim, batch, cu_ptr = _norm_rows(n, x, cu)
+    shape, rows, f32 = x.shape, x.shape[0], torch.float32
+    like = y if y is not None else h
+    if like is None:
+        raise HiloError("hilo_norm_residual", 1)
+    if h_scale is not None:
+        hp = _arg(h, torch.int8, shape, dev, "h")
+        dtype = F32 if y is None else _float_code(y)
+    else:
+        dtype = _float_code(like)
+        hp = _arg(h, like.dtype, shape, dev, "h")
+    _launch("hilo_norm_residual", dev, stream, dtype, ctypes.byref(n),
+            None if y is None else _arg(y, y.dtype, shape, dev, "y"), _arg(x, f32, shape, dev, "x"),
+            _arg(x_out, f32, shape, dev, "x_out"), hp, _arg(h_scale, f32, (rows,), dev, "h_scale"),
+            _arg(stats, f32, (rows, 4), dev, "stats"), rows, dim, batch, text_len, cu_ptr)
+
+
+def hilo_norm_residual_workspace_bytes(rows: int, batch: int, dim: int) -> int:
+    return lib().hilo_norm_residual_workspace_bytes(rows, batch, dim)
+
+
+def hilo_norm_residual_backward(n: hilo_norms, dx_out, dh, y, x_out, stats, dx, dy, grads: Optional[hilo_norm_grads],
+                                cu, text_len: int = 0, workspace=None, stream=None):
+    """Gradients of hilo_norm_residual from dx_out (or None) and dh (or None): dx, dy, and those in grads."""
+    dev, dim, batch, cu_ptr = _norm_rows(n, dx, cu, (grads,))
+    shape, rows, f32 = dx.shape, dx.shape[0], torch.float32
+    like = dh if dh is not None else y
+    if like is None:
+        raise HiloError("hilo_norm_residual_backward", 1)
+    dt, nbytes = like.dtype, 0
+    if workspace is not None:
+        if workspace.get_device() != dev or not workspace.is_contiguous():
+            raise ValueError("workspace: contiguous, on the tensors' device")
+        nbytes = workspace.numel() * workspace.element_size()
+    _launch("hilo_norm_residual_backward", dev, stream, _float_code(like), ctypes.byref(n),
+            _arg(dx_out, f32, shape, dev, "dx_out"), _arg(dh, dt, shape, dev, "dh"), _arg(y, dt, shape, dev, "y"),
+            _arg(x_out, f32, shape, dev, "x_out"), _arg(stats, f32, (rows, 4), dev, "stats"),
+            _arg(dx, f32, shape, dev, "dx"), _arg(dy, dt, shape, dev, "dy"), None if grads is None else ctypes.byref(grads),
+            rows, dim, batch, text_len, cu_ptr, None if workspace is None else workspace.data_ptr(), nbytes)
+
+
+def hilo_quantize_rows_i8(x, codes, scale, cu=None, stream=None):
+    """Per-row int8 codes [rows][cols] and float32 scales [rows] of x; cu: the boundaries, whose last one bounds the rows."""
+    dev, dtype = _on_device(x), _float_code(x)
+    if x.dim() != 2:
+        raise ValueError("x: expected [rows][cols]")
+    end = None
+    if cu is not None:
+        b, end = _packed(cu, dev)
+        end += 4 * b
+    rows, cols = x.shape
+    _launch("hilo_quantize_rows_i8", dev, stream, dtype, _arg(x, x.dtype, x.shape, dev, "x"), rows, cols, end,
+            _arg(codes, torch.int8, x.shape, dev, "codes"), _arg(scale, torch.float32, (rows,), dev, "scale"))
+
+
+def quantize_i8_weights(w, b=None, stream=None) -> dict:
+    """A projection's weights for linear_weights_i8: codes and scales of w [out][in], the bias kept."""
+    codes = torch.empty(w.shape, dtype=torch.int8, device=w.device)
+    scale = torch.empty(w.shape[0], dtype=torch.float32, device=w.device)
+    hilo_quantize_rows_i8(w, codes, scale, stream=stream)
+    return {"w": codes, "s": scale, "b": b}
+
+
+def linear_weights_i8(ws: Sequence[dict]):
+    """Weights of hilo_linear_i8: {"w": int8 [out][in], "s": float32 [out], "b": [out] or None} of the image and the text
+    stream (one dict: of both).  Keeps the tensors alive."""
+    ws = list(ws)
+    if not 1 <= len(ws) <= 2:
+        raise ValueError("weights of one or two streams")
+    arr = (hilo_linear_w_i8 * 2)()
+    arr.kept, arr.shape, arr.bias, arr.dev = ws, ws[0]["w"].shape, None, _on_device(ws[0]["w"])
+    if len(arr.shape) != 2:
+        raise ValueError("w: expected [out][in]")
+    for k in range(2):
+        w = ws[min(k, len(ws) - 1)]
+        b = w.get("b")
+        if b is not None:
+            _float_code(b)
+            if arr.bias not in (None, b.dtype):
+                raise ValueError("b: of one type")
+            arr.bias = b.dtype
+        arr[k] = hilo_linear_w_i8(_arg(w["w"], torch.int8, arr.shape, arr.dev, "w"),
+                                  _arg(w["s"], torch.float32, arr.shape[:1], arr.dev, "s"),
+                                  None if b is None else _arg(b, b.dtype, arr.shape[:1], arr.dev, "b"))
+    return arr
+
+
+def hilo_linear_i8_workspace_bytes(rows: int, in_dim: int) -> int:
+    return lib().hilo_linear_i8_workspace_bytes(rows, in_dim)
+
+
+def hilo_linear_i8(w, x, out, cu, text_len: int = 0, *, x_scale=None, act: int = ACT_NONE, workspace=None, stream=None):
+    """out [rows][out] = act(x w^T) of linear_weights_i8 w: x int8 codes with x_scale, or of out's type, quantised here."""
+    dev, dtype = _on_device(out), _float_code(out)
+    if dev != w.dev:
+        raise ValueError(f"weights on device {w.dev}, out on device {dev}")
+    if w.bias is not None and w.bias is not out.dtype:
+        raise ValueError(f"b: {w.bias}, out: {out.dtype}")
+    if workspace is None:
+        raise HiloError("hilo_linear_i8", 1)
+    if workspace.get_device() != dev or not workspace.is_contiguous():
+        raise ValueError("workspace: contiguous, on the tensors' device")
+    rows = out.shape[0]
+    n, k = w.shape
+    batch, cu_ptr = _packed(cu, dev)
+    _launch("hilo_linear_i8", dev, stream, dtype, w,
+            _arg(x, out.dtype if x_scale is None else torch.int8, (rows, k), dev, "x"),
+            _arg(x_scale, torch.float32, (rows,), dev, "x_scale"), _arg(out, out.dtype, (rows, n), dev, "out"), rows, k, n,
+            act, batch, text_len, cu_ptr, workspace.data_ptr(), workspace.numel() * workspace.element_size())
 
 
 def hilo_profile_enable(on: bool):
