@@ -20,6 +20,13 @@
 
 namespace hilo {
 
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+
+// Operands of the 8-wave tiles; the int8 products' epilogues write bf16 or float32.
+enum Operand { OP_BF16, OP_FP8, OP_I8, OP_I8_F32 };
+constexpr bool op_i8(int op) { return op == OP_I8 || op == OP_I8_F32; }
+constexpr bool op_scaled(int op) { return op != OP_BF16; }  // codes with a scale per row of either operand
+
 template <int EPI, bool BF16OUT>
 HILO_DEV void epilogue4(const GemmProblem &p, const TileRows &tr, int m, int n, const float *acc) {
   // m: output row, n: first of 4 consecutive columns (n + 3 < N guaranteed by N % 4 == 0)
@@ -112,14 +119,14 @@ HILO_DEV bool runs_whole(int T, int nk) {
   return (T < P && nk <= kNoSplitSteps) || whole_waves || full_wave;
 }
 
-// The plan of R row tiles of the problem on BN-column tiles.
-HILO_DEV SkPlan sk_plan(const GemmProblem &p, int R, int BN, int kstep = 64) {
+// The plan of R row tiles of the problem on BN-column tiles, K in steps of kstep (nk of them, where K is no multiple).
+HILO_DEV SkPlan sk_plan(const GemmProblem &p, int R, int BN, int kstep = 64, int nk = 0) {
   constexpr int P = kGemmWorkgroups;
   SkPlan q;
   q.R = R;
   q.TN = (p.N + BN - 1) / BN;
   q.T = q.R * q.TN;
-  q.nk = p.K / kstep;
+  q.nk = nk ? nk : p.K / kstep;
   if (runs_whole(q.T, q.nk)) {
     q.s = 1;
     q.U = q.dp = q.T;
@@ -281,9 +288,10 @@ struct SkTile {
 
   // Epilogue of fragment row i0 of wave wid (each fragment: 4 consecutive columns of one row).  Loads use
   // indices clamped into the tile; values for rows or columns outside it are never stored.
-  template <int EPI, bool F8>
+  template <int EPI, int OP, typename V>
   HILO_DEV static void epilogue_row(const GemmProblem &p, const TileRows &tr, int n0, int wid, int i0, int lane,
-                                    const f32x4 (&acc)[TN]) {
+                                    const V (&acc)[TN]) {
+    constexpr bool F8 = op_scaled(OP);
     const int rl = (wid / WN) * (BM / WM) + i0 * 16 + (lane & 15);
     const int cbase = n0 + (wid % WN) * (BN / WN) + CL * (lane >> 4);
     const size_t m = size_t(tr.row0 + min(rl, tr.nrows - 1));
@@ -294,9 +302,16 @@ struct SkTile {
 #pragma unroll
     for (int j = 0; j < TN; ++j) {
       const int nc = min(cbase + j * CS, p.N - 4);
-      const uint2 bu = *reinterpret_cast<const uint2 *>(bias + nc);
-      bv[j][0] = __uint_as_float(bu.x << 16); bv[j][1] = __uint_as_float(bu.x & 0xffff0000u);
-      bv[j][2] = __uint_as_float(bu.y << 16); bv[j][3] = __uint_as_float(bu.y & 0xffff0000u);
+      if (op_i8(OP) && !bias) {
+        bv[j][0] = bv[j][1] = bv[j][2] = bv[j][3] = 0.f;
+      } else if constexpr (OP == OP_I8_F32) {
+        const float4 bf = *reinterpret_cast<const float4 *>(reinterpret_cast<const float *>(bias) + nc);
+        bv[j][0] = bf.x; bv[j][1] = bf.y; bv[j][2] = bf.z; bv[j][3] = bf.w;
+      } else {
+        const uint2 bu = *reinterpret_cast<const uint2 *>(bias + nc);
+        bv[j][0] = __uint_as_float(bu.x << 16); bv[j][1] = __uint_as_float(bu.x & 0xffff0000u);
+        bv[j][2] = __uint_as_float(bu.y << 16); bv[j][3] = __uint_as_float(bu.y & 0xffff0000u);
+      }
       if constexpr (EPI == EPI_RESID) {
         gt[j] = *reinterpret_cast<const float4 *>(p.mod + (size_t(tr.s * 2 + tr.sigma) * 6 + p.gate_idx) * p.D + nc);
         zv[j] = *reinterpret_cast<const float4 *>(p.z + m * p.ldz + nc);
@@ -311,10 +326,10 @@ struct SkTile {
       if (n >= p.N) continue;
       float v[4];
       if constexpr (F8) {
-        v[0] = acc[j][0] * (asc * wsc[j].x) + bv[j][0];
-        v[1] = acc[j][1] * (asc * wsc[j].y) + bv[j][1];
-        v[2] = acc[j][2] * (asc * wsc[j].z) + bv[j][2];
-        v[3] = acc[j][3] * (asc * wsc[j].w) + bv[j][3];
+        v[0] = float(acc[j][0]) * (asc * wsc[j].x) + bv[j][0];
+        v[1] = float(acc[j][1]) * (asc * wsc[j].y) + bv[j][1];
+        v[2] = float(acc[j][2]) * (asc * wsc[j].z) + bv[j][2];
+        v[3] = float(acc[j][3]) * (asc * wsc[j].w) + bv[j][3];
       } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = acc[j][e] + bv[j][e];
@@ -331,10 +346,14 @@ struct SkTile {
 #pragma unroll
           for (int e = 0; e < 4; ++e) v[e] = gelu_tanh(v[e]);
         }
-        uint2 u;
-        u.x = pack_bf16x2(v[0], v[1]);
-        u.y = pack_bf16x2(v[2], v[3]);
-        *reinterpret_cast<uint2 *>(reinterpret_cast<uint16_t *>(p.out) + m * p.ldo + n) = u;
+        if constexpr (OP == OP_I8_F32) {
+          *reinterpret_cast<float4 *>(reinterpret_cast<float *>(p.out) + m * p.ldo + n) = make_float4(v[0], v[1], v[2], v[3]);
+        } else {
+          uint2 u;
+          u.x = pack_bf16x2(v[0], v[1]);
+          u.y = pack_bf16x2(v[2], v[3]);
+          *reinterpret_cast<uint2 *>(reinterpret_cast<uint16_t *>(p.out) + m * p.ldo + n) = u;
+        }
       }
     }
   }
@@ -379,9 +398,10 @@ HILO_DEV void g2lds4(const void *g, void *lds_wave_base) {
 namespace g8 {
 // A BM x BN tile of bf16 or FP8 operands on 8 waves: WM x WN waves, MB x NB blocks of 16 x 16 each (B32: of
 // 32 x 32).
-template <int BM, int BN, bool F8 = false>
+template <int BM, int BN, int OP = OP_BF16>
 struct Geo {
-  static constexpr bool B32 = F8 && BN == 256;
+  static constexpr bool F8 = op_scaled(OP);
+  static constexpr bool B32 = OP == OP_FP8 && BN == 256;
   static constexpr int WN = B32 ? 2 : 4, WM = 8 / WN;
   static constexpr int MB = BM / WM / (B32 ? 32 : 16), NB = BN / WN / (B32 ? 32 : 16);
   static constexpr int LA = BM / 64, LB = BN / 64;  // load instructions per wave and window
@@ -517,10 +537,11 @@ HILO_DEV void epilogue32_qk8(const GemmProblem &p, const TileRows &tr, int n0, i
 }
 
 // All work items of this workgroup under plan q on BM x BN tiles.
-template <int BM, int BN, int EPI, bool F8 = false>
+template <int BM, int BN, int EPI, int OP = OP_BF16>
 HILO_DEV void gemm8_run(const GemmProblem &p, const SkPlan &q, int pid, uint8_t *lds) {
   using namespace g8;
-  using G = Geo<BM, BN, F8>;
+  using G = Geo<BM, BN, OP>;
+  constexpr bool F8 = G::F8, I8 = op_i8(OP);
   constexpr bool B32 = G::B32;
   using T = SkTile<BM, BN, G::WM, G::WN, !B32>;
   constexpr int MB = G::MB, NB = G::NB, LA = G::LA, LB = G::LB, WB = G::WB, S = G::SLOTS;
@@ -564,16 +585,33 @@ HILO_DEV void gemm8_run(const GemmProblem &p, const SkPlan &q, int pid, uint8_t 
     lk = x.kb;
     lke = x.ke;
   };
+  // int8: a last window of fewer than 128 values (K is a multiple of 16) reads the row's first chunk in the place of
+  // those behind K; its fragments of A are cleared before they are multiplied
+  const int kpart = I8 && p.K % 128 != 0 ? p.K / 128 : -1, cpart = p.K % 128 / 16;
+  auto inside = [&](uint32_t o, int r) __attribute__((always_inline)) {
+    const int c = (lane & 7) ^ swz<B32>(r);
+    return c < cpart ? o : o - uint32_t(c) * 16;
+  };
   auto ld_a = [&]() __attribute__((always_inline)) {
     uint8_t *d = lds + lslot * WB + wid * (BM / 8) * 128;
+    if (I8 && lk == kpart) {
 #pragma unroll
-    for (int i = 0; i < LA; ++i) g2lds16(la + oa[i], d + i * 1024);
+      for (int i = 0; i < LA; ++i) g2lds16(la + inside(oa[i], wid * (BM / 8) + 8 * i + (lane >> 3)), d + i * 1024);
+    } else {
+#pragma unroll
+      for (int i = 0; i < LA; ++i) g2lds16(la + oa[i], d + i * 1024);
+    }
     la += 128;
   };
   auto ld_b = [&]() __attribute__((always_inline)) {
     uint8_t *d = lds + lslot * WB + (BM + wid * (BN / 8)) * 128;
+    if (I8 && lk == kpart) {
 #pragma unroll
-    for (int i = 0; i < LB; ++i) g2lds16(lb + ob[i], d + i * 1024);
+      for (int i = 0; i < LB; ++i) g2lds16(lb + inside(ob[i], wid * (BN / 8) + 8 * i + (lane >> 3)), d + i * 1024);
+    } else {
+#pragma unroll
+      for (int i = 0; i < LB; ++i) g2lds16(lb + ob[i], d + i * 1024);
+    }
     lb += 128;
     ++lk;
     lslot = lslot == S - 1 ? 0 : lslot + 1;
@@ -584,12 +622,13 @@ HILO_DEV void gemm8_run(const GemmProblem &p, const SkPlan &q, int pid, uint8_t 
   // blocks: chunks 4 h + g and 4 h + 2 + g (g = lane / 32) of row lane % 32 for one 64-deep MFMA of half h.
   // W rows of 16 x 16 blocks go in the order that gives the lane's accumulators 4 NB consecutive columns:
   // MFMA output row 4 g + e of block j is column 4 NB g + 4 j + e of the wave
-  constexpr int NC = F8 ? 2 : 1;                       // chunks of a fragment
+  constexpr bool INP = OP == OP_FP8 && !B32;
+  constexpr int NC = OP == OP_FP8 ? 2 : 1;             // chunks of a fragment
   constexpr int NR = (MB + NB) * NC;                   // reads of a set: W first, then A
   constexpr int NA = B32 ? 4 : 2;                      // chunk addresses of a lane
   constexpr int RB = B32 ? 4096 : 2048;                // bytes between blocks
-  using Acc = std::conditional_t<B32, f32x16, f32x4>;
-  using Frag = std::conditional_t<F8, u32x4, bf16x8>;
+  using Acc = std::conditional_t<B32, f32x16, std::conditional_t<I8, i32x4, f32x4>>;
+  using Frag = std::conditional_t<I8, i32x4, std::conditional_t<F8, u32x4, bf16x8>>;
   const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
   uint32_t fa[NA], fb[B32 ? 1 : NB][NA];
 #pragma unroll
@@ -611,13 +650,12 @@ HILO_DEV void gemm8_run(const GemmProblem &p, const SkPlan &q, int pid, uint8_t 
   // Two sets: the halves of a window, or (FP8, 16 x 16) two windows.  The latter has no registers for two
   // whole sets: rows 0 .. MB - 3 of A keep one fragment each, re-read once the row's MFMAs are issued
   Frag a[2][MB][NC], b[2][NB][NC];
-  constexpr bool INP = F8 && !B32;
   auto set_a = [](int h, int i) constexpr { return INP && i < MB - 2 ? 0 : h; };
   uint32_t so = 0;  // byte offset of the window being read
   // read x of set h
   auto rd = [&](auto hh, auto xx) __attribute__((always_inline)) {
     constexpr int h = decltype(hh)::value, x = decltype(xx)::value / NC, c = decltype(xx)::value % NC;
-    constexpr int ad = B32 ? 2 * h + c : F8 ? c : h;
+    constexpr int ad = B32 ? 2 * h + c : INP ? c : h;
     if constexpr (x < NB) {
       if constexpr (B32) ds_read16<(x < NB ? x : 0) * RB>(b[h][x][c], fb[0][ad] + so);
       else ds_read16<0>(b[h][x][c], fb[x][ad] + so);
@@ -637,6 +675,15 @@ HILO_DEV void gemm8_run(const GemmProblem &p, const SkPlan &q, int pid, uint8_t 
       for (int j = 0; j < NB; ++j) asm volatile("" : "+v"(b[h][j][c]));
     }
     __builtin_amdgcn_sched_barrier(0);
+  };
+  // int8: the fragments of A whose values lie behind K
+  auto clear = [&](auto hh) __attribute__((always_inline)) {
+    constexpr int h = decltype(hh)::value;
+    if constexpr (I8) {
+#pragma unroll
+      for (int i = 0; i < MB; ++i)
+        if (4 * h + lg >= cpart) a[h][i][0] = Frag(0);
+    }
   };
   auto rd_all = [&](auto hh) __attribute__((always_inline)) {
     auto r6 = [&](auto x) __attribute__((always_inline)) {
@@ -667,7 +714,9 @@ HILO_DEV void gemm8_run(const GemmProblem &p, const SkPlan &q, int pid, uint8_t 
         } else {
 #pragma unroll
           for (int j = 0; j < NB; ++j) {
-            if constexpr (F8)
+            if constexpr (I8)
+              acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(b[h][j][0], a[h][i][0], acc[i][j], 0, 0, 0);
+            else if constexpr (F8)
               acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
                   cat8(b[h][j][0], b[h][j][1]), cat8(a[set_a(h, i)][i][0], a[set_a(h, i)][i][1]), acc[i][j], 0, 0, 0, 0, 0,
                   0);
@@ -743,7 +792,11 @@ HILO_DEV void gemm8_run(const GemmProblem &p, const SkPlan &q, int pid, uint8_t 
       en0 = uni(tn) * BN + wn * (BN / WN);
       etr = uni(decode_row_tile(p, BM, uni(rt)));
       const uint16_t *bias = reinterpret_cast<const uint16_t *>(etr.sigma ? p.bias[1] : p.bias[0]);
-      g2lds4(bias + min(en0 + 2 * lane, p.N - 2), epi);
+      if constexpr (OP == OP_I8_F32) {
+        if (bias) g2lds4(reinterpret_cast<const float *>(bias) + min(en0 + lane, p.N - 1), epi);
+      } else {
+        if (!I8 || bias) g2lds4(bias + min(en0 + 2 * lane, p.N - 2), epi);
+      }
       if constexpr (EPI == EPI_RESID)
         g2lds4(p.mod + (size_t(etr.s * 2 + etr.sigma) * 6 + p.gate_idx) * p.D + min(en0 + lane, p.N - 1), epi + G::kGate);
       if constexpr (F8) {
@@ -758,7 +811,7 @@ HILO_DEV void gemm8_run(const GemmProblem &p, const SkPlan &q, int pid, uint8_t 
 #pragma unroll
     for (int i = 0; i < MB; ++i)
 #pragma unroll
-      for (int j = 0; j < NB; ++j) acc[i][j] = Acc(0.f);
+      for (int j = 0; j < NB; ++j) acc[i][j] = Acc(0);
     // the first window's first fragments (again, after an epilogue: it needs their registers)
     rd_all(Int<0>{});
     if constexpr (INP) {
@@ -780,8 +833,10 @@ HILO_DEV void gemm8_run(const GemmProblem &p, const SkPlan &q, int pid, uint8_t 
     } else {
 #pragma unroll 1
       for (int kt = cur.kb; kt < cur.ke; ++kt) {
+        if (I8 && kt == kpart) clear(Int<0>{});
         half(Int<0>{}, std::false_type{});
         rd_wait(Int<1>{});
+        if (I8 && kt == kpart) clear(Int<1>{});
         next_window();
         half(Int<1>{}, std::true_type{});
         rd_wait(Int<0>{});
@@ -812,11 +867,18 @@ HILO_DEV void gemm8_run(const GemmProblem &p, const SkPlan &q, int pid, uint8_t 
       }
     } else if (whole) {
       uint2 bu[NB];
+      f32x4 bf[OP == OP_I8_F32 ? NB : 1];
+      const bool biased = !I8 || (etr.sigma ? p.bias[1] : p.bias[0]) != nullptr;
       f32x4 wsc[F8 ? NB : 1];
       f32x4 gv[NB];
 #pragma unroll
       for (int j = 0; j < NB; ++j) {
-        bu[j] = *reinterpret_cast<const uint2 *>(epi + 2 * (4 * NB * lg + 4 * j));
+        if constexpr (OP == OP_I8_F32) bf[j] = *reinterpret_cast<const f32x4 *>(epi + 4 * (4 * NB * lg + 4 * j));
+        else bu[j] = *reinterpret_cast<const uint2 *>(epi + 2 * (4 * NB * lg + 4 * j));
+        if (I8 && !biased) {
+          if constexpr (OP == OP_I8_F32) bf[j] = f32x4(0.f);
+          else bu[j] = make_uint2(0u, 0u);
+        }
         if constexpr (EPI == EPI_RESID) gv[j] = *reinterpret_cast<const f32x4 *>(epi + G::kGate + 4 * (4 * NB * lg + 4 * j));
         if constexpr (F8) wsc[j] = *reinterpret_cast<const f32x4 *>(epi + G::kCol + 4 * (4 * NB * lg + 4 * j));
       }
@@ -862,16 +924,23 @@ HILO_DEV void gemm8_run(const GemmProblem &p, const SkPlan &q, int pid, uint8_t 
           if (rl < etr.nrows) {
             const size_t m = size_t(etr.row0 + rl);
             uint2 o[NB];
+            float4 of[OP == OP_I8_F32 ? NB : 1];
             float sa;
             if constexpr (F8) sa = *reinterpret_cast<const float *>(epi + G::kRow + 4 * (16 * i + lr));
 #pragma unroll
             for (int j = 0; j < NB; ++j) {
               float v[4];
-              const float bv[4] = {__uint_as_float(bu[j].x << 16), __uint_as_float(bu[j].x & 0xffff0000u),
-                                   __uint_as_float(bu[j].y << 16), __uint_as_float(bu[j].y & 0xffff0000u)};
+              float bv[4];
+              if constexpr (OP == OP_I8_F32) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) bv[e] = bf[j][e];
+              } else {
+                bv[0] = __uint_as_float(bu[j].x << 16); bv[1] = __uint_as_float(bu[j].x & 0xffff0000u);
+                bv[2] = __uint_as_float(bu[j].y << 16); bv[3] = __uint_as_float(bu[j].y & 0xffff0000u);
+              }
 #pragma unroll
               for (int e = 0; e < 4; ++e) {
-                if constexpr (F8) v[e] = acc[i][j][e] * (sa * wsc[j][e]) + bv[e];
+                if constexpr (F8) v[e] = float(acc[i][j][e]) * (sa * wsc[j][e]) + bv[e];
                 else v[e] = acc[i][j][e] + bv[e];
               }
               if constexpr (EPI == EPI_RESID) {
@@ -884,14 +953,22 @@ HILO_DEV void gemm8_run(const GemmProblem &p, const SkPlan &q, int pid, uint8_t 
 #pragma unroll
                   for (int e = 0; e < 4; ++e) v[e] = gelu_tanh(v[e]);
                 }
-                o[j] = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+                if constexpr (OP == OP_I8_F32) of[j] = make_float4(v[0], v[1], v[2], v[3]);
+                else o[j] = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
               }
             }
             if constexpr (EPI != EPI_RESID) {
-              uint16_t *op = reinterpret_cast<uint16_t *>(p.out) + m * p.ldo + nc;
+              if constexpr (OP == OP_I8_F32) {
+                float *op = reinterpret_cast<float *>(p.out) + m * p.ldo + nc;
 #pragma unroll
-              for (int j = 0; j < NB; ++j)
-                if (nc + 4 * j < p.N) *reinterpret_cast<uint2 *>(op + 4 * j) = o[j];
+                for (int j = 0; j < NB; ++j)
+                  if (nc + 4 * j < p.N) *reinterpret_cast<float4 *>(op + 4 * j) = of[j];
+              } else {
+                uint16_t *op = reinterpret_cast<uint16_t *>(p.out) + m * p.ldo + nc;
+#pragma unroll
+                for (int j = 0; j < NB; ++j)
+                  if (nc + 4 * j < p.N) *reinterpret_cast<uint2 *>(op + 4 * j) = o[j];
+              }
             }
           }
         }
@@ -905,7 +982,7 @@ HILO_DEV void gemm8_run(const GemmProblem &p, const SkPlan &q, int pid, uint8_t 
 #pragma unroll
       for (int i = 0; i < MB; ++i)
 #pragma unroll
-        for (int j = 0; j < NB; ++j) *reinterpret_cast<f32x4 *>(slot + T::part_index(wid, i, j, lane)) = acc[i][j];
+        for (int j = 0; j < NB; ++j) *reinterpret_cast<Acc *>(slot + T::part_index(wid, i, j, lane)) = acc[i][j];
     }
     cur = uni(sk_next_item(cc, q, rg, pid, p.part, T::kPartFloats));
     if (!cur.valid) break;
@@ -1061,9 +1138,9 @@ HILO_DEV Tile choose_tile(const GemmProblem &p, int &rows) {
 
 template <int BM, int BN, int EPI, int ROLE>
 __global__ __launch_bounds__(512, 2) void k_gemm8_fp8(GemmProblem p) {
-  __shared__ __attribute__((aligned(1024))) uint8_t lds[g8::Geo<BM, BN, true>::LDS];
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[g8::Geo<BM, BN, OP_FP8>::LDS];
   const int pid = xcd_remap(blockIdx.x, kGemmWorkgroups);
-  gemm8_run<BM, BN, EPI, true>(p, sk_plan(p, row_tiles_total(p, BM), BN, 128), pid, lds);
+  gemm8_run<BM, BN, EPI, OP_FP8>(p, sk_plan(p, row_tiles_total(p, BM), BN, 128), pid, lds);
 }
 
 template <int EPI, int ROLE>
@@ -1090,7 +1167,7 @@ __global__ __launch_bounds__(512, 2) void k_gemm8(GemmProblem p) {
 constexpr int kFixThreads = 512;
 constexpr int kFixBatch = 4;
 
-template <int BM, int BN, int WM, int WN, bool CONTIG, int EPI, bool F8>
+template <int BM, int BN, int WM, int WN, bool CONTIG, int EPI, int OP>
 HILO_DEV void gemm_fix(const GemmProblem &p, const SkPlan &q) {
   constexpr int P = kGemmWorkgroups;
   if (q.s == 1 && q.I == 0) return;  // every tile was finished by the main kernel
@@ -1102,18 +1179,19 @@ HILO_DEV void gemm_fix(const GemmProblem &p, const SkPlan &q) {
   for (int x = blockIdx.x * FW + (threadIdx.x >> 6); x < items; x += gridDim.x * FW) {
     const int f = x / (NW * TM), rem = x - f * (NW * TM), wid = rem / TM, i = rem - wid * TM;
     const int t = q.s > 1 ? f : q.dp + f;
-    f32x4 acc[TN];
+    using V = std::conditional_t<op_i8(OP), i32x4, f32x4>;
+    V acc[TN];
 #pragma unroll
-    for (int j = 0; j < TN; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int j = 0; j < TN; ++j) acc[j] = V(0);
     const float *b[kFixBatch];
     int nb = 0;
     auto flush = [&]() {
-      f32x4 v[kFixBatch][TN];
+      V v[kFixBatch][TN];
 #pragma unroll
       for (int c = 0; c < kFixBatch; ++c)
         if (c < nb) {
 #pragma unroll
-          for (int j = 0; j < TN; ++j) v[c][j] = *reinterpret_cast<const f32x4 *>(b[c] + T::part_index(wid, i, j, lane));
+          for (int j = 0; j < TN; ++j) v[c][j] = *reinterpret_cast<const V *>(b[c] + T::part_index(wid, i, j, lane));
         }
 #pragma unroll
       for (int c = 0; c < kFixBatch; ++c)
@@ -1165,28 +1243,68 @@ HILO_DEV void gemm_fix(const GemmProblem &p, const SkPlan &q) {
     int rt, tn;
     tile_coords(q, t, rt, tn);
     const TileRows tr = decode_row_tile(p, BM, rt);
-    if constexpr (F8 && EPI == EPI_BIAS && BN == 256) {
+    if constexpr (OP == OP_FP8 && EPI == EPI_BIAS && BN == 256) {
       if (p.qk8 != nullptr && tn * BN < 2 * p.D) {
         T::epilogue_row_qk8(p, tr, tn * BN, wid, i, lane, acc);
         continue;
       }
     }
-    T::template epilogue_row<EPI, F8>(p, tr, tn * BN, wid, i, lane, acc);
+    T::template epilogue_row<EPI, OP>(p, tr, tn * BN, wid, i, lane, acc);
   }
 }
 
 template <int BM, int BN, int EPI, int ROLE>
 __global__ __launch_bounds__(kFixThreads) void k_gemm8_fp8_fix(GemmProblem p) {
-  using G = g8::Geo<BM, BN, true>;
-  gemm_fix<BM, BN, G::WM, G::WN, !G::B32, EPI, true>(p, sk_plan(p, row_tiles_total(p, BM), BN, 128));
+  using G = g8::Geo<BM, BN, OP_FP8>;
+  gemm_fix<BM, BN, G::WM, G::WN, !G::B32, EPI, OP_FP8>(p, sk_plan(p, row_tiles_total(p, BM), BN, 128));
 }
 
 template <int EPI, int ROLE>
 __global__ __launch_bounds__(kFixThreads) void k_gemm8_fix(GemmProblem p) {
   int rows;
   const Tile t = choose_tile<EPI>(p, rows);
-  if (t == TILE_256) gemm_fix<256, 256, 2, 4, true, EPI, false>(p, sk_plan(p, rows, 256));
-  else if (t == TILE_192) gemm_fix<192, 192, 2, 4, true, EPI, false>(p, sk_plan(p, rows, 192));
+  if (t == TILE_256) gemm_fix<256, 256, 2, 4, true, EPI, OP_BF16>(p, sk_plan(p, rows, 256));
+  else if (t == TILE_192) gemm_fix<192, 192, 2, 4, true, EPI, OP_BF16>(p, sk_plan(p, rows, 192));
+}
+
+// ------------------------------------------------------------------------------- int8 products
+//
+// The loop of the bf16 tiles on int8 codes: a window holds 128 values, v_mfma_i32_16x16x64_i8 takes the 16 bytes a lane
+// and the cycles of v_mfma_f32_16x16x32_bf16, so loads, reads and MFMA time per window are those of bf16 and the tile
+// choice's estimates hold with half as many windows.
+
+// The tile, and its row tiles.
+template <int EPI>
+HILO_DEV Tile choose_tile_i8(const GemmProblem &p, int &rows) {
+  constexpr uint32_t P = kGemmWorkgroups;
+  int r192 = 0, r256 = 0;
+  for (int s = 0; s < p.B; ++s) {
+    const int img = cu_at(p.cu, s + 1) - p.L - cu_at(p.cu, s);
+    r192 += (img + 191) / 192 + (p.L + 191) / 192;
+    r256 += (img + 255) / 256 + (p.L + 255) / 256;
+  }
+  const uint32_t nk = (p.K + 127) / 128;
+  const uint32_t c192 = plan_cost<EPI>(r192 * ((p.N + 191) / 192), nk, TileCost{91, 400, 1400, 2000, 2700, 20, 2500});
+  const uint32_t c256 = plan_cost<EPI>(r256 * ((p.N + 255) / 256), nk, TileCost{146, 700, 3300, 3600, 4500, 35, 4500});
+  rows = c256 < c192 ? r256 : r192;
+  return c256 < c192 ? TILE_256 : TILE_192;
+}
+
+template <int EPI, int OP>
+__global__ __launch_bounds__(512, 2) void k_linear_i8(GemmProblem p) {
+  constexpr int L0 = g8::Geo<192, 192, OP>::LDS, L1 = g8::Geo<256, 256, OP>::LDS;
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[L0 > L1 ? L0 : L1];
+  const int pid = xcd_remap(blockIdx.x, kGemmWorkgroups);
+  int rows;
+  if (choose_tile_i8<EPI>(p, rows) == TILE_256) gemm8_run<256, 256, EPI, OP>(p, sk_plan(p, rows, 256, 128, (p.K + 127) / 128), pid, lds);
+  else gemm8_run<192, 192, EPI, OP>(p, sk_plan(p, rows, 192, 128, (p.K + 127) / 128), pid, lds);
+}
+
+template <int EPI, int OP>
+__global__ __launch_bounds__(kFixThreads) void k_linear_i8_fix(GemmProblem p) {
+  int rows;
+  if (choose_tile_i8<EPI>(p, rows) == TILE_256) gemm_fix<256, 256, 2, 4, true, EPI, OP>(p, sk_plan(p, rows, 256, 128, (p.K + 127) / 128));
+  else gemm_fix<192, 192, 2, 4, true, EPI, OP>(p, sk_plan(p, rows, 192, 128, (p.K + 127) / 128));
 }
 
 // ------------------------------------------------------------------------------- fp32 path
@@ -1338,6 +1456,24 @@ hipError_t launch_gemm_fp8(int role, const GemmProblem &p, hipStream_t st) {
     case GEMM_FC1: return run_fp8<192, 192, GEMM_FC1>(p, st);
     default: return run_fp8<192, 192, GEMM_FC2>(p, st);
   }
+}
+
+template <int EPI, int OP>
+static hipError_t run_i8(const GemmProblem &p, hipStream_t st) {
+  constexpr int P = kGemmWorkgroups;
+  hipLaunchKernelGGL((k_linear_i8<EPI, OP>), dim3(P), dim3(512), 0, st, p);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  // max_img_rows: all rows of the buffers, of which every segment may leave a part of a tile
+  const long long tiles_max = (p.max_img_rows / 192 + 2 * (long long)p.B) * ((p.N + 191) / 192);
+  if (tiles_max < P && (p.K + 127) / 128 <= kNoSplitSteps) return hipSuccess;
+  hipLaunchKernelGGL((k_linear_i8_fix<EPI, OP>), dim3(P), dim3(kFixThreads), 0, st, p);
+  return hipGetLastError();
+}
+
+hipError_t launch_linear_i8_tiled(bool bf16, bool gelu, const GemmProblem &p, hipStream_t st) {
+  if (bf16) return gelu ? run_i8<EPI_GELU, OP_I8>(p, st) : run_i8<EPI_BIAS, OP_I8>(p, st);
+  return gelu ? run_i8<EPI_GELU, OP_I8_F32>(p, st) : run_i8<EPI_BIAS, OP_I8_F32>(p, st);
 }
 
 }  // namespace hilo

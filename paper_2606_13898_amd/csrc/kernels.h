@@ -191,6 +191,8 @@ hipError_t launch_quantize_rows_i8(bool bf16, const void *x, int rows, int cols,
 // A [rows][K] codes with a_scale, W[s] [N][K] codes with w_scale[s], bias[s] dtype or null; out [rows][N] dtype.
 // max_img_rows: the buffers' rows.  K % 16 == 0, N % 4 == 0.
 hipError_t launch_linear_i8(bool bf16, bool gelu, const GemmProblem &p, hipStream_t st);
+// The same on the projections' tiles, with partial tiles in p.part (kSkPartBytes).
+hipError_t launch_linear_i8_tiled(bool bf16, bool gelu, const GemmProblem &p, hipStream_t st);
 // Bytes of partial tiles that launch_linear_i8 needs for buffers of `rows` rows.
 size_t linear_i8_part_bytes(long long rows);
 

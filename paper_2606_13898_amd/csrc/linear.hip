@@ -191,7 +191,9 @@ __global__ __launch_bounds__(64 * NW) void k_linear_i8_direct(GemmProblem p) {
   }
 }
 
-size_t linear_i8_part_bytes(long long rows) { return 0; }
+// Buffers of at most this many rows take the direct tiles.
+constexpr long long kDirectRows = 64;
+size_t linear_i8_part_bytes(long long rows) { return rows <= kDirectRows ? 0 : kSkPartBytes; }
 
 template <bool BF16, bool GELU>
 static hipError_t run_linear_i8(const GemmProblem &p, hipStream_t st) {
@@ -203,6 +205,7 @@ static hipError_t run_linear_i8(const GemmProblem &p, hipStream_t st) {
 }
 
 hipError_t launch_linear_i8(bool bf16, bool gelu, const GemmProblem &p, hipStream_t st) {
+  if (p.max_img_rows > kDirectRows) return launch_linear_i8_tiled(bf16, gelu, p, st);
   if (bf16) return gelu ? run_linear_i8<true, true>(p, st) : run_linear_i8<true, false>(p, st);
   return gelu ? run_linear_i8<false, true>(p, st) : run_linear_i8<false, false>(p, st);
 }

@@ -7,6 +7,7 @@ import numpy as np
 import pytest
 import torch
 
+import linear_schedule
 from oracle import hilo_operators as Q
 from paper_2606_13898_amd import hilo
 
@@ -258,3 +259,11 @@ def test_oracle_int8():
         for n in range(3):
             acc = sum(int(a[m, i]) * int(w[k]["w"][n, i]) for i in range(7))
             assert abs(out[m, n] - (acc * s[m] * w[k]["s"][n] + w[k]["b"][n])) < 1e-9
+
+
+# ---------------------------------------------------------------------------------------- schedule
+
+@pytest.mark.parametrize("shape,plan", linear_schedule.SHAPES, ids=str)
+def test_linear_plans(shape, plan):
+    """The shapes of the GPU tests reach the plans that they are there for."""
+    assert linear_schedule.describe(*shape) == plan

@@ -6,6 +6,7 @@ import numpy as np
 import pytest
 import torch
 
+import linear_schedule
 from oracle import hilo_operators as Q
 from paper_2606_13898_amd import hilo
 
@@ -490,19 +491,31 @@ def run_linear(dtype, lens, text, K, N, gelu, bias, seed, rows=None):
     assert torch.equal(out, out2)
 
 
+# every kind of plan of the large tiles (linear_schedule.py says which each shape reaches), both types of output
+@pytest.mark.parametrize("shape", [s for s, _ in linear_schedule.SHAPES], ids=str)
+@pytest.mark.parametrize("dtype,gelu,bias", [("bf16", True, True), ("f32", False, True), ("bf16", False, False)])
+def test_linear_i8_plans(shape, dtype, gelu, bias):
+    lens, text, K, N = shape
+    print(f"[linear i8 plan] {dtype} lens={lens} text={text} K={K} N={N}", flush=True)
+    T = sum(lens)
+    rows = None if T * N * K < 3e9 else np.sort(np.random.default_rng(1).choice(T, 100, replace=False))
+    run_linear(dtype, lens, text, K, N, gelu, bias, 7, rows)
+
+
 def test_linear_i8_largest_sum():
     """Every product the largest: sums at the edge of what K allows stay exact."""
     K = 65536
-    x = torch.full((2, K), 127, dtype=torch.int8, device="cuda")
-    w = torch.full((4, K), 127, dtype=torch.int8, device="cuda")
-    w[1] = -127
-    plan = hilo.linear_weights_i8([{"w": w, "s": torch.ones(4, device="cuda")}])
-    out = torch.empty(2, 4, device="cuda")
-    ws = torch.empty(hilo.hilo_linear_i8_workspace_bytes(2, K), dtype=torch.uint8, device="cuda")
-    hilo.hilo_linear_i8(plan, x, out, _dev(np.array([0, 2]), torch.int32), x_scale=torch.ones(2, device="cuda"), workspace=ws)
-    torch.cuda.synchronize()
-    top = float(np.float32(127 * 127 * K))
-    assert _np(out).tolist() == [[top, -top, top, top]] * 2
+    for rows in (2, 300):
+        x = torch.full((rows, K), 127, dtype=torch.int8, device="cuda")
+        w = torch.full((4, K), 127, dtype=torch.int8, device="cuda")
+        w[1] = -127
+        plan = hilo.linear_weights_i8([{"w": w, "s": torch.ones(4, device="cuda")}])
+        out = torch.empty(rows, 4, device="cuda")
+        ws = torch.empty(hilo.hilo_linear_i8_workspace_bytes(rows, K), dtype=torch.uint8, device="cuda")
+        hilo.hilo_linear_i8(plan, x, out, _dev(np.array([0, rows]), torch.int32), x_scale=torch.ones(rows, device="cuda"), workspace=ws)
+        torch.cuda.synchronize()
+        top = float(np.float32(127 * 127 * K))
+        assert _np(out).tolist() == [[top, -top, top, top]] * rows
 
 
 def test_linear_i8_not_finite_row():
