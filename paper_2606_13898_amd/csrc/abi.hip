@@ -973,14 +973,6 @@ hilo_status hilo_linear_i8(int32_t dtype, const hilo_linear_w_i8 w[2], const voi
   GemmProblem p{};
   p.A = x;
   p.a_scale = x_scale;
-  if (!x_scale) {
-    const hipError_t he = timed(K_QUANT_I8, st, [&] {
-      return launch_quantize_rows_i8(dtype == HILO_BF16, x, int(rows), in_dim, codes, scales, cu_seqlens + batch, st);
-    });
-    if (he != hipSuccess) return HILO_E_DEVICE;
-    p.A = codes;
-    p.a_scale = scales;
-  }
   p.lda = in_dim;
   p.N = out_dim; p.K = in_dim;
   p.out = out; p.ldo = out_dim;
@@ -992,6 +984,14 @@ hilo_status hilo_linear_i8(int32_t dtype, const hilo_linear_w_i8 w[2], const voi
     p.W[k] = v.w;
     p.w_scale[k] = v.s;
     p.bias[k] = v.b;
+  }
+  if (!x_scale && !linear_i8_fuses(dtype == HILO_BF16, p)) {
+    const hipError_t he = timed(K_QUANT_I8, st, [&] {
+      return launch_quantize_rows_i8(dtype == HILO_BF16, x, int(rows), in_dim, codes, scales, cu_seqlens + batch, st);
+    });
+    if (he != hipSuccess) return HILO_E_DEVICE;
+    p.A = codes;
+    p.a_scale = scales;
   }
   p.part = reinterpret_cast<float *>(ws + align256(size_t(rows) * in_dim) + align256(size_t(rows) * sizeof(float)));
   return dev_status(timed(K_LINEAR_I8, st, [&] { return launch_linear_i8(dtype == HILO_BF16, act == HILO_ACT_GELU, p, st); }));

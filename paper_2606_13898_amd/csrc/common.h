@@ -95,10 +95,27 @@ HILO_DEV int pow2_exponent(float amax) {
 // 2^-k for k in [-127, 127] as a float (always a normal number for the k above)
 HILO_DEV float pow2_inverse(int k) { return __uint_as_float(uint32_t(127 - k) << 23); }
 
+// Reductions over a wave in the vector unit: within rows of 16 lanes by DPP (neighbours, pairs, half rows, rows), then
+// the four rows' values from lanes 0, 16, 32, 48.  A step takes a few cycles where one through LDS takes some sixty.
+template <int CTRL>
+HILO_DEV int dpp(int v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, 0xf, 0xf, true); }
+constexpr int kDppXor1 = 0xb1, kDppXor2 = 0x4e, kDppHalfMirror = 0x141, kDppMirror = 0x140;
+HILO_DEV float lane_f32(float v, int l) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), l)); }
+HILO_DEV float wave_total(float v) {
+  v += __int_as_float(dpp<kDppXor1>(__float_as_int(v)));
+  v += __int_as_float(dpp<kDppXor2>(__float_as_int(v)));
+  v += __int_as_float(dpp<kDppHalfMirror>(__float_as_int(v)));
+  v += __int_as_float(dpp<kDppMirror>(__float_as_int(v)));
+  return (lane_f32(v, 0) + lane_f32(v, 16)) + (lane_f32(v, 32) + lane_f32(v, 48));
+}
 HILO_DEV uint32_t wave_max_u32(uint32_t v) {
-#pragma unroll
-  for (int off = 32; off > 0; off >>= 1) v = max(v, uint32_t(__shfl_xor(int(v), off, 64)));
-  return v;
+  v = max(v, uint32_t(dpp<kDppXor1>(int(v))));
+  v = max(v, uint32_t(dpp<kDppXor2>(int(v))));
+  v = max(v, uint32_t(dpp<kDppHalfMirror>(int(v))));
+  v = max(v, uint32_t(dpp<kDppMirror>(int(v))));
+  const uint32_t a = __builtin_amdgcn_readlane(int(v), 0), b = __builtin_amdgcn_readlane(int(v), 16);
+  const uint32_t c = __builtin_amdgcn_readlane(int(v), 32), d = __builtin_amdgcn_readlane(int(v), 48);
+  return max(max(a, b), max(c, d));
 }
 
 // int8 codes of a row with a float32 scale.  The row's largest magnitude is taken on the bits of |x|: they order as the
@@ -109,9 +126,15 @@ HILO_DEV float i8_inverse(uint32_t top) {
   return top < 0x03800000u || top >= 0x7f800000u ? 0.f : __fdiv_rn(127.0f, __uint_as_float(top));
 }
 HILO_DEV float i8_scale(uint32_t top) { return top < 0x03800000u ? 0.f : __fdiv_rn(__uint_as_float(top), 127.0f); }
-HILO_DEV uint32_t i8_code(float v) { return uint32_t(int(rintf(fminf(fmaxf(v, -127.f), 127.f)))) & 0xffu; }
-HILO_DEV uint32_t i8x4(float a, float b, float c, float d) {
-  return i8_code(a) | (i8_code(b) << 8) | (i8_code(c) << 16) | (i8_code(d) << 24);
+// Codes of four values times the inverse, products at most 127 in magnitude (127 (1 + 2^-23) rounds to 127): adding
+// 1.5 * 2^23 rounds to a whole number, to nearest even, and leaves its low byte in the lowest bits; a NaN's is 0.
+HILO_DEV uint32_t i8x4(float a, float b, float c, float d, float inv) {
+#pragma clang fp contract(off)  // a product is rounded before it is made whole: that is what the codes are
+  constexpr float m = 12582912.0f;
+  const float ma = a * inv, mb = b * inv, mc = c * inv, md = d * inv;
+  const uint32_t lo = __builtin_amdgcn_perm(__float_as_uint(mb + m), __float_as_uint(ma + m), 0x0c0c0400u);
+  const uint32_t hi = __builtin_amdgcn_perm(__float_as_uint(md + m), __float_as_uint(mc + m), 0x04000c0cu);
+  return lo | hi;
 }
 
 // Sample boundary i of the packed sequence.  The boundaries do not change while a kernel runs, so

@@ -189,7 +189,9 @@ hipError_t launch_norm_residual_back(bool bf16, NormBackProblem p, hipStream_t s
 hipError_t launch_quantize_rows_i8(bool bf16, const void *x, int rows, int cols, int8_t *codes, float *scale,
                                    const int *limit, hipStream_t st);
 // A [rows][K] codes with a_scale, W[s] [N][K] codes with w_scale[s], bias[s] dtype or null; out [rows][N] dtype.
-// max_img_rows: the buffers' rows.  K % 16 == 0, N % 4 == 0.
+// max_img_rows: the buffers' rows.  K % 16 == 0, N % 4 == 0.  a_scale null: A is float rows of the dtype, for problems
+// that linear_i8_fuses() says are quantised by the kernel that multiplies them.
+bool linear_i8_fuses(bool bf16, const GemmProblem &p);
 hipError_t launch_linear_i8(bool bf16, bool gelu, const GemmProblem &p, hipStream_t st);
 // The same on the projections' tiles, with partial tiles in p.part (kSkPartBytes).
 hipError_t launch_linear_i8_tiled(bool bf16, bool gelu, const GemmProblem &p, hipStream_t st);

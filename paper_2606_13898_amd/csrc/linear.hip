@@ -3,6 +3,8 @@
 //   acc = sum_k a[m][k] w[n][k] in int32, exact in any order (|acc| < 2^31 for K <= 65536);
 //   out = act(acc * (a_scale[m] * w_scale[n]) + bias[n])
 // Image rows take the image stream's weights, text rows the text stream's; tiles never straddle a segment.
+#include <algorithm>
+
 #include "common.h"
 #include "kernels.h"
 #include "tiles.h"
@@ -11,10 +13,47 @@ namespace hilo {
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 
+// 8 values of a float row as they lie in memory: loads stand apart from what is done with them, so that a lane's are all
+// in flight at once.
+template <bool BF16>
+struct Raw8 {
+  uint4 u[BF16 ? 1 : 2];
+  HILO_DEV void load(const void *x, size_t i) {
+    const uint4 *p = reinterpret_cast<const uint4 *>(reinterpret_cast<const char *>(x) + i * (BF16 ? 2 : 4));
+    u[0] = p[0];
+    if constexpr (!BF16) u[1] = p[1];
+  }
+  HILO_DEV void zero() {
+    u[0] = make_uint4(0u, 0u, 0u, 0u);
+    if constexpr (!BF16) u[1] = u[0];
+  }
+  HILO_DEV void values(float (&f)[8]) const {
+    if constexpr (BF16) {
+      unpack8(u[0], f);
+    } else {
+      f[0] = __uint_as_float(u[0].x); f[1] = __uint_as_float(u[0].y); f[2] = __uint_as_float(u[0].z); f[3] = __uint_as_float(u[0].w);
+      f[4] = __uint_as_float(u[1].x); f[5] = __uint_as_float(u[1].y); f[6] = __uint_as_float(u[1].z); f[7] = __uint_as_float(u[1].w);
+    }
+  }
+  HILO_DEV uint32_t top(uint32_t t) const {
+    float f[8];
+    values(f);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) t = max(t, abs_bits(f[e]));
+    return t;
+  }
+  HILO_DEV uint2 codes(float inv) const {
+    float f[8];
+    values(f);
+    return make_uint2(i8x4(f[0], f[1], f[2], f[3], inv), i8x4(f[4], f[5], f[6], f[7], inv));
+  }
+};
+
 // ------------------------------------------------------------------------------- quantisation
 
 // One row per group of W waves, NC chunks of 8 values a lane (cols <= 512 W NC), read once; LOOP: any number of
-// columns, read twice.
+// columns, NC chunks at a time, read twice.  A lane behind the last column reads the last chunk again, which changes
+// no maximum.
 template <bool BF16, int W, int NC, bool LOOP>
 __global__ __launch_bounds__(256) void k_quantize_rows_i8(const void *__restrict__ x, int rows, int cols,
                                                           int8_t *__restrict__ codes, float *__restrict__ scale,
@@ -23,39 +62,23 @@ __global__ __launch_bounds__(256) void k_quantize_rows_i8(const void *__restrict
   const int row = W == 1 ? blockIdx.x * 4 + wave : blockIdx.x;
   if (row >= (limit ? min(rows, cu_at(limit, 0)) : rows)) return;
   const int c0 = 8 * (W == 1 ? threadIdx.x & 63 : threadIdx.x);
-  auto load = [&](int c, float (&f)[8]) __attribute__((always_inline)) {
-    if constexpr (BF16) {
-      unpack8(*reinterpret_cast<const uint4 *>(reinterpret_cast<const uint16_t *>(x) + size_t(row) * cols + c), f);
-    } else {
-      const float4 *u = reinterpret_cast<const float4 *>(reinterpret_cast<const float *>(x) + size_t(row) * cols + c);
-      const float4 a = u[0], b = u[1];
-      f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w;
-      f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
-    }
-  };
-  auto store = [&](int c, const float (&f)[8], float inv) __attribute__((always_inline)) {
-    *reinterpret_cast<uint2 *>(codes + size_t(row) * cols + c) =
-        make_uint2(i8x4(f[0] * inv, f[1] * inv, f[2] * inv, f[3] * inv), i8x4(f[4] * inv, f[5] * inv, f[6] * inv, f[7] * inv));
-  };
-  float v[NC][8];
+  const size_t at = size_t(row) * cols;
+  Raw8<BF16> v[NC];
   uint32_t top = 0;
-  auto take = [&](const float (&f)[8]) __attribute__((always_inline)) {
+  auto load = [&](int c) __attribute__((always_inline)) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) top = max(top, abs_bits(f[e]));
+    for (int k = 0; k < NC; ++k) v[k].load(x, at + min(c + k * 512 * W, cols - 8));
   };
-  if constexpr (LOOP) {
-    for (int c = c0; c < cols; c += 512 * W) {
-      load(c, v[0]);
-      take(v[0]);
-    }
-  } else {
+  auto take = [&]() __attribute__((always_inline)) {
 #pragma unroll
-    for (int k = 0; k < NC; ++k) {
-      const int c = c0 + k * 512 * W;
-      if (c < cols) {
-        load(c, v[k]);
-        take(v[k]);
-      }
+    for (int k = 0; k < NC; ++k) top = v[k].top(top);
+  };
+  load(c0);
+  take();
+  if constexpr (LOOP) {
+    for (int c = c0 + NC * 512 * W; c < cols; c += NC * 512 * W) {
+      load(c);
+      take();
     }
   }
   top = wave_max_u32(top);
@@ -68,17 +91,11 @@ __global__ __launch_bounds__(256) void k_quantize_rows_i8(const void *__restrict
   }
   const float inv = i8_inverse(top);
   if (c0 == 0) scale[row] = i8_scale(top);
-  if constexpr (LOOP) {
-    for (int c = c0; c < cols; c += 512 * W) {
-      load(c, v[0]);
-      store(c, v[0], inv);
-    }
-  } else {
+  for (int c = c0; c < (LOOP ? cols : c0 + 1); c += NC * 512 * W) {
+    if constexpr (LOOP) load(c);
 #pragma unroll
-    for (int k = 0; k < NC; ++k) {
-      const int c = c0 + k * 512 * W;
-      if (c < cols) store(c, v[k], inv);
-    }
+    for (int k = 0; k < NC; ++k)
+      if (c + k * 512 * W < cols) *reinterpret_cast<uint2 *>(codes + at + c + k * 512 * W) = v[k].codes(inv);
   }
 }
 
@@ -97,21 +114,24 @@ hipError_t launch_quantize_rows_i8(bool bf16, const void *x, int rows, int cols,
   else if (cols <= 4096) HILO_Q8(4, 2, false);
   else if (cols <= 8192) HILO_Q8(4, 4, false);
   else if (cols <= 16384) HILO_Q8(4, 8, false);
-  else HILO_Q8(4, 1, true);
+  else HILO_Q8(4, 4, true);
 #undef HILO_Q8
   return hipGetLastError();
 }
 
 // ------------------------------------------------------------------------------------- products
 
-// Four consecutive columns n .. n + 3 of row m (N % 4 == 0: all inside).
-template <bool BF16, bool GELU>
-HILO_DEV void i8_out4(const GemmProblem &p, int sigma, size_t m, int n, const i32x4 &acc) {
-  const float4 ws = *reinterpret_cast<const float4 *>((sigma ? p.w_scale[1] : p.w_scale[0]) + n);
-  const float sa = p.a_scale[m];
-  const void *bias = sigma ? p.bias[1] : p.bias[0];
-  float b[4] = {0.f, 0.f, 0.f, 0.f};
-  if (bias) {
+// Scales and bias of four consecutive columns n .. n + 3 (N % 4 == 0: inside, or n is behind N and nothing is read),
+// taken early: they arrive while the sums are formed.
+template <bool BF16>
+struct I8Cols {
+  float4 s;
+  float b[4];
+  HILO_DEV I8Cols(const GemmProblem &p, int sigma, int n) : s(make_float4(0.f, 0.f, 0.f, 0.f)), b{0.f, 0.f, 0.f, 0.f} {
+    if (n >= p.N) return;
+    s = *reinterpret_cast<const float4 *>((sigma ? p.w_scale[1] : p.w_scale[0]) + n);
+    const void *bias = sigma ? p.bias[1] : p.bias[0];
+    if (!bias) return;
     if constexpr (BF16) {
       const uint2 u = *reinterpret_cast<const uint2 *>(reinterpret_cast<const uint16_t *>(bias) + n);
       b[0] = __uint_as_float(u.x << 16); b[1] = __uint_as_float(u.x & 0xffff0000u);
@@ -121,9 +141,14 @@ HILO_DEV void i8_out4(const GemmProblem &p, int sigma, size_t m, int n, const i3
       b[0] = u.x; b[1] = u.y; b[2] = u.z; b[3] = u.w;
     }
   }
+};
+
+// Those columns of row m from the sums.
+template <bool BF16, bool GELU>
+HILO_DEV void i8_out4(const GemmProblem &p, size_t m, int n, const i32x4 &acc, float sa, const I8Cols<BF16> &c) {
   // the exact sum is rounded to 24 bits once here; it and the product of the scales are what float32 costs
-  float v[4] = {float(acc[0]) * (sa * ws.x) + b[0], float(acc[1]) * (sa * ws.y) + b[1],
-                float(acc[2]) * (sa * ws.z) + b[2], float(acc[3]) * (sa * ws.w) + b[3]};
+  float v[4] = {float(acc[0]) * (sa * c.s.x) + c.b[0], float(acc[1]) * (sa * c.s.y) + c.b[1],
+                float(acc[2]) * (sa * c.s.z) + c.b[2], float(acc[3]) * (sa * c.s.w) + c.b[3]};
   if constexpr (GELU) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) v[e] = gelu_tanh(v[e]);
@@ -135,77 +160,275 @@ HILO_DEV void i8_out4(const GemmProblem &p, int sigma, size_t m, int n, const i3
     *reinterpret_cast<float4 *>(reinterpret_cast<float *>(p.out) + m * p.N + n) = make_float4(v[0], v[1], v[2], v[3]);
 }
 
-// Tiles of 16 MB rows x 16 NB columns, K split over the NW waves of a workgroup in steps of 64, their sums added
-// through LDS.  Fragments come straight from global memory, 16 bytes a lane: lane (lr, lg) holds bytes 16 lg .. of row
-// lr's step.
-template <bool BF16, bool GELU, int MB, int NB, int NW>
-__global__ __launch_bounds__(64 * NW) void k_linear_i8_direct(GemmProblem p) {
-  __shared__ i32x4 part[NW][MB * NB][64];
+// 16 bytes of a row at k, of which those behind K (a multiple of 16) do not matter.
+HILO_DEV i32x4 chunk_at(const int8_t *row, int k, int K) { return *reinterpret_cast<const i32x4 *>(row + min(k, K - 16)); }
+
+// This wave's LDS writes are done and every wave is here; loads from global memory stay in flight.
+HILO_DEV void lds_barrier() {
+  __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
+  asm volatile("s_barrier" ::: "memory");
+}
+
+// The rows of one stream's tile t of BM rows, gathered over the samples (a sample may have one row), of at most 64 rows
+// in all: rows[i] for i < the count, which is 0 where no such tile is.  Ends with every wave past a barrier.
+struct FewRows {
+  int sigma, n;
+};
+HILO_DEV FewRows few_rows(const GemmProblem &p, int BM, int t, int *rows) {
+  const int lane = threadIdx.x & 63, T = min(cu_at(p.cu, p.B), p.max_img_rows);  // max_img_rows: at most 64
+  const bool in = lane < T;
+  bool text = false;
+  if (p.L > 0 && in) text = lane >= p.cu[sample_of_row(p.cu, p.B, lane) + 1] - p.L;
+  const uint64_t m1 = __ballot(in && text), m0 = __ballot(in && !text);
+  const int n0 = int(__popcll(m0)), n1 = int(__popcll(m1));  // signed: a tile behind the last has fewer than no rows
+  const int tiles0 = (n0 + BM - 1) / BM;
+  const int sigma = t >= tiles0 ? 1 : 0, first = (sigma ? t - tiles0 : t) * BM;
+  const uint64_t mine = sigma ? m1 : m0;
+  const int at = int(__popcll(mine & ((1ull << lane) - 1))) - first, left = (sigma ? n1 : n0) - first;
+  if (threadIdx.x < 64 && ((mine >> lane) & 1) && at >= 0 && at < BM) rows[at] = lane;
+  __syncthreads();
+  return FewRows{uni(sigma), uni(left < 0 ? 0 : left < BM ? left : BM)};
+}
+
+// Few rows: tiles of 16 MB rows x 16 columns, K split over the four waves of a workgroup in steps of 128, their sums
+// added through LDS.  What bounds it is the weights' way from memory: every wave streams its columns' bytes, 32 a lane
+// and step (whole lines of 16 rows), up to 2 GS steps ahead of the matrix core, and tiles are narrow so that the CUs share them
+// evenly.  FUSED (MB = 1): x are float rows, which every workgroup quantises for itself into LDS -- each wave the part
+// of K that it multiplies, while its first weights are on their way; dynamic LDS holds the buffers' rows of codes.
+constexpr int kFewSteps = 3;
+template <bool BF16, bool GELU, int MB, bool FUSED>
+__global__ __launch_bounds__(256) void k_linear_i8_few(GemmProblem p) {
+  constexpr int NW = 4, GS = kFewSteps;
+  __shared__ i32x4 part[NW][MB][64];
+  __shared__ uint32_t tops[16][NW];
+  __shared__ int rows[16 * MB];
+  extern __shared__ __attribute__((aligned(16))) uint8_t codes[];
   const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lr = lane & 15, lg = lane >> 4;
-  const int tilesN = (p.N + 16 * NB - 1) / (16 * NB), tiles = row_tiles_total(p, 16 * MB) * tilesN;
-  const int steps = (p.K + 63) / 64, s0 = steps * wid / NW, s1 = steps * (wid + 1) / NW;
-  for (int t = blockIdx.x; t < tiles; t += gridDim.x) {
-    const int n0 = t % tilesN * (16 * NB);
-    const TileRows tr = uni(decode_row_tile(p, 16 * MB, t / tilesN));
-    const int8_t *A[MB], *W[NB];
+  const int n0 = blockIdx.x * 16;
+  const int steps = (p.K + 127) / 128, s0 = steps * wid / NW, s1 = steps * (wid + 1) / NW;
+  const int kl = 16 * lg;
+  const int8_t *W;
+  i32x4 w[2][GS][2];
+  auto load_w = [&](int s, i32x4 (&d)[GS][2]) __attribute__((always_inline)) {
+    if (s >= s1) return;
 #pragma unroll
-    for (int i = 0; i < MB; ++i)
-      A[i] = reinterpret_cast<const int8_t *>(p.A) + size_t(tr.row0 + min(16 * i + lr, tr.nrows - 1)) * p.K;
+    for (int g = 0; g < GS; ++g)
 #pragma unroll
-    for (int j = 0; j < NB; ++j)
-      W[j] = reinterpret_cast<const int8_t *>(tr.sigma ? p.W[1] : p.W[0]) + size_t(min(n0 + 16 * j + lr, p.N - 1)) * p.K;
-    i32x4 acc[MB][NB];
+      for (int h = 0; h < 2; ++h) d[g][h] = chunk_at(W, 128 * min(s + g, steps - 1) + kl + 64 * h, p.K);
+  };
+  auto first_w = [&](int sigma) __attribute__((always_inline)) {
+    W = reinterpret_cast<const int8_t *>(sigma ? p.W[1] : p.W[0]) + size_t(min(n0 + lr, p.N - 1)) * p.K;
+    load_w(s0, w[0]);
+    load_w(s0 + GS, w[1]);
+  };
+  if (p.L == 0) first_w(0);  // whose rows these are need not be known first
+  const FewRows tr = few_rows(p, 16 * MB, blockIdx.y, rows);
+  if (tr.n == 0) return;
+  if (p.L != 0) first_w(tr.sigma);
+  const I8Cols<BF16> cols(p, tr.sigma, n0 + 4 * lg);
+  const int ldc = 128 * steps + 16;  // 16 rows' chunks at one column fall on all banks
+  float sa = 0.f;
+  if constexpr (FUSED) {
+    const int k0 = 128 * s0, k1 = 128 * s1;
+    // four rows, or their last again, and one chunk of 512 values of each at a time
+    constexpr int MR = 4;
+    const int l8 = 8 * lane;
+    for (int m0 = 0; m0 < tr.n; m0 += MR) {
+      uint32_t top[MR];
+      size_t at[MR];
 #pragma unroll
-    for (int i = 0; i < MB; ++i)
+      for (int m = 0; m < MR; ++m) {
+        top[m] = 0;
+        at[m] = size_t(rows[min(m0 + m, tr.n - 1)]) * p.K;
+      }
+      for (int c = k0; c < min(k1, p.K); c += 512) {
+        Raw8<BF16> v[MR];
 #pragma unroll
-      for (int j = 0; j < NB; ++j) acc[i][j] = i32x4{0, 0, 0, 0};
-    for (int s = s0; s < s1; ++s) {
-      const int k = 64 * s + 16 * lg, kc = min(k, p.K - 16);  // K % 16 == 0: a chunk is inside or behind K
-      i32x4 a[MB], b[NB];
+        for (int m = 0; m < MR; ++m) v[m].load(p.A, at[m] + min(c + l8, p.K - 8));
 #pragma unroll
-      for (int i = 0; i < MB; ++i) {
-        a[i] = *reinterpret_cast<const i32x4 *>(A[i] + kc);
-        if (k != kc) a[i] = i32x4{0, 0, 0, 0};
+        for (int m = 0; m < MR; ++m) top[m] = v[m].top(top[m]);
       }
 #pragma unroll
-      for (int j = 0; j < NB; ++j) b[j] = *reinterpret_cast<const i32x4 *>(W[j] + kc);
-#pragma unroll
-      for (int i = 0; i < MB; ++i)
-#pragma unroll
-        for (int j = 0; j < NB; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(b[j], a[i], acc[i][j], 0, 0, 0);
+      for (int m = 0; m < MR; ++m) {
+        top[m] = wave_max_u32(top[m]);
+        if (lane == 0) tops[min(m0 + m, tr.n - 1)][wid] = top[m];
+      }
     }
+    lds_barrier();
+    for (int m0 = 0; m0 < tr.n; m0 += MR) {
+      float inv[MR];
+      size_t at[MR];
 #pragma unroll
-    for (int i = 0; i < MB; ++i)
+      for (int m = 0; m < MR; ++m) {
+        const int r = min(m0 + m, tr.n - 1);
+        const uint32_t top = max(max(tops[r][0], tops[r][1]), max(tops[r][2], tops[r][3]));
+        inv[m] = i8_inverse(top);
+        if (r == lr) sa = i8_scale(top);
+        at[m] = size_t(rows[r]) * p.K;
+      }
+      for (int c = k0; c < k1; c += 512) {
+        Raw8<BF16> v[MR];
 #pragma unroll
-      for (int j = 0; j < NB; ++j) part[wid][i * NB + j][lane] = acc[i][j];
-    __syncthreads();
-    for (int f = wid; f < MB * NB; f += NW) {
-      i32x4 v = part[0][f][lane];
+        for (int m = 0; m < MR; ++m) v[m].load(p.A, at[m] + min(c + l8, p.K - 8));
+        if (c + l8 >= k1) continue;
 #pragma unroll
-      for (int w = 1; w < NW; ++w) v += part[w][f][lane];
-      const int rl = 16 * (f / NB) + lr, n = n0 + 16 * (f % NB) + 4 * lg;
-      if (rl < tr.nrows && n < p.N) i8_out4<BF16, GELU>(p, tr.sigma, size_t(tr.row0 + rl), n, v);
+        for (int m = 0; m < MR; ++m) {
+          if (c + l8 >= p.K) v[m].zero();
+          if (m0 + m < tr.n) *reinterpret_cast<uint2 *>(codes + (m0 + m) * ldc + c + l8) = v[m].codes(inv[m]);
+        }
+      }
     }
-    __syncthreads();  // the next tile's sums go to the same LDS
+    __builtin_amdgcn_s_waitcnt(0xc07f);  // a wave reads back only what it wrote
+    asm volatile("" ::: "memory");
+  }
+  const int8_t *A[MB];
+#pragma unroll
+  for (int i = 0; i < MB; ++i)
+    A[i] = reinterpret_cast<const int8_t *>(p.A) + size_t(rows[min(16 * i + lr, tr.n - 1)]) * p.K;
+  const uint8_t *cr = codes + min(lr, tr.n - 1) * ldc;
+  i32x4 acc[MB];
+#pragma unroll
+  for (int i = 0; i < MB; ++i) acc[i] = i32x4{0, 0, 0, 0};
+  auto mul = [&](int s, const i32x4 (&d)[GS][2]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int g = 0; g < GS; ++g)
+      if (s + g < s1) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int k = 128 * (s + g) + kl + 64 * h;
+#pragma unroll
+          for (int i = 0; i < MB; ++i) {
+            i32x4 a;
+            if constexpr (FUSED) {
+              a = *reinterpret_cast<const i32x4 *>(cr + k);
+            } else {
+              a = chunk_at(A[i], k, p.K);
+              if (k >= p.K) a = i32x4{0, 0, 0, 0};
+            }
+            acc[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(d[g][h], a, acc[i], 0, 0, 0);
+          }
+        }
+      }
+  };
+#pragma unroll 1
+  for (int s = s0; s < s1; s += 2 * GS) {
+    mul(s, w[0]);
+    load_w(s + 2 * GS, w[0]);
+    mul(s + GS, w[1]);
+    load_w(s + 3 * GS, w[1]);
+  }
+#pragma unroll
+  for (int i = 0; i < MB; ++i) part[wid][i][lane] = acc[i];
+  lds_barrier();
+#pragma unroll
+  for (int i = wid; i < MB; i += NW) {
+    const i32x4 v = (part[0][i][lane] + part[1][i][lane]) + (part[2][i][lane] + part[3][i][lane]);
+    const int rl = 16 * i + lr, n = n0 + 4 * lg;
+    if (rl < tr.n && n < p.N) i8_out4<BF16, GELU>(p, size_t(rows[rl]), n, v, FUSED ? sa : p.a_scale[rows[rl]], cols);
   }
 }
 
-// Buffers of at most this many rows take the direct tiles.
-constexpr long long kDirectRows = 64;
-size_t linear_i8_part_bytes(long long rows) { return rows <= kDirectRows ? 0 : kSkPartBytes; }
+// Small products of float rows: tiles of 32 rows x 64 columns whose rows the workgroup quantises for itself into LDS,
+// 8 lanes a row and NC chunks of 8 values a lane (K <= 64 NC), then every wave multiplies them by its 16 columns.  One
+// launch, no codes in memory; each row is quantised N / 64 times over, which is why only small problems come here.
+constexpr int kSmallK = 768;
+template <bool BF16, bool GELU, int NC>
+__global__ __launch_bounds__(256) void k_linear_i8_small(GemmProblem p) {
+  constexpr int MB = 2, LDC = 64 * NC + 16;  // 16 rows' chunks at one column fall on all banks
+  __shared__ float scale[16 * MB];
+  __shared__ __attribute__((aligned(16))) uint8_t codes[16 * MB * LDC];
+  const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lr = lane & 15, lg = lane >> 4;
+  const int tilesN = (p.N + 63) / 64, t = blockIdx.x;
+  if (t >= row_tiles_total(p, 16 * MB) * tilesN) return;
+  const int n = t % tilesN * 64 + 16 * wid;
+  const TileRows tr = uni(decode_row_tile(p, 16 * MB, t / tilesN));
+  const int steps = (p.K + 63) / 64;
+  // all of the lane's part of its row
+  const int r = threadIdx.x >> 3, l = threadIdx.x & 7;
+  const size_t row = size_t(tr.row0 + min(r, tr.nrows - 1)) * p.K;
+  Raw8<BF16> v[NC];
+#pragma unroll
+  for (int k = 0; k < NC; ++k) v[k].load(p.A, row + min(64 * k + 8 * l, p.K - 8));
+  // and the wave's columns
+  const int8_t *W = reinterpret_cast<const int8_t *>(tr.sigma ? p.W[1] : p.W[0]) + size_t(min(n + lr, p.N - 1)) * p.K;
+  i32x4 w[NC];
+#pragma unroll
+  for (int s = 0; s < NC; ++s) w[s] = chunk_at(W, 64 * min(s, steps - 1) + 16 * lg, p.K);
+  const I8Cols<BF16> cols(p, tr.sigma, n + 4 * lg);
+  uint32_t top = 0;
+#pragma unroll
+  for (int k = 0; k < NC; ++k) top = v[k].top(top);  // behind K: the row's last values again
+#pragma unroll
+  for (int off = 4; off > 0; off >>= 1) top = max(top, uint32_t(__shfl_xor(int(top), off, 64)));
+  const float inv = i8_inverse(top);
+  if (l == 0) scale[r] = i8_scale(top);
+#pragma unroll
+  for (int k = 0; k < NC; ++k) {
+    if (64 * k + 8 * l >= p.K) v[k].zero();
+    *reinterpret_cast<uint2 *>(codes + r * LDC + 64 * k + 8 * l) = v[k].codes(inv);
+  }
+  lds_barrier();
+  i32x4 acc[MB];
+#pragma unroll
+  for (int i = 0; i < MB; ++i) acc[i] = i32x4{0, 0, 0, 0};
+#pragma unroll
+  for (int s = 0; s < NC; ++s)
+    if (s < steps) {
+#pragma unroll
+      for (int i = 0; i < MB; ++i) {
+        const i32x4 a = *reinterpret_cast<const i32x4 *>(codes + (16 * i + lr) * LDC + 64 * s + 16 * lg);
+        acc[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[s], a, acc[i], 0, 0, 0);
+      }
+    }
+  if (n + 4 * lg >= p.N) return;
+#pragma unroll
+  for (int i = 0; i < MB; ++i) {
+    const int rl = 16 * i + lr;
+    if (rl < tr.nrows) i8_out4<BF16, GELU>(p, size_t(tr.row0 + rl), n + 4 * lg, acc[i], scale[rl], cols);
+  }
+}
+
+// Buffers of at most this many rows take the narrow tiles.
+constexpr long long kFewRows = 64;
+size_t linear_i8_part_bytes(long long rows) { return rows <= kFewRows ? 0 : kSkPartBytes; }
+
+// Whether float rows are quantised by the kernel that multiplies them.
+static bool fused_few(const GemmProblem &p) { return p.max_img_rows <= 8 && p.max_img_rows * (p.K + 144) <= 49152; }
+static bool fused_small(const GemmProblem &p, bool bf16) {
+  return p.K <= kSmallK && double(p.max_img_rows) * p.K * (bf16 ? 2 : 4) * ((p.N + 63) / 64) <= 32e6;
+}
+bool linear_i8_fuses(bool bf16, const GemmProblem &p) { return fused_few(p) || fused_small(p, bf16); }
 
 template <bool BF16, bool GELU>
 static hipError_t run_linear_i8(const GemmProblem &p, hipStream_t st) {
-  const long long few = (long long)p.B * ((p.max_img_rows + 63) / 64 + (p.L + 63) / 64) * ((p.N + 31) / 32);
-  if (few <= 0) return hipSuccess;
-  hipLaunchKernelGGL((k_linear_i8_direct<BF16, GELU, 4, 2, 4>), dim3(unsigned(few < (1 << 16) ? few : (1 << 16))), dim3(256),
-                     0, st, p);
+  const int rows = p.max_img_rows;
+  if (p.a_scale == nullptr && !fused_few(p)) {
+    // row tiles: a part of one in every segment that has rows
+    const long long tiles = (rows / 32 + std::min<long long>(2LL * p.B, rows)) * ((p.N + 63) / 64);
+    const dim3 grid{unsigned(tiles)};
+    if (p.K <= 256) hipLaunchKernelGGL((k_linear_i8_small<BF16, GELU, 4>), grid, dim3(256), 0, st, p);
+    else if (p.K <= 512) hipLaunchKernelGGL((k_linear_i8_small<BF16, GELU, 8>), grid, dim3(256), 0, st, p);
+    else hipLaunchKernelGGL((k_linear_i8_small<BF16, GELU, 12>), grid, dim3(256), 0, st, p);
+    return hipGetLastError();
+  }
+  // row tiles of the two streams
+  const int bm = rows <= 16 ? 16 : 64, streams = p.L > 0 ? 2 : 1;
+  const dim3 grid(unsigned((p.N + 15) / 16), unsigned(streams * ((rows + bm - 1) / bm)));
+  if (p.a_scale == nullptr) {
+    const size_t lds = size_t(rows) * ((p.K + 127) / 128 * 128 + 16);
+    hipLaunchKernelGGL((k_linear_i8_few<BF16, GELU, 1, true>), grid, dim3(256), lds, st, p);
+  } else if (rows <= 16) {
+    hipLaunchKernelGGL((k_linear_i8_few<BF16, GELU, 1, false>), grid, dim3(256), 0, st, p);
+  } else {
+    hipLaunchKernelGGL((k_linear_i8_few<BF16, GELU, 4, false>), grid, dim3(256), 0, st, p);
+  }
   return hipGetLastError();
 }
 
 hipError_t launch_linear_i8(bool bf16, bool gelu, const GemmProblem &p, hipStream_t st) {
-  if (p.max_img_rows > kDirectRows) return launch_linear_i8_tiled(bf16, gelu, p, st);
+  if (p.a_scale != nullptr && p.max_img_rows > kFewRows) return launch_linear_i8_tiled(bf16, gelu, p, st);
   if (bf16) return gelu ? run_linear_i8<true, true>(p, st) : run_linear_i8<true, false>(p, st);
   return gelu ? run_linear_i8<false, true>(p, st) : run_linear_i8<false, false>(p, st);
 }

@@ -14,16 +14,40 @@ HILO_DEV float sum4(const float4 &a) { return (a.x + a.y) + (a.z + a.w); }
 HILO_DEV float dot4(const float4 &a, const float4 &b) { return (a.x * b.x + a.y * b.y) + (a.z * b.z + a.w * b.w); }
 HILO_DEV float4 ld4(const float *p) { return *reinterpret_cast<const float4 *>(p); }
 
+HILO_DEV float4 mul4(const float4 &a, const float4 &b) { return make_float4(a.x * b.x, a.y * b.y, a.z * b.z, a.w * b.w); }
+HILO_DEV float4 add4(const float4 &a, const float4 &b) { return make_float4(a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w); }
+HILO_DEV float4 add4(const float4 &a, float b) { return make_float4(a.x + b, a.y + b, a.z + b, a.w + b); }
+HILO_DEV float4 fma4(const float4 &a, const float4 &b, const float4 &c) {
+  return make_float4(a.x * b.x + c.x, a.y * b.y + c.y, a.z * b.z + c.z, a.w * b.w + c.w);
+}
+HILO_DEV float4 zero4() { return make_float4(0.f, 0.f, 0.f, 0.f); }
+HILO_DEV float4 only(bool in, const float4 &v) {
+  return make_float4(in ? v.x : 0.f, in ? v.y : 0.f, in ? v.z : 0.f, in ? v.w : 0.f);
+}
+// (v - mean) * r
+HILO_DEV float4 unit4(const float4 &v, float mean, float r) {
+  return make_float4((v.x - mean) * r, (v.y - mean) * r, (v.z - mean) * r, (v.w - mean) * r);
+}
+
+// Four values of a row of the block's type as they lie in memory.  Loads stand apart from what is done with them, and
+// lanes behind the last column read the last four again: no branch parts a row's loads, so all are in flight at once.
 template <bool BF16>
-HILO_DEV float4 load4(const void *p, size_t i) {
-  if constexpr (BF16) {
-    const uint2 u = *reinterpret_cast<const uint2 *>(reinterpret_cast<const uint16_t *>(p) + i);
+struct Raw4;
+template <>
+struct Raw4<true> {
+  uint2 u;
+  HILO_DEV void load(const void *p, size_t i) { u = *reinterpret_cast<const uint2 *>(reinterpret_cast<const uint16_t *>(p) + i); }
+  HILO_DEV float4 get() const {
     return make_float4(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u), __uint_as_float(u.y << 16),
                        __uint_as_float(u.y & 0xffff0000u));
-  } else {
-    return ld4(reinterpret_cast<const float *>(p) + i);
   }
-}
+};
+template <>
+struct Raw4<false> {
+  float4 u;
+  HILO_DEV void load(const void *p, size_t i) { u = ld4(reinterpret_cast<const float *>(p) + i); }
+  HILO_DEV float4 get() const { return u; }
+};
 
 template <bool BF16>
 HILO_DEV void store4(void *p, size_t i, const float4 &v) {
@@ -34,15 +58,29 @@ HILO_DEV void store4(void *p, size_t i, const float4 &v) {
   }
 }
 
-// Sums of two values over the W waves of a row's group, on every lane.  red: two sets of W pairs, used in turn, so
-// that one barrier per sum is enough (a set is written again only after the barrier of the other).
+// What a vector that is not given is read from: zeros, to which `by` is added (1 for a gate or a gain).
+__device__ const float g_zeros[8192] = {};
+struct Vector {
+  const __attribute__((address_space(1))) float *p;  // global, whichever it is
+  float by;
+  HILO_DEV Vector(const float *q, size_t at, float unless)
+      : p((const __attribute__((address_space(1))) float *)(q ? q + at : g_zeros)), by(q ? 0.f : unless) {}
+  HILO_DEV float4 operator()(int c) const {
+    typedef float f4 __attribute__((ext_vector_type(4)));
+    const f4 v = *(const __attribute__((address_space(1))) f4 *)(p + c);
+    return add4(make_float4(v[0], v[1], v[2], v[3]), by);
+  }
+};
+
+// Sums over the W waves of a row's group, of one value or of two, on every lane.  red: two sets of W pairs, used in turn,
+// so that one barrier per sum is enough (a set is written again only after the barrier of the other).
 template <int W>
 struct GroupSum {
   float2 *red;
   int turn = 0;
   HILO_DEV float2 operator()(float a, float b) {
-    a = wave_sum_f32(a);
-    b = wave_sum_f32(b);
+    a = wave_total(a);
+    b = wave_total(b);
     if constexpr (W == 1) return make_float2(a, b);
     float2 *r = red + turn * W;
     turn ^= 1;
@@ -56,94 +94,110 @@ struct GroupSum {
     }
     return s;
   }
+  HILO_DEV float operator()(float a) {
+    a = wave_total(a);
+    if constexpr (W == 1) return a;
+    float2 *r = red + turn * W;
+    turn ^= 1;
+    if ((threadIdx.x & 63) == 0) r[threadIdx.x >> 6].x = a;
+    __syncthreads();
+    float s = r[0].x;
+#pragma unroll
+    for (int w = 1; w < W; ++w) s += r[w].x;
+    return s;
+  }
 };
 
-// Mean and 1 / deviation of a row held as NV float4 a lane (columns past D are zero and not counted).  The deviation
-// is taken from the differences to the mean, not from the sum of squares: a row far from zero keeps its digits.
+// Mean and 1 / deviation of a row held as NV float4 a lane (zeros, not counted, where in[k] is false).  The deviation is
+// taken from the differences to the mean, not from the sum of squares: a row far from zero keeps its digits.
 template <int W, int NV>
-HILO_DEV float2 row_stats(const float4 (&v)[NV], int c0, int D, bool rms, float eps, GroupSum<W> &sum) {
+HILO_DEV float2 row_stats(const float4 (&v)[NV], const bool (&in)[NV], float inv_d, bool rms, float eps, GroupSum<W> &sum) {
   float mean = 0.f;
   if (!rms) {
     float s = 0.f;
 #pragma unroll
     for (int k = 0; k < NV; ++k) s += sum4(v[k]);
-    mean = sum(s, 0.f).x / float(D);
+    mean = sum(s) * inv_d;
   }
   float q = 0.f;
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
-    if (c0 + k * 256 * W < D) {
-      const float4 d = make_float4(v[k].x - mean, v[k].y - mean, v[k].z - mean, v[k].w - mean);
-      q += dot4(d, d);
-    }
+    const float4 d = only(in[k], add4(v[k], -mean));
+    q += dot4(d, d);
   }
-  return make_float2(mean, 1.0f / sqrtf(sum(q, 0.f).x / float(D) + eps));
+  return make_float2(mean, 1.0f / sqrtf(sum(q) * inv_d + eps));
 }
 
 }  // namespace
 
-// W waves a row, NV float4 a lane: D <= 256 W NV.  A workgroup of 4 waves holds 4 / W rows (8 waves: one).
+// W waves a row, NV float4 a lane: D <= 256 W NV.  W = 1: four rows a workgroup, else one.
 // OUT: h as 0 dtype, 1 int8 codes and row scales.
 template <bool BF16, int OUT, int W, int NV>
-__global__ __launch_bounds__(W > 4 ? 64 * W : 256) void k_norm_residual(NormProblem p) {
+__global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_norm_residual(NormProblem p) {
   __shared__ float2 red[2 * W];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int row = W == 1 ? blockIdx.x * 4 + wave : blockIdx.x;
   if (row >= min(p.rows, cu_at(p.cu, p.B))) return;
+  const size_t at = size_t(row) * p.D;
+  const int c0 = 4 * (W == 1 ? threadIdx.x & 63 : threadIdx.x);
+  int c[NV];
+  bool in[NV];
+  float4 x[NV];
+  Raw4<BF16> y[NV];
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    in[k] = c0 + k * 256 * W < p.D;
+    c[k] = in[k] ? c0 + k * 256 * W : p.D - 4;
+    x[k] = ld4(p.x + at + c[k]);
+  }
+  if (p.y) {
+#pragma unroll
+    for (int k = 0; k < NV; ++k) y[k].load(p.y, at + c[k]);
+  }
   const int s = sample_of_row(p.cu, p.B, row);
   const int sigma = row >= cu_at(p.cu, s + 1) - p.L ? 1 : 0;
   const size_t m = size_t(2 * s + sigma) * p.mod_stride;
-  const int c0 = 4 * (W == 1 ? threadIdx.x & 63 : threadIdx.x);
-  const float *post = sigma ? p.post[1] : p.post[0], *pre = sigma ? p.pre[1] : p.pre[0];
+  const float inv_d = 1.0f / float(p.D);
   GroupSum<W> sum{red};
-  float4 x[NV];
-  const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f), one = make_float4(1.f, 1.f, 1.f, 1.f);
-#pragma unroll
-  for (int k = 0; k < NV; ++k) {
-    const int c = c0 + k * 256 * W;
-    x[k] = c < p.D ? ld4(p.x + size_t(row) * p.D + c) : zero;
-  }
-  float4 st = zero;
+  float4 st = zero4();
   if (p.y) {
-    float4 y[NV];
+    const Vector gate(p.gate, m, 1.f), post(sigma ? p.post[1] : p.post[0], 0, 1.f);
+    float4 v[NV], f[NV];
 #pragma unroll
-    for (int k = 0; k < NV; ++k) {
-      const int c = c0 + k * 256 * W;
-      y[k] = c < p.D ? load4<BF16>(p.y, size_t(row) * p.D + c) : zero;
-    }
-    const float2 t = row_stats<W, NV>(y, c0, p.D, p.rms, p.eps, sum);
+    for (int k = 0; k < NV; ++k) f[k] = mul4(gate(c[k]), post(c[k]));
+#pragma unroll
+    for (int k = 0; k < NV; ++k) v[k] = only(in[k], y[k].get());
+    const float2 t = row_stats<W, NV>(v, in, inv_d, p.rms, p.eps, sum);
     st.x = t.x;
     st.y = t.y;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-      const int c = c0 + k * 256 * W;
-      if (c < p.D) {
-        const float4 g = p.gate ? ld4(p.gate + m + c) : one, w = post ? ld4(post + c) : one;
-        x[k].x = p.alpha * x[k].x + g.x * ((y[k].x - t.x) * t.y * w.x);
-        x[k].y = p.alpha * x[k].y + g.y * ((y[k].y - t.x) * t.y * w.y);
-        x[k].z = p.alpha * x[k].z + g.z * ((y[k].z - t.x) * t.y * w.z);
-        x[k].w = p.alpha * x[k].w + g.w * ((y[k].w - t.x) * t.y * w.w);
-        *reinterpret_cast<float4 *>(p.x_out + size_t(row) * p.D + c) = x[k];
-      }
+      const float4 u = mul4(f[k], unit4(v[k], t.x, t.y));
+      x[k] = make_float4(p.alpha * x[k].x + u.x, p.alpha * x[k].y + u.y, p.alpha * x[k].z + u.z, p.alpha * x[k].w + u.w);
+      if (in[k]) *reinterpret_cast<float4 *>(p.x_out + at + c[k]) = x[k];
     }
   }
   if (p.h) {
-    const float2 t = row_stats<W, NV>(x, c0, p.D, p.rms, p.eps, sum);
+    const Vector scale(p.scale, m, 0.f), shift(p.shift, m, 0.f), pre(sigma ? p.pre[1] : p.pre[0], 0, 1.f);
+    float4 f[NV], b[NV];
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      f[k] = mul4(pre(c[k]), add4(scale(c[k]), 1.f));
+      b[k] = shift(c[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < NV; ++k) x[k] = only(in[k], x[k]);
+    const float2 t = row_stats<W, NV>(x, in, inv_d, p.rms, p.eps, sum);
     st.z = t.x;
     st.w = t.y;
     uint32_t top = 0;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-      const int c = c0 + k * 256 * W;
-      if (c < p.D) {
-        const float4 a = p.scale ? ld4(p.scale + m + c) : zero, b = p.shift ? ld4(p.shift + m + c) : zero;
-        const float4 w = pre ? ld4(pre + c) : one;
-        x[k].x = (x[k].x - t.x) * t.y * w.x * (1.f + a.x) + b.x;
-        x[k].y = (x[k].y - t.x) * t.y * w.y * (1.f + a.y) + b.y;
-        x[k].z = (x[k].z - t.x) * t.y * w.z * (1.f + a.z) + b.z;
-        x[k].w = (x[k].w - t.x) * t.y * w.w * (1.f + a.w) + b.w;
-        if constexpr (OUT == 0) store4<BF16>(p.h, size_t(row) * p.D + c, x[k]);
-        else top = max(max(max(abs_bits(x[k].x), abs_bits(x[k].y)), max(abs_bits(x[k].z), abs_bits(x[k].w))), top);
+      x[k] = fma4(f[k], unit4(x[k], t.x, t.y), b[k]);
+      if constexpr (OUT == 0) {
+        if (in[k]) store4<BF16>(p.h, at + c[k], x[k]);
+      } else if (in[k]) {
+        top = max(max(max(abs_bits(x[k].x), abs_bits(x[k].y)), max(abs_bits(x[k].z), abs_bits(x[k].w))), top);
       }
     }
     if constexpr (OUT == 1) {
@@ -157,13 +211,10 @@ __global__ __launch_bounds__(W > 4 ? 64 * W : 256) void k_norm_residual(NormProb
       }
       const float inv = i8_inverse(top);
       if (c0 == 0) p.h_scale[row] = i8_scale(top);
-      int8_t *o = reinterpret_cast<int8_t *>(p.h) + size_t(row) * p.D;
+      int8_t *o = reinterpret_cast<int8_t *>(p.h) + at;
 #pragma unroll
-      for (int k = 0; k < NV; ++k) {
-        const int c = c0 + k * 256 * W;
-        if (c < p.D)
-          *reinterpret_cast<uint32_t *>(o + c) = i8x4(x[k].x * inv, x[k].y * inv, x[k].z * inv, x[k].w * inv);
-      }
+      for (int k = 0; k < NV; ++k)
+        if (in[k]) *reinterpret_cast<uint32_t *>(o + c[k]) = i8x4(x[k].x, x[k].y, x[k].z, x[k].w, inv);
     }
   }
   if (p.stats && c0 == 0) *reinterpret_cast<float4 *>(p.stats + 4 * size_t(row)) = st;
@@ -173,7 +224,7 @@ hipError_t launch_norm_residual(bool bf16, const NormProblem &p, hipStream_t st)
   if (p.rows <= 0) return hipSuccess;
 #define HILO_NR(W, NV)                                                                                            \
   do {                                                                                                            \
-    const dim3 grid(W == 1 ? (unsigned(p.rows) + 3) / 4 : unsigned(p.rows)), block(W > 4 ? 64 * W : 256);            \
+    const dim3 grid(W == 1 ? (unsigned(p.rows) + 3) / 4 : unsigned(p.rows)), block(W == 1 ? 256 : 64 * W);          \
     if (p.h_scale) {                                                                                                \
       if (bf16) hipLaunchKernelGGL((k_norm_residual<true, 1, W, NV>), grid, block, 0, st, p);                       \
       else hipLaunchKernelGGL((k_norm_residual<false, 1, W, NV>), grid, block, 0, st, p);                           \
@@ -215,16 +266,28 @@ HILO_DEV NormSlots norm_slots(const int *cu, int B, int rows, int P) {
 HILO_DEV int norm_row0(const NormSlots &q, int w) { return int((long long)q.R * w / q.P); }
 HILO_DEV int norm_owner(const NormSlots &q, int row) { return int(((long long)(row + 1) * q.P - 1) / q.R); }
 
+// r (n - mean(n) - v mean(n v)) per value; without the mean of n for RMS (t.x taken as 0).
+HILO_DEV float4 through4(const float4 &n, const float4 &v, float2 t, float r) {
+  return make_float4(r * (n.x - t.x - v.x * t.y), r * (n.y - t.x - v.y * t.y), r * (n.z - t.x - v.z * t.y),
+                     r * (n.w - t.x - v.w * t.y));
+}
+
 template <bool BF16, int W, int NV>
-__global__ __launch_bounds__(W > 4 ? 64 * W : 256) void k_norm_residual_back(NormBackProblem p) {
+__global__ __launch_bounds__(W == 1 ? 256 : 64 * W, NV < 4 ? 3 : 2) void k_norm_residual_back(NormBackProblem p) {
   __shared__ float2 red[2 * W];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int w = W == 1 ? blockIdx.x * 4 + wave : blockIdx.x;
   const NormSlots q = norm_slots(p.cu, p.B, p.rows, p.P);
   if (w >= q.P) return;
   const int c0 = 4 * (W == 1 ? threadIdx.x & 63 : threadIdx.x);
-  const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f), one = make_float4(1.f, 1.f, 1.f, 1.f);
-  const float inv_d = 1.0f / float(p.D), center = p.rms ? 0.f : 1.f;
+  int c[NV];
+  bool in[NV];
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    in[k] = c0 + k * 256 * W < p.D;
+    c[k] = in[k] ? c0 + k * 256 * W : p.D - 4;
+  }
+  const float inv_d = 1.0f / float(p.D), center = p.rms ? 0.f : inv_d;
   GroupSum<W> sum{red};
   const int last = norm_row0(q, w + 1);
   int row = norm_row0(q, w);
@@ -233,120 +296,97 @@ __global__ __launch_bounds__(W > 4 ? 64 * W : 256) void k_norm_residual_back(Nor
     const int ts = cu_at(p.cu, s + 1) - p.L;
     const int sigma = row >= ts ? 1 : 0, end = min(last, sigma ? ts + p.L : ts);
     const size_t m = size_t(2 * s + sigma) * p.mod_stride;
-    const float *post = sigma ? p.post[1] : p.post[0], *pre = sigma ? p.pre[1] : p.pre[0];
-    float4 fx[NV], fy[NV];  // (1 + scale) pre and gate post
-    float4 A[NV], Bs[NV], C[NV];
+    const Vector gate(p.gate, m, 1.f), scale(p.scale, m, 0.f);
+    const Vector post(sigma ? p.post[1] : p.post[0], 0, 1.f), pre(sigma ? p.pre[1] : p.pre[0], 0, 1.f);
+    float4 fx[NV], fy[NV];  // (1 + scale) pre and gate post, zero behind the last column
+    float4 A[NV], B[NV], C[NV];
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-      const int c = c0 + k * 256 * W;
-      A[k] = Bs[k] = C[k] = zero;
-      fx[k] = fy[k] = one;
-      if (c < p.D) {
-        if (p.scale) {
-          const float4 a = ld4(p.scale + m + c);
-          fx[k] = make_float4(1.f + a.x, 1.f + a.y, 1.f + a.z, 1.f + a.w);
-        }
-        if (pre) {
-          const float4 a = ld4(pre + c);
-          fx[k] = make_float4(fx[k].x * a.x, fx[k].y * a.y, fx[k].z * a.z, fx[k].w * a.w);
-        }
-        if (p.gate) fy[k] = ld4(p.gate + m + c);
-        if (post) {
-          const float4 a = ld4(post + c);
-          fy[k] = make_float4(fy[k].x * a.x, fy[k].y * a.y, fy[k].z * a.z, fy[k].w * a.w);
-        }
-      }
+      fx[k] = only(in[k], mul4(add4(scale(c[k]), 1.f), pre(c[k])));
+      fy[k] = only(in[k], mul4(gate(c[k]), post(c[k])));
+      A[k] = B[k] = C[k] = zero4();
     }
     for (; row < end; ++row) {
-      const float4 st = ld4(p.stats + 4 * size_t(row));
-      float4 g[NV];
-#pragma unroll
-      for (int k = 0; k < NV; ++k) {
-        const int c = c0 + k * 256 * W;
-        g[k] = p.dx_out && c < p.D ? ld4(p.dx_out + size_t(row) * p.D + c) : zero;
-      }
+      const size_t at = size_t(row) * p.D;
+      float4 g[NV], x[NV];
+      Raw4<BF16> dh[NV], y[NV];
       if (p.dh) {
-        float4 xh[NV], n[NV];
-        float a = 0.f, b = 0.f;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-          const int c = c0 + k * 256 * W;
-          xh[k] = n[k] = zero;
-          if (c < p.D) {
-            const float4 x = ld4(p.x_out + size_t(row) * p.D + c), d = load4<BF16>(p.dh, size_t(row) * p.D + c);
-            xh[k] = make_float4((x.x - st.z) * st.w, (x.y - st.z) * st.w, (x.z - st.z) * st.w, (x.w - st.z) * st.w);
-            C[k] = make_float4(C[k].x + d.x, C[k].y + d.y, C[k].z + d.z, C[k].w + d.w);
-            Bs[k] = make_float4(Bs[k].x + d.x * xh[k].x, Bs[k].y + d.y * xh[k].y, Bs[k].z + d.z * xh[k].z,
-                                Bs[k].w + d.w * xh[k].w);
-            n[k] = make_float4(d.x * fx[k].x, d.y * fx[k].y, d.z * fx[k].z, d.w * fx[k].w);
-          }
-          a += sum4(n[k]);
-          b += dot4(n[k], xh[k]);
+          dh[k].load(p.dh, at + c[k]);
+          x[k] = ld4(p.x_out + at + c[k]);
         }
-        const float2 t = sum(a, b);
-        const float mn = center * t.x * inv_d, mx = t.y * inv_d;
+      }
+      if (p.dx_out) {
 #pragma unroll
-        for (int k = 0; k < NV; ++k) {
-          g[k].x += st.w * (n[k].x - mn - xh[k].x * mx);
-          g[k].y += st.w * (n[k].y - mn - xh[k].y * mx);
-          g[k].z += st.w * (n[k].z - mn - xh[k].z * mx);
-          g[k].w += st.w * (n[k].w - mn - xh[k].w * mx);
-        }
+        for (int k = 0; k < NV; ++k) g[k] = ld4(p.dx_out + at + c[k]);
+      } else {
+#pragma unroll
+        for (int k = 0; k < NV; ++k) g[k] = zero4();
       }
       if (p.y) {
-        float4 yh[NV], e[NV];
+#pragma unroll
+        for (int k = 0; k < NV; ++k) y[k].load(p.y, at + c[k]);
+      }
+      const float4 st = ld4(p.stats + 4 * size_t(row));
+      if (p.dh) {
+        float4 n[NV];
         float a = 0.f, b = 0.f;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-          const int c = c0 + k * 256 * W;
-          yh[k] = e[k] = zero;
-          if (c < p.D) {
-            const float4 y = load4<BF16>(p.y, size_t(row) * p.D + c);
-            yh[k] = make_float4((y.x - st.x) * st.y, (y.y - st.x) * st.y, (y.z - st.x) * st.y, (y.w - st.x) * st.y);
-            A[k] = make_float4(A[k].x + g[k].x * yh[k].x, A[k].y + g[k].y * yh[k].y, A[k].z + g[k].z * yh[k].z,
-                               A[k].w + g[k].w * yh[k].w);
-            e[k] = make_float4(g[k].x * fy[k].x, g[k].y * fy[k].y, g[k].z * fy[k].z, g[k].w * fy[k].w);
-          }
-          a += sum4(e[k]);
-          b += dot4(e[k], yh[k]);
+          const float4 d = dh[k].get();
+          x[k] = unit4(x[k], st.z, st.w);
+          C[k] = add4(C[k], d);
+          B[k] = fma4(d, x[k], B[k]);
+          n[k] = mul4(d, fx[k]);
+          a += sum4(n[k]);
+          b += dot4(n[k], x[k]);
         }
-        const float2 t = sum(a, b);
-        const float mn = center * t.x * inv_d, mx = t.y * inv_d;
+        float2 t = sum(a, b);
+        t = make_float2(t.x * center, t.y * inv_d);
+#pragma unroll
+        for (int k = 0; k < NV; ++k) g[k] = add4(g[k], through4(n[k], x[k], t, st.w));
+      }
+      if (p.y) {
+        float4 v[NV], e[NV];
+        float a = 0.f, b = 0.f;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-          const int c = c0 + k * 256 * W;
-          if (c < p.D)
-            store4<BF16>(p.dy, size_t(row) * p.D + c,
-                         make_float4(st.y * (e[k].x - mn - yh[k].x * mx), st.y * (e[k].y - mn - yh[k].y * mx),
-                                     st.y * (e[k].z - mn - yh[k].z * mx), st.y * (e[k].w - mn - yh[k].w * mx)));
+          v[k] = unit4(y[k].get(), st.x, st.y);
+          A[k] = fma4(g[k], v[k], A[k]);
+          e[k] = mul4(g[k], fy[k]);
+          a += sum4(e[k]);
+          b += dot4(e[k], v[k]);
         }
+        float2 t = sum(a, b);
+        t = make_float2(t.x * center, t.y * inv_d);
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+          if (in[k]) store4<BF16>(p.dy, at + c[k], through4(e[k], v[k], t, st.y));
       }
 #pragma unroll
-      for (int k = 0; k < NV; ++k) {
-        const int c = c0 + k * 256 * W;
-        if (c < p.D)
-          *reinterpret_cast<float4 *>(p.dx + size_t(row) * p.D + c) =
+      for (int k = 0; k < NV; ++k)
+        if (in[k])
+          *reinterpret_cast<float4 *>(p.dx + at + c[k]) =
               make_float4(p.alpha * g[k].x, p.alpha * g[k].y, p.alpha * g[k].z, p.alpha * g[k].w);
-      }
     }
     if (p.part) {
       float *slot = p.part + size_t(w + 2 * s + sigma) * 3 * p.D;
 #pragma unroll
-      for (int k = 0; k < NV; ++k) {
-        const int c = c0 + k * 256 * W;
-        if (c < p.D) {
-          *reinterpret_cast<float4 *>(slot + c) = A[k];
-          *reinterpret_cast<float4 *>(slot + p.D + c) = Bs[k];
-          *reinterpret_cast<float4 *>(slot + 2 * p.D + c) = C[k];
+      for (int k = 0; k < NV; ++k)
+        if (in[k]) {
+          *reinterpret_cast<float4 *>(slot + c[k]) = A[k];
+          *reinterpret_cast<float4 *>(slot + p.D + c[k]) = B[k];
+          *reinterpret_cast<float4 *>(slot + 2 * p.D + c[k]) = C[k];
         }
-      }
     }
   }
 }
 
 // Sums the slots of one segment: blockIdx.x segment, blockIdx.y 64 columns, blockIdx.z which of A, B, C.  16 lanes of
-// four columns by 16 groups of slots, joined in group order.  A and B go on to the gains (sums: [2 B][2][D]).
-__global__ __launch_bounds__(256) void k_norm_sums(NormBackProblem p, float *sums) {
+// four columns by 16 groups of slots, joined in group order.  A and B go on to the gains (sums: [2 B][2][D]), or with one
+// sample and a gain a stream are all there is to them (gains_here).
+__global__ __launch_bounds__(256) void k_norm_sums(NormBackProblem p, float *sums, bool gains_here) {
   __shared__ float4 red[16][16];
   const int seg = blockIdx.x, s = seg >> 1, sigma = seg & 1, which = blockIdx.z;
   const NormSlots q = norm_slots(p.cu, p.B, p.rows, p.P);
@@ -369,7 +409,13 @@ __global__ __launch_bounds__(256) void k_norm_sums(NormBackProblem p, float *sum
     const float4 t = red[g][lane];
     v = make_float4(v.x + t.x, v.y + t.y, v.z + t.z, v.w + t.w);
   }
-  if (which < 2) *reinterpret_cast<float4 *>(sums + (size_t(seg) * 2 + which) * p.D + c) = v;
+  if (which < 2 && gains_here) {
+    float *to = which ? (sigma ? p.dpre[1] : p.dpre[0]) : (sigma ? p.dpost[1] : p.dpost[0]);
+    const Vector mod(which ? p.scale : p.gate, size_t(seg) * p.mod_stride, which ? 0.f : 1.f);
+    if (to) *reinterpret_cast<float4 *>(to + c) = mul4(v, add4(mod(c), float(which)));
+  } else if (which < 2) {
+    *reinterpret_cast<float4 *>(sums + (size_t(seg) * 2 + which) * p.D + c) = v;
+  }
   const float *gain = which == 0 ? (sigma ? p.post[1] : p.post[0]) : which == 1 ? (sigma ? p.pre[1] : p.pre[0]) : nullptr;
   float *out = which == 0 ? p.dgate : which == 1 ? p.dscale : p.dshift;
   if (!out) return;
@@ -385,11 +431,16 @@ __global__ __launch_bounds__(256) void k_norm_gains(NormBackProblem p, const flo
   const int c = blockIdx.x * 256 + threadIdx.x, which = blockIdx.y;
   if (c >= p.D) return;
   float *out[2] = {which ? p.dpre[0] : p.dpost[0], which ? p.dpre[1] : p.dpost[1]};
+  const float *mod = which ? p.scale : p.gate;
   float v[2] = {0.f, 0.f};
-  for (int seg = 0; seg < 2 * p.B; ++seg) {
-    const float *mod = which ? p.scale : p.gate;
-    const float f = mod ? mod[size_t(seg) * p.mod_stride + c] + float(which) : 1.f;
-    v[seg & 1] += f * sums[(size_t(seg) * 2 + which) * p.D + c];
+#pragma unroll 4
+  for (int s = 0; s < p.B; ++s) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const size_t seg = size_t(2 * s + k);
+      const float f = (mod ? mod : g_zeros)[mod ? seg * p.mod_stride + c : 0];
+      v[k] += (mod ? f + float(which) : 1.f) * sums[(seg * 2 + which) * p.D + c];
+    }
   }
   if (out[0] && out[0] == out[1]) {
     out[0][c] = v[0] + v[1];
@@ -418,7 +469,7 @@ hipError_t launch_norm_residual_back(bool bf16, NormBackProblem p, hipStream_t s
   if (p.rows > 0) {
 #define HILO_NB(W, NV)                                                                                     \
   do {                                                                                                     \
-    const dim3 grid(W == 1 ? unsigned(p.P + 3) / 4 : unsigned(p.P)), block(W > 4 ? 64 * W : 256);           \
+    const dim3 grid(W == 1 ? unsigned(p.P + 3) / 4 : unsigned(p.P)), block(W == 1 ? 256 : 64 * W);          \
     if (bf16) hipLaunchKernelGGL((k_norm_residual_back<true, W, NV>), grid, block, 0, st, p);              \
     else hipLaunchKernelGGL((k_norm_residual_back<false, W, NV>), grid, block, 0, st, p);                  \
   } while (0)
@@ -434,9 +485,12 @@ hipError_t launch_norm_residual_back(bool bf16, NormBackProblem p, hipStream_t s
     if (e != hipSuccess) return e;
   }
   if (!p.part) return hipSuccess;
-  hipLaunchKernelGGL(k_norm_sums, dim3(2 * p.B, (p.D + 63) / 64, 3), dim3(256), 0, st, p, sums);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || !(p.dpost[0] || p.dpost[1] || p.dpre[0] || p.dpre[1])) return e;
+  const bool gains = p.dpost[0] || p.dpost[1] || p.dpre[0] || p.dpre[1];
+  const bool shared = (p.dpost[0] && p.dpost[0] == p.dpost[1]) || (p.dpre[0] && p.dpre[0] == p.dpre[1]);
+  const bool here = p.B == 1 && !shared;
+  hipLaunchKernelGGL(k_norm_sums, dim3(2 * p.B, (p.D + 63) / 64, 3), dim3(256), 0, st, p, sums, here);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || !gains || here) return e;
   hipLaunchKernelGGL(k_norm_gains, dim3((p.D + 255) / 256, 2), dim3(256), 0, st, p, sums);
   return hipGetLastError();
 }

@@ -441,12 +441,16 @@ def _on_device(t: torch.Tensor) -> int:
     return dev
 
 
+# The current stream's handle without a Stream object around it (2.7 us of the 8 us that a small call took).
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
+
+
 def _launch(fn, dev: int, stream, *args):
     """fn(*args, stream) with `dev` as the current device."""
     if dev != torch.cuda.current_device():
         with torch.cuda.device(dev):
             return _launch(fn, dev, stream, *args)
-    st = getattr(lib(), fn)(*args, torch.cuda.current_stream(dev).cuda_stream if stream is None else _stream(stream))
+    st = getattr(lib(), fn)(*args, _raw_stream(dev) if stream is None else _stream(stream))
     if st != 0:
         raise HiloError(fn, st)
 
