@@ -156,8 +156,9 @@ struct NormProblem {
   void *h;              // [rows][D] dtype, int8 codes with h_scale, or null: no norm before the next block
   float *h_scale;       // [rows]
   float *stats;         // [rows][4]: mean and 1 / deviation of y, of x_out; may be null
+  int P;                // workers, set by the launcher
 };
-hipError_t launch_norm_residual(bool bf16, const NormProblem &p, hipStream_t st);
+hipError_t launch_norm_residual(bool bf16, NormProblem p, hipStream_t st);
 
 // Its backward pass.
 struct NormBackProblem {

@@ -29,6 +29,26 @@ HILO_DEV float4 unit4(const float4 &v, float mean, float r) {
   return make_float4((v.x - mean) * r, (v.y - mean) * r, (v.z - mean) * r, (v.w - mean) * r);
 }
 
+// Loads from a uniform base and a 32-bit byte offset of the lane, in global memory.
+typedef const __attribute__((address_space(1))) char *GlobalPtr;
+// The base is made opaque, in scalar registers: otherwise base + offset is formed for every tensor ahead of the loop
+// over rows, in two vector registers each, and the row's part is added to that.
+HILO_DEV GlobalPtr global_ptr(const void *p) {
+  uint64_t v = reinterpret_cast<uint64_t>(p);
+  asm volatile("" : "+s"(v));
+  return (GlobalPtr)v;
+}
+HILO_DEV float4 gld4(GlobalPtr p, uint32_t off) {
+  typedef float f4 __attribute__((ext_vector_type(4)));
+  const f4 v = *(const __attribute__((address_space(1))) f4 *)(p + off);
+  return make_float4(v[0], v[1], v[2], v[3]);
+}
+HILO_DEV uint2 gld2(GlobalPtr p, uint32_t off) {
+  typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+  const u2 v = *(const __attribute__((address_space(1))) u2 *)(p + off);
+  return make_uint2(v[0], v[1]);
+}
+
 // Four values of a row of the block's type as they lie in memory.  Loads stand apart from what is done with them, and
 // lanes behind the last column read the last four again: no branch parts a row's loads, so all are in flight at once.
 template <bool BF16>
@@ -36,7 +56,7 @@ struct Raw4;
 template <>
 struct Raw4<true> {
   uint2 u;
-  HILO_DEV void load(const void *p, size_t i) { u = *reinterpret_cast<const uint2 *>(reinterpret_cast<const uint16_t *>(p) + i); }
+  HILO_DEV void load(GlobalPtr row, uint32_t c) { u = gld2(row, 2 * c); }
   HILO_DEV float4 get() const {
     return make_float4(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u), __uint_as_float(u.y << 16),
                        __uint_as_float(u.y & 0xffff0000u));
@@ -45,31 +65,28 @@ struct Raw4<true> {
 template <>
 struct Raw4<false> {
   float4 u;
-  HILO_DEV void load(const void *p, size_t i) { u = ld4(reinterpret_cast<const float *>(p) + i); }
+  HILO_DEV void load(GlobalPtr row, uint32_t c) { u = gld4(row, 4 * c); }
   HILO_DEV float4 get() const { return u; }
 };
+template <bool BF16>
+HILO_DEV GlobalPtr row_at(const void *p, size_t i) { return global_ptr(reinterpret_cast<const char *>(p) + i * (BF16 ? 2 : 4)); }
 
 template <bool BF16>
-HILO_DEV void store4(void *p, size_t i, const float4 &v) {
-  if constexpr (BF16) {
-    *reinterpret_cast<uint2 *>(reinterpret_cast<uint16_t *>(p) + i) = make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
-  } else {
-    *reinterpret_cast<float4 *>(reinterpret_cast<float *>(p) + i) = v;
-  }
+HILO_DEV void store4(GlobalPtr row, uint32_t c, const float4 &v) {
+  typedef float f4 __attribute__((ext_vector_type(4)));
+  typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+  auto *p = (__attribute__((address_space(1))) char *)row;
+  if constexpr (BF16) *(__attribute__((address_space(1))) u2 *)(p + 2 * c) = u2{pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w)};
+  else *(__attribute__((address_space(1))) f4 *)(p + 4 * c) = f4{v.x, v.y, v.z, v.w};
 }
 
 // What a vector that is not given is read from: zeros, to which `by` is added (1 for a gate or a gain).
 __device__ const float g_zeros[8192] = {};
 struct Vector {
-  const __attribute__((address_space(1))) float *p;  // global, whichever it is
+  GlobalPtr p;
   float by;
-  HILO_DEV Vector(const float *q, size_t at, float unless)
-      : p((const __attribute__((address_space(1))) float *)(q ? q + at : g_zeros)), by(q ? 0.f : unless) {}
-  HILO_DEV float4 operator()(int c) const {
-    typedef float f4 __attribute__((ext_vector_type(4)));
-    const f4 v = *(const __attribute__((address_space(1))) f4 *)(p + c);
-    return add4(make_float4(v[0], v[1], v[2], v[3]), by);
-  }
+  HILO_DEV Vector(const float *q, size_t at, float unless) : p(global_ptr(q ? q + at : g_zeros)), by(q ? 0.f : unless) {}
+  HILO_DEV float4 operator()(uint32_t c) const { return add4(gld4(p, 4 * c), by); }
 };
 
 // Sums over the W waves of a row's group, of one value or of two, on every lane.  red: two sets of W pairs, used in turn,
@@ -130,101 +147,154 @@ HILO_DEV float2 row_stats(const float4 (&v)[NV], const bool (&in)[NV], float inv
 
 }  // namespace
 
-// W waves a row, NV float4 a lane: D <= 256 W NV.  W = 1: four rows a workgroup, else one.
-// OUT: h as 0 dtype, 1 int8 codes and row scales.
-template <bool BF16, int OUT, int W, int NV>
-__global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void k_norm_residual(NormProblem p) {
-  __shared__ float2 red[2 * W];
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int row = W == 1 ? blockIdx.x * 4 + wave : blockIdx.x;
-  if (row >= min(p.rows, cu_at(p.cu, p.B))) return;
-  const size_t at = size_t(row) * p.D;
-  const int c0 = 4 * (W == 1 ? threadIdx.x & 63 : threadIdx.x);
-  int c[NV];
-  bool in[NV];
-  float4 x[NV];
-  Raw4<BF16> y[NV];
-#pragma unroll
-  for (int k = 0; k < NV; ++k) {
-    in[k] = c0 + k * 256 * W < p.D;
-    c[k] = in[k] ? c0 + k * 256 * W : p.D - 4;
-    x[k] = ld4(p.x + at + c[k]);
-  }
-  if (p.y) {
-#pragma unroll
-    for (int k = 0; k < NV; ++k) y[k].load(p.y, at + c[k]);
-  }
-  const int s = sample_of_row(p.cu, p.B, row);
-  const int sigma = row >= cu_at(p.cu, s + 1) - p.L ? 1 : 0;
-  const size_t m = size_t(2 * s + sigma) * p.mod_stride;
-  const float inv_d = 1.0f / float(p.D);
-  GroupSum<W> sum{red};
-  float4 st = zero4();
-  if (p.y) {
-    const Vector gate(p.gate, m, 1.f), post(sigma ? p.post[1] : p.post[0], 0, 1.f);
-    float4 v[NV], f[NV];
-#pragma unroll
-    for (int k = 0; k < NV; ++k) f[k] = mul4(gate(c[k]), post(c[k]));
-#pragma unroll
-    for (int k = 0; k < NV; ++k) v[k] = only(in[k], y[k].get());
-    const float2 t = row_stats<W, NV>(v, in, inv_d, p.rms, p.eps, sum);
-    st.x = t.x;
-    st.y = t.y;
-#pragma unroll
-    for (int k = 0; k < NV; ++k) {
-      const float4 u = mul4(f[k], unit4(v[k], t.x, t.y));
-      x[k] = make_float4(p.alpha * x[k].x + u.x, p.alpha * x[k].y + u.y, p.alpha * x[k].z + u.z, p.alpha * x[k].w + u.w);
-      if (in[k]) *reinterpret_cast<float4 *>(p.x_out + at + c[k]) = x[k];
-    }
-  }
-  if (p.h) {
-    const Vector scale(p.scale, m, 0.f), shift(p.shift, m, 0.f), pre(sigma ? p.pre[1] : p.pre[0], 0, 1.f);
-    float4 f[NV], b[NV];
-#pragma unroll
-    for (int k = 0; k < NV; ++k) {
-      f[k] = mul4(pre(c[k]), add4(scale(c[k]), 1.f));
-      b[k] = shift(c[k]);
-    }
-#pragma unroll
-    for (int k = 0; k < NV; ++k) x[k] = only(in[k], x[k]);
-    const float2 t = row_stats<W, NV>(x, in, inv_d, p.rms, p.eps, sum);
-    st.z = t.x;
-    st.w = t.y;
-    uint32_t top = 0;
-#pragma unroll
-    for (int k = 0; k < NV; ++k) {
-      x[k] = fma4(f[k], unit4(x[k], t.x, t.y), b[k]);
-      if constexpr (OUT == 0) {
-        if (in[k]) store4<BF16>(p.h, at + c[k], x[k]);
-      } else if (in[k]) {
-        top = max(max(max(abs_bits(x[k].x), abs_bits(x[k].y)), max(abs_bits(x[k].z), abs_bits(x[k].w))), top);
-      }
-    }
-    if constexpr (OUT == 1) {
-      top = wave_max_u32(top);
-      if constexpr (W > 1) {
-        __shared__ uint32_t tops[W];
-        if ((threadIdx.x & 63) == 0) tops[wave] = top;
-        __syncthreads();
-#pragma unroll
-        for (int w = 0; w < W; ++w) top = max(top, tops[w]);
-      }
-      const float inv = i8_inverse(top);
-      if (c0 == 0) p.h_scale[row] = i8_scale(top);
-      int8_t *o = reinterpret_cast<int8_t *>(p.h) + at;
-#pragma unroll
-      for (int k = 0; k < NV; ++k)
-        if (in[k]) *reinterpret_cast<uint32_t *>(o + c[k]) = i8x4(x[k].x, x[k].y, x[k].z, x[k].w, inv);
-    }
-  }
-  if (p.stats && c0 == 0) *reinterpret_cast<float4 *>(p.stats + 4 * size_t(row)) = st;
+// Workers take consecutive shares of the R rows in use, none of them empty: no more workers than rows.
+struct NormShares {
+  int R, P;
+};
+HILO_DEV NormShares norm_shares(const int *cu, int B, int rows, int P) {
+  const int R = min(rows, cu_at(cu, B));
+  return NormShares{R, min(P, R)};
+}
+HILO_DEV int share_begin(const NormShares &q, int w) { return int((long long)q.R * w / q.P); }
+HILO_DEV int share_owner(const NormShares &q, int row) { return int(((long long)(row + 1) * q.P - 1) / q.R); }
+
+// The segment of a row and where a share's rows leave it.
+struct RowSegment {
+  int s, sigma, end;
+};
+HILO_DEV RowSegment row_segment(const int *cu, int B, int L, int row, int last) {
+  const int s = B == 1 ? 0 : sample_of_row(cu, B, row);
+  const int hi = cu_at(cu, s + 1), ts = hi - L, sigma = row >= ts ? 1 : 0;
+  return RowSegment{s, sigma, min(last, sigma ? hi : ts)};
 }
 
-hipError_t launch_norm_residual(bool bf16, const NormProblem &p, hipStream_t st) {
+// Waves a SIMD that the registers leave room for.
+constexpr int norm_waves(int NV) { return NV == 1 ? 8 : NV == 2 ? 5 : NV == 3 ? 4 : 3; }
+
+// A worker is W waves, NV float4 a lane (D <= 256 W NV); W = 1: four a workgroup.  It keeps the vectors of the segment
+// that its rows are in -- read for every row they are more than the row itself -- and reads a row ahead.
+// OUT: h as 0 dtype, 1 int8 codes and row scales.
+template <bool BF16, int OUT, int W, int NV>
+__global__ __launch_bounds__(W == 1 ? 256 : 64 * W, norm_waves(NV)) void k_norm_residual(NormProblem p) {
+  __shared__ float2 red[2 * W];
+  __shared__ uint32_t tops[2][W];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int w = W == 1 ? blockIdx.x * 4 + wave : blockIdx.x;
+  const NormShares q = norm_shares(p.cu, p.B, p.rows, p.P);
+  if (w >= q.P) return;
+  const uint32_t c0 = 4 * (W == 1 ? threadIdx.x & 63 : threadIdx.x);
+  uint32_t c[NV];
+  bool in[NV];
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    in[k] = c0 + k * 256 * W < uint32_t(p.D);
+    c[k] = in[k] ? c0 + k * 256 * W : p.D - 4;
+  }
+  const float inv_d = 1.0f / float(p.D);
+  GroupSum<W> sum{red};
+  int turn = 0;
+  const int last = share_begin(q, w + 1);
+  int row = share_begin(q, w);
+  float4 nx[NV];
+  Raw4<BF16> ny[NV];
+  auto load = [&](int r) __attribute__((always_inline)) {
+    const size_t at = size_t(r) * p.D;
+    const GlobalPtr px = global_ptr(p.x + at), py = row_at<BF16>(p.y, at);
+#pragma unroll
+    for (int k = 0; k < NV; ++k) nx[k] = gld4(px, 4 * c[k]);
+    if (p.y) {
+#pragma unroll
+      for (int k = 0; k < NV; ++k) ny[k].load(py, c[k]);
+    }
+  };
+  load(row);
+  while (row < last) {
+    const RowSegment sg = row_segment(p.cu, p.B, p.L, row, last);
+    const size_t m = size_t(2 * sg.s + sg.sigma) * p.mod_stride;
+    float4 fy[NV], fx[NV], b[NV];  // gate post, pre (1 + scale), shift
+    if (p.y) {
+      const Vector gate(p.gate, m, 1.f), post(sg.sigma ? p.post[1] : p.post[0], 0, 1.f);
+#pragma unroll
+      for (int k = 0; k < NV; ++k) fy[k] = mul4(gate(c[k]), post(c[k]));
+    }
+    if (p.h) {
+      const Vector scale(p.scale, m, 0.f), shift(p.shift, m, 0.f), pre(sg.sigma ? p.pre[1] : p.pre[0], 0, 1.f);
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        fx[k] = mul4(pre(c[k]), add4(scale(c[k]), 1.f));
+        b[k] = shift(c[k]);
+      }
+    }
+#pragma unroll 1
+    for (; row < sg.end; ++row) {
+      const size_t at = size_t(row) * p.D;
+      float4 x[NV], v[NV];
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        x[k] = only(in[k], nx[k]);
+        v[k] = only(in[k], ny[k].get());
+      }
+      if (row + 1 < last) load(row + 1);
+      float4 st = zero4();
+      if (p.y) {
+        const float2 t = row_stats<W, NV>(v, in, inv_d, p.rms, p.eps, sum);
+        st.x = t.x;
+        st.y = t.y;
+        const GlobalPtr px = global_ptr(p.x_out + at);
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+          const float4 u = mul4(fy[k], unit4(v[k], t.x, t.y));
+          x[k] = only(in[k], make_float4(p.alpha * x[k].x + u.x, p.alpha * x[k].y + u.y, p.alpha * x[k].z + u.z,
+                                         p.alpha * x[k].w + u.w));
+          if (in[k]) store4<false>(px, c[k], x[k]);
+        }
+      }
+      if (p.h) {
+        const float2 t = row_stats<W, NV>(x, in, inv_d, p.rms, p.eps, sum);
+        st.z = t.x;
+        st.w = t.y;
+        uint32_t top = 0;
+        const GlobalPtr ph = global_ptr(reinterpret_cast<char *>(p.h) + at * (OUT == 1 ? 1 : BF16 ? 2 : 4));
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+          x[k] = fma4(fx[k], unit4(x[k], t.x, t.y), b[k]);
+          if constexpr (OUT == 0) {
+            if (in[k]) store4<BF16>(ph, c[k], x[k]);
+          } else {
+            const uint32_t a = max(max(abs_bits(x[k].x), abs_bits(x[k].y)), max(abs_bits(x[k].z), abs_bits(x[k].w)));
+            top = max(top, in[k] ? a : 0u);
+          }
+        }
+        if constexpr (OUT == 1) {
+          top = wave_max_u32(top);
+          if constexpr (W > 1) {  // two sets in turn, as for the sums
+            turn ^= 1;
+            if ((threadIdx.x & 63) == 0) tops[turn][wave] = top;
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < W; ++i) top = max(top, tops[turn][i]);
+          }
+          const float inv = i8_inverse(top);
+          if (c0 == 0) p.h_scale[row] = i8_scale(top);
+          auto *o = (__attribute__((address_space(1))) char *)ph;
+#pragma unroll
+          for (int k = 0; k < NV; ++k)
+            if (in[k]) *(__attribute__((address_space(1))) uint32_t *)(o + c[k]) = i8x4(x[k].x, x[k].y, x[k].z, x[k].w, inv);
+        }
+      }
+      if (p.stats && c0 == 0) *reinterpret_cast<float4 *>(p.stats + 4 * size_t(row)) = st;
+    }
+  }
+}
+
+hipError_t launch_norm_residual(bool bf16, NormProblem p, hipStream_t st) {
   if (p.rows <= 0) return hipSuccess;
+  // workers: as many as the card holds at once
 #define HILO_NR(W, NV)                                                                                            \
   do {                                                                                                            \
-    const dim3 grid(W == 1 ? (unsigned(p.rows) + 3) / 4 : unsigned(p.rows)), block(W == 1 ? 256 : 64 * W);          \
+    constexpr int waves = 256 * 4 * norm_waves(NV);                                                                \
+    p.P = p.rows < waves / W ? p.rows : waves / W;                                                                 \
+    const dim3 grid(W == 1 ? (unsigned(p.P) + 3) / 4 : unsigned(p.P)), block(W == 1 ? 256 : 64 * W);                \
     if (p.h_scale) {                                                                                                \
       if (bf16) hipLaunchKernelGGL((k_norm_residual<true, 1, W, NV>), grid, block, 0, st, p);                       \
       else hipLaunchKernelGGL((k_norm_residual<false, 1, W, NV>), grid, block, 0, st, p);                           \
@@ -235,11 +305,14 @@ hipError_t launch_norm_residual(bool bf16, const NormProblem &p, hipStream_t st)
   } while (0)
   if (p.D <= 256) HILO_NR(1, 1);
   else if (p.D <= 512) HILO_NR(1, 2);
-  else if (p.D <= 1024) HILO_NR(1, 4);
+  else if (p.D <= 768) HILO_NR(1, 3);
+  else if (p.D <= 1024) HILO_NR(2, 2);
+  else if (p.D <= 1536) HILO_NR(2, 3);
   else if (p.D <= 2048) HILO_NR(4, 2);
   else if (p.D <= 3072) HILO_NR(4, 3);
-  else if (p.D <= 4096) HILO_NR(4, 4);
-  else HILO_NR(4, 8);
+  else if (p.D <= 4096) HILO_NR(8, 2);
+  else if (p.D <= 6144) HILO_NR(8, 3);
+  else HILO_NR(8, 4);
 #undef HILO_NR
   return hipGetLastError();
 }
@@ -251,20 +324,10 @@ hipError_t launch_norm_residual(bool bf16, const NormProblem &p, hipStream_t st)
 //   e = g gate post;  dy = r_y (e - mean(e) - yh mean(e yh))        (RMS: without the means of n and e)
 // and, summed over the rows of a (sample, stream):  A = sum g yh, B = sum dh xh, C = sum dh, from which
 //   dgate = post A;  dscale = pre B;  dshift = C;  dpost = sum over samples of gate A;  dpre = of (1 + scale) B.
-// A worker (W waves) takes a consecutive share of all rows and keeps A, B and C of the segment it is in in registers;
-// where the segment ends, and at its last row, it leaves them in a slot of its own.  Shares are never empty (no more
-// workers than rows), so (worker + segment) numbers the slots without gaps or collisions, and the sums are taken in
-// worker order by k_norm_sums: the same result every time, and no atomics.
-
-struct NormSlots {
-  int R, P;  // rows, workers that have rows
-};
-HILO_DEV NormSlots norm_slots(const int *cu, int B, int rows, int P) {
-  const int R = min(rows, cu_at(cu, B));
-  return NormSlots{R, min(P, R)};
-}
-HILO_DEV int norm_row0(const NormSlots &q, int w) { return int((long long)q.R * w / q.P); }
-HILO_DEV int norm_owner(const NormSlots &q, int row) { return int(((long long)(row + 1) * q.P - 1) / q.R); }
+// A worker takes a consecutive share of all rows and keeps A, B and C of the segment it is in in registers; where the
+// segment ends, and at its last row, it leaves them in a slot of its own.  As shares are never empty, (worker + segment)
+// numbers the slots without collisions, and the sums are taken in worker order by k_norm_sums: the same result every
+// time, and no atomics.
 
 // r (n - mean(n) - v mean(n v)) per value; without the mean of n for RMS (t.x taken as 0).
 HILO_DEV float4 through4(const float4 &n, const float4 &v, float2 t, float r) {
@@ -272,65 +335,73 @@ HILO_DEV float4 through4(const float4 &n, const float4 &v, float2 t, float r) {
                      r * (n.w - t.x - v.w * t.y));
 }
 
+// A worker is a workgroup: W > 1 waves that share a row, or (W = 1) four that take rows in turn and join their sums in
+// LDS where a segment ends, so that a slot holds four times the rows.
 template <bool BF16, int W, int NV>
 __global__ __launch_bounds__(W == 1 ? 256 : 64 * W, NV < 4 ? 3 : 2) void k_norm_residual_back(NormBackProblem p) {
+  constexpr int G = W == 1 ? 4 : 1;
   __shared__ float2 red[2 * W];
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int w = W == 1 ? blockIdx.x * 4 + wave : blockIdx.x;
-  const NormSlots q = norm_slots(p.cu, p.B, p.rows, p.P);
+  __shared__ float4 join[G == 1 ? 1 : G - 1][G == 1 ? 1 : 3 * NV][64];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), grp = W == 1 ? wave : 0;
+  const int w = blockIdx.x;
+  const NormShares q = norm_shares(p.cu, p.B, p.rows, p.P);
   if (w >= q.P) return;
-  const int c0 = 4 * (W == 1 ? threadIdx.x & 63 : threadIdx.x);
-  int c[NV];
+  const uint32_t c0 = 4 * (W == 1 ? threadIdx.x & 63 : threadIdx.x);
+  uint32_t c[NV];
   bool in[NV];
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
-    in[k] = c0 + k * 256 * W < p.D;
+    in[k] = c0 + k * 256 * W < uint32_t(p.D);
     c[k] = in[k] ? c0 + k * 256 * W : p.D - 4;
   }
   const float inv_d = 1.0f / float(p.D), center = p.rms ? 0.f : inv_d;
   GroupSum<W> sum{red};
-  const int last = norm_row0(q, w + 1);
-  int row = norm_row0(q, w);
-  while (row < last) {
-    const int s = sample_of_row(p.cu, p.B, row);
-    const int ts = cu_at(p.cu, s + 1) - p.L;
-    const int sigma = row >= ts ? 1 : 0, end = min(last, sigma ? ts + p.L : ts);
-    const size_t m = size_t(2 * s + sigma) * p.mod_stride;
-    const Vector gate(p.gate, m, 1.f), scale(p.scale, m, 0.f);
-    const Vector post(sigma ? p.post[1] : p.post[0], 0, 1.f), pre(sigma ? p.pre[1] : p.pre[0], 0, 1.f);
+  const int last = share_begin(q, w + 1);
+  int first = share_begin(q, w);
+  while (first < last) {
+    const RowSegment sg = row_segment(p.cu, p.B, p.L, first, last);
+    const size_t m = size_t(2 * sg.s + sg.sigma) * p.mod_stride;
     float4 fx[NV], fy[NV];  // (1 + scale) pre and gate post, zero behind the last column
     float4 A[NV], B[NV], C[NV];
+    {
+      const Vector gate(p.gate, m, 1.f), scale(p.scale, m, 0.f);
+      const Vector post(sg.sigma ? p.post[1] : p.post[0], 0, 1.f), pre(sg.sigma ? p.pre[1] : p.pre[0], 0, 1.f);
 #pragma unroll
-    for (int k = 0; k < NV; ++k) {
-      fx[k] = only(in[k], mul4(add4(scale(c[k]), 1.f), pre(c[k])));
-      fy[k] = only(in[k], mul4(gate(c[k]), post(c[k])));
-      A[k] = B[k] = C[k] = zero4();
+      for (int k = 0; k < NV; ++k) {
+        fx[k] = only(in[k], mul4(add4(scale(c[k]), 1.f), pre(c[k])));
+        fy[k] = only(in[k], mul4(gate(c[k]), post(c[k])));
+        A[k] = B[k] = C[k] = zero4();
+      }
     }
-    for (; row < end; ++row) {
+#pragma unroll 1
+    for (int row = first + grp; row < sg.end; row += G) {
       const size_t at = size_t(row) * p.D;
       float4 g[NV], x[NV];
       Raw4<BF16> dh[NV], y[NV];
+      const float4 st = gld4(global_ptr(p.stats + 4 * size_t(row)), 0);
       if (p.dh) {
+        const GlobalPtr pd = row_at<BF16>(p.dh, at), px = global_ptr(p.x_out + at);
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-          dh[k].load(p.dh, at + c[k]);
-          x[k] = ld4(p.x_out + at + c[k]);
+          dh[k].load(pd, c[k]);
+          x[k] = gld4(px, 4 * c[k]);
         }
       }
       if (p.dx_out) {
+        const GlobalPtr pg = global_ptr(p.dx_out + at);
 #pragma unroll
-        for (int k = 0; k < NV; ++k) g[k] = ld4(p.dx_out + at + c[k]);
+        for (int k = 0; k < NV; ++k) g[k] = gld4(pg, 4 * c[k]);
       } else {
 #pragma unroll
         for (int k = 0; k < NV; ++k) g[k] = zero4();
       }
       if (p.y) {
+        const GlobalPtr py = row_at<BF16>(p.y, at);
 #pragma unroll
-        for (int k = 0; k < NV; ++k) y[k].load(p.y, at + c[k]);
+        for (int k = 0; k < NV; ++k) y[k].load(py, c[k]);
       }
-      const float4 st = ld4(p.stats + 4 * size_t(row));
+      __builtin_amdgcn_sched_barrier(0);
       if (p.dh) {
-        float4 n[NV];
         float a = 0.f, b = 0.f;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
@@ -338,48 +409,72 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W, NV < 4 ? 3 : 2) void k_norm_
           x[k] = unit4(x[k], st.z, st.w);
           C[k] = add4(C[k], d);
           B[k] = fma4(d, x[k], B[k]);
-          n[k] = mul4(d, fx[k]);
-          a += sum4(n[k]);
-          b += dot4(n[k], x[k]);
+          const float4 n = mul4(d, fx[k]);
+          a += sum4(n);
+          b += dot4(n, x[k]);
         }
         float2 t = sum(a, b);
         t = make_float2(t.x * center, t.y * inv_d);
 #pragma unroll
-        for (int k = 0; k < NV; ++k) g[k] = add4(g[k], through4(n[k], x[k], t, st.w));
+        for (int k = 0; k < NV; ++k) g[k] = add4(g[k], through4(mul4(dh[k].get(), fx[k]), x[k], t, st.w));
       }
       if (p.y) {
-        float4 v[NV], e[NV];
         float a = 0.f, b = 0.f;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-          v[k] = unit4(y[k].get(), st.x, st.y);
-          A[k] = fma4(g[k], v[k], A[k]);
-          e[k] = mul4(g[k], fy[k]);
-          a += sum4(e[k]);
-          b += dot4(e[k], v[k]);
+          const float4 v = unit4(y[k].get(), st.x, st.y), e = mul4(g[k], fy[k]);
+          A[k] = fma4(g[k], v, A[k]);
+          a += sum4(e);
+          b += dot4(e, v);
         }
         float2 t = sum(a, b);
         t = make_float2(t.x * center, t.y * inv_d);
+        const GlobalPtr dy = row_at<BF16>(p.dy, at);
 #pragma unroll
         for (int k = 0; k < NV; ++k)
-          if (in[k]) store4<BF16>(p.dy, at + c[k], through4(e[k], v[k], t, st.y));
+          if (in[k]) store4<BF16>(dy, c[k], through4(mul4(g[k], fy[k]), unit4(y[k].get(), st.x, st.y), t, st.y));
       }
+      const GlobalPtr dx = global_ptr(p.dx + at);
 #pragma unroll
       for (int k = 0; k < NV; ++k)
         if (in[k])
-          *reinterpret_cast<float4 *>(p.dx + at + c[k]) =
-              make_float4(p.alpha * g[k].x, p.alpha * g[k].y, p.alpha * g[k].z, p.alpha * g[k].w);
+          store4<false>(dx, c[k], make_float4(p.alpha * g[k].x, p.alpha * g[k].y, p.alpha * g[k].z, p.alpha * g[k].w));
     }
     if (p.part) {
-      float *slot = p.part + size_t(w + 2 * s + sigma) * 3 * p.D;
+      if constexpr (G > 1) {
+        const int lane = threadIdx.x & 63;
+        if (grp > 0) {
+#pragma unroll
+          for (int k = 0; k < NV; ++k) {
+            join[grp - 1][k][lane] = A[k];
+            join[grp - 1][NV + k][lane] = B[k];
+            join[grp - 1][2 * NV + k][lane] = C[k];
+          }
+        }
+        __syncthreads();
+        if (grp == 0) {
+#pragma unroll
+          for (int i = 0; i < G - 1; ++i)
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+              A[k] = add4(A[k], join[i][k][lane]);
+              B[k] = add4(B[k], join[i][NV + k][lane]);
+              C[k] = add4(C[k], join[i][2 * NV + k][lane]);
+            }
+        }
+      }
+      float *slot = p.part + size_t(w + 2 * sg.s + sg.sigma) * 3 * p.D;
+      const GlobalPtr sa = global_ptr(slot), sb = global_ptr(slot + p.D), sc = global_ptr(slot + 2 * p.D);
 #pragma unroll
       for (int k = 0; k < NV; ++k)
-        if (in[k]) {
-          *reinterpret_cast<float4 *>(slot + c[k]) = A[k];
-          *reinterpret_cast<float4 *>(slot + p.D + c[k]) = B[k];
-          *reinterpret_cast<float4 *>(slot + 2 * p.D + c[k]) = C[k];
+        if (in[k] && grp == 0) {
+          store4<false>(sa, c[k], A[k]);
+          store4<false>(sb, c[k], B[k]);
+          store4<false>(sc, c[k], C[k]);
         }
+      if constexpr (G > 1) __syncthreads();  // the next segment's sums go to the same LDS
     }
+    first = sg.end;
   }
 }
 
@@ -389,14 +484,14 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W, NV < 4 ? 3 : 2) void k_norm_
 __global__ __launch_bounds__(256) void k_norm_sums(NormBackProblem p, float *sums, bool gains_here) {
   __shared__ float4 red[16][16];
   const int seg = blockIdx.x, s = seg >> 1, sigma = seg & 1, which = blockIdx.z;
-  const NormSlots q = norm_slots(p.cu, p.B, p.rows, p.P);
+  const NormShares q = norm_shares(p.cu, p.B, p.rows, p.P);
   const int lo = cu_at(p.cu, s), hi = cu_at(p.cu, s + 1), ts = hi - p.L;
   const int a = min(sigma ? ts : lo, q.R), b = min(sigma ? hi : ts, q.R);
   const int lane = threadIdx.x & 15, grp = threadIdx.x >> 4, c = blockIdx.y * 64 + 4 * lane;
   float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
   if (a < b && c < p.D) {
-    const int w1 = norm_owner(q, b - 1);
-    for (int w = norm_owner(q, a) + grp; w <= w1; w += 16) {
+    const int w1 = share_owner(q, b - 1);
+    for (int w = share_owner(q, a) + grp; w <= w1; w += 16) {
       const float4 t = ld4(p.part + (size_t(w + seg) * 3 + which) * p.D + c);
       v = make_float4(v.x + t.x, v.y + t.y, v.z + t.z, v.w + t.w);
     }
@@ -450,12 +545,10 @@ __global__ __launch_bounds__(256) void k_norm_gains(NormBackProblem p, const flo
   if (out[1]) out[1][c] = v[1];
 }
 
-static int norm_back_waves(int D) { return D <= 1024 ? 1 : D <= 4096 ? 4 : 8; }
-
-// Workers: about 8 rows each, so that their slots (12 bytes a column) are a small part of what they read, and no more
-// than fill the card.
+// Workers: eight rows each (W = 1: two a wave), so that their slots (24 bytes a column, written and read) are a small
+// part of what they read, and no more than the card holds at once.
 static int norm_back_workers(int rows, int D) {
-  const int most = norm_back_waves(D) == 1 ? 4096 : 1024, want = (rows + 7) / 8;
+  const int want = (rows + 7) / 8, most = D <= 768 ? 1024 : D <= 1536 ? 1536 : D <= 3072 ? 768 : 384;
   return want < 1 ? 1 : want < most ? want : most;
 }
 
@@ -469,16 +562,19 @@ hipError_t launch_norm_residual_back(bool bf16, NormBackProblem p, hipStream_t s
   if (p.rows > 0) {
 #define HILO_NB(W, NV)                                                                                     \
   do {                                                                                                     \
-    const dim3 grid(W == 1 ? unsigned(p.P + 3) / 4 : unsigned(p.P)), block(W == 1 ? 256 : 64 * W);          \
+    const dim3 grid{unsigned(p.P)}, block(W == 1 ? 256 : 64 * W);                                          \
     if (bf16) hipLaunchKernelGGL((k_norm_residual_back<true, W, NV>), grid, block, 0, st, p);              \
     else hipLaunchKernelGGL((k_norm_residual_back<false, W, NV>), grid, block, 0, st, p);                  \
   } while (0)
     if (p.D <= 256) HILO_NB(1, 1);
     else if (p.D <= 512) HILO_NB(1, 2);
-    else if (p.D <= 1024) HILO_NB(1, 4);
+    else if (p.D <= 768) HILO_NB(1, 3);
+    else if (p.D <= 1024) HILO_NB(2, 2);
+    else if (p.D <= 1536) HILO_NB(2, 3);
     else if (p.D <= 2048) HILO_NB(4, 2);
     else if (p.D <= 3072) HILO_NB(4, 3);
-    else if (p.D <= 4096) HILO_NB(4, 4);
+    else if (p.D <= 4096) HILO_NB(8, 2);
+    else if (p.D <= 6144) HILO_NB(8, 3);
     else HILO_NB(8, 4);
 #undef HILO_NB
     const hipError_t e = hipGetLastError();
