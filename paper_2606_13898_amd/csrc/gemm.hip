@@ -536,6 +536,110 @@ HILO_DEV void epilogue32_qk8(const GemmProblem &p, const TileRows &tr, int n0, i
   }
 }
 
+// int8 tiles: lane (lr, lg) of a wave holds row lr of each row block and, of the wave's columns, 16 consecutive ones (NB =
+// 4) or 4 of every 16 (NB = 3: a store writes 32 consecutive bytes of every row).
+// Four lanes of a row exchange their pieces, so that a store writes 64 consecutive bytes of every row (its pieces apart,
+// 16 bytes of every 32, cost more than the arithmetic: 8192 x 16384 x 3072, 8 tiles a CU, XXXX).
+HILO_DEV void swap16(uint32_t &a, uint32_t &b) {  // b's even rows of 16 lanes against a's odd ones
+  const auto r = __builtin_amdgcn_permlane16_swap(a, b, false, false);
+  a = r[0];
+  b = r[1];
+}
+HILO_DEV void swap32(uint32_t &a, uint32_t &b) {  // b's lower half against a's upper one
+  const auto r = __builtin_amdgcn_permlane32_swap(a, b, false, false);
+  a = r[0];
+  b = r[1];
+}
+
+template <typename G, int EPI, int OP>
+HILO_DEV void epilogue_i8(const GemmProblem &p, const TileRows &tr, int n0, int wm, int lane, const uint8_t *epi,
+                          i32x4 (&acc)[G::MB][G::NB]) {
+  constexpr int MB = G::MB, NB = G::NB, ESZ = OP == OP_I8_F32 ? 4 : 2;
+  constexpr int CS = NB == 4 ? 4 : 16;  // columns between blocks
+  const int lr = lane & 15, lg = lane >> 4, cl = (NB == 4 ? 16 : 4) * lg;
+  const bool biased = (tr.sigma ? p.bias[1] : p.bias[0]) != nullptr;
+  f32x4 s[NB], b[NB];
+#pragma unroll
+  for (int j = 0; j < NB; ++j) {
+    s[j] = *reinterpret_cast<const f32x4 *>(epi + G::kCol + 4 * (cl + CS * j));
+    if constexpr (ESZ == 4) {
+      b[j] = *reinterpret_cast<const f32x4 *>(epi + 4 * (cl + CS * j));
+    } else {
+      const uint2 u = *reinterpret_cast<const uint2 *>(epi + 2 * (cl + CS * j));
+      b[j] = f32x4{__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u), __uint_as_float(u.y << 16),
+                   __uint_as_float(u.y & 0xffff0000u)};
+    }
+    if (!biased) b[j] = f32x4(0.f);
+  }
+  // N % 4 == 0, so rows may start 8 (bf16) bytes off a multiple of 16: wide stores where they do not
+  const bool wide = NB == 4 && n0 + 16 * NB <= p.N && (ESZ == 4 || p.N % 8 == 0);
+  char *out = reinterpret_cast<char *>(p.out) + (size_t(tr.row0 + wm * 16 * MB) * p.N + n0) * ESZ;
+  const uint32_t row = uint32_t(lr) * uint32_t(p.N) * ESZ;  // below 2^30
+#pragma unroll
+  for (int i = 0; i < MB; ++i) {
+    const float sa = *reinterpret_cast<const float *>(epi + G::kRow + 4 * (16 * i + lr));
+    const bool in = wm * 16 * MB + 16 * i + lr < tr.nrows;
+    uint32_t o[NB][ESZ];  // four values of column block j
+#pragma unroll
+    for (int j = 0; j < NB; ++j) {
+      float v[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        v[e] = float(acc[i][j][e]) * (sa * s[j][e]) + b[j][e];
+        if constexpr (EPI == EPI_GELU) v[e] = gelu_tanh(v[e]);
+      }
+      if constexpr (ESZ == 4) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[j][e] = __float_as_uint(v[e]);
+      } else {
+        o[j][0] = pack_bf16x2(v[0], v[1]);
+        o[j][1] = pack_bf16x2(v[2], v[3]);
+      }
+    }
+    char *q = out + size_t(16 * i) * p.N * ESZ;
+    if (wide) {
+      if constexpr (NB == 4 && ESZ == 2) {
+        // pieces (lane group, half): a = (0, 0) (0, 1) (1, 0) (1, 1), b those of groups 2 and 3
+        uint32_t a[4] = {o[0][0], o[0][1], o[1][0], o[1][1]}, c[4] = {o[2][0], o[2][1], o[3][0], o[3][1]};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          swap16(a[e], c[e]);
+          swap32(a[e], c[e]);
+        }
+        if (in) {
+          *reinterpret_cast<uint4 *>(q + row + 16 * lg) = make_uint4(a[0], a[1], a[2], a[3]);
+          *reinterpret_cast<uint4 *>(q + row + 64 + 16 * lg) = make_uint4(c[0], c[1], c[2], c[3]);
+        }
+      }
+      if constexpr (NB == 4 && ESZ == 4) {
+        // 4 x 4 pieces of lane groups and column blocks, transposed
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          swap16(o[0][e], o[1][e]);
+          swap16(o[2][e], o[3][e]);
+          swap32(o[0][e], o[2][e]);
+          swap32(o[1][e], o[3][e]);
+        }
+        if (in) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            *reinterpret_cast<uint4 *>(q + row + 64 * j + 16 * lg) = make_uint4(o[j][0], o[j][1], o[j][2], o[j][3]);
+        }
+      }
+    } else if (in) {
+#pragma unroll
+      for (int j = 0; j < NB; ++j) {
+        if (n0 + cl + CS * j < p.N) {
+          char *d = q + row + (cl + CS * j) * ESZ;
+          if constexpr (ESZ == 4) *reinterpret_cast<uint4 *>(d) = make_uint4(o[j][0], o[j][1], o[j][2], o[j][3]);
+          else *reinterpret_cast<uint2 *>(d) = make_uint2(o[j][0], o[j][1]);
+        }
+      }
+    }
+    asm volatile("" ::: "memory");  // the next block's operands stay below these stores
+  }
+}
+
 // All work items of this workgroup under plan q on BM x BN tiles.
 template <int BM, int BN, int EPI, int OP = OP_BF16>
 HILO_DEV void gemm8_run(const GemmProblem &p, const SkPlan &q, int pid, uint8_t *lds) {
@@ -543,7 +647,8 @@ HILO_DEV void gemm8_run(const GemmProblem &p, const SkPlan &q, int pid, uint8_t 
   using G = Geo<BM, BN, OP>;
   constexpr bool F8 = G::F8, I8 = op_i8(OP);
   constexpr bool B32 = G::B32;
-  using T = SkTile<BM, BN, G::WM, G::WN, !B32>;
+  constexpr bool CONTIG = !B32 && !(I8 && G::NB == 3);
+  using T = SkTile<BM, BN, G::WM, G::WN, CONTIG>;
   constexpr int MB = G::MB, NB = G::NB, LA = G::LA, LB = G::LB, WB = G::WB, S = G::SLOTS;
   constexpr int WM = G::WM, WN = G::WN, ESZ = F8 ? 1 : 2;  // ESZ: operand bytes per element
   const int lane = threadIdx.x & 63;
@@ -620,7 +725,7 @@ HILO_DEV void gemm8_run(const GemmProblem &p, const SkPlan &q, int pid, uint8_t 
   // ---- fragments, in chunks of 16 bytes.  bf16: lane (lr, lg) holds chunk 4 h + lg of row lr of a 16-row
   // block in half h.  FP8, 16 x 16 blocks: both of these at once, for one 128-deep MFMA.  FP8, 32 x 32
   // blocks: chunks 4 h + g and 4 h + 2 + g (g = lane / 32) of row lane % 32 for one 64-deep MFMA of half h.
-  // W rows of 16 x 16 blocks go in the order that gives the lane's accumulators 4 NB consecutive columns:
+  // W rows of 16 x 16 blocks go in the order that gives the lane's accumulators 4 NB consecutive columns (CONTIG):
   // MFMA output row 4 g + e of block j is column 4 NB g + 4 j + e of the wave
   constexpr bool INP = OP == OP_FP8 && !B32;
   constexpr int NC = OP == OP_FP8 ? 2 : 1;             // chunks of a fragment
@@ -641,7 +746,7 @@ HILO_DEV void gemm8_run(const GemmProblem &p, const SkPlan &q, int pid, uint8_t 
       fa[h] = lds0 + (wm * (BM / WM) + lr) * 128 + (((4 * h + lg) ^ swz<B32>(lr)) * 16);
 #pragma unroll
       for (int j = 0; j < NB; ++j) {
-        const int r = wn * (BN / WN) + (lr >> 2) * 4 * NB + 4 * j + (lr & 3);
+        const int r = wn * (BN / WN) + (CONTIG ? (lr >> 2) * 4 * NB + 4 * j + (lr & 3) : 16 * j + lr);
         fb[j][h] = lds0 + (BM + r) * 128 + (((4 * h + lg) ^ swz<B32>(r)) * 16);
       }
     }
@@ -865,20 +970,16 @@ HILO_DEV void gemm8_run(const GemmProblem &p, const SkPlan &q, int pid, uint8_t 
                                                                   lr + 16 * c)) =
                   f32x4{acc[i][j][4 * c], acc[i][j][4 * c + 1], acc[i][j][4 * c + 2], acc[i][j][4 * c + 3]};
       }
+    } else if (I8 && whole) {
+      if constexpr (I8) epilogue_i8<G, EPI, OP>(p, etr, en0, wm, lane, epi, acc);
     } else if (whole) {
+     if constexpr (!I8) {
       uint2 bu[NB];
-      f32x4 bf[OP == OP_I8_F32 ? NB : 1];
-      const bool biased = !I8 || (etr.sigma ? p.bias[1] : p.bias[0]) != nullptr;
       f32x4 wsc[F8 ? NB : 1];
       f32x4 gv[NB];
 #pragma unroll
       for (int j = 0; j < NB; ++j) {
-        if constexpr (OP == OP_I8_F32) bf[j] = *reinterpret_cast<const f32x4 *>(epi + 4 * (4 * NB * lg + 4 * j));
-        else bu[j] = *reinterpret_cast<const uint2 *>(epi + 2 * (4 * NB * lg + 4 * j));
-        if (I8 && !biased) {
-          if constexpr (OP == OP_I8_F32) bf[j] = f32x4(0.f);
-          else bu[j] = make_uint2(0u, 0u);
-        }
+        bu[j] = *reinterpret_cast<const uint2 *>(epi + 2 * (4 * NB * lg + 4 * j));
         if constexpr (EPI == EPI_RESID) gv[j] = *reinterpret_cast<const f32x4 *>(epi + G::kGate + 4 * (4 * NB * lg + 4 * j));
         if constexpr (F8) wsc[j] = *reinterpret_cast<const f32x4 *>(epi + G::kCol + 4 * (4 * NB * lg + 4 * j));
       }
@@ -924,23 +1025,16 @@ HILO_DEV void gemm8_run(const GemmProblem &p, const SkPlan &q, int pid, uint8_t 
           if (rl < etr.nrows) {
             const size_t m = size_t(etr.row0 + rl);
             uint2 o[NB];
-            float4 of[OP == OP_I8_F32 ? NB : 1];
             float sa;
             if constexpr (F8) sa = *reinterpret_cast<const float *>(epi + G::kRow + 4 * (16 * i + lr));
 #pragma unroll
             for (int j = 0; j < NB; ++j) {
               float v[4];
-              float bv[4];
-              if constexpr (OP == OP_I8_F32) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) bv[e] = bf[j][e];
-              } else {
-                bv[0] = __uint_as_float(bu[j].x << 16); bv[1] = __uint_as_float(bu[j].x & 0xffff0000u);
-                bv[2] = __uint_as_float(bu[j].y << 16); bv[3] = __uint_as_float(bu[j].y & 0xffff0000u);
-              }
+              const float bv[4] = {__uint_as_float(bu[j].x << 16), __uint_as_float(bu[j].x & 0xffff0000u),
+                                   __uint_as_float(bu[j].y << 16), __uint_as_float(bu[j].y & 0xffff0000u)};
 #pragma unroll
               for (int e = 0; e < 4; ++e) {
-                if constexpr (F8) v[e] = float(acc[i][j][e]) * (sa * wsc[j][e]) + bv[e];
+                if constexpr (F8) v[e] = acc[i][j][e] * (sa * wsc[j][e]) + bv[e];
                 else v[e] = acc[i][j][e] + bv[e];
               }
               if constexpr (EPI == EPI_RESID) {
@@ -953,22 +1047,14 @@ HILO_DEV void gemm8_run(const GemmProblem &p, const SkPlan &q, int pid, uint8_t 
 #pragma unroll
                   for (int e = 0; e < 4; ++e) v[e] = gelu_tanh(v[e]);
                 }
-                if constexpr (OP == OP_I8_F32) of[j] = make_float4(v[0], v[1], v[2], v[3]);
-                else o[j] = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+                o[j] = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
               }
             }
             if constexpr (EPI != EPI_RESID) {
-              if constexpr (OP == OP_I8_F32) {
-                float *op = reinterpret_cast<float *>(p.out) + m * p.ldo + nc;
+              uint16_t *op = reinterpret_cast<uint16_t *>(p.out) + m * p.ldo + nc;
 #pragma unroll
-                for (int j = 0; j < NB; ++j)
-                  if (nc + 4 * j < p.N) *reinterpret_cast<float4 *>(op + 4 * j) = of[j];
-              } else {
-                uint16_t *op = reinterpret_cast<uint16_t *>(p.out) + m * p.ldo + nc;
-#pragma unroll
-                for (int j = 0; j < NB; ++j)
-                  if (nc + 4 * j < p.N) *reinterpret_cast<uint2 *>(op + 4 * j) = o[j];
-              }
+              for (int j = 0; j < NB; ++j)
+                if (nc + 4 * j < p.N) *reinterpret_cast<uint2 *>(op + 4 * j) = o[j];
             }
           }
         }
@@ -977,6 +1063,7 @@ HILO_DEV void gemm8_run(const GemmProblem &p, const SkPlan &q, int pid, uint8_t 
           if (i0 + ZS * ZR < MB) ld_z(i0 / ZR % ZS, i0 + ZS * ZR);
         }
       }
+     }
     } else {
       float *slot = cur.slot;
 #pragma unroll
@@ -1304,7 +1391,7 @@ template <int EPI, int OP>
 __global__ __launch_bounds__(kFixThreads) void k_linear_i8_fix(GemmProblem p) {
   int rows;
   if (choose_tile_i8<EPI>(p, rows) == TILE_256) gemm_fix<256, 256, 2, 4, true, EPI, OP>(p, sk_plan(p, rows, 256, 128, (p.K + 127) / 128));
-  else gemm_fix<192, 192, 2, 4, true, EPI, OP>(p, sk_plan(p, rows, 192, 128, (p.K + 127) / 128));
+  else gemm_fix<192, 192, 2, 4, false, EPI, OP>(p, sk_plan(p, rows, 192, 128, (p.K + 127) / 128));
 }
 
 // ------------------------------------------------------------------------------- fp32 path
