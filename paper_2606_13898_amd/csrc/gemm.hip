@@ -222,15 +222,24 @@ HILO_DEV SkItem sk_next_item(SkCursor &c, const SkPlan &q, const SkRange &rg, in
 
 // Partial tiles of a BM x BN tile on WM x WN waves, in the 16 x 16 fragment order the fixup
 // reads, and the fixup's epilogue of one fragment row.
-// CONTIG: a lane's columns of all fragment columns are consecutive (16 x 16 blocks), instead of 4 of every 16
-// (the 32 x 32 blocks of the FP8 QKV projection).
-template <int BM, int BN, int WM, int WN, bool CONTIG = false>
+// ORDER: which columns of the wave's 16 TN lane group g (lane / 16) holds in fragment column j, four from
+//   NATURAL  16 j + 4 g (the 32 x 32 blocks of the FP8 QKV projection; float32 rows of int8 products: a store of 16
+//            bytes a lane writes 64 consecutive bytes of every row)
+//   CONTIG   4 TN g + 4 j: a lane's columns are consecutive
+//   PAIRED   fragment columns in pairs, 8 columns a lane of every 32, and a last odd one as NATURAL (bf16 rows of int8
+//            products: a pair is a store of 16 bytes a lane, 64 consecutive bytes of every row)
+enum ColOrder { COLS_NATURAL, COLS_CONTIG, COLS_PAIRED };
+template <int TN>
+HILO_DEV constexpr int col_of(int order, int g, int j) {
+  if (order == COLS_NATURAL) return 16 * j + 4 * g;
+  if (order == COLS_CONTIG) return 4 * TN * g + 4 * j;
+  return (j | 1) < TN ? 32 * (j / 2) + 8 * g + 4 * (j & 1) : 16 * j + 4 * g;
+}
+template <int BM, int BN, int WM, int WN, int ORDER = COLS_NATURAL>
 struct SkTile {
   static constexpr int NW = WM * WN;
   static constexpr int TM = BM / WM / 16;
   static constexpr int TN = BN / WN / 16;
-  static constexpr int CS = CONTIG ? 4 : 16;       // columns between fragment columns
-  static constexpr int CL = CONTIG ? 4 * TN : 4;   // columns between the lane groups
   static constexpr size_t kPartFloats = size_t(BM) * BN;
 
   // partial-sum slot layout: register order, one float4 per lane per (wave, i, j)
@@ -293,7 +302,7 @@ struct SkTile {
                                     const V (&acc)[TN]) {
     constexpr bool F8 = op_scaled(OP);
     const int rl = (wid / WN) * (BM / WM) + i0 * 16 + (lane & 15);
-    const int cbase = n0 + (wid % WN) * (BN / WN) + CL * (lane >> 4);
+    const int cbase = n0 + (wid % WN) * (BN / WN);
     const size_t m = size_t(tr.row0 + min(rl, tr.nrows - 1));
     const uint16_t *bias = reinterpret_cast<const uint16_t *>(p.bias[tr.sigma]);
     float bv[TN][4];
@@ -301,7 +310,7 @@ struct SkTile {
     float asc;
 #pragma unroll
     for (int j = 0; j < TN; ++j) {
-      const int nc = min(cbase + j * CS, p.N - 4);
+      const int nc = min(cbase + col_of<TN>(ORDER, lane >> 4, j), p.N - 4);
       if (op_i8(OP) && !bias) {
         bv[j][0] = bv[j][1] = bv[j][2] = bv[j][3] = 0.f;
       } else if constexpr (OP == OP_I8_F32) {
@@ -322,7 +331,7 @@ struct SkTile {
     if (rl >= tr.nrows) return;
 #pragma unroll
     for (int j = 0; j < TN; ++j) {
-      const int n = cbase + j * CS;
+      const int n = cbase + col_of<TN>(ORDER, lane >> 4, j);
       if (n >= p.N) continue;
       float v[4];
       if constexpr (F8) {
@@ -404,6 +413,7 @@ struct Geo {
   static constexpr bool B32 = OP == OP_FP8 && BN == 256;
   static constexpr int WN = B32 ? 2 : 4, WM = 8 / WN;
   static constexpr int MB = BM / WM / (B32 ? 32 : 16), NB = BN / WN / (B32 ? 32 : 16);
+  static constexpr int ORDER = B32 || OP == OP_I8_F32 ? COLS_NATURAL : OP == OP_I8 ? COLS_PAIRED : COLS_CONTIG;
   static constexpr int LA = BM / 64, LB = BN / 64;  // load instructions per wave and window
   static constexpr int WB = (BM + BN) * 128;        // bytes of a window
   static constexpr int KW = F8 ? 128 : 64;          // values of K in a window
@@ -536,108 +546,77 @@ HILO_DEV void epilogue32_qk8(const GemmProblem &p, const TileRows &tr, int n0, i
   }
 }
 
-// int8 tiles: lane (lr, lg) of a wave holds row lr of each row block and, of the wave's columns, 16 consecutive ones (NB =
-// 4) or 4 of every 16 (NB = 3: a store writes 32 consecutive bytes of every row).
-// Four lanes of a row exchange their pieces, so that a store writes 64 consecutive bytes of every row (its pieces apart,
-// 16 bytes of every 32, cost more than the arithmetic: 8192 x 16384 x 3072, 8 tiles a CU, XXXX).
-HILO_DEV void swap16(uint32_t &a, uint32_t &b) {  // b's even rows of 16 lanes against a's odd ones
-  const auto r = __builtin_amdgcn_permlane16_swap(a, b, false, false);
-  a = r[0];
-  b = r[1];
-}
-HILO_DEV void swap32(uint32_t &a, uint32_t &b) {  // b's lower half against a's upper one
-  const auto r = __builtin_amdgcn_permlane32_swap(a, b, false, false);
-  a = r[0];
-  b = r[1];
-}
-
+// int8 tiles: lane (lr, lg) of a wave holds row lr of each row block and the columns col_of(lg, j).  A store instruction
+// writes 64 consecutive bytes of 16 rows; pieces of 8 bytes 24 or 32 apart, a lane's columns all consecutive, took
+// longer than the arithmetic (8192 x 16384 x 3072, eight 256 x 256 tiles a CU: 364 us, 344 with whole pieces; without
+// stores 322).
 template <typename G, int EPI, int OP>
 HILO_DEV void epilogue_i8(const GemmProblem &p, const TileRows &tr, int n0, int wm, int lane, const uint8_t *epi,
                           i32x4 (&acc)[G::MB][G::NB]) {
   constexpr int MB = G::MB, NB = G::NB, ESZ = OP == OP_I8_F32 ? 4 : 2;
-  constexpr int CS = NB == 4 ? 4 : 16;  // columns between blocks
-  const int lr = lane & 15, lg = lane >> 4, cl = (NB == 4 ? 16 : 4) * lg;
+  const int lr = lane & 15, lg = lane >> 4;
   const bool biased = (tr.sigma ? p.bias[1] : p.bias[0]) != nullptr;
   f32x4 s[NB], b[NB];
 #pragma unroll
   for (int j = 0; j < NB; ++j) {
-    s[j] = *reinterpret_cast<const f32x4 *>(epi + G::kCol + 4 * (cl + CS * j));
+    const int c = col_of<NB>(G::ORDER, lg, j);
+    s[j] = *reinterpret_cast<const f32x4 *>(epi + G::kCol + 4 * c);
     if constexpr (ESZ == 4) {
-      b[j] = *reinterpret_cast<const f32x4 *>(epi + 4 * (cl + CS * j));
+      b[j] = *reinterpret_cast<const f32x4 *>(epi + 4 * c);
     } else {
-      const uint2 u = *reinterpret_cast<const uint2 *>(epi + 2 * (cl + CS * j));
+      const uint2 u = *reinterpret_cast<const uint2 *>(epi + 2 * c);
       b[j] = f32x4{__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u), __uint_as_float(u.y << 16),
                    __uint_as_float(u.y & 0xffff0000u)};
     }
     if (!biased) b[j] = f32x4(0.f);
   }
-  // N % 4 == 0, so rows may start 8 (bf16) bytes off a multiple of 16: wide stores where they do not
-  const bool wide = NB == 4 && n0 + 16 * NB <= p.N && (ESZ == 4 || p.N % 8 == 0);
   char *out = reinterpret_cast<char *>(p.out) + (size_t(tr.row0 + wm * 16 * MB) * p.N + n0) * ESZ;
   const uint32_t row = uint32_t(lr) * uint32_t(p.N) * ESZ;  // below 2^30
+  // INSIDE: all of the wave's rows and columns exist, and rows start at multiples of 16 bytes (N % 4 == 0 alone leaves
+  // bf16 rows 8 off)
+  auto rows = [&](auto inside) __attribute__((always_inline)) {
+    constexpr bool INSIDE = decltype(inside)::value;
 #pragma unroll
-  for (int i = 0; i < MB; ++i) {
-    const float sa = *reinterpret_cast<const float *>(epi + G::kRow + 4 * (16 * i + lr));
-    const bool in = wm * 16 * MB + 16 * i + lr < tr.nrows;
-    uint32_t o[NB][ESZ];  // four values of column block j
-#pragma unroll
-    for (int j = 0; j < NB; ++j) {
-      float v[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        v[e] = float(acc[i][j][e]) * (sa * s[j][e]) + b[j][e];
-        if constexpr (EPI == EPI_GELU) v[e] = gelu_tanh(v[e]);
-      }
-      if constexpr (ESZ == 4) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[j][e] = __float_as_uint(v[e]);
-      } else {
-        o[j][0] = pack_bf16x2(v[0], v[1]);
-        o[j][1] = pack_bf16x2(v[2], v[3]);
-      }
-    }
-    char *q = out + size_t(16 * i) * p.N * ESZ;
-    if (wide) {
-      if constexpr (NB == 4 && ESZ == 2) {
-        // pieces (lane group, half): a = (0, 0) (0, 1) (1, 0) (1, 1), b those of groups 2 and 3
-        uint32_t a[4] = {o[0][0], o[0][1], o[1][0], o[1][1]}, c[4] = {o[2][0], o[2][1], o[3][0], o[3][1]};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          swap16(a[e], c[e]);
-          swap32(a[e], c[e]);
-        }
-        if (in) {
-          *reinterpret_cast<uint4 *>(q + row + 16 * lg) = make_uint4(a[0], a[1], a[2], a[3]);
-          *reinterpret_cast<uint4 *>(q + row + 64 + 16 * lg) = make_uint4(c[0], c[1], c[2], c[3]);
-        }
-      }
-      if constexpr (NB == 4 && ESZ == 4) {
-        // 4 x 4 pieces of lane groups and column blocks, transposed
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          swap16(o[0][e], o[1][e]);
-          swap16(o[2][e], o[3][e]);
-          swap32(o[0][e], o[2][e]);
-          swap32(o[1][e], o[3][e]);
-        }
-        if (in) {
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-            *reinterpret_cast<uint4 *>(q + row + 64 * j + 16 * lg) = make_uint4(o[j][0], o[j][1], o[j][2], o[j][3]);
-        }
-      }
-    } else if (in) {
+    for (int i = 0; i < MB; ++i) {
+      const float sa = *reinterpret_cast<const float *>(epi + G::kRow + 4 * (16 * i + lr));
+      uint32_t o[NB][ESZ];  // four values of column block j
 #pragma unroll
       for (int j = 0; j < NB; ++j) {
-        if (n0 + cl + CS * j < p.N) {
-          char *d = q + row + (cl + CS * j) * ESZ;
-          if constexpr (ESZ == 4) *reinterpret_cast<uint4 *>(d) = make_uint4(o[j][0], o[j][1], o[j][2], o[j][3]);
-          else *reinterpret_cast<uint2 *>(d) = make_uint2(o[j][0], o[j][1]);
+        float v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          v[e] = float(acc[i][j][e]) * (sa * s[j][e]) + b[j][e];
+          if constexpr (EPI == EPI_GELU) v[e] = gelu_tanh(v[e]);
+        }
+        if constexpr (ESZ == 4) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[j][e] = __float_as_uint(v[e]);
+        } else {
+          o[j][0] = pack_bf16x2(v[0], v[1]);
+          o[j][1] = pack_bf16x2(v[2], v[3]);
         }
       }
+      char *q = out + size_t(16 * i) * p.N * ESZ;
+      if (INSIDE || wm * 16 * MB + 16 * i + lr < tr.nrows) {
+#pragma unroll
+        for (int j = 0; j < NB; ++j) {
+          const int c = col_of<NB>(G::ORDER, lg, j);
+          char *d = q + row + c * ESZ;
+          if (!INSIDE && n0 + c >= p.N) continue;
+          if constexpr (ESZ == 4) {
+            *reinterpret_cast<uint4 *>(d) = make_uint4(o[j][0], o[j][1], o[j][2], o[j][3]);
+          } else if (INSIDE && (j | 1) < NB) {
+            if (j % 2 == 0) *reinterpret_cast<uint4 *>(d) = make_uint4(o[j][0], o[j][1], o[j | 1][0], o[j | 1][1]);
+          } else {
+            *reinterpret_cast<uint2 *>(d) = make_uint2(o[j][0], o[j][1]);
+          }
+        }
+      }
+      asm volatile("" ::: "memory");  // the next block's operands stay below these stores
     }
-    asm volatile("" ::: "memory");  // the next block's operands stay below these stores
-  }
+  };
+  if (uni(int((wm + 1) * 16 * MB <= tr.nrows && n0 + 16 * NB <= p.N && p.N % 8 == 0))) rows(std::true_type{});
+  else rows(std::false_type{});
 }
 
 // All work items of this workgroup under plan q on BM x BN tiles.
@@ -647,8 +626,8 @@ HILO_DEV void gemm8_run(const GemmProblem &p, const SkPlan &q, int pid, uint8_t 
   using G = Geo<BM, BN, OP>;
   constexpr bool F8 = G::F8, I8 = op_i8(OP);
   constexpr bool B32 = G::B32;
-  constexpr bool CONTIG = !B32 && !(I8 && G::NB == 3);
-  using T = SkTile<BM, BN, G::WM, G::WN, CONTIG>;
+  constexpr int ORDER = G::ORDER;
+  using T = SkTile<BM, BN, G::WM, G::WN, ORDER>;
   constexpr int MB = G::MB, NB = G::NB, LA = G::LA, LB = G::LB, WB = G::WB, S = G::SLOTS;
   constexpr int WM = G::WM, WN = G::WN, ESZ = F8 ? 1 : 2;  // ESZ: operand bytes per element
   const int lane = threadIdx.x & 63;
@@ -725,8 +704,8 @@ HILO_DEV void gemm8_run(const GemmProblem &p, const SkPlan &q, int pid, uint8_t 
   // ---- fragments, in chunks of 16 bytes.  bf16: lane (lr, lg) holds chunk 4 h + lg of row lr of a 16-row
   // block in half h.  FP8, 16 x 16 blocks: both of these at once, for one 128-deep MFMA.  FP8, 32 x 32
   // blocks: chunks 4 h + g and 4 h + 2 + g (g = lane / 32) of row lane % 32 for one 64-deep MFMA of half h.
-  // W rows of 16 x 16 blocks go in the order that gives the lane's accumulators 4 NB consecutive columns (CONTIG):
-  // MFMA output row 4 g + e of block j is column 4 NB g + 4 j + e of the wave
+  // W rows of 16 x 16 blocks go in the order that gives the lane's accumulators the columns they are to have:
+  // MFMA output row 4 g + e of block j is column col_of(g, j) + e of the wave
   constexpr bool INP = OP == OP_FP8 && !B32;
   constexpr int NC = OP == OP_FP8 ? 2 : 1;             // chunks of a fragment
   constexpr int NR = (MB + NB) * NC;                   // reads of a set: W first, then A
@@ -746,7 +725,7 @@ HILO_DEV void gemm8_run(const GemmProblem &p, const SkPlan &q, int pid, uint8_t 
       fa[h] = lds0 + (wm * (BM / WM) + lr) * 128 + (((4 * h + lg) ^ swz<B32>(lr)) * 16);
 #pragma unroll
       for (int j = 0; j < NB; ++j) {
-        const int r = wn * (BN / WN) + (CONTIG ? (lr >> 2) * 4 * NB + 4 * j + (lr & 3) : 16 * j + lr);
+        const int r = wn * (BN / WN) + col_of<NB>(ORDER, lr >> 2, j) + (lr & 3);
         fb[j][h] = lds0 + (BM + r) * 128 + (((4 * h + lg) ^ swz<B32>(r)) * 16);
       }
     }
@@ -1254,11 +1233,11 @@ __global__ __launch_bounds__(512, 2) void k_gemm8(GemmProblem p) {
 constexpr int kFixThreads = 512;
 constexpr int kFixBatch = 4;
 
-template <int BM, int BN, int WM, int WN, bool CONTIG, int EPI, int OP>
+template <typename G, int BM, int BN, int EPI, int OP>
 HILO_DEV void gemm_fix(const GemmProblem &p, const SkPlan &q) {
   constexpr int P = kGemmWorkgroups;
   if (q.s == 1 && q.I == 0) return;  // every tile was finished by the main kernel
-  using T = SkTile<BM, BN, WM, WN, CONTIG>;
+  using T = SkTile<BM, BN, G::WM, G::WN, G::ORDER>;
   constexpr int TM = T::TM, TN = T::TN, NW = T::NW, FW = kFixThreads / 64;
   const int nfix = q.s > 1 ? q.T : q.U - q.dp;
   const int lane = threadIdx.x & 63;
@@ -1342,16 +1321,15 @@ HILO_DEV void gemm_fix(const GemmProblem &p, const SkPlan &q) {
 
 template <int BM, int BN, int EPI, int ROLE>
 __global__ __launch_bounds__(kFixThreads) void k_gemm8_fp8_fix(GemmProblem p) {
-  using G = g8::Geo<BM, BN, OP_FP8>;
-  gemm_fix<BM, BN, G::WM, G::WN, !G::B32, EPI, OP_FP8>(p, sk_plan(p, row_tiles_total(p, BM), BN, 128));
+  gemm_fix<g8::Geo<BM, BN, OP_FP8>, BM, BN, EPI, OP_FP8>(p, sk_plan(p, row_tiles_total(p, BM), BN, 128));
 }
 
 template <int EPI, int ROLE>
 __global__ __launch_bounds__(kFixThreads) void k_gemm8_fix(GemmProblem p) {
   int rows;
   const Tile t = choose_tile<EPI>(p, rows);
-  if (t == TILE_256) gemm_fix<256, 256, 2, 4, true, EPI, OP_BF16>(p, sk_plan(p, rows, 256));
-  else if (t == TILE_192) gemm_fix<192, 192, 2, 4, true, EPI, OP_BF16>(p, sk_plan(p, rows, 192));
+  if (t == TILE_256) gemm_fix<g8::Geo<256, 256>, 256, 256, EPI, OP_BF16>(p, sk_plan(p, rows, 256));
+  else if (t == TILE_192) gemm_fix<g8::Geo<192, 192>, 192, 192, EPI, OP_BF16>(p, sk_plan(p, rows, 192));
 }
 
 // ------------------------------------------------------------------------------- int8 products
@@ -1390,8 +1368,8 @@ __global__ __launch_bounds__(512, 2) void k_linear_i8(GemmProblem p) {
 template <int EPI, int OP>
 __global__ __launch_bounds__(kFixThreads) void k_linear_i8_fix(GemmProblem p) {
   int rows;
-  if (choose_tile_i8<EPI>(p, rows) == TILE_256) gemm_fix<256, 256, 2, 4, true, EPI, OP>(p, sk_plan(p, rows, 256, 128, (p.K + 127) / 128));
-  else gemm_fix<192, 192, 2, 4, false, EPI, OP>(p, sk_plan(p, rows, 192, 128, (p.K + 127) / 128));
+  if (choose_tile_i8<EPI>(p, rows) == TILE_256) gemm_fix<g8::Geo<256, 256, OP>, 256, 256, EPI, OP>(p, sk_plan(p, rows, 256, 128, (p.K + 127) / 128));
+  else gemm_fix<g8::Geo<192, 192, OP>, 192, 192, EPI, OP>(p, sk_plan(p, rows, 192, 128, (p.K + 127) / 128));
 }
 
 // ------------------------------------------------------------------------------- fp32 path
