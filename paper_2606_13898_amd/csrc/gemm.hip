@@ -119,15 +119,16 @@ HILO_DEV bool runs_whole(int T, int nk) {
   return (T < P && nk <= kNoSplitSteps) || whole_waves || full_wave;
 }
 
-// The plan of R row tiles of the problem on BN-column tiles, K in steps of kstep (nk of them, where K is no multiple).
-HILO_DEV SkPlan sk_plan(const GemmProblem &p, int R, int BN, int kstep = 64, int nk = 0) {
+// The plan of R row tiles of the problem on BN-column tiles, K in steps of kstep (nk of them, where K is no multiple);
+// without tails, P tiles or more run whole.
+HILO_DEV SkPlan sk_plan(const GemmProblem &p, int R, int BN, int kstep = 64, int nk = 0, bool tails = true) {
   constexpr int P = kGemmWorkgroups;
   SkPlan q;
   q.R = R;
   q.TN = (p.N + BN - 1) / BN;
   q.T = q.R * q.TN;
   q.nk = nk ? nk : p.K / kstep;
-  if (runs_whole(q.T, q.nk)) {
+  if (runs_whole(q.T, q.nk) || (!tails && q.T >= P)) {
     q.s = 1;
     q.U = q.dp = q.T;
     q.len = q.nk;
@@ -550,8 +551,11 @@ HILO_DEV void epilogue32_qk8(const GemmProblem &p, const TileRows &tr, int n0, i
 // writes 64 consecutive bytes of 16 rows; pieces of 8 bytes 24 or 32 apart, a lane's columns all consecutive, took
 // longer than the arithmetic (8192 x 16384 x 3072, eight 256 x 256 tiles a CU: 364 us, 344 with whole pieces; without
 // stores 322).
+// Returns whether all of the wave's stores were issued, kStoresI8 of them.
+template <typename G, int OP>
+constexpr int kStoresI8 = G::MB * (OP == OP_I8_F32 ? G::NB : (G::NB + 1) / 2);
 template <typename G, int EPI, int OP>
-HILO_DEV void epilogue_i8(const GemmProblem &p, const TileRows &tr, int n0, int wm, int lane, const uint8_t *epi,
+HILO_DEV bool epilogue_i8(const GemmProblem &p, const TileRows &tr, int n0, int wm, int lane, const uint8_t *epi,
                           i32x4 (&acc)[G::MB][G::NB]) {
   constexpr int MB = G::MB, NB = G::NB, ESZ = OP == OP_I8_F32 ? 4 : 2;
   const int lr = lane & 15, lg = lane >> 4;
@@ -615,8 +619,10 @@ HILO_DEV void epilogue_i8(const GemmProblem &p, const TileRows &tr, int n0, int 
       asm volatile("" ::: "memory");  // the next block's operands stay below these stores
     }
   };
-  if (uni(int((wm + 1) * 16 * MB <= tr.nrows && n0 + 16 * NB <= p.N && p.N % 8 == 0))) rows(std::true_type{});
+  const bool inside = uni(int((wm + 1) * 16 * MB <= tr.nrows && n0 + 16 * NB <= p.N && p.N % 8 == 0)) != 0;
+  if (inside) rows(std::true_type{});
   else rows(std::false_type{});
+  return inside;
 }
 
 // All work items of this workgroup under plan q on BM x BN tiles.
@@ -844,8 +850,20 @@ HILO_DEV void gemm8_run(const GemmProblem &p, const SkPlan &q, int pid, uint8_t 
   };
   // this wave has read the window; all but the last window issued have landed (the epilogue's DMA, issued
   // behind that one, only makes this wait stricter); on to the next
+  // int8: the S - 1 waits after an epilogue are for windows issued before its stores, so those may still be on their way
+  // (waited for, they held up the first window of every tile)
+  int behind = 0;
   auto next_window = [&]() __attribute__((always_inline)) {
-    wait_vm<(S - 2) * (LA + LB)>();
+    if constexpr (I8) {
+      if (behind > 0) {
+        wait_vm<(S - 2) * (LA + LB) + kStoresI8<G, OP>>();
+        --behind;
+      } else {
+        wait_vm<(S - 2) * (LA + LB)>();
+      }
+    } else {
+      wait_vm<(S - 2) * (LA + LB)>();
+    }
     asm volatile("s_barrier" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
     so = so == (S - 1) * WB ? 0 : so + WB;
@@ -927,8 +945,8 @@ HILO_DEV void gemm8_run(const GemmProblem &p, const SkPlan &q, int pid, uint8_t 
       }
     }
     if (whole) {
-      // a one-step item's epilogue operands may still be in flight
-      if (cur.ke - cur.kb < 2) wait_vm<0>();
+      // the epilogue operands of a one-step item, or with laxer waits of one of up to S steps, may still be in flight
+      if (cur.ke - cur.kb < (I8 ? S + 1 : 2)) wait_vm<0>();
     }
     const int lane = opaque(threadIdx.x & 63), lr = lane & 15, lg = lane >> 4;
     if constexpr (B32) {
@@ -950,7 +968,7 @@ HILO_DEV void gemm8_run(const GemmProblem &p, const SkPlan &q, int pid, uint8_t 
                   f32x4{acc[i][j][4 * c], acc[i][j][4 * c + 1], acc[i][j][4 * c + 2], acc[i][j][4 * c + 3]};
       }
     } else if (I8 && whole) {
-      if constexpr (I8) epilogue_i8<G, EPI, OP>(p, etr, en0, wm, lane, epi, acc);
+      if constexpr (I8) behind = epilogue_i8<G, EPI, OP>(p, etr, en0, wm, lane, epi, acc) ? S - 1 : 0;
     } else if (whole) {
      if constexpr (!I8) {
       uint2 bu[NB];
@@ -1338,21 +1356,132 @@ __global__ __launch_bounds__(kFixThreads) void k_gemm8_fix(GemmProblem p) {
 // and the cycles of v_mfma_f32_16x16x32_bf16, so loads, reads and MFMA time per window are those of bf16 and the tile
 // choice's estimates hold with half as many windows.
 
-// The tile, and its row tiles.
+// Two things differ.  Half the K steps of a tile leave its epilogue twice the share, so its stores write whole pieces of
+// rows and the next tile's first windows do not wait for them.  And 256 tiles or more always run whole: a stream-K tail
+// is a launch that finishes it (4.2 us where there is nothing to finish, and only the device knows), and where one size
+// of tile would leave a poor last wave the other mostly does not -- so up to K = 8192, where fewer tiles run whole too,
+// there is no second launch at all.
+
+// Small problems: 64 x 32 tiles, two a workgroup, each on four waves that split K in steps of 128; their sums are added
+// through LDS (gemm_small_run's layout, and its cost per step).
+template <int EPI, int OP>
+HILO_DEV void small_run_i8(const GemmProblem &p, int rows, int pid, uint8_t *lds) {
+  constexpr int BM = 64, BN = 32, MB = 4, NB = 2;
+  i32x4 *part = reinterpret_cast<i32x4 *>(lds);  // [2 tiles][4 waves][8 blocks][64 lanes]
+  const int lane = threadIdx.x & 63;
+  const int wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), w = wid & 3;
+  const int lr = lane & 15, lg = lane >> 4;
+  const int tilesN = (p.N + BN - 1) / BN, tiles = rows * tilesN;
+  const int steps = (p.K + 127) / 128, s0 = steps * w / 4, s1 = steps * (w + 1) / 4;
+  for (int t0 = pid; t0 < tiles; t0 += 2 * kGemmWorkgroups) {  // the same number of turns for both tiles
+    const int t = t0 + (wid >> 2) * kGemmWorkgroups;
+    const bool on = t < tiles;
+    const int tn = on ? t % tilesN : 0, n0 = tn * BN;
+    const TileRows tr = uni(decode_row_tile(p, BM, on ? t / tilesN : 0));
+    const char *A[MB], *W[NB];
+#pragma unroll
+    for (int i = 0; i < MB; ++i)
+      A[i] = reinterpret_cast<const char *>(p.A) + size_t(tr.row0 + min(16 * i + lr, tr.nrows - 1)) * p.K;
+#pragma unroll
+    for (int j = 0; j < NB; ++j)
+      W[j] = reinterpret_cast<const char *>(tr.sigma ? p.W[1] : p.W[0]) + size_t(min(n0 + 16 * j + lr, p.N - 1)) * p.K;
+    i32x4 acc[MB][NB];
+#pragma unroll
+    for (int i = 0; i < MB; ++i)
+#pragma unroll
+      for (int j = 0; j < NB; ++j) acc[i][j] = i32x4{0, 0, 0, 0};
+    // chunks of 16 bytes: those behind K are the row's last again, and A's are cleared
+    auto load = [&](int s, i32x4 (&a)[2][MB], i32x4 (&b)[2][NB]) __attribute__((always_inline)) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int k = min(128 * s + 64 * h + 16 * lg, p.K - 16);
+#pragma unroll
+        for (int i = 0; i < MB; ++i) a[h][i] = *reinterpret_cast<const i32x4 *>(A[i] + k);
+#pragma unroll
+        for (int j = 0; j < NB; ++j) b[h][j] = *reinterpret_cast<const i32x4 *>(W[j] + k);
+      }
+    };
+    auto mul = [&](int s, i32x4 (&a)[2][MB], const i32x4 (&b)[2][NB]) __attribute__((always_inline)) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const bool in = 128 * s + 64 * h + 16 * lg < p.K;
+#pragma unroll
+        for (int i = 0; i < MB; ++i) {
+          if (!in) a[h][i] = i32x4{0, 0, 0, 0};
+#pragma unroll
+          for (int j = 0; j < NB; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(b[h][j], a[h][i], acc[i][j], 0, 0, 0);
+        }
+      }
+    };
+    if (on && s0 < s1) {
+      i32x4 xa[2][MB], xb[2][NB], ya[2][MB], yb[2][NB];
+      load(s0, xa, xb);
+#pragma unroll 1
+      for (int s = s0; s < s1; s += 2) {
+        if (s + 1 < s1) load(s + 1, ya, yb);
+        mul(s, xa, xb);
+        if (s + 1 >= s1) break;
+        if (s + 2 < s1) load(s + 2, xa, xb);
+        mul(s + 1, ya, yb);
+      }
+    }
+    i32x4 *mine = part + (wid * MB * NB) * 64 + lane;
+#pragma unroll
+    for (int i = 0; i < MB; ++i)
+#pragma unroll
+      for (int j = 0; j < NB; ++j) mine[(i * NB + j) * 64] = acc[i][j];
+    __syncthreads();
+    // wave w finishes row block w
+    i32x4 v[NB];
+#pragma unroll
+    for (int j = 0; j < NB; ++j) {
+      const i32x4 *src = part + ((wid & 4) * MB * NB + w * NB + j) * 64 + lane;
+      v[j] = (src[0] + src[MB * NB * 64]) + (src[2 * MB * NB * 64] + src[3 * MB * NB * 64]);
+    }
+    if (on) SkTile<BM, BN, 4, 1>::template epilogue_row<EPI, OP>(p, tr, n0, w, 0, lane, v);
+    __syncthreads();  // the next tiles' sums go to the same LDS
+  }
+}
+
+// The tile, and its row tiles: the shortest of three estimates in units of 10 ns, as choose_tile's.  Eight tiles a
+// workgroup, K 1536 .. 6144: a step of a 256 x 256 tile takes 1.48 us and the tile's rest 6.0 (8.7 with GELU), of a 192 x
+// 192 tile 0.91 and 5.6 (7.3).
 template <int EPI>
 HILO_DEV Tile choose_tile_i8(const GemmProblem &p, int &rows) {
   constexpr uint32_t P = kGemmWorkgroups;
-  int r192 = 0, r256 = 0;
+  constexpr bool GELU = EPI == EPI_GELU;
+  uint32_t r64 = 0, r192 = 0, r256 = 0;
   for (int s = 0; s < p.B; ++s) {
     const int img = cu_at(p.cu, s + 1) - p.L - cu_at(p.cu, s);
+    r64 += (img + 63) / 64 + (p.L + 63) / 64;
     r192 += (img + 191) / 192 + (p.L + 191) / 192;
     r256 += (img + 255) / 256 + (p.L + 255) / 256;
   }
-  const uint32_t nk = (p.K + 127) / 128;
-  const uint32_t c192 = plan_cost<EPI>(r192 * ((p.N + 191) / 192), nk, TileCost{91, 400, 1400, 2000, 2700, 20, 2500});
-  const uint32_t c256 = plan_cost<EPI>(r256 * ((p.N + 255) / 256), nk, TileCost{146, 700, 3300, 3600, 4500, 35, 4500});
-  rows = c256 < c192 ? r256 : r192;
-  return c256 < c192 ? TILE_256 : TILE_192;
+  const uint32_t nk = (p.K + 127) / 128, tiles = r64 * ((p.N + 31) / 32);
+  auto cost = [&](uint32_t T, uint32_t step, uint32_t tile, uint32_t piece, uint32_t piece_t) __attribute__((always_inline)) {
+    if (T >= P || runs_whole(T, nk)) return (T + P - 1) / P * (nk * step + tile);
+    return T * nk / P * step + piece + piece_t * T;
+  };
+  uint32_t best = cost(r192 * ((p.N + 191) / 192), 91, GELU ? 730 : 560, 2700, 20);
+  rows = r192;
+  Tile t = TILE_192;
+  const uint32_t c256 = cost(r256 * ((p.N + 255) / 256), 148, GELU ? 870 : 600, 4500, 35);
+  if (c256 < best) {
+    best = c256;
+    rows = r256;
+    t = TILE_256;
+  }
+  const uint32_t turns = (tiles + 2 * P - 1) / (2 * P);
+  if (turns * ((nk + 3) / 4 * (tiles <= P ? 140 : 265) + 300) < best) {
+    rows = r64;
+    t = TILE_SMALL;
+  }
+  return t;
+}
+
+template <int BN>
+HILO_DEV SkPlan plan_i8(const GemmProblem &p, int rows) {
+  return sk_plan(p, rows, BN, 128, (p.K + 127) / 128, false);
 }
 
 template <int EPI, int OP>
@@ -1361,15 +1490,19 @@ __global__ __launch_bounds__(512, 2) void k_linear_i8(GemmProblem p) {
   __shared__ __attribute__((aligned(1024))) uint8_t lds[L0 > L1 ? L0 : L1];
   const int pid = xcd_remap(blockIdx.x, kGemmWorkgroups);
   int rows;
-  if (choose_tile_i8<EPI>(p, rows) == TILE_256) gemm8_run<256, 256, EPI, OP>(p, sk_plan(p, rows, 256, 128, (p.K + 127) / 128), pid, lds);
-  else gemm8_run<192, 192, EPI, OP>(p, sk_plan(p, rows, 192, 128, (p.K + 127) / 128), pid, lds);
+  switch (choose_tile_i8<EPI>(p, rows)) {
+    case TILE_SMALL: small_run_i8<EPI, OP>(p, rows, pid, lds); break;
+    case TILE_256: gemm8_run<256, 256, EPI, OP>(p, plan_i8<256>(p, rows), pid, lds); break;
+    default: gemm8_run<192, 192, EPI, OP>(p, plan_i8<192>(p, rows), pid, lds);
+  }
 }
 
 template <int EPI, int OP>
 __global__ __launch_bounds__(kFixThreads) void k_linear_i8_fix(GemmProblem p) {
   int rows;
-  if (choose_tile_i8<EPI>(p, rows) == TILE_256) gemm_fix<g8::Geo<256, 256, OP>, 256, 256, EPI, OP>(p, sk_plan(p, rows, 256, 128, (p.K + 127) / 128));
-  else gemm_fix<g8::Geo<192, 192, OP>, 192, 192, EPI, OP>(p, sk_plan(p, rows, 192, 128, (p.K + 127) / 128));
+  const Tile t = choose_tile_i8<EPI>(p, rows);
+  if (t == TILE_256) gemm_fix<g8::Geo<256, 256, OP>, 256, 256, EPI, OP>(p, plan_i8<256>(p, rows));
+  else if (t == TILE_192) gemm_fix<g8::Geo<192, 192, OP>, 192, 192, EPI, OP>(p, plan_i8<192>(p, rows));
 }
 
 // ------------------------------------------------------------------------------- fp32 path
@@ -1529,9 +1662,7 @@ static hipError_t run_i8(const GemmProblem &p, hipStream_t st) {
   hipLaunchKernelGGL((k_linear_i8<EPI, OP>), dim3(P), dim3(512), 0, st, p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  // max_img_rows: all rows of the buffers, of which every segment may leave a part of a tile
-  const long long tiles_max = (p.max_img_rows / 192 + 2 * (long long)p.B) * ((p.N + 191) / 192);
-  if (tiles_max < P && (p.K + 127) / 128 <= kNoSplitSteps) return hipSuccess;
+  if ((p.K + 127) / 128 <= kNoSplitSteps) return hipSuccess;  // no tile is ever cut
   hipLaunchKernelGGL((k_linear_i8_fix<EPI, OP>), dim3(P), dim3(kFixThreads), 0, st, p);
   return hipGetLastError();
 }

@@ -2,25 +2,54 @@
 the shapes with which the GPU tests reach each kind."""
 import schedule_model as M
 
+WORKGROUPS = 256
+# estimates of choose_tile_i8 in units of 10 ns: a K step, a tile's rest without and with GELU, K pieces in all, per tile
+COSTS = {192: (91, 560, 730, 2700, 20), 256: (148, 600, 870, 4500, 35)}
+
 # (sample lengths, text rows, K, N) and (tile, tiles, pieces per tile, data-parallel units, stream-K units, workgroups
-# sharing those).  K is no multiple of 128 in most: the last step is part of one
+# sharing those), or ("small", tiles, turns).  K is no multiple of 128 in most: the last step is part of one
 SHAPES = [
-    # 192 x 192: whole tiles in one wave; one tile in 128 pieces of a step; pieces with a stream-K tail; one piece, a tail
-    (([300], 100, 528, 520), (192, 9, 1, 9, 0, 256)),
-    (([128], 0, 16384, 100), (192, 1, 128, 0, 128, 128)),
-    (([200, 90], 40, 8336, 1000), (192, 24, 11, 256, 8, 8)),
-    (([5000], 0, 2064, 13312), (192, 1890, 1, 1792, 98, 139)),
-    # 256 x 256: one wave of whole tiles; four; pieces
+    # 64 x 32: one turn; two (many samples of a row)
+    (([300], 100, 1040, 520), ("small", 102, 1)),
+    (([1] * 300, 0, 80, 64), ("small", 600, 2)),
+    # 192 x 192: whole tiles in one wave, and in two; one tile in 256 pieces; pieces with a stream-K tail, whole and cut
+    (([2500], 30, 528, 2048), (192, 154, 1, 154, 0, 256)),
+    (([2766], 512, 1552, 6144), (192, 480, 1, 480, 0, 256)),
+    (([190], 0, 65536, 100), (192, 1, 256, 256, 0, 0)),
+    (([500], 40, 8336, 2040), (192, 44, 6, 256, 8, 8)),
+    (([700], 40, 16400, 2000), (192, 55, 5, 256, 19, 42)),
+    # 256 x 256: one wave of whole tiles; five; pieces
     (([4096], 0, 1040, 4096), (256, 256, 1, 256, 0, 256)),
-    (([15000], 0, 2048, 3900), (256, 944, 1, 944, 0, 256)),
-    (([2040], 0, 16400, 2040), (256, 64, 4, 256, 0, 0)),
+    (([5000], 0, 2064, 13312), (256, 1040, 1, 1040, 0, 256)),
+    (([2048], 0, 65536, 2044), (256, 64, 4, 256, 0, 0)),
 ]
 
 
-def describe(lens, text, K, N):
+def choose(segs, nk, N, gelu=False):
+    P, found = WORKGROUPS, []
+    for tile in (192, 256):
+        step, rest, rest_gelu, piece, piece_t = COSTS[tile]
+        T = M.row_tiles(segs, tile) * -(-N // tile)
+        if T >= P or M.whole_tiles(T, P, nk):
+            found.append((-(-T // P) * (nk * step + (rest_gelu if gelu else rest)), tile))
+        else:
+            found.append((T * nk // P * step + piece + piece_t * T, tile))
+    tiles = M.row_tiles(segs, 64) * -(-N // 32)
+    one, two, turn = M.SMALL_COSTS
+    found.append((-(-tiles // (2 * P)) * (-(-nk // 4) * (one if tiles <= P else two) + turn), "small"))
+    return min(found, key=lambda f: f[0])[1]
+
+
+def plan(T, P, nk):
+    return (1, T, T, nk, 0, P) if T >= P else M.plan(T, P, nk)
+
+
+def describe(lens, text, K, N, gelu=False):
     segs, nk = [(n - text, text) for n in lens], -(-K // 128)
-    c192, c256 = (M.cost(False, M.row_tiles(segs, t) * -(-N // t), nk, *M.TILE_COSTS[t]) for t in (192, 256))
-    tile = 256 if c256 < c192 else 192
+    tile = choose(segs, nk, N, gelu)
+    if tile == "small":
+        tiles = M.row_tiles(segs, 64) * -(-N // 32)
+        return tile, tiles, -(-tiles // (2 * WORKGROUPS))
     T = M.row_tiles(segs, tile) * -(-N // tile)
-    s, U, dp, _, _, Pk = M.plan(T, M.WORKGROUPS, nk)
+    s, U, dp, _, _, Pk = plan(T, WORKGROUPS, nk)
     return tile, T, s, dp, U - dp, Pk

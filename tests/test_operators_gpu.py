@@ -456,36 +456,35 @@ def test_linear_i8(dtype, lens, text, K, N, gelu, bias):
 
 
 def run_linear(dtype, lens, text, K, N, gelu, bias, seed, rows=None):
-    rng = np.random.default_rng(seed)
+    """hilo_linear_i8 on float rows and on their codes, `rows` of them (all) compared."""
+    g = torch.Generator().manual_seed(seed)
     cu, T = _cu(lens), int(sum(lens))
-    x, _ = _rand(rng, dtype, T + 3, K)
+    x = torch.randn(T + 3, K, generator=g).to(DT[dtype])
     ws, ref = [], []
     for _ in range(2):
-        w = {"w": torch.from_numpy(rng.integers(-127, 128, (N, K)).astype(np.int8)).cuda(), "s": _dev(rng.uniform(0.5, 2, N) * 1e-3),
-             "b": _rand(rng, dtype, N)[0] if bias else None}
-        ws.append(w)
-        ref.append({"w": w["w"].cpu().numpy(), "s": _np(w["s"]), "b": None if w["b"] is None else _np(w["b"])})
+        w = {"w": torch.randint(-127, 128, (N, K), dtype=torch.int8, generator=g), "s": (torch.rand(N, generator=g) + 0.5) * 1e-3,
+             "b": torch.randn(N, generator=g).to(DT[dtype]) if bias else None}
+        ws.append({k: None if v is None else v.cuda() for k, v in w.items()})
+        ref.append({k: None if v is None else v.numpy() if k == "w" else v.double().numpy() for k, v in w.items()})
     plan = hilo.linear_weights_i8(ws)
     out = torch.full((T + 3, N), 9.0, dtype=DT[dtype], device="cuda")
     act = hilo.ACT_GELU if gelu else hilo.ACT_NONE
     wsp = torch.full((hilo.hilo_linear_i8_workspace_bytes(T + 3, K),), 255, dtype=torch.uint8, device="cuda")
-    cud = _dev(cu, torch.int32)
-    hilo.hilo_linear_i8(plan, x, out, cud, text, act=act, workspace=wsp)
+    cud, xd = _dev(cu, torch.int32), x.cuda()
+    hilo.hilo_linear_i8(plan, xd, out, cud, text, act=act, workspace=wsp)
     torch.cuda.synchronize()
-    codes, scale = Q.quantize_rows_i8(x.float().cpu().numpy())
     pick = np.arange(T) if rows is None else rows
-    keep = np.zeros(T, bool)
-    keep[pick] = True
-    want, size = np.zeros((T, N)), np.zeros((T, N))
+    codes, scale = Q.quantize_rows_i8(x[torch.from_numpy(pick)].float().numpy())
+    want, size = np.zeros((len(pick), N)), np.zeros((len(pick), N))
     for a, b, _, k in Q.segments(cu, text):
-        at = a + np.flatnonzero(keep[a:b])
+        at = np.flatnonzero((pick >= a) & (pick < b))
         if len(at):
             want[at], size[at] = Q.linear_i8(codes[at], scale[at], [ref[k]], np.array([0, len(at)]), 0, gelu)
-    _within(_np(out)[pick], want[pick], _linear_bound(want[pick], size[pick], gelu, dtype), "linear")
+    _within(_np(out[torch.from_numpy(pick).cuda()]), want, _linear_bound(want, size, gelu, dtype), "linear")
     assert (out[T:] == 9).all()
     # codes in: the same bits
     cd, sd = torch.empty(T + 3, K, dtype=torch.int8, device="cuda"), torch.empty(T + 3, device="cuda")
-    hilo.hilo_quantize_rows_i8(x, cd, sd)
+    hilo.hilo_quantize_rows_i8(xd, cd, sd)
     out2 = torch.full_like(out, 9.0)
     hilo.hilo_linear_i8(plan, cd, out2, cud, text, x_scale=sd, act=act, workspace=wsp)
     torch.cuda.synchronize()
@@ -493,7 +492,7 @@ def run_linear(dtype, lens, text, K, N, gelu, bias, seed, rows=None):
 
 
 # every kind of plan of the large tiles (linear_schedule.py says which each shape reaches), both types of output
-@pytest.mark.parametrize("shape", [s for s, _ in linear_schedule.SHAPES], ids=str)
+@pytest.mark.parametrize("shape", [s for s, _ in linear_schedule.SHAPES], ids=lambda s: f"{sum(s[0])}x{s[2]}x{s[3]}")
 @pytest.mark.parametrize("dtype,gelu,bias", [("bf16", True, True), ("f32", False, True), ("bf16", False, False)])
 def test_linear_i8_plans(shape, dtype, gelu, bias):
     lens, text, K, N = shape
