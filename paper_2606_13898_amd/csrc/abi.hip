@@ -813,19 +813,13 @@ hilo_status hilo_rope(int32_t dtype, const hilo_rotary *r, const void *x, int64_
   p.heads = r->heads; p.hd = r->head_dim; p.axes = r->axes; p.n = int(n);
   p.adjacent = (r->flags & HILO_ROPE_ADJACENT) != 0;
   p.backward = backward != 0;
-  // frequencies in turns: a geometric series by one power and products (off by less than 128 roundings of 64 bits)
-  const bool one = (r->flags & HILO_ROPE_ONE_SPECTRUM) != 0;
-  constexpr double kTurn = 1.0 / 6.283185307179586476925;
-  double w = kTurn, step = one ? std::pow(r->base[0], -1.0 / double(n)) : 1.0;
+  p.one_spectrum = (r->flags & HILO_ROPE_ONE_SPECTRUM) != 0;
   int j = 0;
   for (int a = 0; a < 4; ++a) {
-    p.first[a] = j;
+    p.first[a] = a < r->axes ? j : p.n;
     if (a >= r->axes || r->pairs[a] == 0) continue;
-    if (!one) {
-      w = kTurn;
-      step = std::pow(r->base[a], -1.0 / double(r->pairs[a]));
-    }
-    for (int i = 0; i < r->pairs[a]; ++i, w *= step) p.freq[j++] = w;
+    p.step[a] = std::log2(r->base[p.one_spectrum ? 0 : a]) / double(p.one_spectrum ? n : r->pairs[a]);
+    j += r->pairs[a];
   }
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   return dev_status(timed(K_ROPE, st, [&] { return launch_rope(dtype == HILO_BF16, p, st); }));

@@ -119,7 +119,8 @@ size_t attention_part_bytes(bool bf16, int hd);
 
 // Rotary positions: rows [rows][ldx] of `heads` heads of hd values each; rows at or behind *rows_end (device,
 // may be null) are left alone.  The first 2 n columns of a head turn: pair j is columns (j, j + n), or (2 j, 2 j + 1)
-// if adjacent, its axis the largest a with first[a] <= j, its angle pos[row][axis] * freq[j] turns.
+// if adjacent, its axis the largest a with first[a] <= j, its frequency 2^(-step[a] (j - first[a])), or with one
+// spectrum 2^(-step[a] j).  (A table of frequencies would be read from the launch's arguments, in host memory.)
 constexpr int kRopeMaxPairs = 128;
 constexpr int kRopeTable = 1024;  // (row, pair) cosines and sines a workgroup holds
 struct RopeProblem {
@@ -131,9 +132,9 @@ struct RopeProblem {
   const int *rows_end;
   int rows, heads, hd, axes, n;
   int first[4];  // first pair of each axis (n behind the last axis)
-  int adjacent, backward;
+  int adjacent, backward, one_spectrum;
   int units_head, block_rows, block_heads;  // set by the launcher
-  double freq[kRopeMaxPairs];
+  double step[4];
 };
 hipError_t launch_rope(bool bf16, RopeProblem p, hipStream_t st);
 hipError_t launch_token_positions(const int *fine_idx, const int *pool_idx, const int *counts, const int *cu,

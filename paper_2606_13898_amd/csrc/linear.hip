@@ -190,35 +190,40 @@ HILO_DEV FewRows few_rows(const GemmProblem &p, int BM, int t, int *rows) {
   return FewRows{uni(sigma), uni(left < 0 ? 0 : left < BM ? left : BM)};
 }
 
-// Few rows: tiles of 16 MB rows x 16 columns, K split over the four waves of a workgroup in steps of 128, their sums
+// Few rows: tiles of 16 MB rows x 16 NB columns, K split over the four waves of a workgroup in steps of 128, their sums
 // added through LDS.  What bounds it is the weights' way from memory: every wave streams its columns' bytes, 32 a lane
 // and step (whole lines of 16 rows), up to 2 GS steps ahead of the matrix core, and tiles are narrow so that the CUs share them
-// evenly.  FUSED (MB = 1): x are float rows, which every workgroup quantises for itself into LDS -- each wave the part
-// of K that it multiplies, while its first weights are on their way; dynamic LDS holds the buffers' rows of codes.
-constexpr int kFewSteps = 3;
-template <bool BF16, bool GELU, int MB, bool FUSED>
+// evenly.  MR > 0 (MB = 1): x are float rows, which every workgroup quantises for itself into LDS, MR at a time -- each
+// wave the part of K that it multiplies, while its first weights are on their way; dynamic LDS holds the buffers' rows of
+// codes.
+template <bool BF16, bool GELU, int MB, int NB, int MR>
 __global__ __launch_bounds__(256) void k_linear_i8_few(GemmProblem p) {
-  constexpr int NW = 4, GS = kFewSteps;
-  __shared__ i32x4 part[NW][MB][64];
+  constexpr int NW = 4, GS = NB == 1 ? 3 : 2;
+  constexpr bool FUSED = MR > 0;
+  __shared__ i32x4 part[NW][MB * NB][64];
   __shared__ uint32_t tops[16][NW];
   __shared__ int rows[16 * MB];
   extern __shared__ __attribute__((aligned(16))) uint8_t codes[];
   const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lr = lane & 15, lg = lane >> 4;
-  const int n0 = blockIdx.x * 16;
+  const int n0 = blockIdx.x * 16 * NB;
   const int steps = (p.K + 127) / 128, s0 = steps * wid / NW, s1 = steps * (wid + 1) / NW;
   const int kl = 16 * lg;
-  const int8_t *W;
-  i32x4 w[2][GS][2];
-  auto load_w = [&](int s, i32x4 (&d)[GS][2]) __attribute__((always_inline)) {
+  const int8_t *W[NB];
+  i32x4 w[2][GS][2][NB];
+  auto load_w = [&](int s, i32x4 (&d)[GS][2][NB]) __attribute__((always_inline)) {
     if (s >= s1) return;
 #pragma unroll
     for (int g = 0; g < GS; ++g)
 #pragma unroll
-      for (int h = 0; h < 2; ++h) d[g][h] = chunk_at(W, 128 * min(s + g, steps - 1) + kl + 64 * h, p.K);
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int j = 0; j < NB; ++j) d[g][h][j] = chunk_at(W[j], 128 * min(s + g, steps - 1) + kl + 64 * h, p.K);
   };
   auto first_w = [&](int sigma) __attribute__((always_inline)) {
-    W = reinterpret_cast<const int8_t *>(sigma ? p.W[1] : p.W[0]) + size_t(min(n0 + lr, p.N - 1)) * p.K;
+#pragma unroll
+    for (int j = 0; j < NB; ++j)
+      W[j] = reinterpret_cast<const int8_t *>(sigma ? p.W[1] : p.W[0]) + size_t(min(n0 + 16 * j + lr, p.N - 1)) * p.K;
     load_w(s0, w[0]);
     load_w(s0 + GS, w[1]);
   };
@@ -226,13 +231,14 @@ __global__ __launch_bounds__(256) void k_linear_i8_few(GemmProblem p) {
   const FewRows tr = few_rows(p, 16 * MB, blockIdx.y, rows);
   if (tr.n == 0) return;
   if (p.L != 0) first_w(tr.sigma);
-  const I8Cols<BF16> cols(p, tr.sigma, n0 + 4 * lg);
+  // wave wid finishes blocks wid, wid + NW, ... of the tile, all of one column block
+  static_assert(MB * NB == 1 || NW % NB == 0, "blocks of a wave");
+  const I8Cols<BF16> cols(p, tr.sigma, n0 + 16 * (wid % NB) + 4 * lg);
   const int ldc = 128 * steps + 16;  // 16 rows' chunks at one column fall on all banks
   float sa = 0.f;
   if constexpr (FUSED) {
     const int k0 = 128 * s0, k1 = 128 * s1;
-    // four rows, or their last again, and one chunk of 512 values of each at a time
-    constexpr int MR = 4;
+    // MR rows, or their last again, and one chunk of 512 values of each at a time
     const int l8 = 8 * lane;
     for (int m0 = 0; m0 < tr.n; m0 += MR) {
       uint32_t top[MR];
@@ -287,10 +293,12 @@ __global__ __launch_bounds__(256) void k_linear_i8_few(GemmProblem p) {
   for (int i = 0; i < MB; ++i)
     A[i] = reinterpret_cast<const int8_t *>(p.A) + size_t(rows[min(16 * i + lr, tr.n - 1)]) * p.K;
   const uint8_t *cr = codes + min(lr, tr.n - 1) * ldc;
-  i32x4 acc[MB];
+  i32x4 acc[MB][NB];
 #pragma unroll
-  for (int i = 0; i < MB; ++i) acc[i] = i32x4{0, 0, 0, 0};
-  auto mul = [&](int s, const i32x4 (&d)[GS][2]) __attribute__((always_inline)) {
+  for (int i = 0; i < MB; ++i)
+#pragma unroll
+    for (int j = 0; j < NB; ++j) acc[i][j] = i32x4{0, 0, 0, 0};
+  auto mul = [&](int s, const i32x4 (&d)[GS][2][NB]) __attribute__((always_inline)) {
 #pragma unroll
     for (int g = 0; g < GS; ++g)
       if (s + g < s1) {
@@ -306,7 +314,9 @@ __global__ __launch_bounds__(256) void k_linear_i8_few(GemmProblem p) {
               a = chunk_at(A[i], k, p.K);
               if (k >= p.K) a = i32x4{0, 0, 0, 0};
             }
-            acc[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(d[g][h], a, acc[i], 0, 0, 0);
+#pragma unroll
+            for (int j = 0; j < NB; ++j)
+              acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(d[g][h][j], a, acc[i][j], 0, 0, 0);
           }
         }
       }
@@ -319,12 +329,14 @@ __global__ __launch_bounds__(256) void k_linear_i8_few(GemmProblem p) {
     load_w(s + 3 * GS, w[1]);
   }
 #pragma unroll
-  for (int i = 0; i < MB; ++i) part[wid][i][lane] = acc[i];
+  for (int i = 0; i < MB; ++i)
+#pragma unroll
+    for (int j = 0; j < NB; ++j) part[wid][i * NB + j][lane] = acc[i][j];
   lds_barrier();
 #pragma unroll
-  for (int i = wid; i < MB; i += NW) {
-    const i32x4 v = (part[0][i][lane] + part[1][i][lane]) + (part[2][i][lane] + part[3][i][lane]);
-    const int rl = 16 * i + lr, n = n0 + 4 * lg;
+  for (int f = wid; f < MB * NB; f += NW) {
+    const i32x4 v = (part[0][f][lane] + part[1][f][lane]) + (part[2][f][lane] + part[3][f][lane]);
+    const int rl = 16 * (f / NB) + lr, n = n0 + 16 * (f % NB) + 4 * lg;
     if (rl < tr.n && n < p.N) i8_out4<BF16, GELU>(p, size_t(rows[rl]), n, v, FUSED ? sa : p.a_scale[rows[rl]], cols);
   }
 }
@@ -395,7 +407,7 @@ constexpr long long kFewRows = 64;
 size_t linear_i8_part_bytes(long long rows) { return rows <= kFewRows ? 0 : kSkPartBytes; }
 
 // Whether float rows are quantised by the kernel that multiplies them.
-static bool fused_few(const GemmProblem &p) { return p.max_img_rows <= 8 && p.max_img_rows * (p.K + 144) <= 49152; }
+static bool fused_few(const GemmProblem &p) { return p.max_img_rows <= 4 && p.max_img_rows * (p.K + 144) <= 49152; }
 static bool fused_small(const GemmProblem &p, bool bf16) {
   return p.K <= kSmallK && double(p.max_img_rows) * p.K * (bf16 ? 2 : 4) * ((p.N + 63) / 64) <= 32e6;
 }
@@ -414,15 +426,19 @@ static hipError_t run_linear_i8(const GemmProblem &p, hipStream_t st) {
     return hipGetLastError();
   }
   // row tiles of the two streams
-  const int bm = rows <= 16 ? 16 : 64, streams = p.L > 0 ? 2 : 1;
-  const dim3 grid(unsigned((p.N + 15) / 16), unsigned(streams * ((rows + bm - 1) / bm)));
+  const int bm = rows <= 16 ? 16 : 64, bn = rows <= 16 || p.N < 8192 ? 16 : 32, streams = p.L > 0 ? 2 : 1;
+  const dim3 grid(unsigned((p.N + bn - 1) / bn), unsigned(streams * ((rows + bm - 1) / bm)));
   if (p.a_scale == nullptr) {
     const size_t lds = size_t(rows) * ((p.K + 127) / 128 * 128 + 16);
-    hipLaunchKernelGGL((k_linear_i8_few<BF16, GELU, 1, true>), grid, dim3(256), lds, st, p);
+    if (rows == 1) hipLaunchKernelGGL((k_linear_i8_few<BF16, GELU, 1, 1, 1>), grid, dim3(256), lds, st, p);
+    else if (rows == 2) hipLaunchKernelGGL((k_linear_i8_few<BF16, GELU, 1, 1, 2>), grid, dim3(256), lds, st, p);
+    else hipLaunchKernelGGL((k_linear_i8_few<BF16, GELU, 1, 1, 4>), grid, dim3(256), lds, st, p);
   } else if (rows <= 16) {
-    hipLaunchKernelGGL((k_linear_i8_few<BF16, GELU, 1, false>), grid, dim3(256), 0, st, p);
+    hipLaunchKernelGGL((k_linear_i8_few<BF16, GELU, 1, 1, 0>), grid, dim3(256), 0, st, p);
+  } else if (bn == 16) {
+    hipLaunchKernelGGL((k_linear_i8_few<BF16, GELU, 4, 1, 0>), grid, dim3(256), 0, st, p);
   } else {
-    hipLaunchKernelGGL((k_linear_i8_few<BF16, GELU, 4, false>), grid, dim3(256), 0, st, p);
+    hipLaunchKernelGGL((k_linear_i8_few<BF16, GELU, 4, 2, 0>), grid, dim3(256), 0, st, p);
   }
   return hipGetLastError();
 }

@@ -18,11 +18,22 @@ HILO_DEV float2 turn(double t) {
   const double q = rint(4.0 * t);
   const double x = (t - 0.25 * q) * 6.283185307179586476925;
   const double y = x * x;
-  const double s = x * (1.0 + y * (-1.0 / 6 + y * (1.0 / 120 + y * (-1.0 / 5040 + y * (1.0 / 362880 + y * (-1.0 / 39916800 + y / 6227020800.0))))));
-  const double c = 1.0 + y * (-0.5 + y * (1.0 / 24 + y * (-1.0 / 720 + y * (1.0 / 40320 + y * (-1.0 / 3628800 + y / 479001600.0)))));
+  const double s = x * (1.0 + y * (-1.0 / 6 + y * (1.0 / 120 + y * (-1.0 / 5040 + y * (1.0 / 362880 + y * (-1.0 / 39916800 + y * (1.0 / 6227020800.0)))))));
+  const double c = 1.0 + y * (-0.5 + y * (1.0 / 24 + y * (-1.0 / 720 + y * (1.0 / 40320 + y * (-1.0 / 3628800 + y * (1.0 / 479001600.0))))));
   const int k = int(q - 4.0 * floor(0.25 * q));  // quarter 0 .. 3 (a NaN position: 0, with a NaN series)
   const double cc = (k & 1) ? s : c, ss = (k & 1) ? c : s;
   return make_float2(float(k == 1 || k == 2 ? -cc : cc), float(k >= 2 ? -ss : ss));
+}
+
+// 2^x, |x| kept to 1000: the whole part in the exponent, e^y of the rest, at most half an octave, by its Taylor series to
+// the 14th power (off by less than 2^-56).
+HILO_DEV double pow2(double x) {
+  x = fmin(fmax(x, -1000.0), 1000.0);
+  const double k = rint(x), y = (x - k) * 0.69314718055994530942;
+  double s = 1.0;
+#pragma unroll
+  for (int i = 14; i > 0; --i) s = 1.0 + (y * s) * (1.0 / double(i));
+  return s * __longlong_as_double((long long)(int(k) + 1023) << 52);
 }
 
 template <int BYTES>
@@ -66,8 +77,11 @@ __global__ __launch_bounds__(256) void k_rope(RopeProblem p) {
   const int h0 = blockIdx.y * p.block_heads, nh = min(p.block_heads, p.heads - h0);
   for (int i = threadIdx.x; i < nr * p.n; i += 256) {
     const int r = i / p.n, j = i - r * p.n;
-    const int axis = (j >= p.first[1]) + (j >= p.first[2]) + (j >= p.first[3]);
-    float2 v = turn(double(p.pos[size_t(row0 + r) * p.axes + axis]) * p.freq[j]);
+    const int a = (j >= p.first[1]) + (j >= p.first[2]) + (j >= p.first[3]);
+    const int first = a == 0 ? 0 : a == 1 ? p.first[1] : a == 2 ? p.first[2] : p.first[3];
+    const double step = a == 0 ? p.step[0] : a == 1 ? p.step[1] : a == 2 ? p.step[2] : p.step[3];
+    const double freq = pow2(-step * double(p.one_spectrum ? j : j - first)) * 0.15915494309189533577;  // in turns
+    float2 v = turn(double(p.pos[size_t(row0 + r) * p.axes + a]) * freq);
     if (p.backward) v.y = -v.y;
     cs[i] = v;
   }

@@ -444,7 +444,7 @@ def _linear_bound(want, size, gelu, dtype):
 LINEAR = [([1], 0, 16, 4), ([1], 0, 3072, 96), ([2, 1], 0, 64, 20), ([17], 0, 80, 36), ([40, 0, 33], 0, 128, 100),
           ([31, 60], 9, 272, 64), ([70], 5, 1040, 132), ([5, 3], 3, 48, 260), ([129, 66], 65, 256, 192),
           ([300], 100, 512, 520), ([64], 64, 192, 32), ([3, 2], 1, 5008, 40), ([1, 0, 1], 0, 9200, 52), ([4], 4, 1552, 28),
-          ([13], 5, 2304, 48), ([30, 25], 0, 12304, 36), ([500, 333], 77, 768, 196), ([61], 61, 784, 68)]
+          ([13], 5, 2304, 48), ([30, 25], 0, 12304, 36), ([40, 9], 3, 2064, 8212), ([500, 333], 77, 768, 196), ([61], 61, 784, 68)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
