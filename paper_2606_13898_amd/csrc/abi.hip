@@ -757,9 +757,12 @@ bool aligned(const void *p, size_t a) { return reinterpret_cast<uintptr_t>(p) % 
 
 hilo_status check_dtype(int32_t dtype) { return dtype == HILO_F32 || dtype == HILO_BF16 ? HILO_OK : HILO_E_DTYPE; }
 
+// Grids have at most a workgroup of 256 threads a row, and fewer than 2^32 threads.
+constexpr int64_t kMaxRows = 1LL << 24;
+
 hilo_status check_rows(int64_t rows, int32_t batch, int32_t text_len) {
-  if (rows < 0 || rows >= (1LL << 28) || batch <= 0 || text_len < 0) return HILO_E_SHAPE;
-  return (long long)batch * text_len <= rows && batch < (1 << 20) ? HILO_OK : HILO_E_SHAPE;
+  if (rows < 0 || rows >= kMaxRows || batch <= 0 || batch > (1 << 20) || text_len < 0) return HILO_E_SHAPE;
+  return (long long)batch * text_len <= rows ? HILO_OK : HILO_E_SHAPE;
 }
 
 hilo_status check_norms(int32_t dtype, const hilo_norms *n, int32_t dim) {
@@ -798,10 +801,11 @@ hilo_status hilo_rope(int32_t dtype, const hilo_rotary *r, const void *x, int64_
   }
   const long long width = (long long)r->heads * r->head_dim;
   if (n < 1 || 2 * n > r->head_dim || width > (1 << 24)) return HILO_E_SHAPE;
-  if (rows < 0 || rows >= (1LL << 28) || ldx < width || ldo < width || ldx >= (1LL << 31) || ldo >= (1LL << 31)) return HILO_E_SHAPE;
-  if (!x || !pos || !out) return HILO_E_NULL;
+  if (rows < 0 || rows >= kMaxRows || ldx < width || ldo < width || ldx >= (1LL << 31) || ldo >= (1LL << 31)) return HILO_E_SHAPE;
+  if (rows > 0 && (!x || !pos || !out)) return HILO_E_NULL;
   const size_t es = dtype == HILO_BF16 ? 2 : 4;
-  if (!aligned(x, es) || !aligned(out, es) || !aligned(pos, 4) || (x == out && ldx != ldo)) return HILO_E_PARAM;
+  if (!aligned(x, es) || !aligned(out, es) || !aligned(pos, 4) || (rows > 1 && x == out && ldx != ldo))
+    return HILO_E_PARAM;
   if (rows == 0) return HILO_OK;
   if (!have_device()) return HILO_E_DEVICE;
   RopeProblem p{};
@@ -844,7 +848,8 @@ hilo_status hilo_norm_residual(int32_t dtype, const hilo_norms *n, const void *y
                                int32_t text_len, const int32_t *cu_seqlens, void *stream) {
   hilo_status e = check_norms(dtype, n, dim);
   if (e != HILO_OK || (e = check_rows(rows, batch, text_len)) != HILO_OK) return e;
-  if (!x || !cu_seqlens || (!y && !h) || (y != nullptr) != (x_out != nullptr) || (h_scale && !h)) return HILO_E_NULL;
+  if (!cu_seqlens) return HILO_E_NULL;
+  if (rows > 0 && (!x || (!y && !h) || (y != nullptr) != (x_out != nullptr) || (h_scale && !h))) return HILO_E_NULL;
   if (!aligned(x, 16) || !aligned(x_out, 16) || !aligned(y, vec_align(dtype)) || !aligned(stats, 16) ||
       !aligned(h, h_scale ? 4 : vec_align(dtype)) || !aligned(h_scale, 4))
     return HILO_E_PARAM;
@@ -881,8 +886,8 @@ hilo_status hilo_norm_residual_backward(int32_t dtype, const hilo_norms *n, cons
                                         void *stream) {
   hilo_status e = check_norms(dtype, n, dim);
   if (e != HILO_OK || (e = check_rows(rows, batch, text_len)) != HILO_OK) return e;
-  if (!stats || !dx || !cu_seqlens || (!y && !dh) || (dh && !x_out) || (y != nullptr) != (dy != nullptr) || (g && !workspace))
-    return HILO_E_NULL;
+  if (!cu_seqlens || (g && !workspace)) return HILO_E_NULL;
+  if (rows > 0 && (!stats || !dx || (!y && !dh) || (dh && !x_out) || (y != nullptr) != (dy != nullptr))) return HILO_E_NULL;
   if (!aligned(dx_out, 16) || !aligned(dh, vec_align(dtype)) || !aligned(y, vec_align(dtype)) || !aligned(x_out, 16) ||
       !aligned(stats, 16) || !aligned(dx, 16) || !aligned(dy, vec_align(dtype)) || !aligned(workspace, 16))
     return HILO_E_PARAM;
@@ -925,8 +930,8 @@ hilo_status hilo_quantize_rows_i8(int32_t dtype, const void *x, int64_t rows, in
                                   int8_t *codes, float *scale, void *stream) {
   hilo_status e = check_dtype(dtype);
   if (e != HILO_OK) return e;
-  if (rows < 0 || rows >= (1LL << 28) || cols <= 0 || cols % 16 != 0 || cols > 65536) return HILO_E_SHAPE;
-  if (!x || !codes || !scale) return HILO_E_NULL;
+  if (rows < 0 || rows >= kMaxRows || cols <= 0 || cols % 16 != 0 || cols > 65536) return HILO_E_SHAPE;
+  if (rows > 0 && (!x || !codes || !scale)) return HILO_E_NULL;
   if (!aligned(x, 16) || !aligned(codes, 8) || !aligned(scale, 4)) return HILO_E_PARAM;
   if (rows == 0) return HILO_OK;
   if (!have_device()) return HILO_E_DEVICE;
@@ -947,17 +952,19 @@ hilo_status hilo_linear_i8(int32_t dtype, const hilo_linear_w_i8 w[2], const voi
                            const int32_t *cu_seqlens, void *workspace, size_t ws_bytes, void *stream) {
   hilo_status e = check_dtype(dtype);
   if (e != HILO_OK || (e = check_rows(rows, batch, text_len)) != HILO_OK) return e;
-  if (in_dim < 16 || in_dim > 65536 || in_dim % 16 != 0 || out_dim < 4 || out_dim > (1 << 24) || out_dim % 4 != 0)
+  if (in_dim < 16 || in_dim > 65536 || in_dim % 16 != 0 || out_dim < 4 || out_dim >= (1 << 24) || out_dim % 4 != 0)
     return HILO_E_SHAPE;
+  // tiles are counted in 32 bits, the smallest of them 64 x 32, and every segment may leave a part of one
+  if ((rows / 64 + 2LL * batch) * (out_dim / 32 + 1) >= (1LL << 31)) return HILO_E_SHAPE;
   if (act != HILO_ACT_NONE && act != HILO_ACT_GELU) return HILO_E_PARAM;
-  if (!w || !x || !out || !cu_seqlens || !workspace) return HILO_E_NULL;
+  if (!w || !cu_seqlens || (rows > 0 && (!x || !out || !workspace))) return HILO_E_NULL;
   const int streams = text_len > 0 ? 2 : 1;
   for (int k = 0; k < streams; ++k) {
     if (!w[k].w || !w[k].s) return HILO_E_NULL;
     if (!aligned(w[k].w, 16) || !aligned(w[k].s, 16) || !aligned(w[k].b, vec_align(dtype))) return HILO_E_PARAM;
   }
   if (!aligned(x, 16) || !aligned(x_scale, 4) || !aligned(out, vec_align(dtype)) || !aligned(workspace, 256)) return HILO_E_PARAM;
-  if (ws_bytes < hilo_linear_i8_workspace_bytes(rows, in_dim)) return HILO_E_WORKSPACE;
+  if (rows > 0 && ws_bytes < hilo_linear_i8_workspace_bytes(rows, in_dim)) return HILO_E_WORKSPACE;
   if (rows == 0) return HILO_OK;
   if (!have_device()) return HILO_E_DEVICE;
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);

@@ -425,13 +425,13 @@ def _arg(t: Optional[torch.Tensor], dtype: torch.dtype, shape, dev: int, what: s
     """The pointer of a contiguous tensor of this type and shape on device `dev`, or None."""
     if t is None:
         return None
+    if t.dtype is dtype and t.get_device() == dev and t.shape == shape and t.is_contiguous():
+        return t.data_ptr()
     if t.dtype is not dtype or t.shape != shape:
         raise ValueError(f"{what}: expected {dtype} {tuple(shape)}, not {t.dtype} {tuple(t.shape)}")
     if t.get_device() != dev:
         raise ValueError(f"{what}: on {t.device}, other tensors on device {dev}")
-    if not t.is_contiguous():
-        raise ValueError(f"{what}: libhilo takes contiguous tensors only")
-    return t.data_ptr()
+    raise ValueError(f"{what}: libhilo takes contiguous tensors only")
 
 
 def _on_device(t: torch.Tensor) -> int:
@@ -443,11 +443,12 @@ def _on_device(t: torch.Tensor) -> int:
 
 # The current stream's handle without a Stream object around it (2.7 us of the 8 us that a small call took).
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 def _launch(fn, dev: int, stream, *args):
     """fn(*args, stream) with `dev` as the current device."""
-    if dev != torch.cuda.current_device():
+    if dev != _current_device():
         with torch.cuda.device(dev):
             return _launch(fn, dev, stream, *args)
     st = getattr(lib(), fn)(*args, _raw_stream(dev) if stream is None else _stream(stream))
@@ -531,6 +532,7 @@ def _vectors(h, vectors: dict, gains: dict):
             h.dim = g.numel()
             _same_device(h, g, name)
             getattr(h, name)[k] = g.data_ptr()
+    h.fits = (h.dim, h.batch, h.dev)
     return h
 
 
@@ -556,16 +558,22 @@ def norm_grads(*, gate=None, shift=None, scale=None, post_gain=None, pre_gain=No
                     {"post_gain": post_gain, "pre_gain": pre_gain})
 
 
-def _norm_rows(n, like: torch.Tensor, cu: torch.Tensor, others=()):
+def _norm_rows(n, like: torch.Tensor, cu: torch.Tensor, others=None):
     if like.dim() != 2:
         raise ValueError("expected [rows][dim] tensors")
     dev, dim = _on_device(like), like.shape[1]
     batch, cu_ptr = _packed(cu, dev)
-    for h in (n, *others):
-        if h is not None and (h.dim not in (None, dim) or h.batch not in (None, batch) or h.dev not in (None, dev)):
-            raise ValueError(f"vectors for dim {h.dim}, batch {h.batch} on device {h.dev}; rows have dim {dim}, batch "
-                             f"{batch} on device {dev}")
+    if n.fits != (dim, batch, dev):
+        _fit(n, dim, batch, dev)
+    if others is not None and others.fits != (dim, batch, dev):
+        _fit(others, dim, batch, dev)
     return dev, dim, batch, cu_ptr
+
+
+def _fit(h, dim: int, batch: int, dev: int):
+    if h.dim not in (None, dim) or h.batch not in (None, batch) or h.dev not in (None, dev):
+        raise ValueError(f"vectors for dim {h.dim}, batch {h.batch} on device {h.dev}; rows have dim {dim}, batch {batch} "
+                         f"on device {dev}")
 
 
 def hilo_norm_residual(n: hilo_norms, y, x, x_out, h, cu, text_len: int = 0, *, h_scale=None, stats=None, stream=None):
@@ -595,7 +603,7 @@ def hilo_norm_residual_workspace_bytes(rows: int, batch: int, dim: int) -> int:
 def hilo_norm_residual_backward(n: hilo_norms, dx_out, dh, y, x_out, stats, dx, dy, grads: Optional[hilo_norm_grads],
                                 cu, text_len: int = 0, workspace=None, stream=None):
     """Gradients of hilo_norm_residual from dx_out (or None) and dh (or None): dx, dy, and those in grads."""
-    dev, dim, batch, cu_ptr = _norm_rows(n, dx, cu, (grads,))
+    dev, dim, batch, cu_ptr = _norm_rows(n, dx, cu, grads)
     shape, rows, f32 = dx.shape, dx.shape[0], torch.float32
     like = dh if dh is not None else y
     if like is None:
@@ -673,6 +681,8 @@ def hilo_linear_i8(w, x, out, cu, text_len: int = 0, *, x_scale=None, act: int =
         raise HiloError("hilo_linear_i8", 1)
     if workspace.get_device() != dev or not workspace.is_contiguous():
         raise ValueError("workspace: contiguous, on the tensors' device")
+    if out.dim() != 2:
+        raise ValueError("out: expected [rows][out]")
     rows = out.shape[0]
     n, k = w.shape
     batch, cu_ptr = _packed(cu, dev)

@@ -34,7 +34,7 @@ def rope(r=None, dtype=hilo.BF16, x=F, ldx=256, pos=F, rows=4, out=F, ldo=256, *
     (dict(dtype=2), DTYPE), (dict(x=None), NULL), (dict(pos=None), NULL), (dict(out=None), NULL), (dict(heads=0), SHAPE),
     (dict(head_dim=127), SHAPE), (dict(head_dim=258, ldx=1000, ldo=1000), SHAPE), (dict(axes=0), SHAPE), (dict(axes=5), SHAPE),
     (dict(flags=4), PARAM), (dict(pairs=-1), PARAM), (dict(pairs=17), SHAPE), (dict(base=0.0), PARAM),
-    (dict(base=float("nan")), PARAM), (dict(base=float("inf")), PARAM), (dict(rows=-1), SHAPE), (dict(rows=1 << 28), SHAPE),
+    (dict(base=float("nan")), PARAM), (dict(base=float("inf")), PARAM), (dict(rows=-1), SHAPE), (dict(rows=1 << 24), SHAPE),
     (dict(ldx=255), SHAPE), (dict(ldo=255, out=F * 2), SHAPE), (dict(ldo=300), PARAM), (dict(x=F + 1), PARAM),
     (dict(pos=F + 2), PARAM), (dict(out=F + 3), PARAM), (dict(heads=1 << 20, ldx=1 << 27, ldo=1 << 27), SHAPE), (dict(rows=0), 0)])
 def test_rope_refusals(kw, status):
@@ -73,7 +73,7 @@ def norm(dtype=hilo.BF16, y=F, x=F, x_out=F, h=F, h_scale=None, stats=None, rows
 
 
 BAD_NORMS = [(dict(dtype=7), DTYPE), (dict(dim=0), SHAPE), (dict(dim=66), SHAPE), (dict(dim=8196), SHAPE), (dict(rows=-1), SHAPE),
-             (dict(rows=1 << 28), SHAPE), (dict(batch=0), SHAPE), (dict(text=-1), SHAPE), (dict(text=5), SHAPE), (dict(kind=2), PARAM),
+             (dict(rows=1 << 24), SHAPE), (dict(batch=0), SHAPE), (dict(text=-1), SHAPE), (dict(text=5), SHAPE), (dict(kind=2), PARAM),
              (dict(eps=-1.0), PARAM), (dict(eps=float("nan")), PARAM), (dict(residual_scale=float("inf")), PARAM),
              (dict(mod_stride=60), PARAM), (dict(mod_stride=66), PARAM), (dict(gate=F + 4), PARAM), (dict(scale=F + 8), PARAM),
              (dict(pre_gain=F + 4), PARAM), (dict(cu=None), NULL)]
@@ -84,7 +84,7 @@ BAD_NORMS = [(dict(dtype=7), DTYPE), (dict(dim=0), SHAPE), (dict(dim=66), SHAPE)
     (dict(x=None), NULL), (dict(y=None), NULL), (dict(x_out=None), NULL), (dict(y=None, x_out=None, h=None), NULL),
     (dict(h=None, h_scale=F), NULL), (dict(x=F + 8), PARAM), (dict(x_out=F + 4), PARAM), (dict(y=F + 4), PARAM),
     (dict(h=F + 4), PARAM), (dict(h=F + 2, h_scale=F), PARAM), (dict(stats=F + 8), PARAM), (dict(dtype=hilo.F32, y=F + 8), PARAM),
-    (dict(rows=0, text=0), 0)])
+    (dict(rows=0, text=0), 0), (dict(rows=0, text=0, x=None, y=None, x_out=None, h=None), 0)])
 def test_norm_refusals(kw, status):
     assert norm(**kw) == status
 
@@ -109,7 +109,8 @@ def norm_back(dtype=hilo.BF16, dx_out=F, dh=F, y=F, x_out=F, stats=F, dx=F, dy=F
     (dict(x_out=None), NULL), (dict(ws=None), NULL), (dict(ws_bytes=10), WORKSPACE), (dict(ws=F + 4), PARAM), (dict(dx=F + 4), PARAM),
     (dict(dy=F + 4), PARAM), (dict(dh=F + 2), PARAM), (dict(stats=F + 4), PARAM), (dict(dx_out=F + 4), PARAM),
     (dict(grad_stride=60), PARAM), (dict(grad_stride=70), PARAM), (dict(grad_gate=F + 4), PARAM), (dict(grad_gain=F + 4), PARAM),
-    (dict(rows=0, text=0, grads=False), 0)])
+    (dict(rows=0, text=0, grads=False), 0), (dict(rows=0, text=0, ws=None), NULL),
+    (dict(rows=0, text=0, grads=False, ws=None, dx=None, dy=None, stats=None, dh=None, y=None, x_out=None), 0)])
 def test_norm_backward_refusals(kw, status):
     assert norm_back(**kw) == status
 
@@ -117,7 +118,7 @@ def test_norm_backward_refusals(kw, status):
 @built
 @pytest.mark.parametrize("args,status", [
     ((3, F, 4, 64, None, F, F), DTYPE), ((0, F, -1, 64, None, F, F), SHAPE), ((0, F, 4, 0, None, F, F), SHAPE),
-    ((0, F, 4, 72, None, F, F), SHAPE), ((0, F, 4, 65552, None, F, F), SHAPE), ((0, F, 1 << 28, 64, None, F, F), SHAPE),
+    ((0, F, 4, 72, None, F, F), SHAPE), ((0, F, 4, 65552, None, F, F), SHAPE), ((0, F, 1 << 24, 64, None, F, F), SHAPE),
     ((0, None, 4, 64, None, F, F), NULL), ((0, F, 4, 64, None, None, F), NULL), ((0, F, 4, 64, None, F, None), NULL),
     ((0, F + 8, 4, 64, None, F, F), PARAM), ((0, F, 4, 64, None, F + 4, F), PARAM), ((0, F, 4, 64, None, F, F + 2), PARAM),
     ((0, F, 0, 64, None, F, F), 0)])
@@ -133,12 +134,14 @@ def linear(dtype=hilo.BF16, w0=(F, F, F), w1=(F, F, F), x=F, x_scale=None, out=F
 
 @built
 @pytest.mark.parametrize("kw,status", [
-    (dict(dtype=2), DTYPE), (dict(rows=-1), SHAPE), (dict(rows=1 << 28), SHAPE), (dict(batch=0), SHAPE), (dict(text=-1), SHAPE),
+    (dict(dtype=2), DTYPE), (dict(rows=-1), SHAPE), (dict(rows=1 << 24), SHAPE), (dict(batch=0), SHAPE), (dict(text=-1), SHAPE),
     (dict(text=5), SHAPE), (dict(k=0), SHAPE), (dict(k=72), SHAPE), (dict(k=65552), SHAPE), (dict(n=0), SHAPE), (dict(n=66), SHAPE),
-    (dict(n=(1 << 24) + 4), SHAPE), (dict(act=2), PARAM), (dict(x=None), NULL), (dict(out=None), NULL), (dict(cu=None), NULL),
+    (dict(n=1 << 24), SHAPE), (dict(n=(1 << 24) - 4, rows=(1 << 24) - 1), SHAPE), (dict(batch=(1 << 20) + 1, rows=1 << 23), SHAPE),
+    (dict(act=2), PARAM), (dict(x=None), NULL), (dict(out=None), NULL), (dict(cu=None), NULL),
     (dict(ws=None), NULL), (dict(w0=(None, F, F)), NULL), (dict(w1=(F, None, F)), NULL), (dict(w0=(F + 8, F, F)), PARAM),
     (dict(w1=(F, F + 4, F)), PARAM), (dict(w0=(F, F, F + 4)), PARAM), (dict(x=F + 8), PARAM), (dict(x_scale=F + 2), PARAM),
-    (dict(out=F + 4), PARAM), (dict(ws=F + 16), PARAM), (dict(ws_bytes=100), WORKSPACE), (dict(rows=0, text=0), 0)])
+    (dict(out=F + 4), PARAM), (dict(ws=F + 16), PARAM), (dict(ws_bytes=100), WORKSPACE), (dict(rows=0, text=0), 0),
+    (dict(rows=0, text=0, x=None, out=None, ws=None, ws_bytes=0), 0)])
 def test_linear_refusals(kw, status):
     assert linear(**kw) == status
 

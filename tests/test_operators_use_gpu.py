@@ -1,0 +1,379 @@
+"""The rotary, sandwich-norm and int8 operators as programs use them: together as a block on a compressed sequence, captured
+into graphs, on several streams, with nothing to do, past 32-bit offsets, and what the binding refuses of device tensors."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import hilo_operators as Q
+from oracle import hilo_oracle as O
+from paper_2606_13898_amd import hilo
+
+pytestmark = pytest.mark.gpu
+
+E = 2.0 ** -24
+BF, F32, I8, I32 = torch.bfloat16, torch.float32, torch.int8, torch.int32
+
+
+def _cu(*ends):
+    return torch.tensor([0, *ends], dtype=I32, device="cuda")
+
+
+def _empty(*shape, dtype=F32):
+    return torch.empty(*shape, dtype=dtype, device="cuda")
+
+
+def _np(t):
+    return t.detach().cpu().double().numpy()
+
+
+# --------------------------------------------------------------------------------------- the block
+
+class Block:
+    """A block with rotary positions, norms on both sides of its halves and int8 projections, on the tokens of a
+    compressed batch: the calls of a program, and the same block in float64."""
+
+    def __init__(self, seed, heads, hd, grid, text, mlp):
+        g = np.random.default_rng(seed)
+        self.B, self.H, self.W, self.L = 2, *grid, text
+        self.heads, self.hd, self.D, self.F = heads, hd, heads * hd, mlp
+        D, B = self.D, self.B
+        self.shape = hilo.hilo_shape(B, 1, self.H, self.W, text, D, heads, hd, mlp, hilo.BF16)
+        t = lambda a, dt=F32: torch.from_numpy(np.asarray(a, np.float32)).to(dt).cuda()  # noqa: E731
+        self.x_img, self.x_txt = t(g.standard_normal((B, self.H * self.W, D)), BF), t(g.standard_normal((B, text, D)), BF)
+        self.mod = t(g.standard_normal((B, 2, 6, D)) * 0.3)
+        self.gains = t(1 + 0.2 * g.standard_normal((4, 2, D)))  # pre 1, post 1, pre 2, post 2
+        dims = dict(qkv=(3 * D, D), o=(D, D), up=(mlp, D), down=(D, mlp))
+        self.w = {k: [hilo.quantize_i8_weights(t(g.standard_normal(s) * s[1] ** -0.5, BF), t(g.standard_normal(s[0]) * 0.1, BF))
+                      for _ in range(2)] for k, s in dims.items()}
+        self.plan = {k: hilo.linear_weights_i8(v) for k, v in self.w.items()}
+        m, ga = self.mod, self.gains
+        self.norm1 = hilo.norms(hilo.NORM_LAYER, shift=m[:, :, 0], scale=m[:, :, 1], pre_gain=ga[0])
+        self.norm2 = hilo.norms(hilo.NORM_LAYER, residual_scale=0.9, gate=m[:, :, 2], shift=m[:, :, 3], scale=m[:, :, 4],
+                                post_gain=ga[1], pre_gain=ga[2])
+        self.norm3 = hilo.norms(hilo.NORM_LAYER, residual_scale=0.9, gate=m[:, :, 5], post_gain=ga[3])
+        n = hd // 2
+        self.pairs = (n // 4, (n - n // 4) // 2, n - n // 4 - (n - n // 4) // 2)
+        self.rotary = hilo.rotary(2 * heads, hd, self.pairs, 10000.0, hilo.ROPE_ADJACENT)
+        T = self.T = hilo.hilo_max_tokens(self.shape)
+        G, N = B, self.H * self.W
+        self.energy, self.cu, self.seg = _empty(G, N, dtype=torch.int64), _empty(B + 1, dtype=I32), _empty(G, dtype=I32)
+        self.idx, self.fine, self.pool = _empty(G, N, dtype=I32), _empty(G, N, dtype=I32), _empty(G, N // 4, dtype=I32)
+        self.counts, self.pos = _empty(G, 2, dtype=I32), _empty(T, 3)
+        self.z, self.codes, self.scale = _empty(T, D), _empty(T, D, dtype=I8), _empty(T)
+        self.qkv, self.a, self.o = _empty(T, 3 * D, dtype=BF), _empty(T, D, dtype=BF), _empty(T, D, dtype=BF)
+        self.up, self.d = _empty(T, mlp, dtype=BF), _empty(T, D, dtype=BF)
+        self.ws = _empty(max(hilo.hilo_linear_i8_workspace_bytes(T, k) for k in (D, mlp)), dtype=torch.uint8)
+        self.core_ws = _empty(hilo.hilo_workspace_bytes(self.shape), dtype=torch.uint8)
+        self.y_img, self.y_txt = torch.empty_like(self.x_img), torch.empty_like(self.x_txt)
+
+    def front(self, keep):
+        h = hilo
+        h.hilo_score(self.shape, self.x_img, self.energy)
+        h.hilo_select(self.shape, self.energy, None, 0, h.TOPK, None, keep, self.idx, self.fine, self.pool, self.counts,
+                      self.cu, self.seg)
+
+    def run(self):
+        h, cu, L, D = hilo, self.cu, self.L, self.D
+        h.hilo_compress(self.shape, self.x_img, self.x_txt, self.fine, self.pool, self.counts, cu, self.seg, self.z)
+        h.hilo_token_positions(self.shape, self.fine, self.pool, self.counts, cu, self.seg, None, self.pos)
+        h.hilo_norm_residual(self.norm1, None, self.z, None, self.codes, cu, L, h_scale=self.scale)
+        h.hilo_linear_i8(self.plan["qkv"], self.codes, self.qkv, cu, L, x_scale=self.scale, workspace=self.ws)
+        qk = self.qkv[:, :2 * D]
+        h.hilo_rope(self.rotary, qk, self.pos, qk, cu)
+        h.hilo_attention_core(self.shape, self.qkv, cu, self.a, self.core_ws)
+        h.hilo_linear_i8(self.plan["o"], self.a, self.o, cu, L, workspace=self.ws)
+        h.hilo_norm_residual(self.norm2, self.o, self.z, self.z, self.codes, cu, L, h_scale=self.scale)
+        h.hilo_linear_i8(self.plan["up"], self.codes, self.up, cu, L, x_scale=self.scale, act=h.ACT_GELU, workspace=self.ws)
+        h.hilo_linear_i8(self.plan["down"], self.up, self.d, cu, L, workspace=self.ws)
+        h.hilo_norm_residual(self.norm3, self.d, self.z, self.z, None, cu, L)
+        h.hilo_decompress(self.shape, self.z, self.idx, cu, self.seg, self.y_img, self.y_txt)
+
+    def reference(self):
+        """z before and after, of the tokens in use."""
+        cu, L, D = self.cu.cpu().numpy(), self.L, self.D
+        z = torch.empty(self.T, D, device="cuda")
+        hilo.hilo_compress(self.shape, self.x_img, self.x_txt, self.fine, self.pool, self.counts, self.cu, self.seg, z)
+        n, m, ga = int(cu[-1]), _np(self.mod), _np(self.gains)
+        z0 = _np(z)[:n]
+        w = {k: [{"w": s["w"].cpu().numpy(), "s": _np(s["s"]), "b": _np(s["b"])} for s in v] for k, v in self.w.items()}
+
+        def linear(x, k, gelu=False):
+            c, s = Q.quantize_rows_i8(x.astype(np.float32))
+            return Q.linear_i8(c, s, w[k], cu, L, gelu)[0]
+
+        pos = Q.token_positions(self.B, 1, self.W, L, self.fine.cpu().numpy(), self.pool.cpu().numpy(), self.counts.cpu().numpy())
+        _, h, _ = Q.norm_residual(None, z0, cu, L, shift=m[:, :, 0], scale=m[:, :, 1], pre_gain=ga[0])
+        qkv = linear(h, "qkv")
+        qkv[:, :2 * D] = Q.rope(qkv[:, :2 * D], pos, 2 * self.heads, self.pairs, 10000.0, adjacent=True)
+        o = linear(O.attention_core(qkv, cu, self.heads), "o")
+        z1, h, _ = Q.norm_residual(o, z0, cu, L, alpha=0.9, gate=m[:, :, 2], shift=m[:, :, 3], scale=m[:, :, 4],
+                                   post_gain=ga[1], pre_gain=ga[2])
+        d = linear(linear(h, "up", True), "down")
+        return z0, Q.norm_residual(d, z1, cu, L, alpha=0.9, gate=m[:, :, 5], post_gain=ga[3])[0]
+
+
+# A row's largest of 256 .. 1024 normal values is 3 to 3.3 deviations, so a code is a step of 0.025 of one.  The device's
+# bf16 rows (and the sums before them) are off by about 2^-9 of a value, which changes about 1 code in 13 by one step: 0.7%
+# of a product's operand, and 0.3% for the rounding of its result; four products in a row, two of them behind the
+# attention or the GELU: below 2% of the update in the root mean square.  A wrong code, scale, column, row or position is
+# an error of the size of the update.
+@pytest.mark.parametrize("heads,hd,grid,text,mlp,keep", [(2, 128, (8, 12), 5, 1024, [3, 20]), (4, 64, (16, 10), 33, 528 + 48, [0, 40])])
+def test_block(heads, hd, grid, text, mlp, keep):
+    print(f"[block] heads={heads} hd={hd} grid={grid} text={text} mlp={mlp}", flush=True)
+    b = Block(heads, heads, hd, grid, text, mlp)
+    b.front(keep)
+    b.run()
+    torch.cuda.synchronize()
+    z0, want = b.reference()
+    n = len(want)
+    got = _np(b.z)[:n]
+    assert np.isfinite(got).all()
+    off = np.linalg.norm(got - want) / np.linalg.norm(want - z0)
+    assert off <= 2e-2, off
+    assert np.abs(_np(b.y_img)).max() < 50 and np.isfinite(_np(b.y_txt)).all()
+
+
+# ---------------------------------------------------------------------------------- graphs, streams
+
+def _replays(body, inputs, outputs, rounds=3):
+    """body() captured once, then replayed on fresh inputs with eager work in between: equal bits to eager calls."""
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        body()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        body()
+    for r in range(rounds):
+        g = torch.Generator(device="cuda").manual_seed(r)
+        for t in inputs:
+            t.copy_(torch.randn(t.shape, generator=g, device="cuda"))
+        for t in outputs:
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in outputs]
+        for t in outputs:
+            t.zero_()
+        body()
+        torch.cuda.synchronize()
+        for i, (a, b) in enumerate(zip(got, outputs)):
+            assert torch.equal(a, b), f"replay {r}, output {i}"
+            assert a.float().abs().max() > 0
+
+
+# few rows, small rows, tiles with and without K pieces (whose fixup is a second launch), codes and float rows
+@pytest.mark.parametrize("rows,K,N", [(2, 256, 96), (40, 2064, 100), (200, 128, 64), (500, 8336, 2040), (700, 1040, 512)])
+def test_linear_i8_graph(rows, K, N):
+    print(f"[graph] linear {rows} x {K} x {N}", flush=True)
+    w = hilo.quantize_i8_weights(torch.randn(N, K, device="cuda").to(BF), torch.randn(N, device="cuda").to(BF))
+    plan, cu = hilo.linear_weights_i8([w]), _cu(rows // 2, rows)
+    x, out = _empty(rows, K, dtype=BF).normal_(), _empty(rows, N, dtype=BF)
+    ws = _empty(hilo.hilo_linear_i8_workspace_bytes(rows, K), dtype=torch.uint8)
+    _replays(lambda: hilo.hilo_linear_i8(plan, x, out, cu, workspace=ws), [x], [out])
+
+
+@pytest.mark.parametrize("batch", [1, 3])
+def test_norm_and_rope_graph(batch):
+    T, D = 30 * batch, 512
+    cu = _cu(*[30 * (i + 1) for i in range(batch)])
+    y, x, dxo, dh = (_empty(T, D).normal_() for _ in range(4))
+    mod, gain, pos = _empty(batch, 2, 3, D).normal_(), _empty(2, 2, D).normal_(), _empty(T, 2).normal_()
+    xo, h, dx, dy, turned = (_empty(T, D) for _ in range(5))
+    stats, dmod, dgain = _empty(T, 4), _empty(batch, 2, 3, D), _empty(2, 2, D)
+    n = hilo.norms(gate=mod[:, :, 0], shift=mod[:, :, 1], scale=mod[:, :, 2], post_gain=gain[0], pre_gain=gain[1])
+    g = hilo.norm_grads(gate=dmod[:, :, 0], shift=dmod[:, :, 1], scale=dmod[:, :, 2], post_gain=dgain[0], pre_gain=dgain[1])
+    ws = _empty(hilo.hilo_norm_residual_workspace_bytes(T, batch, D), dtype=torch.uint8)
+    r = hilo.rotary(8, 64, (16, 16))
+
+    def body():
+        hilo.hilo_norm_residual(n, y, x, xo, h, cu, 4, stats=stats)
+        hilo.hilo_norm_residual_backward(n, dxo, dh, y, xo, stats, dx, dy, g, cu, 4, ws)
+        hilo.hilo_rope(r, h, pos, turned, cu)
+
+    _replays(body, [y, x, dxo, dh, mod, gain, pos], [xo, h, dx, dy, turned, stats, dmod, dgain])
+
+
+def test_two_streams():
+    """The same handles on two streams at once, each with buffers and a workspace of its own, and on a stream given by
+    name: the bits of one after the other."""
+    D, N, rows = 1040, 1024, 500
+    w = hilo.quantize_i8_weights(torch.randn(N, D, device="cuda"), torch.randn(N, device="cuda"))
+    plan, cu = hilo.linear_weights_i8([w]), _cu(rows)
+    mod = _empty(1, 2, 3, D).normal_()
+    n = hilo.norms(gate=mod[:, :, 0], shift=mod[:, :, 1], scale=mod[:, :, 2])
+    g = [hilo.norm_grads(gate=_empty(1, 2, D), shift=_empty(1, 2, D), scale=_empty(1, 2, D)) for _ in range(2)]
+    sets = []
+    for k in range(2):
+        t = dict(y=_empty(rows, D).normal_(), x=_empty(rows, D).normal_(), dh=_empty(rows, D).normal_())
+        t |= {k2: _empty(rows, D) for k2 in ("xo", "h", "dx", "dy")}
+        t |= dict(stats=_empty(rows, 4), out=_empty(rows, N), ws=_empty(hilo.hilo_linear_i8_workspace_bytes(rows, D), dtype=torch.uint8),
+                  nws=_empty(hilo.hilo_norm_residual_workspace_bytes(rows, 1, D), dtype=torch.uint8), g=g[k])
+        sets.append(t)
+
+    def body(t, stream=None):
+        hilo.hilo_norm_residual(n, t["y"], t["x"], t["xo"], t["h"], cu, stats=t["stats"], stream=stream)
+        hilo.hilo_linear_i8(plan, t["h"], t["out"], cu, workspace=t["ws"], stream=stream)
+        hilo.hilo_norm_residual_backward(n, None, t["dh"], t["y"], t["xo"], t["stats"], t["dx"], t["dy"], t["g"], cu, 0,
+                                         t["nws"], stream=stream)
+
+    def results(t):
+        return [t[k] for k in ("xo", "h", "out", "dx", "dy")] + [t["g"].kept[0][k] for k in ("gate", "shift", "scale")]
+
+    for t in sets:
+        body(t)
+    torch.cuda.synchronize()
+    want = [[r.clone() for r in results(t)] for t in sets]
+    for t in sets:
+        for r in results(t):
+            r.zero_()
+    torch.cuda.synchronize()
+    a, b = torch.cuda.Stream(), torch.cuda.Stream()
+    for _ in range(3):
+        with torch.cuda.stream(a):
+            body(sets[0])
+        body(sets[1], stream=b)
+    torch.cuda.synchronize()
+    for t, ws in zip(sets, want):
+        for r, w0 in zip(results(t), ws):
+            assert torch.equal(r, w0)
+
+
+# ---------------------------------------------------------------------------------- nothing to do
+
+def test_no_rows_in_use():
+    """Boundaries that all are 0 leave every buffer alone; sums over no rows are 0."""
+    D, N = 256, 64
+    cu = _cu(0, 0)
+    w = hilo.linear_weights_i8([hilo.quantize_i8_weights(torch.randn(N, D, device="cuda"))])
+    mod, dmod = _empty(2, 2, 3, D).normal_(), torch.full((2, 2, 3, D), 9.0, device="cuda")
+    n = hilo.norms(gate=mod[:, :, 0], shift=mod[:, :, 1], scale=mod[:, :, 2])
+    g = hilo.norm_grads(gate=dmod[:, :, 0], shift=dmod[:, :, 1], scale=dmod[:, :, 2])
+    r = hilo.rotary(4, 64, (32,))
+    for rows in (0, 2, 40, 300):
+        print(f"[empty] {rows} rows", flush=True)
+        x, y = torch.randn(rows, D, device="cuda"), torch.randn(rows, D, device="cuda")
+        keep = lambda *s, dtype=F32: torch.full(s, 9, dtype=dtype, device="cuda")  # noqa: E731
+        xo, h, dx, dy, out, stats = (keep(rows, c) for c in (D, D, D, D, N, 4))
+        codes, scale = keep(rows, D, dtype=I8), keep(rows)
+        ws = _empty(max(256, hilo.hilo_linear_i8_workspace_bytes(rows, D)), dtype=torch.uint8)
+        nws = _empty(hilo.hilo_norm_residual_workspace_bytes(rows, 2, D), dtype=torch.uint8)
+        hilo.hilo_norm_residual(n, y, x, xo, h, cu, stats=stats)
+        hilo.hilo_norm_residual(n, y, x, xo, codes, cu, h_scale=scale)
+        hilo.hilo_norm_residual_backward(n, x, y, y, x, stats, dx, dy, g, cu, 0, nws)
+        hilo.hilo_quantize_rows_i8(x, codes, scale, cu)
+        hilo.hilo_linear_i8(w, x, out, cu, workspace=ws)
+        hilo.hilo_linear_i8(w, codes, out, cu, x_scale=scale, workspace=ws)
+        hilo.hilo_rope(r, x, torch.zeros(rows, 1, device="cuda"), dx, cu)
+        torch.cuda.synchronize()
+        assert all((t == 9).all() for t in (xo, h, dx, dy, out, stats, codes, scale))
+        assert (dmod == 0).all()
+        dmod.fill_(9.0)
+
+
+# ---------------------------------------------------------------------------------- past 32 bits
+
+def test_offsets_past_32_bits():
+    """Rows behind the first 2^31 values of a tensor."""
+    rows, D = 265000, 8192
+    last = slice(rows - 3, rows)
+    cu = _cu(rows - 3, rows)
+    x, y = torch.zeros(rows, D, dtype=F32, device="cuda"), torch.zeros(rows, D, dtype=BF, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(0)
+    x[last] = torch.randn(3, D, generator=g, device="cuda")
+    y[last] = torch.randn(3, D, generator=g, device="cuda").to(BF)
+    xo, h = torch.empty_like(x), torch.empty_like(y)
+    stats = _empty(rows, 4)
+    n = hilo.norms(hilo.NORM_RMS, 1e-6, 0.5)
+    hilo.hilo_norm_residual(n, y, x, xo, h, cu, stats=stats)
+    torch.cuda.synchronize()
+    wx, wh, _ = Q.norm_residual(_np(y[last]), _np(x[last]), np.array([0, 3]), 0, True, 1e-6, 0.5)
+    np.testing.assert_allclose(_np(xo[last]), wx, rtol=0, atol=256 * E * 8)
+    np.testing.assert_allclose(_np(h[last]), wh, rtol=2.0 ** -8 + 256 * E, atol=256 * E * 8)
+    x0, y0 = _np(x[last]), _np(y[last])
+    hilo.hilo_norm_residual_backward(n, x, h, y, xo, stats, x, y, None, cu)  # in place
+    torch.cuda.synchronize()
+    dx, dy, _ = Q.norm_residual_backward(x0, _np(h[last]), y0, _np(xo[last]), np.array([0, 3]), 0, True, 1e-6, 0.5)
+    np.testing.assert_allclose(_np(x[last]), dx, rtol=0, atol=256 * E * 8)
+    np.testing.assert_allclose(_np(y[last]), dy, rtol=2.0 ** -8 + 256 * E, atol=256 * E * 8)
+    del xo, y
+    # rope of the same rows, and a product whose output passes 2^31 values
+    r = hilo.rotary(64, 128, (64,))
+    pos = torch.arange(rows, device="cuda", dtype=F32)[:, None]
+    before = _np(x[last])
+    hilo.hilo_rope(r, x, pos, x)
+    torch.cuda.synchronize()
+    turned = Q.rope(before, _np(pos[last]), 64, (64,))
+    np.testing.assert_allclose(_np(x[last]), turned, rtol=0, atol=8 * E * 2 * np.abs(before).max())
+    del x, h
+    K, N = 64, 8448
+    a = torch.randn(rows, K, generator=g, device="cuda").to(BF)
+    w = hilo.quantize_i8_weights(torch.randn(N, K, generator=g, device="cuda"))
+    out = _empty(rows, N, dtype=BF)
+    ws = _empty(hilo.hilo_linear_i8_workspace_bytes(rows, K), dtype=torch.uint8)
+    hilo.hilo_linear_i8(hilo.linear_weights_i8([w]), a, out, cu, workspace=ws)
+    torch.cuda.synchronize()
+    c, s = Q.quantize_rows_i8(a[last].float().cpu().numpy())
+    want, size = Q.linear_i8(c, s, [{"w": w["w"].cpu().numpy(), "s": _np(w["s"]), "b": None}], np.array([0, 3]), 0)
+    np.testing.assert_array_less(np.abs(_np(out[last]) - want), 2.0 ** -8 * np.abs(want) + 4 * E * size + 1e-30)
+
+
+# ---------------------------------------------------------------------------------- refusals
+
+def test_binding_refuses_device_tensors():
+    """Wrong types, shapes, layouts and devices raise before anything is enqueued."""
+    T, D, N = 8, 64, 32
+    x, y, cu = torch.zeros(T, D, device="cuda"), torch.zeros(T, D, device="cuda", dtype=BF), _cu(T)
+    f = lambda *s, dtype=F32: torch.zeros(*s, dtype=dtype, device="cuda")  # noqa: E731
+    n, r = hilo.norms(), hilo.rotary(1, 64, (32,))
+    ws = f(4096, dtype=torch.uint8)
+    w = hilo.linear_weights_i8([{"w": f(N, D, dtype=I8), "s": f(N), "b": f(N, dtype=BF)}])
+    bad = [
+        lambda: hilo.hilo_norm_residual(n, y, x, f(T, D), f(T, D), cu),                  # h of another type than y
+        lambda: hilo.hilo_norm_residual(n, y, x, f(T, D + 4), f(T, D, dtype=BF), cu),
+        lambda: hilo.hilo_norm_residual(n, y, x, f(T, 2 * D)[:, :D], f(T, D, dtype=BF), cu),
+        lambda: hilo.hilo_norm_residual(n, y, x, x, y, cu.long()),
+        lambda: hilo.hilo_norm_residual(n, y, x, x, y, cu.cpu()),
+        lambda: hilo.hilo_norm_residual(n, y.cpu(), x, x, y, cu),
+        lambda: hilo.hilo_norm_residual(n, y.half(), x, x, y.half(), cu),
+        lambda: hilo.hilo_norm_residual(n, y, x, x, y, cu, stats=f(T, 3)),
+        lambda: hilo.hilo_norm_residual(n, y, x, x, y, cu, h_scale=f(T)),                # codes are int8
+        lambda: hilo.hilo_norm_residual(hilo.norms(gate=f(2, 2, D)), y, x, x, y, cu),    # vectors of another batch
+        lambda: hilo.hilo_norm_residual(hilo.norms(post_gain=f(2, D + 4)), y, x, x, y, cu),
+        lambda: hilo.norms(gate=f(1, 2, D), shift=f(1, 2, 2 * D)[:, :, :D]),             # spaced differently
+        lambda: hilo.norms(gate=f(2, 3, D)[:, :2]),                                      # unevenly spaced
+        lambda: hilo.hilo_norm_residual_backward(n, x, y, y, x, f(T, 4), x, f(T, D), None, cu),
+        lambda: hilo.hilo_norm_residual_backward(n, x, y, y, x, f(T, 4), x, y, hilo.norm_grads(gate=f(2, 2, D)), cu, 0, ws),
+        lambda: hilo.hilo_rope(r, x, f(T, 2), x),
+        lambda: hilo.hilo_rope(r, x, f(T, 1), f(T, D, dtype=BF)),
+        lambda: hilo.hilo_rope(r, f(D, T).T, f(T, 1), x),
+        lambda: hilo.hilo_rope(hilo.rotary(2, 64, (32,)), x, f(T, 1), x),
+        lambda: hilo.hilo_rope(r, x, f(T, 1).cpu(), x),
+        lambda: hilo.hilo_quantize_rows_i8(x, f(T, D, dtype=torch.uint8), f(T)),
+        lambda: hilo.hilo_quantize_rows_i8(x, f(T, D, dtype=I8), f(T + 1)),
+        lambda: hilo.hilo_linear_i8(w, y, f(T, N), cu, workspace=ws),                    # out float32, bias bf16
+        lambda: hilo.hilo_linear_i8(w, x, f(T, N, dtype=BF), cu, workspace=ws),          # x of another type than out
+        lambda: hilo.hilo_linear_i8(w, f(T, D, dtype=I8), f(T, N, dtype=BF), cu, workspace=ws),
+        lambda: hilo.hilo_linear_i8(w, y, f(T, N + 4, dtype=BF), cu, workspace=ws),
+        lambda: hilo.hilo_linear_i8(w, y, f(T, N, dtype=BF), cu, workspace=ws.cpu()),
+        lambda: hilo.linear_weights_i8([{"w": f(N, D, dtype=I8), "s": f(N + 4)}]),
+        lambda: hilo.linear_weights_i8([{"w": f(N, D, dtype=I8), "s": f(N)}, {"w": f(N, D + 16, dtype=I8), "s": f(N)}]),
+    ]
+    for i, call in enumerate(bad):
+        with pytest.raises(ValueError):
+            call()
+            pytest.fail(f"call {i} was not refused")
+    status = [
+        (lambda: hilo.hilo_norm_residual(n, None, x, None, None, cu), 1),
+        (lambda: hilo.hilo_norm_residual(n, y, x, None, y, cu), 1),
+        (lambda: hilo.hilo_norm_residual(n, y, x, x, y, cu, 9), 2),                      # more text than rows
+        (lambda: hilo.hilo_linear_i8(w, y, f(T, N, dtype=BF), cu, workspace=None), 1),
+        (lambda: hilo.hilo_linear_i8(w, y, f(T, N, dtype=BF), cu, workspace=ws[:256]), 5),
+        (lambda: hilo.hilo_linear_i8(w, y, f(T, N, dtype=BF), cu, act=3, workspace=ws), 4),
+    ]
+    for call, want in status:
+        with pytest.raises(hilo.HiloError) as e:
+            call()
+        assert e.value.status == want
+    torch.cuda.synchronize()
