@@ -459,7 +459,7 @@ hilo_status hilo_norm_residual_backward(int32_t dtype, const hilo_norms *norms, 
 size_t hilo_norm_residual_workspace_bytes(int64_t rows, int32_t batch, int32_t dim); /* 0 if invalid */
 
 /* Per-row int8 quantisation of x [rows][cols] dtype (every step one float32 operation):
- *   amax = max |x|;  inv = 127 / amax;  code = round-to-nearest-even(clamp(x * inv, -127, 127));
+ *   amax = max |x|;  inv = (1 / amax) * 127;  code = round-to-nearest-even(clamp(x * inv, -127, 127));
  *   scale = amax / 127
  * rows with amax < 2^-120 get codes and scale 0; a row that holds an infinity or a NaN gets a scale that is
  * not finite.  codes [rows][cols] int8, scale [rows] float32.  cols > 0, cols % 16 == 0, cols <= 65536.

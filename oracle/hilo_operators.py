@@ -127,7 +127,7 @@ def quantize_rows_i8(x):
     top = np.abs(x).max(1)
     ok = top >= np.float32(2.0 ** -120)
     inv = np.zeros_like(top)
-    inv[ok] = np.float32(127.0) / top[ok]
+    inv[ok] = (np.float32(1.0) / top[ok]) * np.float32(127.0)
     codes = np.rint(np.clip(x * inv[:, None], -127, 127).astype(np.float32))
     return codes.astype(np.int8), np.where(ok, top / np.float32(127.0), np.float32(0)).astype(np.float32)
 

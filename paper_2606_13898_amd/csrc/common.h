@@ -123,10 +123,10 @@ HILO_DEV uint32_t wave_max_u32(uint32_t v) {
 // finite and nothing formed from it passes for a number.  Rows below 2^-120, whose inverse would overflow, count as 0.
 HILO_DEV uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7fffffffu; }
 HILO_DEV float i8_inverse(uint32_t top) {
-  return top < 0x03800000u || top >= 0x7f800000u ? 0.f : __fdiv_rn(127.0f, __uint_as_float(top));
+  return top < 0x03800000u || top >= 0x7f800000u ? 0.f : __fmul_rn(__fdiv_rn(1.0f, __uint_as_float(top)), 127.0f);
 }
 HILO_DEV float i8_scale(uint32_t top) { return top < 0x03800000u ? 0.f : __fdiv_rn(__uint_as_float(top), 127.0f); }
-// Codes of four values times the inverse, products at most 127 in magnitude (127 (1 + 2^-23) rounds to 127): adding
+// Codes of four values times the inverse, products at most 127 in magnitude (three roundings above it round to 127): adding
 // 1.5 * 2^23 rounds to a whole number, to nearest even, and leaves its low byte in the lowest bits; a NaN's is 0.
 HILO_DEV uint32_t i8x4(float a, float b, float c, float d, float inv) {
 #pragma clang fp contract(off)  // a product is rounded before it is made whole: that is what the codes are

@@ -455,11 +455,11 @@ def test_linear_i8(dtype, lens, text, K, N, gelu, bias):
     run_linear(dtype, lens, text, K, N, gelu, bias, K + N)
 
 
-def run_linear(dtype, lens, text, K, N, gelu, bias, seed, rows=None):
-    """hilo_linear_i8 on float rows and on their codes, `rows` of them (all) compared."""
+def run_linear(dtype, lens, text, K, N, gelu, bias, seed, rows=None, spare=3):
+    """hilo_linear_i8 on float rows and on their codes, `rows` of them (all) compared; `spare` rows behind the last."""
     g = torch.Generator().manual_seed(seed)
     cu, T = _cu(lens), int(sum(lens))
-    x = torch.randn(T + 3, K, generator=g).to(DT[dtype])
+    x = torch.randn(T + spare, K, generator=g).to(DT[dtype])
     ws, ref = [], []
     for _ in range(2):
         w = {"w": torch.randint(-127, 128, (N, K), dtype=torch.int8, generator=g), "s": (torch.rand(N, generator=g) + 0.5) * 1e-3,
@@ -467,9 +467,9 @@ def run_linear(dtype, lens, text, K, N, gelu, bias, seed, rows=None):
         ws.append({k: None if v is None else v.cuda() for k, v in w.items()})
         ref.append({k: None if v is None else v.numpy() if k == "w" else v.double().numpy() for k, v in w.items()})
     plan = hilo.linear_weights_i8(ws)
-    out = torch.full((T + 3, N), 9.0, dtype=DT[dtype], device="cuda")
+    out = torch.full((T + spare, N), 9.0, dtype=DT[dtype], device="cuda")
     act = hilo.ACT_GELU if gelu else hilo.ACT_NONE
-    wsp = torch.full((hilo.hilo_linear_i8_workspace_bytes(T + 3, K),), 255, dtype=torch.uint8, device="cuda")
+    wsp = torch.full((hilo.hilo_linear_i8_workspace_bytes(T + spare, K),), 255, dtype=torch.uint8, device="cuda")
     cud, xd = _dev(cu, torch.int32), x.cuda()
     hilo.hilo_linear_i8(plan, xd, out, cud, text, act=act, workspace=wsp)
     torch.cuda.synchronize()
@@ -483,12 +483,22 @@ def run_linear(dtype, lens, text, K, N, gelu, bias, seed, rows=None):
     _within(_np(out[torch.from_numpy(pick).cuda()]), want, _linear_bound(want, size, gelu, dtype), "linear")
     assert (out[T:] == 9).all()
     # codes in: the same bits
-    cd, sd = torch.empty(T + 3, K, dtype=torch.int8, device="cuda"), torch.empty(T + 3, device="cuda")
+    cd, sd = torch.empty(T + spare, K, dtype=torch.int8, device="cuda"), torch.empty(T + spare, device="cuda")
     hilo.hilo_quantize_rows_i8(xd, cd, sd)
     out2 = torch.full_like(out, 9.0)
     hilo.hilo_linear_i8(plan, cd, out2, cud, text, x_scale=sd, act=act, workspace=wsp)
     torch.cuda.synchronize()
     assert torch.equal(out, out2)
+
+
+# buffers of exactly these rows: the forms for one, two and up to four rows, up to 16, up to 64, and the first behind each
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("lens,text,K,N", [([1], 0, 1552, 100), ([1, 1], 0, 3072, 96), ([1, 1, 1], 1, 784, 64), ([3], 1, 12240, 36),
+                                           ([2, 1, 1], 0, 4096, 52), ([5], 2, 1024, 68), ([9, 7], 0, 2064, 36), ([17], 3, 896, 132),
+                                           ([40, 24], 7, 1168, 8260), ([65], 1, 1040, 72)])
+def test_linear_i8_few_rows(dtype, lens, text, K, N):
+    print(f"[linear i8 few] {dtype} lens={lens} text={text} K={K} N={N}", flush=True)
+    run_linear(dtype, lens, text, K, N, False, True, K, spare=0)
 
 
 # every kind of plan of the large tiles (linear_schedule.py says which each shape reaches), both types of output
