@@ -21,6 +21,10 @@ HILO_DEV float4 fma4(const float4 &a, const float4 &b, const float4 &c) {
   return make_float4(a.x * b.x + c.x, a.y * b.y + c.y, a.z * b.z + c.z, a.w * b.w + c.w);
 }
 HILO_DEV float4 zero4() { return make_float4(0.f, 0.f, 0.f, 0.f); }
+HILO_DEV float4 ones4() { return make_float4(1.f, 1.f, 1.f, 1.f); }
+HILO_DEV float4 shfl_xor4(const float4 &v, int m) {
+  return make_float4(__shfl_xor(v.x, m), __shfl_xor(v.y, m), __shfl_xor(v.z, m), __shfl_xor(v.w, m));
+}
 HILO_DEV float4 only(bool in, const float4 &v) {
   return make_float4(in ? v.x : 0.f, in ? v.y : 0.f, in ? v.z : 0.f, in ? v.w : 0.f);
 }
@@ -162,9 +166,7 @@ HILO_DEV NormShares norm_shares(const int *cu, int B, int rows, int P) {
 HILO_DEV int share_begin(const NormShares &q, int w) {
   return __builtin_amdgcn_readfirstlane(int(double(q.R) * double(w) / double(q.P)));
 }
-HILO_DEV int share_owner(const NormShares &q, int row) {
-  return __builtin_amdgcn_readfirstlane(int((double(row + 1) * double(q.P) - 1.0) / double(q.R)));
-}
+HILO_DEV int share_owner(const NormShares &q, int row) { return int((double(row + 1) * double(q.P) - 1.0) / double(q.R)); }
 
 // The segment of a row and where a share's rows leave it.
 struct RowSegment {
@@ -492,75 +494,74 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W, NV < 4 ? 3 : 2) void k_norm_
   }
 }
 
-// Sums the slots of one segment: blockIdx.x segment, blockIdx.y 64 columns, blockIdx.z which of A, B, C.  16 lanes of
-// four columns by 16 groups of slots, joined in group order.  A and B go on to the gains (sums: [2 B][2][D]), or with one
-// sample and a gain a stream are all there is to them (gains_here).
-__global__ __launch_bounds__(256) void k_norm_sums(NormBackProblem p, float *sums, bool gains_here) {
-  __shared__ float4 red[16][16];
-  const int seg = blockIdx.x, s = seg >> 1, sigma = seg & 1, which = blockIdx.z;
+// The sums over a stream's slots: blockIdx.x stream (or, where both share a gain, both in turn), blockIdx.y 64 columns,
+// blockIdx.z which of A, B, C.  16 lanes of four columns by 64 groups; a sample's slots are dealt to 64 / samples groups
+// (a power of two), whose sums are joined in group order and written with the sample's vectors; then the gain's gradient
+// over the samples, in their order.
+__global__ __launch_bounds__(1024) void k_norm_sums(NormBackProblem p, bool both) {
+  constexpr int G = 64;
+  __shared__ float4 red[G][16];
+  const int which = blockIdx.z, lane = threadIdx.x & 15, grp = threadIdx.x >> 4, c = blockIdx.y * 64 + 4 * lane;
+  const bool in = c < p.D;
   const NormShares q = norm_shares(p.cu, p.B, p.rows, p.P);
-  const int lo = cu_at(p.cu, s), hi = cu_at(p.cu, s + 1), ts = hi - p.L;
-  const int a = min(sigma ? ts : lo, q.R), b = min(sigma ? hi : ts, q.R);
-  const int lane = threadIdx.x & 15, grp = threadIdx.x >> 4, c = blockIdx.y * 64 + 4 * lane;
-  float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-  if (a < b && c < p.D) {
-    const int w1 = share_owner(q, b - 1);
-    for (int w = share_owner(q, a) + grp; w <= w1; w += 16 * 4) {  // four slots' loads at a time
-      float4 t[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) t[i] = ld4(p.part + (size_t(min(w + 16 * i, w1) + seg) * 3 + which) * p.D + c);
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (w + 16 * i <= w1) v = add4(v, t[i]);
-    }
-  }
-  red[grp][lane] = v;
-  __syncthreads();
-  if (grp != 0 || c >= p.D) return;
-#pragma unroll
-  for (int g = 1; g < 16; ++g) {
-    const float4 t = red[g][lane];
-    v = make_float4(v.x + t.x, v.y + t.y, v.z + t.z, v.w + t.w);
-  }
-  if (which < 2 && gains_here) {
-    float *to = which ? (sigma ? p.dpre[1] : p.dpre[0]) : (sigma ? p.dpost[1] : p.dpost[0]);
-    const Vector mod(which ? p.scale : p.gate, size_t(seg) * p.mod_stride, which ? 0.f : 1.f);
-    if (to) *reinterpret_cast<float4 *>(to + c) = mul4(v, add4(mod(c), float(which)));
-  } else if (which < 2) {
-    *reinterpret_cast<float4 *>(sums + (size_t(seg) * 2 + which) * p.D + c) = v;
-  }
-  const float *gain = which == 0 ? (sigma ? p.post[1] : p.post[0]) : which == 1 ? (sigma ? p.pre[1] : p.pre[0]) : nullptr;
+  int per = G;  // groups of a sample
+  while (per > 1 && per * p.B > G) per /= 2;
+  const int part = grp % per, samples = G / per, step = min(per, 4);  // four groups of a wave are joined by shuffles
+  const float *mod = which == 0 ? p.gate : which == 1 ? p.scale : nullptr;
   float *out = which == 0 ? p.dgate : which == 1 ? p.dscale : p.dshift;
-  if (!out) return;
-  if (gain) {
-    const float4 t = ld4(gain + c);
-    v = make_float4(v.x * t.x, v.y * t.y, v.z * t.z, v.w * t.w);
-  }
-  *reinterpret_cast<float4 *>(out + size_t(seg) * p.dmod_stride + c) = v;
-}
-
-// The gains' gradients: blockIdx.y 0 post, 1 pre; over the samples of a stream, or of both where they share one gain.
-__global__ __launch_bounds__(256) void k_norm_gains(NormBackProblem p, const float *sums) {
-  const int c = blockIdx.x * 256 + threadIdx.x, which = blockIdx.y;
-  if (c >= p.D) return;
-  float *out[2] = {which ? p.dpre[0] : p.dpost[0], which ? p.dpre[1] : p.dpost[1]};
-  const float *mod = which ? p.scale : p.gate;
-  float v[2] = {0.f, 0.f};
-#pragma unroll 4
-  for (int s = 0; s < p.B; ++s) {
+  float4 shared_gain = zero4();
+  for (int sigma = both ? 0 : blockIdx.x; sigma <= (both ? 1 : int(blockIdx.x)); ++sigma) {
+    const float *post = sigma ? p.post[1] : p.post[0], *pre = sigma ? p.pre[1] : p.pre[0];
+    const float *w = which == 0 ? post : which == 1 ? pre : nullptr;
+    const float4 weight = w && in ? ld4(w + c) : ones4();
+    float4 gain = zero4();
+    for (int s0 = 0; s0 < p.B; s0 += samples) {
+      const int s = s0 + grp / per;
+      const size_t seg = 2 * size_t(s) + sigma;
+      float4 v = zero4(), factor = ones4();
+      if (s < p.B && in) {
+        if (mod && part == 0) factor = add4(ld4(mod + seg * p.mod_stride + c), float(which));
+        const int lo = p.cu[s], hi = p.cu[s + 1], ts = hi - p.L;
+        const int a = min(sigma ? ts : lo, q.R), b = min(sigma ? hi : ts, q.R);
+        if (a < b) {
+          const int w1 = share_owner(q, b - 1);
+          for (int w = share_owner(q, a) + part; w <= w1; w += 4 * per) {  // four slots' loads at a time
+            float4 t[4];
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      const size_t seg = size_t(2 * s + k);
-      const float f = (mod ? mod : g_zeros)[mod ? seg * p.mod_stride + c : 0];
-      v[k] += (mod ? f + float(which) : 1.f) * sums[(seg * 2 + which) * p.D + c];
+            for (int i = 0; i < 4; ++i) t[i] = ld4(p.part + (size_t(min(w + per * i, w1) + seg) * 3 + which) * p.D + c);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if (w + per * i <= w1) v = add4(v, t[i]);
+          }
+        }
+      }
+      if (per >= 2) v = add4(v, shfl_xor4(v, 16));
+      if (per >= 4) v = add4(v, shfl_xor4(v, 32));
+      __syncthreads();  // the last samples' sums have been read
+      red[grp][lane] = v;
+      __syncthreads();
+      if (part == 0 && s < p.B && in) {
+#pragma unroll 4
+        for (int i = step; i < per; i += step) v = add4(v, red[grp + i][lane]);
+        if (out) *reinterpret_cast<float4 *>(out + seg * p.dmod_stride + c) = mul4(v, weight);
+        red[grp][lane] = mul4(v, factor);
+      }
+      __syncthreads();
+      if (which < 2 && grp == 0 && in) {
+#pragma unroll 4
+        for (int i = 0; i < min(samples, p.B - s0); ++i) gain = add4(gain, red[i * per][lane]);
+      }
+    }
+    float *const *d = which ? p.dpre : p.dpost;
+    if (which < 2 && grp == 0 && in) {
+      if (d[0] && d[0] == d[1]) {
+        shared_gain = add4(shared_gain, gain);
+        if (sigma == 1) *reinterpret_cast<float4 *>(d[0] + c) = shared_gain;
+      } else if (sigma ? d[1] : d[0]) {
+        *reinterpret_cast<float4 *>((sigma ? d[1] : d[0]) + c) = gain;
+      }
     }
   }
-  if (out[0] && out[0] == out[1]) {
-    out[0][c] = v[0] + v[1];
-    return;
-  }
-  if (out[0]) out[0][c] = v[0];
-  if (out[1]) out[1][c] = v[1];
 }
 
 // Workers: eight rows each (W = 1: two a wave), so that their slots (24 bytes a column, written and read) are a small
@@ -571,12 +572,11 @@ static int norm_back_workers(int rows, int D) {
 }
 
 size_t norm_back_bytes(int rows, int B, int D) {
-  return ((size_t(norm_back_workers(rows, D)) + 2 * size_t(B)) * 3 + 4 * size_t(B)) * size_t(D) * sizeof(float);
+  return (size_t(norm_back_workers(rows, D)) + 2 * size_t(B)) * 3 * size_t(D) * sizeof(float);
 }
 
 hipError_t launch_norm_residual_back(bool bf16, NormBackProblem p, hipStream_t st) {
   p.P = norm_back_workers(p.rows, p.D);
-  float *sums = p.part ? p.part + (size_t(p.P) + 2 * size_t(p.B)) * 3 * p.D : nullptr;
   if (p.rows > 0) {
 #define HILO_NB(W, NV)                                                                                     \
   do {                                                                                                     \
@@ -599,13 +599,8 @@ hipError_t launch_norm_residual_back(bool bf16, NormBackProblem p, hipStream_t s
     if (e != hipSuccess) return e;
   }
   if (!p.part) return hipSuccess;
-  const bool gains = p.dpost[0] || p.dpost[1] || p.dpre[0] || p.dpre[1];
-  const bool shared = (p.dpost[0] && p.dpost[0] == p.dpost[1]) || (p.dpre[0] && p.dpre[0] == p.dpre[1]);
-  const bool here = p.B == 1 && !shared;
-  hipLaunchKernelGGL(k_norm_sums, dim3(2 * p.B, (p.D + 63) / 64, 3), dim3(256), 0, st, p, sums, here);
-  const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || !gains || here) return e;
-  hipLaunchKernelGGL(k_norm_gains, dim3((p.D + 255) / 256, 2), dim3(256), 0, st, p, sums);
+  const bool both = (p.dpost[0] && p.dpost[0] == p.dpost[1]) || (p.dpre[0] && p.dpre[0] == p.dpre[1]);
+  hipLaunchKernelGGL(k_norm_sums, dim3(both ? 1 : 2, (p.D + 63) / 64, 3), dim3(1024), 0, st, p, both);
   return hipGetLastError();
 }
 
