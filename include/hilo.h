@@ -367,7 +367,7 @@ hilo_status hilo_attention_core_noalloc(const hilo_shape *shape, const void *qkv
  * the type of every tensor called "dtype" below.  Pointers are aligned to 16 bytes, tensors of bf16
  * and of 8-bit codes that are read or written 8 bytes at a time to 8 (HILO_E_PARAM otherwise),
  * unless an entry says that any alignment will do.  rows == 0 enqueues nothing (gradients of vectors
- * become 0), and the tensors with rows may then be NULL.  At most 2^20 samples.
+ * become 0), and the tensors with rows may then be NULL.  At most 2^20 samples (hilo_linear_i8: 4096).
  * --------------------------------------------------------------------------------------------- */
 
 /* Rotary positions with several axes (time, height, width, ...) on the heads of packed rows.  The
@@ -474,8 +474,8 @@ hilo_status hilo_quantize_rows_i8(int32_t dtype, const void *x, int64_t rows, in
  * act: none, or GELU_tanh as in hilo_mlp.  w: image and text stream's weights (stream 1 is not looked at when
  * text_len is 0).  x [rows][in_dim]: int8 codes with x_scale [rows] float32, or with x_scale NULL dtype,
  * quantised as hilo_quantize_rows_i8 does within the call.  out [rows][out_dim] dtype.
- * in_dim % 16 == 0, 16 .. 65536; out_dim % 4 == 0, below 2^24; (rows / 64 + 2 batch) * (out_dim / 32 + 1) < 2^31
- * (HILO_E_SHAPE); act unknown: HILO_E_PARAM.
+ * in_dim % 16 == 0, 16 .. 65536; out_dim % 4 == 0, below 2^24; batch <= 4096;
+ * (rows / 64 + 2 batch) * (out_dim / 32 + 1) < 2^31 (HILO_E_SHAPE); act unknown: HILO_E_PARAM.
  * workspace: ws_bytes >= hilo_linear_i8_workspace_bytes(rows, in_dim) of device scratch, contents undefined
  * after; calls that may overlap, two captured graphs among them, need one each.                 */
 typedef enum { HILO_ACT_NONE = 0, HILO_ACT_GELU = 1 } hilo_act;

@@ -954,6 +954,8 @@ hilo_status hilo_linear_i8(int32_t dtype, const hilo_linear_w_i8 w[2], const voi
   if (e != HILO_OK || (e = check_rows(rows, batch, text_len)) != HILO_OK) return e;
   if (in_dim < 16 || in_dim > 65536 || in_dim % 16 != 0 || out_dim < 4 || out_dim >= (1 << 24) || out_dim % 4 != 0)
     return HILO_E_SHAPE;
+  // workgroups find their tiles by walking the samples
+  if (batch > 4096) return HILO_E_SHAPE;
   // tiles are counted in 32 bits, the smallest of them 64 x 32, and every segment may leave a part of one
   if ((rows / 64 + 2LL * batch) * (out_dim / 32 + 1) >= (1LL << 31)) return HILO_E_SHAPE;
   if (act != HILO_ACT_NONE && act != HILO_ACT_GELU) return HILO_E_PARAM;

@@ -133,7 +133,7 @@ struct RopeProblem {
   int rows, heads, hd, axes, n;
   int first[4];  // first pair of each axis (n behind the last axis)
   int adjacent, backward, one_spectrum;
-  int units_head, block_rows, block_heads;  // set by the launcher
+  int units_head, block_rows;  // set by the launcher
   double step[4];
 };
 hipError_t launch_rope(bool bf16, RopeProblem p, hipStream_t st);

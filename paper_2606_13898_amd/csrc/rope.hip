@@ -65,7 +65,7 @@ struct Vec {
 }  // namespace
 
 // A unit is V pairs of one head (two vectors of V values: at columns j and j + n, or 2 j and 2 j + V), or, where
-// rows are copied, V columns behind the rotated ones.  blockIdx.x: p.block_rows rows; blockIdx.y: p.block_heads heads.
+// rows are copied, V columns behind the rotated ones.  A workgroup takes p.block_rows rows.
 template <bool BF16, int V, bool ADJ>
 __global__ __launch_bounds__(256) void k_rope(RopeProblem p) {
   using E = std::conditional_t<BF16, uint16_t, float>;
@@ -74,7 +74,6 @@ __global__ __launch_bounds__(256) void k_rope(RopeProblem p) {
   const int rows = p.rows_end ? min((long long)p.rows, (long long)cu_at(p.rows_end, 0)) : p.rows;
   const int row0 = blockIdx.x * p.block_rows, nr = min(p.block_rows, rows - row0);
   if (nr <= 0) return;
-  const int h0 = blockIdx.y * p.block_heads, nh = min(p.block_heads, p.heads - h0);
   for (int i = threadIdx.x; i < nr * p.n; i += 256) {
     const int r = i / p.n, j = i - r * p.n;
     const int a = (j >= p.first[1]) + (j >= p.first[2]) + (j >= p.first[3]);
@@ -86,10 +85,10 @@ __global__ __launch_bounds__(256) void k_rope(RopeProblem p) {
     cs[i] = v;
   }
   __syncthreads();
-  const int per_head = p.units_head, units = nr * nh * per_head;
+  const int per_head = p.units_head, units = nr * p.heads * per_head;
   const int turned = p.n / V;
   for (int i = threadIdx.x; i < units; i += 256) {
-    const int q = i / per_head, u = i - q * per_head, r = q / nh, h = h0 + (q - r * nh);
+    const int q = i / per_head, u = i - q * per_head, r = q / p.heads, h = q - r * p.heads;
     const size_t row = size_t(row0 + r);
     const E *x = reinterpret_cast<const E *>(p.x) + row * p.ldx + size_t(h) * p.hd;
     E *o = reinterpret_cast<E *>(p.out) + row * p.ldo + size_t(h) * p.hd;
@@ -121,7 +120,7 @@ __global__ __launch_bounds__(256) void k_rope(RopeProblem p) {
 }
 
 hipError_t launch_rope(bool bf16, RopeProblem p, hipStream_t st) {
-  if (p.rows <= 0 || p.heads <= 0) return hipSuccess;
+  if (p.rows <= 0) return hipSuccess;
   const bool copy = p.x != p.out || p.ldx != p.ldo;
   const int e = bf16 ? 2 : 4, rest = p.hd - 2 * p.n;
   // the widest vectors that the columns and both addresses allow
@@ -133,14 +132,12 @@ hipError_t launch_rope(bool bf16, RopeProblem p, hipStream_t st) {
   while (V > 1 && !fits(V)) V /= 2;
   p.units_head = p.n / V + (copy ? rest / V : 0);
   if (p.units_head == 0) return hipSuccess;  // in place, nothing turns
-  // rows of a workgroup: about six units a thread, and a table that fits; few rows: heads over more workgroups
+  // rows of a workgroup: about six units a thread, and a table that fits
   const int row_units = p.heads * p.units_head;
   int br = (6 * 256 + row_units - 1) / row_units;
   if (p.n > 0) br = br < kRopeTable / p.n ? br : kRopeTable / p.n;
   p.block_rows = br < 1 ? 1 : br;
-  p.block_heads = p.heads;
-  const long long gx = (p.rows + p.block_rows - 1) / p.block_rows;
-  const dim3 grid(unsigned(gx), unsigned((p.heads + p.block_heads - 1) / p.block_heads));
+  const dim3 grid{unsigned((p.rows + p.block_rows - 1) / p.block_rows)};
 #define HILO_ROPE(B, VV)                                                              \
   do {                                                                                \
     if (p.adjacent) hipLaunchKernelGGL((k_rope<B, VV, true>), grid, dim3(256), 0, st, p); \

@@ -137,6 +137,7 @@ def linear(dtype=hilo.BF16, w0=(F, F, F), w1=(F, F, F), x=F, x_scale=None, out=F
     (dict(dtype=2), DTYPE), (dict(rows=-1), SHAPE), (dict(rows=1 << 24), SHAPE), (dict(batch=0), SHAPE), (dict(text=-1), SHAPE),
     (dict(text=5), SHAPE), (dict(k=0), SHAPE), (dict(k=72), SHAPE), (dict(k=65552), SHAPE), (dict(n=0), SHAPE), (dict(n=66), SHAPE),
     (dict(n=1 << 24), SHAPE), (dict(n=(1 << 24) - 4, rows=(1 << 24) - 1), SHAPE), (dict(batch=(1 << 20) + 1, rows=1 << 23), SHAPE),
+    (dict(batch=4097, rows=8194), SHAPE), (dict(batch=4096, rows=4095), SHAPE),
     (dict(act=2), PARAM), (dict(x=None), NULL), (dict(out=None), NULL), (dict(cu=None), NULL),
     (dict(ws=None), NULL), (dict(w0=(None, F, F)), NULL), (dict(w1=(F, None, F)), NULL), (dict(w0=(F + 8, F, F)), PARAM),
     (dict(w1=(F, F + 4, F)), PARAM), (dict(w0=(F, F, F + 4)), PARAM), (dict(x=F + 8), PARAM), (dict(x_scale=F + 2), PARAM),

@@ -347,6 +347,13 @@ def test_norm_residual_backward(dtype, lens, text, D, rms, gains, mod):
     assert torch.equal(shared[0], first[3][0, 0] + first[3][0, 1]) and torch.equal(shared[1], first[3][1, 0])
 
 
+# samples over the groups that sum their slots: 8, 2 and 1 group a sample, more samples than groups, many slots a sample
+@pytest.mark.parametrize("B,most,text,D", [(5, 30, 2, 64), (20, 5, 1, 132), (40, 3, 0, 64), (70, 4, 1, 72), (2, 2000, 77, 64)])
+def test_norm_backward_many_samples(B, most, text, D):
+    lens = [int(n) + text for n in np.random.default_rng(B).integers(0, most + 1, B)]
+    test_norm_residual_backward("f32", lens, text, D, False, True, True)
+
+
 def test_norm_backward_parts():
     """Without a gradient from elsewhere, without h, without y: the formula with that part left out."""
     rng, c = _norm_case(8, "f32", [5, 3], 2, 128, True, True)
@@ -510,6 +517,13 @@ def test_linear_i8_plans(shape, dtype, gelu, bias):
     T = sum(lens)
     rows = None if T * N * K < 3e9 else np.sort(np.random.default_rng(1).choice(T, 100, replace=False))
     run_linear(dtype, lens, text, K, N, gelu, bias, 7, rows)
+
+
+@pytest.mark.parametrize("spare", [0, 40000])
+def test_linear_i8_most_samples(spare):
+    """4096 samples, most of two rows: in one launch, and from codes on the larger tiles' kernel."""
+    lens = [2, 1, 3, 2] * 1024
+    run_linear("bf16", lens, 1, 80, 96, False, True, 3, spare=spare)
 
 
 def test_linear_i8_largest_sum():
