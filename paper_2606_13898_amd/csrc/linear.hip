@@ -402,14 +402,24 @@ __global__ __launch_bounds__(256) void k_linear_i8_small(GemmProblem p) {
   }
 }
 
-// Buffers of at most this many rows take the narrow tiles.
+// Buffers of at most this many rows take the narrow tiles (few_rows numbers no more).  Codes in, on one side and on the
+// other the projections' tiles: 16 rows of 3072 -> 9216 11.3 and 14.8 us, 64 rows 19.8 and 20.7, of 3072 -> 3072 9.5 and
+// 12.6, of 12288 -> 3072 29.4 and 30.0, of 1024 -> 1024 6.8 and 6.9.
 constexpr long long kFewRows = 64;
 size_t linear_i8_part_bytes(long long rows) { return rows <= kFewRows ? 0 : kSkPartBytes; }
 
-// Whether float rows are quantised by the kernel that multiplies them.
+// Whether float rows are quantised by the kernel that multiplies them, or by a launch before it.
+// Up to four rows, whose codes fit the LDS: every workgroup reads them all, so more of them cost what the launch does.
+// bf16, fused and apart: 1 row of 3072 -> 18432 12.6 and 15.8 us, 4 rows 16.5 and 16.1, of 3072 -> 3072 7.4 and 9.6, of
+// 8192 -> 3072 12.2 and 15.7; 8 rows of 3072 -> 18432 22.7 and 17.8.
 static bool fused_few(const GemmProblem &p) { return p.max_img_rows <= 4 && p.max_img_rows * (p.K + 144) <= 49152; }
+// Short rows: a tile of 32 rows takes the time of its rows' bytes and 400 more each; apart costs the launch, the codes'
+// way through memory and a larger kernel's start.  Fused and apart at the product below, in us:
+//   bf16     551 x 256 -> 1024  (8e6)  6.9,  9.3    2000 x 512 -> 1024 (46e6) 10.4, 16.9    8000 x 128 -> 512  (42e6) 10.2, 14.8
+//           1000 x 768 -> 2048 (62e6) 14.3, 18.9    4000 x 512 -> 1024 (91e6) 17.0, 17.9   16000 x 128 -> 1024 (168e6) 26.7, 18.5
+//   float32 1000 x 768 -> 1536 (83e6) 13.3, 20.1    8000 x 128 -> 1024 (117e6) 18.5, 16.7
 static bool fused_small(const GemmProblem &p, bool bf16) {
-  return p.K <= kSmallK && double(p.max_img_rows) * p.K * (bf16 ? 2 : 4) * ((p.N + 63) / 64) <= 32e6;
+  return p.K <= kSmallK && double(p.max_img_rows) * ((p.N + 63) / 64) * (p.K * (bf16 ? 2 : 4) + 400) <= 90e6;
 }
 bool linear_i8_fuses(bool bf16, const GemmProblem &p) { return fused_few(p) || fused_small(p, bf16); }
 
@@ -425,7 +435,8 @@ static hipError_t run_linear_i8(const GemmProblem &p, hipStream_t st) {
     else hipLaunchKernelGGL((k_linear_i8_small<BF16, GELU, 12>), grid, dim3(256), 0, st, p);
     return hipGetLastError();
   }
-  // row tiles of the two streams
+  // row tiles of the two streams.  Two column blocks a tile halve what is read of x per weight and leave half the
+  // workgroups: 64 rows of 3072, one and two, N = 4096 10.2 and 12.8 us, 8192 17.0 and 13.7, 18432 36.6 and 28.2
   const int bm = rows <= 16 ? 16 : 64, bn = rows <= 16 || p.N < 8192 ? 16 : 32, streams = p.L > 0 ? 2 : 1;
   const dim3 grid(unsigned((p.N + bn - 1) / bn), unsigned(streams * ((rows + bm - 1) / bm)));
   if (p.a_scale == nullptr) {
