@@ -3,6 +3,9 @@
 //   u = norm(y) * post;  x' = alpha x + gate u;  h = norm(x') * pre * (1 + scale) + shift
 // Everything in float32; x and x' are float32, y and h the block's type, or h int8 codes with a scale per row.
 // What bounds both directions is memory: a row is read once, stays in registers through both norms and is written once.
+// A copy of 4 GiB reaches 4.74 TB/s; the forward pass on bf16 y 4.2 (2766 rows of 3072 in 24.2 us; with codes out 4708
+// rows of 1536 in 18.3 us, 4.4 TB/s), the backward pass 4.7 (22560 rows of 3072, 1.2 GB, in 257 us, and 16 us for the
+// sums).  Four rows of 3072 take 4.6 us: a load, two sums over four waves and a store, one behind the other.
 #include "common.h"
 #include "kernels.h"
 
@@ -188,7 +191,10 @@ HILO_DEV RowSegment row_segment(const int *cu, int B, int L, int row, int last) 
 constexpr int norm_waves(int NV) { return NV == 1 ? 8 : NV == 2 ? 5 : NV == 3 ? 4 : 3; }
 
 // A worker is W waves, NV float4 a lane (D <= 256 W NV); W = 1: four a workgroup.  It keeps the vectors of the segment
-// that its rows are in -- read for every row they are more than the row itself -- and reads a row ahead.
+// that its rows are in -- read for every row they are more than the row itself -- and reads a row ahead.  W and NV are
+// chosen so that at most three float4 a lane leave room for four waves a SIMD or more: six on one wave a row (D = 1536)
+// took 36.6 us where three on two take 20.3, and two on four 19.9 (20.0 and 18.3 with codes, whose maximum is one more
+// sum over the row's waves).
 // OUT: h as 0 dtype, 1 int8 codes and row scales.
 template <bool BF16, int OUT, int W, int NV>
 __global__ __launch_bounds__(W == 1 ? 256 : 64 * W, norm_waves(NV)) void k_norm_residual(NormProblem p) {
@@ -497,7 +503,8 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W, NV < 4 ? 3 : 2) void k_norm_
 // The sums over a stream's slots: blockIdx.x stream (or, where both share a gain, both in turn), blockIdx.y 64 columns,
 // blockIdx.z which of A, B, C.  16 lanes of four columns by 64 groups; a sample's slots are dealt to 64 / samples groups
 // (a power of two), whose sums are joined in group order and written with the sample's vectors; then the gain's gradient
-// over the samples, in their order.
+// over the samples, in their order.  One launch for both: the slots and the gains' sums in two took as long for 8 samples
+// (16 us at D = 3072, 30 MB of slots) and a launch of 5 us more for few rows.
 __global__ __launch_bounds__(1024) void k_norm_sums(NormBackProblem p, bool both) {
   constexpr int G = 64;
   __shared__ float4 red[G][16];
