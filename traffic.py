@@ -40,12 +40,12 @@ XCDS = 8
 
 CSRC = "paper_2606_13898_amd/csrc/"
 HDRS = [CSRC + "common.h", CSRC + "kernels.h"]
+GEMM = [CSRC + "gemm.hip", CSRC + "tiles.h"]
 SOURCES = {
     "score": [CSRC + "select.hip"], "select": [CSRC + "select.hip"], "layout": [CSRC + "select.hip"],
     "compress": [CSRC + "pack.hip"], "decompress": [CSRC + "pack.hip"],
     "rownorm_attn": [CSRC + "pack.hip"], "rownorm_mlp": [CSRC + "pack.hip"],
-    "gemm_qkv": [CSRC + "gemm.hip"], "gemm_o": [CSRC + "gemm.hip"], "gemm_fc1": [CSRC + "gemm.hip"],
-    "gemm_fc2": [CSRC + "gemm.hip"], "attention_core": [CSRC + "attention.hip"],
+    "gemm_qkv": GEMM, "gemm_o": GEMM, "gemm_fc1": GEMM, "gemm_fc2": GEMM, "attention_core": [CSRC + "attention.hip"],
 }
 ROLES = {"0": "gemm_qkv", "1": "gemm_o", "2": "gemm_fc1", "3": "gemm_fc2"}
 
