@@ -431,6 +431,14 @@ HILO_DEV int swz(int r) {
   if constexpr (B32) return ((r >> 1) & 3) ^ ((((r >> 3) ^ (r >> 4)) & 1) << 2);
   else return (r >> 1) & 7;
 }
+// The rows of W.  In PAIRED order they are read as 8 g + 4 p + 0 .. 3 (pairs of fragment columns) and 4 g + 0 .. 3: bits
+// 1, 3 and 4 tell the first apart, bits 1 to 3 the second.  By swz two lanes of a group fell on one bank group: a quarter
+// of the LDS cycles, though only 1% of the time (22560 x 12288 x 3072 753 -> 749 us).
+template <typename G>
+HILO_DEV int swz_w(int r) {
+  if constexpr (G::ORDER == COLS_PAIRED) return ((r >> 1) & 1) | ((r >> 2) & 2) | ((r ^ (r >> 2)) & 4);
+  else return swz<G::B32>(r);
+}
 // W row read by fragment lane r of a 32 x 32 block.  The MFMA's output row i (the W side) lands in
 // accumulator register 4 (i / 8) + i % 4 of the lanes of half (i / 4) % 2; reading W row perm_w(i) there
 // gives lane half g the columns 16 g .. 16 g + 15 in register order.
@@ -668,7 +676,7 @@ HILO_DEV void gemm8_run(const GemmProblem &p, const SkPlan &q, int pid, uint8_t 
 #pragma unroll
     for (int i = 0; i < LB; ++i) {
       const int r = wid * (BN / 8) + 8 * i + (lane >> 3);
-      ob[i] = uint32_t(min(r, p.N - 1 - n0)) * uint32_t(p.K) * ESZ + uint32_t((lane & 7) ^ swz<B32>(r)) * 16;
+      ob[i] = uint32_t(min(r, p.N - 1 - n0)) * uint32_t(p.K) * ESZ + uint32_t((lane & 7) ^ swz_w<G>(r)) * 16;
     }
     la = reinterpret_cast<const char *>(p.A) + (size_t(tr.row0) * p.lda + size_t(x.kb) * G::KW) * ESZ;
     lb = reinterpret_cast<const char *>(tr.sigma ? p.W[1] : p.W[0]) + (size_t(n0) * p.K + size_t(x.kb) * G::KW) * ESZ;
@@ -678,15 +686,15 @@ HILO_DEV void gemm8_run(const GemmProblem &p, const SkPlan &q, int pid, uint8_t 
   // int8: a last window of fewer than 128 values (K is a multiple of 16) reads the row's first chunk in the place of
   // those behind K; its fragments of A are cleared before they are multiplied
   const int kpart = I8 && p.K % 128 != 0 ? p.K / 128 : -1, cpart = p.K % 128 / 16;
-  auto inside = [&](uint32_t o, int r) __attribute__((always_inline)) {
-    const int c = (lane & 7) ^ swz<B32>(r);
+  auto inside = [&](uint32_t o, int swizzle) __attribute__((always_inline)) {
+    const int c = (lane & 7) ^ swizzle;
     return c < cpart ? o : o - uint32_t(c) * 16;
   };
   auto ld_a = [&]() __attribute__((always_inline)) {
     uint8_t *d = lds + lslot * WB + wid * (BM / 8) * 128;
     if (I8 && lk == kpart) {
 #pragma unroll
-      for (int i = 0; i < LA; ++i) g2lds16(la + inside(oa[i], wid * (BM / 8) + 8 * i + (lane >> 3)), d + i * 1024);
+      for (int i = 0; i < LA; ++i) g2lds16(la + inside(oa[i], swz<B32>(wid * (BM / 8) + 8 * i + (lane >> 3))), d + i * 1024);
     } else {
 #pragma unroll
       for (int i = 0; i < LA; ++i) g2lds16(la + oa[i], d + i * 1024);
@@ -697,7 +705,7 @@ HILO_DEV void gemm8_run(const GemmProblem &p, const SkPlan &q, int pid, uint8_t 
     uint8_t *d = lds + lslot * WB + (BM + wid * (BN / 8)) * 128;
     if (I8 && lk == kpart) {
 #pragma unroll
-      for (int i = 0; i < LB; ++i) g2lds16(lb + inside(ob[i], wid * (BN / 8) + 8 * i + (lane >> 3)), d + i * 1024);
+      for (int i = 0; i < LB; ++i) g2lds16(lb + inside(ob[i], swz_w<G>(wid * (BN / 8) + 8 * i + (lane >> 3))), d + i * 1024);
     } else {
 #pragma unroll
       for (int i = 0; i < LB; ++i) g2lds16(lb + ob[i], d + i * 1024);
@@ -726,13 +734,13 @@ HILO_DEV void gemm8_run(const GemmProblem &p, const SkPlan &q, int pid, uint8_t 
     if constexpr (B32) {
       const int r = lane & 31, w = perm_w(r), c = 2 * h + (lane >> 5);
       fa[h] = lds0 + (wm * (BM / WM) + r) * 128 + ((c ^ swz<B32>(r)) * 16);
-      fb[0][h] = lds0 + (BM + wn * (BN / WN) + w) * 128 + ((c ^ swz<B32>(w)) * 16);
+      fb[0][h] = lds0 + (BM + wn * (BN / WN) + w) * 128 + ((c ^ swz_w<G>(w)) * 16);
     } else {
       fa[h] = lds0 + (wm * (BM / WM) + lr) * 128 + (((4 * h + lg) ^ swz<B32>(lr)) * 16);
 #pragma unroll
       for (int j = 0; j < NB; ++j) {
         const int r = wn * (BN / WN) + col_of<NB>(ORDER, lr >> 2, j) + (lr & 3);
-        fb[j][h] = lds0 + (BM + r) * 128 + (((4 * h + lg) ^ swz<B32>(r)) * 16);
+        fb[j][h] = lds0 + (BM + r) * 128 + (((4 * h + lg) ^ swz_w<G>(r)) * 16);
       }
     }
   }
