@@ -1370,10 +1370,11 @@ __global__ __launch_bounds__(kFixThreads) void k_gemm8_fix(GemmProblem p) {
 // of tile would leave a poor last wave the other mostly does not -- so up to K = 8192, where fewer tiles run whole too,
 // there is no second launch at all.
 //
-// 22560 x 12288 x 3072 (rows, columns, K; GELU) 808 us, 2.1 POP/s, where the library's product alone, without scales, bias
-// and GELU, takes 831; 2766 x 9216 x 3072 92 us (88); 4708 x 6144 x 1536 with GELU 63.  At K = 12288 the loop runs at 2.7
-// POP/s, bound as the bf16 one by the window's LDS reads and the way from the L2; what keeps shorter K below that is the
-// epilogue (of a 256 x 256 tile 6.0 us, 8.7 with GELU, an exponential and a reciprocal a value) and the last wave of tiles.
+// 22560 x 12288 x 3072 (rows, columns, K; GELU) 750 us, 2.3 POP/s, on the same operands again and again (808 on three sets
+// in turn), where the library's product alone, without scales, bias and GELU, takes 831; 2766 x 9216 x 3072 87 us (92; the
+// library 88); 4708 x 6144 x 1536 with GELU 59 (63).  At K = 12288 the loop runs at 2.7 POP/s, the matrix cores busy half
+// the time at 2.2 to 2.3 GHz; neither a quarter fewer LDS cycles nor wave priorities changed that by more than 1%.  What
+// keeps shorter K below it is the epilogue (of a 256 x 256 tile 6.0 us, 8.7 with GELU, an exponential and a reciprocal a value) and the last wave of tiles.
 
 // Small problems: 64 x 32 tiles, two a workgroup, each on four waves that split K in steps of 128; their sums are added
 // through LDS (gemm_small_run's layout, and its cost per step).
