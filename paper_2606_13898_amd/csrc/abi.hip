@@ -944,7 +944,7 @@ hilo_status hilo_quantize_rows_i8(int32_t dtype, const void *x, int64_t rows, in
 // Workspace: the codes and scales of float rows, then the partial tiles.
 size_t hilo_linear_i8_workspace_bytes(int64_t rows, int32_t in_dim) {
   if (check_rows(rows, 1, 0) != HILO_OK || in_dim < 16 || in_dim > 65536 || in_dim % 16 != 0) return 0;
-  return align256(size_t(rows) * in_dim) + align256(size_t(rows) * sizeof(float)) + linear_i8_part_bytes(rows) + 256;
+  return align256(size_t(rows) * in_dim) + align256(size_t(rows) * sizeof(float)) + linear_i8_part_bytes(rows, in_dim) + 256;
 }
 
 hilo_status hilo_linear_i8(int32_t dtype, const hilo_linear_w_i8 w[2], const void *x, const float *x_scale, void *out,

@@ -1670,13 +1670,16 @@ hipError_t launch_gemm_fp8(int role, const GemmProblem &p, hipStream_t st) {
   }
 }
 
+// Whether tiles may be cut along K (plan_i8: 256 or more run whole, and fewer do up to this K).
+bool linear_i8_cuts(int K) { return (K + 127) / 128 > kNoSplitSteps; }
+
 template <int EPI, int OP>
 static hipError_t run_i8(const GemmProblem &p, hipStream_t st) {
   constexpr int P = kGemmWorkgroups;
   hipLaunchKernelGGL((k_linear_i8<EPI, OP>), dim3(P), dim3(512), 0, st, p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  if ((p.K + 127) / 128 <= kNoSplitSteps) return hipSuccess;  // no tile is ever cut
+  if (!linear_i8_cuts(p.K)) return hipSuccess;
   hipLaunchKernelGGL((k_linear_i8_fix<EPI, OP>), dim3(P), dim3(kFixThreads), 0, st, p);
   return hipGetLastError();
 }

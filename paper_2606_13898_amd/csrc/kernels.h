@@ -195,9 +195,10 @@ hipError_t launch_quantize_rows_i8(bool bf16, const void *x, int rows, int cols,
 // that linear_i8_fuses() says are quantised by the kernel that multiplies them.
 bool linear_i8_fuses(bool bf16, const GemmProblem &p);
 hipError_t launch_linear_i8(bool bf16, bool gelu, const GemmProblem &p, hipStream_t st);
-// The same on the projections' tiles, with partial tiles in p.part (kSkPartBytes).
+// The same on the projections' tiles; where linear_i8_cuts(K), with partial tiles in p.part (kSkPartBytes).
 hipError_t launch_linear_i8_tiled(bool bf16, bool gelu, const GemmProblem &p, hipStream_t st);
+bool linear_i8_cuts(int K);
 // Bytes of partial tiles that launch_linear_i8 needs for buffers of `rows` rows.
-size_t linear_i8_part_bytes(long long rows);
+size_t linear_i8_part_bytes(long long rows, int K);
 
 }  // namespace hilo

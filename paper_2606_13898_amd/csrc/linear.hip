@@ -408,7 +408,7 @@ __global__ __launch_bounds__(256) void k_linear_i8_small(GemmProblem p) {
 // other the projections' tiles: 16 rows of 3072 -> 9216 11.3 and 14.8 us, 64 rows 19.8 and 20.7, of 3072 -> 3072 9.5 and
 // 12.6, of 12288 -> 3072 29.4 and 30.0, of 1024 -> 1024 6.8 and 6.9.
 constexpr long long kFewRows = 64;
-size_t linear_i8_part_bytes(long long rows) { return rows <= kFewRows ? 0 : kSkPartBytes; }
+size_t linear_i8_part_bytes(long long rows, int K) { return rows <= kFewRows || !linear_i8_cuts(K) ? 0 : kSkPartBytes; }
 
 // Whether float rows are quantised by the kernel that multiplies them, or by a launch before it.
 // Up to four rows, whose codes fit the LDS: every workgroup reads them all, so more of them cost what the launch does.

@@ -163,6 +163,10 @@ def test_good_calls_reach_the_device():
 def test_workspace_bytes():
     assert hilo.hilo_linear_i8_workspace_bytes(-1, 64) == hilo.hilo_linear_i8_workspace_bytes(4, 24) == 0
     assert hilo.hilo_linear_i8_workspace_bytes(100, 64) >= 100 * 64 + 400
+    # partial tiles only where K may be cut: longer than 64 steps of 128, and more rows than the narrow tiles take
+    whole, cut = (hilo.hilo_linear_i8_workspace_bytes(100, k) - 100 * k for k in (8192, 8208))
+    assert whole < 1 << 16 and cut >= 256 * 3 * 256 * 256 * 4
+    assert hilo.hilo_linear_i8_workspace_bytes(64, 8208) < 1 << 20
     assert hilo.hilo_norm_residual_workspace_bytes(8, 0, 64) == hilo.hilo_norm_residual_workspace_bytes(8, 1, 66) == 0
     small, large = (hilo.hilo_norm_residual_workspace_bytes(r, 3, 256) for r in (1, 4000))
     assert 0 < small < large
@@ -271,3 +275,14 @@ def test_oracle_int8():
 def test_linear_plans(shape, plan):
     """The shapes of the GPU tests reach the plans that they are there for."""
     assert linear_schedule.describe(*shape) == plan
+
+
+def test_linear_plans_cut_no_tile_of_short_k():
+    """Up to 64 steps of 128 every tile runs whole, so such a call has no partial tiles and no second launch."""
+    rng = np.random.default_rng(3)
+    for _ in range(3000):
+        text = int(rng.choice([0, 1, 77, 300]))
+        lens = [int(n) + text for n in rng.integers(1, 4000, rng.choice([1, 2, 8]))]
+        K, N = 16 * int(rng.integers(1, 513)), 4 * int(rng.integers(1, 3000))
+        plan = linear_schedule.describe(lens, text, K, N, bool(rng.integers(2)))
+        assert plan[0] == "small" or (plan[2] == 1 and plan[4] == 0), (lens, text, K, N, plan)
