@@ -309,13 +309,21 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W, norm_waves(NV)) void k_norm_
   }
 }
 
+// Workers: the same number on every CU, whose memory time they share, and no more than eight waves there (one wave a row:
+// sixteen), each with a row on its way: 22560 rows of 3072 on 512, 768, 1024 workers 172.7, 176.2, 178.4 us; 1500 13.0,
+// 13.5, 14.5; 6000 of 4096 on 256, 512, 768 64.7, 66.2, 69.3; 2000 of 8192 on 256 and 384 45.6 and 50.4; 9000 of 1536 on
+// 768, 1024, 1280 39.4, 38.7, 40.2; 13000 of 768 on 1024, 2048, 4096 27.4, 27.8, 27.1.
+template <int W>
+static int norm_workers(int rows) {
+  constexpr int most = W == 1 ? 4096 : 2048 / W;
+  return rows < most ? rows : most;
+}
+
 hipError_t launch_norm_residual(bool bf16, NormProblem p, hipStream_t st) {
   if (p.rows <= 0) return hipSuccess;
-  // workers: as many as the card holds at once
 #define HILO_NR(W, NV)                                                                                            \
   do {                                                                                                            \
-    constexpr int waves = 256 * 4 * norm_waves(NV);                                                                \
-    p.P = p.rows < waves / W ? p.rows : waves / W;                                                                 \
+    p.P = norm_workers<W>(p.rows);                                                                                  \
     const dim3 grid(W == 1 ? (unsigned(p.P) + 3) / 4 : unsigned(p.P)), block(W == 1 ? 256 : 64 * W);                \
     if (p.h_scale) {                                                                                                \
       if (bf16) hipLaunchKernelGGL((k_norm_residual<true, 1, W, NV>), grid, block, 0, st, p);                       \
@@ -571,11 +579,15 @@ __global__ __launch_bounds__(1024) void k_norm_sums(NormBackProblem p, bool both
   }
 }
 
-// Workers: eight rows each (W = 1: two a wave), so that their slots (24 bytes a column, written and read) are a small
-// part of what they read, and no more than the card holds at once.
+// Workers: the same number on every CU here too, about five rows for each (one wave a row: ten for its four), since a slot
+// costs 24 bytes a column where a row costs 18 and more, and at most one, two or three a CU: 22560 rows of 3072 on 256, 512,
+// 768 workers 291.6, 265.2, 270.9 us, 2766 51.3, 51.1, 54.0, 1100 27.5, 30.9, 33.8; 5000 of 5120 on 256, 384, 512 111.5,
+// 130.6, 117.5; 9000 of 1536 on 512, 768, 1024 68.3, 65.0, 66.2; 13000 of 512 39.1, 36.8, 38.2, 2000 of 512 on 256 and 512
+// 13.9 and 14.5.
 static int norm_back_workers(int rows, int D) {
-  const int want = (rows + 7) / 8, most = D <= 768 ? 1024 : D <= 1536 ? 1536 : D <= 3072 ? 768 : 384;
-  return want < 1 ? 1 : want < most ? want : most;
+  const int share = 256 * (D <= 768 ? 10 : 5), most = D <= 1536 ? 3 : D <= 3072 ? 2 : 1;
+  const int a_cu = (rows + share / 2) / share, workers = 256 * (a_cu < 1 ? 1 : a_cu < most ? a_cu : most);
+  return rows < 1 ? 1 : rows < workers ? rows : workers;
 }
 
 size_t norm_back_bytes(int rows, int B, int D) {
