@@ -368,7 +368,7 @@ HILO_DEV float4 through4(const float4 &n, const float4 &v, float2 t, float r) {
 // A worker is a workgroup: W > 1 waves that share a row, or (W = 1) four that take rows in turn and join their sums in
 // LDS where a segment ends, so that a slot holds four times the rows.
 template <bool BF16, int W, int NV>
-__global__ __launch_bounds__(W == 1 ? 256 : 64 * W, NV < 4 ? 3 : 2) void k_norm_residual_back(NormBackProblem p) {
+__global__ __launch_bounds__(W == 1 ? 256 : 64 * W, NV < 3 ? 3 : 2) void k_norm_residual_back(NormBackProblem p) {
   constexpr int G = W == 1 ? 4 : 1;
   __shared__ float2 red[2 * W];
   __shared__ float4 join[G == 1 ? 1 : G - 1][G == 1 ? 1 : 3 * NV][64];
@@ -403,34 +403,46 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W, NV < 4 ? 3 : 2) void k_norm_
         A[k] = B[k] = C[k] = zero4();
       }
     }
-#pragma unroll 1
-    for (int row = first + grp; row < sg.end; row += G) {
-      const size_t at = size_t(row) * p.D;
-      float4 g[NV], x[NV];
-      Raw4<BF16> dh[NV], y[NV];
-      const float4 st = gld4(global_ptr(p.stats + 4 * size_t(row)), 0);
+    // a row's loads, a row ahead: they are in flight while the row before is summed
+    float4 ng[NV], nx[NV], nst;
+    Raw4<BF16> ndh[NV], ny[NV];
+    auto load = [&](int r) __attribute__((always_inline)) {
+      const size_t at = size_t(r) * p.D;
+      nst = gld4(global_ptr(p.stats + 4 * size_t(r)), 0);
       if (p.dh) {
         const GlobalPtr pd = row_at<BF16>(p.dh, at), px = global_ptr(p.x_out + at);
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-          dh[k].load(pd, c[k]);
-          x[k] = gld4(px, 4 * c[k]);
+          ndh[k].load(pd, c[k]);
+          nx[k] = gld4(px, 4 * c[k]);
         }
       }
       if (p.dx_out) {
         const GlobalPtr pg = global_ptr(p.dx_out + at);
 #pragma unroll
-        for (int k = 0; k < NV; ++k) g[k] = gld4(pg, 4 * c[k]);
-      } else {
-#pragma unroll
-        for (int k = 0; k < NV; ++k) g[k] = zero4();
+        for (int k = 0; k < NV; ++k) ng[k] = gld4(pg, 4 * c[k]);
       }
       if (p.y) {
         const GlobalPtr py = row_at<BF16>(p.y, at);
 #pragma unroll
-        for (int k = 0; k < NV; ++k) y[k].load(py, c[k]);
+        for (int k = 0; k < NV; ++k) ny[k].load(py, c[k]);
       }
-      __builtin_amdgcn_sched_barrier(0);
+    };
+    if (first + grp < sg.end) load(first + grp);
+#pragma unroll 1
+    for (int row = first + grp; row < sg.end; row += G) {
+      const size_t at = size_t(row) * p.D;
+      float4 g[NV], x[NV];
+      Raw4<BF16> dh[NV], y[NV];
+      const float4 st = nst;
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        g[k] = p.dx_out ? ng[k] : zero4();
+        x[k] = nx[k];
+        dh[k] = ndh[k];
+        y[k] = ny[k];
+      }
+      if (row + G < sg.end) load(row + G);
       if (p.dh) {
         float a = 0.f, b = 0.f;
 #pragma unroll
@@ -585,7 +597,7 @@ __global__ __launch_bounds__(1024) void k_norm_sums(NormBackProblem p, bool both
 // 130.6, 117.5; 9000 of 1536 on 512, 768, 1024 68.3, 65.0, 66.2; 13000 of 512 39.1, 36.8, 38.2, 2000 of 512 on 256 and 512
 // 13.9 and 14.5.
 static int norm_back_workers(int rows, int D) {
-  const int share = 256 * (D <= 768 ? 10 : 5), most = D <= 1536 ? 3 : D <= 3072 ? 2 : 1;
+  const int share = 256 * (D <= 768 ? 10 : 5), most = D > 3072 ? 1 : D > 1536 || (D > 512 && D <= 768) ? 2 : 3;
   const int a_cu = (rows + share / 2) / share, workers = 256 * (a_cu < 1 ? 1 : a_cu < most ? a_cu : most);
   return rows < 1 ? 1 : rows < workers ? rows : workers;
 }
