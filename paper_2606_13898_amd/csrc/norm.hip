@@ -3,8 +3,8 @@
 //   u = norm(y) * post;  x' = alpha x + gate u;  h = norm(x') * pre * (1 + scale) + shift
 // Everything in float32; x and x' are float32, y and h the block's type, or h int8 codes with a scale per row.
 // What bounds both directions is memory: a row is read once, stays in registers through both norms and is written once.
-// A copy of 4 GiB reaches 4.74 TB/s; the forward pass on bf16 y 4.2 (2766 rows of 3072 in 24.2 us; with codes out 4708
-// rows of 1536 in 18.3 us, 4.4 TB/s), the backward pass 4.7 (22560 rows of 3072, 1.2 GB, in 257 us, and 16 us for the
+// A copy of 4 GiB reaches 4.74 TB/s; the forward pass on bf16 y 4.2 (2766 rows of 3072 in 24.0 us; with codes out 4708
+// rows of 1536 in 18.0 us, 4.4 TB/s), the backward pass 4.9 (22560 rows of 3072, 1.2 GB, in 253 us, and 11 us for the
 // sums).  Four rows of 3072 take 4.6 us: a load, two sums over four waves and a store, one behind the other.
 #include "common.h"
 #include "kernels.h"
@@ -523,9 +523,10 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W, NV < 3 ? 3 : 2) void k_norm_
 // The sums over a stream's slots: blockIdx.x stream (or, where both share a gain, both in turn), blockIdx.y 64 columns,
 // blockIdx.z which of A, B, C.  16 lanes of four columns by 64 groups; a sample's slots are dealt to 64 / samples groups
 // (a power of two), whose sums are joined in group order and written with the sample's vectors; then the gain's gradient
-// over the samples, in their order.  One launch for both: the slots and the gains' sums in two took as long for 8 samples
-// (16 us at D = 3072, 30 MB of slots) and a launch of 5 us more for few rows.
-__global__ __launch_bounds__(1024) void k_norm_sums(NormBackProblem p, bool both) {
+// over the samples, in their order.  One launch for both: the gains' sums in a second one took 5 us more for few rows.
+// Registers for two workgroups a CU, which hold all of them at once (D = 3072: 288; one a CU and a second round 11.6 us
+// for 19 MB of slots, 8.8 now).
+__global__ __launch_bounds__(1024, 8) void k_norm_sums(NormBackProblem p, bool both) {
   constexpr int G = 64;
   __shared__ float4 red[G][16];
   const int which = blockIdx.z, lane = threadIdx.x & 15, grp = threadIdx.x >> 4, c = blockIdx.y * 64 + 4 * lane;
