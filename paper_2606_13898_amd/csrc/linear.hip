@@ -191,14 +191,14 @@ HILO_DEV FewRows few_rows(const GemmProblem &p, int BM, int t, int *rows) {
   return FewRows{uni(sigma), uni(left < 0 ? 0 : left < BM ? left : BM)};
 }
 
-// Few rows: tiles of 16 MB rows x 16 NB columns, K split over the four waves of a workgroup in steps of 128, their sums
-// added through LDS.  What bounds it is the weights' way from memory: every wave streams its columns' bytes, 32 a lane
-// and step (whole lines of 16 rows), up to 2 GS steps ahead of the matrix core, and tiles are narrow so that the CUs share
-// them evenly (2 rows of 3072 -> 18432: 57 MB of weights in 13.0 us, 4.4 TB/s).  MR > 0 (MB = 1): x are float rows, which every workgroup quantises for itself into LDS, MR at a time -- each
-// wave the part of K that it multiplies, while its first weights are on their way; dynamic LDS holds the buffers' rows of
-// codes.
+// Few rows: tiles of 16 MB rows x `width` columns (at most 16 NB), K split over the four waves of a workgroup in steps of
+// 128, their sums added through LDS.  What bounds it is the weights' way from memory: every wave streams its columns'
+// bytes, 32 a lane and step (whole lines of 16 rows), up to 2 GS steps ahead of the matrix core, and tiles are narrow so
+// that the CUs share them evenly (2 rows of 3072 -> 18432: 57 MB of weights in 12.5 us, 4.5 TB/s).  MR > 0 (MB = 1): x are
+// float rows, which every workgroup quantises for itself into LDS, MR at a time -- each wave the part of K that it
+// multiplies, while its first weights are on their way; dynamic LDS holds the buffers' rows of codes.
 template <bool BF16, bool GELU, int MB, int NB, int MR>
-__global__ __launch_bounds__(256) void k_linear_i8_few(GemmProblem p) {
+__global__ __launch_bounds__(256) void k_linear_i8_few(GemmProblem p, int width) {
   constexpr int NW = 4, GS = NB == 1 ? 3 : 2;
   constexpr bool FUSED = MR > 0;
   __shared__ i32x4 part[NW][MB * NB][64];
@@ -207,7 +207,7 @@ __global__ __launch_bounds__(256) void k_linear_i8_few(GemmProblem p) {
   extern __shared__ __attribute__((aligned(16))) uint8_t codes[];
   const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lr = lane & 15, lg = lane >> 4;
-  const int n0 = blockIdx.x * 16 * NB;
+  const int n0 = blockIdx.x * width, n1 = min(n0 + width, p.N);
   const int steps = (p.K + 127) / 128, s0 = steps * wid / NW, s1 = steps * (wid + 1) / NW;
   const int kl = 16 * lg;
   const int8_t *W[NB];
@@ -224,7 +224,7 @@ __global__ __launch_bounds__(256) void k_linear_i8_few(GemmProblem p) {
   auto first_w = [&](int sigma) __attribute__((always_inline)) {
 #pragma unroll
     for (int j = 0; j < NB; ++j)
-      W[j] = reinterpret_cast<const int8_t *>(sigma ? p.W[1] : p.W[0]) + size_t(min(n0 + 16 * j + lr, p.N - 1)) * p.K;
+      W[j] = reinterpret_cast<const int8_t *>(sigma ? p.W[1] : p.W[0]) + size_t(min(n0 + 16 * j + lr, n1 - 1)) * p.K;
     load_w(s0, w[0]);
     load_w(s0 + GS, w[1]);
   };
@@ -338,7 +338,7 @@ __global__ __launch_bounds__(256) void k_linear_i8_few(GemmProblem p) {
   for (int f = wid; f < MB * NB; f += NW) {
     const i32x4 v = (part[0][f][lane] + part[1][f][lane]) + (part[2][f][lane] + part[3][f][lane]);
     const int rl = 16 * (f / NB) + lr, n = n0 + 16 * (f % NB) + 4 * lg;
-    if (rl < tr.n && n < p.N) i8_out4<BF16, GELU>(p, size_t(rows[rl]), n, v, FUSED ? sa : p.a_scale[rows[rl]], cols);
+    if (rl < tr.n && n < n1) i8_out4<BF16, GELU>(p, size_t(rows[rl]), n, v, FUSED ? sa : p.a_scale[rows[rl]], cols);
   }
 }
 
@@ -405,15 +405,15 @@ __global__ __launch_bounds__(256) void k_linear_i8_small(GemmProblem p) {
 }
 
 // Buffers of at most this many rows take the narrow tiles (few_rows numbers no more).  Codes in, on one side and on the
-// other the projections' tiles: 16 rows of 3072 -> 9216 11.3 and 14.8 us, 64 rows 19.8 and 20.7, of 3072 -> 3072 9.5 and
-// 12.6, of 12288 -> 3072 29.4 and 30.0, of 1024 -> 1024 6.8 and 6.9.
+// other the projections' tiles: 16 rows of 3072 -> 9216 9.8 and 15.0 us, 64 rows 18.7 and 20.9, of 3072 -> 3072 9.5 and
+// 12.6, of 12288 -> 3072 28.8 and 30.7, of 1024 -> 1024 6.8 and 6.9 (both near a launch's own time).
 constexpr long long kFewRows = 64;
 size_t linear_i8_part_bytes(long long rows, int K) { return rows <= kFewRows || !linear_i8_cuts(K) ? 0 : kSkPartBytes; }
 
 // Whether float rows are quantised by the kernel that multiplies them, or by a launch before it.
 // Up to four rows, whose codes fit the LDS: every workgroup reads them all, so more of them cost what the launch does.
-// bf16, fused and apart: 1 row of 3072 -> 18432 12.6 and 15.8 us, 4 rows 16.5 and 16.1, of 3072 -> 3072 7.4 and 9.6, of
-// 8192 -> 3072 12.2 and 15.7; 8 rows of 3072 -> 18432 22.7 and 17.8.
+// bf16, fused and apart: 1 row of 3072 -> 18432 12.4 and 14.7 us, 4 rows 14.3 and 15.0, of 3072 -> 3072 7.6 and 10.6, of
+// 8192 -> 3072 12.1 and 15.5; 5 rows of 3072 -> 9216 14.4 and 12.3, 8 rows -> 18432 18.9 and 15.7.
 static bool fused_few(const GemmProblem &p) { return p.max_img_rows <= 4 && p.max_img_rows * (p.K + 144) <= 49152; }
 // Short rows: a tile of 32 rows takes the time of its rows' bytes and 400 more each; apart costs the launch, the codes'
 // way through memory and a larger kernel's start.  Fused and apart at the product below, in us:
@@ -424,6 +424,28 @@ static bool fused_small(const GemmProblem &p, bool bf16) {
   return p.K <= kSmallK && double(p.max_img_rows) * ((p.N + 63) / 64) * (p.K * (bf16 ? 2 : 4) + 400) <= 90e6;
 }
 bool linear_i8_fuses(bool bf16, const GemmProblem &p) { return fused_few(p) || fused_small(p, bf16); }
+
+// Columns of a tile, up to 32 in one or two MFMA blocks (lanes behind them read the last column again, which costs no
+// memory time): those with which the fullest CU has the least to do, as the workgroups of a CU share its way to memory.
+// A workgroup costs its columns, the rows it reads for them and a start; two blocks, which leave fewer steps in flight,
+// a little more.  12, 16, 20, 24, 32 columns, K = 3072, in us (18432 / 256 CUs = 72):
+//    2 rows -> 18432 15.1, 13.6, 14.1, 12.8, 14.6     4 rows 17.2, 16.4, 15.7, 14.3, 15.6
+//   16 rows -> 18432 18.1, 17.1, 16.5, 14.6, 15.8     -> 9216 10.6, 11.3, 9.9, 10.1, 11.3
+//   64 rows -> 18432 42.5, 36.9, 34.1, 27.2, 28.2     -> 9216 22.9, 23.3, 18.3, 18.9, 19.6    -> 3072 9.5, 9.6, 11.8, 12.0, 12.4
+//    2 rows -> 12288 10.6, 10.3, 11.3, 10.6, 11.0
+static int few_width(int rows, int N, int row_tiles) {
+  int best = 0;
+  long long least = 0;
+  for (int w = 8; w <= 32; w += 4) {
+    const long long tiles = (long long)((N + w - 1) / w) * row_tiles;
+    const long long cost = (tiles + 255) / 256 * (w + (w > 16 ? 4 : 0) + 4 + rows);
+    if (best == 0 || cost < least) {
+      best = w;
+      least = cost;
+    }
+  }
+  return best;
+}
 
 template <bool BF16, bool GELU>
 static hipError_t run_linear_i8(const GemmProblem &p, hipStream_t st) {
@@ -437,22 +459,24 @@ static hipError_t run_linear_i8(const GemmProblem &p, hipStream_t st) {
     else hipLaunchKernelGGL((k_linear_i8_small<BF16, GELU, 12>), grid, dim3(256), 0, st, p);
     return hipGetLastError();
   }
-  // row tiles of the two streams.  Two column blocks a tile halve what is read of x per weight and leave half the
-  // workgroups: 64 rows of 3072, one and two, N = 4096 10.2 and 12.8 us, 8192 17.0 and 13.7, 18432 36.6 and 28.2
-  const int bm = rows <= 16 ? 16 : 64, bn = rows <= 16 || p.N < 8192 ? 16 : 32, streams = p.L > 0 ? 2 : 1;
-  const dim3 grid(unsigned((p.N + bn - 1) / bn), unsigned(streams * ((rows + bm - 1) / bm)));
-  if (p.a_scale == nullptr) {
-    const size_t lds = size_t(rows) * ((p.K + 127) / 128 * 128 + 16);
-    if (rows == 1) hipLaunchKernelGGL((k_linear_i8_few<BF16, GELU, 1, 1, 1>), grid, dim3(256), lds, st, p);
-    else if (rows == 2) hipLaunchKernelGGL((k_linear_i8_few<BF16, GELU, 1, 1, 2>), grid, dim3(256), lds, st, p);
-    else hipLaunchKernelGGL((k_linear_i8_few<BF16, GELU, 1, 1, 4>), grid, dim3(256), lds, st, p);
-  } else if (rows <= 16) {
-    hipLaunchKernelGGL((k_linear_i8_few<BF16, GELU, 1, 1, 0>), grid, dim3(256), 0, st, p);
-  } else if (bn == 16) {
-    hipLaunchKernelGGL((k_linear_i8_few<BF16, GELU, 4, 1, 0>), grid, dim3(256), 0, st, p);
-  } else {
-    hipLaunchKernelGGL((k_linear_i8_few<BF16, GELU, 4, 2, 0>), grid, dim3(256), 0, st, p);
-  }
+  const int bm = rows <= 16 ? 16 : 64, row_tiles = (p.L > 0 ? 2 : 1) * ((rows + bm - 1) / bm);  // of either stream
+  const int bn = few_width(rows, p.N, row_tiles);
+  const dim3 grid(unsigned((p.N + bn - 1) / bn), unsigned(row_tiles));
+  const size_t lds = p.a_scale == nullptr ? size_t(rows) * ((p.K + 127) / 128 * 128 + 16) : 0;
+#define HILO_FEW(MB, NB, MR) hipLaunchKernelGGL((k_linear_i8_few<BF16, GELU, MB, NB, MR>), grid, dim3(256), lds, st, p, bn)
+#define HILO_FEW_ROWS(NB)                        \
+  do {                                           \
+    if (p.a_scale != nullptr) {                  \
+      if (rows <= 16) HILO_FEW(1, NB, 0);        \
+      else HILO_FEW(4, NB, 0);                   \
+    } else if (rows == 1) HILO_FEW(1, NB, 1);    \
+    else if (rows == 2) HILO_FEW(1, NB, 2);      \
+    else HILO_FEW(1, NB, 4);                     \
+  } while (0)
+  if (bn <= 16) HILO_FEW_ROWS(1);
+  else HILO_FEW_ROWS(2);
+#undef HILO_FEW_ROWS
+#undef HILO_FEW
   return hipGetLastError();
 }
 

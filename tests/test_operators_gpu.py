@@ -508,6 +508,15 @@ def test_linear_i8_few_rows(dtype, lens, text, K, N):
     run_linear(dtype, lens, text, K, N, False, True, K, spare=0)
 
 
+# every width of the few rows' tiles (8 to 32 columns by fours, the last tile part of one), one and two streams
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("lens,text", [([2], 0), ([1, 3], 1), ([9, 5], 2), ([33, 20], 6)])
+@pytest.mark.parametrize("N", [1028, 2052, 4100, 5132, 6148, 7172, 12300])
+def test_linear_i8_few_rows_widths(dtype, lens, text, N):
+    print(f"[linear i8 few width] {dtype} lens={lens} text={text} N={N}", flush=True)
+    run_linear(dtype, lens, text, 144, N, True, True, N, spare=0)
+
+
 # every kind of plan of the large tiles (linear_schedule.py says which each shape reaches), both types of output
 @pytest.mark.parametrize("shape", [s for s, _ in linear_schedule.SHAPES], ids=lambda s: f"{sum(s[0])}x{s[2]}x{s[3]}")
 @pytest.mark.parametrize("dtype,gelu,bias", [("bf16", True, True), ("f32", False, True), ("bf16", False, False)])
