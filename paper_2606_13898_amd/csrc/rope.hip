@@ -4,8 +4,8 @@
 // Pair j of a head turns by t = position(axis of j) * frequency(j):  (a, b) -> (a cos t - b sin t, b cos t + a sin t).
 // All heads of a row turn alike, so a workgroup forms the cosines and sines of its rows once, in 64 bits, keeps them
 // as floats in LDS and streams the heads past them.  What bounds it is memory: every value is read and written once.
-// 2766 rows of 48 bf16 heads of 128 out of a packed projection, 68 MB, in 12.2 us (5.6 TB/s: a part comes from the last
-// level's cache; a copy of 4 GiB reaches 4.7); 22560 rows of 16 float32 heads of 64, 185 MB, in 39.2 us (4.7 TB/s).  One
+// 2766 rows of 48 bf16 heads of 128 out of a packed projection, 68 MB, in 11.8 us (5.7 TB/s: a part comes from the last
+// level's cache; a copy of 4 GiB reaches 4.7); 22560 rows of 16 float32 heads of 64, 185 MB, in 35.0 us (5.3 TB/s).  One
 // row takes 2.8 us, most of it the launch and the one chain of doubles to a cosine.
 #include "common.h"
 #include "kernels.h"
@@ -134,13 +134,13 @@ hipError_t launch_rope(bool bf16, RopeProblem p, hipStream_t st) {
   };
   while (V > 1 && !fits(V)) V /= 2;
   p.units_head = p.n / V + (copy ? rest / V : 0);
-  if (p.units_head == 0) return hipSuccess;  // in place, nothing turns
-  // rows of a workgroup: about six units a thread, so that forming the table (about 70 operations in doubles a row
-  // and pair, for all heads) hides behind the loads of the other workgroups, and a table that fits
+  // rows of a workgroup: a unit a thread and no more than one row over, and a table that fits.  Forming the table (about 70
+  // operations in doubles a row and pair, for all heads) hides behind other workgroups' loads, better the more there are:
+  // with 1, 2, 4, 9 units a thread 7680 rows of 48 heads of 128 38.1, 39.1, 40.6, 41.5 us, 1100 6.8, 6.7, 7.4, 9.6,
+  // 22560 float32 rows of 16 heads of 64 35.0, 36.0, 36.6, 40.7
   const int row_units = p.heads * p.units_head;
-  int br = (6 * 256 + row_units - 1) / row_units;
-  if (p.n > 0) br = br < kRopeTable / p.n ? br : kRopeTable / p.n;
-  p.block_rows = br < 1 ? 1 : br;
+  const int br = (256 + row_units - 1) / row_units;
+  p.block_rows = br < kRopeTable / p.n ? br : kRopeTable / p.n;
   const dim3 grid{unsigned((p.rows + p.block_rows - 1) / p.block_rows)};
 #define HILO_ROPE(B, VV)                                                              \
   do {                                                                                \
