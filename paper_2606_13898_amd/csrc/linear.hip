@@ -53,8 +53,9 @@ struct Raw8 {
 
 // One row per group of W waves, NC chunks of 8 values a lane (cols <= 512 W NC), read once; LOOP: any number of
 // columns, NC chunks at a time, read twice.  A lane behind the last column reads the last chunk again, which changes
-// no maximum.  Bound by memory: 22560 rows of 3072 bf16, 208 MB, in 45 us (4.6 TB/s, a large copy's rate); 2766 rows,
-// which the last level's cache holds, in 7.6.
+// no maximum.  Bound by memory: 22560 rows of 3072 bf16, 208 MB, in 37 us where the last level's cache holds what was
+// written before (5.6 TB/s), 46 where it does not (4.5); 2766 rows in 7 to 8.  One wave a row up to 2048 columns, four
+// above (22560 rows of 1536 on one and four 19.7 and 22.5 us, of 2048 25.7 and 26.5, of 3072 38.9 and 37.3).
 template <bool BF16, int W, int NC, bool LOOP>
 __global__ __launch_bounds__(256) void k_quantize_rows_i8(const void *__restrict__ x, int rows, int cols,
                                                           int8_t *__restrict__ codes, float *__restrict__ scale,
@@ -111,7 +112,7 @@ hipError_t launch_quantize_rows_i8(bool bf16, const void *x, int rows, int cols,
   } while (0)
   if (cols <= 512) HILO_Q8(1, 1, false);
   else if (cols <= 1024) HILO_Q8(1, 2, false);
-  else if (cols <= 2048) HILO_Q8(4, 1, false);
+  else if (cols <= 2048) HILO_Q8(1, 4, false);
   else if (cols <= 4096) HILO_Q8(4, 2, false);
   else if (cols <= 8192) HILO_Q8(4, 4, false);
   else if (cols <= 16384) HILO_Q8(4, 8, false);
