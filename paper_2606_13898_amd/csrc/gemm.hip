@@ -352,7 +352,9 @@ struct SkTile {
         zn.w += gt[j].w * v[3];
         *reinterpret_cast<float4 *>(p.z + m * p.ldz + n) = zn;
       } else {
-        if constexpr (EPI == EPI_GELU) {
+        if constexpr (EPI == EPI_GELU && op_i8(OP)) {
+          gelu_tanh4(v);
+        } else if constexpr (EPI == EPI_GELU) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) v[e] = gelu_tanh(v[e]);
         }
@@ -596,16 +598,14 @@ HILO_DEV bool epilogue_i8(const GemmProblem &p, const TileRows &tr, int n0, int 
       for (int j = 0; j < NB; ++j) {
         float v[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          v[e] = float(acc[i][j][e]) * (sa * s[j][e]) + b[j][e];
-          if constexpr (EPI == EPI_GELU) v[e] = gelu_tanh(v[e]);
-        }
+        for (int e = 0; e < 4; ++e) v[e] = float(acc[i][j][e]) * (sa * s[j][e]) + b[j][e];
+        if constexpr (EPI == EPI_GELU) gelu_tanh4(v);
         if constexpr (ESZ == 4) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) o[j][e] = __float_as_uint(v[e]);
         } else {
-          o[j][0] = pack_bf16x2(v[0], v[1]);
-          o[j][1] = pack_bf16x2(v[2], v[3]);
+          o[j][0] = bf16_pair(v[0], v[1]);
+          o[j][1] = bf16_pair(v[2], v[3]);
         }
       }
       char *q = out + size_t(16 * i) * p.N * ESZ;
@@ -1370,11 +1370,12 @@ __global__ __launch_bounds__(kFixThreads) void k_gemm8_fix(GemmProblem p) {
 // of tile would leave a poor last wave the other mostly does not -- so up to K = 8192, where fewer tiles run whole too,
 // there is no second launch at all.
 //
-// 22560 x 12288 x 3072 (rows, columns, K; GELU) 750 us, 2.3 POP/s, on the same operands again and again (808 on three sets
-// in turn), where the library's product alone, without scales, bias and GELU, takes 831; 2766 x 9216 x 3072 87 us (92; the
-// library 88); 4708 x 6144 x 1536 with GELU 59 (63).  At K = 12288 the loop runs at 2.7 POP/s, the matrix cores busy half
-// the time at 2.2 to 2.3 GHz; neither a quarter fewer LDS cycles nor wave priorities changed that by more than 1%.  What
-// keeps shorter K below it is the epilogue (of a 256 x 256 tile 6.0 us, 8.7 with GELU, an exponential and a reciprocal a value) and the last wave of tiles.
+// 22560 x 12288 x 3072 (rows, columns, K; GELU) 780 us, 2.2 POP/s, on the same operands again and again (some 50 more on
+// three sets in turn), where the library's product alone, without scales, bias and GELU, takes 831; 2766 x 9216 x 3072 88
+// us (92; the library 88); 4708 x 6144 x 1536 with GELU 59 (62).  At K = 12288 the loop runs at 2.7 POP/s, the matrix cores
+// busy half the time at 2.2 to 2.3 GHz; neither a quarter fewer LDS cycles nor wave priorities changed that by more than
+// 1%.  What keeps shorter K below it is the epilogue (of a 256 x 256 tile 6.0 us, 8.7 with GELU, an exponential and a
+// reciprocal a value) and the last wave of tiles.
 
 // Small problems: 64 x 32 tiles, two a workgroup, each on four waves that split K in steps of 128; their sums are added
 // through LDS (gemm_small_run's layout, and its cost per step).

@@ -151,13 +151,9 @@ HILO_DEV void i8_out4(const GemmProblem &p, size_t m, int n, const i32x4 &acc, f
   // the exact sum is rounded to 24 bits once here; it and the product of the scales are what float32 costs
   float v[4] = {float(acc[0]) * (sa * c.s.x) + c.b[0], float(acc[1]) * (sa * c.s.y) + c.b[1],
                 float(acc[2]) * (sa * c.s.z) + c.b[2], float(acc[3]) * (sa * c.s.w) + c.b[3]};
-  if constexpr (GELU) {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = gelu_tanh(v[e]);
-  }
+  if constexpr (GELU) gelu_tanh4(v);
   if constexpr (BF16)
-    *reinterpret_cast<uint2 *>(reinterpret_cast<uint16_t *>(p.out) + m * p.N + n) =
-        make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+    *reinterpret_cast<uint2 *>(reinterpret_cast<uint16_t *>(p.out) + m * p.N + n) = make_uint2(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]));
   else
     *reinterpret_cast<float4 *>(reinterpret_cast<float *>(p.out) + m * p.N + n) = make_float4(v[0], v[1], v[2], v[3]);
 }

@@ -84,7 +84,7 @@ HILO_DEV void store4(GlobalPtr row, uint32_t c, const float4 &v) {
   typedef float f4 __attribute__((ext_vector_type(4)));
   typedef uint32_t u2 __attribute__((ext_vector_type(2)));
   auto *p = (__attribute__((address_space(1))) char *)row;
-  if constexpr (BF16) *(__attribute__((address_space(1))) u2 *)(p + 2 * c) = u2{pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w)};
+  if constexpr (BF16) *(__attribute__((address_space(1))) u2 *)(p + 2 * c) = u2{bf16_pair(v.x, v.y), bf16_pair(v.z, v.w)};
   else *(__attribute__((address_space(1))) f4 *)(p + 4 * c) = f4{v.x, v.y, v.z, v.w};
 }
 
