@@ -1195,7 +1195,7 @@ HILO_DEV uint32_t plan_cost(uint32_t T, uint32_t nk, TileCost c) {
   return steps + ((T & (T - 1)) == 0 ? c.even : c.piece + c.piece_t * T);
 }
 
-enum Tile { TILE_192, TILE_256, TILE_SMALL };
+enum Tile { TILE_192, TILE_256, TILE_SMALL, TILE_128 };
 
 // The tile and its row tiles.  Nothing here divides by a value that is not a constant: every launch
 // waits for this, about 2 us when it formed the three plans instead.
@@ -1458,23 +1458,26 @@ HILO_DEV void small_run_i8(const GemmProblem &p, int rows, int pid, uint8_t *lds
   }
 }
 
-// The tile, and its row tiles: the shortest of three estimates in units of 10 ns, as choose_tile's.  Eight tiles a
+// The tile, and its row tiles: the shortest of four estimates in units of 10 ns, as choose_tile's.  Eight tiles a
 // workgroup, K 1536 .. 6144: a step of a 256 x 256 tile takes 1.48 us and the tile's rest 6.0 (8.7 with GELU), of a 192 x
-// 192 tile 0.91 and 5.6 (7.3).
+// 192 tile 0.91 and 5.6 (7.3), of 128 x 128 0.46 and 3.9 (4.3); the first windows take some 2.5 us more than the small
+// tiles' start.  128 x 128 is for problems that leave CUs without a larger tile: 700 x 4096 x 4096 25.1 us, 38.4 without it,
+// 512 x 3072 x 3072 20.6 and 31.3, 1404 x 1356 x 960 14.1 and 21.0; forced on 2766 x 9216 x 3072 106 and 94.
 template <int EPI>
 HILO_DEV Tile choose_tile_i8(const GemmProblem &p, int &rows) {
   constexpr uint32_t P = kGemmWorkgroups;
   constexpr bool GELU = EPI == EPI_GELU;
-  uint32_t r64 = 0, r192 = 0, r256 = 0;
+  uint32_t r64 = 0, r128 = 0, r192 = 0, r256 = 0;
   for (int s = 0; s < p.B; ++s) {
     const int img = cu_at(p.cu, s + 1) - p.L - cu_at(p.cu, s);
     r64 += (img + 63) / 64 + (p.L + 63) / 64;
+    r128 += (img + 127) / 128 + (p.L + 127) / 128;
     r192 += (img + 191) / 192 + (p.L + 191) / 192;
     r256 += (img + 255) / 256 + (p.L + 255) / 256;
   }
   const uint32_t nk = (p.K + 127) / 128, tiles = r64 * ((p.N + 31) / 32);
   auto cost = [&](uint32_t T, uint32_t step, uint32_t tile, uint32_t piece, uint32_t piece_t) __attribute__((always_inline)) {
-    if (T >= P || runs_whole(T, nk)) return (T + P - 1) / P * (nk * step + tile);
+    if (T >= P || runs_whole(T, nk)) return (T + P - 1) / P * (nk * step + tile) + 250;
     return T * nk / P * step + piece + piece_t * T;
   };
   uint32_t best = cost(r192 * ((p.N + 191) / 192), 91, GELU ? 730 : 560, 2700, 20);
@@ -1485,6 +1488,15 @@ HILO_DEV Tile choose_tile_i8(const GemmProblem &p, int &rows) {
     best = c256;
     rows = r256;
     t = TILE_256;
+  }
+  const uint32_t t128 = r128 * ((p.N + 127) / 128);
+  if (t128 >= P || runs_whole(t128, nk)) {  // whole tiles only: the fixup knows no others of this size
+    const uint32_t c128 = cost(t128, 46, GELU ? 430 : 390, 0, 0);
+    if (c128 < best) {
+      best = c128;
+      rows = r128;
+      t = TILE_128;
+    }
   }
   const uint32_t turns = (tiles + 2 * P - 1) / (2 * P);
   if (turns * ((nk + 3) / 4 * (tiles <= P ? 140 : 265) + 300) < best) {
@@ -1508,6 +1520,7 @@ __global__ __launch_bounds__(512, 2) void k_linear_i8(GemmProblem p) {
   switch (choose_tile_i8<EPI>(p, rows)) {
     case TILE_SMALL: small_run_i8<EPI, OP>(p, rows, pid, lds); break;
     case TILE_256: gemm8_run<256, 256, EPI, OP>(p, plan_i8<256>(p, rows), pid, lds); break;
+    case TILE_128: gemm8_run<128, 128, EPI, OP>(p, plan_i8<128>(p, rows), pid, lds); break;
     default: gemm8_run<192, 192, EPI, OP>(p, plan_i8<192>(p, rows), pid, lds);
   }
 }
