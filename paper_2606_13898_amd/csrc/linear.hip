@@ -402,8 +402,8 @@ __global__ __launch_bounds__(256) void k_linear_i8_small(GemmProblem p) {
 }
 
 // Buffers of at most this many rows take the narrow tiles (few_rows numbers no more).  Codes in, on one side and on the
-// other the projections' tiles: 16 rows of 3072 -> 9216 9.8 and 15.0 us, 64 rows 18.7 and 20.9, of 3072 -> 3072 9.5 and
-// 12.6, of 12288 -> 3072 28.8 and 30.7, of 1024 -> 1024 6.8 and 6.9 (both near a launch's own time).
+// other the projections' tiles: 16 rows of 3072 -> 9216 9.8 and 19.4 us, 64 rows 18.7 and 19.1, of 3072 -> 3072 9.5 and
+// 13.2, of 12288 -> 3072 28.7 and 30.9, of 1024 -> 1024 7.7 and 7.8 (both near a launch's own time).
 constexpr long long kFewRows = 64;
 size_t linear_i8_part_bytes(long long rows, int K) { return rows <= kFewRows || !linear_i8_cuts(K) ? 0 : kSkPartBytes; }
 
@@ -412,13 +412,13 @@ size_t linear_i8_part_bytes(long long rows, int K) { return rows <= kFewRows || 
 // bf16, fused and apart: 1 row of 3072 -> 18432 12.4 and 14.7 us, 4 rows 14.3 and 15.0, of 3072 -> 3072 7.6 and 10.6, of
 // 8192 -> 3072 12.1 and 15.5; 5 rows of 3072 -> 9216 14.4 and 12.3, 8 rows -> 18432 18.9 and 15.7.
 static bool fused_few(const GemmProblem &p) { return p.max_img_rows <= 4 && p.max_img_rows * (p.K + 144) <= 49152; }
-// Short rows: a tile of 32 rows takes the time of its rows' bytes and 400 more each; apart costs the launch, the codes'
-// way through memory and a larger kernel's start.  Fused and apart at the product below, in us:
-//   bf16     551 x 256 -> 1024  (8e6)  6.9,  9.3    2000 x 512 -> 1024 (46e6) 10.4, 16.9    8000 x 128 -> 512  (42e6) 10.2, 14.8
-//           1000 x 768 -> 2048 (62e6) 14.3, 18.9    4000 x 512 -> 1024 (91e6) 17.0, 17.9   16000 x 128 -> 1024 (168e6) 26.7, 18.5
-//   float32 1000 x 768 -> 1536 (83e6) 13.3, 20.1    8000 x 128 -> 1024 (117e6) 18.5, 16.7
+// Short rows: a tile of 32 rows takes the time of its rows' bytes (float32's count three quarters) and 400 more each; apart
+// costs the launch, the codes' way through memory and a larger kernel's start.  Fused and apart at the product below, in us:
+//   bf16     551 x 256 -> 1024  (8e6)  7.6, 10.6    2000 x 512 -> 1024 (46e6) 10.7, 13.2    8000 x 128 -> 512  (42e6) 10.5, 11.7
+//           1000 x 768 -> 2048 (62e6) 14.4, 14.2    1500 x 768 -> 2048 (93e6) 18.0, 14.2   16000 x 128 -> 1024 (168e6) 27.5, 18.8
+//   float32 1000 x 768 -> 1536 (65e6) 13.4, 15.4    8000 x 128 -> 1024 (100e6) 18.1, 17.0
 static bool fused_small(const GemmProblem &p, bool bf16) {
-  return p.K <= kSmallK && double(p.max_img_rows) * ((p.N + 63) / 64) * (p.K * (bf16 ? 2 : 4) + 400) <= 90e6;
+  return p.K <= kSmallK && double(p.max_img_rows) * ((p.N + 63) / 64) * (p.K * (bf16 ? 2 : 3) + 400) <= 65e6;
 }
 bool linear_i8_fuses(bool bf16, const GemmProblem &p) { return fused_few(p) || fused_small(p, bf16); }
 
