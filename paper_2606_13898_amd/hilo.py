@@ -498,9 +498,22 @@ def hilo_rope(r: hilo_rotary, x: torch.Tensor, pos: torch.Tensor, out: torch.Ten
 
 
 def hilo_token_positions(shape, fine_idx, pool_idx, counts, cu_seqlens, seg_off, text_pos, pos, stream=None):
-    _check("hilo_token_positions", lib().hilo_token_positions(
-        ctypes.byref(shape), _ptr(fine_idx), _ptr(pool_idx), _ptr(counts), _ptr(cu_seqlens), _ptr(seg_off),
-        _ptr(text_pos), _ptr(pos), _stream(stream)))
+    """pos [hilo_max_tokens(shape) rows or more][3] float32 of a compressed sequence's tokens from the int32 index lists of
+    hilo_select, shaped as it leaves them: fine_idx [G][N], pool_idx [G][N / 4], counts [G][2], cu_seqlens [batch + 1],
+    seg_off [G]; text_pos [text_len][3] float32 or None.  How many tokens there are only the device knows, so pos has to
+    hold the most that any token set can have."""
+    rows = hilo_max_tokens(shape)
+    if rows < 0:
+        raise HiloError("hilo_token_positions", 2)
+    if pos is None:
+        raise HiloError("hilo_token_positions", 1)
+    dev, grids, patches, i32, f32 = _on_device(pos), shape.batch * shape.images, shape.grid_h * shape.grid_w, torch.int32, torch.float32
+    if len(pos.shape) != 2 or pos.shape[0] < rows:
+        raise ValueError(f"pos: expected [{rows} rows or more][3], not {tuple(pos.shape)}")
+    _launch("hilo_token_positions", dev, stream, ctypes.byref(shape), _arg(fine_idx, i32, (grids, patches), dev, "fine_idx"),
+            _arg(pool_idx, i32, (grids, patches // 4), dev, "pool_idx"), _arg(counts, i32, (grids, 2), dev, "counts"),
+            _arg(cu_seqlens, i32, (shape.batch + 1,), dev, "cu_seqlens"), _arg(seg_off, i32, (grids,), dev, "seg_off"),
+            _arg(text_pos, f32, (shape.text_len, 3), dev, "text_pos"), _arg(pos, f32, (pos.shape[0], 3), dev, "pos"))
 
 
 def _vectors(h, vectors: dict, gains: dict):

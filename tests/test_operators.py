@@ -194,6 +194,69 @@ def test_binding_refuses():
         hilo.norms(post_gain=torch.zeros(2, 64, dtype=torch.bfloat16))
 
 
+class OnDevice:
+    """What the binding looks at of a tensor on a device: it has no memory, and a call that is not refused ends without one."""
+    is_cuda = True
+
+    def __init__(self, dtype, *shape, dev=0, contiguous=True):
+        self.dtype, self.shape, self.dev, self.contiguous = dtype, torch.Size(shape), dev, contiguous
+        self.device = torch.device("cuda", dev) if dev >= 0 else torch.device("cpu")
+
+    def __repr__(self):
+        return f"{self.dtype}{list(self.shape)} on {self.device}{'' if self.contiguous else ', strided'}"
+
+    def dim(self):
+        return len(self.shape)
+
+    def numel(self):
+        return self.shape.numel()
+
+    def get_device(self):
+        return self.dev
+
+    def is_contiguous(self):
+        return self.contiguous
+
+    def data_ptr(self):
+        return F
+
+
+def _position_args(**changed):
+    """hilo_token_positions of 2 samples of 3 grids of 4 x 6 patches and 5 text rows; `changed` by name."""
+    i, f = torch.int32, torch.float32
+    a = dict(fine_idx=OnDevice(i, 6, 24), pool_idx=OnDevice(i, 6, 6), counts=OnDevice(i, 6, 2), cu_seqlens=OnDevice(i, 3),
+             seg_off=OnDevice(i, 6), text_pos=OnDevice(f, 5, 3), pos=OnDevice(f, 2 * (3 * 30 + 5), 3))
+    return [hilo.hilo_shape(2, 3, 4, 6, 5, 64, 1, 64, 64, hilo.BF16), *dict(a, **changed).values()]
+
+
+@built
+@pytest.mark.parametrize("changed", [
+    dict(pos=OnDevice(torch.float32, 190, 2)), dict(pos=OnDevice(torch.float32, 189, 3)), dict(pos=OnDevice(torch.float32, 570)),
+    dict(pos=OnDevice(torch.bfloat16, 190, 3)), dict(pos=OnDevice(torch.float32, 190, 3, contiguous=False)),
+    dict(pos=OnDevice(torch.float32, 190, 3, dev=-1)), dict(pos=OnDevice(torch.float32, 190, 3, dev=1)),
+    dict(fine_idx=OnDevice(torch.int64, 6, 24)), dict(fine_idx=OnDevice(torch.int32, 5, 24)), dict(pool_idx=OnDevice(torch.int32, 6, 5)),
+    dict(pool_idx=OnDevice(torch.int32, 6, 6, dev=1)), dict(counts=OnDevice(torch.int32, 12)), dict(counts=OnDevice(torch.int32, 6, 1)),
+    dict(cu_seqlens=OnDevice(torch.int32, 2)), dict(cu_seqlens=OnDevice(torch.int64, 3)), dict(seg_off=OnDevice(torch.int32, 2)),
+    dict(text_pos=OnDevice(torch.float32, 4, 3)), dict(text_pos=OnDevice(torch.float64, 5, 3)),
+    dict(text_pos=OnDevice(torch.float32, 5, 3, contiguous=False))], ids=str)
+def test_token_positions_binding_refuses(changed):
+    """Tensors that the kernel would read or write past their ends, or as what they are not."""
+    with pytest.raises(ValueError):
+        hilo.hilo_token_positions(*_position_args(**changed), stream=0)
+
+
+@built
+def test_token_positions_binding_status():
+    with pytest.raises(hilo.HiloError) as e:
+        hilo.hilo_token_positions(*_position_args(pos=None), stream=0)
+    assert e.value.status == NULL
+    args = _position_args()
+    args[0].grid_w = 5
+    with pytest.raises(hilo.HiloError) as e:
+        hilo.hilo_token_positions(*args, stream=0)
+    assert e.value.status == SHAPE
+
+
 # ------------------------------------------------------------------------------------------ oracle
 
 @pytest.mark.parametrize("rms", [False, True])

@@ -377,3 +377,29 @@ def test_binding_refuses_device_tensors():
             call()
         assert e.value.status == want
     torch.cuda.synchronize()
+
+
+def test_token_positions_refuses_device_tensors():
+    """Tensors that are short, of another type or layout, or elsewhere raise; those that fit run, with a longer pos too."""
+    shape = hilo.hilo_shape(1, 1, 4, 4, 2, 64, 1, 64, 64, hilo.BF16)
+    T = hilo.hilo_max_tokens(shape)
+    i = lambda *s: torch.zeros(*s, dtype=I32, device="cuda")  # noqa: E731
+    # every patch fine: 16 image tokens in raster order, then the text
+    good = dict(fine_idx=torch.arange(16, dtype=I32, device="cuda")[None], pool_idx=i(1, 4),
+                counts=torch.tensor([[16, 0]], dtype=I32, device="cuda"), cu_seqlens=_cu(18), seg_off=i(1),
+                text_pos=torch.ones(2, 3, device="cuda"), pos=torch.full((T + 5, 3), 9.0, device="cuda"))
+    bad = [dict(pos=_empty(T - 1, 3)), dict(pos=_empty(T, 2)), dict(pos=_empty(T, 3, dtype=torch.float64)), dict(pos=_empty(T, 6)[:, ::2]),
+           dict(pos=_empty(T, 3).cpu()), dict(fine_idx=good["fine_idx"].long()), dict(fine_idx=i(1, 12)), dict(pool_idx=i(1, 3)),
+           dict(counts=i(2)), dict(cu_seqlens=_cu(9, 18)), dict(cu_seqlens=_cu(18).cpu()), dict(seg_off=i(2)),
+           dict(text_pos=torch.ones(1, 3, device="cuda")), dict(text_pos=torch.ones(3, 2, device="cuda").T)]
+    for k, changed in enumerate(bad):
+        with pytest.raises(ValueError):
+            hilo.hilo_token_positions(shape, *dict(good, **changed).values())
+            pytest.fail(f"call {k} was not refused")
+    with pytest.raises(hilo.HiloError) as e:
+        hilo.hilo_token_positions(shape, *dict(good, counts=None).values())
+    assert e.value.status == 1
+    hilo.hilo_token_positions(shape, *good.values())
+    torch.cuda.synchronize()
+    want = [[0, p // 4, p % 4] for p in range(16)] + [[1, 1, 1]] * 2
+    assert good["pos"][:18].tolist() == want and (good["pos"][18:] == 9).all()
