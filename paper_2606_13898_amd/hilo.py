@@ -408,8 +408,9 @@ def hilo_attention_core_noalloc(shape, qkv, cu_seqlens, out, stream=None):
 
 # ---------------------------------------------------- rotary positions, sandwich norms, int8 products
 #
-# These calls check what the library cannot see: types, shapes, layouts and devices of the tensors.  They run on the
-# current stream of the tensors' device, or on `stream`, which has to be one of that device.
+# These calls check what the library cannot see: types, shapes, layouts and devices of the tensors, and sizes that its
+# 32-bit arguments would cut to others.  They run on the current stream of the tensors' device, or on `stream`, which has
+# to be one of that device.
 
 _FLOATS = {torch.float32: F32, torch.bfloat16: BF16}
 
@@ -456,6 +457,12 @@ def _launch(fn, dev: int, stream, *args):
         raise HiloError(fn, st)
 
 
+def _int32(*values: int):
+    for v in values:
+        if not -(1 << 31) <= v < 1 << 31:
+            raise ValueError(f"{v} does not fit 32 bits")
+
+
 def _packed(cu: torch.Tensor, dev: int):
     if cu.dtype is not torch.int32 or cu.dim() != 1 or cu.numel() < 2 or not cu.is_contiguous():
         raise ValueError("cu_seqlens: expected int32 [batch + 1]")
@@ -472,6 +479,7 @@ def rotary(heads: int, head_dim: int, pairs: Sequence[int], base=10000.0, flags:
     bases = [float(base)] * axes if isinstance(base, (int, float)) else [float(b) for b in base]
     if len(bases) != axes:
         raise ValueError("one base, or one per axis")
+    _int32(heads, head_dim, flags, *pairs)
     return hilo_rotary(heads, head_dim, axes, flags, (ctypes.c_int32 * 4)(*pairs), (ctypes.c_double * 4)(*bases))
 
 
@@ -561,6 +569,7 @@ def norms(kind: int = NORM_LAYER, eps: float = 1e-6, residual_scale: float = 1.0
     """The norms on both sides of a block: gate, shift, scale float32 [batch][2][dim] (views of one modulation tensor
     will do: mod[:, :, 2] of [batch][2][6][dim]), gains a pair of float32 [dim] (image, text stream).  Keeps the
     tensors alive; their values are read by each call."""
+    _int32(kind)
     return _vectors(hilo_norms(kind, eps, residual_scale), {"gate": gate, "shift": shift, "scale": scale},
                     {"post_gain": post_gain, "pre_gain": pre_gain})
 
@@ -571,11 +580,13 @@ def norm_grads(*, gate=None, shift=None, scale=None, post_gain=None, pre_gain=No
                     {"post_gain": post_gain, "pre_gain": pre_gain})
 
 
-def _norm_rows(n, like: torch.Tensor, cu: torch.Tensor, others=None):
+def _norm_rows(fn: str, n, like: torch.Tensor, cu: torch.Tensor, text_len: int, others=None):
     if like.dim() != 2:
         raise ValueError("expected [rows][dim] tensors")
     dev, dim = _on_device(like), like.shape[1]
     batch, cu_ptr = _packed(cu, dev)
+    if (dim | batch | text_len) >> 31:  # negative, or more than 31 bits
+        raise HiloError(fn, 2)
     if n.fits != (dim, batch, dev):
         _fit(n, dim, batch, dev)
     if others is not None and others.fits != (dim, batch, dev):
@@ -592,7 +603,7 @@ def _fit(h, dim: int, batch: int, dev: int):
 def hilo_norm_residual(n: hilo_norms, y, x, x_out, h, cu, text_len: int = 0, *, h_scale=None, stats=None, stream=None):
     """x_out = residual_scale x + gate norm(y), h = norm(x_out) (1 + scale) + shift; y and x_out, or h, may be None.
     h int8 with h_scale [rows]: codes and row scales.  stats [rows][4] float32: for the backward pass."""
-    dev, dim, batch, cu_ptr = _norm_rows(n, x, cu)
+    dev, dim, batch, cu_ptr = _norm_rows("hilo_norm_residual", n, x, cu, text_len)
     shape, rows, f32 = x.shape, x.shape[0], torch.float32
     like = y if y is not None else h
     if like is None:
@@ -610,13 +621,13 @@ def hilo_norm_residual(n: hilo_norms, y, x, x_out, h, cu, text_len: int = 0, *, 
 
 
 def hilo_norm_residual_workspace_bytes(rows: int, batch: int, dim: int) -> int:
-    return lib().hilo_norm_residual_workspace_bytes(rows, batch, dim)
+    return 0 if (batch | dim) >> 31 else lib().hilo_norm_residual_workspace_bytes(rows, batch, dim)
 
 
 def hilo_norm_residual_backward(n: hilo_norms, dx_out, dh, y, x_out, stats, dx, dy, grads: Optional[hilo_norm_grads],
                                 cu, text_len: int = 0, workspace=None, stream=None):
     """Gradients of hilo_norm_residual from dx_out (or None) and dh (or None): dx, dy, and those in grads."""
-    dev, dim, batch, cu_ptr = _norm_rows(n, dx, cu, grads)
+    dev, dim, batch, cu_ptr = _norm_rows("hilo_norm_residual_backward", n, dx, cu, text_len, grads)
     shape, rows, f32 = dx.shape, dx.shape[0], torch.float32
     like = dh if dh is not None else y
     if like is None:
@@ -680,7 +691,7 @@ def linear_weights_i8(ws: Sequence[dict]):
 
 
 def hilo_linear_i8_workspace_bytes(rows: int, in_dim: int) -> int:
-    return lib().hilo_linear_i8_workspace_bytes(rows, in_dim)
+    return 0 if in_dim >> 31 else lib().hilo_linear_i8_workspace_bytes(rows, in_dim)
 
 
 def hilo_linear_i8(w, x, out, cu, text_len: int = 0, *, x_scale=None, act: int = ACT_NONE, workspace=None, stream=None):
@@ -699,6 +710,10 @@ def hilo_linear_i8(w, x, out, cu, text_len: int = 0, *, x_scale=None, act: int =
     rows = out.shape[0]
     n, k = w.shape
     batch, cu_ptr = _packed(cu, dev)
+    if (n | k | batch | text_len) >> 31:
+        raise HiloError("hilo_linear_i8", 2)
+    if act >> 31:
+        raise HiloError("hilo_linear_i8", 4)
     _launch("hilo_linear_i8", dev, stream, dtype, w,
             _arg(x, out.dtype if x_scale is None else torch.int8, (rows, k), dev, "x"),
             _arg(x_scale, torch.float32, (rows,), dev, "x_scale"), _arg(out, out.dtype, (rows, n), dev, "out"), rows, k, n,

@@ -217,6 +217,9 @@ class OnDevice:
     def is_contiguous(self):
         return self.contiguous
 
+    def element_size(self):
+        return self.dtype.itemsize
+
     def data_ptr(self):
         return F
 
@@ -255,6 +258,48 @@ def test_token_positions_binding_status():
     with pytest.raises(hilo.HiloError) as e:
         hilo.hilo_token_positions(*args, stream=0)
     assert e.value.status == SHAPE
+
+
+def _cuts_to(good):
+    """A size that 32 bits would cut to `good`."""
+    return (1 << 32) + good
+
+
+@built
+@pytest.mark.parametrize("dim,text", [(_cuts_to(64), 0), (1 << 31, 0), (64, _cuts_to(1)), (64, -1)])
+def test_norm_binding_keeps_sizes(dim, text, monkeypatch):
+    """Sizes past 32 bits are refused, and not taken for what is left of them."""
+    monkeypatch.setattr(hilo, "_current_device", lambda: 0)
+    x, cu, stats = OnDevice(torch.float32, 8, dim), OnDevice(torch.int32, 2), OnDevice(torch.float32, 8, 4)
+    for call in (lambda: hilo.hilo_norm_residual(hilo.norms(), x, x, x, x, cu, text, stream=0),
+                 lambda: hilo.hilo_norm_residual_backward(hilo.norms(), x, x, x, x, stats, x, x, None, cu, text, stream=0)):
+        with pytest.raises(hilo.HiloError) as e:
+            call()
+        assert e.value.status == SHAPE
+
+
+@built
+@pytest.mark.parametrize("k,n,text,act,status", [(_cuts_to(64), 64, 0, 0, SHAPE), (64, _cuts_to(64), 0, 0, SHAPE), (64, 64, _cuts_to(1), 0, SHAPE),
+                                                 (64, 64, -1, 0, SHAPE), (64, 64, 0, _cuts_to(1), PARAM), (64, 64, 0, -1, PARAM)])
+def test_linear_binding_keeps_sizes(k, n, text, act, status, monkeypatch):
+    monkeypatch.setattr(hilo, "_current_device", lambda: 0)
+    f = torch.float32
+    w = hilo.linear_weights_i8([{"w": OnDevice(torch.int8, n, k), "s": OnDevice(f, n)}])
+    with pytest.raises(hilo.HiloError) as e:
+        hilo.hilo_linear_i8(w, OnDevice(f, 8, k), OnDevice(f, 8, n), OnDevice(torch.int32, 2), text, act=act,
+                            workspace=OnDevice(torch.uint8, 1 << 30), stream=0)
+    assert e.value.status == status
+
+
+@built
+def test_handles_keep_sizes():
+    for bad in (lambda: hilo.rotary(_cuts_to(1), 64, (32,)), lambda: hilo.rotary(1, _cuts_to(64), (32,)),
+                lambda: hilo.rotary(1, 64, (_cuts_to(32),)), lambda: hilo.rotary(1, 64, (32,), flags=_cuts_to(1)),
+                lambda: hilo.norms(_cuts_to(1))):
+        with pytest.raises(ValueError, match="32 bits"):
+            bad()
+    assert hilo.hilo_linear_i8_workspace_bytes(8, _cuts_to(64)) == 0
+    assert hilo.hilo_norm_residual_workspace_bytes(8, _cuts_to(1), 64) == hilo.hilo_norm_residual_workspace_bytes(8, 1, _cuts_to(64)) == 0
 
 
 # ------------------------------------------------------------------------------------------ oracle
