@@ -49,19 +49,18 @@ template <> struct Raw<16> { using T = uint4; };
 // V consecutive values of a row.
 template <bool BF16, int V>
 struct Vec {
-  using T = typename Raw<V * (BF16 ? 2 : 4)>::T;
+  using E = std::conditional_t<BF16, uint16_t, float>;
   union {
-    T raw;
-    uint16_t h[V * (BF16 ? 1 : 2)];
-    float f[BF16 ? 1 : V];
+    typename Raw<V * sizeof(E)>::T raw;
+    E e[V];
   };
   HILO_DEV float get(int i) const {
-    if constexpr (BF16) return bf2f(h[i]);
-    else return f[i];
+    if constexpr (BF16) return bf2f(e[i]);
+    else return e[i];
   }
   HILO_DEV void set(int i, float v) {
-    if constexpr (BF16) h[i] = f2bf(v);
-    else f[i] = v;
+    if constexpr (BF16) e[i] = f2bf(v);
+    else e[i] = v;
   }
 };
 
@@ -73,6 +72,8 @@ template <bool BF16, int V, bool ADJ>
 __global__ __launch_bounds__(256) void k_rope(RopeProblem p) {
   using E = std::conditional_t<BF16, uint16_t, float>;
   using VV = Vec<BF16, V>;
+  // rows may start at any value: the launcher takes a V whose bytes divide every address, and a VV asks for no more
+  static_assert(sizeof(VV) == V * sizeof(E) && alignof(VV) == V * sizeof(E), "a vector is its values and no more");
   __shared__ float2 cs[kRopeTable];
   const int rows = p.rows_end ? min((long long)p.rows, (long long)cu_at(p.rows_end, 0)) : p.rows;
   const int row0 = blockIdx.x * p.block_rows, nr = min(p.block_rows, rows - row0);
