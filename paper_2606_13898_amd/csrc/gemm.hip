@@ -586,8 +586,8 @@ HILO_DEV bool epilogue_i8(const GemmProblem &p, const TileRows &tr, int n0, int 
   }
   char *out = reinterpret_cast<char *>(p.out) + (size_t(tr.row0 + wm * 16 * MB) * p.N + n0) * ESZ;
   const uint32_t row = uint32_t(lr) * uint32_t(p.N) * ESZ;  // below 2^30
-  // INSIDE: all of the wave's rows and columns exist, and rows start at multiples of 16 bytes (N % 4 == 0 alone leaves
-  // bf16 rows 8 off)
+  // INSIDE: all of the wave's rows and columns exist, and bf16 rows start at multiples of 16 bytes (N % 4 == 0, or an
+  // output that is aligned to 8 only, leaves them 8 off)
   auto rows = [&](auto inside) __attribute__((always_inline)) {
     constexpr bool INSIDE = decltype(inside)::value;
 #pragma unroll
@@ -627,7 +627,8 @@ HILO_DEV bool epilogue_i8(const GemmProblem &p, const TileRows &tr, int n0, int 
       asm volatile("" ::: "memory");  // the next block's operands stay below these stores
     }
   };
-  const bool inside = uni(int((wm + 1) * 16 * MB <= tr.nrows && n0 + 16 * NB <= p.N && p.N % 8 == 0)) != 0;
+  const bool inside = uni(int((wm + 1) * 16 * MB <= tr.nrows && n0 + 16 * NB <= p.N && p.N % 8 == 0 &&
+                              (ESZ == 4 || reinterpret_cast<uintptr_t>(p.out) % 16 == 0))) != 0;
   if (inside) rows(std::true_type{});
   else rows(std::false_type{});
   return inside;

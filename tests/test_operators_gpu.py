@@ -566,3 +566,27 @@ def test_linear_i8_not_finite_row():
     torch.cuda.synchronize()
     assert not torch.isfinite(bad[[2, 4]].float()).any()
     assert torch.equal(bad[[0, 1, 3, 5]], out[[0, 1, 3, 5]])
+
+
+# small tiles, 128 x 128, 192 x 192 and 256 x 256 ones (linear_schedule.py), whole tiles inside; buffers of few rows
+@pytest.mark.parametrize("lens,text,K,N,spare", [([300], 100, 1040, 520, 3), ([900], 100, 2064, 2040, 3), ([2500], 30, 528, 2048, 3),
+                                                 ([4096], 0, 1040, 4096, 3), ([30], 4, 272, 136, 0)])
+def test_linear_i8_output_at_8_bytes(lens, text, K, N, spare):
+    """bf16 rows that start 8 bytes behind a multiple of 16: the bits of rows that do not, and nothing beside them."""
+    print(f"[linear i8 out] lens={lens} K={K} N={N}", flush=True)
+    T, cu = sum(lens) + spare, _dev(_cu(lens), torch.int32)
+    g = torch.Generator(device="cuda").manual_seed(N)
+    w = [hilo.quantize_i8_weights(torch.randn(N, K, device="cuda", generator=g), torch.randn(N, device="cuda", generator=g).bfloat16())
+         for _ in range(2)]
+    plan, x = hilo.linear_weights_i8(w), torch.randn(T, K, device="cuda", generator=g).bfloat16()
+    ws = torch.empty(hilo.hilo_linear_i8_workspace_bytes(T, K), dtype=torch.uint8, device="cuda")
+    out = torch.full((T, N), 9.0, dtype=torch.bfloat16, device="cuda")
+    buf = torch.full((T * N + 8,), 9.0, dtype=torch.bfloat16, device="cuda")
+    off = buf[4:4 + T * N].view(T, N)
+    assert out.data_ptr() % 16 == 0 and off.data_ptr() % 16 == 8
+    for act in (hilo.ACT_NONE, hilo.ACT_GELU):
+        hilo.hilo_linear_i8(plan, x, out, cu, text, act=act, workspace=ws)
+        hilo.hilo_linear_i8(plan, x, off, cu, text, act=act, workspace=ws)
+        torch.cuda.synchronize()
+        assert torch.equal(off, out) and (off[sum(lens):] == 9).all() and (buf[:4] == 9).all() and (buf[-4:] == 9).all()
+        assert out[:sum(lens)].float().std() > 0.1
