@@ -2,12 +2,14 @@
 enqueued, and the float64 oracle against other ways to the same values (CPU only)."""
 import ctypes
 import os
+import re
 
 import numpy as np
 import pytest
 import torch
 
 import linear_schedule
+import norm_schedule
 from oracle import hilo_operators as Q
 from paper_2606_13898_amd import hilo
 
@@ -394,3 +396,31 @@ def test_linear_plans_cut_no_tile_of_short_k():
         K, N = 16 * int(rng.integers(1, 513)), 4 * int(rng.integers(1, 3000))
         plan = linear_schedule.describe(lens, text, K, N, bool(rng.integers(2)))
         assert plan[0] == "small" or (plan[2] == 1 and plan[4] == 0), (lens, text, K, N, plan)
+
+
+def test_norm_forms_are_the_launchers():
+    """The widths of norm_schedule.FORMS are those that the launchers go by, forward and backward."""
+    source = open(os.path.join(os.path.dirname(hilo.__file__), "csrc", "norm.hip")).read()
+    for macro in ("HILO_NR", "HILO_NB"):
+        found = re.findall(r"if \(p\.D <= (\d+)\) %s\((\d), (\d)\);" % macro, source)
+        last = re.findall(r"else %s\((\d), (\d)\);" % macro, source)
+        assert [tuple(map(int, f)) for f in found] + [(8192, *map(int, last[-1]))] == norm_schedule.FORMS
+
+
+@pytest.mark.parametrize("shapes,workers", [(norm_schedule.FORWARD, norm_schedule.workers), (norm_schedule.BACKWARD, norm_schedule.back_workers)],
+                         ids=["forward", "backward"])
+def test_norm_shapes_share_rows(shapes, workers):
+    """Every form, at both ends of its widths, with shares of several rows, some of which cross into the next segment.
+    Backward: no sum is longer than the tolerances of its test allow."""
+    reached, back = {}, workers is norm_schedule.back_workers
+    for D, rows in shapes:
+        lens, P = norm_schedule.lens(rows), workers(rows + 2, D)
+        most, crossing, met = norm_schedule.describe(lens, norm_schedule.TEXT, P)
+        several = 9 if back and norm_schedule.form(D)[0] == 1 else 3
+        assert sum(lens) == rows > P and most >= several and crossing >= 2 and met >= 2, (D, rows, most, crossing, met)
+        reached.setdefault(norm_schedule.form(D), set()).add(D)
+        if back:
+            assert norm_schedule.longest_sum(lens, norm_schedule.TEXT, D, P) <= 80
+    for low, (top, W, NV) in zip([0] + [f[0] for f in norm_schedule.FORMS], norm_schedule.FORMS):
+        assert {low + 4, top} <= reached[W, NV]
+    assert len({workers(rows + 2, D) for D, rows in shapes}) >= 3

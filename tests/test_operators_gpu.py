@@ -7,6 +7,7 @@ import pytest
 import torch
 
 import linear_schedule
+import norm_schedule
 from oracle import hilo_operators as Q
 from paper_2606_13898_amd import hilo
 
@@ -590,3 +591,31 @@ def test_linear_i8_output_at_8_bytes(lens, text, K, N, spare):
         torch.cuda.synchronize()
         assert torch.equal(off, out) and (off[sum(lens):] == 9).all() and (buf[:4] == 9).all() and (buf[-4:] == 9).all()
         assert out[:sum(lens)].float().std() > 0.1
+
+
+# ------------------------------------------------------------------- norms whose workers take several rows
+#
+# The same checks on more rows than there are workers, every form at both ends of its widths (norm_schedule.py): rows read
+# ahead, vectors kept over a segment's rows and read again where a share crosses into the next one, sums over a row's waves
+# in turn, slots of several segments.  A row's own sums are no longer than above, so its tolerances hold; a segment's are
+# within the 80 additions that the backward pass' count (the longest of these shapes' is checked on the host).
+
+def _types(i):
+    return [("bf16", False), ("f32", True), ("f32", False), ("bf16", True)][i % 4]
+
+
+@pytest.mark.parametrize("i,D,rows", [(i, *s) for i, s in enumerate(norm_schedule.FORWARD)])
+def test_norm_residual_many_rows(i, D, rows):
+    dtype, rms = _types(i)
+    test_norm_residual(dtype, norm_schedule.lens(rows), norm_schedule.TEXT, D, rms, True, True)
+
+
+@pytest.mark.parametrize("i,D,rows", [(i, *s) for i, s in enumerate(norm_schedule.FORWARD)])
+def test_norm_residual_codes_many_rows(i, D, rows):
+    test_norm_residual_codes(_types(i + 2)[0], norm_schedule.lens(rows), norm_schedule.TEXT, D)
+
+
+@pytest.mark.parametrize("i,D,rows", [(i, *s) for i, s in enumerate(norm_schedule.BACKWARD)])
+def test_norm_residual_backward_many_rows(i, D, rows):
+    dtype, rms = _types(i + 1)
+    test_norm_residual_backward(dtype, norm_schedule.lens(rows), norm_schedule.TEXT, D, rms, True, True)
