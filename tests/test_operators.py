@@ -424,3 +424,11 @@ def test_norm_shapes_share_rows(shapes, workers):
     for low, (top, W, NV) in zip([0] + [f[0] for f in norm_schedule.FORMS], norm_schedule.FORMS):
         assert {low + 4, top} <= reached[W, NV]
     assert len({workers(rows + 2, D) for D, rows in shapes}) >= 3
+
+
+def test_linear_plans_with_gelu():
+    """With GELU, whose tiles cost more, the same shapes reach whole tiles of every size, cut ones of both and the small ones."""
+    kinds = {(p[0], p[0] != "small" and p[2] > 1, p[0] != "small" and p[4] > 0)
+             for p in (linear_schedule.describe(*shape, True) for shape, _ in linear_schedule.SHAPES)}
+    assert kinds == {("small", False, False), (128, False, False), (192, False, False), (256, False, False), (192, True, False),
+                     (192, True, True), (256, True, True)}

@@ -619,3 +619,25 @@ def test_norm_residual_codes_many_rows(i, D, rows):
 def test_norm_residual_backward_many_rows(i, D, rows):
     dtype, rms = _types(i + 1)
     test_norm_residual_backward(dtype, norm_schedule.lens(rows), norm_schedule.TEXT, D, rms, True, True)
+
+
+# ------------------------------------------------------------ int8 products: forms that the cases above leave out
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("text,K", [(0, 144), (1, 144), (0, 3088)])
+@pytest.mark.parametrize("N", [4100, 5132, 6148, 7172])
+def test_linear_i8_one_row_wide(dtype, text, K, N):
+    """One float row on tiles of two column blocks (20, 24, 28 and 32 columns, and where a stream has none 12 and 16)."""
+    print(f"[linear i8 one row] {dtype} text={text} K={K} N={N}", flush=True)
+    run_linear(dtype, [1], text, K, N, text == 0, True, N, spare=0)
+
+
+@pytest.mark.parametrize("shape", [s for s, _ in linear_schedule.SHAPES], ids=lambda s: f"{sum(s[0])}x{s[2]}x{s[3]}")
+@pytest.mark.parametrize("gelu,bias", [(True, True), (False, False)])
+def test_linear_i8_plans_f32(shape, gelu, bias):
+    """float32 rows out of the large tiles with GELU, and without a bias; test_operators.py holds which plans GELU reaches."""
+    lens, text, K, N = shape
+    print(f"[linear i8 plan f32] lens={lens} text={text} K={K} N={N} gelu={gelu}", flush=True)
+    T = sum(lens)
+    rows = None if T * N * K < 3e9 else np.sort(np.random.default_rng(1).choice(T, 100, replace=False))
+    run_linear("f32", lens, text, K, N, gelu, bias, 8, rows)
