@@ -477,7 +477,10 @@ hilo_status hilo_quantize_rows_i8(int32_t dtype, const void *x, int64_t rows, in
  * in_dim % 16 == 0, 16 .. 65536; out_dim % 4 == 0, below 2^24; batch <= 4096;
  * (rows / 64 + 2 batch) * (out_dim / 32 + 1) < 2^31 (HILO_E_SHAPE); act unknown: HILO_E_PARAM.
  * workspace: ws_bytes >= hilo_linear_i8_workspace_bytes(rows, in_dim) of device scratch, contents undefined
- * after; calls that may overlap, two captured graphs among them, need one each.                 */
+ * after; calls that may overlap, two captured graphs among them, need one each.  It holds codes and scales of
+ * float rows and, for in_dim above 8192, partial tiles; calls with codes, or that cut no tile, take the same size.
+ * Above 64 rows, time grows with the samples times the tiles (each looks its segment up among all samples): some
+ * tens of samples a call are meant, hundreds are slow, and thousands take a fraction of a second.   */
 typedef enum { HILO_ACT_NONE = 0, HILO_ACT_GELU = 1 } hilo_act;
 typedef struct {
   const int8_t *w; /* [out_dim][in_dim] codes */

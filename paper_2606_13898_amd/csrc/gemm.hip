@@ -434,8 +434,9 @@ HILO_DEV int swz(int r) {
   else return (r >> 1) & 7;
 }
 // The rows of W.  In PAIRED order they are read as 8 g + 4 p + 0 .. 3 (pairs of fragment columns) and 4 g + 0 .. 3: bits
-// 1, 3 and 4 tell the first apart, bits 1 to 3 the second.  By swz two lanes of a group fell on one bank group: a quarter
-// of the LDS cycles, though only 1% of the time (22560 x 12288 x 3072 753 -> 749 us).
+// 1, 3 and 4 tell the first apart, bits 1 to 3 the second.  By swz two lanes of a group fall on one bank group: a quarter
+// of the LDS cycles, though of the time no more than the noise (22560 x 12288 x 3072 with GELU, codes in, in turn: 750 to
+// 758 us, by swz 754 to 756).
 template <typename G>
 HILO_DEV int swz_w(int r) {
   if constexpr (G::ORDER == COLS_PAIRED) return ((r >> 1) & 1) | ((r >> 2) & 2) | ((r ^ (r >> 2)) & 4);
@@ -1371,12 +1372,17 @@ __global__ __launch_bounds__(kFixThreads) void k_gemm8_fix(GemmProblem p) {
 // of tile would leave a poor last wave the other mostly does not -- so up to K = 8192, where fewer tiles run whole too,
 // there is no second launch at all.
 //
-// 22560 x 12288 x 3072 (rows, columns, K; GELU) 780 us, 2.2 POP/s, on the same operands again and again (some 50 more on
-// three sets in turn), where the library's product alone, without scales, bias and GELU, takes 831; 2766 x 9216 x 3072 88
-// us (92; the library 88); 4708 x 6144 x 1536 with GELU 59 (62).  At K = 12288 the loop runs at 2.7 POP/s, the matrix cores
-// busy half the time at 2.2 to 2.3 GHz; neither a quarter fewer LDS cycles nor wave priorities changed that by more than
-// 1%.  What keeps shorter K below it is the epilogue (of a 256 x 256 tile 6.0 us, 8.7 with GELU, an exponential and a
-// reciprocal a value) and the last wave of tiles.
+// Codes in, bf16 out, over several boxes: 22560 x 12288 x 3072 (rows, columns, K; GELU) as one sample 740 to 760 us, 2.2 to
+// 2.3 POP/s, and some 800 as a ragged batch of 8 with text, 18 rounds of tiles in the place of 17 (the library's product
+// alone, without scales, bias and GELU: 830); 2766 x 9216 x 3072 88 on the same operands again and again, 92 to 98 on three
+// sets in turn (the library 86 to 88); 4708 x 6144 x 1536 with GELU 55 to 59.  float32 out, whose rows are twice as long:
+// 814, 101 (against 96) and 76 us.  At K = 12288 the loop runs at 2.7 POP/s, the matrix cores busy half the time at 2.2 to
+// 2.3 GHz; neither a quarter fewer LDS cycles nor wave priorities changed that by more than 1%.  What keeps shorter K below it
+// is the epilogue (of a 256 x 256 tile 6.0 us, 8.7 with GELU, an exponential and a reciprocal a value) and the last wave of
+// tiles.
+//
+// Every tile finds its segment by walking the samples, and short segments leave most of a tile empty: 8192 rows -> 6144, K =
+// 1536, as 1, 16, 64 samples 80, 85, 215 us, as 256 and 1024 1.9 and 25 ms, as 4096 387 ms.
 
 // Small problems: 64 x 32 tiles, two a workgroup, each on four waves that split K in steps of 128; their sums are added
 // through LDS (gemm_small_run's layout, and its cost per step).

@@ -417,6 +417,10 @@ static bool fused_few(const GemmProblem &p) { return p.max_img_rows <= 4 && p.ma
 //   bf16     551 x 256 -> 1024  (8e6)  7.6, 10.6    2000 x 512 -> 1024 (46e6) 10.7, 13.2    8000 x 128 -> 512  (42e6) 10.5, 11.7
 //           1000 x 768 -> 2048 (62e6) 14.4, 14.2    1500 x 768 -> 2048 (93e6) 18.0, 14.2   16000 x 128 -> 1024 (168e6) 27.5, 18.8
 //   float32 1000 x 768 -> 1536 (65e6) 13.4, 15.4    8000 x 128 -> 1024 (100e6) 18.1, 17.0
+//            700 x 768 -> 2048 (61e6) 14.0, 16.0     900 x 768 -> 2048 (78e6)  16.5, 16.0
+//           2500 x 512 -> 1024 (77e6) 14.4, 15.5    3000 x 512 -> 1024 (93e6)  16.2, 15.7
+// The two meet at 65e6 to 75e6 in bf16 and 75e6 to 90e6 in float32, but for K = 256, where fused stays ahead further than that:
+// 5000 x 256 -> 1024 12.6, 15.9 (bf16, 73e6) and 14.9, 17.7 (float32, 93e6).
 static bool fused_small(const GemmProblem &p, bool bf16) {
   return p.K <= kSmallK && double(p.max_img_rows) * ((p.N + 63) / 64) * (p.K * (bf16 ? 2 : 3) + 400) <= 65e6;
 }

@@ -3,9 +3,11 @@
 //   u = norm(y) * post;  x' = alpha x + gate u;  h = norm(x') * pre * (1 + scale) + shift
 // Everything in float32; x and x' are float32, y and h the block's type, or h int8 codes with a scale per row.
 // What bounds both directions is memory: a row is read once, stays in registers through both norms and is written once.
-// A copy of 4 GiB reaches 4.74 TB/s; the forward pass on bf16 y 4.2 (2766 rows of 3072 in 24.0 us; with codes out 4708
-// rows of 1536 in 18.0 us, 4.4 TB/s), the backward pass 4.9 (22560 rows of 3072, 1.2 GB, in 253 us, and 11 us for the
-// sums).  Four rows of 3072 take 4.6 us: a load, two sums over four waves and a store, one behind the other.
+// A copy of 4 GiB reaches 4.74 TB/s; the forward pass on bf16 y 4.2 (2766 rows of 3072 in 24.0 us, with or without
+// statistics; with codes out 4708 rows of 1536 in 19 us call after call, 22 to 23 between products that fill the cache), the
+// backward pass 4.9 (22560 rows of 3072, 1.2 GB, in 253 us, and 11 us for the sums).  Fewer rows stay further from it: 1100
+// rows of 3072 12.9 and 23 us (3.1 and 2.6 TB/s), 300 6.0 and 17.  Four rows of 3072 take 4.6 us: a load, two sums over
+// four waves and a store, one behind the other.
 #include "common.h"
 #include "kernels.h"
 
@@ -524,8 +526,8 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W, NV < 3 ? 3 : 2) void k_norm_
 // blockIdx.z which of A, B, C.  16 lanes of four columns by 64 groups; a sample's slots are dealt to 64 / samples groups
 // (a power of two), whose sums are joined in group order and written with the sample's vectors; then the gain's gradient
 // over the samples, in their order.  One launch for both: the gains' sums in a second one took 5 us more for few rows.
-// Registers for two workgroups a CU, which hold all of them at once (D = 3072: 288; one a CU and a second round 11.6 us
-// for 19 MB of slots, 8.8 now).
+// Registers for two workgroups a CU, which hold all of them at once (D = 3072: 288; one a CU and a second round 13.8 us
+// for 19 MB of slots, 10.8 now).
 __global__ __launch_bounds__(1024, 8) void k_norm_sums(NormBackProblem p, bool both) {
   constexpr int G = 64;
   __shared__ float4 red[G][16];
