@@ -14,9 +14,9 @@ namespace hilo {
 
 namespace {
 
-// cos and sin of 2 pi t.  The turn is reduced in double (a position of millions of turns keeps its fraction: k_rope
-// forms the frequencies in double too, pow2 of steps that the host takes logarithms for), to at most an eighth from the nearest quarter; there the Taylor series of
-// both, to the 13th and 12th power, are off by less than 2^-40.  Rounded to float once.
+// cos and sin of 2 pi t.  The turn is reduced in double (a position of millions of turns keeps its fraction: k_rope forms
+// the frequencies in double too, as powers of 2 whose logarithms the host takes), to at most an eighth from the nearest
+// quarter; there the Taylor series of both, to the 13th and 12th power, are off by less than 2^-40.  Rounded to float once.
 HILO_DEV float2 turn(double t) {
   const double q = rint(4.0 * t);
   const double x = (t - 0.25 * q) * 6.283185307179586476925;
