@@ -481,7 +481,7 @@ hilo_status hilo_quantize_rows_i8(int32_t dtype, const void *x, int64_t rows, in
  * float rows and, for in_dim above 8192, partial tiles; calls with codes, or that cut no tile, take the same size.
  * Above 64 rows, time grows with the samples times the tiles (each looks its segment up among all samples): some
  * tens of samples a call are meant, hundreds are slow, and thousands take a fraction of a second.   */
-typedef enum { HILO_ACT_NONE = 0, HILO_ACT_GELU = 1 } hilo_act;
+typedef enum { HILO_ACT_NONE = 0, HILO_ACT_GELU = 1, HILO_ACT_SILU = 2 /* gates only */ } hilo_act;
 typedef struct {
   const int8_t *w; /* [out_dim][in_dim] codes */
   const float *s;  /* [out_dim] scales        */
@@ -492,6 +492,86 @@ hilo_status hilo_linear_i8(int32_t dtype, const hilo_linear_w_i8 w[2], const voi
                            int32_t text_len, const int32_t *cu_seqlens, void *workspace, size_t ws_bytes,
                            void *stream);
 size_t hilo_linear_i8_workspace_bytes(int64_t rows, int32_t in_dim); /* 0 if invalid */
+
+/* ---------------------------------------------------------------------------------------------
+ * The products of a feed-forward, with a gate or without, and their gradients.  Rows as for the operators
+ * above; batch <= 4096.  Per row, with the weights of its stream:
+ *   u = x w^T + b                          no gate: out = u, act NONE
+ *   g = x w_gate^T + b_gate                with one: out = act(g) u, act SILU or GELU
+ * SILU(g) = g / (1 + exp(-g)), GELU the tanh form of hilo_mlp.  Products and sums are float32 (of float32
+ * values as well); out is rounded to dtype once.  Either both streams have a gate or neither (HILO_E_NULL);
+ * stream 1 is not looked at when text_len is 0.  Where all pointers of both streams are the same, rows are
+ * not split by stream, which is faster on many short samples.
+ * in_dim and out_dim: multiples of 8, 8 .. 65536 (HILO_E_SHAPE).  Every tensor is aligned to 16 bytes, the
+ * workspace to 256 (HILO_E_PARAM).  Outputs do not overlap inputs.  Workspace: device scratch of at least the
+ * bytes that the function beside it gives (HILO_E_WORKSPACE; NULL will do where that is 0), contents undefined
+ * after; calls that may overlap, two captured graphs among them, need one each.  Sums are taken in a fixed
+ * order: equal inputs give equal bits.
+ * --------------------------------------------------------------------------------------------- */
+typedef struct {
+  const void *w;      /* [out_dim][in_dim] dtype */
+  const void *b;      /* [out_dim] dtype or NULL */
+  const void *w_gate; /* the gate's, or NULL: no gate */
+  const void *b_gate;
+} hilo_linear_w;
+
+/* x [rows][in_dim], out [rows][out_dim]; pre [rows][2][out_dim] or NULL: g, then u, for the backward pass
+ * (only with a gate: HILO_E_PARAM otherwise); all dtype.                                          */
+hilo_status hilo_linear(int32_t dtype, const hilo_linear_w w[2], const void *x, void *out, void *pre, int64_t rows,
+                        int32_t in_dim, int32_t out_dim, int32_t act, int32_t batch, int32_t text_len,
+                        const int32_t *cu_seqlens, void *workspace, size_t ws_bytes, void *stream);
+/* 0 where none is needed, or if invalid */
+size_t hilo_linear_workspace_bytes(int32_t dtype, int64_t rows, int32_t in_dim, int32_t out_dim, int32_t batch, int32_t gated);
+
+/* Gradients of the weights by stream, shaped as they are, dtype; any NULL.  The same pointer for both streams:
+ * the sum over both (weights that both share).  Zero where a stream has no rows.                  */
+typedef struct {
+  void *w, *b, *w_gate, *b_gate;
+} hilo_linear_grads;
+
+/* The backward pass of hilo_linear from dout [rows][out_dim], x, and with a gate what it left in pre:
+ *   du = dout act(g), dg = dout u act'(g)   (no gate: du = dout; pre is not looked at)
+ *   dx = du w + dg w_gate;  dw = du^T x, dw_gate = dg^T x, db, db_gate: sums over the stream's rows of du, dg
+ * du and dg are rounded to dtype before the products, as the matrix cores take them; biases are not looked
+ * at.  dx [rows][in_dim] dtype, or NULL: not formed; grads NULL: none.  grads' w_gate and b_gate
+ * need a gate (HILO_E_PARAM).                                                                     */
+hilo_status hilo_linear_backward(int32_t dtype, const hilo_linear_w w[2], const void *x, const void *pre, const void *dout,
+                                 void *dx, const hilo_linear_grads grads[2], int64_t rows, int32_t in_dim, int32_t out_dim,
+                                 int32_t act, int32_t batch, int32_t text_len, const int32_t *cu_seqlens,
+                                 void *workspace, size_t ws_bytes, void *stream);
+size_t hilo_linear_backward_workspace_bytes(int32_t dtype, int64_t rows, int32_t in_dim, int32_t out_dim, int32_t batch,
+                                            int32_t gated); /* 0 if invalid */
+
+/* E4M3 codes (the format of hilo_quantize_rows) with a power-of-two scale 2^k for each block of 128 columns of a row,
+ * or of 128 rows by 128 columns (block_rows 1 or 128; the last block of a row or column may be smaller):
+ *   k: the least with 448 2^k >= amax, at least -127, 0 for a block of zeros;  code = x 2^-k rounded to nearest even
+ * A block that holds an infinity or a NaN gets codes and scale of NaN.  codes [rows][cols]; scales: E8M0 bytes
+ * 127 + k (255: NaN), [rows / block_rows, rounded up][4 * (cols / 512, rounded up)], bytes behind the last block 0.
+ * Rounding by itself is the loss: scales are exact, and the matrix cores apply them.
+ * cols: a multiple of 16, 16 .. 65536.  x aligned to 16 bytes, codes to 8.  limit: device pointer to the number of
+ * rows in use, or NULL for `rows`.                                                                */
+hilo_status hilo_quantize_blocks(int32_t dtype, const void *x, int64_t rows, int64_t cols, int32_t block_rows,
+                                 const int32_t *limit, uint8_t *codes, uint8_t *scales, void *stream);
+
+/* hilo_linear on such codes: w in blocks of 128 x 128, x in blocks of 128 of a row.
+ *   u[m][n] = sum over blocks c of 2^(kx[m][c] + kw[n / 128][c]) sum_k x[m][k] w[n][k]  + b[n]
+ * Products are exact and added up in float32 by the matrix cores.  x: codes with x_scale, or with x_scale NULL
+ * dtype, quantised as hilo_quantize_blocks does within the call.  out: dtype, or with out_scale (a gate only,
+ * HILO_E_PARAM) codes and scales of its float32 values in blocks of 128 of a row, for the next product.
+ * Biases are dtype.  in_dim and out_dim: multiples of 16, 16 .. 65536.                            */
+typedef struct {
+  const uint8_t *w;      /* [out_dim][in_dim] codes                                        */
+  const uint8_t *s;      /* [out_dim / 128, rounded up][4 * (in_dim / 512, rounded up)]    */
+  const void *b;         /* [out_dim] dtype or NULL                                        */
+  const uint8_t *w_gate; /* the gate's, or NULL: no gate                                   */
+  const uint8_t *s_gate;
+  const void *b_gate;
+} hilo_linear_w_fp8;
+hilo_status hilo_linear_fp8(int32_t dtype, const hilo_linear_w_fp8 w[2], const void *x, const uint8_t *x_scale, void *out,
+                            uint8_t *out_scale, int64_t rows, int32_t in_dim, int32_t out_dim, int32_t act,
+                            int32_t batch, int32_t text_len, const int32_t *cu_seqlens, void *workspace,
+                            size_t ws_bytes, void *stream);
+size_t hilo_linear_fp8_workspace_bytes(int64_t rows, int32_t in_dim, int32_t out_dim, int32_t gated); /* 0 if invalid */
 
 size_t hilo_workspace_bytes(const hilo_shape *shape); /* 0 if the shape is invalid */
 /* T_max = batch * (images * (N + N/4) + text_len): the most rows any token set can produce

@@ -16,13 +16,15 @@ namespace {
 enum Kind {
   K_SCORE, K_SELECT, K_LAYOUT, K_COMPRESS, K_NORM_ATTN, K_GEMM_QKV, K_ATTN_CORE, K_GEMM_O,
   K_NORM_MLP, K_GEMM_FC1, K_GEMM_FC2, K_DECOMPRESS, K_QUANT_ATTN, K_QUANT_MLP,
-  K_ROPE, K_POSITIONS, K_NORM_RESIDUAL, K_NORM_RESIDUAL_BACK, K_QUANT_I8, K_LINEAR_I8, K_COUNT
+  K_ROPE, K_POSITIONS, K_NORM_RESIDUAL, K_NORM_RESIDUAL_BACK, K_QUANT_I8, K_LINEAR_I8,
+  K_LINEAR, K_LINEAR_GATE_BACK, K_LINEAR_DX, K_LINEAR_DW, K_QUANT_BLOCKS, K_LINEAR_FP8, K_COUNT
 };
 const char *kKindNames[K_COUNT] = {"score", "select", "layout", "compress", "rownorm_attn",
                                    "gemm_qkv", "attention_core", "gemm_o", "rownorm_mlp",
                                    "gemm_fc1", "gemm_fc2", "decompress", "quantize_attn",
                                    "quantize_mlp", "rope", "token_positions", "norm_residual",
-                                   "norm_residual_backward", "quantize_i8", "linear_i8"};
+                                   "norm_residual_backward", "quantize_i8", "linear_i8", "linear",
+                                   "linear_gate_backward", "linear_dx", "linear_dw", "quantize_blocks", "linear_fp8"};
 
 struct ProfRec {
   int kind;
@@ -998,6 +1000,302 @@ hilo_status hilo_linear_i8(int32_t dtype, const hilo_linear_w_i8 w[2], const voi
   }
   p.part = reinterpret_cast<float *>(ws + align256(size_t(rows) * in_dim) + align256(size_t(rows) * sizeof(float)));
   return dev_status(timed(K_LINEAR_I8, st, [&] { return launch_linear_i8(dtype == HILO_BF16, act == HILO_ACT_GELU, p, st); }));
+}
+
+// ------------------------------------------------------------------- products of a feed-forward
+
+}  // extern "C"
+
+namespace {
+
+// out_dim and in_dim in steps of `step` values
+hilo_status check_product(int64_t rows, int32_t in_dim, int32_t out_dim, int32_t batch, int32_t text_len, int step) {
+  const hilo_status e = check_rows(rows, batch, text_len);
+  if (e != HILO_OK) return e;
+  if (in_dim < step || in_dim > 65536 || in_dim % step != 0 || out_dim < step || out_dim > 65536 || out_dim % step != 0)
+    return HILO_E_SHAPE;
+  return batch > 4096 ? HILO_E_SHAPE : HILO_OK;  // segments are looked through for each tile
+}
+
+// Whether the streams' weights have a gate, and that act fits it.
+hilo_status check_gate(const void *const gate[2], int streams, int32_t act, bool *gated) {
+  *gated = gate[0] != nullptr;
+  if (streams == 2 && (gate[1] != nullptr) != *gated) return HILO_E_NULL;
+  if (*gated ? act != HILO_ACT_GELU && act != HILO_ACT_SILU : act != HILO_ACT_NONE) return HILO_E_PARAM;
+  return HILO_OK;
+}
+
+// Backward workspace: dpre (with a gate), the rows' sums, partial products.
+struct BackwardLayout {
+  size_t sums, part, total;
+};
+BackwardLayout backward_layout(bool bf16, int64_t rows, int K, int N, int batch, bool gated) {
+  const int parts = gated ? 2 : 1;
+  BackwardLayout l;
+  l.sums = gated ? align256(size_t(rows) * 2 * N * (bf16 ? 2 : 4)) : 0;
+  l.part = l.sums + align256(gate_back_bytes(rows, N, parts, batch));
+  const size_t dx = product_part_bytes(bf16, PRODUCT_DX, rows, K, N, parts);
+  const size_t dw = product_part_bytes(bf16, PRODUCT_DW, rows, K, N, parts);
+  l.total = l.part + align256(dx > dw ? dx : dw);
+  return l;
+}
+
+// FP8 workspace: codes and scales of float rows, float32 rows that leave as codes, partial products.
+struct Fp8Layout {
+  size_t scale, out, part, total;
+};
+Fp8Layout fp8_layout(int64_t rows, int K, int N, bool gated) {
+  Fp8Layout l;
+  l.scale = align256(size_t(rows) * K);
+  l.out = l.scale + align256(size_t(rows) * scale_stride(K));
+  l.part = l.out + (gated ? align256(size_t(rows) * N * sizeof(float)) : 0);
+  l.total = l.part + align256(product_fp8_part_bytes(rows, K, N, gated ? 2 : 1)) + 256;
+  return l;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t hilo_linear_workspace_bytes(int32_t dtype, int64_t rows, int32_t in_dim, int32_t out_dim, int32_t batch, int32_t gated) {
+  if (check_dtype(dtype) != HILO_OK || check_product(rows, in_dim, out_dim, batch, 0, 8) != HILO_OK) return 0;
+  return align256(product_part_bytes(dtype == HILO_BF16, PRODUCT_OUT, rows, in_dim, out_dim, gated ? 2 : 1));
+}
+
+hilo_status hilo_linear(int32_t dtype, const hilo_linear_w w[2], const void *x, void *out, void *pre, int64_t rows,
+                        int32_t in_dim, int32_t out_dim, int32_t act, int32_t batch, int32_t text_len,
+                        const int32_t *cu_seqlens, void *workspace, size_t ws_bytes, void *stream) {
+  hilo_status e = check_dtype(dtype);
+  if (e != HILO_OK || (e = check_product(rows, in_dim, out_dim, batch, text_len, 8)) != HILO_OK) return e;
+  if (!w || !cu_seqlens || (rows > 0 && (!x || !out))) return HILO_E_NULL;
+  const int streams = text_len > 0 ? 2 : 1;
+  const void *const gate[2] = {w[0].w_gate, streams == 2 ? w[1].w_gate : nullptr};
+  bool gated;
+  if ((e = check_gate(gate, streams, act, &gated)) != HILO_OK) return e;
+  if (pre && !gated) return HILO_E_PARAM;
+  for (int k = 0; k < streams; ++k) {
+    if (!w[k].w) return HILO_E_NULL;
+    if (!aligned(w[k].w, 16) || !aligned(w[k].b, 16) || !aligned(w[k].w_gate, 16) || !aligned(w[k].b_gate, 16)) return HILO_E_PARAM;
+  }
+  if (!aligned(x, 16) || !aligned(out, 16) || !aligned(pre, 16) || !aligned(workspace, 256)) return HILO_E_PARAM;
+  const size_t need = hilo_linear_workspace_bytes(dtype, rows, in_dim, out_dim, batch, gated);
+  if (need > 0 && !workspace) return HILO_E_NULL;
+  if (ws_bytes < need) return HILO_E_WORKSPACE;
+  if (rows == 0) return HILO_OK;
+  if (!have_device()) return HILO_E_DEVICE;
+  ProductProblem p{};
+  p.cu = cu_seqlens;
+  p.B = batch; p.L = text_len; p.rows = int(rows);
+  p.K = in_dim; p.N = out_dim;
+  p.parts = gated ? 2 : 1;
+  p.silu = act == HILO_ACT_SILU;
+  p.bf16 = dtype == HILO_BF16;
+  p.out_bf16 = p.bf16;
+  p.x = x; p.out = out; p.pre = pre;
+  p.merged = streams == 1 || (w[0].w == w[1].w && w[0].b == w[1].b && (!gated || (w[0].w_gate == w[1].w_gate && w[0].b_gate == w[1].b_gate)));
+  for (int k = 0; k < 2; ++k) {
+    const hilo_linear_w &v = w[k < streams ? k : 0];
+    p.w[k][0] = gated ? v.w_gate : v.w;
+    p.w[k][1] = v.w;
+    p.bias[k][0] = gated ? v.b_gate : v.b;
+    p.bias[k][1] = v.b;
+  }
+  p.part = reinterpret_cast<float *>(workspace);
+  hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  return dev_status(timed(K_LINEAR, st, [&] { return launch_product(PRODUCT_OUT, p, st); }));
+}
+
+size_t hilo_linear_backward_workspace_bytes(int32_t dtype, int64_t rows, int32_t in_dim, int32_t out_dim, int32_t batch,
+                                            int32_t gated) {
+  if (check_dtype(dtype) != HILO_OK || check_product(rows, in_dim, out_dim, batch, 0, 8) != HILO_OK) return 0;
+  return backward_layout(dtype == HILO_BF16, rows, in_dim, out_dim, batch, gated != 0).total;
+}
+
+hilo_status hilo_linear_backward(int32_t dtype, const hilo_linear_w w[2], const void *x, const void *pre, const void *dout,
+                                 void *dx, const hilo_linear_grads grads[2], int64_t rows, int32_t in_dim, int32_t out_dim,
+                                 int32_t act, int32_t batch, int32_t text_len, const int32_t *cu_seqlens,
+                                 void *workspace, size_t ws_bytes, void *stream) {
+  hilo_status e = check_dtype(dtype);
+  if (e != HILO_OK || (e = check_product(rows, in_dim, out_dim, batch, text_len, 8)) != HILO_OK) return e;
+  if (!w || !cu_seqlens || !workspace || (rows > 0 && !dout)) return HILO_E_NULL;
+  const int streams = text_len > 0 ? 2 : 1;
+  const void *const gate[2] = {w[0].w_gate, streams == 2 ? w[1].w_gate : nullptr};
+  bool gated;
+  if ((e = check_gate(gate, streams, act, &gated)) != HILO_OK) return e;
+  if (rows > 0 && gated && !pre) return HILO_E_NULL;
+  for (int k = 0; k < streams; ++k) {
+    if (!w[k].w) return HILO_E_NULL;
+    if (!aligned(w[k].w, 16) || !aligned(w[k].w_gate, 16)) return HILO_E_PARAM;
+  }
+  if (!aligned(x, 16) || !aligned(pre, 16) || !aligned(dout, 16) || !aligned(dx, 16) || !aligned(workspace, 256)) return HILO_E_PARAM;
+  const int parts = gated ? 2 : 1;
+  void *dw[2][2] = {}, *db[2][2] = {};  // [stream][part]
+  bool any_dw = false, any_db = false;
+  if (grads) {
+    for (int k = 0; k < 2; ++k) {
+      const hilo_linear_grads &g = grads[k];
+      if (!gated && (g.w_gate || g.b_gate)) return HILO_E_PARAM;
+      if (!aligned(g.w, 16) || !aligned(g.b, 16) || !aligned(g.w_gate, 16) || !aligned(g.b_gate, 16)) return HILO_E_PARAM;
+      dw[k][parts - 1] = g.w;
+      db[k][parts - 1] = g.b;
+      if (gated) {
+        dw[k][0] = g.w_gate;
+        db[k][0] = g.b_gate;
+      }
+      any_dw = any_dw || g.w || g.w_gate;
+      any_db = any_db || g.b || g.b_gate;
+    }
+  }
+  if (rows > 0 && any_dw && !x) return HILO_E_NULL;
+  if (ws_bytes < hilo_linear_backward_workspace_bytes(dtype, rows, in_dim, out_dim, batch, gated)) return HILO_E_WORKSPACE;
+  if (rows == 0 && !any_dw && !any_db) return HILO_OK;
+  if (!have_device()) return HILO_E_DEVICE;
+  const bool bf16 = dtype == HILO_BF16;
+  const BackwardLayout l = backward_layout(bf16, rows, in_dim, out_dim, batch, gated);
+  char *ws = reinterpret_cast<char *>(workspace);
+  hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+
+  GateBackProblem b{};
+  b.cu = cu_seqlens;
+  b.B = batch; b.L = text_len; b.rows = int(rows);
+  b.merged = text_len == 0;
+  b.N = out_dim; b.parts = parts;
+  b.silu = act == HILO_ACT_SILU;
+  b.pre = pre; b.dout = dout;
+  b.dpre = gated ? ws : nullptr;
+  for (int k = 0; k < 2; ++k)
+    for (int q = 0; q < 2; ++q) b.db[k][q] = db[k][q];
+  b.part = any_db ? reinterpret_cast<float *>(ws + l.sums) : nullptr;
+  hipError_t he = timed(K_LINEAR_GATE_BACK, st, [&] { return launch_gate_back(bf16, b, st); });
+  if (he != hipSuccess) return HILO_E_DEVICE;
+
+  ProductProblem p{};
+  p.cu = cu_seqlens;
+  p.B = batch; p.L = text_len; p.rows = int(rows);
+  p.K = in_dim; p.N = out_dim;
+  p.parts = parts;
+  p.bf16 = bf16;
+  p.x = x;
+  p.d = gated ? ws : dout;
+  p.dx = dx;
+  for (int k = 0; k < 2; ++k) {
+    const hilo_linear_w &v = w[k < streams ? k : 0];
+    p.w[k][0] = gated ? v.w_gate : v.w;
+    p.w[k][1] = v.w;
+  }
+  p.part = reinterpret_cast<float *>(ws + l.part);
+  if (dx && rows > 0) {
+    p.merged = streams == 1 || (p.w[0][0] == p.w[1][0] && p.w[0][1] == p.w[1][1]);
+    he = timed(K_LINEAR_DX, st, [&] { return launch_product(PRODUCT_DX, p, st); });
+    if (he != hipSuccess) return HILO_E_DEVICE;
+  }
+  // gradients that both streams share run over all rows; those of one stream over its own
+  for (int both = 0; both < 2; ++both) {
+    p.merged = both || text_len == 0;
+    p.outs = 0;
+    for (int k = 0; k < 2; ++k)
+      for (int q = 0; q < parts; ++q) {
+        const bool same = dw[0][q] == dw[1][q];
+        if (!dw[k][q] || same != (both != 0) || (both && k)) continue;
+        p.out_stream[p.outs] = k;
+        p.out_part[p.outs] = q;
+        p.dw[p.outs++] = dw[k][q];
+      }
+    if (p.outs == 0) continue;
+    he = timed(K_LINEAR_DW, st, [&] { return launch_product(PRODUCT_DW, p, st); });
+    if (he != hipSuccess) return HILO_E_DEVICE;
+  }
+  return HILO_OK;
+}
+
+hilo_status hilo_quantize_blocks(int32_t dtype, const void *x, int64_t rows, int64_t cols, int32_t block_rows,
+                                 const int32_t *limit, uint8_t *codes, uint8_t *scales, void *stream) {
+  const hilo_status e = check_dtype(dtype);
+  if (e != HILO_OK) return e;
+  if (rows < 0 || rows >= kMaxRows || cols < 16 || cols > 65536 || cols % 16 != 0) return HILO_E_SHAPE;
+  if (block_rows != 1 && block_rows != 128) return HILO_E_PARAM;
+  if (rows > 0 && (!x || !codes || !scales)) return HILO_E_NULL;
+  if (!aligned(x, 16) || !aligned(codes, 8)) return HILO_E_PARAM;
+  if (rows == 0) return HILO_OK;
+  if (!have_device()) return HILO_E_DEVICE;
+  hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  return dev_status(timed(K_QUANT_BLOCKS, st, [&] {
+    return launch_quantize_blocks(dtype == HILO_BF16, x, int(rows), int(cols), block_rows, limit, codes, scales, st);
+  }));
+}
+
+size_t hilo_linear_fp8_workspace_bytes(int64_t rows, int32_t in_dim, int32_t out_dim, int32_t gated) {
+  if (check_product(rows, in_dim, out_dim, 1, 0, 16) != HILO_OK) return 0;
+  return fp8_layout(rows, in_dim, out_dim, gated != 0).total;
+}
+
+hilo_status hilo_linear_fp8(int32_t dtype, const hilo_linear_w_fp8 w[2], const void *x, const uint8_t *x_scale, void *out,
+                            uint8_t *out_scale, int64_t rows, int32_t in_dim, int32_t out_dim, int32_t act,
+                            int32_t batch, int32_t text_len, const int32_t *cu_seqlens, void *workspace,
+                            size_t ws_bytes, void *stream) {
+  hilo_status e = check_dtype(dtype);
+  if (e != HILO_OK || (e = check_product(rows, in_dim, out_dim, batch, text_len, 16)) != HILO_OK) return e;
+  if (!w || !cu_seqlens || !workspace || (rows > 0 && (!x || !out))) return HILO_E_NULL;
+  const int streams = text_len > 0 ? 2 : 1;
+  const void *const gate[2] = {w[0].w_gate, streams == 2 ? w[1].w_gate : nullptr};
+  bool gated;
+  if ((e = check_gate(gate, streams, act, &gated)) != HILO_OK) return e;
+  if (out_scale && !gated) return HILO_E_PARAM;
+  for (int k = 0; k < streams; ++k) {
+    if (!w[k].w || !w[k].s || (gated && !w[k].s_gate)) return HILO_E_NULL;
+    if (!aligned(w[k].w, 16) || !aligned(w[k].s, 16) || !aligned(w[k].b, 16) || !aligned(w[k].w_gate, 16) ||
+        !aligned(w[k].s_gate, 16) || !aligned(w[k].b_gate, 16))
+      return HILO_E_PARAM;
+  }
+  if (!aligned(x, 16) || !aligned(x_scale, 16) || !aligned(out, 16) || !aligned(out_scale, 16) || !aligned(workspace, 256))
+    return HILO_E_PARAM;
+  if (ws_bytes < hilo_linear_fp8_workspace_bytes(rows, in_dim, out_dim, gated)) return HILO_E_WORKSPACE;
+  if (rows == 0) return HILO_OK;
+  if (!have_device()) return HILO_E_DEVICE;
+  const Fp8Layout l = fp8_layout(rows, in_dim, out_dim, gated);
+  char *ws = reinterpret_cast<char *>(workspace);
+  hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  ProductProblem p{};
+  p.cu = cu_seqlens;
+  p.B = batch; p.L = text_len; p.rows = int(rows);
+  p.K = in_dim; p.N = out_dim;
+  p.parts = gated ? 2 : 1;
+  p.silu = act == HILO_ACT_SILU;
+  p.bf16 = dtype == HILO_BF16;
+  p.out_bf16 = !out_scale && p.bf16;
+  p.x = x; p.x_scale = x_scale;
+  p.out = out_scale ? ws + l.out : out;
+  p.merged = streams == 1;
+  for (int k = 0; k < 2; ++k) {
+    const hilo_linear_w_fp8 &v = w[k < streams ? k : 0];
+    p.w[k][0] = gated ? v.w_gate : v.w;
+    p.w[k][1] = v.w;
+    p.w_scale[k][0] = gated ? v.s_gate : v.s;
+    p.w_scale[k][1] = v.s;
+    p.bias[k][0] = gated ? v.b_gate : v.b;
+    p.bias[k][1] = v.b;
+  }
+  if (streams == 2) {
+    p.merged = 1;
+    for (int q = 0; q < 2; ++q)
+      p.merged = p.merged && p.w[0][q] == p.w[1][q] && p.w_scale[0][q] == p.w_scale[1][q] && p.bias[0][q] == p.bias[1][q];
+  }
+  if (!x_scale) {
+    const hipError_t he = timed(K_QUANT_BLOCKS, st, [&] {
+      return launch_quantize_blocks(p.bf16, x, int(rows), in_dim, 1, cu_seqlens + batch, reinterpret_cast<uint8_t *>(ws),
+                                    reinterpret_cast<uint8_t *>(ws + l.scale), st);
+    });
+    if (he != hipSuccess) return HILO_E_DEVICE;
+    p.x = ws;
+    p.x_scale = reinterpret_cast<const uint8_t *>(ws + l.scale);
+  }
+  p.part = reinterpret_cast<float *>(ws + l.part);
+  hipError_t he = timed(K_LINEAR_FP8, st, [&] { return launch_product_fp8(p, st); });
+  if (he == hipSuccess && out_scale)
+    he = timed(K_QUANT_BLOCKS, st, [&] {
+      return launch_quantize_blocks(false, p.out, int(rows), out_dim, 1, cu_seqlens + batch, reinterpret_cast<uint8_t *>(out), out_scale, st);
+    });
+  return dev_status(he);
 }
 
 hilo_status hilo_profile_enable(int32_t on) {

@@ -201,4 +201,59 @@ bool linear_i8_cuts(int K);
 // Bytes of partial tiles that launch_linear_i8 needs for buffers of `rows` rows.
 size_t linear_i8_part_bytes(long long rows, int K);
 
+// Products of a feed-forward, their gradients, and the same on E4M3 codes with a scale for each block of 128 (product.h).
+// Rows are packed as everywhere; part 0 is the product, or with a gate part 0 the gate's and part 1 the other one's.
+struct ProductProblem {
+  const int *cu;
+  int B, L, rows;
+  int merged;            // all rows are one segment of stream 0 (no text, or the same weights for both streams)
+  int K, N, parts;       // in_dim, out_dim, 1 or 2
+  int silu;              // the gate's activation: SiLU, or GELU
+  int bf16;              // type of x, pre, biases, gradients
+  int out_bf16;          // of out
+  const void *x;         // [rows][K]
+  const void *w[2][2];   // [stream][part]: [N][K]
+  const void *bias[2][2];  // [stream][part]: [N] or null
+  void *out;             // [rows][N]
+  void *pre;             // [rows][2][N] or null: the gate's values before the activation, then the other's
+  const void *d;         // [rows][parts][N]: gradients of the products' values
+  void *dx;              // [rows][K]
+  int outs;              // weight gradients to form, in the order of:
+  int out_stream[4], out_part[4];
+  void *dw[4];           // [N][K]
+  float *part;           // partial sums, `splits` times what the product leaves
+  int splits;
+  // FP8: x holds codes, w codes
+  const uint8_t *x_scale;        // [rows][scale_stride(K)] E8M0 bytes
+  const uint8_t *w_scale[2][2];  // [ceil(N / 128)][scale_stride(K)]
+  uint8_t *out_scale;            // [rows][scale_stride(N)]: out is codes; or null
+};
+// Bytes between rows of E8M0 scales: one for each 128 columns, in whole groups of four.
+constexpr int scale_stride(int cols) { return (cols + 511) / 512 * 4; }
+
+enum ProductKind { PRODUCT_OUT, PRODUCT_DX, PRODUCT_DW };
+size_t product_part_bytes(bool bf16, int kind, long long rows, int K, int N, int parts);
+size_t product_fp8_part_bytes(long long rows, int K, int N, int parts);
+hipError_t launch_product(int kind, ProductProblem p, hipStream_t st);
+hipError_t launch_product_fp8(ProductProblem p, hipStream_t st);
+
+// The step between: dpre [rows][2][N] from dout and pre (gated), and the sums over rows of dpre, or of dout, by stream
+// into db[stream][part] (any null; the two streams' the same: sums over both).
+struct GateBackProblem {
+  const int *cu;
+  int B, L, rows, merged;
+  int N, parts, silu;
+  const void *pre, *dout;
+  void *dpre;            // with a gate
+  void *db[2][2];        // [stream][part]: [N]
+  float *part;           // gate_back_bytes
+};
+size_t gate_back_bytes(long long rows, int N, int parts, int B);
+hipError_t launch_gate_back(bool bf16, const GateBackProblem &p, hipStream_t st);
+
+// E4M3 codes and E8M0 scales (scale_stride(cols) a row) of x [rows][cols], a scale for each 128 columns of a row, or
+// for block_rows 128 of 128 rows; limit: a device pointer to the number of rows, or null.
+hipError_t launch_quantize_blocks(bool bf16, const void *x, int rows, int cols, int block_rows, const int *limit, uint8_t *codes,
+                                  uint8_t *scale, hipStream_t st);
+
 }  // namespace hilo

@@ -1,0 +1,547 @@
+// Products of a feed-forward with their gradients (hilo_linear, hilo_linear_backward, hilo_linear_fp8):
+//   PRODUCT_OUT  u = x w^T + b, or with a gate act(x wg^T + bg) u
+//   PRODUCT_DX   dx = sum over parts of d_part w_part
+//   PRODUCT_DW   dw_part = d_part^T x over the rows of a stream
+// in float32 on the matrix cores, whatever the operands' type.
+#include <algorithm>
+
+#include "product.h"
+
+namespace hilo {
+
+enum ProductType { TYPE_F32, TYPE_BF16, TYPE_FP8 };
+
+// 8 consecutive values of an operand
+template <int TYPE>
+struct Chunk {
+  uint4 u[TYPE == TYPE_F32 ? 2 : 1];
+  float scale;
+  HILO_DEV void zero() {
+    u[0] = make_uint4(0u, 0u, 0u, 0u);
+    if constexpr (TYPE == TYPE_F32) u[1] = u[0];
+    scale = 0.f;
+  }
+  HILO_DEV void load(const void *x, size_t i) {
+    if constexpr (TYPE == TYPE_FP8) {
+      const uint2 v = *reinterpret_cast<const uint2 *>(reinterpret_cast<const uint8_t *>(x) + i);
+      u[0].x = v.x;
+      u[0].y = v.y;
+    } else {
+      const uint4 *p = reinterpret_cast<const uint4 *>(reinterpret_cast<const char *>(x) + i * (TYPE == TYPE_BF16 ? 2 : 4));
+      u[0] = p[0];
+      if constexpr (TYPE == TYPE_F32) u[1] = p[1];
+    }
+  }
+  HILO_DEV void values(float (&f)[8]) const {
+    if constexpr (TYPE == TYPE_BF16) {
+      unpack8(u[0], f);
+    } else if constexpr (TYPE == TYPE_FP8) {
+      const uint32_t w[2] = {u[0].x, u[0].y};
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const auto a = __builtin_amdgcn_cvt_pk_f32_fp8(w[h], false), b = __builtin_amdgcn_cvt_pk_f32_fp8(w[h], true);
+        f[4 * h] = a[0] * scale; f[4 * h + 1] = a[1] * scale;
+        f[4 * h + 2] = b[0] * scale; f[4 * h + 3] = b[1] * scale;
+      }
+    } else {
+      f[0] = __uint_as_float(u[0].x); f[1] = __uint_as_float(u[0].y); f[2] = __uint_as_float(u[0].z); f[3] = __uint_as_float(u[0].w);
+      f[4] = __uint_as_float(u[1].x); f[5] = __uint_as_float(u[1].y); f[6] = __uint_as_float(u[1].z); f[7] = __uint_as_float(u[1].w);
+    }
+  }
+};
+
+// The value of an E8M0 byte; 255 stands for NaN.
+HILO_DEV float e8m0(uint8_t b) {
+  return b == 255 ? __uint_as_float(0x7fc00000u) : b == 0 ? __uint_as_float(0x00400000u) : __uint_as_float(uint32_t(b) << 23);
+}
+
+// Tiles of 64 x 64 outputs (with a gate, of 32 columns of either part) on 4 waves of 32 x 32, K in steps of 32 through two
+// LDS buffers: while one is multiplied, the next step's values are on their way to registers.  Both operands lie in LDS
+// as [k][row], so that any layout in memory will do; a lane of group lg takes k = 8 lg + s in step s of 8.
+constexpr int kStep = 32, kPad = 66;
+
+template <int TYPE, int KIND, bool GATED>
+__global__ __launch_bounds__(256) void k_product(ProductProblem p) {
+  constexpr bool AK = KIND != PRODUCT_DW, BK = KIND == PRODUCT_OUT;  // operand's last index is k
+  constexpr int BN = GATED && KIND == PRODUCT_OUT ? 32 : 64;         // columns of a tile
+  __shared__ __attribute__((aligned(16))) float lds[2][2][kStep][kPad];
+  const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lr = lane & 15, lg = lane >> 4, wm = wid >> 1, wn = wid & 1;
+  const int cols = KIND == PRODUCT_OUT ? p.N : p.K, tn_count = (cols + BN - 1) / BN;
+  const int tm_count = KIND == PRODUCT_DW ? (p.N + 63) / 64 : count_row_tiles(p, 64);
+  const long long tiles = (long long)tm_count * tn_count * (KIND == PRODUCT_DW ? p.outs : 1);
+  // steps of the whole sum; of a segment's rows in DW
+  const int parts = KIND == PRODUCT_DX ? p.parts : 1, per = (KIND == PRODUCT_OUT ? p.K : p.N) + kStep - 1;
+  for (long long item = blockIdx.x; item < tiles * p.splits; item += gridDim.x) {
+    const long long tile = item / p.splits;
+    const int split = int(item - tile * p.splits);
+    const int tn = int(tile % tn_count), tr = int(tile / tn_count), n0 = tn * BN;
+    int o = 0, stream = 0, part = 0, row0 = 0, rows = 64;
+    if constexpr (KIND == PRODUCT_DW) {
+      o = tr / tm_count;
+      row0 = (tr - o * tm_count) * 64;
+      stream = p.out_stream[o];
+      part = p.out_part[o];
+      rows = min(64, p.N - row0);
+    } else {
+      const RowTile rt = find_row_tile(p, 64, tr);
+      row0 = rt.row0;
+      rows = rt.n;
+      stream = rt.stream;
+    }
+    // ---- where the sum runs: pieces of k, walked from step s0 to s1
+    int total = 0;
+    if constexpr (KIND == PRODUCT_DW) {
+      for (int i = p.merged ? 0 : stream; i < segments(p); i += 2) total += (max(segment(p, i).n, 0) + kStep - 1) / kStep;
+    } else {
+      total = parts * (per / kStep);
+    }
+    const int s0 = int((long long)total * split / p.splits), s1 = int((long long)total * (split + 1) / p.splits);
+    int seg = p.merged ? 0 : stream, seg_lo = 0, seg_n = 0, seg_s = 0;  // DW: the segment of the step, its first step
+    if constexpr (KIND == PRODUCT_DW) {
+      if (s0 < s1) {
+        Segment g = segment(p, seg);
+        while ((g.n + kStep - 1) / kStep <= s0 - seg_s) {
+          seg_s += (max(g.n, 0) + kStep - 1) / kStep;
+          seg += 2;
+          g = segment(p, seg);
+        }
+        seg_lo = g.lo;
+        seg_n = g.n;
+      }
+    }
+    Chunk<TYPE> a, b;
+    auto load = [&](int s) __attribute__((always_inline)) {
+      a.zero();
+      b.zero();
+      int k0, kn;  // first k of the step in its piece, and the piece's length
+      int dpart = part;
+      if constexpr (KIND == PRODUCT_DW) {
+        while (s - seg_s >= (seg_n + kStep - 1) / kStep) {
+          seg_s += (max(seg_n, 0) + kStep - 1) / kStep;
+          seg += 2;
+          const Segment g = segment(p, seg);
+          seg_lo = g.lo;
+          seg_n = g.n;
+        }
+        k0 = (s - seg_s) * kStep;
+        kn = seg_n;
+      } else {
+        const int each = per / kStep;
+        dpart = s / each;
+        k0 = (s - dpart * each) * kStep;
+        kn = per - kStep + 1;
+      }
+      const int r = tid >> 2, c = 8 * (tid & 3);  // k last: row, k
+      const int q = tid >> 3, m = 8 * (tid & 7);  // k first: k, row
+      if constexpr (KIND == PRODUCT_OUT) {
+        if (r < rows && k0 + c < kn) {
+          a.load(p.x, size_t(row0 + r) * p.K + k0 + c);
+          if constexpr (TYPE == TYPE_FP8) a.scale = e8m0(p.x_scale[size_t(row0 + r) * scale_stride(p.K) + (k0 + c) / 128]);
+        }
+        const int wp = GATED ? (r >> 4) & 1 : 0, n = n0 + (GATED ? 16 * (r >> 5) + (r & 15) : r);
+        if (n < p.N && k0 + c < kn) {
+          const void *w = stream ? (wp ? p.w[1][1] : p.w[1][0]) : (wp ? p.w[0][1] : p.w[0][0]);
+          b.load(w, size_t(n) * p.K + k0 + c);
+          if constexpr (TYPE == TYPE_FP8) {
+            const uint8_t *ws = stream ? (wp ? p.w_scale[1][1] : p.w_scale[1][0]) : (wp ? p.w_scale[0][1] : p.w_scale[0][0]);
+            b.scale = e8m0(ws[size_t(n / 128) * scale_stride(p.K) + (k0 + c) / 128]);
+          }
+        }
+      } else if constexpr (KIND == PRODUCT_DX) {
+        if (r < rows && k0 + c < kn) a.load(p.d, (size_t(row0 + r) * p.parts + dpart) * p.N + k0 + c);
+        const void *w = stream ? (dpart ? p.w[1][1] : p.w[1][0]) : (dpart ? p.w[0][1] : p.w[0][0]);
+        if (k0 + q < kn && n0 + m < p.K) b.load(w, size_t(k0 + q) * p.K + n0 + m);
+      } else {
+        if (k0 + q < kn) {
+          const size_t row = size_t(seg_lo) + k0 + q;
+          if (row0 + m < p.N) a.load(p.d, (row * p.parts + dpart) * p.N + row0 + m);
+          if (n0 + m < p.K) b.load(p.x, row * p.K + n0 + m);
+        }
+      }
+    };
+    auto store = [&](int buf) __attribute__((always_inline)) {
+      float f[8];
+      a.values(f);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        if constexpr (AK) lds[buf][0][8 * (tid & 3) + e][tid >> 2] = f[e];
+        else lds[buf][0][tid >> 3][8 * (tid & 7) + e] = f[e];
+      }
+      b.values(f);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        if constexpr (BK) lds[buf][1][8 * (tid & 3) + e][tid >> 2] = f[e];
+        else lds[buf][1][tid >> 3][8 * (tid & 7) + e] = f[e];
+      }
+    };
+    f32x4 acc[2][2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (s0 < s1) {
+      load(s0);
+      store(0);
+      __syncthreads();
+#pragma unroll 1
+      for (int s = s0; s < s1; ++s) {
+        const int buf = (s - s0) & 1;
+        if (s + 1 < s1) load(s + 1);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          float av[2], bv[2];
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            av[i] = lds[buf][0][8 * lg + e][32 * wm + 16 * i + lr];
+            bv[i] = lds[buf][1][8 * lg + e][32 * wn + 16 * i + lr];
+          }
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(bv[j], av[i], acc[i][j], 0, 0, 0);
+        }
+        if (s + 1 < s1) store(buf ^ 1);
+        __syncthreads();
+      }
+    }
+    // ---- lane (lr, lg) holds rows 16 i + lr and columns 16 j + 4 lg .. + 3 of its wave's 32 x 32
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int r = 32 * wm + 16 * i + lr;
+      if (r >= rows) continue;
+      const size_t row = size_t(row0) + r;
+      if constexpr (KIND == PRODUCT_OUT && GATED) {
+        const int n = n0 + 16 * wn + 4 * lg;
+        if (n >= p.N) continue;
+        if (p.splits > 1) {
+          float *q = p.part + (size_t(split) * p.rows + row) * 2 * p.N + n;
+          *reinterpret_cast<f32x4 *>(q) = acc[i][0];
+          *reinterpret_cast<f32x4 *>(q + p.N) = acc[i][1];
+        } else {
+          finish_out<true>(p, stream, row, n, acc[i][0], acc[i][1]);
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const int n = n0 + 32 * wn + 16 * j + 4 * lg;
+          if (n >= cols) continue;
+          if (p.splits > 1) {
+            const size_t all = KIND == PRODUCT_DW ? size_t(p.outs) * p.N : size_t(p.rows);
+            const size_t at = KIND == PRODUCT_DW ? size_t(o) * p.N + row : row;
+            *reinterpret_cast<f32x4 *>(p.part + (split * all + at) * cols + n) = acc[i][j];
+          } else if constexpr (KIND == PRODUCT_OUT) {
+            finish_out<false>(p, stream, row, n, acc[i][j], acc[i][j]);
+          } else if constexpr (KIND == PRODUCT_DX) {
+            store4(p.dx, row * p.K + n, acc[i][j], p.bf16);
+          } else {
+            store4(p.dw[o], row * p.K + n, acc[i][j], p.bf16);
+          }
+        }
+      }
+    }
+  }
+}
+
+// Sums of the splits, in order, and the last step.  A thread has four columns of a row.
+template <int KIND, bool GATED>
+__global__ __launch_bounds__(256) void k_product_join(ProductProblem p) {
+  const int cols = KIND == PRODUCT_OUT ? p.N : p.K, quads = cols / 4;
+  const long long all = KIND == PRODUCT_DW ? (long long)p.outs * p.N : p.rows;
+  const long long rows = KIND == PRODUCT_DW ? all : cu_at(p.cu, p.B);
+  constexpr int W = KIND == PRODUCT_OUT && GATED ? 2 : 1;
+  for (long long t = blockIdx.x * 256ll + threadIdx.x; t < rows * quads; t += gridDim.x * 256ll) {
+    const long long row = t / quads;
+    const int n = int(t - row * quads) * 4;
+    f32x4 v[W];
+#pragma unroll
+    for (int w = 0; w < W; ++w) v[w] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < p.splits; ++s)
+#pragma unroll
+      for (int w = 0; w < W; ++w)
+        v[w] += *reinterpret_cast<const f32x4 *>(p.part + (s * all + row) * (W * cols) + w * cols + n);
+    if constexpr (KIND == PRODUCT_OUT) {
+      int stream = 0;
+      if (!p.merged) {
+        const int s = sample_of_row(p.cu, p.B, int(row));
+        stream = row >= p.cu[s + 1] - p.L;
+      }
+      finish_out<GATED>(p, stream, size_t(row), n, v[0], v[W - 1]);
+    } else if constexpr (KIND == PRODUCT_DX) {
+      store4(p.dx, row * p.K + n, v[0], p.bf16);
+    } else {
+      const int o = int(row / p.N);
+      store4(p.dw[o], (row - (long long)o * p.N) * p.K + n, v[0], p.bf16);
+    }
+  }
+}
+
+// Splits of the sum where tiles are fewer than two for each of the 256 CUs, no shorter than 4 steps each.
+static int splits_of(int kind, long long rows, int K, int N, int parts, int outs, int B, bool merged) {
+  const long long tm = kind == PRODUCT_DW ? (long long)outs * ((N + 63) / 64) : (rows + 63) / 64 + (merged ? 0 : 2 * B - 1);
+  const int bn = kind == PRODUCT_OUT && parts == 2 ? 32 : 64, cols = kind == PRODUCT_OUT ? N : K;
+  const long long tiles = std::max(1ll, tm * ((cols + bn - 1) / bn));
+  const long long steps = kind == PRODUCT_OUT ? K / kStep : kind == PRODUCT_DX ? (long long)parts * N / kStep : rows / kStep;
+  return int(std::min(std::max(1ll, 512 / tiles), std::max(1ll, steps / 4)));
+}
+
+// Most partial sums of any call: one segment has the fewest tiles, so the most splits.
+size_t product_part_bytes(bool bf16, int kind, long long rows, int K, int N, int parts) {
+  size_t most = 0;
+  for (int outs = 1; outs <= (kind == PRODUCT_DW ? 4 : 1); ++outs) {
+    const int s = splits_of(kind, rows, K, N, parts, outs, 1, true);
+    const size_t each = kind == PRODUCT_OUT ? size_t(rows) * parts * N : kind == PRODUCT_DX ? size_t(rows) * K : size_t(outs) * N * K;
+    if (s > 1) most = std::max(most, s * each * sizeof(float));
+  }
+  return most;
+}
+size_t product_fp8_part_bytes(long long rows, int K, int N, int parts) {
+  return product_part_bytes(true, PRODUCT_OUT, rows, K, N, parts);
+}
+
+template <int TYPE, int KIND, bool GATED>
+static hipError_t run(ProductProblem &p, hipStream_t st) {
+  p.splits = splits_of(KIND, p.rows, p.K, p.N, p.parts, p.outs, p.B, p.merged);
+  const long long tm = KIND == PRODUCT_DW ? (long long)p.outs * ((p.N + 63) / 64) : (p.rows + 63) / 64 + (p.merged ? 0 : 2 * p.B - 1);
+  const int cols = KIND == PRODUCT_OUT ? p.N : p.K, bn = KIND == PRODUCT_OUT && GATED ? 32 : 64;
+  const long long items = tm * ((cols + bn - 1) / bn) * p.splits;
+  if (items <= 0) return hipSuccess;
+  hipLaunchKernelGGL((k_product<TYPE, KIND, GATED>), dim3(unsigned(std::min(items, 1ll << 20))), dim3(256), 0, st, p);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || p.splits == 1) return e;
+  const long long quads = (KIND == PRODUCT_DW ? (long long)p.outs * p.N : p.rows) * (cols / 4);
+  hipLaunchKernelGGL((k_product_join<KIND, GATED>), dim3(unsigned(std::min((quads + 255) / 256, 4096ll))), dim3(256), 0, st, p);
+  return hipGetLastError();
+}
+
+template <int TYPE>
+static hipError_t run_kind(int kind, ProductProblem &p, hipStream_t st) {
+  const bool gated = p.parts == 2;
+  if (kind == PRODUCT_OUT) return gated ? run<TYPE, PRODUCT_OUT, true>(p, st) : run<TYPE, PRODUCT_OUT, false>(p, st);
+  if (kind == PRODUCT_DX) return run<TYPE, PRODUCT_DX, false>(p, st);
+  return p.outs > 0 ? run<TYPE, PRODUCT_DW, false>(p, st) : hipSuccess;
+}
+
+hipError_t launch_product(int kind, ProductProblem p, hipStream_t st) {
+  return p.bf16 ? run_kind<TYPE_BF16>(kind, p, st) : run_kind<TYPE_F32>(kind, p, st);
+}
+
+hipError_t launch_product_fp8(ProductProblem p, hipStream_t st) {
+  return p.parts == 2 ? run<TYPE_FP8, PRODUCT_OUT, true>(p, st) : run<TYPE_FP8, PRODUCT_OUT, false>(p, st);
+}
+
+// ------------------------------------------------------------------------ through the gate, and sums over rows
+//
+// A workgroup has 64 rows of a segment and 512 columns: a wave every fourth row, a lane 8 columns.  What a column's rows
+// sum to goes to part[row tile][parts * N], and k_gate_back_sum adds those of a stream's tiles in their order.
+constexpr int kBackRows = 64, kBackCols = 512;
+
+template <bool BF16, bool GATED>
+__global__ __launch_bounds__(256) void k_gate_back(GateBackProblem p) {
+  constexpr int PARTS = GATED ? 2 : 1;
+  __shared__ float sums[3][PARTS][8][64];
+  const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int tn_count = (p.N + kBackCols - 1) / kBackCols;
+  const long long tiles = (long long)count_row_tiles(p, kBackRows) * tn_count;
+  for (long long t = blockIdx.x; t < tiles; t += gridDim.x) {
+    const int tr = int(t / tn_count), n = int(t - (long long)tr * tn_count) * kBackCols + 8 * lane;
+    const RowTile rt = find_row_tile(p, kBackRows, tr);
+    float db[PARTS][8];
+#pragma unroll
+    for (int q = 0; q < PARTS; ++q)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) db[q][e] = 0.f;
+    if (n < p.N) {
+      for (int r = wid; r < rt.n; r += 4) {
+        const size_t row = size_t(rt.row0) + r;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const f32x4 d = load4(p.dout, row * p.N + n + 4 * h, BF16);
+          if constexpr (GATED) {
+            const f32x4 g = load4(p.pre, row * 2 * p.N + n + 4 * h, BF16), u = load4(p.pre, row * 2 * p.N + p.N + n + 4 * h, BF16);
+            f32x4 dg, du;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              float act, slope;
+              gate_slope<!BF16>(g[e], p.silu, act, slope);
+              dg[e] = d[e] * u[e] * slope;
+              du[e] = d[e] * act;
+              db[0][4 * h + e] += dg[e];
+              db[1][4 * h + e] += du[e];
+            }
+            store4(p.dpre, row * 2 * p.N + n + 4 * h, dg, BF16);
+            store4(p.dpre, row * 2 * p.N + p.N + n + 4 * h, du, BF16);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) db[0][4 * h + e] += d[e];
+          }
+        }
+      }
+    }
+    if (p.part) {
+      if (wid > 0) {
+#pragma unroll
+        for (int q = 0; q < PARTS; ++q)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) sums[wid - 1][q][e][lane] = db[q][e];
+      }
+      __syncthreads();
+      if (wid == 0 && n < p.N) {
+#pragma unroll
+        for (int q = 0; q < PARTS; ++q)
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            p.part[(size_t(tr) * PARTS + q) * p.N + n + e] = ((db[q][e] + sums[0][q][e][lane]) + sums[1][q][e][lane]) + sums[2][q][e][lane];
+      }
+      __syncthreads();
+    }
+  }
+}
+
+// A workgroup has 64 columns of one sum, a wave a quarter of the row tiles.
+template <bool BF16>
+__global__ __launch_bounds__(256) void k_gate_back_sum(GateBackProblem p) {
+  __shared__ float sums[4][64];
+  const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int stream = blockIdx.y / p.parts, part = blockIdx.y % p.parts;
+  void *db = stream ? p.db[1][part] : p.db[0][part];
+  const bool both = p.db[0][part] == p.db[1][part];
+  if (!db || (both && stream)) return;
+  const int n = blockIdx.x * 64 + lane;
+  float v = 0.f;
+  int t0 = 0;  // tiles before the segment
+  for (int i = 0; i < segments(p); ++i) {
+    const Segment s = segment(p, i);
+    const int tiles = (s.n + kBackRows - 1) / kBackRows;
+    if (both || s.stream == stream) {
+      for (int t = wid; t < tiles; t += 4)
+        if (n < p.N) v += p.part[(size_t(t0 + t) * p.parts + part) * p.N + n];
+    }
+    t0 += tiles;
+  }
+  sums[wid][lane] = v;
+  __syncthreads();
+  if (wid == 0 && n < p.N) {
+    const float s = (sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]);
+    if (BF16) reinterpret_cast<uint16_t *>(db)[n] = f2bf(s);
+    else reinterpret_cast<float *>(db)[n] = s;
+  }
+}
+
+size_t gate_back_bytes(long long rows, int N, int parts, int B) {
+  return (size_t(rows + kBackRows - 1) / kBackRows + 2 * size_t(B)) * parts * N * sizeof(float);
+}
+
+template <bool BF16, bool GATED>
+static hipError_t run_gate_back(const GateBackProblem &p, hipStream_t st) {
+  if (p.rows > 0 && (GATED || p.part)) {
+    const long long tiles = ((p.rows + kBackRows - 1) / kBackRows + (p.merged ? 0 : 2LL * p.B)) * ((p.N + kBackCols - 1) / kBackCols);
+    hipLaunchKernelGGL((k_gate_back<BF16, GATED>), dim3(unsigned(std::min(tiles, 1ll << 20))), dim3(256), 0, st, p);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  if (!p.part) return hipSuccess;
+  hipLaunchKernelGGL((k_gate_back_sum<BF16>), dim3((p.N + 63) / 64, 2 * p.parts), dim3(256), 0, st, p);
+  return hipGetLastError();
+}
+
+hipError_t launch_gate_back(bool bf16, const GateBackProblem &p, hipStream_t st) {
+  if (p.parts == 2) return bf16 ? run_gate_back<true, true>(p, st) : run_gate_back<false, true>(p, st);
+  return bf16 ? run_gate_back<true, false>(p, st) : run_gate_back<false, false>(p, st);
+}
+
+// ----------------------------------------------------------------------------------- quantisation of blocks
+
+// The codes of 8 values times 2^-k, and the bits that say whether they are finite: the largest |x|'s, as they order.
+HILO_DEV uint2 block_codes(const float (&f)[8], uint32_t top) {
+  if (top >= 0x7f800000u) return make_uint2(0x7f7f7f7fu, 0x7f7f7f7fu);
+  const float inv = pow2_inverse(pow2_exponent(__uint_as_float(top)));
+  return make_uint2(fp8x4(f[0] * inv, f[1] * inv, f[2] * inv, f[3] * inv), fp8x4(f[4] * inv, f[5] * inv, f[6] * inv, f[7] * inv));
+}
+HILO_DEV uint8_t block_scale(uint32_t top) {
+  return top >= 0x7f800000u ? 255 : uint8_t(127 + pow2_exponent(__uint_as_float(top)));
+}
+
+// Rows: 16 lanes have the 128 columns of a scale, 8 a lane; a wave 512 columns of a row at a time.
+template <bool BF16>
+__global__ __launch_bounds__(256) void k_quantize_blocks(const void *__restrict__ x, int rows, int cols, const int *__restrict__ limit,
+                                                         uint8_t *__restrict__ codes, uint8_t *__restrict__ scale) {
+  const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int end = limit ? min(rows, cu_at(limit, 0)) : rows, groups = scale_stride(cols) / 4;
+  const long long units = (long long)end * groups;
+  for (long long t = blockIdx.x * 4ll + wid; t < units; t += gridDim.x * 4ll) {
+    const int row = int(t / groups), c = int(t - (long long)row * groups) * 512 + 8 * lane;
+    Chunk<BF16 ? TYPE_BF16 : TYPE_F32> v;
+    v.zero();
+    if (c < cols) v.load(x, size_t(row) * cols + c);
+    float f[8];
+    v.values(f);
+    uint32_t top = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) top = max(top, abs_bits(f[e]));
+    top = max(top, uint32_t(dpp<kDppXor1>(int(top))));
+    top = max(top, uint32_t(dpp<kDppXor2>(int(top))));
+    top = max(top, uint32_t(dpp<kDppHalfMirror>(int(top))));
+    top = max(top, uint32_t(dpp<kDppMirror>(int(top))));
+    if (c < cols) *reinterpret_cast<uint2 *>(codes + size_t(row) * cols + c) = block_codes(f, top);
+    if ((lane & 15) == 0) scale[size_t(row) * scale_stride(cols) + c / 128] = c < cols ? block_scale(top) : 0;
+  }
+}
+
+// Blocks of 128 x 128: a workgroup each, a thread 8 rows of 8 columns, held while the largest is found.
+template <bool BF16>
+__global__ __launch_bounds__(256) void k_quantize_tiles(const void *__restrict__ x, int rows, int cols, const int *__restrict__ limit,
+                                                        uint8_t *__restrict__ codes, uint8_t *__restrict__ scale) {
+  __shared__ uint32_t tops[4];
+  const int end = limit ? min(rows, cu_at(limit, 0)) : rows;
+  const int c = blockIdx.x * 128 + 8 * (threadIdx.x & 15);
+  for (int r0 = blockIdx.y * 128; r0 < end; r0 += gridDim.y * 128) {
+    Chunk<BF16 ? TYPE_BF16 : TYPE_F32> v[8];
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int r = r0 + 16 * i + (threadIdx.x >> 4);
+      v[i].zero();
+      if (r < end && c < cols) v[i].load(x, size_t(r) * cols + c);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      float f[8];
+      v[i].values(f);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) top = max(top, abs_bits(f[e]));
+    }
+    top = wave_max_u32(top);
+    if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
+    __syncthreads();
+    top = max(max(tops[0], tops[1]), max(tops[2], tops[3]));
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int r = r0 + 16 * i + (threadIdx.x >> 4);
+      float f[8];
+      v[i].values(f);
+      if (r < end && c < cols) *reinterpret_cast<uint2 *>(codes + size_t(r) * cols + c) = block_codes(f, top);
+    }
+    // the last blocks' threads fill the group of four up with zeros
+    if (threadIdx.x == 0) scale[size_t(r0 / 128) * scale_stride(cols) + blockIdx.x] = blockIdx.x * 128 < cols ? block_scale(top) : 0;
+    __syncthreads();
+  }
+}
+
+hipError_t launch_quantize_blocks(bool bf16, const void *x, int rows, int cols, int block_rows, const int *limit, uint8_t *codes,
+                                  uint8_t *scale, hipStream_t st) {
+  if (rows <= 0) return hipSuccess;
+  if (block_rows == 1) {
+    const long long units = (long long)rows * (scale_stride(cols) / 4);
+    const dim3 grid(unsigned(std::min((units + 3) / 4, 1ll << 20)));
+    if (bf16) hipLaunchKernelGGL((k_quantize_blocks<true>), grid, dim3(256), 0, st, x, rows, cols, limit, codes, scale);
+    else hipLaunchKernelGGL((k_quantize_blocks<false>), grid, dim3(256), 0, st, x, rows, cols, limit, codes, scale);
+  } else {
+    const dim3 grid(scale_stride(cols), unsigned(std::min((rows + 127) / 128, 4096)));
+    if (bf16) hipLaunchKernelGGL((k_quantize_tiles<true>), grid, dim3(256), 0, st, x, rows, cols, limit, codes, scale);
+    else hipLaunchKernelGGL((k_quantize_tiles<false>), grid, dim3(256), 0, st, x, rows, cols, limit, codes, scale);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace hilo

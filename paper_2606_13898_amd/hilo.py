@@ -21,7 +21,7 @@ THRESHOLD, TOPK = 0, 1
 PARTITION, OVERLAP, DROP = 0, 1, 2  # hilo_token_set
 ROPE_ADJACENT, ROPE_ONE_SPECTRUM = 1, 2  # hilo_rope_flags
 NORM_LAYER, NORM_RMS = 0, 1  # hilo_norm_kind
-ACT_NONE, ACT_GELU = 0, 1  # hilo_act
+ACT_NONE, ACT_GELU, ACT_SILU = 0, 1, 2  # hilo_act
 DTYPES = {"f32": F32, "bf16": BF16}
 TORCH_DTYPES = {F32: torch.float32, BF16: torch.bfloat16}
 
@@ -74,6 +74,18 @@ class hilo_linear_w_i8(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("w", "s", "b")]
 
 
+class hilo_linear_w(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("w", "b", "w_gate", "b_gate")]
+
+
+class hilo_linear_grads(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("w", "b", "w_gate", "b_gate")]
+
+
+class hilo_linear_w_fp8(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("w", "s", "b", "w_gate", "s_gate", "b_gate")]
+
+
 _lib = None
 
 _P = ctypes.c_void_p
@@ -124,6 +136,18 @@ _SIG = {
     "hilo_linear_i8": [ctypes.c_int32, ctypes.POINTER(hilo_linear_w_i8), _P, _P, _P, ctypes.c_int64, ctypes.c_int32,
                        ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, _P, _P, ctypes.c_size_t, _P],
     "hilo_linear_i8_workspace_bytes": [ctypes.c_int64, ctypes.c_int32],
+    "hilo_linear": [ctypes.c_int32, ctypes.POINTER(hilo_linear_w), _P, _P, _P, ctypes.c_int64, ctypes.c_int32,
+                    ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, _P, _P, ctypes.c_size_t, _P],
+    "hilo_linear_workspace_bytes": [ctypes.c_int32, ctypes.c_int64] + [ctypes.c_int32] * 4,
+    "hilo_linear_backward": [ctypes.c_int32, ctypes.POINTER(hilo_linear_w), _P, _P, _P, _P,
+                             ctypes.POINTER(hilo_linear_grads), ctypes.c_int64, ctypes.c_int32, ctypes.c_int32,
+                             ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, _P, _P, ctypes.c_size_t, _P],
+    "hilo_linear_backward_workspace_bytes": [ctypes.c_int32, ctypes.c_int64] + [ctypes.c_int32] * 4,
+    "hilo_quantize_blocks": [ctypes.c_int32, _P, ctypes.c_int64, ctypes.c_int64, ctypes.c_int32, _P, _P, _P, _P],
+    "hilo_linear_fp8": [ctypes.c_int32, ctypes.POINTER(hilo_linear_w_fp8), _P, _P, _P, _P, ctypes.c_int64,
+                        ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, _P, _P,
+                        ctypes.c_size_t, _P],
+    "hilo_linear_fp8_workspace_bytes": [ctypes.c_int64] + [ctypes.c_int32] * 3,
     "hilo_workspace_bytes": [ctypes.POINTER(hilo_shape)],
     "hilo_workspace_bytes_fp8": [ctypes.POINTER(hilo_shape)],
     "hilo_max_tokens": [ctypes.POINTER(hilo_shape)],
@@ -137,6 +161,8 @@ _SIG = {
 }
 _RES = {"hilo_workspace_bytes": ctypes.c_size_t, "hilo_workspace_bytes_fp8": ctypes.c_size_t, "hilo_max_tokens": ctypes.c_int64,
         "hilo_norm_residual_workspace_bytes": ctypes.c_size_t, "hilo_linear_i8_workspace_bytes": ctypes.c_size_t,
+        "hilo_linear_workspace_bytes": ctypes.c_size_t, "hilo_linear_backward_workspace_bytes": ctypes.c_size_t,
+        "hilo_linear_fp8_workspace_bytes": ctypes.c_size_t,
         "hilo_status_str": ctypes.c_char_p, "hilo_profile_name": ctypes.c_char_p}
 
 
@@ -718,6 +744,209 @@ def hilo_linear_i8(w, x, out, cu, text_len: int = 0, *, x_scale=None, act: int =
             _arg(x, out.dtype if x_scale is None else torch.int8, (rows, k), dev, "x"),
             _arg(x_scale, torch.float32, (rows,), dev, "x_scale"), _arg(out, out.dtype, (rows, n), dev, "out"), rows, k, n,
             act, batch, text_len, cu_ptr, workspace.data_ptr(), workspace.numel() * workspace.element_size())
+
+
+# ---------------------------------------------------------- products of a feed-forward, gradients, FP8 blocks
+
+def _workspace(workspace, dev: int):
+    """Pointer and bytes of a workspace, or of none."""
+    if workspace is None:
+        return None, 0
+    if workspace.get_device() != dev or not workspace.is_contiguous():
+        raise ValueError("workspace: contiguous, on the tensors' device")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def _gated_pointers(struct, ds: Sequence[dict], dtype):
+    """Two of `struct` from dicts of tensors (one dict: for both streams): weights of one shape [out][in], biases [out] of one
+    type; dtype the weights' type, or None: float32 or bfloat16, that of the biases too.  Any may be missing."""
+    ds = list(ds)
+    if not 1 <= len(ds) <= 2:
+        raise ValueError("of one or two streams")
+    arr = (struct * 2)()
+    arr.kept, arr.shape, arr.dtype, arr.dev, arr.gated = ds, None, dtype, None, False
+    biases = []
+    for d in ds:
+        for name in ("w", "w_gate"):
+            w = d.get(name)
+            if w is None:
+                continue
+            if arr.shape is None:
+                arr.shape, arr.dev = w.shape, _on_device(w)
+                if len(arr.shape) != 2:
+                    raise ValueError("w: expected [out][in]")
+                if dtype is None:
+                    _float_code(w)
+                    arr.dtype = w.dtype
+            arr.gated = arr.gated or name == "w_gate"
+        biases += [(name, d[name]) for name in ("b", "b_gate") if d.get(name) is not None]
+    arr.bias = None
+    for name, b in biases:
+        _float_code(b)
+        if arr.dev is None:
+            arr.dev = _on_device(b)
+        if arr.bias not in (None, b.dtype) or (dtype is None and arr.dtype not in (None, b.dtype)):
+            raise ValueError(f"{name}: of one type")
+        arr.bias = b.dtype
+        arr.gated = arr.gated or name == "b_gate"
+    arr.out = arr.shape[0] if arr.shape is not None else biases[0][1].numel() if biases else None
+    for k in range(2):
+        d = ds[min(k, len(ds) - 1)]
+        for name in [f[0] for f in struct._fields_]:
+            t = d.get(name)
+            if t is None:
+                continue
+            if name[0] == "w":
+                ptr = _arg(t, arr.dtype, arr.shape, arr.dev, name)
+            elif name[0] == "s":
+                ptr = _arg(t, torch.uint8, (-(-arr.shape[0] // 128), scale_stride(arr.shape[1])), arr.dev, name)
+            else:
+                ptr = _arg(t, arr.bias, (arr.out,), arr.dev, name)
+            setattr(arr[k], name, ptr)
+    return arr
+
+
+def linear_weights(ws: Sequence[dict]):
+    """Weights of hilo_linear: {"w": [out][in], "b": [out] or None, "w_gate", "b_gate": the gate's, or missing} of the image
+    and the text stream (one dict: of both), all float32 or all bfloat16.  Keeps the tensors alive."""
+    ws = list(ws)
+    if any(d.get("w") is None for d in ws):
+        raise ValueError("w: missing")
+    return _gated_pointers(hilo_linear_w, ws, None)
+
+
+def linear_grads(ds: Sequence[dict]):
+    """Where hilo_linear_backward leaves the gradients: dicts as in linear_weights, any tensor None (one dict: sums over
+    both streams)."""
+    return _gated_pointers(hilo_linear_grads, ds, None)
+
+
+def _product_rows(fn: str, w, rows_of: torch.Tensor, cols: int, cu: torch.Tensor, text_len: int, act: int):
+    dev = _on_device(rows_of)
+    if dev != w.dev:
+        raise ValueError(f"weights on device {w.dev}, rows on device {dev}")
+    if rows_of.dim() != 2 or rows_of.shape[1] != cols:
+        raise ValueError(f"expected [rows][{cols}], not {tuple(rows_of.shape)}")
+    n, k = w.shape
+    batch, cu_ptr = _packed(cu, dev)
+    if (n | k | batch | text_len) >> 31:
+        raise HiloError(fn, 2)
+    if act >> 31:
+        raise HiloError(fn, 4)
+    return dev, rows_of.shape[0], n, k, batch, cu_ptr
+
+
+def hilo_linear_workspace_bytes(dtype: torch.dtype, rows: int, in_dim: int, out_dim: int, batch: int, gated: bool = False) -> int:
+    return 0 if (in_dim | out_dim | batch) >> 31 else lib().hilo_linear_workspace_bytes(
+        _FLOATS.get(dtype, -1), rows, in_dim, out_dim, batch, 1 if gated else 0)
+
+
+def hilo_linear(w, x, out, cu, text_len: int = 0, *, act: int = ACT_NONE, pre=None, workspace=None, stream=None):
+    """out [rows][out] = x w^T + b of linear_weights w, or act(x w_gate^T + b_gate) (x w^T + b); pre [rows][2][out]: g and u
+    for the backward pass."""
+    dev, rows, n, k, batch, cu_ptr = _product_rows("hilo_linear", w, out, w.shape[0], cu, text_len, act)
+    dt = w.dtype
+    ws, nbytes = _workspace(workspace, dev)
+    _launch("hilo_linear", dev, stream, _FLOATS[dt], w, _arg(x, dt, (rows, k), dev, "x"), _arg(out, dt, (rows, n), dev, "out"),
+            _arg(pre, dt, (rows, 2, n), dev, "pre"), rows, k, n, act, batch, text_len, cu_ptr, ws, nbytes)
+
+
+def hilo_linear_backward_workspace_bytes(dtype: torch.dtype, rows: int, in_dim: int, out_dim: int, batch: int,
+                                         gated: bool = False) -> int:
+    return 0 if (in_dim | out_dim | batch) >> 31 else lib().hilo_linear_backward_workspace_bytes(
+        _FLOATS.get(dtype, -1), rows, in_dim, out_dim, batch, 1 if gated else 0)
+
+
+def hilo_linear_backward(w, x, pre, dout, dx, grads, cu, text_len: int = 0, *, act: int = ACT_NONE, workspace=None,
+                         stream=None):
+    """Gradients of hilo_linear from dout: dx (or None), and those in linear_grads grads (or None)."""
+    dev, rows, n, k, batch, cu_ptr = _product_rows("hilo_linear_backward", w, dout, w.shape[0], cu, text_len, act)
+    dt = w.dtype
+    if grads is not None:
+        if grads.dev not in (None, dev):
+            raise ValueError(f"gradients on device {grads.dev}, rows on device {dev}")
+        if grads.shape not in (None, w.shape) or grads.out not in (None, n):
+            raise ValueError(f"gradients: expected the shapes of w {tuple(w.shape)}")
+        if grads.dtype not in (None, dt) or grads.bias not in (None, dt):
+            raise ValueError(f"gradients: expected {dt}")
+    ws, nbytes = _workspace(workspace, dev)
+    _launch("hilo_linear_backward", dev, stream, _FLOATS[dt], w, _arg(x, dt, (rows, k), dev, "x"),
+            _arg(pre, dt, (rows, 2, n), dev, "pre"), _arg(dout, dt, (rows, n), dev, "dout"), _arg(dx, dt, (rows, k), dev, "dx"),
+            grads, rows, k, n, act, batch, text_len, cu_ptr, ws, nbytes)
+
+
+def scale_stride(cols: int) -> int:
+    """Bytes in a row of E8M0 scales: one for each 128 columns, in whole groups of four."""
+    return 4 * -(-cols // 512)
+
+
+def hilo_quantize_blocks(x, codes, scales, block_rows: int = 1, cu=None, stream=None):
+    """E4M3 codes (uint8 [rows][cols]) of x and E8M0 scales (uint8 [rows / block_rows][scale_stride(cols)]), one for each
+    block of block_rows (1 or 128) rows and 128 columns; cu: the boundaries, whose last one bounds the rows."""
+    dev, dtype = _on_device(x), _float_code(x)
+    if x.dim() != 2:
+        raise ValueError("x: expected [rows][cols]")
+    if block_rows not in (1, 128):
+        raise HiloError("hilo_quantize_blocks", 4)
+    end = None
+    if cu is not None:
+        b, end = _packed(cu, dev)
+        end += 4 * b
+    rows, cols = x.shape
+    _launch("hilo_quantize_blocks", dev, stream, dtype, _arg(x, x.dtype, x.shape, dev, "x"), rows, cols, block_rows, end,
+            _arg(codes, torch.uint8, x.shape, dev, "codes"),
+            _arg(scales, torch.uint8, (-(-rows // block_rows), scale_stride(cols)), dev, "scales"))
+
+
+def quantize_block_weights(w, b=None, w_gate=None, b_gate=None, stream=None) -> dict:
+    """A product's weights for linear_weights_fp8: codes and scales of w [out][in] and w_gate, the biases kept."""
+    d = {"b": b, "b_gate": b_gate}
+    for name, sname, t in (("w", "s", w), ("w_gate", "s_gate", w_gate)):
+        if t is None:
+            continue
+        d[name] = torch.empty(t.shape, dtype=torch.uint8, device=t.device)
+        d[sname] = torch.empty(-(-t.shape[0] // 128), scale_stride(t.shape[1]), dtype=torch.uint8, device=t.device)
+        hilo_quantize_blocks(t, d[name], d[sname], 128, stream=stream)
+    return d
+
+
+def linear_weights_fp8(ws: Sequence[dict]):
+    """Weights of hilo_linear_fp8: {"w": uint8 [out][in], "s": uint8 [out / 128][scale_stride(in)], "b": [out] or None, and
+    "w_gate", "s_gate", "b_gate" with a gate} of the image and the text stream (one dict: of both).  Keeps the tensors alive."""
+    ws = list(ws)
+    for d in ws:
+        if d.get("w") is None or d.get("s") is None or (d.get("w_gate") is None) != (d.get("s_gate") is None):
+            raise ValueError("weights and scales go together")
+    return _gated_pointers(hilo_linear_w_fp8, ws, torch.uint8)
+
+
+def hilo_linear_fp8_workspace_bytes(rows: int, in_dim: int, out_dim: int, gated: bool = False) -> int:
+    return 0 if (in_dim | out_dim) >> 31 else lib().hilo_linear_fp8_workspace_bytes(rows, in_dim, out_dim, 1 if gated else 0)
+
+
+def hilo_linear_fp8(w, x, out, cu, text_len: int = 0, *, x_scale=None, out_scale=None, act: int = ACT_NONE, workspace=None,
+                    stream=None):
+    """hilo_linear on E4M3 codes with block scales: x uint8 codes with x_scale [rows][scale_stride(in)], or float rows,
+    quantised here; out of a float type, or with out_scale [rows][scale_stride(out)] uint8 codes (a gate only).  Float tensors
+    and biases are of one type; where there is none, sums and activations are rounded only to codes."""
+    dev, rows, n, k, batch, cu_ptr = _product_rows("hilo_linear_fp8", w, out, w.shape[0], cu, text_len, act)
+    u8, floats = torch.uint8, []
+    if out_scale is None:
+        floats.append(("out", out.dtype))
+    if x_scale is None:
+        floats.append(("x", x.dtype))
+    if w.bias is not None:
+        floats.append(("b", w.bias))
+    dt = floats[0][1] if floats else torch.float32
+    for name, t in floats:
+        if t is not dt:
+            raise ValueError(f"{name}: {t}, other tensors {dt}")
+    if dt not in _FLOATS:
+        raise ValueError(f"float32 or bfloat16 expected, not {dt}")
+    ws, nbytes = _workspace(workspace, dev)
+    _launch("hilo_linear_fp8", dev, stream, _FLOATS[dt], w, _arg(x, dt if x_scale is None else u8, (rows, k), dev, "x"),
+            _arg(x_scale, u8, (rows, scale_stride(k)), dev, "x_scale"), _arg(out, dt if out_scale is None else u8, (rows, n), dev, "out"),
+            _arg(out_scale, u8, (rows, scale_stride(n)), dev, "out_scale"), rows, k, n, act, batch, text_len, cu_ptr, ws, nbytes)
 
 
 def hilo_profile_enable(on: bool):

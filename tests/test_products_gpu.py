@@ -1,0 +1,262 @@
+"""The products of a feed-forward against their definitions in float64: forward, gradients, FP8 blocks.
+
+Tolerances.  A float32 sum of K products x w is off by at most (K + 2) 2^-24 sum |x w| in any order; the FP8 matrix
+instruction adds products that it aligns to the largest of a group, each cut by at most a step, 2^-23 of it, so (K + 2) 2^-23.  What
+the activation adds, and how errors of g and u reach the output, is oracle.hilo_products'; the last rounding is half a
+step: 2^-8 (bf16) or 2^-24 of the value, of codes 2^-4 and half the least step, 2^-10 of the scale."""
+import pytest
+import torch
+
+from oracle import hilo_products as P
+from paper_2606_13898_amd import hilo
+
+pytestmark = pytest.mark.gpu
+
+F64 = torch.float64
+HALF = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8}
+ACTS = {None: hilo.ACT_NONE, "silu": hilo.ACT_SILU, "gelu": hilo.ACT_GELU}
+BEHIND = 3  # rows behind the last sample: NaN in, left alone out
+
+
+def pack(images, text):
+    cu = [0]
+    for n in images:
+        cu.append(cu[-1] + n + text)
+    return cu
+
+
+def weights(g, streams, n, k, dt, gate, bias):
+    ws = []
+    for _ in range(streams):
+        d = {}
+        for part in ("", "_gate") if gate else ("",):
+            d["w" + part] = (torch.randn(n, k, generator=g) * k ** -0.5).to(dt)
+            d["b" + part] = (torch.randn(n, generator=g) * 0.3).to(dt) if bias else None
+        ws.append(d)
+    return ws
+
+
+def cuda(ds):
+    return [{k: None if v is None else v.cuda() for k, v in d.items()} for d in ds]
+
+
+def rows_like(t, behind):
+    """t on the device with `behind` more rows of NaN (of 0x7f codes)."""
+    pad = torch.full((BEHIND, *t.shape[1:]), float("nan") if t.dtype.is_floating_point else behind, dtype=t.dtype)
+    return torch.cat([t, pad]).cuda()
+
+
+def near(got, want, bound, what):
+    got = got.cpu().to(F64)
+    off = (got - want).abs()
+    bad = ~(off <= bound + 1e-30)
+    assert not bad.any(), (what, int(bad.sum()), float((off / (bound + 1e-30)).nan_to_num(1e9).max()),
+                           float(got[bad][0]), float(want[bad][0]))
+
+
+# image rows of each sample, text rows, in, out, streams of weights
+SHAPES = [
+    ([1], 0, 8, 8, 1),
+    ([1], 0, 1024, 520, 1),
+    ([7], 0, 264, 136, 1),
+    ([33, 0, 5], 3, 64, 72, 2),
+    ([0], 9, 40, 1000, 2),
+    ([64, 64], 64, 128, 256, 2),
+    ([129], 0, 8, 640, 1),
+    ([100, 31, 260], 17, 200, 344, 2),
+    ([100, 31, 260], 17, 200, 344, 1),
+    ([300], 213, 520, 264, 2),
+    ([1, 1, 1, 1], 0, 2056, 648, 1),
+    ([600], 0, 1032, 1288, 1),
+    ([513, 2, 700], 40, 328, 776, 2),
+]
+KINDS = [(torch.bfloat16, "silu", True), (torch.bfloat16, "gelu", False), (torch.bfloat16, None, True),
+         (torch.float32, "silu", False), (torch.float32, "gelu", True), (torch.float32, None, False)]
+
+
+def case_id(v):
+    return str(v).replace("torch.", "").replace(" ", "")
+
+
+@pytest.mark.parametrize("shape", SHAPES, ids=case_id)
+@pytest.mark.parametrize("kind", KINDS, ids=case_id)
+def test_forward(shape, kind):
+    (images, text, k, n, streams), (dt, act, bias) = shape, kind
+    g = torch.Generator().manual_seed(len(images) * 1000 + k + n)
+    cu = pack(images, text)
+    x = torch.randn(cu[-1], k, generator=g).to(dt)
+    ws = weights(g, streams, n, k, dt, act, bias)
+    T = cu[-1] + BEHIND
+    out = torch.full((T, n), 7.0, dtype=dt, device="cuda")
+    pre = torch.full((T, 2, n), 7.0, dtype=dt, device="cuda") if act else None
+    need = hilo.hilo_linear_workspace_bytes(dt, T, k, n, len(images), gated=act is not None)
+    ws_dev = torch.empty(need, dtype=torch.uint8, device="cuda").fill_(0xff)
+    plan = hilo.linear_weights(cuda(ws))
+    cud = torch.tensor(cu, dtype=torch.int32, device="cuda")
+    hilo.hilo_linear(plan, rows_like(x, 0), out, cud, text, act=ACTS[act], pre=pre, workspace=ws_dev)
+    torch.cuda.synchronize()
+    assert (out[cu[-1]:] == 7.0).all()
+    xd, ulp = x.to(F64), 2.0 ** -24
+    u, su = P.affine(xd, ws, "", cu, text)
+    eu = (k + 2) * ulp * su
+    if act is None:
+        near(out[:cu[-1]], u, eu + HALF[dt] * (u.abs() + eu), "out")
+        return
+    v, sv = P.affine(xd, ws, "_gate", cu, text)
+    ev = (k + 2) * ulp * sv
+    want, off = P.gated(act, v, u, ev, eu, dt is torch.bfloat16)
+    near(out[:cu[-1]], want, off + HALF[dt] * (want.abs() + off), "out")
+    assert (pre[cu[-1]:] == 7.0).all()
+    near(pre[:cu[-1], 0], v, ev + HALF[dt] * (v.abs() + ev), "g")
+    near(pre[:cu[-1], 1], u, eu + HALF[dt] * (u.abs() + eu), "u")
+    # without pre: the same bits
+    again = torch.zeros_like(out)
+    hilo.hilo_linear(plan, rows_like(x, 0), again, cud, text, act=ACTS[act], workspace=ws_dev)
+    assert torch.equal(again[:cu[-1]], out[:cu[-1]])
+
+
+@pytest.mark.parametrize("shape", SHAPES, ids=case_id)
+@pytest.mark.parametrize("kind", KINDS, ids=case_id)
+def test_backward(shape, kind):
+    (images, text, k, n, streams), (dt, act, bias) = shape, kind
+    g = torch.Generator().manual_seed(len(images) * 1000 + k + n + 1)
+    cu = pack(images, text)
+    x = torch.randn(cu[-1], k, generator=g).to(dt)
+    dout = torch.randn(cu[-1], n, generator=g).to(dt)
+    pre = torch.randn(cu[-1], 2, n, generator=g).to(dt) if act else None
+    ws = weights(g, streams, n, k, dt, act, True)
+    T = cu[-1] + BEHIND
+    dx = torch.full((T, k), 7.0, dtype=dt, device="cuda")
+    got = [{name: torch.full_like(v, 7.0, device="cuda") for name, v in d.items()} for d in ws]
+    need = hilo.hilo_linear_backward_workspace_bytes(dt, T, k, n, len(images), gated=act is not None)
+    ws_dev = torch.empty(need, dtype=torch.uint8, device="cuda").fill_(0xff)
+    cud = torch.tensor(cu, dtype=torch.int32, device="cuda")
+    args = (hilo.linear_weights(cuda(ws)), rows_like(x, 0), None if pre is None else rows_like(pre, 0), rows_like(dout, 0))
+    hilo.hilo_linear_backward(*args, dx, hilo.linear_grads(got), cud, text, act=ACTS[act], workspace=ws_dev)
+    torch.cuda.synchronize()
+    assert (dx[cu[-1]:] == 7.0).all()
+    (wx, bx), want = P.backward(x.to(F64), ws, None if pre is None else pre.to(F64), dout.to(F64), act, cu, text, HALF[dt],
+                                streams == 1)
+    near(dx[:cu[-1]], wx, bx, "dx")
+    for kk, d in enumerate(got):
+        for name, t in d.items():
+            near(t, *want[kk][name], f"{name} of {kk}")
+    # each output alone: the same bits
+    alone = torch.zeros_like(dx)
+    hilo.hilo_linear_backward(*args, alone, None, cud, text, act=ACTS[act], workspace=ws_dev)
+    assert torch.equal(alone[:cu[-1]], dx[:cu[-1]])
+    for kk, d in enumerate(got):
+        for name, t in d.items():
+            one = [{name: torch.zeros_like(t)} if j == kk else {} for j in range(streams)]
+            hilo.hilo_linear_backward(*args, None, hilo.linear_grads(one), cud, text, act=ACTS[act], workspace=ws_dev)
+            if streams == 2 or len(want) == 1:
+                near(one[kk][name], *want[kk][name], f"{name} of {kk} alone")
+
+
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32], ids=case_id)
+@pytest.mark.parametrize("rows, cols", [(1, 16), (5, 128), (130, 144), (77, 1040), (300, 512), (3, 4112)])
+@pytest.mark.parametrize("block_rows", [1, 128])
+def test_quantize(dt, rows, cols, block_rows):
+    g = torch.Generator().manual_seed(rows + cols)
+    x = torch.randn(rows, cols, generator=g) * torch.exp2(torch.randint(-30, 30, (rows, 1), generator=g).float())
+    x[0, :16] = 0
+    if rows > 2:
+        x[1] = 0
+        x[2] *= 2.0 ** -118  # to float32's least numbers
+    x[-1, -1] = 448 * 2.0 ** 9  # the largest value that a scale reaches
+    x = x.to(dt)
+    codes = torch.full((rows + 2, cols), 9, dtype=torch.uint8, device="cuda")
+    scales = torch.full((-(-(rows + 2) // block_rows), hilo.scale_stride(cols)), 9, dtype=torch.uint8, device="cuda")
+    cu = torch.tensor([0, rows], dtype=torch.int32, device="cuda")
+    hilo.hilo_quantize_blocks(torch.cat([x, torch.full((2, cols), float("inf"), dtype=dt)]).cuda(), codes, scales, block_rows, cu)
+    want, k = P.quantize(x.to(F64), block_rows)
+    n = -(-rows // block_rows)
+    assert torch.equal(scales[:n, :k.shape[1]].cpu().to(F64), k + 127)
+    assert (scales[:n, k.shape[1]:] == 0).all() and (codes[rows:] == 9).all() and (scales[n:] == 9).all()
+    assert torch.equal(P.decode(codes[:rows].cpu(), scales[:n].cpu(), block_rows), want)
+
+
+def test_quantize_not_finite():
+    for bad in (float("inf"), float("nan"), -float("inf")):
+        for block_rows in (1, 128):
+            x = torch.ones(2, 256)
+            x[1, 130] = bad
+            codes, scales = torch.zeros(2, 256, dtype=torch.uint8, device="cuda"), torch.zeros(2 // block_rows or 1, 4, dtype=torch.uint8, device="cuda")
+            hilo.hilo_quantize_blocks(x.cuda(), codes, scales, block_rows)
+            v = P.decode(codes.cpu(), scales.cpu(), block_rows)
+            assert v[1, 128:].isnan().all() and (v[:, :128] == 1).all() and v[0, 128:].isnan().all() == (block_rows == 128)
+
+
+FP8_SHAPES = [
+    ([1], 0, 16, 16, 1),
+    ([1], 0, 2064, 528, 1),
+    ([7], 0, 272, 144, 1),
+    ([33, 0, 5], 3, 64, 80, 2),
+    ([0], 9, 48, 1008, 2),
+    ([64, 64], 64, 128, 256, 2),
+    ([100, 31, 260], 17, 208, 352, 2),
+    ([100, 31, 260], 17, 528, 352, 1),
+    ([4, 1], 0, 1168, 640, 1),
+    ([600], 0, 1040, 1296, 1),
+    ([513, 2, 700], 40, 336, 784, 2),
+]
+
+
+def fp8_weights(g, streams, n, k, dt, act, bias):
+    ws = weights(g, streams, n, k, torch.float32, act, bias)
+    for d in ws:
+        for part in ("", "_gate") if act else ("",):
+            if d["b" + part] is not None:
+                d["b" + part] = d["b" + part].to(dt)
+    plans = [hilo.quantize_block_weights(**{name: None if v is None else v.cuda() for name, v in d.items()}) for d in ws]
+    for d in ws:
+        for part in ("", "_gate") if act else ("",):
+            d["w" + part] = P.quantize(d["w" + part].to(F64), 128)[0]
+    return ws, hilo.linear_weights_fp8(plans)
+
+
+@pytest.mark.parametrize("shape", FP8_SHAPES, ids=case_id)
+@pytest.mark.parametrize("kind", KINDS, ids=case_id)
+@pytest.mark.parametrize("coded", [False, True])
+def test_fp8(shape, kind, coded):
+    (images, text, k, n, streams), (dt, act, bias) = shape, kind
+    g = torch.Generator().manual_seed(len(images) * 1000 + k + n + 2)
+    cu = pack(images, text)
+    x = torch.randn(cu[-1], k, generator=g) * torch.exp2(torch.randint(-3, 4, (1, k), generator=g).float())
+    x = x.to(dt)
+    ws, plan = fp8_weights(g, streams, n, k, dt, act, bias)
+    T = cu[-1] + BEHIND
+    need = hilo.hilo_linear_fp8_workspace_bytes(T, k, n, gated=act is not None)
+    ws_dev = torch.empty(need, dtype=torch.uint8, device="cuda").fill_(0xff)
+    cud = torch.tensor(cu, dtype=torch.int32, device="cuda")
+    out = torch.full((T, n), 7.0, dtype=dt, device="cuda")
+    xin, a = rows_like(x, 0), {}
+    if coded:
+        codes = torch.full((T, k), 0x7f, dtype=torch.uint8, device="cuda")
+        a["x_scale"] = torch.full((T, hilo.scale_stride(k)), 255, dtype=torch.uint8, device="cuda")
+        hilo.hilo_quantize_blocks(xin, codes, a["x_scale"], cu=cud)
+        xin = codes
+    hilo.hilo_linear_fp8(plan, xin, out, cud, text, act=ACTS[act], workspace=ws_dev, **a)
+    torch.cuda.synchronize()
+    assert (out[cu[-1]:] == 7.0).all()
+    xq, step = P.quantize(x.to(F64), 1)[0], 2.0 ** -23
+    u, su = P.affine(xq, ws, "", cu, text)
+    eu = (k + 2) * step * su
+    if act is None:
+        near(out[:cu[-1]], u, eu + HALF[dt] * (u.abs() + eu), "out")
+        return
+    v, sv = P.affine(xq, ws, "_gate", cu, text)
+    want, off = P.gated(act, v, u, (k + 2) * step * sv, eu, True)
+    near(out[:cu[-1]], want, off + HALF[dt] * (want.abs() + off), "out")
+    # codes out: of the float32 values, whose block may just have another scale
+    h = torch.full((T, n), 9, dtype=torch.uint8, device="cuda")
+    hs = torch.full((T, hilo.scale_stride(n)), 9, dtype=torch.uint8, device="cuda")
+    hilo.hilo_linear_fp8(plan, xin, h, cud, text, act=ACTS[act], workspace=ws_dev, out_scale=hs, **a)
+    assert (h[cu[-1]:] == 9).all() and (hs[cu[-1]:] == 9).all()
+    blocks = -(-n // 128)
+    kk = hs[:cu[-1], :blocks].cpu().to(F64) - 127
+    lo = torch.stack([(b[0].abs() - b[1]).clamp(min=0).amax(1) for b in zip(want.split(128, 1), off.split(128, 1))], 1)
+    hi = torch.stack([(b[0].abs() + b[1]).amax(1) for b in zip(want.split(128, 1), off.split(128, 1))], 1)
+    assert ((kk >= P.block_exponent(lo)) & (kk <= P.block_exponent(hi))).all()
+    scale = torch.exp2(kk).repeat_interleave(128, 1)[:, :n]
+    near(P.decode(h[:cu[-1]].cpu(), hs[:cu[-1]].cpu(), 1), want, off + 2.0 ** -4 * (want.abs() + off) + 2.0 ** -10 * scale, "codes")
