@@ -236,6 +236,9 @@ size_t product_part_bytes(bool bf16, int kind, long long rows, int K, int N, int
 size_t product_fp8_part_bytes(long long rows, int K, int N, int parts);
 hipError_t launch_product(int kind, ProductProblem p, hipStream_t st);
 hipError_t launch_product_fp8(ProductProblem p, hipStream_t st);
+// bf16 on large tiles (product_bf16.hip), with partial tiles in p.part.
+size_t product_tiles_part_bytes();
+hipError_t launch_product_tiles(int kind, const ProductProblem &p, hipStream_t st);
 
 // The step between: dpre [rows][2][N] from dout and pre (gated), and the sums over rows of dpre, or of dout, by stream
 // into db[stream][part] (any null; the two streams' the same: sums over both).

@@ -287,6 +287,7 @@ static int splits_of(int kind, long long rows, int K, int N, int parts, int outs
 
 // Most partial sums of any call: one segment has the fewest tiles, so the most splits.
 size_t product_part_bytes(bool bf16, int kind, long long rows, int K, int N, int parts) {
+  if (bf16) return product_tiles_part_bytes();
   size_t most = 0;
   for (int outs = 1; outs <= (kind == PRODUCT_DW ? 4 : 1); ++outs) {
     const int s = splits_of(kind, rows, K, N, parts, outs, 1, true);
@@ -296,7 +297,7 @@ size_t product_part_bytes(bool bf16, int kind, long long rows, int K, int N, int
   return most;
 }
 size_t product_fp8_part_bytes(long long rows, int K, int N, int parts) {
-  return product_part_bytes(true, PRODUCT_OUT, rows, K, N, parts);
+  return product_part_bytes(false, PRODUCT_OUT, rows, K, N, parts);
 }
 
 template <int TYPE, int KIND, bool GATED>
@@ -323,7 +324,8 @@ static hipError_t run_kind(int kind, ProductProblem &p, hipStream_t st) {
 }
 
 hipError_t launch_product(int kind, ProductProblem p, hipStream_t st) {
-  return p.bf16 ? run_kind<TYPE_BF16>(kind, p, st) : run_kind<TYPE_F32>(kind, p, st);
+  if (kind == PRODUCT_DW && p.outs == 0) return hipSuccess;
+  return p.bf16 ? launch_product_tiles(kind, p, st) : run_kind<TYPE_F32>(kind, p, st);
 }
 
 hipError_t launch_product_fp8(ProductProblem p, hipStream_t st) {

@@ -1,0 +1,636 @@
+// The bf16 products of a feed-forward and their gradients on large tiles (product.hip has their mathematics).
+//
+// One persistent workgroup of 8 waves a CU (2 x 4, a wave's tile BM / 2 x BN / 4 in 16 x 16 MFMA blocks).  K goes through
+// LDS in windows of 64 values, filled by direct loads to LDS some windows ahead, also of the tiles to come; while the MFMAs of one half of
+// a window run, the fragments of the next half are read.  One barrier a window.
+//
+// An operand lies in memory with k last (x and w of the forward product, the gradients dpre of dx), or with k first (w of
+// dx, both of dw), and goes to LDS as it lies there:
+//   k last   a window is 128-byte rows, a fragment read 16 bytes a lane; 16-byte chunk c of row r at c ^ (r / 2) % 8
+//   k first  a window is 64 rows of the tile's columns; a fragment is two transposing reads, in which 16 lanes take four
+//            rows of 16 columns and each gets a column's four values; 32-byte chunk c of row k at c ^ f(k), f(k) = k % 4 + 4
+//            (k / 8 % 2), so that the rows that 32 lanes read at once lie in eight groups of banks
+// What lies behind the last row, column or k is never read: the loads' buffer ends there, and they leave zeros.
+#include <algorithm>
+
+#include "product.h"
+
+namespace hilo {
+
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+namespace pt {
+
+constexpr int P = kGemmWorkgroups;
+
+template <int BM_, int BN_, int KIND_, bool GATED_>
+struct Geo {
+  static constexpr int BM = BM_, BN = BN_, KIND = KIND_;
+  static constexpr bool GATED = GATED_ && KIND == PRODUCT_OUT;  // two products a tile, half its columns each
+  static constexpr bool AK = KIND != PRODUCT_DW, BK = KIND == PRODUCT_OUT;  // k last
+  static constexpr int MB = BM / 32, NB = BN / 64;
+  static constexpr int LA = BM / 64, LB = BN / 64;  // load instructions of a wave for a window
+  static constexpr int WB = (BM + BN) * 128;
+  static constexpr int SLOTS = 3 * WB <= 160 * 1024 ? 3 : 2;
+  static constexpr int COLS = GATED ? BN / 2 : BN;  // columns of the output
+};
+
+// Tiles in groups of 8 row tiles by all column tiles, row tile fastest: the 32 workgroups of an XCD then share 8 + 4 slices
+// of the operands.
+HILO_DEV void tile_at(int R, int TN, int t, int &r, int &c) {
+  const int grp = t / (8 * TN), in = t - grp * 8 * TN, gm = min(8, R - grp * 8);
+  c = in / gm;
+  r = grp * 8 + in - c * gm;
+}
+
+// Tiles run whole, P at a time; what is left over for a last turn is cut along k into s pieces each, as many as there are
+// workgroups for, where that is quicker than a whole turn.  Pieces leave float32 tiles that k_product_fix adds up.
+struct Plan {
+  int R, TN, T, full, tail, s;
+};
+struct Item {
+  int t, pc, n, slot;  // tile, piece of n, slot of its partial sums (n > 1)
+  bool valid;
+};
+HILO_DEV Item item_at(const Plan &q, int u) {
+  if (u < q.full) return Item{u, 0, 1, 0, true};
+  const int v = u - q.full;
+  if (v >= q.tail * q.s) return Item{0, 0, 1, 0, false};
+  const int pc = v / q.tail;
+  return Item{q.full + v - pc * q.tail, pc, q.s, v, true};
+}
+
+// In units of 10 ns: a window of 64 and a tile's rest, and what pieces of the last turn cost beside their windows.
+struct Cost {
+  int window, tile, fix;
+};
+HILO_DEV int plan_tail(int tail, int nk, Cost c) {
+  if (tail == 0) return 1;
+  const int s = min(P / tail, nk / 4);
+  return s > 1 && nk * c.window > nk * c.window / s + c.fix ? s : 1;
+}
+HILO_DEV int plan_cost(int T, int nk, Cost c) {
+  const int tail = T % P, s = plan_tail(tail, nk, c);
+  return T / P * (nk * c.window + c.tile) + (tail ? nk * c.window / s + c.tile + (s > 1 ? c.fix : 0) : 0);
+}
+template <typename G>
+HILO_DEV Plan make_plan(const ProductProblem &p, int R, int nk, Cost c) {
+  Plan q;
+  q.R = R;
+  q.TN = ((G::KIND == PRODUCT_OUT ? p.N : p.K) + G::COLS - 1) / G::COLS;
+  q.T = q.R * q.TN;
+  q.tail = q.T % P;
+  q.full = q.T - q.tail;
+  q.s = plan_tail(q.tail, nk, c);
+  return q;
+}
+
+// Where a tile lies: rows row0 .. + rows of the output (DW: of output o), columns from n0, stream, and for the backward
+// products the part.
+struct Place {
+  int row0, rows, n0, stream, part, o;
+};
+template <typename G>
+HILO_DEV Place place_of(const ProductProblem &p, const Plan &q, int t) {
+  int r, c;
+  Place z;
+  if constexpr (G::KIND == PRODUCT_DW) {
+    const int per = q.R / p.outs * q.TN;  // R: the row tiles of all outputs
+    z.o = t / per;
+    tile_at(q.R / p.outs, q.TN, t - z.o * per, r, c);
+    z.stream = p.out_stream[z.o];
+    z.part = p.out_part[z.o];
+    z.row0 = r * G::BM;
+    z.rows = min(G::BM, p.N - z.row0);
+  } else {
+    tile_at(q.R, q.TN, t, r, c);
+    z.o = z.part = 0;
+    RowTile rt{0, 0, 0};
+    if (p.merged || p.B > 32) {
+      rt = find_row_tile(p, G::BM, r);
+    } else {  // few samples: by scalar loads, which wait for no load of a tile
+      for (int i = 0; i < 2 * p.B; ++i) {
+        const Segment s = segment(p, i);
+        const int tiles = (s.n + G::BM - 1) / G::BM;
+        if (r < tiles) {
+          rt = RowTile{s.lo + r * G::BM, min(G::BM, s.n - r * G::BM), s.stream};
+          break;
+        }
+        r -= tiles;
+      }
+    }
+    z.row0 = rt.row0;
+    z.rows = rt.n;
+    z.stream = rt.stream;
+  }
+  z.n0 = c * G::COLS;
+  return Place{uni(z.row0), uni(z.rows), uni(z.n0), uni(z.stream), uni(z.part), uni(z.o)};
+}
+
+// Windows of a tile's sum; of a stream's segments in DW.
+template <int KIND>
+HILO_DEV int windows(const ProductProblem &p, int stream) {
+  if constexpr (KIND == PRODUCT_OUT) return (p.K + 63) / 64;
+  if constexpr (KIND == PRODUCT_DX) return p.parts * ((p.N + 63) / 64);
+  int n = 0;
+  for (int i = p.merged ? 0 : stream; i < segments(p); i += 2) n += (segment(p, i).n + 63) / 64;
+  return n;
+}
+
+// One 16-byte load per lane straight to LDS, zeros where the offset lies behind the buffer's end: lane l's bytes land at
+// 16 l of the wave's 1 KiB.
+HILO_DEV void buffer_to_lds(const char *base, uint32_t bytes, uint32_t offset, void *lds_wave_base) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(
+      __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(base), 0, int(bytes), 0x00020000),
+      (__attribute__((address_space(3))) void *)lds_wave_base, 16, int(offset), 0, 0, 0);
+}
+constexpr uint32_t kBehind = 0xffffff00u;  // an offset behind any buffer's end
+
+template <int N>
+HILO_DEV void wait_vm() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
+template <int V>
+struct Int {
+  static constexpr int value = V;
+};
+template <int OFF>
+HILO_DEV void read16(u32x4 &d, uint32_t addr) {
+  asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(d) : "v"(addr), "n"(OFF) : "memory");
+}
+template <int OFF>
+HILO_DEV void read_tr(u32x2 &d, uint32_t addr) {
+  asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(d) : "v"(addr), "n"(OFF) : "memory");
+}
+
+// A fragment: 8 values of k of a row, in one read or two.
+template <bool LAST>
+struct Frag;
+template <>
+struct Frag<true> {
+  u32x4 v;
+  HILO_DEV bf16x8 get() const { return __builtin_bit_cast(bf16x8, v); }
+  HILO_DEV void pin() { asm volatile("" : "+v"(v)); }
+};
+template <>
+struct Frag<false> {
+  u32x2 lo, hi;
+  HILO_DEV bf16x8 get() const { return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3)); }
+  HILO_DEV void pin() { asm volatile("" : "+v"(lo), "+v"(hi)); }
+};
+
+HILO_DEV void swap16(uint32_t &x, uint32_t &y) {
+  const auto r = __builtin_amdgcn_permlane16_swap(x, y, false, false);
+  x = r[0];
+  y = r[1];
+}
+
+// Two blocks of 16 columns of a row, four a lane: lanes of groups 0 and 2 get 8 of the first's, of 1 and 3 of the second's,
+// so that a store writes 64 consecutive bytes of 16 rows.  c: the first block's column.
+HILO_DEV void store_blocks(uint16_t *row, int c, int end, int lg, f32x4 a, f32x4 b, bool inside) {
+  uint32_t x0 = bf16_pair(a[0], a[1]), x1 = bf16_pair(a[2], a[3]), y0 = bf16_pair(b[0], b[1]), y1 = bf16_pair(b[2], b[3]);
+  swap16(x0, y0);
+  swap16(x1, y1);
+  c += 16 * (lg & 1) + 8 * (lg >> 1);
+  if (inside && c < end) *reinterpret_cast<uint4 *>(row + c) = make_uint4(x0, x1, y0, y1);
+}
+HILO_DEV void store_block(uint16_t *row, int c, int end, int lg, f32x4 a, bool inside) {
+  c += 4 * lg;
+  if (inside && c < end) *reinterpret_cast<uint2 *>(row + c) = make_uint2(bf16_pair(a[0], a[1]), bf16_pair(a[2], a[3]));
+}
+
+// Biases of a wave's columns, four a lane of every block.
+template <typename G>
+struct Bias {
+  uint2 v[G::NB];
+  HILO_DEV void load(const ProductProblem &p, const Place &z, int wn, int lg) {
+#pragma unroll
+    for (int j = 0; j < G::NB; ++j) {
+      const int part = G::GATED ? j / (G::NB / 2) : 0, jj = G::GATED ? j % (G::NB / 2) : j;
+      const void *b = z.stream ? (part ? p.bias[1][1] : p.bias[1][0]) : (part ? p.bias[0][1] : p.bias[0][0]);
+      const int n = min(z.n0 + wn * (G::COLS / 4) + 16 * jj + 4 * lg, p.N - 4);
+      v[j] = b ? *reinterpret_cast<const uint2 *>(reinterpret_cast<const uint16_t *>(b) + n) : make_uint2(0u, 0u);
+    }
+  }
+  HILO_DEV f32x4 of(int j) const {
+    return f32x4{__uint_as_float(v[j].x << 16), __uint_as_float(v[j].x & 0xffff0000u), __uint_as_float(v[j].y << 16),
+                 __uint_as_float(v[j].y & 0xffff0000u)};
+  }
+};
+
+// The last step of a row block: row 16 i + lr of the wave's rows, columns 16 j + 4 lg .. + 3 of block j.
+template <typename G>
+HILO_DEV void finish_row(const ProductProblem &p, const Place &z, const Bias<G> &bias, int wid, int i, int lane, f32x4 (&acc)[G::NB]) {
+  const int lr = lane & 15, lg = lane >> 4, wn = wid & 3;
+  const int rl = (wid >> 2) * (G::BM / 2) + 16 * i + lr;
+  const bool in = rl < z.rows;
+  const size_t row = size_t(z.row0) + rl;
+  const int n = z.n0 + wn * (G::COLS / 4), end = G::KIND == PRODUCT_OUT ? p.N : p.K;
+  // blocks J0 .. J0 + COUNT - 1
+  auto put = [&](uint16_t *r, auto first, auto count) __attribute__((always_inline)) {
+    constexpr int J0 = decltype(first)::value, COUNT = decltype(count)::value;
+#pragma unroll
+    for (int j = 0; j + 1 < COUNT; j += 2) store_blocks(r, n + 16 * j, end, lg, acc[J0 + j], acc[J0 + j + 1], in);
+    if constexpr (COUNT % 2 == 1) store_block(r, n + 16 * (COUNT - 1), end, lg, acc[J0 + COUNT - 1], in);
+  };
+  if constexpr (G::KIND == PRODUCT_OUT) {
+#pragma unroll
+    for (int j = 0; j < G::NB; ++j) acc[j] += bias.of(j);
+    if constexpr (G::GATED) {
+      constexpr int H = G::NB / 2;
+      if (p.pre) {
+        uint16_t *pre = reinterpret_cast<uint16_t *>(p.pre) + row * 2 * p.N;
+        put(pre, Int<0>{}, Int<H>{});
+        put(pre + p.N, Int<H>{}, Int<H>{});
+      }
+#pragma unroll
+      for (int j = 0; j < H; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[j][e] = gate_act<false>(acc[j][e], p.silu) * acc[H + j][e];
+      put(reinterpret_cast<uint16_t *>(p.out) + row * p.N, Int<0>{}, Int<H>{});
+    } else {
+      put(reinterpret_cast<uint16_t *>(p.out) + row * p.N, Int<0>{}, Int<G::NB>{});
+    }
+  } else if constexpr (G::KIND == PRODUCT_DX) {
+    put(reinterpret_cast<uint16_t *>(p.dx) + row * p.K, Int<0>{}, Int<G::NB>{});
+  } else {
+    put(reinterpret_cast<uint16_t *>(p.dw[z.o]) + row * p.K, Int<0>{}, Int<G::NB>{});
+  }
+}
+
+// Partial sums in register order.
+template <typename G>
+HILO_DEV size_t part_at(int slot, int wid, int i, int j, int lane) {
+  return size_t(slot) * G::BM * G::BN + ((size_t(wid) * G::MB * G::NB + i * G::NB + j) * 64 + lane) * 4;
+}
+
+template <typename G>
+HILO_DEV void run(const ProductProblem &p, const Plan &q, int pid, uint8_t *lds) {
+  constexpr int BM = G::BM, BN = G::BN, KIND = G::KIND, MB = G::MB, NB = G::NB, LA = G::LA, LB = G::LB, WB = G::WB, S = G::SLOTS;
+  constexpr bool AK = G::AK, BK = G::BK;
+  const int lane = threadIdx.x & 63;
+  const int wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lr = lane & 15, lg = lane >> 4, wm = wid >> 2, wn = wid & 3;
+  // bytes between rows of the operands as they lie in memory
+  const uint32_t lda = 2u * (KIND == PRODUCT_OUT ? p.K : p.parts * p.N), ldb = 2u * p.K;
+
+  // ---- loads: wave wid fills 1 / 8 of either operand's window, LA and LB instructions; offsets into the window's rows
+  uint32_t oa[LA], ob[LB];
+  int ca = 0, cb = 0;  // 16-byte chunk of k of the lane's loads (k last), the same for all of them
+  auto offsets = [&](auto last, auto blk, uint32_t ld, int row_base, uint32_t (&o)[decltype(blk)::value / 64], int &chunk) {
+    constexpr int BLK = decltype(blk)::value;
+#pragma unroll
+    for (int i = 0; i < BLK / 64; ++i) {
+      if constexpr (decltype(last)::value != 0) {
+        const int r = 8 * i + (lane >> 3);  // of the wave's rows; wid * BLK / 8 is a multiple of 16
+        chunk = (lane & 7) ^ ((lane >> 4) & 3);
+        const int c = (lane & 7) ^ ((r >> 1) & 7);
+        o[i] = uint32_t(row_base + r) * ld + 16u * c;
+      } else {
+        const int at = wid * (BLK * 16) + i * 1024 + lane * 16, k = at / (BLK * 2), c = at % (BLK * 2) / 16;
+        const int f = (k & 3) | ((k >> 3) & 1) << 2;
+        o[i] = uint32_t(k) * ld + 16u * (c ^ (2 * f));
+      }
+    }
+  };
+  // with a gate, a wave's columns of W are half the gate's, half the other's: even waves load the gate's rows
+  offsets(Int<AK>{}, Int<BM>{}, lda, wid * (BM / 8), oa, ca);
+  offsets(Int<BK>{}, Int<BN>{}, ldb, G::GATED ? (wid >> 1) * (BN / 8) : wid * (BN / 8), ob, cb);
+
+  int lu = pid, lslot = 0;
+  int lw = 0, lwe = 0;              // windows of the item yet to load
+  int lk = 0, lkn = 0, lpiece = 0;  // k within the piece, the piece's length, which piece
+  const char *la = nullptr, *lb = nullptr;
+  uint32_t ra = 0, rb = 0;          // bytes: rows of the tile (k last), or columns of a row (k first)
+  Place lz{0, 0, 0, 0, 0, 0};
+  bool more = true;
+  auto ld_piece = [&]() __attribute__((always_inline)) {  // bases of piece lpiece
+    if constexpr (KIND == PRODUCT_OUT) {
+      const int part = G::GATED ? wid & 1 : 0;
+      const void *w = lz.stream ? (part ? p.w[1][1] : p.w[1][0]) : (part ? p.w[0][1] : p.w[0][0]);
+      la = reinterpret_cast<const char *>(p.x) + size_t(lz.row0) * lda;
+      lb = reinterpret_cast<const char *>(w) + size_t(lz.n0) * ldb;
+      lkn = p.K;
+      ra = uint32_t(lz.rows - 1) * lda + 2u * p.K;
+      rb = uint32_t(min(G::COLS, p.N - lz.n0) - 1) * ldb + 2u * p.K;
+    } else if constexpr (KIND == PRODUCT_DX) {
+      const void *w = lz.stream ? (lpiece ? p.w[1][1] : p.w[1][0]) : (lpiece ? p.w[0][1] : p.w[0][0]);
+      la = reinterpret_cast<const char *>(p.d) + size_t(lz.row0) * lda + size_t(lpiece) * p.N * 2;
+      lb = reinterpret_cast<const char *>(w) + size_t(lz.n0) * 2;
+      lkn = p.N;
+      ra = uint32_t(lz.rows - 1) * lda + 2u * p.N;
+      rb = 2u * (p.K - lz.n0);
+    } else {
+      const Segment s = segment(p, lpiece);
+      la = reinterpret_cast<const char *>(p.d) + size_t(s.lo) * lda + (size_t(lz.part) * p.N + lz.row0) * 2;
+      lb = reinterpret_cast<const char *>(p.x) + size_t(s.lo) * ldb + size_t(lz.n0) * 2;
+      lkn = s.n;
+      ra = 2u * (p.N - lz.row0);
+      rb = 2u * (p.K - lz.n0);
+    }
+  };
+  auto ld_item = [&]() __attribute__((always_inline)) {  // the next item that has windows
+    while (true) {
+      const Item it = item_at(q, lu);
+      if (!it.valid) {
+        more = false;
+        return;
+      }
+      lu += P;
+      lz = place_of<G>(p, q, it.t);
+      const int n = windows<KIND>(p, lz.stream);
+      lw = int((long long)n * it.pc / it.n);
+      lwe = int((long long)n * (it.pc + 1) / it.n);
+      if (lw == lwe) continue;
+      int w = lw;  // windows before it within its piece
+      if constexpr (KIND == PRODUCT_OUT) {
+        lpiece = 0;
+      } else if constexpr (KIND == PRODUCT_DX) {
+        const int per = (p.N + 63) / 64;
+        lpiece = w / per;
+        w -= lpiece * per;
+      } else {
+        lpiece = p.merged ? 0 : lz.stream;
+        int n1 = (segment(p, lpiece).n + 63) / 64;
+        while (w >= n1) {
+          w -= n1;
+          lpiece += 2;
+          n1 = (segment(p, lpiece).n + 63) / 64;
+        }
+      }
+      ld_piece();
+      lk = 64 * w;
+      return;
+    }
+  };
+  // the next window: to the next piece or item where this one ends
+  auto ld_step = [&]() __attribute__((always_inline)) {
+    if (!more) return;
+    if (lw == lwe) {
+      ld_item();
+    } else if (KIND != PRODUCT_OUT && lk >= lkn) {
+      if constexpr (KIND == PRODUCT_DX) {
+        ++lpiece;
+        ld_piece();
+      } else {
+        do {
+          lpiece += 2;
+          ld_piece();
+        } while (lkn <= 0);
+      }
+      lk = 0;
+    }
+  };
+  auto ld_operand = [&](auto last, auto blk, const char *base, uint32_t reach, uint32_t ld, const uint32_t (&o)[decltype(blk)::value / 64],
+                        int chunk, uint8_t *d) __attribute__((always_inline)) {
+    constexpr int BLK = decltype(blk)::value;
+    const int kv = min(64, lkn - lk);
+    uint32_t bytes;
+    if constexpr (decltype(last)::value != 0) {
+      bytes = reach - 2u * uint32_t(lk);
+      base += size_t(lk) * 2;
+    } else {
+      bytes = uint32_t(kv - 1) * ld + reach;
+      base += size_t(lk) * ld;
+    }
+    if (!more) bytes = 0;
+    if (decltype(last)::value != 0 && kv < 64) {
+      // chunks of k behind the end: offsets behind the buffer's
+#pragma unroll
+      for (int i = 0; i < BLK / 64; ++i) {
+        const int c = (lane & 7) ^ (((8 * i + (lane >> 3)) >> 1) & 7);
+        buffer_to_lds(base, bytes, 8 * c < kv ? o[i] : kBehind, d + i * 1024);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < BLK / 64; ++i) buffer_to_lds(base, bytes, o[i], d + i * 1024);
+    }
+  };
+  auto ld_a = [&]() __attribute__((always_inline)) {
+    ld_operand(Int<AK>{}, Int<BM>{}, la, ra, lda, oa, ca, lds + lslot * WB + wid * (BM * 16));
+  };
+  auto ld_b = [&]() __attribute__((always_inline)) {
+    ld_operand(Int<BK>{}, Int<BN>{}, lb, rb, ldb, ob, cb, lds + lslot * WB + BM * 128 + wid * (BN * 16));
+    lk += 64;
+    ++lw;
+    lslot = lslot == S - 1 ? 0 : lslot + 1;
+  };
+
+  // ---- fragments
+  const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
+  const int f = (lr >> 2) | (lg & 1) << 2;
+  uint32_t fa[2], fb[2];  // k last: of either half; k first: [0]
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const uint32_t chunk = uint32_t((4 * h + lg) ^ ((lr >> 1) & 7)) * 16;
+    fa[h] = lds0 + (AK ? (wm * (BM / 2) + lr) * 128 + chunk : (8 * lg + (lr >> 2)) * (BM * 2) + 8 * (lr & 3) + (f << 5));
+    fb[h] = lds0 + BM * 128 + (BK ? (wn * (BN / 4) + lr) * 128 + chunk : (8 * lg + (lr >> 2)) * (BN * 2) + 8 * (lr & 3) + (f << 5));
+  }
+  f32x4 acc[MB][NB];
+  Frag<AK> a[2][MB];
+  Frag<BK> b[2][NB];
+  uint32_t so = 0;  // byte offset of the window being read
+  // read x of set h: W's fragments first
+  auto rd = [&](auto hh, auto xx) __attribute__((always_inline)) {
+    constexpr int h = decltype(hh)::value, x = decltype(xx)::value;
+    if constexpr (x < NB) {
+      if constexpr (BK) {
+        read16<x * 2048>(b[h][x].v, fb[h] + so);
+      } else {
+        const uint32_t at = (fb[0] + so) ^ uint32_t((wn * NB + x) << 5);
+        read_tr<h * 32 * BN * 2>(b[h][x].lo, at);
+        read_tr<(h * 32 + 4) * BN * 2>(b[h][x].hi, at);
+      }
+    } else if constexpr (x < NB + MB) {
+      constexpr int i = x - NB;
+      if constexpr (AK) {
+        read16<i * 2048>(a[h][i].v, fa[h] + so);
+      } else {
+        const uint32_t at = (fa[0] + so) ^ uint32_t((wm * MB + i) << 5);
+        read_tr<h * 32 * BM * 2>(a[h][i].lo, at);
+        read_tr<(h * 32 + 4) * BM * 2>(a[h][i].hi, at);
+      }
+    }
+  };
+  auto rd_wait = [&](auto hh) __attribute__((always_inline)) {
+    constexpr int h = decltype(hh)::value;
+    __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0), in the form the compiler's own wait tracking sees
+#pragma unroll
+    for (int i = 0; i < MB; ++i) a[h][i].pin();
+#pragma unroll
+    for (int j = 0; j < NB; ++j) b[h][j].pin();
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  auto rd_all = [&](auto hh) __attribute__((always_inline)) {
+    auto r4 = [&](auto x) __attribute__((always_inline)) {
+      constexpr int x0 = decltype(x)::value;
+      rd(hh, Int<x0>{}); rd(hh, Int<x0 + 1>{}); rd(hh, Int<x0 + 2>{}); rd(hh, Int<x0 + 3>{});
+    };
+    static_assert(MB + NB <= 12, "reads of a set");
+    r4(Int<0>{}); r4(Int<4>{}); r4(Int<8>{});
+    rd_wait(hh);
+  };
+  // the MFMAs of set h, row by row; after each row but the last a share of the reads of the other set; with ld the loads of a window
+  auto half = [&](auto hh, auto ldd) __attribute__((always_inline)) {
+    constexpr int h = decltype(hh)::value;
+    constexpr int RPB = (NB + MB + MB - 2) / (MB - 1);
+    auto row = [&](auto ii) __attribute__((always_inline)) {
+      constexpr int i = decltype(ii)::value;
+      if constexpr (i < MB) {
+#pragma unroll
+        for (int j = 0; j < NB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[h][j].get(), a[h][i].get(), acc[i][j], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (i < MB - 1) {
+          static_assert(RPB <= 3, "reads per row");
+          rd(Int<1 - h>{}, Int<i * RPB>{});
+          if constexpr (RPB > 1) rd(Int<1 - h>{}, Int<i * RPB + 1>{});
+          if constexpr (RPB > 2) rd(Int<1 - h>{}, Int<i * RPB + 2>{});
+        }
+        if constexpr (decltype(ldd)::value != 0) {
+          if constexpr (i == 0) ld_a();
+          if constexpr (i == MB / 2) ld_b();
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    };
+    row(Int<0>{}); row(Int<1>{}); row(Int<2>{}); row(Int<3>{});
+    row(Int<4>{}); row(Int<5>{}); row(Int<6>{}); row(Int<7>{});
+  };
+  // this wave has read the window, and all but the last issued windows have landed; on to the next
+  auto next_window = [&]() __attribute__((always_inline)) {
+    wait_vm<(S - 2) * (LA + LB)>();
+    asm volatile("s_barrier" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    so = so == (S - 1) * WB ? 0 : so + WB;
+    ld_step();
+  };
+
+#pragma unroll 1
+  for (int w = 0; w < S; ++w) {
+    ld_step();
+    ld_a();
+    ld_b();
+  }
+  wait_vm<(S - 1) * (LA + LB)>();
+  asm volatile("s_barrier" ::: "memory");
+  for (int u = pid;; u += P) {
+    const Item it = item_at(q, u);
+    if (!it.valid) break;
+    const Place z = place_of<G>(p, q, it.t);
+    const int n = windows<KIND>(p, z.stream);
+    const int w0 = int((long long)n * it.pc / it.n), w1 = int((long long)n * (it.pc + 1) / it.n);
+#pragma unroll
+    for (int i = 0; i < MB; ++i)
+#pragma unroll
+      for (int j = 0; j < NB; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    rd_all(Int<0>{});
+#pragma unroll 1
+    for (int w = w0; w < w1; ++w) {
+      half(Int<0>{}, Int<0>{});
+      rd_wait(Int<1>{});
+      next_window();
+      half(Int<1>{}, Int<1>{});
+      rd_wait(Int<0>{});
+    }
+    const int lane = opaque(threadIdx.x & 63);
+    if (it.n > 1) {
+#pragma unroll
+      for (int i = 0; i < MB; ++i)
+#pragma unroll
+        for (int j = 0; j < NB; ++j) *reinterpret_cast<f32x4 *>(p.part + part_at<G>(it.slot, wid, i, j, lane)) = acc[i][j];
+    } else {
+      Bias<G> bias;
+      if constexpr (KIND == PRODUCT_OUT) bias.load(p, z, wn, lane >> 4);
+#pragma unroll
+      for (int i = 0; i < MB; ++i) {
+        finish_row<G>(p, z, bias, wid, i, lane, acc[i]);
+        asm volatile("" ::: "memory");
+      }
+    }
+  }
+  wait_vm<0>();
+}
+
+// A wave of the fixup adds one row block of one wave's part of a cut tile, pieces in order.
+template <typename G>
+HILO_DEV void fix(const ProductProblem &p, const Plan &q) {
+  if (q.s == 1) return;
+  const int lane = threadIdx.x & 63;
+  const int items = q.tail * 8 * G::MB;
+  for (int x = blockIdx.x * 8 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); x < items; x += gridDim.x * 8) {
+    const int v = x / (8 * G::MB), rem = x - v * 8 * G::MB, wid = rem / G::MB, i = rem - wid * G::MB;
+    const Place z = place_of<G>(p, q, q.full + v);
+    Bias<G> bias;
+    if constexpr (G::KIND == PRODUCT_OUT) bias.load(p, z, wid & 3, lane >> 4);
+    f32x4 acc[G::NB];
+#pragma unroll
+    for (int j = 0; j < G::NB; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int pc = 0; pc < q.s; ++pc)
+#pragma unroll
+      for (int j = 0; j < G::NB; ++j)
+        acc[j] += *reinterpret_cast<const f32x4 *>(p.part + part_at<G>(pc * q.tail + v, wid, i, j, lane));
+    finish_row<G>(p, z, bias, wid, i, lane, acc);
+  }
+}
+
+constexpr Cost kCost256{146, 700, 2500}, kCost128{46, 400, 1500};
+
+// The plan of either tile and whether the larger one is taken; the main kernel and the fixup find the same.
+template <int KIND, bool GATED>
+HILO_DEV bool choose(const ProductProblem &p, Plan &q) {
+  int nk = windows<KIND>(p, 0), r256, r128;
+  if constexpr (KIND == PRODUCT_DW) {
+    if (!p.merged) nk = max(nk, windows<KIND>(p, 1));
+    r256 = p.outs * ((p.N + 255) / 256);
+    r128 = p.outs * ((p.N + 127) / 128);
+  } else {
+    r256 = count_row_tiles(p, 256);
+    r128 = count_row_tiles(p, 128);
+  }
+  using G256 = Geo<256, 256, KIND, GATED>;
+  using G128 = Geo<128, 128, KIND, GATED>;
+  const Plan a = make_plan<G256>(p, r256, nk, kCost256), b = make_plan<G128>(p, r128, nk, kCost128);
+  const bool large = plan_cost(a.T, nk, kCost256) <= plan_cost(b.T, nk, kCost128);
+  q = large ? a : b;
+  return large;
+}
+
+template <int KIND, bool GATED>
+__global__ __launch_bounds__(512, 2) void k_product_tiles(ProductProblem p) {
+  using G256 = Geo<256, 256, KIND, GATED>;
+  using G128 = Geo<128, 128, KIND, GATED>;
+  constexpr int L0 = G256::WB * G256::SLOTS, L1 = G128::WB * G128::SLOTS;
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[L0 > L1 ? L0 : L1];
+  const int pid = xcd_remap(blockIdx.x, P);
+  Plan q;
+  if (choose<KIND, GATED>(p, q)) run<G256>(p, q, pid, lds);
+  else run<G128>(p, q, pid, lds);
+}
+
+template <int KIND, bool GATED>
+__global__ __launch_bounds__(512) void k_product_fix(ProductProblem p) {
+  Plan q;
+  if (choose<KIND, GATED>(p, q)) fix<Geo<256, 256, KIND, GATED>>(p, q);
+  else fix<Geo<128, 128, KIND, GATED>>(p, q);
+}
+
+}  // namespace pt
+
+size_t product_tiles_part_bytes() { return size_t(pt::P) * 256 * 256 * sizeof(float); }
+
+template <int KIND, bool GATED>
+static hipError_t run_tiles(const ProductProblem &p, hipStream_t st) {
+  hipLaunchKernelGGL((pt::k_product_tiles<KIND, GATED>), dim3(pt::P), dim3(512), 0, st, p);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((pt::k_product_fix<KIND, GATED>), dim3(pt::P), dim3(512), 0, st, p);
+  return hipGetLastError();
+}
+
+hipError_t launch_product_tiles(int kind, const ProductProblem &p, hipStream_t st) {
+  if (kind == PRODUCT_OUT) return p.parts == 2 ? run_tiles<PRODUCT_OUT, true>(p, st) : run_tiles<PRODUCT_OUT, false>(p, st);
+  if (kind == PRODUCT_DX) return run_tiles<PRODUCT_DX, false>(p, st);
+  return run_tiles<PRODUCT_DW, false>(p, st);
+}
+
+}  // namespace hilo
