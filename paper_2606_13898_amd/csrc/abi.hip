@@ -1040,16 +1040,15 @@ BackwardLayout backward_layout(bool bf16, int64_t rows, int K, int N, int batch,
   return l;
 }
 
-// FP8 workspace: codes and scales of float rows, float32 rows that leave as codes, partial products.
+// FP8 workspace: codes and scales of float rows, partial products.
 struct Fp8Layout {
-  size_t scale, out, part, total;
+  size_t scale, part, total;
 };
 Fp8Layout fp8_layout(int64_t rows, int K, int N, bool gated) {
   Fp8Layout l;
   l.scale = align256(size_t(rows) * K);
-  l.out = l.scale + align256(size_t(rows) * scale_stride(K));
-  l.part = l.out + (gated ? align256(size_t(rows) * N * sizeof(float)) : 0);
-  l.total = l.part + align256(product_fp8_part_bytes(rows, K, N, gated ? 2 : 1)) + 256;
+  l.part = l.scale + align256(size_t(rows) * scale_stride(K));
+  l.total = l.part + align256(product_fp8_part_bytes(rows, K, N, gated ? 2 : 1));
   return l;
 }
 
@@ -1090,7 +1089,6 @@ hilo_status hilo_linear(int32_t dtype, const hilo_linear_w w[2], const void *x, 
   p.parts = gated ? 2 : 1;
   p.silu = act == HILO_ACT_SILU;
   p.bf16 = dtype == HILO_BF16;
-  p.out_bf16 = p.bf16;
   p.x = x; p.out = out; p.pre = pre;
   p.merged = streams == 1 || (w[0].w == w[1].w && w[0].b == w[1].b && (!gated || (w[0].w_gate == w[1].w_gate && w[0].b_gate == w[1].b_gate)));
   for (int k = 0; k < 2; ++k) {
@@ -1262,9 +1260,8 @@ hilo_status hilo_linear_fp8(int32_t dtype, const hilo_linear_w_fp8 w[2], const v
   p.parts = gated ? 2 : 1;
   p.silu = act == HILO_ACT_SILU;
   p.bf16 = dtype == HILO_BF16;
-  p.out_bf16 = !out_scale && p.bf16;
   p.x = x; p.x_scale = x_scale;
-  p.out = out_scale ? ws + l.out : out;
+  p.out = out; p.out_scale = out_scale;
   p.merged = streams == 1;
   for (int k = 0; k < 2; ++k) {
     const hilo_linear_w_fp8 &v = w[k < streams ? k : 0];
@@ -1290,12 +1287,7 @@ hilo_status hilo_linear_fp8(int32_t dtype, const hilo_linear_w_fp8 w[2], const v
     p.x_scale = reinterpret_cast<const uint8_t *>(ws + l.scale);
   }
   p.part = reinterpret_cast<float *>(ws + l.part);
-  hipError_t he = timed(K_LINEAR_FP8, st, [&] { return launch_product_fp8(p, st); });
-  if (he == hipSuccess && out_scale)
-    he = timed(K_QUANT_BLOCKS, st, [&] {
-      return launch_quantize_blocks(false, p.out, int(rows), out_dim, 1, cu_seqlens + batch, reinterpret_cast<uint8_t *>(out), out_scale, st);
-    });
-  return dev_status(he);
+  return dev_status(timed(K_LINEAR_FP8, st, [&] { return launch_product_fp8(p, st); }));
 }
 
 hilo_status hilo_profile_enable(int32_t on) {

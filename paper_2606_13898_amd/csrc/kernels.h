@@ -209,8 +209,7 @@ struct ProductProblem {
   int merged;            // all rows are one segment of stream 0 (no text, or the same weights for both streams)
   int K, N, parts;       // in_dim, out_dim, 1 or 2
   int silu;              // the gate's activation: SiLU, or GELU
-  int bf16;              // type of x, pre, biases, gradients
-  int out_bf16;          // of out
+  int bf16;              // type of x, out, pre, biases, gradients
   const void *x;         // [rows][K]
   const void *w[2][2];   // [stream][part]: [N][K]
   const void *bias[2][2];  // [stream][part]: [N] or null
@@ -239,6 +238,8 @@ hipError_t launch_product_fp8(ProductProblem p, hipStream_t st);
 // bf16 on large tiles (product_bf16.hip), with partial tiles in p.part.
 size_t product_tiles_part_bytes();
 hipError_t launch_product_tiles(int kind, const ProductProblem &p, hipStream_t st);
+// FP8 on large tiles (product_fp8.hip): out bf16 or codes.
+hipError_t launch_product_fp8_tiles(const ProductProblem &p, hipStream_t st);
 
 // The step between: dpre [rows][2][N] from dout and pre (gated), and the sums over rows of dpre, or of dout, by stream
 // into db[stream][part] (any null; the two streams' the same: sums over both).

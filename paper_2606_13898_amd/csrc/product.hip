@@ -296,10 +296,6 @@ size_t product_part_bytes(bool bf16, int kind, long long rows, int K, int N, int
   }
   return most;
 }
-size_t product_fp8_part_bytes(long long rows, int K, int N, int parts) {
-  return product_part_bytes(false, PRODUCT_OUT, rows, K, N, parts);
-}
-
 template <int TYPE, int KIND, bool GATED>
 static hipError_t run(ProductProblem &p, hipStream_t st) {
   p.splits = splits_of(KIND, p.rows, p.K, p.N, p.parts, p.outs, p.B, p.merged);
@@ -328,7 +324,13 @@ hipError_t launch_product(int kind, ProductProblem p, hipStream_t st) {
   return p.bf16 ? launch_product_tiles(kind, p, st) : run_kind<TYPE_F32>(kind, p, st);
 }
 
+// Float32 outputs want float32 sums of the codes' products; the tiles' matrix instruction has not the bits for that.
+static bool fp8_tiles(const ProductProblem &p) { return p.bf16 || p.out_scale; }
+size_t product_fp8_part_bytes(long long rows, int K, int N, int parts) {
+  return std::max(product_tiles_part_bytes(), product_part_bytes(false, PRODUCT_OUT, rows, K, N, parts));
+}
 hipError_t launch_product_fp8(ProductProblem p, hipStream_t st) {
+  if (fp8_tiles(p)) return launch_product_fp8_tiles(p, st);
   return p.parts == 2 ? run<TYPE_FP8, PRODUCT_OUT, true>(p, st) : run<TYPE_FP8, PRODUCT_OUT, false>(p, st);
 }
 

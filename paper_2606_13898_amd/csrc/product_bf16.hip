@@ -13,16 +13,10 @@
 // What lies behind the last row, column or k is never read: the loads' buffer ends there, and they leave zeros.
 #include <algorithm>
 
-#include "product.h"
+#include "product_tiles.h"
 
 namespace hilo {
-
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-
 namespace pt {
-
-constexpr int P = kGemmWorkgroups;
 
 template <int BM_, int BN_, int KIND_, bool GATED_>
 struct Geo {
@@ -36,98 +30,6 @@ struct Geo {
   static constexpr int COLS = GATED ? BN / 2 : BN;  // columns of the output
 };
 
-// Tiles in groups of 8 row tiles by all column tiles, row tile fastest: the 32 workgroups of an XCD then share 8 + 4 slices
-// of the operands.
-HILO_DEV void tile_at(int R, int TN, int t, int &r, int &c) {
-  const int grp = t / (8 * TN), in = t - grp * 8 * TN, gm = min(8, R - grp * 8);
-  c = in / gm;
-  r = grp * 8 + in - c * gm;
-}
-
-// Tiles run whole, P at a time; what is left over for a last turn is cut along k into s pieces each, as many as there are
-// workgroups for, where that is quicker than a whole turn.  Pieces leave float32 tiles that k_product_fix adds up.
-struct Plan {
-  int R, TN, T, full, tail, s;
-};
-struct Item {
-  int t, pc, n, slot;  // tile, piece of n, slot of its partial sums (n > 1)
-  bool valid;
-};
-HILO_DEV Item item_at(const Plan &q, int u) {
-  if (u < q.full) return Item{u, 0, 1, 0, true};
-  const int v = u - q.full;
-  if (v >= q.tail * q.s) return Item{0, 0, 1, 0, false};
-  const int pc = v / q.tail;
-  return Item{q.full + v - pc * q.tail, pc, q.s, v, true};
-}
-
-// In units of 10 ns: a window of 64 and a tile's rest, and what pieces of the last turn cost beside their windows.
-struct Cost {
-  int window, tile, fix;
-};
-HILO_DEV int plan_tail(int tail, int nk, Cost c) {
-  if (tail == 0) return 1;
-  const int s = min(P / tail, nk / 4);
-  return s > 1 && nk * c.window > nk * c.window / s + c.fix ? s : 1;
-}
-HILO_DEV int plan_cost(int T, int nk, Cost c) {
-  const int tail = T % P, s = plan_tail(tail, nk, c);
-  return T / P * (nk * c.window + c.tile) + (tail ? nk * c.window / s + c.tile + (s > 1 ? c.fix : 0) : 0);
-}
-template <typename G>
-HILO_DEV Plan make_plan(const ProductProblem &p, int R, int nk, Cost c) {
-  Plan q;
-  q.R = R;
-  q.TN = ((G::KIND == PRODUCT_OUT ? p.N : p.K) + G::COLS - 1) / G::COLS;
-  q.T = q.R * q.TN;
-  q.tail = q.T % P;
-  q.full = q.T - q.tail;
-  q.s = plan_tail(q.tail, nk, c);
-  return q;
-}
-
-// Where a tile lies: rows row0 .. + rows of the output (DW: of output o), columns from n0, stream, and for the backward
-// products the part.
-struct Place {
-  int row0, rows, n0, stream, part, o;
-};
-template <typename G>
-HILO_DEV Place place_of(const ProductProblem &p, const Plan &q, int t) {
-  int r, c;
-  Place z;
-  if constexpr (G::KIND == PRODUCT_DW) {
-    const int per = q.R / p.outs * q.TN;  // R: the row tiles of all outputs
-    z.o = t / per;
-    tile_at(q.R / p.outs, q.TN, t - z.o * per, r, c);
-    z.stream = p.out_stream[z.o];
-    z.part = p.out_part[z.o];
-    z.row0 = r * G::BM;
-    z.rows = min(G::BM, p.N - z.row0);
-  } else {
-    tile_at(q.R, q.TN, t, r, c);
-    z.o = z.part = 0;
-    RowTile rt{0, 0, 0};
-    if (p.merged || p.B > 32) {
-      rt = find_row_tile(p, G::BM, r);
-    } else {  // few samples: by scalar loads, which wait for no load of a tile
-      for (int i = 0; i < 2 * p.B; ++i) {
-        const Segment s = segment(p, i);
-        const int tiles = (s.n + G::BM - 1) / G::BM;
-        if (r < tiles) {
-          rt = RowTile{s.lo + r * G::BM, min(G::BM, s.n - r * G::BM), s.stream};
-          break;
-        }
-        r -= tiles;
-      }
-    }
-    z.row0 = rt.row0;
-    z.rows = rt.n;
-    z.stream = rt.stream;
-  }
-  z.n0 = c * G::COLS;
-  return Place{uni(z.row0), uni(z.rows), uni(z.n0), uni(z.stream), uni(z.part), uni(z.o)};
-}
-
 // Windows of a tile's sum; of a stream's segments in DW.
 template <int KIND>
 HILO_DEV int windows(const ProductProblem &p, int stream) {
@@ -138,25 +40,6 @@ HILO_DEV int windows(const ProductProblem &p, int stream) {
   return n;
 }
 
-// One 16-byte load per lane straight to LDS, zeros where the offset lies behind the buffer's end: lane l's bytes land at
-// 16 l of the wave's 1 KiB.
-HILO_DEV void buffer_to_lds(const char *base, uint32_t bytes, uint32_t offset, void *lds_wave_base) {
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(
-      __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(base), 0, int(bytes), 0x00020000),
-      (__attribute__((address_space(3))) void *)lds_wave_base, 16, int(offset), 0, 0, 0);
-}
-constexpr uint32_t kBehind = 0xffffff00u;  // an offset behind any buffer's end
-
-template <int N>
-HILO_DEV void wait_vm() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
-template <int V>
-struct Int {
-  static constexpr int value = V;
-};
-template <int OFF>
-HILO_DEV void read16(u32x4 &d, uint32_t addr) {
-  asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(d) : "v"(addr), "n"(OFF) : "memory");
-}
 template <int OFF>
 HILO_DEV void read_tr(u32x2 &d, uint32_t addr) {
   asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(d) : "v"(addr), "n"(OFF) : "memory");
@@ -275,14 +158,12 @@ HILO_DEV void run(const ProductProblem &p, const Plan &q, int pid, uint8_t *lds)
 
   // ---- loads: wave wid fills 1 / 8 of either operand's window, LA and LB instructions; offsets into the window's rows
   uint32_t oa[LA], ob[LB];
-  int ca = 0, cb = 0;  // 16-byte chunk of k of the lane's loads (k last), the same for all of them
-  auto offsets = [&](auto last, auto blk, uint32_t ld, int row_base, uint32_t (&o)[decltype(blk)::value / 64], int &chunk) {
+  auto offsets = [&](auto last, auto blk, uint32_t ld, int row_base, uint32_t (&o)[decltype(blk)::value / 64]) {
     constexpr int BLK = decltype(blk)::value;
 #pragma unroll
     for (int i = 0; i < BLK / 64; ++i) {
       if constexpr (decltype(last)::value != 0) {
         const int r = 8 * i + (lane >> 3);  // of the wave's rows; wid * BLK / 8 is a multiple of 16
-        chunk = (lane & 7) ^ ((lane >> 4) & 3);
         const int c = (lane & 7) ^ ((r >> 1) & 7);
         o[i] = uint32_t(row_base + r) * ld + 16u * c;
       } else {
@@ -293,8 +174,8 @@ HILO_DEV void run(const ProductProblem &p, const Plan &q, int pid, uint8_t *lds)
     }
   };
   // with a gate, a wave's columns of W are half the gate's, half the other's: even waves load the gate's rows
-  offsets(Int<AK>{}, Int<BM>{}, lda, wid * (BM / 8), oa, ca);
-  offsets(Int<BK>{}, Int<BN>{}, ldb, G::GATED ? (wid >> 1) * (BN / 8) : wid * (BN / 8), ob, cb);
+  offsets(Int<AK>{}, Int<BM>{}, lda, wid * (BM / 8), oa);
+  offsets(Int<BK>{}, Int<BN>{}, ldb, G::GATED ? (wid >> 1) * (BN / 8) : wid * (BN / 8), ob);
 
   int lu = pid, lslot = 0;
   int lw = 0, lwe = 0;              // windows of the item yet to load
@@ -381,7 +262,7 @@ HILO_DEV void run(const ProductProblem &p, const Plan &q, int pid, uint8_t *lds)
     }
   };
   auto ld_operand = [&](auto last, auto blk, const char *base, uint32_t reach, uint32_t ld, const uint32_t (&o)[decltype(blk)::value / 64],
-                        int chunk, uint8_t *d) __attribute__((always_inline)) {
+                        uint8_t *d) __attribute__((always_inline)) {
     constexpr int BLK = decltype(blk)::value;
     const int kv = min(64, lkn - lk);
     uint32_t bytes;
@@ -393,23 +274,19 @@ HILO_DEV void run(const ProductProblem &p, const Plan &q, int pid, uint8_t *lds)
       base += size_t(lk) * ld;
     }
     if (!more) bytes = 0;
-    if (decltype(last)::value != 0 && kv < 64) {
-      // chunks of k behind the end: offsets behind the buffer's
+    // chunks of k behind the end: offsets behind the buffer's.  The chunk of instruction i is that of 0, or its bit 2 the other
+    // way round
+    const int lane = opaque(threadIdx.x & 63), c = (lane & 7) ^ ((lane >> 4) & 3);
+    const bool in[2] = {8 * c < kv, 8 * (c ^ 4) < kv};
 #pragma unroll
-      for (int i = 0; i < BLK / 64; ++i) {
-        const int c = (lane & 7) ^ (((8 * i + (lane >> 3)) >> 1) & 7);
-        buffer_to_lds(base, bytes, 8 * c < kv ? o[i] : kBehind, d + i * 1024);
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < BLK / 64; ++i) buffer_to_lds(base, bytes, o[i], d + i * 1024);
-    }
+    for (int i = 0; i < BLK / 64; ++i)
+      buffer_to_lds(base, bytes, decltype(last)::value == 0 || in[i & 1] ? o[i] : kBehind, d + i * 1024);
   };
   auto ld_a = [&]() __attribute__((always_inline)) {
-    ld_operand(Int<AK>{}, Int<BM>{}, la, ra, lda, oa, ca, lds + lslot * WB + wid * (BM * 16));
+    ld_operand(Int<AK>{}, Int<BM>{}, la, ra, lda, oa, lds + lslot * WB + wid * (BM * 16));
   };
   auto ld_b = [&]() __attribute__((always_inline)) {
-    ld_operand(Int<BK>{}, Int<BN>{}, lb, rb, ldb, ob, cb, lds + lslot * WB + BM * 128 + wid * (BN * 16));
+    ld_operand(Int<BK>{}, Int<BN>{}, lb, rb, ldb, ob, lds + lslot * WB + BM * 128 + wid * (BN * 16));
     lk += 64;
     ++lw;
     lslot = lslot == S - 1 ? 0 : lslot + 1;
@@ -501,7 +378,6 @@ HILO_DEV void run(const ProductProblem &p, const Plan &q, int pid, uint8_t *lds)
     asm volatile("s_barrier" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
     so = so == (S - 1) * WB ? 0 : so + WB;
-    ld_step();
   };
 
 #pragma unroll 1
@@ -525,6 +401,7 @@ HILO_DEV void run(const ProductProblem &p, const Plan &q, int pid, uint8_t *lds)
     rd_all(Int<0>{});
 #pragma unroll 1
     for (int w = w0; w < w1; ++w) {
+      ld_step();  // its branch lies here because MFMAs before a branch are moved behind it
       half(Int<0>{}, Int<0>{});
       rd_wait(Int<1>{});
       next_window();

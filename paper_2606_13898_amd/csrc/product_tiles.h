@@ -1,0 +1,129 @@
+// The schedule of the products on large tiles, bf16 and FP8: whole tiles in turns of a tile a workgroup, the last turn cut along
+// k; where a tile lies; loads to LDS.
+#pragma once
+
+#include "product.h"
+
+namespace hilo {
+
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+namespace pt {
+
+constexpr int P = kGemmWorkgroups;
+
+// Tiles in groups of 8 row tiles by all column tiles, row tile fastest: the 32 workgroups of an XCD then share 8 + 4 slices
+// of the operands.
+HILO_DEV void tile_at(int R, int TN, int t, int &r, int &c) {
+  const int grp = t / (8 * TN), in = t - grp * 8 * TN, gm = min(8, R - grp * 8);
+  c = in / gm;
+  r = grp * 8 + in - c * gm;
+}
+
+// Tiles run whole, P at a time; what is left over for a last turn is cut along k into s pieces each, as many as there are
+// workgroups for, where that is quicker than a whole turn.  Pieces leave float32 tiles that k_product_fix adds up.
+struct Plan {
+  int R, TN, T, full, tail, s;
+};
+struct Item {
+  int t, pc, n, slot;  // tile, piece of n, slot of its partial sums (n > 1)
+  bool valid;
+};
+HILO_DEV Item item_at(const Plan &q, int u) {
+  if (u < q.full) return Item{u, 0, 1, 0, true};
+  const int v = u - q.full;
+  if (v >= q.tail * q.s) return Item{0, 0, 1, 0, false};
+  const int pc = v / q.tail;
+  return Item{q.full + v - pc * q.tail, pc, q.s, v, true};
+}
+
+// In units of 10 ns: a window of 64 and a tile's rest, and what pieces of the last turn cost beside their windows.
+struct Cost {
+  int window, tile, fix;
+};
+HILO_DEV int plan_tail(int tail, int nk, Cost c) {
+  if (tail == 0) return 1;
+  const int s = min(P / tail, nk / 4);
+  return s > 1 && nk * c.window > nk * c.window / s + c.fix ? s : 1;
+}
+HILO_DEV int plan_cost(int T, int nk, Cost c) {
+  const int tail = T % P, s = plan_tail(tail, nk, c);
+  return T / P * (nk * c.window + c.tile) + (tail ? nk * c.window / s + c.tile + (s > 1 ? c.fix : 0) : 0);
+}
+template <typename G>
+HILO_DEV Plan make_plan(const ProductProblem &p, int R, int nk, Cost c) {
+  Plan q;
+  q.R = R;
+  q.TN = ((G::KIND == PRODUCT_OUT ? p.N : p.K) + G::COLS - 1) / G::COLS;
+  q.T = q.R * q.TN;
+  q.tail = q.T % P;
+  q.full = q.T - q.tail;
+  q.s = plan_tail(q.tail, nk, c);
+  return q;
+}
+
+// Where a tile lies: rows row0 .. + rows of the output (DW: of output o), columns from n0, stream, and for the backward
+// products the part.
+struct Place {
+  int row0, rows, n0, stream, part, o;
+};
+template <typename G>
+HILO_DEV Place place_of(const ProductProblem &p, const Plan &q, int t) {
+  int r, c;
+  Place z;
+  if constexpr (G::KIND == PRODUCT_DW) {
+    const int per = q.R / p.outs * q.TN;  // R: the row tiles of all outputs
+    z.o = t / per;
+    tile_at(q.R / p.outs, q.TN, t - z.o * per, r, c);
+    z.stream = p.out_stream[z.o];
+    z.part = p.out_part[z.o];
+    z.row0 = r * G::BM;
+    z.rows = min(G::BM, p.N - z.row0);
+  } else {
+    tile_at(q.R, q.TN, t, r, c);
+    z.o = z.part = 0;
+    RowTile rt{0, 0, 0};
+    if (p.merged || p.B > 32) {
+      rt = find_row_tile(p, G::BM, r);
+    } else {  // few samples: by scalar loads, which wait for no load of a tile
+      for (int i = 0; i < 2 * p.B; ++i) {
+        const Segment s = segment(p, i);
+        const int tiles = (s.n + G::BM - 1) / G::BM;
+        if (r < tiles) {
+          rt = RowTile{s.lo + r * G::BM, min(G::BM, s.n - r * G::BM), s.stream};
+          break;
+        }
+        r -= tiles;
+      }
+    }
+    z.row0 = rt.row0;
+    z.rows = rt.n;
+    z.stream = rt.stream;
+  }
+  z.n0 = c * G::COLS;
+  return Place{uni(z.row0), uni(z.rows), uni(z.n0), uni(z.stream), uni(z.part), uni(z.o)};
+}
+
+// One 16-byte load per lane straight to LDS, zeros where the offset lies behind the buffer's end: lane l's bytes land at
+// 16 l of the wave's 1 KiB.
+HILO_DEV void buffer_to_lds(const char *base, uint32_t bytes, uint32_t offset, void *lds_wave_base) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(
+      __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(base), 0, int(bytes), 0x00020000),
+      (__attribute__((address_space(3))) void *)lds_wave_base, 16, int(offset), 0, 0, 0);
+}
+constexpr uint32_t kBehind = 0x80000000u;  // an offset behind any buffer's end, also with rows of the tile added
+
+template <int N>
+HILO_DEV void wait_vm() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
+template <int V>
+struct Int {
+  static constexpr int value = V;
+};
+template <int OFF>
+HILO_DEV void read16(u32x4 &d, uint32_t addr) {
+  asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(d) : "v"(addr), "n"(OFF) : "memory");
+}
+
+}  // namespace pt
+}  // namespace hilo

@@ -1,8 +1,8 @@
 """The products of a feed-forward against their definitions in float64: forward, gradients, FP8 blocks.
 
-Tolerances.  A float32 sum of K products x w is off by at most (K + 2) 2^-24 sum |x w| in any order; the FP8 matrix
-instruction adds products that it aligns to the largest of a group, each cut by at most a step, 2^-23 of it, so (K + 2) 2^-23.  What
-the activation adds, and how errors of g and u reach the output, is oracle.hilo_products'; the last rounding is half a
+Tolerances.  A float32 sum of K products x w is off by at most (K + 2) 2^-24 sum |x w| in any order, or (K + 2) 2^-23
+where additions cut instead of rounding (the FP8 matrix instruction); what that instruction cuts beside is
+oracle.hilo_products.cut's, for outputs of bf16 and codes (float32 outputs are formed without it).  What the activation adds, and how errors of g and u reach the output, is oracle.hilo_products'; the last rounding is half a
 step: 2^-8 (bf16) or 2^-24 of the value, of codes 2^-4 and half the least step, 2^-10 of the scale."""
 import pytest
 import torch
@@ -209,10 +209,11 @@ def fp8_weights(g, streams, n, k, dt, act, bias):
             if d["b" + part] is not None:
                 d["b" + part] = d["b" + part].to(dt)
     plans = [hilo.quantize_block_weights(**{name: None if v is None else v.cuda() for name, v in d.items()}) for d in ws]
-    for d in ws:
+    exponents = [{} for _ in ws]
+    for d, e in zip(ws, exponents):
         for part in ("", "_gate") if act else ("",):
-            d["w" + part] = P.quantize(d["w" + part].to(F64), 128)[0]
-    return ws, hilo.linear_weights_fp8(plans)
+            d["w" + part], e["w" + part] = P.quantize(d["w" + part].to(F64), 128)
+    return ws, exponents, hilo.linear_weights_fp8(plans)
 
 
 @pytest.mark.parametrize("shape", FP8_SHAPES, ids=case_id)
@@ -224,7 +225,7 @@ def test_fp8(shape, kind, coded):
     cu = pack(images, text)
     x = torch.randn(cu[-1], k, generator=g) * torch.exp2(torch.randint(-3, 4, (1, k), generator=g).float())
     x = x.to(dt)
-    ws, plan = fp8_weights(g, streams, n, k, dt, act, bias)
+    ws, kws, plan = fp8_weights(g, streams, n, k, dt, act, bias)
     T = cu[-1] + BEHIND
     need = hilo.hilo_linear_fp8_workspace_bytes(T, k, n, gated=act is not None)
     ws_dev = torch.empty(need, dtype=torch.uint8, device="cuda").fill_(0xff)
@@ -239,16 +240,20 @@ def test_fp8(shape, kind, coded):
     hilo.hilo_linear_fp8(plan, xin, out, cud, text, act=ACTS[act], workspace=ws_dev, **a)
     torch.cuda.synchronize()
     assert (out[cu[-1]:] == 7.0).all()
-    xq, step = P.quantize(x.to(F64), 1)[0], 2.0 ** -23
+    (xq, kx), step = P.quantize(x.to(F64), 1), 2.0 ** -23
     u, su = P.affine(xq, ws, "", cu, text)
     eu = (k + 2) * step * su
+    cu_, full = P.cut(xq, kx, ws, kws, "", cu, text), dt is torch.float32
+    eu = eu if full else eu + cu_
     if act is None:
         near(out[:cu[-1]], u, eu + HALF[dt] * (u.abs() + eu), "out")
         return
     v, sv = P.affine(xq, ws, "_gate", cu, text)
-    want, off = P.gated(act, v, u, (k + 2) * step * sv, eu, True)
+    ev, cv = (k + 2) * step * sv, P.cut(xq, kx, ws, kws, "_gate", cu, text)
+    want, off = P.gated(act, v, u, ev if full else ev + cv, eu, True)
     near(out[:cu[-1]], want, off + HALF[dt] * (want.abs() + off), "out")
     # codes out: of the float32 values, whose block may just have another scale
+    want, off = P.gated(act, v, u, ev + cv, eu + cu_ if full else eu, True)
     h = torch.full((T, n), 9, dtype=torch.uint8, device="cuda")
     hs = torch.full((T, hilo.scale_stride(n)), 9, dtype=torch.uint8, device="cuda")
     hilo.hilo_linear_fp8(plan, xin, h, cud, text, act=ACTS[act], workspace=ws_dev, out_scale=hs, **a)
