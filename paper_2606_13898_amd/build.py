@@ -17,7 +17,7 @@ BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libhilo.so")
 SOURCES = ["select.hip", "pack.hip", "gemm.hip", "attention.hip", "rope.hip", "norm.hip", "linear.hip",
            "product.hip", "product_bf16.hip", "product_fp8.hip",
-           "abi.hip"]
+           "product_few.hip", "abi.hip"]
 ARCH = "gfx950"
 # Per-source flags.  attention.hip: its maxima see only finite scores and -inf masks, and without
 # NaN semantics fmaxf needs no quieting of each MFMA result before the comparison

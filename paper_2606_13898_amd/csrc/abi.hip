@@ -1277,7 +1277,7 @@ hilo_status hilo_linear_fp8(int32_t dtype, const hilo_linear_w_fp8 w[2], const v
     for (int q = 0; q < 2; ++q)
       p.merged = p.merged && p.w[0][q] == p.w[1][q] && p.w_scale[0][q] == p.w_scale[1][q] && p.bias[0][q] == p.bias[1][q];
   }
-  if (!x_scale) {
+  if (!x_scale && !product_fp8_quantises(p)) {
     const hipError_t he = timed(K_QUANT_BLOCKS, st, [&] {
       return launch_quantize_blocks(p.bf16, x, int(rows), in_dim, 1, cu_seqlens + batch, reinterpret_cast<uint8_t *>(ws),
                                     reinterpret_cast<uint8_t *>(ws + l.scale), st);

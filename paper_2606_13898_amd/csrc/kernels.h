@@ -226,6 +226,7 @@ struct ProductProblem {
   const uint8_t *x_scale;        // [rows][scale_stride(K)] E8M0 bytes
   const uint8_t *w_scale[2][2];  // [ceil(N / 128)][scale_stride(K)]
   uint8_t *out_scale;            // [rows][scale_stride(N)]: out is codes; or null
+  int out_f32;                   // out is float32 whatever the others are
 };
 // Bytes between rows of E8M0 scales: one for each 128 columns, in whole groups of four.
 constexpr int scale_stride(int cols) { return (cols + 511) / 512 * 4; }
@@ -234,10 +235,14 @@ enum ProductKind { PRODUCT_OUT, PRODUCT_DX, PRODUCT_DW };
 size_t product_part_bytes(bool bf16, int kind, long long rows, int K, int N, int parts);
 size_t product_fp8_part_bytes(long long rows, int K, int N, int parts);
 hipError_t launch_product(int kind, ProductProblem p, hipStream_t st);
+bool product_fp8_quantises(const ProductProblem &p);  // x may be bf16 rows without scales
 hipError_t launch_product_fp8(ProductProblem p, hipStream_t st);
 // bf16 on large tiles (product_bf16.hip), with partial tiles in p.part.
 size_t product_tiles_part_bytes();
 hipError_t launch_product_tiles(int kind, const ProductProblem &p, hipStream_t st);
+// At most kProductFewRows rows, bf16 or FP8 (product_few.hip): x bf16 or codes, out bf16, or float32 with out_f32.
+constexpr int kProductFewRows = 64;
+hipError_t launch_product_few(const ProductProblem &p, hipStream_t st);
 // FP8 on large tiles (product_fp8.hip): out bf16 or codes.
 hipError_t launch_product_fp8_tiles(const ProductProblem &p, hipStream_t st);
 

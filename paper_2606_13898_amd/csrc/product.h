@@ -118,7 +118,7 @@ HILO_DEV void finish_out(const ProductProblem &p, int stream, size_t row, int n,
 #pragma unroll
     for (int e = 0; e < 4; ++e) u[e] *= p.bf16 ? gate_act<false>(g[e], p.silu) : gate_act<true>(g[e], p.silu);
   }
-  store4(p.out, row * p.N + n, u, p.bf16);
+  store4(p.out, row * p.N + n, u, p.bf16 && !p.out_f32);
 }
 
 }  // namespace hilo

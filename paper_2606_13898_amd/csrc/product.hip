@@ -287,7 +287,7 @@ static int splits_of(int kind, long long rows, int K, int N, int parts, int outs
 
 // Most partial sums of any call: one segment has the fewest tiles, so the most splits.
 size_t product_part_bytes(bool bf16, int kind, long long rows, int K, int N, int parts) {
-  if (bf16) return product_tiles_part_bytes();
+  if (bf16) return kind == PRODUCT_OUT && rows <= kProductFewRows ? 0 : product_tiles_part_bytes();
   size_t most = 0;
   for (int outs = 1; outs <= (kind == PRODUCT_DW ? 4 : 1); ++outs) {
     const int s = splits_of(kind, rows, K, N, parts, outs, 1, true);
@@ -321,16 +321,28 @@ static hipError_t run_kind(int kind, ProductProblem &p, hipStream_t st) {
 
 hipError_t launch_product(int kind, ProductProblem p, hipStream_t st) {
   if (kind == PRODUCT_DW && p.outs == 0) return hipSuccess;
-  return p.bf16 ? launch_product_tiles(kind, p, st) : run_kind<TYPE_F32>(kind, p, st);
+  if (!p.bf16) return run_kind<TYPE_F32>(kind, p, st);
+  return kind == PRODUCT_OUT && p.rows <= kProductFewRows ? launch_product_few(p, st) : launch_product_tiles(kind, p, st);
 }
 
 // Float32 outputs want float32 sums of the codes' products; the tiles' matrix instruction has not the bits for that.
-static bool fp8_tiles(const ProductProblem &p) { return p.bf16 || p.out_scale; }
 size_t product_fp8_part_bytes(long long rows, int K, int N, int parts) {
-  return std::max(product_tiles_part_bytes(), product_part_bytes(false, PRODUCT_OUT, rows, K, N, parts));
+  const size_t few = rows <= kProductFewRows ? size_t(rows) * N * sizeof(float) : product_tiles_part_bytes();
+  return std::max(few, product_part_bytes(false, PRODUCT_OUT, rows, K, N, parts));
 }
+bool product_fp8_quantises(const ProductProblem &p) { return p.rows <= 16 && p.bf16; }
 hipError_t launch_product_fp8(ProductProblem p, hipStream_t st) {
-  if (fp8_tiles(p)) return launch_product_fp8_tiles(p, st);
+  if (p.rows <= kProductFewRows && (p.bf16 || p.out_scale)) {
+    if (!p.out_scale) return launch_product_few(p, st);
+    // codes: a scale's 128 columns are eight workgroups', so they are formed from float32 rows in a launch of their own
+    void *codes = p.out;
+    p.out = p.part;
+    p.out_f32 = 1;
+    const hipError_t e = launch_product_few(p, st);
+    if (e != hipSuccess) return e;
+    return launch_quantize_blocks(false, p.out, p.rows, p.N, 1, p.cu + p.B, reinterpret_cast<uint8_t *>(codes), p.out_scale, st);
+  }
+  if (p.bf16 || p.out_scale) return launch_product_fp8_tiles(p, st);
   return p.parts == 2 ? run<TYPE_FP8, PRODUCT_OUT, true>(p, st) : run<TYPE_FP8, PRODUCT_OUT, false>(p, st);
 }
 
