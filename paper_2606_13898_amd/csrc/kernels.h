@@ -221,7 +221,7 @@ struct ProductProblem {
   int out_stream[4], out_part[4];
   void *dw[4];           // [N][K]
   float *part;           // partial sums, `splits` times what the product leaves
-  int splits;
+  int splits;            // how many; on large tiles whether the last turn's tiles may be cut
   // FP8: x holds codes, w codes
   const uint8_t *x_scale;        // [rows][scale_stride(K)] E8M0 bytes
   const uint8_t *w_scale[2][2];  // [ceil(N / 128)][scale_stride(K)]
@@ -256,9 +256,10 @@ struct GateBackProblem {
   void *dpre;            // with a gate
   void *db[2][2];        // [stream][part]: [N]
   float *part;           // gate_back_bytes
+  int block_rows;        // set by the launcher
 };
 size_t gate_back_bytes(long long rows, int N, int parts, int B);
-hipError_t launch_gate_back(bool bf16, const GateBackProblem &p, hipStream_t st);
+hipError_t launch_gate_back(bool bf16, GateBackProblem p, hipStream_t st);
 
 // E4M3 codes and E8M0 scales (scale_stride(cols) a row) of x [rows][cols], a scale for each 128 columns of a row, or
 // for block_rows 128 of 128 rows; limit: a device pointer to the number of rows, or null.

@@ -50,6 +50,18 @@ struct Chunk {
   }
 };
 
+template <bool BF16>
+HILO_DEV void store8(void *o, size_t i, const float (&f)[8]) {
+  if constexpr (BF16) {
+    *reinterpret_cast<uint4 *>(reinterpret_cast<uint16_t *>(o) + i) =
+        make_uint4(bf16_pair(f[0], f[1]), bf16_pair(f[2], f[3]), bf16_pair(f[4], f[5]), bf16_pair(f[6], f[7]));
+  } else {
+    float4 *q = reinterpret_cast<float4 *>(reinterpret_cast<float *>(o) + i);
+    q[0] = make_float4(f[0], f[1], f[2], f[3]);
+    q[1] = make_float4(f[4], f[5], f[6], f[7]);
+  }
+}
+
 // The value of an E8M0 byte; 255 stands for NaN.
 HILO_DEV float e8m0(uint8_t b) {
   return b == 255 ? __uint_as_float(0x7fc00000u) : b == 0 ? __uint_as_float(0x00400000u) : __uint_as_float(uint32_t(b) << 23);
@@ -110,8 +122,7 @@ __global__ __launch_bounds__(256) void k_product(ProductProblem p) {
         seg_n = g.n;
       }
     }
-    Chunk<TYPE> a, b;
-    auto load = [&](int s) __attribute__((always_inline)) {
+    auto load = [&](int s, Chunk<TYPE> &a, Chunk<TYPE> &b) __attribute__((always_inline)) {
       a.zero();
       b.zero();
       int k0, kn;  // first k of the step in its piece, and the piece's length
@@ -160,7 +171,7 @@ __global__ __launch_bounds__(256) void k_product(ProductProblem p) {
         }
       }
     };
-    auto store = [&](int buf) __attribute__((always_inline)) {
+    auto store = [&](int buf, const Chunk<TYPE> &a, const Chunk<TYPE> &b) __attribute__((always_inline)) {
       float f[8];
       a.values(f);
 #pragma unroll
@@ -180,14 +191,19 @@ __global__ __launch_bounds__(256) void k_product(ProductProblem p) {
     for (int i = 0; i < 2; ++i)
 #pragma unroll
       for (int j = 0; j < 2; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    // ---- a step is multiplied out of one LDS buffer, the next lies in the other or is on its way there, and kAhead more are on
+    // their way to registers
     if (s0 < s1) {
-      load(s0);
-      store(0);
-      __syncthreads();
-#pragma unroll 1
-      for (int s = s0; s < s1; ++s) {
+      constexpr int kAhead = 3;
+      Chunk<TYPE> a[kAhead], b[kAhead];
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k)
+        if (s0 + k < s1) load(s0 + k, a[k], b[k]);
+      auto step = [&](int s, Chunk<TYPE> &ca, Chunk<TYPE> &cb) __attribute__((always_inline)) {
         const int buf = (s - s0) & 1;
-        if (s + 1 < s1) load(s + 1);
+        store(buf, ca, cb);
+        if (s + kAhead < s1) load(s + kAhead, ca, cb);
+        __syncthreads();
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           float av[2], bv[2];
@@ -201,9 +217,14 @@ __global__ __launch_bounds__(256) void k_product(ProductProblem p) {
 #pragma unroll
             for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(bv[j], av[i], acc[i][j], 0, 0, 0);
         }
-        if (s + 1 < s1) store(buf ^ 1);
-        __syncthreads();
+      };
+#pragma unroll 1
+      for (int s = s0; s < s1; s += kAhead) {
+        step(s, a[0], b[0]);
+        if (s + 1 < s1) step(s + 1, a[1], b[1]);
+        if (s + 2 < s1) step(s + 2, a[2], b[2]);
       }
+      __syncthreads();  // the next item's first step goes to either buffer
     }
     // ---- lane (lr, lg) holds rows 16 i + lr and columns 16 j + 4 lg .. + 3 of its wave's 32 x 32
 #pragma unroll
@@ -348,48 +369,64 @@ hipError_t launch_product_fp8(ProductProblem p, hipStream_t st) {
 
 // ------------------------------------------------------------------------ through the gate, and sums over rows
 //
-// A workgroup has 64 rows of a segment and 512 columns: a wave every fourth row, a lane 8 columns.  What a column's rows
-// sum to goes to part[row tile][parts * N], and k_gate_back_sum adds those of a stream's tiles in their order.
-constexpr int kBackRows = 64, kBackCols = 512;
+// Bound by memory: with a gate five values a column are read or written.  A workgroup has block_rows rows of a segment and
+// 512 columns: a wave every fourth row, a lane 8 columns, four rows on their way.  What a column's rows sum to goes to
+// part[row block][parts][N], and k_gate_back_sum adds those of a stream's blocks in their order.
+constexpr int kBackCols = 512;
+static int back_rows(long long rows) { return rows >= 8192 ? 256 : rows >= 2048 ? 64 : 16; }
 
 template <bool BF16, bool GATED>
 __global__ __launch_bounds__(256) void k_gate_back(GateBackProblem p) {
-  constexpr int PARTS = GATED ? 2 : 1;
+  constexpr int PARTS = GATED ? 2 : 1, TYPE = BF16 ? TYPE_BF16 : TYPE_F32, AHEAD = BF16 ? 4 : 2;
   __shared__ float sums[3][PARTS][8][64];
   const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int tn_count = (p.N + kBackCols - 1) / kBackCols;
-  const long long tiles = (long long)count_row_tiles(p, kBackRows) * tn_count;
+  const long long tiles = (long long)count_row_tiles(p, p.block_rows) * tn_count;
   for (long long t = blockIdx.x; t < tiles; t += gridDim.x) {
     const int tr = int(t / tn_count), n = int(t - (long long)tr * tn_count) * kBackCols + 8 * lane;
-    const RowTile rt = find_row_tile(p, kBackRows, tr);
+    const RowTile rt = find_row_tile(p, p.block_rows, tr);
     float db[PARTS][8];
 #pragma unroll
     for (int q = 0; q < PARTS; ++q)
 #pragma unroll
       for (int e = 0; e < 8; ++e) db[q][e] = 0.f;
     if (n < p.N) {
-      for (int r = wid; r < rt.n; r += 4) {
-        const size_t row = size_t(rt.row0) + r;
+#pragma unroll 1
+      for (int r0 = wid; r0 < rt.n; r0 += 4 * AHEAD) {
+        Chunk<TYPE> d[AHEAD], g[AHEAD], u[AHEAD];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const f32x4 d = load4(p.dout, row * p.N + n + 4 * h, BF16);
+        for (int a = 0; a < AHEAD; ++a) {
+          const size_t row = size_t(rt.row0) + min(r0 + 4 * a, rt.n - 1);  // behind the last row: it again, left out below
+          d[a].load(p.dout, row * p.N + n);
           if constexpr (GATED) {
-            const f32x4 g = load4(p.pre, row * 2 * p.N + n + 4 * h, BF16), u = load4(p.pre, row * 2 * p.N + p.N + n + 4 * h, BF16);
-            f32x4 dg, du;
+            g[a].load(p.pre, row * 2 * p.N + n);
+            u[a].load(p.pre, row * 2 * p.N + p.N + n);
+          }
+        }
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
+        for (int a = 0; a < AHEAD; ++a) {
+          if (r0 + 4 * a >= rt.n) break;
+          float dv[8];
+          d[a].values(dv);
+          if constexpr (GATED) {
+            float gv[8], uv[8];
+            g[a].values(gv);
+            u[a].values(uv);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
               float act, slope;
-              gate_slope<!BF16>(g[e], p.silu, act, slope);
-              dg[e] = d[e] * u[e] * slope;
-              du[e] = d[e] * act;
-              db[0][4 * h + e] += dg[e];
-              db[1][4 * h + e] += du[e];
+              gate_slope<!BF16>(gv[e], p.silu, act, slope);
+              gv[e] = dv[e] * uv[e] * slope;
+              uv[e] = dv[e] * act;
+              db[0][e] += gv[e];
+              db[1][e] += uv[e];
             }
-            store4(p.dpre, row * 2 * p.N + n + 4 * h, dg, BF16);
-            store4(p.dpre, row * 2 * p.N + p.N + n + 4 * h, du, BF16);
+            const size_t at = (size_t(rt.row0) + r0 + 4 * a) * 2 * p.N + n;
+            store8<BF16>(p.dpre, at, gv);
+            store8<BF16>(p.dpre, at + p.N, uv);
           } else {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) db[0][4 * h + e] += d[e];
+            for (int e = 0; e < 8; ++e) db[0][e] += dv[e];
           }
         }
       }
@@ -404,20 +441,21 @@ __global__ __launch_bounds__(256) void k_gate_back(GateBackProblem p) {
       __syncthreads();
       if (wid == 0 && n < p.N) {
 #pragma unroll
-        for (int q = 0; q < PARTS; ++q)
+        for (int q = 0; q < PARTS; ++q) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e)
-            p.part[(size_t(tr) * PARTS + q) * p.N + n + e] = ((db[q][e] + sums[0][q][e][lane]) + sums[1][q][e][lane]) + sums[2][q][e][lane];
+          for (int e = 0; e < 8; ++e) db[q][e] = ((db[q][e] + sums[0][q][e][lane]) + sums[1][q][e][lane]) + sums[2][q][e][lane];
+          store8<false>(p.part, (size_t(tr) * PARTS + q) * p.N + n, db[q]);
+        }
       }
       __syncthreads();
     }
   }
 }
 
-// A workgroup has 64 columns of one sum, a wave a quarter of the row tiles.
+// A workgroup has 64 columns of one sum, a wave every eighth row block, eight on their way.
 template <bool BF16>
-__global__ __launch_bounds__(256) void k_gate_back_sum(GateBackProblem p) {
-  __shared__ float sums[4][64];
+__global__ __launch_bounds__(512) void k_gate_back_sum(GateBackProblem p) {
+  __shared__ float sums[8][64];
   const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int stream = blockIdx.y / p.parts, part = blockIdx.y % p.parts;
   void *db = stream ? p.db[1][part] : p.db[0][part];
@@ -425,43 +463,54 @@ __global__ __launch_bounds__(256) void k_gate_back_sum(GateBackProblem p) {
   if (!db || (both && stream)) return;
   const int n = blockIdx.x * 64 + lane;
   float v = 0.f;
-  int t0 = 0;  // tiles before the segment
+  int t0 = 0;  // blocks before the segment
   for (int i = 0; i < segments(p); ++i) {
     const Segment s = segment(p, i);
-    const int tiles = (s.n + kBackRows - 1) / kBackRows;
+    const int tiles = (s.n + p.block_rows - 1) / p.block_rows;
     if (both || s.stream == stream) {
-      for (int t = wid; t < tiles; t += 4)
-        if (n < p.N) v += p.part[(size_t(t0 + t) * p.parts + part) * p.N + n];
+      const float *from = p.part + (size_t(t0) * p.parts + part) * p.N + min(n, p.N - 1);
+#pragma unroll 1
+      for (int t = wid; t < tiles; t += 64) {
+        float w[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) w[k] = from[size_t(min(t + 8 * k, tiles - 1)) * p.parts * p.N];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v += t + 8 * k < tiles ? w[k] : 0.f;
+      }
     }
     t0 += tiles;
   }
   sums[wid][lane] = v;
   __syncthreads();
   if (wid == 0 && n < p.N) {
-    const float s = (sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]);
+    float s = sums[0][lane];
+#pragma unroll
+    for (int k = 1; k < 8; ++k) s += sums[k][lane];
     if (BF16) reinterpret_cast<uint16_t *>(db)[n] = f2bf(s);
     else reinterpret_cast<float *>(db)[n] = s;
   }
 }
 
 size_t gate_back_bytes(long long rows, int N, int parts, int B) {
-  return (size_t(rows + kBackRows - 1) / kBackRows + 2 * size_t(B)) * parts * N * sizeof(float);
+  const int block = back_rows(rows);
+  return (size_t(rows + block - 1) / block + 2 * size_t(B)) * parts * N * sizeof(float);
 }
 
 template <bool BF16, bool GATED>
 static hipError_t run_gate_back(const GateBackProblem &p, hipStream_t st) {
   if (p.rows > 0 && (GATED || p.part)) {
-    const long long tiles = ((p.rows + kBackRows - 1) / kBackRows + (p.merged ? 0 : 2LL * p.B)) * ((p.N + kBackCols - 1) / kBackCols);
+    const long long tiles = ((p.rows + p.block_rows - 1) / p.block_rows + (p.merged ? 0 : 2LL * p.B)) * ((p.N + kBackCols - 1) / kBackCols);
     hipLaunchKernelGGL((k_gate_back<BF16, GATED>), dim3(unsigned(std::min(tiles, 1ll << 20))), dim3(256), 0, st, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
   if (!p.part) return hipSuccess;
-  hipLaunchKernelGGL((k_gate_back_sum<BF16>), dim3((p.N + 63) / 64, 2 * p.parts), dim3(256), 0, st, p);
+  hipLaunchKernelGGL((k_gate_back_sum<BF16>), dim3((p.N + 63) / 64, 2 * p.parts), dim3(512), 0, st, p);
   return hipGetLastError();
 }
 
-hipError_t launch_gate_back(bool bf16, const GateBackProblem &p, hipStream_t st) {
+hipError_t launch_gate_back(bool bf16, GateBackProblem p, hipStream_t st) {
+  p.block_rows = back_rows(p.rows);
   if (p.parts == 2) return bf16 ? run_gate_back<true, true>(p, st) : run_gate_back<false, true>(p, st);
   return bf16 ? run_gate_back<true, false>(p, st) : run_gate_back<false, false>(p, st);
 }

@@ -1,6 +1,6 @@
 // The bf16 products of a feed-forward and their gradients on large tiles (product.hip has their mathematics).
 //
-// One persistent workgroup of 8 waves a CU (2 x 4, a wave's tile BM / 2 x BN / 4 in 16 x 16 MFMA blocks).  K goes through
+// One persistent workgroup of 8 waves a CU (WM x WN, a wave's tile in 16 x 16 MFMA blocks).  K goes through
 // LDS in windows of 64 values, filled by direct loads to LDS some windows ahead, also of the tiles to come; while the MFMAs of one half of
 // a window run, the fragments of the next half are read.  One barrier a window.
 //
@@ -20,10 +20,11 @@ namespace pt {
 
 template <int BM_, int BN_, int KIND_, bool GATED_>
 struct Geo {
+  static constexpr int WM = BM_ > BN_ ? 4 : 2, WN = 8 / WM;  // waves
   static constexpr int BM = BM_, BN = BN_, KIND = KIND_;
   static constexpr bool GATED = GATED_ && KIND == PRODUCT_OUT;  // two products a tile, half its columns each
   static constexpr bool AK = KIND != PRODUCT_DW, BK = KIND == PRODUCT_OUT;  // k last
-  static constexpr int MB = BM / 32, NB = BN / 64;
+  static constexpr int MB = BM / WM / 16, NB = BN / WN / 16;
   static constexpr int LA = BM / 64, LB = BN / 64;  // load instructions of a wave for a window
   static constexpr int WB = (BM + BN) * 128;
   static constexpr int SLOTS = 3 * WB <= 160 * 1024 ? 3 : 2;
@@ -90,7 +91,7 @@ struct Bias {
     for (int j = 0; j < G::NB; ++j) {
       const int part = G::GATED ? j / (G::NB / 2) : 0, jj = G::GATED ? j % (G::NB / 2) : j;
       const void *b = z.stream ? (part ? p.bias[1][1] : p.bias[1][0]) : (part ? p.bias[0][1] : p.bias[0][0]);
-      const int n = min(z.n0 + wn * (G::COLS / 4) + 16 * jj + 4 * lg, p.N - 4);
+      const int n = min(z.n0 + wn * (G::COLS / G::WN) + 16 * jj + 4 * lg, p.N - 4);
       v[j] = b ? *reinterpret_cast<const uint2 *>(reinterpret_cast<const uint16_t *>(b) + n) : make_uint2(0u, 0u);
     }
   }
@@ -103,11 +104,11 @@ struct Bias {
 // The last step of a row block: row 16 i + lr of the wave's rows, columns 16 j + 4 lg .. + 3 of block j.
 template <typename G>
 HILO_DEV void finish_row(const ProductProblem &p, const Place &z, const Bias<G> &bias, int wid, int i, int lane, f32x4 (&acc)[G::NB]) {
-  const int lr = lane & 15, lg = lane >> 4, wn = wid & 3;
-  const int rl = (wid >> 2) * (G::BM / 2) + 16 * i + lr;
+  const int lr = lane & 15, lg = lane >> 4, wn = wid % G::WN;
+  const int rl = (wid / G::WN) * (G::BM / G::WM) + 16 * i + lr;
   const bool in = rl < z.rows;
   const size_t row = size_t(z.row0) + rl;
-  const int n = z.n0 + wn * (G::COLS / 4), end = G::KIND == PRODUCT_OUT ? p.N : p.K;
+  const int n = z.n0 + wn * (G::COLS / G::WN), end = G::KIND == PRODUCT_OUT ? p.N : p.K;
   // blocks J0 .. J0 + COUNT - 1
   auto put = [&](uint16_t *r, auto first, auto count) __attribute__((always_inline)) {
     constexpr int J0 = decltype(first)::value, COUNT = decltype(count)::value;
@@ -152,7 +153,7 @@ HILO_DEV void run(const ProductProblem &p, const Plan &q, int pid, uint8_t *lds)
   constexpr bool AK = G::AK, BK = G::BK;
   const int lane = threadIdx.x & 63;
   const int wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int lr = lane & 15, lg = lane >> 4, wm = wid >> 2, wn = wid & 3;
+  const int lr = lane & 15, lg = lane >> 4, wm = wid / G::WN, wn = wid % G::WN;
   // bytes between rows of the operands as they lie in memory
   const uint32_t lda = 2u * (KIND == PRODUCT_OUT ? p.K : p.parts * p.N), ldb = 2u * p.K;
 
@@ -173,9 +174,11 @@ HILO_DEV void run(const ProductProblem &p, const Plan &q, int pid, uint8_t *lds)
       }
     }
   };
-  // with a gate, a wave's columns of W are half the gate's, half the other's: even waves load the gate's rows
+  // with a gate, the columns of W of a wave of the product are half the gate's, half the other's; a wave loads rows of one part
+  constexpr int WC = BN / G::WN;
+  const int wgrp = wid * (BN / 8) / WC, win = wid * (BN / 8) % WC, wpart = G::GATED ? win / (WC / 2) : 0;
   offsets(Int<AK>{}, Int<BM>{}, lda, wid * (BM / 8), oa);
-  offsets(Int<BK>{}, Int<BN>{}, ldb, G::GATED ? (wid >> 1) * (BN / 8) : wid * (BN / 8), ob);
+  offsets(Int<BK>{}, Int<BN>{}, ldb, G::GATED ? wgrp * (WC / 2) + win % (WC / 2) : wid * (BN / 8), ob);
 
   int lu = pid, lslot = 0;
   int lw = 0, lwe = 0;              // windows of the item yet to load
@@ -186,7 +189,7 @@ HILO_DEV void run(const ProductProblem &p, const Plan &q, int pid, uint8_t *lds)
   bool more = true;
   auto ld_piece = [&]() __attribute__((always_inline)) {  // bases of piece lpiece
     if constexpr (KIND == PRODUCT_OUT) {
-      const int part = G::GATED ? wid & 1 : 0;
+      const int part = wpart;
       const void *w = lz.stream ? (part ? p.w[1][1] : p.w[1][0]) : (part ? p.w[0][1] : p.w[0][0]);
       la = reinterpret_cast<const char *>(p.x) + size_t(lz.row0) * lda;
       lb = reinterpret_cast<const char *>(w) + size_t(lz.n0) * ldb;
@@ -299,8 +302,8 @@ HILO_DEV void run(const ProductProblem &p, const Plan &q, int pid, uint8_t *lds)
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     const uint32_t chunk = uint32_t((4 * h + lg) ^ ((lr >> 1) & 7)) * 16;
-    fa[h] = lds0 + (AK ? (wm * (BM / 2) + lr) * 128 + chunk : (8 * lg + (lr >> 2)) * (BM * 2) + 8 * (lr & 3) + (f << 5));
-    fb[h] = lds0 + BM * 128 + (BK ? (wn * (BN / 4) + lr) * 128 + chunk : (8 * lg + (lr >> 2)) * (BN * 2) + 8 * (lr & 3) + (f << 5));
+    fa[h] = lds0 + (AK ? (wm * (BM / G::WM) + lr) * 128 + chunk : (8 * lg + (lr >> 2)) * (BM * 2) + 8 * (lr & 3) + (f << 5));
+    fb[h] = lds0 + BM * 128 + (BK ? (wn * (BN / G::WN) + lr) * 128 + chunk : (8 * lg + (lr >> 2)) * (BN * 2) + 8 * (lr & 3) + (f << 5));
   }
   f32x4 acc[MB][NB];
   Frag<AK> a[2][MB];
@@ -437,7 +440,7 @@ HILO_DEV void fix(const ProductProblem &p, const Plan &q) {
     const int v = x / (8 * G::MB), rem = x - v * 8 * G::MB, wid = rem / G::MB, i = rem - wid * G::MB;
     const Place z = place_of<G>(p, q, q.full + v);
     Bias<G> bias;
-    if constexpr (G::KIND == PRODUCT_OUT) bias.load(p, z, wid & 3, lane >> 4);
+    if constexpr (G::KIND == PRODUCT_OUT) bias.load(p, z, wid % G::WN, lane >> 4);
     f32x4 acc[G::NB];
 #pragma unroll
     for (int j = 0; j < G::NB; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -450,45 +453,64 @@ HILO_DEV void fix(const ProductProblem &p, const Plan &q) {
   }
 }
 
-constexpr Cost kCost256{146, 700, 2500}, kCost128{46, 400, 1500};
+// 256 x 256, 256 x 128, 128 x 128
+constexpr Cost kCost[3] = {{146, 700, 2500}, {80, 500, 2000}, {46, 400, 1500}};
+template <int I, int KIND, bool GATED>
+using Tile = Geo<I < 2 ? 256 : 128, I < 1 ? 256 : 128, KIND, GATED>;
 
-// The plan of either tile and whether the larger one is taken; the main kernel and the fixup find the same.
+// Row tiles of outputs (DW) or as the caller counts them, for each tile the plan and its cost: which is quickest.
+template <int KIND, bool GATED, typename F>
+HILO_BOTH int choose(const ProductProblem &p, int nk, F &&row_tiles, Plan &q) {
+  q = make_plan<Tile<0, KIND, GATED>>(p, row_tiles(256), nk, kCost[0]);
+  const Plan a = make_plan<Tile<1, KIND, GATED>>(p, q.R, nk, kCost[1]);
+  const Plan b = make_plan<Tile<2, KIND, GATED>>(p, row_tiles(128), nk, kCost[2]);
+  int best = 0;
+  long long cost = plan_cost(q.T, nk, kCost[0], p.splits != 0);
+  const long long ca = plan_cost(a.T, nk, kCost[1], p.splits != 0), cb = plan_cost(b.T, nk, kCost[2], p.splits != 0);
+  if (ca < cost) {
+    best = 1;
+    cost = ca;
+    q = a;
+  }
+  if (cb < cost) {
+    best = 2;
+    q = b;
+  }
+  return best;
+}
+// On the device, which knows the rows; the main kernel and the fixup find the same.
 template <int KIND, bool GATED>
-HILO_DEV bool choose(const ProductProblem &p, Plan &q) {
-  int nk = windows<KIND>(p, 0), r256, r128;
+HILO_DEV int choose(const ProductProblem &p, Plan &q) {
+  int nk = windows<KIND>(p, 0);
   if constexpr (KIND == PRODUCT_DW) {
     if (!p.merged) nk = max(nk, windows<KIND>(p, 1));
-    r256 = p.outs * ((p.N + 255) / 256);
-    r128 = p.outs * ((p.N + 127) / 128);
-  } else {
-    r256 = count_row_tiles(p, 256);
-    r128 = count_row_tiles(p, 128);
+    return choose<KIND, GATED>(p, nk, [&](int bm) { return p.outs * ((p.N + bm - 1) / bm); }, q);
   }
-  using G256 = Geo<256, 256, KIND, GATED>;
-  using G128 = Geo<128, 128, KIND, GATED>;
-  const Plan a = make_plan<G256>(p, r256, nk, kCost256), b = make_plan<G128>(p, r128, nk, kCost128);
-  const bool large = plan_cost(a.T, nk, kCost256) <= plan_cost(b.T, nk, kCost128);
-  q = large ? a : b;
-  return large;
+  return choose<KIND, GATED>(p, nk, [&](int bm) { return count_row_tiles(p, bm); }, q);
 }
 
 template <int KIND, bool GATED>
 __global__ __launch_bounds__(512, 2) void k_product_tiles(ProductProblem p) {
-  using G256 = Geo<256, 256, KIND, GATED>;
-  using G128 = Geo<128, 128, KIND, GATED>;
-  constexpr int L0 = G256::WB * G256::SLOTS, L1 = G128::WB * G128::SLOTS;
-  __shared__ __attribute__((aligned(1024))) uint8_t lds[L0 > L1 ? L0 : L1];
+  constexpr auto bytes = [](auto g) { return decltype(g)::WB * decltype(g)::SLOTS; };
+  constexpr int L0 = bytes(Tile<0, KIND, GATED>{}), L1 = bytes(Tile<1, KIND, GATED>{}), L2 = bytes(Tile<2, KIND, GATED>{});
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[std::max(L0, std::max(L1, L2))];
   const int pid = xcd_remap(blockIdx.x, P);
   Plan q;
-  if (choose<KIND, GATED>(p, q)) run<G256>(p, q, pid, lds);
-  else run<G128>(p, q, pid, lds);
+  switch (choose<KIND, GATED>(p, q)) {
+    case 0: run<Tile<0, KIND, GATED>>(p, q, pid, lds); break;
+    case 1: run<Tile<1, KIND, GATED>>(p, q, pid, lds); break;
+    default: run<Tile<2, KIND, GATED>>(p, q, pid, lds);
+  }
 }
 
 template <int KIND, bool GATED>
 __global__ __launch_bounds__(512) void k_product_fix(ProductProblem p) {
   Plan q;
-  if (choose<KIND, GATED>(p, q)) fix<Geo<256, 256, KIND, GATED>>(p, q);
-  else fix<Geo<128, 128, KIND, GATED>>(p, q);
+  switch (choose<KIND, GATED>(p, q)) {
+    case 0: fix<Tile<0, KIND, GATED>>(p, q); break;
+    case 1: fix<Tile<1, KIND, GATED>>(p, q); break;
+    default: fix<Tile<2, KIND, GATED>>(p, q);
+  }
 }
 
 }  // namespace pt
@@ -496,10 +518,15 @@ __global__ __launch_bounds__(512) void k_product_fix(ProductProblem p) {
 size_t product_tiles_part_bytes() { return size_t(pt::P) * 256 * 256 * sizeof(float); }
 
 template <int KIND, bool GATED>
-static hipError_t run_tiles(const ProductProblem &p, hipStream_t st) {
+static hipError_t run_tiles(ProductProblem p, hipStream_t st) {
+  const int nk = KIND == PRODUCT_OUT ? (p.K + 63) / 64 : KIND == PRODUCT_DX ? p.parts * ((p.N + 63) / 64) : (p.rows + 63) / 64;
+  pt::Plan q;
+  p.splits = 1;
+  pt::choose<KIND, GATED>(p, nk, [&](int bm) { return KIND == PRODUCT_DW ? p.outs * ((p.N + bm - 1) / bm) : (p.rows + bm - 1) / bm; }, q);
+  p.splits = q.s > 1;
   hipLaunchKernelGGL((pt::k_product_tiles<KIND, GATED>), dim3(pt::P), dim3(512), 0, st, p);
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
+  if (e != hipSuccess || !p.splits) return e;
   hipLaunchKernelGGL((pt::k_product_fix<KIND, GATED>), dim3(pt::P), dim3(512), 0, st, p);
   return hipGetLastError();
 }

@@ -397,18 +397,21 @@ HILO_DEV void fix8(const ProductProblem &p, const Plan &q) {
   }
 }
 
-constexpr Cost kCost8Large{150, 600, 2500}, kCost8Small{80, 400, 1800};
+constexpr Cost kCost8[2] = {{150, 600, 2500}, {80, 400, 1800}};
 
-// 256 x 256 tiles or 128 x 256; codes leave whole tiles only.
+// 256 x 256 tiles or 128 x 256.
+template <bool GATED, typename F>
+HILO_BOTH bool choose8(const ProductProblem &p, F &&row_tiles, Plan &q) {
+  const int nk = (p.K + 127) / 128;
+  const Plan a = make_plan<Geo8<256, 256, GATED>>(p, row_tiles(256), nk, kCost8[0]);
+  const Plan b = make_plan<Geo8<128, 256, GATED>>(p, row_tiles(128), nk, kCost8[1]);
+  const bool large = plan_cost(a.T, nk, kCost8[0], p.splits != 0) <= plan_cost(b.T, nk, kCost8[1], p.splits != 0);
+  q = large ? a : b;
+  return large;
+}
 template <bool GATED>
 HILO_DEV bool choose8(const ProductProblem &p, Plan &q) {
-  const int nk = (p.K + 127) / 128;
-  Plan a = make_plan<Geo8<256, 256, GATED>>(p, count_row_tiles(p, 256), nk, kCost8Large);
-  Plan b = make_plan<Geo8<128, 256, GATED>>(p, count_row_tiles(p, 128), nk, kCost8Small);
-  const bool large = plan_cost(a.T, nk, kCost8Large) <= plan_cost(b.T, nk, kCost8Small);
-  q = large ? a : b;
-  if (p.out_scale) q.s = 1;
-  return large;
+  return choose8<GATED>(p, [&](int bm) { return count_row_tiles(p, bm); }, q);
 }
 
 template <bool GATED>
@@ -432,10 +435,14 @@ __global__ __launch_bounds__(512) void k_product_fp8_fix(ProductProblem p) {
 }  // namespace pt
 
 template <bool GATED>
-static hipError_t run_tiles8(const ProductProblem &p, hipStream_t st) {
+static hipError_t run_tiles8(ProductProblem p, hipStream_t st) {
+  pt::Plan q;
+  p.splits = !p.out_scale;  // codes leave whole tiles
+  pt::choose8<GATED>(p, [&](int bm) { return (p.rows + bm - 1) / bm; }, q);
+  p.splits = q.s > 1;
   hipLaunchKernelGGL((pt::k_product_fp8<GATED>), dim3(pt::P), dim3(512), 0, st, p);
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || p.out_scale) return e;
+  if (e != hipSuccess || !p.splits) return e;
   hipLaunchKernelGGL((pt::k_product_fp8_fix<GATED>), dim3(pt::P), dim3(512), 0, st, p);
   return hipGetLastError();
 }

@@ -22,7 +22,9 @@ HILO_DEV void tile_at(int R, int TN, int t, int &r, int &c) {
 }
 
 // Tiles run whole, P at a time; what is left over for a last turn is cut along k into s pieces each, as many as there are
-// workgroups for, where that is quicker than a whole turn.  Pieces leave float32 tiles that k_product_fix adds up.
+// workgroups for, where that is quicker than a whole turn.  Pieces leave float32 tiles that the fixup adds up, a launch of
+// its own.  Only the device knows the rows: the host launches the fixup, and allows pieces (splits), where all the rows
+// of the buffers would be cut.
 struct Plan {
   int R, TN, T, full, tail, s;
 };
@@ -42,24 +44,25 @@ HILO_DEV Item item_at(const Plan &q, int u) {
 struct Cost {
   int window, tile, fix;
 };
-HILO_DEV int plan_tail(int tail, int nk, Cost c) {
-  if (tail == 0) return 1;
-  const int s = min(P / tail, nk / 4);
+#define HILO_BOTH __host__ __device__ __forceinline__
+HILO_BOTH int plan_tail(int tail, int nk, Cost c, bool cuts) {
+  if (tail == 0 || !cuts) return 1;
+  const int s = P / tail < nk / 4 ? P / tail : nk / 4;
   return s > 1 && nk * c.window > nk * c.window / s + c.fix ? s : 1;
 }
-HILO_DEV int plan_cost(int T, int nk, Cost c) {
-  const int tail = T % P, s = plan_tail(tail, nk, c);
-  return T / P * (nk * c.window + c.tile) + (tail ? nk * c.window / s + c.tile + (s > 1 ? c.fix : 0) : 0);
+HILO_BOTH long long plan_cost(int T, int nk, Cost c, bool cuts) {
+  const int tail = T % P, s = plan_tail(tail, nk, c, cuts);
+  return (long long)(T / P) * (nk * c.window + c.tile) + (tail ? nk * c.window / s + c.tile + (s > 1 ? c.fix : 0) : 0);
 }
 template <typename G>
-HILO_DEV Plan make_plan(const ProductProblem &p, int R, int nk, Cost c) {
+HILO_BOTH Plan make_plan(const ProductProblem &p, int R, int nk, Cost c) {
   Plan q;
   q.R = R;
   q.TN = ((G::KIND == PRODUCT_OUT ? p.N : p.K) + G::COLS - 1) / G::COLS;
   q.T = q.R * q.TN;
   q.tail = q.T % P;
   q.full = q.T - q.tail;
-  q.s = plan_tail(q.tail, nk, c);
+  q.s = plan_tail(q.tail, nk, c, p.splits != 0);
   return q;
 }
 
