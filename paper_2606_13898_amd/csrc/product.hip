@@ -67,17 +67,20 @@ HILO_DEV float e8m0(uint8_t b) {
   return b == 255 ? __uint_as_float(0x7fc00000u) : b == 0 ? __uint_as_float(0x00400000u) : __uint_as_float(uint32_t(b) << 23);
 }
 
-// Tiles of 64 x 64 outputs (with a gate, of 32 columns of either part) on 4 waves of 32 x 32, K in steps of 32 through two
-// LDS buffers: while one is multiplied, the next step's values are on their way to registers.  Both operands lie in LDS
-// as [k][row], so that any layout in memory will do; a lane of group lg takes k = 8 lg + s in step s of 8.
-constexpr int kStep = 32, kPad = 66;
+// Tiles of 64 x 64 outputs (with a gate, of 32 columns of either part) on two groups of 4 waves of 32 x 32: a group takes every
+// other step of 32 values of k, through two LDS buffers of its own, with kAhead steps more on their way to registers, and
+// the groups' sums meet in LDS.  Both operands lie in LDS as [row][k], whichever index is last in memory; rows are kPad
+// values long, so that 16 lanes' 16-byte reads fall on all banks once.  A lane of group lg takes k = 16 s + 4 lg .. + 3.
+constexpr int kStep = 32, kPad = 36, kAhead = 2;
 
 template <int TYPE, int KIND, bool GATED>
-__global__ __launch_bounds__(256) void k_product(ProductProblem p) {
+__global__ __launch_bounds__(512) void k_product(ProductProblem p) {
   constexpr bool AK = KIND != PRODUCT_DW, BK = KIND == PRODUCT_OUT;  // operand's last index is k
   constexpr int BN = GATED && KIND == PRODUCT_OUT ? 32 : 64;         // columns of a tile
-  __shared__ __attribute__((aligned(16))) float lds[2][2][kStep][kPad];
-  const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(tid >> 6);
+  __shared__ __attribute__((aligned(16))) float buffers[2][2][2][64][kPad];
+  const int tid = threadIdx.x & 255, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int group = __builtin_amdgcn_readfirstlane(threadIdx.x >> 8);
+  float (&lds)[2][2][64][kPad] = buffers[group];
   const int lr = lane & 15, lg = lane >> 4, wm = wid >> 1, wn = wid & 1;
   const int cols = KIND == PRODUCT_OUT ? p.N : p.K, tn_count = (cols + BN - 1) / BN;
   const int tm_count = KIND == PRODUCT_DW ? (p.N + 63) / 64 : count_row_tiles(p, 64);
@@ -176,14 +179,14 @@ __global__ __launch_bounds__(256) void k_product(ProductProblem p) {
       a.values(f);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        if constexpr (AK) lds[buf][0][8 * (tid & 3) + e][tid >> 2] = f[e];
-        else lds[buf][0][tid >> 3][8 * (tid & 7) + e] = f[e];
+        if constexpr (AK) lds[buf][0][tid >> 2][8 * (tid & 3) + e] = f[e];
+        else lds[buf][0][8 * (tid & 7) + e][tid >> 3] = f[e];
       }
       b.values(f);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        if constexpr (BK) lds[buf][1][8 * (tid & 3) + e][tid >> 2] = f[e];
-        else lds[buf][1][tid >> 3][8 * (tid & 7) + e] = f[e];
+        if constexpr (BK) lds[buf][1][tid >> 2][8 * (tid & 3) + e] = f[e];
+        else lds[buf][1][8 * (tid & 7) + e][tid >> 3] = f[e];
       }
     };
     f32x4 acc[2][2];
@@ -191,56 +194,72 @@ __global__ __launch_bounds__(256) void k_product(ProductProblem p) {
     for (int i = 0; i < 2; ++i)
 #pragma unroll
       for (int j = 0; j < 2; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    // ---- a step is multiplied out of one LDS buffer, the next lies in the other or is on its way there, and kAhead more are on
-    // their way to registers
     if (s0 < s1) {
-      constexpr int kAhead = 3;
       Chunk<TYPE> a[kAhead], b[kAhead];
-#pragma unroll
-      for (int k = 0; k < kAhead; ++k)
-        if (s0 + k < s1) load(s0 + k, a[k], b[k]);
-      auto step = [&](int s, Chunk<TYPE> &ca, Chunk<TYPE> &cb) __attribute__((always_inline)) {
-        const int buf = (s - s0) & 1;
-        store(buf, ca, cb);
-        if (s + kAhead < s1) load(s + kAhead, ca, cb);
-        __syncthreads();
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          float av[2], bv[2];
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            av[i] = lds[buf][0][8 * lg + e][32 * wm + 16 * i + lr];
-            bv[i] = lds[buf][1][8 * lg + e][32 * wn + 16 * i + lr];
-          }
-#pragma unroll
-          for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(bv[j], av[i], acc[i][j], 0, 0, 0);
+      auto fetch = [&](int s, Chunk<TYPE> &ca, Chunk<TYPE> &cb) __attribute__((always_inline)) {
+        if (s < s1) {
+          load(s, ca, cb);
+        } else {  // the group without a last step
+          ca.zero();
+          cb.zero();
         }
       };
-#pragma unroll 1
-      for (int s = s0; s < s1; s += kAhead) {
-        step(s, a[0], b[0]);
-        if (s + 1 < s1) step(s + 1, a[1], b[1]);
-        if (s + 2 < s1) step(s + 2, a[2], b[2]);
-      }
-      __syncthreads();  // the next item's first step goes to either buffer
-    }
-    // ---- lane (lr, lg) holds rows 16 i + lr and columns 16 j + 4 lg .. + 3 of its wave's 32 x 32
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int r = 32 * wm + 16 * i + lr;
-      if (r >= rows) continue;
+      for (int k = 0; k < kAhead; ++k) fetch(s0 + group + 2 * k, a[k], b[k]);
+      // step s of the group out of buffer buf
+      auto step = [&](int s, int buf, Chunk<TYPE> &ca, Chunk<TYPE> &cb) __attribute__((always_inline)) {
+        store(buf, ca, cb);
+        fetch(s + 2 * kAhead, ca, cb);
+        __syncthreads();
+#pragma unroll
+        for (int h = 0; h < kStep / 16; ++h) {
+          f32x4 av[2], bv[2];
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            av[i] = *reinterpret_cast<const f32x4 *>(&lds[buf][0][32 * wm + 16 * i + lr][16 * h + 4 * lg]);
+            bv[i] = *reinterpret_cast<const f32x4 *>(&lds[buf][1][32 * wn + 16 * i + lr][16 * h + 4 * lg]);
+          }
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+              for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(bv[j][e], av[i][e], acc[i][j], 0, 0, 0);
+        }
+      };
+      static_assert(kAhead == 2, "a buffer for every other step");
+#pragma unroll 1
+      for (int s = s0; s < s1; s += 2 * kAhead) {  // both groups the same number of steps
+        step(s + group, 0, a[0], b[0]);
+        if (s + 2 < s1) step(s + 2 + group, 1, a[1], b[1]);
+      }
+    }
+    // ---- group g finishes row block g of every wave's two
+    __syncthreads();
+    f32x4 *meet = reinterpret_cast<f32x4 *>(buffers) + (group * 4 + wid) * 128 + lane;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) meet[64 * j] = group ? acc[0][j] : acc[1][j];
+    __syncthreads();
+    f32x4 sum[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const f32x4 other = (reinterpret_cast<f32x4 *>(buffers) + ((1 - group) * 4 + wid) * 128 + lane)[64 * j];
+      sum[j] = group ? other + acc[1][j] : acc[0][j] + other;  // group 0's first, in either group
+    }
+    __syncthreads();  // the next item's first steps go to the same LDS
+    // lane (lr, lg): row lr of the block, columns 16 j + 4 lg .. + 3 of the wave's 32
+    const int r = 32 * wm + 16 * group + lr;
+    if (r < rows) {
       const size_t row = size_t(row0) + r;
       if constexpr (KIND == PRODUCT_OUT && GATED) {
         const int n = n0 + 16 * wn + 4 * lg;
-        if (n >= p.N) continue;
+        if (n >= p.N) continue;  // nothing behind it in this item
         if (p.splits > 1) {
           float *q = p.part + (size_t(split) * p.rows + row) * 2 * p.N + n;
-          *reinterpret_cast<f32x4 *>(q) = acc[i][0];
-          *reinterpret_cast<f32x4 *>(q + p.N) = acc[i][1];
+          *reinterpret_cast<f32x4 *>(q) = sum[0];
+          *reinterpret_cast<f32x4 *>(q + p.N) = sum[1];
         } else {
-          finish_out<true>(p, stream, row, n, acc[i][0], acc[i][1]);
+          finish_out<true>(p, stream, row, n, sum[0], sum[1]);
         }
       } else {
 #pragma unroll
@@ -250,13 +269,13 @@ __global__ __launch_bounds__(256) void k_product(ProductProblem p) {
           if (p.splits > 1) {
             const size_t all = KIND == PRODUCT_DW ? size_t(p.outs) * p.N : size_t(p.rows);
             const size_t at = KIND == PRODUCT_DW ? size_t(o) * p.N + row : row;
-            *reinterpret_cast<f32x4 *>(p.part + (split * all + at) * cols + n) = acc[i][j];
+            *reinterpret_cast<f32x4 *>(p.part + (split * all + at) * cols + n) = sum[j];
           } else if constexpr (KIND == PRODUCT_OUT) {
-            finish_out<false>(p, stream, row, n, acc[i][j], acc[i][j]);
+            finish_out<false>(p, stream, row, n, sum[j], sum[j]);
           } else if constexpr (KIND == PRODUCT_DX) {
-            store4(p.dx, row * p.K + n, acc[i][j], p.bf16);
+            store4(p.dx, row * p.K + n, sum[j], p.bf16);
           } else {
-            store4(p.dw[o], row * p.K + n, acc[i][j], p.bf16);
+            store4(p.dw[o], row * p.K + n, sum[j], p.bf16);
           }
         }
       }
@@ -324,7 +343,7 @@ static hipError_t run(ProductProblem &p, hipStream_t st) {
   const int cols = KIND == PRODUCT_OUT ? p.N : p.K, bn = KIND == PRODUCT_OUT && GATED ? 32 : 64;
   const long long items = tm * ((cols + bn - 1) / bn) * p.splits;
   if (items <= 0) return hipSuccess;
-  hipLaunchKernelGGL((k_product<TYPE, KIND, GATED>), dim3(unsigned(std::min(items, 1ll << 20))), dim3(256), 0, st, p);
+  hipLaunchKernelGGL((k_product<TYPE, KIND, GATED>), dim3(unsigned(std::min(items, 1ll << 20))), dim3(512), 0, st, p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.splits == 1) return e;
   const long long quads = (KIND == PRODUCT_DW ? (long long)p.outs * p.N : p.rows) * (cols / 4);
