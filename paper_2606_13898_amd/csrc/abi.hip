@@ -1040,13 +1040,13 @@ BackwardLayout backward_layout(bool bf16, int64_t rows, int K, int N, int batch,
   return l;
 }
 
-// FP8 workspace: codes and scales of float rows, partial products.
+// FP8 workspace: rows as codes and scales or as bf16 values, partial products.
 struct Fp8Layout {
   size_t scale, part, total;
 };
 Fp8Layout fp8_layout(int64_t rows, int K, int N, bool gated) {
   Fp8Layout l;
-  l.scale = align256(size_t(rows) * K);
+  l.scale = align256(size_t(rows) * K * 2);
   l.part = l.scale + align256(size_t(rows) * scale_stride(K));
   l.total = l.part + align256(product_fp8_part_bytes(rows, K, N, gated ? 2 : 1));
   return l;
@@ -1277,14 +1277,16 @@ hilo_status hilo_linear_fp8(int32_t dtype, const hilo_linear_w_fp8 w[2], const v
     for (int q = 0; q < 2; ++q)
       p.merged = p.merged && p.w[0][q] == p.w[1][q] && p.w_scale[0][q] == p.w_scale[1][q] && p.bias[0][q] == p.bias[1][q];
   }
-  if (!x_scale && !product_fp8_quantises(p)) {
+  const Fp8Rows want = product_fp8_rows(p);
+  if (want == FP8_ROWS_WIDE || (want == FP8_ROWS_CODES && !x_scale)) {
+    uint8_t *scale = reinterpret_cast<uint8_t *>(ws + l.scale);
     const hipError_t he = timed(K_QUANT_BLOCKS, st, [&] {
-      return launch_quantize_blocks(p.bf16, x, int(rows), in_dim, 1, cu_seqlens + batch, reinterpret_cast<uint8_t *>(ws),
-                                    reinterpret_cast<uint8_t *>(ws + l.scale), st);
+      if (want == FP8_ROWS_WIDE) return launch_widen_rows(p.bf16, x, x_scale, int(rows), in_dim, cu_seqlens + batch, ws, st);
+      return launch_quantize_blocks(p.bf16, x, int(rows), in_dim, 1, cu_seqlens + batch, reinterpret_cast<uint8_t *>(ws), scale, st);
     });
     if (he != hipSuccess) return HILO_E_DEVICE;
     p.x = ws;
-    p.x_scale = reinterpret_cast<const uint8_t *>(ws + l.scale);
+    p.x_scale = scale;
   }
   p.part = reinterpret_cast<float *>(ws + l.part);
   return dev_status(timed(K_LINEAR_FP8, st, [&] { return launch_product_fp8(p, st); }));

@@ -235,7 +235,10 @@ enum ProductKind { PRODUCT_OUT, PRODUCT_DX, PRODUCT_DW };
 size_t product_part_bytes(bool bf16, int kind, long long rows, int K, int N, int parts);
 size_t product_fp8_part_bytes(long long rows, int K, int N, int parts);
 hipError_t launch_product(int kind, ProductProblem p, hipStream_t st);
-bool product_fp8_quantises(const ProductProblem &p);  // x may be bf16 rows without scales
+// What launch_product_fp8 takes as x: codes with scales; those or bf16 rows; or bf16 rows of the values that codes and
+// scales stand for (launch_widen_rows).
+enum Fp8Rows { FP8_ROWS_CODES, FP8_ROWS_ANY, FP8_ROWS_WIDE };
+Fp8Rows product_fp8_rows(const ProductProblem &p);
 hipError_t launch_product_fp8(ProductProblem p, hipStream_t st);
 // bf16 on large tiles (product_bf16.hip), with partial tiles in p.part.
 size_t product_tiles_part_bytes();
@@ -243,8 +246,9 @@ hipError_t launch_product_tiles(int kind, const ProductProblem &p, hipStream_t s
 // At most kProductFewRows rows, bf16 or FP8 (product_few.hip): x bf16 or codes, out bf16, or float32 with out_f32.
 constexpr int kProductFewRows = 64;
 hipError_t launch_product_few(const ProductProblem &p, hipStream_t st);
-// FP8 on large tiles (product_fp8.hip): out bf16 or codes.
+// FP8 on large tiles (product_fp8.hip): out bf16; and of widened rows: out float32 or bf16, or codes.
 hipError_t launch_product_fp8_tiles(const ProductProblem &p, hipStream_t st);
+hipError_t launch_product_fp8_wide(ProductProblem p, hipStream_t st);
 
 // The step between: dpre [rows][2][N] from dout and pre (gated), and the sums over rows of dpre, or of dout, by stream
 // into db[stream][part] (any null; the two streams' the same: sums over both).
@@ -265,5 +269,8 @@ hipError_t launch_gate_back(bool bf16, GateBackProblem p, hipStream_t st);
 // for block_rows 128 of 128 rows; limit: a device pointer to the number of rows, or null.
 hipError_t launch_quantize_blocks(bool bf16, const void *x, int rows, int cols, int block_rows, const int *limit, uint8_t *codes,
                                   uint8_t *scale, hipStream_t st);
+// The values of such codes of x [rows][cols], or with scale of x's own codes, as bf16.
+hipError_t launch_widen_rows(bool bf16, const void *x, const uint8_t *scale, int rows, int cols, const int *limit, void *out,
+                             hipStream_t st);
 
 }  // namespace hilo

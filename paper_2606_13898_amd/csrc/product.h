@@ -90,6 +90,15 @@ HILO_DEV void gate_slope(float g, bool silu, float &act, float &slope) {
   slope = q == 0.f ? p : p + g * q * (silu ? 1.0f : c * (1.0f + 3.0f * 0.044715f * g * g));
 }
 
+// 8 E4M3 codes times their scale as bf16, exact; scale: the bits of a float32 whose exponent is the E8M0 byte.
+HILO_DEV bf16x8 wide_codes(uint32_t x, uint32_t y, uint32_t scale) {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  const float s = __uint_as_float(scale);
+  const bf16x2 q0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, s, false), q1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, s, true);
+  const bf16x2 q2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(y, s, false), q3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(y, s, true);
+  return bf16x8{q0[0], q0[1], q1[0], q1[1], q2[0], q2[1], q3[0], q3[1]};
+}
+
 // 4 values of a vector of the dtype, or 0 where there is none
 HILO_DEV f32x4 load4(const void *v, size_t i, bool bf16) {
   if (!v) return f32x4{0.f, 0.f, 0.f, 0.f};

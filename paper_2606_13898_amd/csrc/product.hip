@@ -365,25 +365,42 @@ hipError_t launch_product(int kind, ProductProblem p, hipStream_t st) {
   return kind == PRODUCT_OUT && p.rows <= kProductFewRows ? launch_product_few(p, st) : launch_product_tiles(kind, p, st);
 }
 
-// Float32 outputs want float32 sums of the codes' products; the tiles' matrix instruction has not the bits for that.
-size_t product_fp8_part_bytes(long long rows, int K, int N, int parts) {
-  const size_t few = rows <= kProductFewRows ? size_t(rows) * N * sizeof(float) : product_tiles_part_bytes();
-  return std::max(few, product_part_bytes(false, PRODUCT_OUT, rows, K, N, parts));
+// How an FP8 product is formed: of few rows; on FP8 tiles where bf16 leaves; from widened rows where codes or float32 leave; and
+// where that makes few tiles for a long k, float32 ones cut along it.
+enum Fp8Way { FP8_FEW, FP8_TILES, FP8_WIDE, FP8_SPLIT };
+static Fp8Way fp8_way(bool bf16, bool coded, long long rows, int N, int parts) {
+  if (rows <= kProductFewRows) return FP8_FEW;
+  if (coded) return FP8_WIDE;
+  if (bf16) return FP8_TILES;
+  const int cols = parts == 2 ? 128 : 256;
+  return (rows + 127) / 128 * ((N + cols - 1) / cols) >= 64 ? FP8_WIDE : FP8_SPLIT;
 }
-bool product_fp8_quantises(const ProductProblem &p) { return p.rows <= 16 && p.bf16; }
+size_t product_fp8_part_bytes(long long rows, int K, int N, int parts) {
+  if (rows <= kProductFewRows) return size_t(rows) * N * sizeof(float);
+  return std::max(product_tiles_part_bytes(), product_part_bytes(false, PRODUCT_OUT, rows, K, N, parts));
+}
+Fp8Rows product_fp8_rows(const ProductProblem &p) {
+  const Fp8Way way = fp8_way(p.bf16, p.out_scale != nullptr, p.rows, p.N, p.parts);
+  if (way == FP8_WIDE) return FP8_ROWS_WIDE;
+  return way == FP8_FEW && p.bf16 && p.rows <= 16 ? FP8_ROWS_ANY : FP8_ROWS_CODES;
+}
 hipError_t launch_product_fp8(ProductProblem p, hipStream_t st) {
-  if (p.rows <= kProductFewRows && (p.bf16 || p.out_scale)) {
-    if (!p.out_scale) return launch_product_few(p, st);
-    // codes: a scale's 128 columns are eight workgroups', so they are formed from float32 rows in a launch of their own
-    void *codes = p.out;
-    p.out = p.part;
-    p.out_f32 = 1;
-    const hipError_t e = launch_product_few(p, st);
-    if (e != hipSuccess) return e;
-    return launch_quantize_blocks(false, p.out, p.rows, p.N, 1, p.cu + p.B, reinterpret_cast<uint8_t *>(codes), p.out_scale, st);
+  switch (fp8_way(p.bf16, p.out_scale != nullptr, p.rows, p.N, p.parts)) {
+    case FP8_FEW: {
+      p.out_f32 = !p.bf16;
+      if (!p.out_scale) return launch_product_few(p, st);
+      // codes: a scale's 128 columns are eight workgroups', so they are formed from float32 rows in a launch of their own
+      void *codes = p.out;
+      p.out = p.part;
+      p.out_f32 = 1;
+      const hipError_t e = launch_product_few(p, st);
+      if (e != hipSuccess) return e;
+      return launch_quantize_blocks(false, p.out, p.rows, p.N, 1, p.cu + p.B, reinterpret_cast<uint8_t *>(codes), p.out_scale, st);
+    }
+    case FP8_TILES: return launch_product_fp8_tiles(p, st);
+    case FP8_WIDE: return launch_product_fp8_wide(p, st);
+    default: return p.parts == 2 ? run<TYPE_FP8, PRODUCT_OUT, true>(p, st) : run<TYPE_FP8, PRODUCT_OUT, false>(p, st);
   }
-  if (p.bf16 || p.out_scale) return launch_product_fp8_tiles(p, st);
-  return p.parts == 2 ? run<TYPE_FP8, PRODUCT_OUT, true>(p, st) : run<TYPE_FP8, PRODUCT_OUT, false>(p, st);
 }
 
 // ------------------------------------------------------------------------ through the gate, and sums over rows
@@ -546,6 +563,17 @@ HILO_DEV uint8_t block_scale(uint32_t top) {
   return top >= 0x7f800000u ? 255 : uint8_t(127 + pow2_exponent(__uint_as_float(top)));
 }
 
+// The largest magnitude's bits over 16 lanes' 8 values each
+HILO_DEV uint32_t top16(const float (&f)[8]) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) top = max(top, abs_bits(f[e]));
+  top = max(top, uint32_t(dpp<kDppXor1>(int(top))));
+  top = max(top, uint32_t(dpp<kDppXor2>(int(top))));
+  top = max(top, uint32_t(dpp<kDppHalfMirror>(int(top))));
+  return max(top, uint32_t(dpp<kDppMirror>(int(top))));
+}
+
 // Rows: 16 lanes have the 128 columns of a scale, 8 a lane; a wave 512 columns of a row at a time.
 template <bool BF16>
 __global__ __launch_bounds__(256) void k_quantize_blocks(const void *__restrict__ x, int rows, int cols, const int *__restrict__ limit,
@@ -560,16 +588,48 @@ __global__ __launch_bounds__(256) void k_quantize_blocks(const void *__restrict_
     if (c < cols) v.load(x, size_t(row) * cols + c);
     float f[8];
     v.values(f);
-    uint32_t top = 0;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) top = max(top, abs_bits(f[e]));
-    top = max(top, uint32_t(dpp<kDppXor1>(int(top))));
-    top = max(top, uint32_t(dpp<kDppXor2>(int(top))));
-    top = max(top, uint32_t(dpp<kDppHalfMirror>(int(top))));
-    top = max(top, uint32_t(dpp<kDppMirror>(int(top))));
+    const uint32_t top = top16(f);
     if (c < cols) *reinterpret_cast<uint2 *>(codes + size_t(row) * cols + c) = block_codes(f, top);
     if ((lane & 15) == 0) scale[size_t(row) * scale_stride(cols) + c / 128] = c < cols ? block_scale(top) : 0;
   }
+}
+
+// Rows as the values that codes and scales stand for, in bf16, which holds them exactly: of x, or of codes of it (TYPE_FP8).
+template <int TYPE>
+__global__ __launch_bounds__(256) void k_widen_rows(const void *__restrict__ x, const uint8_t *__restrict__ scale, int rows, int cols,
+                                                    const int *__restrict__ limit, uint16_t *__restrict__ out) {
+  const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int end = min(rows, cu_at(limit, 0)), groups = (cols + 511) / 512;
+  const long long units = (long long)end * groups;
+  for (long long t = blockIdx.x * 4ll + wid; t < units; t += gridDim.x * 4ll) {
+    const int row = int(t / groups), c = int(t - (long long)row * groups) * 512 + 8 * lane;
+    Chunk<TYPE> v;
+    v.zero();
+    if (c < cols) v.load(x, size_t(row) * cols + c);
+    uint2 codes;
+    uint32_t s;
+    if constexpr (TYPE == TYPE_FP8) {
+      codes = make_uint2(v.u[0].x, v.u[0].y);
+      s = c < cols ? scale[size_t(row) * scale_stride(cols) + c / 128] : 0;
+    } else {
+      float f[8];
+      v.values(f);
+      const uint32_t top = top16(f);
+      codes = block_codes(f, top);
+      s = block_scale(top);
+    }
+    if (c < cols) *reinterpret_cast<bf16x8 *>(out + size_t(row) * cols + c) = wide_codes(codes.x, codes.y, s << 23);
+  }
+}
+
+hipError_t launch_widen_rows(bool bf16, const void *x, const uint8_t *scale, int rows, int cols, const int *limit, void *out, hipStream_t st) {
+  const long long units = (long long)rows * ((cols + 511) / 512);
+  const dim3 grid(unsigned(std::min((units + 3) / 4, 1ll << 20)));
+  uint16_t *o = reinterpret_cast<uint16_t *>(out);
+  if (scale) hipLaunchKernelGGL((k_widen_rows<TYPE_FP8>), grid, dim3(256), 0, st, x, scale, rows, cols, limit, o);
+  else if (bf16) hipLaunchKernelGGL((k_widen_rows<TYPE_BF16>), grid, dim3(256), 0, st, x, scale, rows, cols, limit, o);
+  else hipLaunchKernelGGL((k_widen_rows<TYPE_F32>), grid, dim3(256), 0, st, x, scale, rows, cols, limit, o);
+  return hipGetLastError();
 }
 
 // Blocks of 128 x 128: a workgroup each, a thread 8 rows of 8 columns, held while the largest is found.

@@ -62,12 +62,6 @@ struct Frag<false> {
   HILO_DEV void pin() { asm volatile("" : "+v"(lo), "+v"(hi)); }
 };
 
-HILO_DEV void swap16(uint32_t &x, uint32_t &y) {
-  const auto r = __builtin_amdgcn_permlane16_swap(x, y, false, false);
-  x = r[0];
-  y = r[1];
-}
-
 // Two blocks of 16 columns of a row, four a lane: lanes of groups 0 and 2 get 8 of the first's, of 1 and 3 of the second's,
 // so that a store writes 64 consecutive bytes of 16 rows.  c: the first block's column.
 HILO_DEV void store_blocks(uint16_t *row, int c, int end, int lg, f32x4 a, f32x4 b, bool inside) {

@@ -6,7 +6,8 @@
 // lie side by side: each is looked up.
 //
 // FP8: up to 16 float rows are quantised where they are read, by every workgroup anew: a row's block of 128 is in four lanes, so
-// its largest value takes two exchanges, and a launch less is worth more than the arithmetic.
+// its largest value takes two exchanges, and a launch less is worth more than the arithmetic.  Codes are multiplied as
+// bf16, which holds a code times its scale exactly: the FP8 instruction keeps fewer bits, and its rate is of no use here.
 #include <algorithm>
 
 #include "product.h"
@@ -155,10 +156,10 @@ __global__ __launch_bounds__(64 * kWaves) void k_product_few(ProductProblem p) {
             acc[q][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v.w[q].half(h), v.x[i][0].half(h), acc[q][i], 0, 0, 0);
       } else {
         i32x8 xc;
-        int sx;
+        uint32_t sx;
         if constexpr (ROWS == ROWS_CODES) {
           xc = v.x[i][0].all();
-          sx = int(v.sx[i]);
+          sx = v.sx[i];
         } else {
           float f[4][8];
           uint32_t top = 0;
@@ -181,8 +182,15 @@ __global__ __launch_bounds__(64 * kWaves) void k_product_few(ProductProblem p) {
           sx = finite ? 127 + k : 255;
         }
 #pragma unroll
-        for (int q = 0; q < PARTS; ++q)
-          acc[q][i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(v.w[q].all(), xc, acc[q][i], 0, 0, 0, int(v.sw[q]), 0, sx);
+        for (int m = 0; m < 4; ++m) {
+          const bf16x8 xb = wide_codes(uint32_t(xc[2 * m]), uint32_t(xc[2 * m + 1]), sx << 23);
+#pragma unroll
+          for (int q = 0; q < PARTS; ++q) {
+            const i32x8 wc = v.w[q].all();
+            acc[q][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wide_codes(uint32_t(wc[2 * m]), uint32_t(wc[2 * m + 1]), v.sw[q] << 23), xb,
+                                                                acc[q][i], 0, 0, 0);
+          }
+        }
       }
     }
   };

@@ -6,8 +6,8 @@
 // columns (128 x 128 blocks).
 //
 // The instruction aligns the products of eight consecutive k to the one with the largest exponents and cuts what lies more than 13
-// bits below (each group's sum is then added in float32's precision): enough for outputs of 8 bits, not for float32's,
-// which go another way (launch_product_fp8).
+// bits below (each group's sum is then added in float32's precision): enough for outputs of bf16, not for float32's or for
+// codes, which go another way (run_wide).
 //
 // A wave's 128 x 64 are 32 x 32 blocks: lane l holds row l % 32 and, W's rows being read in the order perm, columns
 // 16 (l / 32) .. + 15 of a block in register order.  With a gate the two blocks of columns are the gate's and the other's.
@@ -29,9 +29,8 @@ struct Geo8 {
   static constexpr int LA = BM / 64, LB = BN / 64;
   static constexpr int WB = (BM + BN) * 128;
   static constexpr int RING = 4, RB = BM * 4;        // windows' scales of x, bytes of one
-  static constexpr int TOPS = BM * 16;               // a row's largest values by wave
-  static constexpr int SLOTS = 3 * WB + RING * RB + TOPS <= 160 * 1024 ? 3 : 2;
-  static constexpr int LDS = SLOTS * WB + RING * RB + TOPS;
+  static constexpr int SLOTS = 3 * WB + RING * RB <= 160 * 1024 ? 3 : 2;
+  static constexpr int LDS = SLOTS * WB + RING * RB;
   static constexpr int COLS = GATED ? BN / 2 : BN;
   static_assert(RING > SLOTS, "a window's scales last until it is multiplied");
   static_assert(!GATED || NB == 2, "a block of either part");
@@ -110,33 +109,36 @@ HILO_DEV size_t part_at8(int slot, int wid, int i, int j, int lane) {
   return size_t(slot) * G::BM * G::BN + ((size_t(wid) * G::MB * G::NB + i * G::NB + j) * 64 + lane) * 16;
 }
 
+// A workgroup's loads, product_bf16.hip's with k last, and a window's scales: windows of its items one after another.
 template <typename G>
-HILO_DEV void run8(const ProductProblem &p, const Plan &q, int pid, uint8_t *lds) {
-  constexpr int BM = G::BM, BN = G::BN, MB = G::MB, NB = G::NB, LA = G::LA, LB = G::LB, WB = G::WB, S = G::SLOTS;
-  const int lane = threadIdx.x & 63;
-  const int wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int wm = wid >> 2, wn = wid & 3;
-  const uint32_t ld = p.K, lds_scale = scale_stride(p.K);
-  const int nk = (p.K + 127) / 128;
-
-  // ---- loads, as product_bf16.hip's
+struct Loads8 {
+  static constexpr int BM = G::BM, BN = G::BN, LA = G::LA, LB = G::LB, WB = G::WB, S = G::SLOTS;
+  const ProductProblem &p;
+  const Plan &q;
+  uint8_t *lds;
+  int wid;
+  uint32_t ld, lds_scale;
+  int nk;
   // the chunk of instruction i (8 rows) is that of instruction 0, or its bit 2 the other way round
   uint32_t oa[2], ob[2];
-  const int wrow = G::GATED ? (wid >> 1) * (BN / 8) : wid * (BN / 8);  // first row of W, of its part, that the wave loads
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int r = lane >> 3;
-    oa[i] = uint32_t(wid * (BM / 8) + r) * ld + 16u * ((lane & 7) ^ swz(wid * (BM / 8) + r) ^ (4 * i));
-    ob[i] = uint32_t(wrow + r) * ld + 16u * ((lane & 7) ^ swz(wid * (BN / 8) + r) ^ (4 * i));
-  }
-  int lu = pid, lslot = 0, lring = 0;
-  int lw = 0, lwe = 0;
+  int lu, slot = 0, ring = 0, w = 0, we = 0, rows = 0;
   const char *la = nullptr, *lb = nullptr, *lsc = nullptr;
   uint32_t ra = 0, rb = 0;
-  int lrows = 0;
   bool more = true;
-  auto ld_step = [&]() __attribute__((always_inline)) {
-    if (!more || lw < lwe) return;
+
+  HILO_DEV Loads8(const ProductProblem &p_, const Plan &q_, int pid, uint8_t *lds_, int wid_)
+      : p(p_), q(q_), lds(lds_), wid(wid_), ld(p_.K), lds_scale(scale_stride(p_.K)), nk((p_.K + 127) / 128), lu(pid) {
+    const int lane = threadIdx.x & 63, r = lane >> 3;
+    const int wrow = G::GATED ? (wid >> 1) * (BN / 8) : wid * (BN / 8);  // first row of W, of its part, that the wave loads
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      oa[i] = uint32_t(wid * (BM / 8) + r) * ld + 16u * ((lane & 7) ^ swz(wid * (BM / 8) + r) ^ (4 * i));
+      ob[i] = uint32_t(wrow + r) * ld + 16u * ((lane & 7) ^ swz(wid * (BN / 8) + r) ^ (4 * i));
+    }
+  }
+  // to the next item where this one ends
+  HILO_DEV void step() {
+    if (!more || w < we) return;
     const Item it = item_at(q, lu);
     if (!it.valid) {
       more = false;
@@ -144,43 +146,69 @@ HILO_DEV void run8(const ProductProblem &p, const Plan &q, int pid, uint8_t *lds
     }
     lu += P;
     const Place z = place_of<G>(p, q, it.t);
-    lw = int((long long)nk * it.pc / it.n);
-    lwe = int((long long)nk * (it.pc + 1) / it.n);
+    w = int((long long)nk * it.pc / it.n);
+    we = int((long long)nk * (it.pc + 1) / it.n);
     const int part = G::GATED ? wid & 1 : 0;
-    const void *w = z.stream ? (part ? p.w[1][1] : p.w[1][0]) : (part ? p.w[0][1] : p.w[0][0]);
+    const void *m = z.stream ? (part ? p.w[1][1] : p.w[1][0]) : (part ? p.w[0][1] : p.w[0][0]);
     la = reinterpret_cast<const char *>(p.x) + size_t(z.row0) * ld;
-    lb = reinterpret_cast<const char *>(w) + size_t(z.n0) * ld;
+    lb = reinterpret_cast<const char *>(m) + size_t(z.n0) * ld;
     lsc = reinterpret_cast<const char *>(p.x_scale) + size_t(z.row0) * lds_scale;
-    lrows = z.rows;
+    rows = z.rows;
     ra = uint32_t(z.rows) * ld;
     rb = uint32_t(min(G::COLS, p.N - z.n0)) * ld;
-  };
-  auto ld_rows = [&](auto count, const char *base, uint32_t reach, const uint32_t (&o)[2], int lds_base, uint8_t *d) __attribute__((always_inline)) {
-    constexpr int L = decltype(count)::value;
+  }
+  template <int L>
+  HILO_DEV void window(const char *base, uint32_t reach, const uint32_t (&o)[2], int lds_base, uint8_t *d) {
     // chunks of k behind the end: offsets behind the buffer's
-    const int kv = p.K - 128 * lw, lane = opaque(threadIdx.x & 63), c = (lane & 7) ^ swz(lds_base + (lane >> 3));
+    const int kv = p.K - 128 * w, lane = opaque(threadIdx.x & 63), c = (lane & 7) ^ swz(lds_base + (lane >> 3));
     const uint32_t o0 = 16 * c < kv ? o[0] : kBehind, o1 = 16 * (c ^ 4) < kv ? o[1] : kBehind;
-    auto at = [&](int i) __attribute__((always_inline)) { return ((i ^ (i >> 1)) & 1 ? o1 : o0) + uint32_t(8 * i) * ld; };
-    const uint32_t bytes = more ? reach - 128u * uint32_t(lw) : 0u;
-    base += size_t(lw) * 128;
+    const uint32_t bytes = more ? reach - 128u * uint32_t(w) : 0u;
+    base += size_t(w) * 128;
 #pragma unroll
-    for (int i = 0; i < L; ++i) buffer_to_lds(base, bytes, at(i), d + i * 1024);
-  };
-  auto ld_a = [&]() __attribute__((always_inline)) {
+    for (int i = 0; i < L; ++i) buffer_to_lds(base, bytes, ((i ^ (i >> 1)) & 1 ? o1 : o0) + uint32_t(8 * i) * ld, d + i * 1024);
+  }
+  HILO_DEV void a() {
     constexpr int N = BM / 64;
     const int r = 64 * (wid % N) + opaque(threadIdx.x & 63);
     __builtin_amdgcn_raw_ptr_buffer_load_lds(
-        __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(lsc), 0, more ? int(uint32_t(lrows) * lds_scale) : 0, 0x00020000),
-        (__attribute__((address_space(3))) void *)(lds + S * WB + lring * G::RB + 256 * (wid % N)), 4,
-        int(uint32_t(r) * lds_scale + 4u * (uint32_t(lw) >> 2)), 0, 0, 0);
-    lring = (lring + 1) & (G::RING - 1);
-    ld_rows(Int<LA>{}, la, ra, oa, wid * (BM / 8), lds + lslot * WB + wid * (BM * 16));
-  };
-  auto ld_b = [&]() __attribute__((always_inline)) {
-    ld_rows(Int<LB>{}, lb, rb, ob, wid * (BN / 8), lds + lslot * WB + BM * 128 + wid * (BN * 16));
-    ++lw;
-    lslot = lslot == S - 1 ? 0 : lslot + 1;
-  };
+        __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(lsc), 0, more ? int(uint32_t(rows) * lds_scale) : 0, 0x00020000),
+        (__attribute__((address_space(3))) void *)(lds + S * WB + ring * G::RB + 256 * (wid % N)), 4,
+        int(uint32_t(r) * lds_scale + 4u * (uint32_t(w) >> 2)), 0, 0, 0);
+    ring = (ring + 1) & (G::RING - 1);
+    window<LA>(la, ra, oa, wid * (BM / 8), lds + slot * WB + wid * (BM * 16));
+  }
+  HILO_DEV void b() {
+    window<LB>(lb, rb, ob, wid * (BN / 8), lds + slot * WB + BM * 128 + wid * (BN * 16));
+    ++w;
+    slot = slot == S - 1 ? 0 : slot + 1;
+  }
+  // the first S windows, of which one has landed
+  HILO_DEV void start() {
+#pragma unroll 1
+    for (int i = 0; i < S; ++i) {
+      step();
+      a();
+      b();
+    }
+    wait_vm<(S - 1) * (LA + LB + 1)>();
+    asm volatile("s_barrier" ::: "memory");
+  }
+  // this wave has read a window, and all but the last issued windows have landed
+  HILO_DEV void next() {
+    wait_vm<(S - 2) * (LA + LB + 1)>();
+    asm volatile("s_barrier" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+  }
+};
+
+template <typename G>
+HILO_DEV void run8(const ProductProblem &p, const Plan &q, int pid, uint8_t *lds) {
+  constexpr int BM = G::BM, BN = G::BN, MB = G::MB, NB = G::NB, WB = G::WB, S = G::SLOTS;
+  const int lane = threadIdx.x & 63;
+  const int wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wid >> 2, wn = wid & 3;
+  Loads8<G> loads(p, q, pid, lds, wid);
+  const int nk = loads.nk;
 
   // ---- fragments: of half h, chunks 4 h + g and 4 h + 2 + g of a row (g = lane / 32)
   const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
@@ -259,8 +287,8 @@ HILO_DEV void run8(const ProductProblem &p, const Plan &q, int pid, uint8_t *lds
           if constexpr (RPB > 5) rd(Int<1 - h>{}, Int<i * RPB + 5>{});
         }
         if constexpr (decltype(ldd)::value != 0) {
-          if constexpr (i == 0) ld_a();
-          if constexpr (i == GR / 2) ld_b();
+          if constexpr (i == 0) loads.a();
+          if constexpr (i == GR / 2) loads.b();
         }
         __builtin_amdgcn_sched_barrier(0);
       }
@@ -269,14 +297,7 @@ HILO_DEV void run8(const ProductProblem &p, const Plan &q, int pid, uint8_t *lds
     group(Int<4>{}); group(Int<5>{}); group(Int<6>{}); group(Int<7>{});
   };
 
-#pragma unroll 1
-  for (int w = 0; w < S; ++w) {
-    ld_step();
-    ld_a();
-    ld_b();
-  }
-  wait_vm<(S - 1) * (LA + LB + 1)>();
-  asm volatile("s_barrier" ::: "memory");
+  loads.start();
   for (int u = pid;; u += P) {
     const Item it = item_at(q, u);
     if (!it.valid) break;
@@ -285,7 +306,7 @@ HILO_DEV void run8(const ProductProblem &p, const Plan &q, int pid, uint8_t *lds
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       const uint8_t *s = z.stream ? (j ? p.w_scale[1][1] : p.w_scale[1][0]) : (j ? p.w_scale[0][1] : p.w_scale[0][0]);
-      ws[j] = s + size_t((G::GATED ? z.n0 : min(z.n0 + wn * (BN / 4), p.N - 1)) / 128) * lds_scale;
+      ws[j] = s + size_t((G::GATED ? z.n0 : min(z.n0 + wn * (BN / 4), p.N - 1)) / 128) * loads.lds_scale;
     }
 #pragma unroll
     for (int i = 0; i < MB; ++i)
@@ -296,13 +317,10 @@ HILO_DEV void run8(const ProductProblem &p, const Plan &q, int pid, uint8_t *lds
     take_scales(w0);
 #pragma unroll 1
     for (int w = w0; w < w1; ++w) {
-      ld_step();  // its branch lies here because MFMAs before a branch are moved behind it
+      loads.step();  // its branch lies here because MFMAs before a branch are moved behind it
       half(Int<0>{}, Int<0>{});
       rd_wait(Int<1>{});
-      // this wave has read the window, and all but the last issued windows have landed; on to the next
-      wait_vm<(S - 2) * (LA + LB + 1)>();
-      asm volatile("s_barrier" ::: "memory");
-      __builtin_amdgcn_sched_barrier(0);
+      loads.next();
       so = so == (S - 1) * WB ? 0 : so + WB;
       ring = (ring + 1) & (G::RING - 1);
       rd_scales();
@@ -320,56 +338,257 @@ HILO_DEV void run8(const ProductProblem &p, const Plan &q, int pid, uint8_t *lds
     }
     float bias[NB][16];
     load_bias<G>(p, z, wn, lane >> 5, bias);
-    if constexpr (G::GATED && G::COLS == 128) {
-      if (p.out_scale) {
-        // codes: the tile's 128 columns have one scale a row, from the largest of four waves' 32 columns
-        const int n = col8<G>(z, wn, 0, lane >> 5);
-        const uint32_t tops = lds0 + S * WB + G::RING * G::RB;
-#pragma unroll
-        for (int i = 0; i < MB; ++i) {
-          gate16(p, bias[0], bias[1], acc[i][0], acc[i][1]);
-          uint32_t top = 0;
-#pragma unroll
-          for (int e = 0; e < 16; ++e) top = max(top, abs_bits(acc[i][0][e]));
-          top = n < p.N ? top : 0u;
-          top = max(top, uint32_t(__shfl_xor(int(top), 32, 64)));
-          if (lane < 32)
-            asm volatile("ds_write_b32 %0, %1" ::"v"(tops + 16 * (wm * (BM / 2) + 32 * i + lane) + 4 * wn), "v"(top) : "memory");
-        }
-        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-#pragma unroll
-        for (int i = 0; i < MB; ++i) {
-          const int rl = wm * (BM / 2) + 32 * i + (lane & 31);
-          u32x4 t;
-          asm volatile("ds_read_b128 %0, %1\n\ts_waitcnt lgkmcnt(0)" : "=v"(t) : "v"(tops + 16 * rl) : "memory");
-          const uint32_t top = max(max(t[0], t[1]), max(t[2], t[3]));
-          const bool finite = top < 0x7f800000u;
-          const int k = pow2_exponent(__uint_as_float(top));
-          const float inv = pow2_inverse(finite ? k : 0);
-          uint4 c;
-          c.x = fp8x4(acc[i][0][0] * inv, acc[i][0][1] * inv, acc[i][0][2] * inv, acc[i][0][3] * inv);
-          c.y = fp8x4(acc[i][0][4] * inv, acc[i][0][5] * inv, acc[i][0][6] * inv, acc[i][0][7] * inv);
-          c.z = fp8x4(acc[i][0][8] * inv, acc[i][0][9] * inv, acc[i][0][10] * inv, acc[i][0][11] * inv);
-          c.w = fp8x4(acc[i][0][12] * inv, acc[i][0][13] * inv, acc[i][0][14] * inv, acc[i][0][15] * inv);
-          if (!finite) c = make_uint4(0x7f7f7f7fu, 0x7f7f7f7fu, 0x7f7f7f7fu, 0x7f7f7f7fu);
-          if (rl < z.rows) {
-            const size_t row = size_t(z.row0) + rl;
-            if (n < p.N) *reinterpret_cast<uint4 *>(reinterpret_cast<uint8_t *>(p.out) + row * p.N + n) = c;
-            if (wn == 0 && lane < 32) {
-              uint8_t *s = p.out_scale + row * scale_stride(p.N);
-              const int at = z.n0 / 128, end = z.n0 + 128 >= p.N ? scale_stride(p.N) : at + 1;
-              s[at] = finite ? uint8_t(127 + k) : 255;
-              for (int x = at + 1; x < end; ++x) s[x] = 0;
-            }
-          }
-        }
-        continue;
-      }
-    }
 #pragma unroll
     for (int i = 0; i < MB; ++i) {
       finish8<G>(p, z, bias, wid, i, lane, acc[i]);
       asm volatile("" ::: "memory");
+    }
+  }
+  wait_vm<0>();
+}
+
+// Where the instruction's 13 bits are too few -- codes out, since h next to the border between two codes gets the other one
+// some ten times as often as with float32 sums, and float32 out -- the products are of bf16, which holds a code times its
+// scale exactly, at half the rate.  x comes as such bf16 rows (k_widen_rows); W's codes are widened behind LDS, 16 of a row by
+// a lane, which takes about as long as the MFMAs they feed (16 cycles for two values).  Tiles of 128 x 256, windows of 64 values: 128-byte
+// rows of x, 64-byte rows of W, whose 16-byte chunk c of row r lies at c ^ (r / 4) % 4.  An MFMA of half h multiplies
+// values 16 g + 8 h .. + 7 of lane group g.
+template <bool GATED_>
+struct GeoW {
+  static constexpr int BM = 128, BN = 256, KIND = PRODUCT_OUT;
+  static constexpr bool GATED = GATED_;
+  static constexpr int MB = 4, NB = 4;  // blocks of 16 x 16 of a wave, 2 x 4 waves
+  static constexpr int COLS = GATED ? BN / 2 : BN;
+  static constexpr int WA = BM * 128, WB = WA + BN * 64, SLOTS = 4;
+  static constexpr int TOPS = BM * 16;  // codes out: a row's largest values by wave
+  static constexpr int LDS = SLOTS * WB + TOPS;
+  static_assert(LDS <= 160 * 1024, "LDS");
+};
+
+template <typename G>
+HILO_DEV void run_wide(const ProductProblem &p, const Plan &q, int pid, uint8_t *lds) {
+  constexpr int BM = G::BM, BN = G::BN, MB = G::MB, NB = G::NB, WA = G::WA, WB = G::WB, S = G::SLOTS, L = 4;  // loads of a window
+  const int lane = threadIdx.x & 63;
+  const int wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lr = lane & 15, lg = lane >> 4, wm = wid >> 2, wn = wid & 3;
+  const uint32_t lda = 2u * p.K, ldb = p.K;
+  const int nk = (p.K + 63) / 64, stride = scale_stride(p.K);
+
+  // ---- loads: 16 rows of x and 32 of W a wave, two instructions each; with a gate a wave's rows of W are of one part
+  uint32_t oa[2], ob[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int r = 8 * i + (lane >> 3), s = 16 * i + (lane >> 2);
+    oa[i] = uint32_t(wid * 16 + r) * lda + 16u * ((lane & 7) ^ ((r >> 1) & 7));
+    ob[i] = uint32_t((G::GATED ? wid >> 1 : wid) * 32 + s) * ldb + 16u * ((lane & 3) ^ ((s >> 2) & 3));
+  }
+  int lu = pid, lslot = 0, lw = nk;
+  const char *la = nullptr, *lb = nullptr;
+  uint32_t ra = 0, rb = 0;
+  bool more = true;
+  auto ld_step = [&]() __attribute__((always_inline)) {
+    if (!more || lw < nk) return;
+    const Item it = item_at(q, lu);
+    if (!it.valid) {
+      more = false;
+      return;
+    }
+    lu += P;
+    const Place z = place_of<G>(p, q, it.t);
+    lw = 0;
+    const int part = G::GATED ? wid & 1 : 0;
+    const void *w = z.stream ? (part ? p.w[1][1] : p.w[1][0]) : (part ? p.w[0][1] : p.w[0][0]);
+    la = reinterpret_cast<const char *>(p.x) + size_t(z.row0) * lda;
+    lb = reinterpret_cast<const char *>(w) + size_t(z.n0) * ldb;
+    ra = uint32_t(z.rows) * lda;
+    rb = uint32_t(min(G::COLS, p.N - z.n0)) * ldb;
+  };
+  auto ld = [&]() __attribute__((always_inline)) {
+    // chunks behind the end of k: offsets behind the buffer's
+    const int kv = p.K - 64 * lw, lane = opaque(threadIdx.x & 63);
+    const int c = (lane & 7) ^ ((lane >> 4) & 3), d = (lane & 3) ^ ((lane >> 4) & 3);
+    uint8_t *at = lds + lslot * WB;
+    const uint32_t na = more ? ra - 128u * uint32_t(lw) : 0u, nb = more ? rb - 64u * uint32_t(lw) : 0u;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      buffer_to_lds(la + size_t(lw) * 128, na, 8 * (i ? c ^ 4 : c) < kv ? oa[i] : kBehind, at + wid * 2048 + i * 1024);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) buffer_to_lds(lb + size_t(lw) * 64, nb, 16 * d < kv ? ob[i] : kBehind, at + WA + wid * 2048 + i * 1024);
+    ++lw;
+    lslot = (lslot + 1) & (S - 1);
+  };
+
+  // ---- fragments
+  const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
+  uint32_t fa[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) fa[h] = lds0 + (wm * (BM / 2) + lr) * 128 + ((2 * lg + h) ^ ((lr >> 1) & 7)) * 16;
+  const uint32_t fb = lds0 + WA + (wn * (BN / 4) + lr) * 64 + (lg ^ ((lr >> 2) & 3)) * 16;
+  f32x4 acc[MB][NB];
+  u32x4 a[2][MB], b[NB];  // halves of x's window; all of W's
+  bf16x8 wb[2][NB];
+  uint32_t so = 0;
+  auto rd_a = [&](auto hh, auto ii) __attribute__((always_inline)) {
+    constexpr int h = decltype(hh)::value, i = decltype(ii)::value;
+    read16<i * 2048>(a[h][i], fa[h] + so);
+  };
+  auto rd_b = [&](auto jj) __attribute__((always_inline)) {
+    constexpr int j = decltype(jj)::value;
+    read16<j * 1024>(b[j], fb + so);
+  };
+  auto pin = [&](u32x4 &v) __attribute__((always_inline)) { asm volatile("" : "+v"(v)); };
+  const uint8_t *ws[2] = {nullptr, nullptr};
+  auto scale = [&](int j, int w) __attribute__((always_inline)) {  // of part j, block w / 2: a float32 number's exponent
+    return (scales_at(ws[G::GATED ? j : 0], w >> 3) >> (4 * (w & 6)) & 255u) << 23;
+  };
+  // wb of half h
+  auto widen = [&](auto hh, uint32_t s0, uint32_t s1) __attribute__((always_inline)) {
+    constexpr int h = decltype(hh)::value;
+#pragma unroll
+    for (int j = 0; j < NB; ++j) wb[h][j] = wide_codes(b[j][2 * h], b[j][2 * h + 1], j < NB / 2 ? s0 : s1);
+  };
+  // row block i of half h
+  auto row = [&](auto hh, auto ii) __attribute__((always_inline)) {
+    constexpr int h = decltype(hh)::value, i = decltype(ii)::value;
+#pragma unroll
+    for (int j = 0; j < NB; ++j)
+      acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wb[h][j], __builtin_bit_cast(bf16x8, a[h][i]), acc[i][j], 0, 0, 0);
+  };
+#pragma unroll 1
+  for (int w = 0; w < S; ++w) {
+    ld_step();
+    ld();
+  }
+  wait_vm<(S - 1) * L>();
+  asm volatile("s_barrier" ::: "memory");
+  for (int u = pid;; u += P) {
+    const Item it = item_at(q, u);
+    if (!it.valid) break;
+    const Place z = place_of<G>(p, q, it.t);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const uint8_t *s = z.stream ? (j ? p.w_scale[1][1] : p.w_scale[1][0]) : (j ? p.w_scale[0][1] : p.w_scale[0][0]);
+      ws[j] = s + size_t((G::GATED ? z.n0 : min(z.n0 + wn * (BN / 4), p.N - 1)) / 128) * stride;
+    }
+#pragma unroll
+    for (int i = 0; i < MB; ++i)
+#pragma unroll
+      for (int j = 0; j < NB; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    rd_b(Int<0>{}); rd_b(Int<1>{}); rd_b(Int<2>{}); rd_b(Int<3>{});
+    rd_a(Int<0>{}, Int<0>{}); rd_a(Int<0>{}, Int<1>{}); rd_a(Int<0>{}, Int<2>{}); rd_a(Int<0>{}, Int<3>{});
+    __builtin_amdgcn_s_waitcnt(0xc07f);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      pin(a[0][i]);
+      pin(b[i]);
+    }
+    uint32_t s0 = scale(0, 0), s1 = scale(1, 0);
+    widen(Int<0>{}, s0, s1);
+#pragma unroll 1
+    for (int w = 0; w < nk; ++w) {
+      ld_step();
+      // half 0, beside it half 1's rows of x read and W's codes of half 1 widened
+      rd_a(Int<1>{}, Int<0>{}); rd_a(Int<1>{}, Int<1>{}); rd_a(Int<1>{}, Int<2>{}); rd_a(Int<1>{}, Int<3>{});
+      __builtin_amdgcn_sched_barrier(0);
+      row(Int<0>{}, Int<0>{}); row(Int<0>{}, Int<1>{}); row(Int<0>{}, Int<2>{}); row(Int<0>{}, Int<3>{});
+      widen(Int<1>{}, s0, s1);
+      s0 = scale(0, min(w + 1, nk - 1));
+      s1 = scale(1, min(w + 1, nk - 1));
+      __builtin_amdgcn_s_waitcnt(0xc07f);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) pin(a[1][i]);
+      __builtin_amdgcn_sched_barrier(0);
+      // this wave has read the window, and all but the last issued windows have landed; on to the next
+      wait_vm<(S - 2) * L>();
+      asm volatile("s_barrier" ::: "memory");
+      __builtin_amdgcn_sched_barrier(0);
+      so = so == (S - 1) * WB ? 0 : so + WB;
+      rd_b(Int<0>{}); rd_b(Int<1>{}); rd_b(Int<2>{}); rd_b(Int<3>{});
+      rd_a(Int<0>{}, Int<0>{}); rd_a(Int<0>{}, Int<1>{}); rd_a(Int<0>{}, Int<2>{}); rd_a(Int<0>{}, Int<3>{});
+      __builtin_amdgcn_sched_barrier(0);
+      row(Int<1>{}, Int<0>{}); row(Int<1>{}, Int<1>{});
+      __builtin_amdgcn_sched_barrier(0);
+      ld();
+      __builtin_amdgcn_s_waitcnt(0xc07f);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        pin(a[0][i]);
+        pin(b[i]);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      // the next window's half 0 beside the other rows of half 1
+      row(Int<1>{}, Int<2>{}); row(Int<1>{}, Int<3>{});
+      widen(Int<0>{}, s0, s1);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    const int lane = opaque(threadIdx.x & 63), lr = lane & 15, lg = lane >> 4;
+    // lane (lr, lg): rows 16 i + lr, columns 16 j + 4 lg .. + 3 of block j; with a gate blocks 0 and 1 are the gate's
+    const int n = z.n0 + wn * (G::COLS / 4) + 4 * lg;
+    if (!p.out_scale) {
+#pragma unroll
+      for (int i = 0; i < MB; ++i) {
+        const int rl = wm * (BM / 2) + 16 * i + lr;
+        const size_t row = size_t(z.row0) + rl;
+#pragma unroll
+        for (int j = 0; j < (G::GATED ? 2 : NB); ++j)
+          if (rl < z.rows && n + 16 * j < p.N) finish_out<G::GATED>(p, z.stream, row, n + 16 * j, acc[i][j], acc[i][G::GATED ? 2 + j : j]);
+        asm volatile("" ::: "memory");
+      }
+      continue;
+    }
+    if constexpr (G::GATED) {
+      // the tile's 128 columns have one scale a row, from the largest of four waves' 32 columns
+      const uint32_t tops = lds0 + S * WB;
+      f32x4 bias[NB];
+#pragma unroll
+      for (int j = 0; j < NB; ++j) {
+        const void *v = z.stream ? (j / 2 ? p.bias[1][1] : p.bias[1][0]) : (j / 2 ? p.bias[0][1] : p.bias[0][0]);
+        bias[j] = load4(v, min(n + 16 * (j & 1), p.N - 4), p.bf16);
+      }
+#pragma unroll
+      for (int i = 0; i < MB; ++i) {
+        uint32_t top = 0;
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float h = gate_act<false>(acc[i][j][e] + bias[j][e], p.silu) * (acc[i][2 + j][e] + bias[2 + j][e]);
+            acc[i][j][e] = h;
+            top = n + 16 * j < p.N ? max(top, abs_bits(h)) : top;
+          }
+        top = max(top, uint32_t(__shfl_xor(int(top), 16, 64)));
+        top = max(top, uint32_t(__shfl_xor(int(top), 32, 64)));
+        if (lg == 0) asm volatile("ds_write_b32 %0, %1" ::"v"(tops + 16 * (wm * (BM / 2) + 16 * i + lr) + 4 * wn), "v"(top) : "memory");
+      }
+      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+#pragma unroll
+      for (int i = 0; i < MB; ++i) {
+        const int rl = wm * (BM / 2) + 16 * i + lr;
+        u32x4 t;
+        asm volatile("ds_read_b128 %0, %1\n\ts_waitcnt lgkmcnt(0)" : "=v"(t) : "v"(tops + 16 * rl) : "memory");
+        const uint32_t top = max(max(t[0], t[1]), max(t[2], t[3]));
+        const bool finite = top < 0x7f800000u;
+        const int k = finite ? pow2_exponent(__uint_as_float(top)) : 0;
+        const float inv = pow2_inverse(k);
+        uint32_t c[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          c[j] = fp8x4(acc[i][j][0] * inv, acc[i][j][1] * inv, acc[i][j][2] * inv, acc[i][j][3] * inv);
+          c[j] = finite ? c[j] : 0x7f7f7f7fu;
+        }
+        swap16(c[0], c[1]);  // 8 columns of a block a lane
+        const int col = z.n0 + wn * 32 + 16 * (lg & 1) + 8 * (lg >> 1);
+        if (rl < z.rows) {
+          const size_t row = size_t(z.row0) + rl;
+          if (col < p.N) *reinterpret_cast<uint2 *>(reinterpret_cast<uint8_t *>(p.out) + row * p.N + col) = make_uint2(c[0], c[1]);
+          if (wn == 0 && lg == 0) {
+            uint8_t *s = p.out_scale + row * scale_stride(p.N);
+            const int at = z.n0 / 128, end = z.n0 + 128 >= p.N ? scale_stride(p.N) : at + 1;
+            s[at] = finite ? uint8_t(127 + k) : 255;
+            for (int x = at + 1; x < end; ++x) s[x] = 0;
+          }
+        }
+      }
     }
   }
   wait_vm<0>();
@@ -432,18 +651,33 @@ __global__ __launch_bounds__(512) void k_product_fp8_fix(ProductProblem p) {
   else fix8<Geo8<128, 256, GATED>>(p, q);
 }
 
+template <bool GATED>
+__global__ __launch_bounds__(512, 2) void k_product_fp8_wide(ProductProblem p) {
+  using G = GeoW<GATED>;
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[G::LDS];
+  const Plan q = make_plan<G>(p, count_row_tiles(p, G::BM), 1, kCost8[1]);
+  run_wide<G>(p, q, xcd_remap(blockIdx.x, P), lds);
+}
+
 }  // namespace pt
 
 template <bool GATED>
 static hipError_t run_tiles8(ProductProblem p, hipStream_t st) {
   pt::Plan q;
-  p.splits = !p.out_scale;  // codes leave whole tiles
+  p.splits = 1;
   pt::choose8<GATED>(p, [&](int bm) { return (p.rows + bm - 1) / bm; }, q);
   p.splits = q.s > 1;
   hipLaunchKernelGGL((pt::k_product_fp8<GATED>), dim3(pt::P), dim3(512), 0, st, p);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || !p.splits) return e;
   hipLaunchKernelGGL((pt::k_product_fp8_fix<GATED>), dim3(pt::P), dim3(512), 0, st, p);
+  return hipGetLastError();
+}
+
+hipError_t launch_product_fp8_wide(ProductProblem p, hipStream_t st) {
+  p.splits = 0;  // whole tiles
+  if (p.parts == 2) hipLaunchKernelGGL(pt::k_product_fp8_wide<true>, dim3(pt::P), dim3(512), 0, st, p);
+  else hipLaunchKernelGGL(pt::k_product_fp8_wide<false>, dim3(pt::P), dim3(512), 0, st, p);
   return hipGetLastError();
 }
 

@@ -128,5 +128,12 @@ HILO_DEV void read16(u32x4 &d, uint32_t addr) {
   asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(d) : "v"(addr), "n"(OFF) : "memory");
 }
 
+// Exchanges rows of 16 lanes: x gets y's row 0 in its row 1, its row 2 in its row 3; y x's rows 1 and 3 in its rows 0 and 2.
+HILO_DEV void swap16(uint32_t &x, uint32_t &y) {
+  const auto r = __builtin_amdgcn_permlane16_swap(x, y, false, false);
+  x = r[0];
+  y = r[1];
+}
+
 }  // namespace pt
 }  // namespace hilo
