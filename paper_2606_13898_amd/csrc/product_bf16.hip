@@ -27,7 +27,8 @@ struct Geo {
   static constexpr int MB = BM / WM / 16, NB = BN / WN / 16;
   static constexpr int LA = BM / 64, LB = BN / 64;  // load instructions of a wave for a window
   static constexpr int WB = (BM + BN) * 128;
-  static constexpr int SLOTS = 3 * WB <= 160 * 1024 ? 3 : 2;
+  static constexpr int SLOTS = 3 * WB + 2048 <= 160 * 1024 ? 3 : 2;
+  static constexpr int LDS = SLOTS * WB + 2048;  // and 256 bytes a wave for biases
   static constexpr int COLS = GATED ? BN / 2 : BN;  // columns of the output
 };
 
@@ -63,30 +64,49 @@ struct Frag<false> {
 };
 
 // Two blocks of 16 columns of a row, four a lane: lanes of groups 0 and 2 get 8 of the first's, of 1 and 3 of the second's,
-// so that a store writes 64 consecutive bytes of 16 rows.  c: the first block's column.
-HILO_DEV void store_blocks(uint16_t *row, int c, int end, int lg, f32x4 a, f32x4 b, bool inside) {
+// so that a store writes 64 consecutive bytes of 16 rows.  tile: its first row, row: values to the lane's, c: the first
+// block's column.
+HILO_DEV void store_blocks(uint16_t *tile, uint32_t row, int c, int end, int lg, f32x4 a, f32x4 b, bool in) {
   uint32_t x0 = bf16_pair(a[0], a[1]), x1 = bf16_pair(a[2], a[3]), y0 = bf16_pair(b[0], b[1]), y1 = bf16_pair(b[2], b[3]);
   swap16(x0, y0);
   swap16(x1, y1);
   c += 16 * (lg & 1) + 8 * (lg >> 1);
-  if (inside && c < end) *reinterpret_cast<uint4 *>(row + c) = make_uint4(x0, x1, y0, y1);
+  if (in && c < end) *reinterpret_cast<uint4 *>(tile + (row + c)) = make_uint4(x0, x1, y0, y1);
 }
-HILO_DEV void store_block(uint16_t *row, int c, int end, int lg, f32x4 a, bool inside) {
+HILO_DEV void store_block(uint16_t *tile, uint32_t row, int c, int end, int lg, f32x4 a, bool in) {
   c += 4 * lg;
-  if (inside && c < end) *reinterpret_cast<uint2 *>(row + c) = make_uint2(bf16_pair(a[0], a[1]), bf16_pair(a[2], a[3]));
+  if (in && c < end) *reinterpret_cast<uint2 *>(tile + (row + c)) = make_uint2(bf16_pair(a[0], a[1]), bf16_pair(a[2], a[3]));
 }
 
 // Biases of a wave's columns, four a lane of every block.
 template <typename G>
 struct Bias {
   uint2 v[G::NB];
+  HILO_DEV static int part(int j) { return G::GATED ? j / (G::NB / 2) : 0; }
+  HILO_DEV static const void *of_part(const ProductProblem &p, const Place &z, int q) {
+    return z.stream ? (q ? p.bias[1][1] : p.bias[1][0]) : (q ? p.bias[0][1] : p.bias[0][0]);
+  }
   HILO_DEV void load(const ProductProblem &p, const Place &z, int wn, int lg) {
 #pragma unroll
     for (int j = 0; j < G::NB; ++j) {
-      const int part = G::GATED ? j / (G::NB / 2) : 0, jj = G::GATED ? j % (G::NB / 2) : j;
-      const void *b = z.stream ? (part ? p.bias[1][1] : p.bias[1][0]) : (part ? p.bias[0][1] : p.bias[0][0]);
-      const int n = min(z.n0 + wn * (G::COLS / G::WN) + 16 * jj + 4 * lg, p.N - 4);
+      const void *b = of_part(p, z, part(j));
+      const int n = min(z.n0 + wn * (G::COLS / G::WN) + 16 * (G::GATED ? j % (G::NB / 2) : j) + 4 * lg, p.N - 4);
       v[j] = b ? *reinterpret_cast<const uint2 *>(reinterpret_cast<const uint16_t *>(b) + n) : make_uint2(0u, 0u);
+    }
+  }
+  // of what bias_to_lds left
+  HILO_DEV void take(const ProductProblem &p, const Place &z, uint32_t area, int lg) {
+    u32x2 r[G::NB];
+    auto rd = [&](auto jj) __attribute__((always_inline)) {
+      constexpr int j = decltype(jj)::value;
+      if constexpr (j < G::NB) read8<32 * j>(r[j], area + 8 * lg);
+    };
+    rd(Int<0>{}); rd(Int<1>{}); rd(Int<2>{}); rd(Int<3>{});
+    __builtin_amdgcn_s_waitcnt(0xc07f);
+#pragma unroll
+    for (int j = 0; j < G::NB; ++j) {
+      asm volatile("" : "+v"(r[j]));
+      v[j] = of_part(p, z, part(j)) ? make_uint2(r[j][0], r[j][1]) : make_uint2(0u, 0u);
     }
   }
   HILO_DEV f32x4 of(int j) const {
@@ -101,14 +121,15 @@ HILO_DEV void finish_row(const ProductProblem &p, const Place &z, const Bias<G> 
   const int lr = lane & 15, lg = lane >> 4, wn = wid % G::WN;
   const int rl = (wid / G::WN) * (G::BM / G::WM) + 16 * i + lr;
   const bool in = rl < z.rows;
-  const size_t row = size_t(z.row0) + rl;
   const int n = z.n0 + wn * (G::COLS / G::WN), end = G::KIND == PRODUCT_OUT ? p.N : p.K;
   // blocks J0 .. J0 + COUNT - 1
-  auto put = [&](uint16_t *r, auto first, auto count) __attribute__((always_inline)) {
+  auto put = [&](void *out, size_t ld, size_t from, auto first, auto count) __attribute__((always_inline)) {
+    uint16_t *tile = reinterpret_cast<uint16_t *>(out) + size_t(z.row0) * ld + from;
+    const uint32_t r = uint32_t(rl) * uint32_t(ld);
     constexpr int J0 = decltype(first)::value, COUNT = decltype(count)::value;
 #pragma unroll
-    for (int j = 0; j + 1 < COUNT; j += 2) store_blocks(r, n + 16 * j, end, lg, acc[J0 + j], acc[J0 + j + 1], in);
-    if constexpr (COUNT % 2 == 1) store_block(r, n + 16 * (COUNT - 1), end, lg, acc[J0 + COUNT - 1], in);
+    for (int j = 0; j + 1 < COUNT; j += 2) store_blocks(tile, r, n + 16 * j, end, lg, acc[J0 + j], acc[J0 + j + 1], in);
+    if constexpr (COUNT % 2 == 1) store_block(tile, r, n + 16 * (COUNT - 1), end, lg, acc[J0 + COUNT - 1], in);
   };
   if constexpr (G::KIND == PRODUCT_OUT) {
 #pragma unroll
@@ -116,22 +137,21 @@ HILO_DEV void finish_row(const ProductProblem &p, const Place &z, const Bias<G> 
     if constexpr (G::GATED) {
       constexpr int H = G::NB / 2;
       if (p.pre) {
-        uint16_t *pre = reinterpret_cast<uint16_t *>(p.pre) + row * 2 * p.N;
-        put(pre, Int<0>{}, Int<H>{});
-        put(pre + p.N, Int<H>{}, Int<H>{});
+        put(p.pre, 2 * size_t(p.N), 0, Int<0>{}, Int<H>{});
+        put(p.pre, 2 * size_t(p.N), p.N, Int<H>{}, Int<H>{});
       }
 #pragma unroll
       for (int j = 0; j < H; ++j)
 #pragma unroll
         for (int e = 0; e < 4; ++e) acc[j][e] = gate_act<false>(acc[j][e], p.silu) * acc[H + j][e];
-      put(reinterpret_cast<uint16_t *>(p.out) + row * p.N, Int<0>{}, Int<H>{});
+      put(p.out, p.N, 0, Int<0>{}, Int<H>{});
     } else {
-      put(reinterpret_cast<uint16_t *>(p.out) + row * p.N, Int<0>{}, Int<G::NB>{});
+      put(p.out, p.N, 0, Int<0>{}, Int<G::NB>{});
     }
   } else if constexpr (G::KIND == PRODUCT_DX) {
-    put(reinterpret_cast<uint16_t *>(p.dx) + row * p.K, Int<0>{}, Int<G::NB>{});
+    put(p.dx, p.K, 0, Int<0>{}, Int<G::NB>{});
   } else {
-    put(reinterpret_cast<uint16_t *>(p.dw[z.o]) + row * p.K, Int<0>{}, Int<G::NB>{});
+    put(p.dw[z.o], p.K, 0, Int<0>{}, Int<G::NB>{});
   }
 }
 
@@ -391,6 +411,10 @@ HILO_DEV void run(const ProductProblem &p, const Plan &q, int pid, uint8_t *lds)
     const Place z = place_of<G>(p, q, it.t);
     const int n = windows<KIND>(p, z.stream);
     const int w0 = int((long long)n * it.pc / it.n), w1 = int((long long)n * (it.pc + 1) / it.n);
+    uint8_t *area = lds + S * WB + wid * 256;
+    if constexpr (KIND == PRODUCT_OUT) {
+      if (it.n == 1) bias_to_lds<BN / G::WN, G::GATED ? 2 : 1>(p, z, z.n0 + wn * (G::COLS / G::WN), area, true);
+    }
 #pragma unroll
     for (int i = 0; i < MB; ++i)
 #pragma unroll
@@ -413,7 +437,10 @@ HILO_DEV void run(const ProductProblem &p, const Plan &q, int pid, uint8_t *lds)
         for (int j = 0; j < NB; ++j) *reinterpret_cast<f32x4 *>(p.part + part_at<G>(it.slot, wid, i, j, lane)) = acc[i][j];
     } else {
       Bias<G> bias;
-      if constexpr (KIND == PRODUCT_OUT) bias.load(p, z, wn, lane >> 4);
+      if constexpr (KIND == PRODUCT_OUT) {
+        if (w1 - w0 < S) wait_vm<0>();  // the biases may still be on their way
+        bias.take(p, z, lds0 + S * WB + wid * 256, lane >> 4);
+      }
 #pragma unroll
       for (int i = 0; i < MB; ++i) {
         finish_row<G>(p, z, bias, wid, i, lane, acc[i]);
@@ -485,7 +512,7 @@ HILO_DEV int choose(const ProductProblem &p, Plan &q) {
 
 template <int KIND, bool GATED>
 __global__ __launch_bounds__(512, 2) void k_product_tiles(ProductProblem p) {
-  constexpr auto bytes = [](auto g) { return decltype(g)::WB * decltype(g)::SLOTS; };
+  constexpr auto bytes = [](auto g) { return decltype(g)::LDS; };
   constexpr int L0 = bytes(Tile<0, KIND, GATED>{}), L1 = bytes(Tile<1, KIND, GATED>{}), L2 = bytes(Tile<2, KIND, GATED>{});
   __shared__ __attribute__((aligned(1024))) uint8_t lds[std::max(L0, std::max(L1, L2))];
   const int pid = xcd_remap(blockIdx.x, P);

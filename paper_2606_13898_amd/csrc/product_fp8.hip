@@ -29,8 +29,8 @@ struct Geo8 {
   static constexpr int LA = BM / 64, LB = BN / 64;
   static constexpr int WB = (BM + BN) * 128;
   static constexpr int RING = 4, RB = BM * 4;        // windows' scales of x, bytes of one
-  static constexpr int SLOTS = 3 * WB + RING * RB <= 160 * 1024 ? 3 : 2;
-  static constexpr int LDS = SLOTS * WB + RING * RB;
+  static constexpr int SLOTS = 3 * WB + RING * RB + 2048 <= 160 * 1024 ? 3 : 2;
+  static constexpr int AREAS = SLOTS * WB + RING * RB, LDS = AREAS + 2048;  // 256 bytes a wave for biases
   static constexpr int COLS = GATED ? BN / 2 : BN;
   static_assert(RING > SLOTS, "a window's scales last until it is multiplied");
   static_assert(!GATED || NB == 2, "a block of either part");
@@ -52,14 +52,6 @@ HILO_DEV i32x8 cat8(u32x4 lo, u32x4 hi) {
   return __builtin_bit_cast(i32x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
-// 16 values of a vector of the bias' type, or zeros
-HILO_DEV void load16(const void *v, int n, bool bf16, float (&f)[16]) {
-#pragma unroll
-  for (int e = 0; e < 16; e += 4) {
-    const f32x4 q = load4(v, size_t(n) + e, bf16);
-    f[e] = q[0]; f[e + 1] = q[1]; f[e + 2] = q[2]; f[e + 3] = q[3];
-  }
-}
 HILO_DEV void store16(uint16_t *o, const float (&v)[16]) {
 #pragma unroll
   for (int h = 0; h < 2; ++h)
@@ -72,35 +64,65 @@ template <typename G>
 HILO_DEV int col8(const Place &z, int wn, int j, int g) {
   return z.n0 + wn * (G::COLS / 4) + (G::GATED ? 0 : 32 * j) + 16 * g;
 }
+// Biases of a lane's 16 columns of every block, bf16.
 template <typename G>
-HILO_DEV void load_bias(const ProductProblem &p, const Place &z, int wn, int g, float (&bias)[G::NB][16]) {
-#pragma unroll
-  for (int j = 0; j < G::NB; ++j) {
-    const int part = G::GATED ? j : 0;
-    const void *b = z.stream ? (part ? p.bias[1][1] : p.bias[1][0]) : (part ? p.bias[0][1] : p.bias[0][0]);
-    load16(b, min(col8<G>(z, wn, j, g), p.N - 16), p.bf16, bias[j]);
+struct Bias8 {
+  u32x4 v[G::NB][2];
+  HILO_DEV static const void *of_block(const ProductProblem &p, const Place &z, int j) {
+    const int q = G::GATED ? j : 0;
+    return z.stream ? (q ? p.bias[1][1] : p.bias[1][0]) : (q ? p.bias[0][1] : p.bias[0][0]);
   }
-}
-// act(g) u of a row's 16 columns, in place of the gate's sums
-template <typename V>
-HILO_DEV void gate16(const ProductProblem &p, const float (&bg)[16], const float (&bu)[16], V &g, const V &u) {
+  HILO_DEV void load(const ProductProblem &p, const Place &z, int wn, int g) {
 #pragma unroll
-  for (int e = 0; e < 16; ++e) g[e] = gate_act<false>(g[e] + bg[e], p.silu) * (u[e] + bu[e]);
-}
+    for (int j = 0; j < G::NB; ++j) {
+      const uint16_t *b = reinterpret_cast<const uint16_t *>(of_block(p, z, j));
+      const int n = min(col8<G>(z, wn, j, g), p.N - 16);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) v[j][h] = b ? *reinterpret_cast<const u32x4 *>(b + n + 8 * h) : u32x4(0u);
+    }
+  }
+  // of what bias_to_lds left
+  HILO_DEV void take(const ProductProblem &p, const Place &z, uint32_t area, int g) {
+    auto rd = [&](auto jj) __attribute__((always_inline)) {
+      constexpr int j = decltype(jj)::value;
+      if constexpr (j < G::NB) {
+        read16<64 * j>(v[j][0], area + 32 * g);
+        read16<64 * j + 16>(v[j][1], area + 32 * g);
+      }
+    };
+    rd(Int<0>{}); rd(Int<1>{});
+    __builtin_amdgcn_s_waitcnt(0xc07f);
+#pragma unroll
+    for (int j = 0; j < G::NB; ++j)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        asm volatile("" : "+v"(v[j][h]));
+        if (!of_block(p, z, j)) v[j][h] = u32x4(0u);
+      }
+  }
+  HILO_DEV float of(int j, int e) const {
+    const uint32_t w = v[j][e >> 3][(e >> 1) & 3];
+    return __uint_as_float(e & 1 ? w & 0xffff0000u : w << 16);
+  }
+};
 
 // The last step of a row block but for codes: rows 32 i + l % 32 of the wave's.
 template <typename G>
-HILO_DEV void finish8(const ProductProblem &p, const Place &z, const float (&bias)[G::NB][16], int wid, int i, int lane, f32x16 (&acc)[G::NB]) {
+HILO_DEV void finish8(const ProductProblem &p, const Place &z, const Bias8<G> &bias, int wid, int i, int lane, f32x16 (&acc)[G::NB]) {
   const int rl = (wid >> 2) * (G::BM / 2) + 32 * i + (lane & 31), wn = wid & 3, g = lane >> 5;
-  const size_t row = size_t(z.row0) + rl;
-  if constexpr (G::GATED) gate16(p, bias[0], bias[1], acc[0], acc[1]);
+  uint16_t *tile = reinterpret_cast<uint16_t *>(p.out) + size_t(z.row0) * p.N;
+  const uint32_t row = uint32_t(rl) * uint32_t(p.N);
+  if constexpr (G::GATED) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) acc[0][e] = gate_act<false>(acc[0][e] + bias.of(0, e), p.silu) * (acc[1][e] + bias.of(1, e));
+  }
 #pragma unroll
   for (int j = 0; j < (G::GATED ? 1 : G::NB); ++j) {
     const int n = col8<G>(z, wn, j, g);
     float v[16];
 #pragma unroll
-    for (int e = 0; e < 16; ++e) v[e] = G::GATED ? acc[j][e] : acc[j][e] + bias[j][e];
-    if (rl < z.rows && n < p.N) store16(reinterpret_cast<uint16_t *>(p.out) + row * p.N + n, v);
+    for (int e = 0; e < 16; ++e) v[e] = G::GATED ? acc[j][e] : acc[j][e] + bias.of(j, e);
+    if (rl < z.rows && n < p.N) store16(tile + (row + uint32_t(n)), v);
   }
 }
 
@@ -119,8 +141,7 @@ struct Loads8 {
   int wid;
   uint32_t ld, lds_scale;
   int nk;
-  // the chunk of instruction i (8 rows) is that of instruction 0, or its bit 2 the other way round
-  uint32_t oa[2], ob[2];
+  uint32_t oa, ob;  // of instruction 0
   int lu, slot = 0, ring = 0, w = 0, we = 0, rows = 0;
   const char *la = nullptr, *lb = nullptr, *lsc = nullptr;
   uint32_t ra = 0, rb = 0;
@@ -130,11 +151,8 @@ struct Loads8 {
       : p(p_), q(q_), lds(lds_), wid(wid_), ld(p_.K), lds_scale(scale_stride(p_.K)), nk((p_.K + 127) / 128), lu(pid) {
     const int lane = threadIdx.x & 63, r = lane >> 3;
     const int wrow = G::GATED ? (wid >> 1) * (BN / 8) : wid * (BN / 8);  // first row of W, of its part, that the wave loads
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      oa[i] = uint32_t(wid * (BM / 8) + r) * ld + 16u * ((lane & 7) ^ swz(wid * (BM / 8) + r) ^ (4 * i));
-      ob[i] = uint32_t(wrow + r) * ld + 16u * ((lane & 7) ^ swz(wid * (BN / 8) + r) ^ (4 * i));
-    }
+    oa = uint32_t(wid * (BM / 8) + r) * ld + 16u * ((lane & 7) ^ swz(wid * (BM / 8) + r));
+    ob = uint32_t(wrow + r) * ld + 16u * ((lane & 7) ^ swz(wid * (BN / 8) + r));
   }
   // to the next item where this one ends
   HILO_DEV void step() {
@@ -158,10 +176,10 @@ struct Loads8 {
     rb = uint32_t(min(G::COLS, p.N - z.n0)) * ld;
   }
   template <int L>
-  HILO_DEV void window(const char *base, uint32_t reach, const uint32_t (&o)[2], int lds_base, uint8_t *d) {
-    // chunks of k behind the end: offsets behind the buffer's
+  HILO_DEV void window(const char *base, uint32_t reach, uint32_t o, int lds_base, uint8_t *d) {
+    // the chunk of instruction i (8 rows) is that of instruction 0, or its bit 2 the other way round; chunks of k behind the end: offsets behind the buffer's
     const int kv = p.K - 128 * w, lane = opaque(threadIdx.x & 63), c = (lane & 7) ^ swz(lds_base + (lane >> 3));
-    const uint32_t o0 = 16 * c < kv ? o[0] : kBehind, o1 = 16 * (c ^ 4) < kv ? o[1] : kBehind;
+    const uint32_t o0 = 16 * c < kv ? o : kBehind, o1 = 16 * (c ^ 4) < kv ? o + (c & 4 ? -64 : 64) : kBehind;
     const uint32_t bytes = more ? reach - 128u * uint32_t(w) : 0u;
     base += size_t(w) * 128;
 #pragma unroll
@@ -308,6 +326,7 @@ HILO_DEV void run8(const ProductProblem &p, const Plan &q, int pid, uint8_t *lds
       const uint8_t *s = z.stream ? (j ? p.w_scale[1][1] : p.w_scale[1][0]) : (j ? p.w_scale[0][1] : p.w_scale[0][0]);
       ws[j] = s + size_t((G::GATED ? z.n0 : min(z.n0 + wn * (BN / 4), p.N - 1)) / 128) * loads.lds_scale;
     }
+    if (it.n == 1) bias_to_lds<BN / 4, G::GATED ? 2 : 1>(p, z, z.n0 + wn * (G::COLS / 4), lds + G::AREAS + wid * 256, true);
 #pragma unroll
     for (int i = 0; i < MB; ++i)
 #pragma unroll
@@ -336,8 +355,9 @@ HILO_DEV void run8(const ProductProblem &p, const Plan &q, int pid, uint8_t *lds
         for (int j = 0; j < NB; ++j) *reinterpret_cast<f32x16 *>(p.part + part_at8<G>(it.slot, wid, i, j, lane)) = acc[i][j];
       continue;
     }
-    float bias[NB][16];
-    load_bias<G>(p, z, wn, lane >> 5, bias);
+    Bias8<G> bias;
+    if (w1 - w0 < S) wait_vm<0>();  // the biases may still be on their way
+    bias.take(p, z, lds0 + G::AREAS + wid * 256, lane >> 5);
 #pragma unroll
     for (int i = 0; i < MB; ++i) {
       finish8<G>(p, z, bias, wid, i, lane, acc[i]);
@@ -361,9 +381,22 @@ struct GeoW {
   static constexpr int COLS = GATED ? BN / 2 : BN;
   static constexpr int WA = BM * 128, WB = WA + BN * 64, SLOTS = 4;
   static constexpr int TOPS = BM * 16;  // codes out: a row's largest values by wave
-  static constexpr int LDS = SLOTS * WB + TOPS;
+  static constexpr int AREAS = SLOTS * WB + TOPS, LDS = AREAS + 2048;  // 256 bytes a wave for biases
   static_assert(LDS <= 160 * 1024, "LDS");
 };
+
+// Four of a wave's biases from value i on, of either type.
+HILO_DEV f32x4 take_bias4(uint32_t area, int i, bool some, bool bf16) {
+  u32x4 r;
+  u32x2 h;
+  if (bf16) {
+    asm volatile("ds_read_b64 %0, %1\n\ts_waitcnt lgkmcnt(0)" : "=v"(h) : "v"(area + 2 * i) : "memory");
+    r = u32x4{h[0] << 16, h[0] & 0xffff0000u, h[1] << 16, h[1] & 0xffff0000u};
+  } else {
+    asm volatile("ds_read_b128 %0, %1\n\ts_waitcnt lgkmcnt(0)" : "=v"(r) : "v"(area + 4 * i) : "memory");
+  }
+  return some ? __builtin_bit_cast(f32x4, r) : f32x4(0.f);
+}
 
 template <typename G>
 HILO_DEV void run_wide(const ProductProblem &p, const Plan &q, int pid, uint8_t *lds) {
@@ -425,34 +458,64 @@ HILO_DEV void run_wide(const ProductProblem &p, const Plan &q, int pid, uint8_t 
   for (int h = 0; h < 2; ++h) fa[h] = lds0 + (wm * (BM / 2) + lr) * 128 + ((2 * lg + h) ^ ((lr >> 1) & 7)) * 16;
   const uint32_t fb = lds0 + WA + (wn * (BN / 4) + lr) * 64 + (lg ^ ((lr >> 2) & 3)) * 16;
   f32x4 acc[MB][NB];
-  u32x4 a[2][MB], b[NB];  // halves of x's window; all of W's
+  u32x4 a[2][2][MB], b[2][NB];  // two windows: x by halves, W
   bf16x8 wb[2][NB];
   uint32_t so = 0;
-  auto rd_a = [&](auto hh, auto ii) __attribute__((always_inline)) {
-    constexpr int h = decltype(hh)::value, i = decltype(ii)::value;
-    read16<i * 2048>(a[h][i], fa[h] + so);
+  auto read = [&](auto set) __attribute__((always_inline)) {
+    constexpr int s = decltype(set)::value;
+    read16<0>(b[s][0], fb + so); read16<1024>(b[s][1], fb + so); read16<2048>(b[s][2], fb + so); read16<3072>(b[s][3], fb + so);
+    read16<0>(a[s][0][0], fa[0] + so); read16<2048>(a[s][0][1], fa[0] + so);
+    read16<4096>(a[s][0][2], fa[0] + so); read16<6144>(a[s][0][3], fa[0] + so);
+    read16<0>(a[s][1][0], fa[1] + so); read16<2048>(a[s][1][1], fa[1] + so);
+    read16<4096>(a[s][1][2], fa[1] + so); read16<6144>(a[s][1][3], fa[1] + so);
   };
-  auto rd_b = [&](auto jj) __attribute__((always_inline)) {
-    constexpr int j = decltype(jj)::value;
-    read16<j * 1024>(b[j], fb + so);
+  auto wait = [&](auto set) __attribute__((always_inline)) {
+    constexpr int s = decltype(set)::value;
+    __builtin_amdgcn_s_waitcnt(0xc07f);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      asm volatile("" : "+v"(a[s][0][i]));
+      asm volatile("" : "+v"(a[s][1][i]));
+      asm volatile("" : "+v"(b[s][i]));
+    }
+    __builtin_amdgcn_sched_barrier(0);
   };
-  auto pin = [&](u32x4 &v) __attribute__((always_inline)) { asm volatile("" : "+v"(v)); };
   const uint8_t *ws[2] = {nullptr, nullptr};
   auto scale = [&](int j, int w) __attribute__((always_inline)) {  // of part j, block w / 2: a float32 number's exponent
     return (scales_at(ws[G::GATED ? j : 0], w >> 3) >> (4 * (w & 6)) & 255u) << 23;
   };
-  // wb of half h
-  auto widen = [&](auto hh, uint32_t s0, uint32_t s1) __attribute__((always_inline)) {
-    constexpr int h = decltype(hh)::value;
+  uint32_t s0, s1;
+  // the window in a set, while the next one is read into the other; one barrier, at which every wave has read this window
+  auto window = [&](auto set, int w) __attribute__((always_inline)) {
+    constexpr int s = decltype(set)::value;
+    auto widen = [&](int h, int j) __attribute__((always_inline)) { wb[h][j] = wide_codes(b[s][j][2 * h], b[s][j][2 * h + 1], j < NB / 2 ? s0 : s1); };
+    auto row = [&](int h, int i) __attribute__((always_inline)) {
 #pragma unroll
-    for (int j = 0; j < NB; ++j) wb[h][j] = wide_codes(b[j][2 * h], b[j][2 * h + 1], j < NB / 2 ? s0 : s1);
-  };
-  // row block i of half h
-  auto row = [&](auto hh, auto ii) __attribute__((always_inline)) {
-    constexpr int h = decltype(hh)::value, i = decltype(ii)::value;
+      for (int j = 0; j < NB; ++j)
+        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wb[h][j], __builtin_bit_cast(bf16x8, a[s][h][i]), acc[i][j], 0, 0, 0);
+    };
+    ld_step();
+    wait_vm<(S - 2) * L>();
+    asm volatile("s_barrier" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    so = so == (S - 1) * WB ? 0 : so + WB;
+    read(Int<1 - s>{});
+    ld();
 #pragma unroll
-    for (int j = 0; j < NB; ++j)
-      acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wb[h][j], __builtin_bit_cast(bf16x8, a[h][i]), acc[i][j], 0, 0, 0);
+    for (int j = 0; j < NB; ++j) widen(0, j);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < MB; ++i) {
+      row(0, i);
+      widen(1, i);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    s0 = scale(0, min(w + 1, nk - 1));
+    s1 = scale(1, min(w + 1, nk - 1));
+#pragma unroll
+    for (int i = 0; i < MB; ++i) row(1, i);
+    __builtin_amdgcn_sched_barrier(0);
+    wait(Int<1 - s>{});
   };
 #pragma unroll 1
   for (int w = 0; w < S; ++w) {
@@ -470,57 +533,22 @@ HILO_DEV void run_wide(const ProductProblem &p, const Plan &q, int pid, uint8_t 
       const uint8_t *s = z.stream ? (j ? p.w_scale[1][1] : p.w_scale[1][0]) : (j ? p.w_scale[0][1] : p.w_scale[0][0]);
       ws[j] = s + size_t((G::GATED ? z.n0 : min(z.n0 + wn * (BN / 4), p.N - 1)) / 128) * stride;
     }
+    if (G::GATED && p.out_scale) bias_to_lds<BN / 4, 2>(p, z, z.n0 + wn * (G::COLS / 4), lds + G::AREAS + wid * 256, p.bf16);
 #pragma unroll
     for (int i = 0; i < MB; ++i)
 #pragma unroll
       for (int j = 0; j < NB; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    rd_b(Int<0>{}); rd_b(Int<1>{}); rd_b(Int<2>{}); rd_b(Int<3>{});
-    rd_a(Int<0>{}, Int<0>{}); rd_a(Int<0>{}, Int<1>{}); rd_a(Int<0>{}, Int<2>{}); rd_a(Int<0>{}, Int<3>{});
-    __builtin_amdgcn_s_waitcnt(0xc07f);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      pin(a[0][i]);
-      pin(b[i]);
-    }
-    uint32_t s0 = scale(0, 0), s1 = scale(1, 0);
-    widen(Int<0>{}, s0, s1);
+    s0 = scale(0, 0);
+    s1 = scale(1, 0);
+    read(Int<0>{});
+    wait(Int<0>{});
+    int w = 0;
 #pragma unroll 1
-    for (int w = 0; w < nk; ++w) {
-      ld_step();
-      // half 0, beside it half 1's rows of x read and W's codes of half 1 widened
-      rd_a(Int<1>{}, Int<0>{}); rd_a(Int<1>{}, Int<1>{}); rd_a(Int<1>{}, Int<2>{}); rd_a(Int<1>{}, Int<3>{});
-      __builtin_amdgcn_sched_barrier(0);
-      row(Int<0>{}, Int<0>{}); row(Int<0>{}, Int<1>{}); row(Int<0>{}, Int<2>{}); row(Int<0>{}, Int<3>{});
-      widen(Int<1>{}, s0, s1);
-      s0 = scale(0, min(w + 1, nk - 1));
-      s1 = scale(1, min(w + 1, nk - 1));
-      __builtin_amdgcn_s_waitcnt(0xc07f);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) pin(a[1][i]);
-      __builtin_amdgcn_sched_barrier(0);
-      // this wave has read the window, and all but the last issued windows have landed; on to the next
-      wait_vm<(S - 2) * L>();
-      asm volatile("s_barrier" ::: "memory");
-      __builtin_amdgcn_sched_barrier(0);
-      so = so == (S - 1) * WB ? 0 : so + WB;
-      rd_b(Int<0>{}); rd_b(Int<1>{}); rd_b(Int<2>{}); rd_b(Int<3>{});
-      rd_a(Int<0>{}, Int<0>{}); rd_a(Int<0>{}, Int<1>{}); rd_a(Int<0>{}, Int<2>{}); rd_a(Int<0>{}, Int<3>{});
-      __builtin_amdgcn_sched_barrier(0);
-      row(Int<1>{}, Int<0>{}); row(Int<1>{}, Int<1>{});
-      __builtin_amdgcn_sched_barrier(0);
-      ld();
-      __builtin_amdgcn_s_waitcnt(0xc07f);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        pin(a[0][i]);
-        pin(b[i]);
-      }
-      __builtin_amdgcn_sched_barrier(0);
-      // the next window's half 0 beside the other rows of half 1
-      row(Int<1>{}, Int<2>{}); row(Int<1>{}, Int<3>{});
-      widen(Int<0>{}, s0, s1);
-      __builtin_amdgcn_sched_barrier(0);
+    for (; w + 1 < nk; w += 2) {
+      window(Int<0>{}, w);
+      window(Int<1>{}, w + 1);
     }
+    if (w < nk) window(Int<0>{}, w);
     const int lane = opaque(threadIdx.x & 63), lr = lane & 15, lg = lane >> 4;
     // lane (lr, lg): rows 16 i + lr, columns 16 j + 4 lg .. + 3 of block j; with a gate blocks 0 and 1 are the gate's
     const int n = z.n0 + wn * (G::COLS / 4) + 4 * lg;
@@ -540,10 +568,11 @@ HILO_DEV void run_wide(const ProductProblem &p, const Plan &q, int pid, uint8_t 
       // the tile's 128 columns have one scale a row, from the largest of four waves' 32 columns
       const uint32_t tops = lds0 + S * WB;
       f32x4 bias[NB];
+      if (nk < S) wait_vm<0>();  // the biases may still be on their way
 #pragma unroll
       for (int j = 0; j < NB; ++j) {
         const void *v = z.stream ? (j / 2 ? p.bias[1][1] : p.bias[1][0]) : (j / 2 ? p.bias[0][1] : p.bias[0][0]);
-        bias[j] = load4(v, min(n + 16 * (j & 1), p.N - 4), p.bf16);
+        bias[j] = take_bias4(lds0 + G::AREAS + wid * 256, 32 * (j / 2) + 16 * (j & 1) + 4 * lg, v != nullptr, p.bf16);
       }
 #pragma unroll
       for (int i = 0; i < MB; ++i) {
@@ -556,8 +585,12 @@ HILO_DEV void run_wide(const ProductProblem &p, const Plan &q, int pid, uint8_t 
             acc[i][j][e] = h;
             top = n + 16 * j < p.N ? max(top, abs_bits(h)) : top;
           }
-        top = max(top, uint32_t(__shfl_xor(int(top), 16, 64)));
-        top = max(top, uint32_t(__shfl_xor(int(top), 32, 64)));
+        uint32_t other = top;
+        swap16(top, other);
+        top = max(top, other);
+        other = top;
+        swap32(top, other);
+        top = max(top, other);
         if (lg == 0) asm volatile("ds_write_b32 %0, %1" ::"v"(tops + 16 * (wm * (BM / 2) + 16 * i + lr) + 4 * wn), "v"(top) : "memory");
       }
       asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
@@ -602,8 +635,8 @@ HILO_DEV void fix8(const ProductProblem &p, const Plan &q) {
   for (int x = blockIdx.x * 8 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); x < items; x += gridDim.x * 8) {
     const int v = x / (8 * G::MB), rem = x - v * 8 * G::MB, wid = rem / G::MB, i = rem - wid * G::MB;
     const Place z = place_of<G>(p, q, q.full + v);
-    float bias[G::NB][16];
-    load_bias<G>(p, z, wid & 3, lane >> 5, bias);
+    Bias8<G> bias;
+    bias.load(p, z, wid & 3, lane >> 5);
     f32x16 acc[G::NB];
 #pragma unroll
     for (int j = 0; j < G::NB; ++j) acc[j] = f32x16(0.f);

@@ -135,5 +135,30 @@ HILO_DEV void swap16(uint32_t &x, uint32_t &y) {
   y = r[1];
 }
 
+// The same of halves of 32 lanes.
+HILO_DEV void swap32(uint32_t &x, uint32_t &y) {
+  const auto r = __builtin_amdgcn_permlane32_swap(x, y, false, false);
+  x = r[0];
+  y = r[1];
+}
+
+// Biases of a wave's WC columns (PARTS: half of either part) for the end of its tile: by a direct load to LDS when the tile begins, as
+// they lie in memory, so that nothing is waited for then.  n: the wave's first column of its part; area: 256 bytes.
+template <int WC, int PARTS>
+HILO_DEV void bias_to_lds(const ProductProblem &p, const Place &z, int n, void *area, bool bf16) {
+  const char *b[2];
+#pragma unroll
+  for (int q = 0; q < 2; ++q) b[q] = reinterpret_cast<const char *>(z.stream ? (q ? p.bias[1][1] : p.bias[1][0]) : (q ? p.bias[0][1] : p.bias[0][0]));
+  if (!b[0] && (PARTS == 1 || !b[1])) return;
+  const int each = bf16 ? 2 : 1, at = opaque(threadIdx.x & 63) * each % WC;  // values of a lane's 4 bytes
+  const int part = at / (WC / PARTS), col = at % (WC / PARTS);
+  const char *base = PARTS == 1 || (part == 0 ? b[0] != nullptr : b[1] == nullptr) ? b[0] : b[1];  // a part without: the other's
+  __builtin_amdgcn_global_load_lds(base + size_t(min(n + col, p.N - each)) * (4 / each), (__attribute__((address_space(3))) void *)area, 4, 0, 0);
+}
+template <int OFF>
+HILO_DEV void read8(u32x2 &d, uint32_t addr) {
+  asm volatile("ds_read_b64 %0, %1 offset:%2" : "=v"(d) : "v"(addr), "n"(OFF) : "memory");
+}
+
 }  // namespace pt
 }  // namespace hilo
