@@ -458,71 +458,73 @@ HILO_DEV void run_wide(const ProductProblem &p, const Plan &q, int pid, uint8_t 
   for (int h = 0; h < 2; ++h) fa[h] = lds0 + (wm * (BM / 2) + lr) * 128 + ((2 * lg + h) ^ ((lr >> 1) & 7)) * 16;
   const uint32_t fb = lds0 + WA + (wn * (BN / 4) + lr) * 64 + (lg ^ ((lr >> 2) & 3)) * 16;
   f32x4 acc[MB][NB];
-  u32x4 a[2][2][MB], b[2][NB];  // two windows: x by halves, W
-  bf16x8 wb[2][NB];
-  uint32_t so = 0;
-  auto read = [&](auto set) __attribute__((always_inline)) {
-    constexpr int s = decltype(set)::value;
-    read16<0>(b[s][0], fb + so); read16<1024>(b[s][1], fb + so); read16<2048>(b[s][2], fb + so); read16<3072>(b[s][3], fb + so);
-    read16<0>(a[s][0][0], fa[0] + so); read16<2048>(a[s][0][1], fa[0] + so);
-    read16<4096>(a[s][0][2], fa[0] + so); read16<6144>(a[s][0][3], fa[0] + so);
-    read16<0>(a[s][1][0], fa[1] + so); read16<2048>(a[s][1][1], fa[1] + so);
-    read16<4096>(a[s][1][2], fa[1] + so); read16<6144>(a[s][1][3], fa[1] + so);
+  // of two windows: x by halves; W's codes, read a window before they are widened, and that one before they are multiplied
+  u32x4 a[2][2][MB], b[2][NB];
+  bf16x8 wb[2][2][NB];
+  uint32_t so = 0, so1 = WB, so2 = 2 * WB;  // byte offsets of this window and of the next two
+  const uint8_t *ws[2] = {nullptr, nullptr};
+  uint32_t s0, s1;  // of the window that is widened
+  auto scales = [&](int w) __attribute__((always_inline)) {  // of block w / 2: a float32 number's exponent
+    const int shift = 4 * (w & 6);
+    s0 = (scales_at(ws[0], w >> 3) >> shift & 255u) << 23;
+    s1 = (scales_at(ws[G::GATED ? 1 : 0], w >> 3) >> shift & 255u) << 23;
   };
-  auto wait = [&](auto set) __attribute__((always_inline)) {
+  auto rd_a = [&](auto set, auto gg) __attribute__((always_inline)) {
+    constexpr int s = decltype(set)::value, h = decltype(gg)::value / 4, i = decltype(gg)::value % 4;
+    read16<i * 2048>(a[s][h][i], fa[h] + so1);
+  };
+  auto rd_b = [&](auto set, auto jj, uint32_t at) __attribute__((always_inline)) {
+    constexpr int s = decltype(set)::value, j = decltype(jj)::value;
+    read16<j * 1024>(b[s][j], fb + at);
+  };
+  auto wait = [&](auto set) __attribute__((always_inline)) {  // for a of a set, b of the other
     constexpr int s = decltype(set)::value;
+    __builtin_amdgcn_sched_barrier(0);
     __builtin_amdgcn_s_waitcnt(0xc07f);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       asm volatile("" : "+v"(a[s][0][i]));
       asm volatile("" : "+v"(a[s][1][i]));
-      asm volatile("" : "+v"(b[s][i]));
+      asm volatile("" : "+v"(b[1 - s][i]));
     }
     __builtin_amdgcn_sched_barrier(0);
   };
-  const uint8_t *ws[2] = {nullptr, nullptr};
-  auto scale = [&](int j, int w) __attribute__((always_inline)) {  // of part j, block w / 2: a float32 number's exponent
-    return (scales_at(ws[G::GATED ? j : 0], w >> 3) >> (4 * (w & 6)) & 255u) << 23;
-  };
-  uint32_t s0, s1;
-  // the window in a set, while the next one is read into the other; one barrier, at which every wave has read this window
+  // window w of a set, while W's codes of w + 1 are widened, x of w + 1 and W of w + 2 are read.  One barrier, at which every
+  // wave has read window w
   auto window = [&](auto set, int w) __attribute__((always_inline)) {
     constexpr int s = decltype(set)::value;
-    auto widen = [&](int h, int j) __attribute__((always_inline)) { wb[h][j] = wide_codes(b[s][j][2 * h], b[s][j][2 * h + 1], j < NB / 2 ? s0 : s1); };
-    auto row = [&](int h, int i) __attribute__((always_inline)) {
-#pragma unroll
-      for (int j = 0; j < NB; ++j)
-        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wb[h][j], __builtin_bit_cast(bf16x8, a[s][h][i]), acc[i][j], 0, 0, 0);
-    };
     ld_step();
-    wait_vm<(S - 2) * L>();
+    wait_vm<(S - 3) * L>();
     asm volatile("s_barrier" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
-    so = so == (S - 1) * WB ? 0 : so + WB;
-    read(Int<1 - s>{});
-    ld();
+    auto group = [&](auto gg) __attribute__((always_inline)) {
+      constexpr int g = decltype(gg)::value, h = g / 4, i = g % 4;
 #pragma unroll
-    for (int j = 0; j < NB; ++j) widen(0, j);
-    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int i = 0; i < MB; ++i) {
-      row(0, i);
-      widen(1, i);
+      for (int j = 0; j < NB; ++j)
+        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wb[s][h][j], __builtin_bit_cast(bf16x8, a[s][h][i]), acc[i][j], 0, 0, 0);
+      wb[1 - s][h][i] = wide_codes(b[1 - s][i][2 * h], b[1 - s][i][2 * h + 1], i < NB / 2 ? s0 : s1);
+      if constexpr (g < 4) {
+        rd_b(Int<s>{}, Int<g>{}, so2);
+        rd_a(Int<1 - s>{}, Int<2 * g>{});
+        rd_a(Int<1 - s>{}, Int<2 * g + 1>{});
+      }
+      if constexpr (g == 4) ld();
       __builtin_amdgcn_sched_barrier(0);
-    }
-    s0 = scale(0, min(w + 1, nk - 1));
-    s1 = scale(1, min(w + 1, nk - 1));
-#pragma unroll
-    for (int i = 0; i < MB; ++i) row(1, i);
-    __builtin_amdgcn_sched_barrier(0);
+    };
+    group(Int<0>{}); group(Int<1>{}); group(Int<2>{}); group(Int<3>{});
+    group(Int<4>{}); group(Int<5>{}); group(Int<6>{}); group(Int<7>{});
+    scales(min(w + 2, nk - 1));
     wait(Int<1 - s>{});
+    so = so1;
+    so1 = so2;
+    so2 = so2 == (S - 1) * WB ? 0 : so2 + WB;
   };
 #pragma unroll 1
   for (int w = 0; w < S; ++w) {
     ld_step();
     ld();
   }
-  wait_vm<(S - 1) * L>();
+  wait_vm<(S - 2) * L>();
   asm volatile("s_barrier" ::: "memory");
   for (int u = pid;; u += P) {
     const Item it = item_at(q, u);
@@ -538,10 +540,25 @@ HILO_DEV void run_wide(const ProductProblem &p, const Plan &q, int pid, uint8_t 
     for (int i = 0; i < MB; ++i)
 #pragma unroll
       for (int j = 0; j < NB; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    s0 = scale(0, 0);
-    s1 = scale(1, 0);
-    read(Int<0>{});
+    // the first window and W of the second: all have landed
+    rd_b(Int<0>{}, Int<0>{}, so); rd_b(Int<0>{}, Int<1>{}, so); rd_b(Int<0>{}, Int<2>{}, so); rd_b(Int<0>{}, Int<3>{}, so);
+    rd_b(Int<1>{}, Int<0>{}, so1); rd_b(Int<1>{}, Int<1>{}, so1); rd_b(Int<1>{}, Int<2>{}, so1); rd_b(Int<1>{}, Int<3>{}, so1);
+    {
+      const uint32_t next = so1;
+      so1 = so;
+      rd_a(Int<0>{}, Int<0>{}); rd_a(Int<0>{}, Int<1>{}); rd_a(Int<0>{}, Int<2>{}); rd_a(Int<0>{}, Int<3>{});
+      rd_a(Int<0>{}, Int<4>{}); rd_a(Int<0>{}, Int<5>{}); rd_a(Int<0>{}, Int<6>{}); rd_a(Int<0>{}, Int<7>{});
+      so1 = next;
+    }
+    scales(0);
     wait(Int<0>{});
+#pragma unroll
+    for (int j = 0; j < NB; ++j) {
+      asm volatile("" : "+v"(b[0][j]));
+#pragma unroll
+      for (int h = 0; h < 2; ++h) wb[0][h][j] = wide_codes(b[0][j][2 * h], b[0][j][2 * h + 1], j < NB / 2 ? s0 : s1);
+    }
+    scales(min(1, nk - 1));
     int w = 0;
 #pragma unroll 1
     for (; w + 1 < nk; w += 2) {
