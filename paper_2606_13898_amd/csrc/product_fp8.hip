@@ -370,18 +370,18 @@ HILO_DEV void run8(const ProductProblem &p, const Plan &q, int pid, uint8_t *lds
 // Where the instruction's 13 bits are too few -- codes out, since h next to the border between two codes gets the other one
 // some ten times as often as with float32 sums, and float32 out -- the products are of bf16, which holds a code times its
 // scale exactly, at half the rate.  x comes as such bf16 rows (k_widen_rows); W's codes are widened behind LDS, 16 of a row by
-// a lane, which takes about as long as the MFMAs they feed (16 cycles for two values).  Tiles of 128 x 256, windows of 64 values: 128-byte
-// rows of x, 64-byte rows of W, whose 16-byte chunk c of row r lies at c ^ (r / 4) % 4.  An MFMA of half h multiplies
-// values 16 g + 8 h .. + 7 of lane group g.
+// a lane, which takes about as long as the MFMAs they feed (16 cycles for two values).  Tiles of 128 x 256, windows of 64 values;
+// W is loaded for two windows at once, whole lines.  An MFMA of half h of a window multiplies values 16 g + 8 h .. + 7 of
+// lane group g.
 template <bool GATED_>
 struct GeoW {
   static constexpr int BM = 128, BN = 256, KIND = PRODUCT_OUT;
   static constexpr bool GATED = GATED_;
   static constexpr int MB = 4, NB = 4;  // blocks of 16 x 16 of a wave, 2 x 4 waves
   static constexpr int COLS = GATED ? BN / 2 : BN;
-  static constexpr int WA = BM * 128, WB = WA + BN * 64, SLOTS = 4;
-  static constexpr int TOPS = BM * 16;  // codes out: a row's largest values by wave
-  static constexpr int AREAS = SLOTS * WB + TOPS, LDS = AREAS + 2048;  // 256 bytes a wave for biases
+  static constexpr int XB = BM * 128, XSLOTS = 4, WB = BN * 128;  // a window of x, two of W in two slots
+  static constexpr int W0 = XSLOTS * XB, TOPS = W0 + 2 * WB;      // codes out: a row's largest values by wave
+  static constexpr int AREAS = TOPS + BM * 16, LDS = AREAS + 2048;  // 256 bytes a wave for biases
   static_assert(LDS <= 160 * 1024, "LDS");
 };
 
@@ -400,27 +400,24 @@ HILO_DEV f32x4 take_bias4(uint32_t area, int i, bool some, bool bf16) {
 
 template <typename G>
 HILO_DEV void run_wide(const ProductProblem &p, const Plan &q, int pid, uint8_t *lds) {
-  constexpr int BM = G::BM, BN = G::BN, MB = G::MB, NB = G::NB, WA = G::WA, WB = G::WB, S = G::SLOTS, L = 4;  // loads of a window
+  constexpr int BM = G::BM, BN = G::BN, MB = G::MB, NB = G::NB;
   const int lane = threadIdx.x & 63;
   const int wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lr = lane & 15, lg = lane >> 4, wm = wid >> 2, wn = wid & 3;
   const uint32_t lda = 2u * p.K, ldb = p.K;
-  const int nk = (p.K + 63) / 64, stride = scale_stride(p.K);
+  const int nv = (p.K + 127) / 128, stride = scale_stride(p.K);  // pairs of windows
 
-  // ---- loads: 16 rows of x and 32 of W a wave, two instructions each; with a gate a wave's rows of W are of one part
-  uint32_t oa[2], ob[2];
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int r = 8 * i + (lane >> 3), s = 16 * i + (lane >> 2);
-    oa[i] = uint32_t(wid * 16 + r) * lda + 16u * ((lane & 7) ^ ((r >> 1) & 7));
-    ob[i] = uint32_t((G::GATED ? wid >> 1 : wid) * 32 + s) * ldb + 16u * ((lane & 3) ^ ((s >> 2) & 3));
-  }
-  int lu = pid, lslot = 0, lw = nk;
+  // ---- loads of a pair of windows: 16 rows of x a wave, two instructions for each window, and 32 of W, four; with a gate a
+  // wave's rows of W are of one part.  The chunk of instruction i (8 rows) is that of instruction 0, or its bit 2 the
+  // other way round
+  const uint32_t oa = uint32_t(wid * 16 + (lane >> 3)) * lda + 16u * ((lane & 7) ^ (lane >> 4));
+  const uint32_t ob = uint32_t((G::GATED ? wid >> 1 : wid) * 32 + (lane >> 3)) * ldb + 16u * ((lane & 7) ^ (lane >> 4));
+  int lu = pid, lv = nv, lx = 0, lslot = 0;
   const char *la = nullptr, *lb = nullptr;
   uint32_t ra = 0, rb = 0;
   bool more = true;
-  auto ld_step = [&]() __attribute__((always_inline)) {
-    if (!more || lw < nk) return;
+  auto ld_step = [&]() __attribute__((always_inline)) {  // before a pair of windows
+    if (!more || lv < nv) return;
     const Item it = item_at(q, lu);
     if (!it.valid) {
       more = false;
@@ -428,7 +425,7 @@ HILO_DEV void run_wide(const ProductProblem &p, const Plan &q, int pid, uint8_t 
     }
     lu += P;
     const Place z = place_of<G>(p, q, it.t);
-    lw = 0;
+    lv = 0;
     const int part = G::GATED ? wid & 1 : 0;
     const void *w = z.stream ? (part ? p.w[1][1] : p.w[1][0]) : (part ? p.w[0][1] : p.w[0][0]);
     la = reinterpret_cast<const char *>(p.x) + size_t(z.row0) * lda;
@@ -436,19 +433,23 @@ HILO_DEV void run_wide(const ProductProblem &p, const Plan &q, int pid, uint8_t 
     ra = uint32_t(z.rows) * lda;
     rb = uint32_t(min(G::COLS, p.N - z.n0)) * ldb;
   };
-  auto ld = [&]() __attribute__((always_inline)) {
-    // chunks behind the end of k: offsets behind the buffer's
-    const int kv = p.K - 64 * lw, lane = opaque(threadIdx.x & 63);
-    const int c = (lane & 7) ^ ((lane >> 4) & 3), d = (lane & 3) ^ ((lane >> 4) & 3);
-    uint8_t *at = lds + lslot * WB;
-    const uint32_t na = more ? ra - 128u * uint32_t(lw) : 0u, nb = more ? rb - 64u * uint32_t(lw) : 0u;
+  // chunks behind the end of k: offsets behind the buffer's
+  auto ld_x = [&](int h) __attribute__((always_inline)) {  // window h of the pair
+    const int k = 128 * lv + 64 * h, kv = p.K - k, lane = opaque(threadIdx.x & 63), c = (lane & 7) ^ (lane >> 4);
+    const uint32_t bytes = more && kv > 0 ? ra - 2u * uint32_t(k) : 0u, o1 = oa + 8 * lda + (c & 4 ? -64 : 64);
+    uint8_t *at = lds + lx * G::XB + wid * 2048;
+    buffer_to_lds(la + size_t(k) * 2, bytes, 8 * c < kv ? oa : kBehind, at);
+    buffer_to_lds(la + size_t(k) * 2, bytes, 8 * (c ^ 4) < kv ? o1 : kBehind, at + 1024);
+    lx = (lx + 1) & (G::XSLOTS - 1);
+  };
+  auto ld_w = [&]() __attribute__((always_inline)) {
+    const int kv = p.K - 128 * lv, lane = opaque(threadIdx.x & 63), c = (lane & 7) ^ (lane >> 4);
+    const uint32_t bytes = more ? rb - 128u * uint32_t(lv) : 0u;
+    const uint32_t o0 = 16 * c < kv ? ob : kBehind, o1 = 16 * (c ^ 4) < kv ? ob + (c & 4 ? -64 : 64) : kBehind;
+    uint8_t *at = lds + G::W0 + lslot * G::WB + wid * 4096;
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
-      buffer_to_lds(la + size_t(lw) * 128, na, 8 * (i ? c ^ 4 : c) < kv ? oa[i] : kBehind, at + wid * 2048 + i * 1024);
-#pragma unroll
-    for (int i = 0; i < 2; ++i) buffer_to_lds(lb + size_t(lw) * 64, nb, 16 * d < kv ? ob[i] : kBehind, at + WA + wid * 2048 + i * 1024);
-    ++lw;
-    lslot = (lslot + 1) & (S - 1);
+    for (int i = 0; i < 4; ++i) buffer_to_lds(lb + size_t(lv) * 128, bytes, (i & 1 ? o1 : o0) + uint32_t(8 * i) * ldb, at + i * 1024);
+    lslot ^= 1;
   };
 
   // ---- fragments
@@ -456,26 +457,28 @@ HILO_DEV void run_wide(const ProductProblem &p, const Plan &q, int pid, uint8_t 
   uint32_t fa[2];
 #pragma unroll
   for (int h = 0; h < 2; ++h) fa[h] = lds0 + (wm * (BM / 2) + lr) * 128 + ((2 * lg + h) ^ ((lr >> 1) & 7)) * 16;
-  const uint32_t fb = lds0 + WA + (wn * (BN / 4) + lr) * 64 + (lg ^ ((lr >> 2) & 3)) * 16;
+  uint32_t fb[2];  // of either window of a pair
+#pragma unroll
+  for (int h = 0; h < 2; ++h) fb[h] = lds0 + G::W0 + (wn * (BN / 4) + lr) * 128 + ((4 * h + lg) ^ ((lr >> 1) & 7)) * 16;
   f32x4 acc[MB][NB];
   // of two windows: x by halves; W's codes, read a window before they are widened, and that one before they are multiplied
   u32x4 a[2][2][MB], b[2][NB];
   bf16x8 wb[2][2][NB];
-  uint32_t so = 0, so1 = WB, so2 = 2 * WB;  // byte offsets of this window and of the next two
+  uint32_t sx = G::XB, sw = G::WB;  // byte offsets of the next window of x, and of the next pair of W
   const uint8_t *ws[2] = {nullptr, nullptr};
   uint32_t s0, s1;  // of the window that is widened
-  auto scales = [&](int w) __attribute__((always_inline)) {  // of block w / 2: a float32 number's exponent
-    const int shift = 4 * (w & 6);
-    s0 = (scales_at(ws[0], w >> 3) >> shift & 255u) << 23;
-    s1 = (scales_at(ws[G::GATED ? 1 : 0], w >> 3) >> shift & 255u) << 23;
+  auto scales = [&](int v) __attribute__((always_inline)) {  // of pair v: a float32 number's exponent
+    const int shift = 8 * (v & 3);
+    s0 = (scales_at(ws[0], v >> 2) >> shift & 255u) << 23;
+    s1 = (scales_at(ws[G::GATED ? 1 : 0], v >> 2) >> shift & 255u) << 23;
   };
   auto rd_a = [&](auto set, auto gg) __attribute__((always_inline)) {
     constexpr int s = decltype(set)::value, h = decltype(gg)::value / 4, i = decltype(gg)::value % 4;
-    read16<i * 2048>(a[s][h][i], fa[h] + so1);
+    read16<i * 2048>(a[s][h][i], fa[h] + sx);
   };
-  auto rd_b = [&](auto set, auto jj, uint32_t at) __attribute__((always_inline)) {
+  auto rd_b = [&](auto set, auto jj) __attribute__((always_inline)) {  // window `set` of the pair
     constexpr int s = decltype(set)::value, j = decltype(jj)::value;
-    read16<j * 1024>(b[s][j], fb + at);
+    read16<j * 2048>(b[s][j], fb[s] + sw);
   };
   auto wait = [&](auto set) __attribute__((always_inline)) {  // for a of a set, b of the other
     constexpr int s = decltype(set)::value;
@@ -489,12 +492,17 @@ HILO_DEV void run_wide(const ProductProblem &p, const Plan &q, int pid, uint8_t 
     }
     __builtin_amdgcn_sched_barrier(0);
   };
-  // window w of a set, while W's codes of w + 1 are widened, x of w + 1 and W of w + 2 are read.  One barrier, at which every
-  // wave has read window w
-  auto window = [&](auto set, int w) __attribute__((always_inline)) {
+  // Window w = 2 v + s, while W's codes of w + 1 are widened, x of w + 1 and W of w + 2 are read.  One barrier, at which every
+  // wave has read x of w and W of w + 1, so that x of w + 4 goes to the slot of w, and for even w W's pair v + 2 to that of
+  // v.  What is read behind it has landed: of the loads issued since, 2 + 2 of x (even w), or 2 of x, 4 of W and 2 of x
+  auto window = [&](auto set, int v) __attribute__((always_inline)) {  // window s of pair v
     constexpr int s = decltype(set)::value;
-    ld_step();
-    wait_vm<(S - 3) * L>();
+    if constexpr (s == 0) {
+      ld_step();
+      wait_vm<4>();
+    } else {
+      wait_vm<8>();
+    }
     asm volatile("s_barrier" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
     auto group = [&](auto gg) __attribute__((always_inline)) {
@@ -504,27 +512,31 @@ HILO_DEV void run_wide(const ProductProblem &p, const Plan &q, int pid, uint8_t 
         acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wb[s][h][j], __builtin_bit_cast(bf16x8, a[s][h][i]), acc[i][j], 0, 0, 0);
       wb[1 - s][h][i] = wide_codes(b[1 - s][i][2 * h], b[1 - s][i][2 * h + 1], i < NB / 2 ? s0 : s1);
       if constexpr (g < 4) {
-        rd_b(Int<s>{}, Int<g>{}, so2);
+        rd_b(Int<s>{}, Int<g>{});
         rd_a(Int<1 - s>{}, Int<2 * g>{});
         rd_a(Int<1 - s>{}, Int<2 * g + 1>{});
       }
-      if constexpr (g == 4) ld();
+      if constexpr (g == 4 && s == 0) ld_w();
+      if constexpr (g == 5) ld_x(s);
+      if constexpr (g == 5 && s == 1) ++lv;
       __builtin_amdgcn_sched_barrier(0);
     };
     group(Int<0>{}); group(Int<1>{}); group(Int<2>{}); group(Int<3>{});
     group(Int<4>{}); group(Int<5>{}); group(Int<6>{}); group(Int<7>{});
-    scales(min(w + 2, nk - 1));
+    if constexpr (s == 0) scales(min(v + 1, nv - 1));
     wait(Int<1 - s>{});
-    so = so1;
-    so1 = so2;
-    so2 = so2 == (S - 1) * WB ? 0 : so2 + WB;
+    sx = sx == 3 * G::XB ? 0 : sx + G::XB;
+    if constexpr (s == 1) sw ^= G::WB;
   };
 #pragma unroll 1
-  for (int w = 0; w < S; ++w) {
+  for (int v = 0; v < 2; ++v) {
     ld_step();
-    ld();
+    ld_w();
+    ld_x(0);
+    ld_x(1);
+    ++lv;
   }
-  wait_vm<(S - 2) * L>();
+  wait_vm<0>();
   asm volatile("s_barrier" ::: "memory");
   for (int u = pid;; u += P) {
     const Item it = item_at(q, u);
@@ -540,16 +552,16 @@ HILO_DEV void run_wide(const ProductProblem &p, const Plan &q, int pid, uint8_t 
     for (int i = 0; i < MB; ++i)
 #pragma unroll
       for (int j = 0; j < NB; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    // the first window and W of the second: all have landed
-    rd_b(Int<0>{}, Int<0>{}, so); rd_b(Int<0>{}, Int<1>{}, so); rd_b(Int<0>{}, Int<2>{}, so); rd_b(Int<0>{}, Int<3>{}, so);
-    rd_b(Int<1>{}, Int<0>{}, so1); rd_b(Int<1>{}, Int<1>{}, so1); rd_b(Int<1>{}, Int<2>{}, so1); rd_b(Int<1>{}, Int<3>{}, so1);
-    {
-      const uint32_t next = so1;
-      so1 = so;
-      rd_a(Int<0>{}, Int<0>{}); rd_a(Int<0>{}, Int<1>{}); rd_a(Int<0>{}, Int<2>{}); rd_a(Int<0>{}, Int<3>{});
-      rd_a(Int<0>{}, Int<4>{}); rd_a(Int<0>{}, Int<5>{}); rd_a(Int<0>{}, Int<6>{}); rd_a(Int<0>{}, Int<7>{});
-      so1 = next;
-    }
+    // x of the first window, and W of the first two: all have landed.  (The last window of the item before read them too, but
+    // widened W with its own scales)
+    sx = sx == 0 ? 3 * G::XB : sx - G::XB;
+    sw ^= G::WB;
+    rd_b(Int<0>{}, Int<0>{}); rd_b(Int<0>{}, Int<1>{}); rd_b(Int<0>{}, Int<2>{}); rd_b(Int<0>{}, Int<3>{});
+    rd_b(Int<1>{}, Int<0>{}); rd_b(Int<1>{}, Int<1>{}); rd_b(Int<1>{}, Int<2>{}); rd_b(Int<1>{}, Int<3>{});
+    rd_a(Int<0>{}, Int<0>{}); rd_a(Int<0>{}, Int<1>{}); rd_a(Int<0>{}, Int<2>{}); rd_a(Int<0>{}, Int<3>{});
+    rd_a(Int<0>{}, Int<4>{}); rd_a(Int<0>{}, Int<5>{}); rd_a(Int<0>{}, Int<6>{}); rd_a(Int<0>{}, Int<7>{});
+    sx = sx == 3 * G::XB ? 0 : sx + G::XB;
+    sw ^= G::WB;
     scales(0);
     wait(Int<0>{});
 #pragma unroll
@@ -558,14 +570,11 @@ HILO_DEV void run_wide(const ProductProblem &p, const Plan &q, int pid, uint8_t 
 #pragma unroll
       for (int h = 0; h < 2; ++h) wb[0][h][j] = wide_codes(b[0][j][2 * h], b[0][j][2 * h + 1], j < NB / 2 ? s0 : s1);
     }
-    scales(min(1, nk - 1));
-    int w = 0;
 #pragma unroll 1
-    for (; w + 1 < nk; w += 2) {
-      window(Int<0>{}, w);
-      window(Int<1>{}, w + 1);
+    for (int v = 0; v < nv; ++v) {
+      window(Int<0>{}, v);
+      window(Int<1>{}, v);
     }
-    if (w < nk) window(Int<0>{}, w);
     const int lane = opaque(threadIdx.x & 63), lr = lane & 15, lg = lane >> 4;
     // lane (lr, lg): rows 16 i + lr, columns 16 j + 4 lg .. + 3 of block j; with a gate blocks 0 and 1 are the gate's
     const int n = z.n0 + wn * (G::COLS / 4) + 4 * lg;
@@ -583,9 +592,9 @@ HILO_DEV void run_wide(const ProductProblem &p, const Plan &q, int pid, uint8_t 
     }
     if constexpr (G::GATED) {
       // the tile's 128 columns have one scale a row, from the largest of four waves' 32 columns
-      const uint32_t tops = lds0 + S * WB;
+      const uint32_t tops = lds0 + G::TOPS;
       f32x4 bias[NB];
-      if (nk < S) wait_vm<0>();  // the biases may still be on their way
+      if (nv < 4) wait_vm<0>();  // the biases may still be on their way
 #pragma unroll
       for (int j = 0; j < NB; ++j) {
         const void *v = z.stream ? (j / 2 ? p.bias[1][1] : p.bias[1][0]) : (j / 2 ? p.bias[0][1] : p.bias[0][0]);
