@@ -389,9 +389,17 @@ HILO_DEV void run(const ProductProblem &p, const Plan &q, int pid, uint8_t *lds)
     row(Int<0>{}); row(Int<1>{}); row(Int<2>{}); row(Int<3>{});
     row(Int<4>{}); row(Int<5>{}); row(Int<6>{}); row(Int<7>{});
   };
-  // this wave has read the window, and all but the last issued windows have landed; on to the next
+  // this wave has read the window, and all but the last issued windows have landed; on to the next.  Not waited for in the
+  // first S - 1 windows of a tile: theirs have landed before the stores of the tile before, which wait_vm would wait for as well
+  int landed = S - 1;
   auto next_window = [&]() __attribute__((always_inline)) {
-    wait_vm<(S - 2) * (LA + LB)>();
+    // (MFMAs before a branch would be moved behind it, past the reads that they are to run beside)
+#pragma unroll
+    for (int i = 0; i < MB; ++i)
+#pragma unroll
+      for (int j = 0; j < NB; ++j) asm volatile("" : "+v"(acc[i][j]));
+    if (landed > 0) --landed;
+    else wait_vm<(S - 2) * (LA + LB)>();
     asm volatile("s_barrier" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
     so = so == (S - 1) * WB ? 0 : so + WB;
@@ -403,7 +411,7 @@ HILO_DEV void run(const ProductProblem &p, const Plan &q, int pid, uint8_t *lds)
     ld_a();
     ld_b();
   }
-  wait_vm<(S - 1) * (LA + LB)>();
+  wait_vm<0>();
   asm volatile("s_barrier" ::: "memory");
   for (int u = pid;; u += P) {
     const Item it = item_at(q, u);
@@ -422,13 +430,15 @@ HILO_DEV void run(const ProductProblem &p, const Plan &q, int pid, uint8_t *lds)
     rd_all(Int<0>{});
 #pragma unroll 1
     for (int w = w0; w < w1; ++w) {
-      ld_step();  // its branch lies here because MFMAs before a branch are moved behind it
+      ld_step();
       half(Int<0>{}, Int<0>{});
       rd_wait(Int<1>{});
       next_window();
       half(Int<1>{}, Int<1>{});
       rd_wait(Int<0>{});
     }
+    wait_vm<0>();  // the next tile's first windows, and the biases
+    landed = S - 1;
     const int lane = opaque(threadIdx.x & 63);
     if (it.n > 1) {
 #pragma unroll
@@ -438,7 +448,6 @@ HILO_DEV void run(const ProductProblem &p, const Plan &q, int pid, uint8_t *lds)
     } else {
       Bias<G> bias;
       if constexpr (KIND == PRODUCT_OUT) {
-        if (w1 - w0 < S) wait_vm<0>();  // the biases may still be on their way
         bias.take(p, z, lds0 + S * WB + wid * 256, lane >> 4);
       }
 #pragma unroll

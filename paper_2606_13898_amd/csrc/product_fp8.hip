@@ -200,7 +200,7 @@ struct Loads8 {
     ++w;
     slot = slot == S - 1 ? 0 : slot + 1;
   }
-  // the first S windows, of which one has landed
+  // the first S windows
   HILO_DEV void start() {
 #pragma unroll 1
     for (int i = 0; i < S; ++i) {
@@ -208,12 +208,13 @@ struct Loads8 {
       a();
       b();
     }
-    wait_vm<(S - 1) * (LA + LB + 1)>();
+    wait_vm<0>();
     asm volatile("s_barrier" ::: "memory");
   }
-  // this wave has read a window, and all but the last issued windows have landed
+  // this wave has read a window, and all but the last issued windows have landed; first: as product_bf16.hip's next_window
+  template <bool FIRST>
   HILO_DEV void next() {
-    wait_vm<(S - 2) * (LA + LB + 1)>();
+    if constexpr (!FIRST) wait_vm<(S - 2) * (LA + LB + 1)>();
     asm volatile("s_barrier" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
   }
@@ -334,19 +335,28 @@ HILO_DEV void run8(const ProductProblem &p, const Plan &q, int pid, uint8_t *lds
     rd_scales();
     rd_all(Int<0>{});
     take_scales(w0);
-#pragma unroll 1
-    for (int w = w0; w < w1; ++w) {
+    auto window = [&](auto first, int w) __attribute__((always_inline)) {
       loads.step();  // its branch lies here because MFMAs before a branch are moved behind it
       half(Int<0>{}, Int<0>{});
       rd_wait(Int<1>{});
-      loads.next();
+      loads.template next<decltype(first)::value != 0>();
       so = so == (S - 1) * WB ? 0 : so + WB;
       ring = (ring + 1) & (G::RING - 1);
       rd_scales();
       half(Int<1>{}, Int<1>{});
       rd_wait(Int<0>{});
       take_scales(min(w + 1, nk - 1));
-    }
+    };
+    int w = w0;
+#pragma unroll
+    for (int k = 0; k < S - 1; ++k)
+      if (w < w1) {
+        window(Int<1>{}, w);
+        ++w;
+      }
+#pragma unroll 1
+    for (; w < w1; ++w) window(Int<0>{}, w);
+    wait_vm<0>();  // the next tile's first windows, and the biases
     const int lane = opaque(threadIdx.x & 63);
     if (it.n > 1) {
 #pragma unroll
@@ -356,7 +366,6 @@ HILO_DEV void run8(const ProductProblem &p, const Plan &q, int pid, uint8_t *lds
       continue;
     }
     Bias8<G> bias;
-    if (w1 - w0 < S) wait_vm<0>();  // the biases may still be on their way
     bias.take(p, z, lds0 + G::AREAS + wid * 256, lane >> 5);
 #pragma unroll
     for (int i = 0; i < MB; ++i) {
@@ -495,14 +504,11 @@ HILO_DEV void run_wide(const ProductProblem &p, const Plan &q, int pid, uint8_t 
   // Window w = 2 v + s, while W's codes of w + 1 are widened, x of w + 1 and W of w + 2 are read.  One barrier, at which every
   // wave has read x of w and W of w + 1, so that x of w + 4 goes to the slot of w, and for even w W's pair v + 2 to that of
   // v.  What is read behind it has landed: of the loads issued since, 2 + 2 of x (even w), or 2 of x, 4 of W and 2 of x
-  auto window = [&](auto set, int v) __attribute__((always_inline)) {  // window s of pair v
+  auto window = [&](auto set, auto first, int v) __attribute__((always_inline)) {  // window s of pair v
     constexpr int s = decltype(set)::value;
-    if constexpr (s == 0) {
-      ld_step();
-      wait_vm<4>();
-    } else {
-      wait_vm<8>();
-    }
+    if constexpr (s == 0) ld_step();
+    // in a tile's first pair it has landed before the stores of the tile before, which would be waited for as well
+    if constexpr (decltype(first)::value == 0) wait_vm<s == 0 ? 4 : 8>();
     asm volatile("s_barrier" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
     auto group = [&](auto gg) __attribute__((always_inline)) {
@@ -570,11 +576,14 @@ HILO_DEV void run_wide(const ProductProblem &p, const Plan &q, int pid, uint8_t 
 #pragma unroll
       for (int h = 0; h < 2; ++h) wb[0][h][j] = wide_codes(b[0][j][2 * h], b[0][j][2 * h + 1], j < NB / 2 ? s0 : s1);
     }
+    window(Int<0>{}, Int<1>{}, 0);
+    window(Int<1>{}, Int<1>{}, 0);
 #pragma unroll 1
-    for (int v = 0; v < nv; ++v) {
-      window(Int<0>{}, v);
-      window(Int<1>{}, v);
+    for (int v = 1; v < nv; ++v) {
+      window(Int<0>{}, Int<0>{}, v);
+      window(Int<1>{}, Int<0>{}, v);
     }
+    wait_vm<0>();  // the next tile's first windows, and the biases
     const int lane = opaque(threadIdx.x & 63), lr = lane & 15, lg = lane >> 4;
     // lane (lr, lg): rows 16 i + lr, columns 16 j + 4 lg .. + 3 of block j; with a gate blocks 0 and 1 are the gate's
     const int n = z.n0 + wn * (G::COLS / 4) + 4 * lg;
@@ -594,7 +603,6 @@ HILO_DEV void run_wide(const ProductProblem &p, const Plan &q, int pid, uint8_t 
       // the tile's 128 columns have one scale a row, from the largest of four waves' 32 columns
       const uint32_t tops = lds0 + G::TOPS;
       f32x4 bias[NB];
-      if (nv < 4) wait_vm<0>();  // the biases may still be on their way
 #pragma unroll
       for (int j = 0; j < NB; ++j) {
         const void *v = z.stream ? (j / 2 ? p.bias[1][1] : p.bias[1][0]) : (j / 2 ? p.bias[0][1] : p.bias[0][0]);
