@@ -1233,7 +1233,7 @@ hilo_status hilo_linear_fp8(int32_t dtype, const hilo_linear_w_fp8 w[2], const v
                             size_t ws_bytes, void *stream) {
   hilo_status e = check_dtype(dtype);
   if (e != HILO_OK || (e = check_product(rows, in_dim, out_dim, batch, text_len, 16)) != HILO_OK) return e;
-  if (!w || !cu_seqlens || !workspace || (rows > 0 && (!x || !out))) return HILO_E_NULL;
+  if (!w || !cu_seqlens || (rows > 0 && (!x || !out || !workspace))) return HILO_E_NULL;
   const int streams = text_len > 0 ? 2 : 1;
   const void *const gate[2] = {w[0].w_gate, streams == 2 ? w[1].w_gate : nullptr};
   bool gated;

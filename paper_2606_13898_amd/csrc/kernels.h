@@ -206,7 +206,7 @@ size_t linear_i8_part_bytes(long long rows, int K);
 struct ProductProblem {
   const int *cu;
   int B, L, rows;
-  int merged;            // all rows are one segment of stream 0 (no text, or the same weights for both streams)
+  int merged;            // all rows are one segment of stream 0, and stream 1 has none (no text, or the same for both streams)
   int K, N, parts;       // in_dim, out_dim, 1 or 2
   int silu;              // the gate's activation: SiLU, or GELU
   int bf16;              // type of x, out, pre, biases, gradients

@@ -107,12 +107,12 @@ __global__ __launch_bounds__(512) void k_product(ProductProblem p) {
     // ---- where the sum runs: pieces of k, walked from step s0 to s1
     int total = 0;
     if constexpr (KIND == PRODUCT_DW) {
-      for (int i = p.merged ? 0 : stream; i < segments(p); i += 2) total += (max(segment(p, i).n, 0) + kStep - 1) / kStep;
+      for (int i = stream; i < segments(p); i += 2) total += (max(segment(p, i).n, 0) + kStep - 1) / kStep;
     } else {
       total = parts * (per / kStep);
     }
     const int s0 = int((long long)total * split / p.splits), s1 = int((long long)total * (split + 1) / p.splits);
-    int seg = p.merged ? 0 : stream, seg_lo = 0, seg_n = 0, seg_s = 0;  // DW: the segment of the step, its first step
+    int seg = stream, seg_lo = 0, seg_n = 0, seg_s = 0;  // DW: the segment of the step, its first step
     if constexpr (KIND == PRODUCT_DW) {
       if (s0 < s1) {
         Segment g = segment(p, seg);

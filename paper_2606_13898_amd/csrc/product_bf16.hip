@@ -38,7 +38,7 @@ HILO_DEV int windows(const ProductProblem &p, int stream) {
   if constexpr (KIND == PRODUCT_OUT) return (p.K + 63) / 64;
   if constexpr (KIND == PRODUCT_DX) return p.parts * ((p.N + 63) / 64);
   int n = 0;
-  for (int i = p.merged ? 0 : stream; i < segments(p); i += 2) n += (segment(p, i).n + 63) / 64;
+  for (int i = stream; i < segments(p); i += 2) n += (segment(p, i).n + 63) / 64;
   return n;
 }
 
@@ -247,7 +247,7 @@ HILO_DEV void run(const ProductProblem &p, const Plan &q, int pid, uint8_t *lds)
         lpiece = w / per;
         w -= lpiece * per;
       } else {
-        lpiece = p.merged ? 0 : lz.stream;
+        lpiece = lz.stream;
         int n1 = (segment(p, lpiece).n + 63) / 64;
         while (w >= n1) {
           w -= n1;

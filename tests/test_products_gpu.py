@@ -65,6 +65,7 @@ SHAPES = [
     ([13, 4], 3, 328, 248, 2),
     ([64, 64], 64, 128, 256, 2),
     ([129], 0, 8, 640, 1),
+    ([129, 5], 0, 72, 136, 2),
     ([100, 31, 260], 17, 200, 344, 2),
     ([100, 31, 260], 17, 200, 344, 1),
     ([300], 213, 520, 264, 2),
