@@ -20,8 +20,9 @@ HILO_DEV Segment segment(const P &p, int i) {
   return (i & 1) ? Segment{hi - p.L, p.L, 1} : Segment{lo, hi - p.L - lo, 0};
 }
 
-// Rows of a row tile of BM rows: first row, how many, stream; n = 0 behind the last tile.  A lane looks at a segment, 64
-// at a time: the first whose tiles, and those of all before, number more than t.  The whole wave calls it with the same t.
+// Rows of a row tile of BM rows: first row, how many, stream; n = 0 behind the last tile.  Of few samples by scalar loads, one
+// after the other, which wait for no load of a tile.  Of many a lane looks at a segment, 64 at a time: the first whose
+// tiles, and those of all before, number more than t.  The whole wave calls it with the same t.
 struct RowTile {
   int row0, n, stream;
 };
@@ -30,6 +31,15 @@ HILO_DEV RowTile find_row_tile(const P &p, int BM, int t) {
   if (p.merged) {
     const int end = cu_at(p.cu, p.B);
     return RowTile{t * BM, max(0, min(BM, end - t * BM)), 0};
+  }
+  if (p.B <= 32) {
+    for (int i = 0; i < 2 * p.B; ++i) {
+      const Segment s = segment(p, i);
+      const int tiles = (s.n + BM - 1) / BM;
+      if (t < tiles) return RowTile{s.lo + t * BM, min(BM, s.n - t * BM), s.stream};
+      t -= tiles;
+    }
+    return RowTile{0, 0, 0};
   }
   const int lane = threadIdx.x & 63, ns = 2 * p.B;
   for (int i0 = 0; i0 < ns; i0 += 64) {
@@ -55,6 +65,11 @@ HILO_DEV RowTile find_row_tile(const P &p, int BM, int t) {
     t -= __builtin_amdgcn_readlane(upto, 63);
   }
   return RowTile{0, 0, 0};
+}
+// As many row tiles as the buffers' rows can make: every segment but one may end in a part of one.
+template <typename P>
+__host__ __device__ __forceinline__ int row_tiles_bound(const P &p, int BM) {
+  return (p.rows + BM - 1) / BM + (p.merged ? 0 : 2 * p.B - 1);
 }
 template <typename P>
 HILO_DEV int count_row_tiles(const P &p, int BM) {

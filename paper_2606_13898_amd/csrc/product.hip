@@ -83,7 +83,7 @@ __global__ __launch_bounds__(512) void k_product(ProductProblem p) {
   float (&lds)[2][2][64][kPad] = buffers[group];
   const int lr = lane & 15, lg = lane >> 4, wm = wid >> 1, wn = wid & 1;
   const int cols = KIND == PRODUCT_OUT ? p.N : p.K, tn_count = (cols + BN - 1) / BN;
-  const int tm_count = KIND == PRODUCT_DW ? (p.N + 63) / 64 : count_row_tiles(p, 64);
+  const int tm_count = KIND == PRODUCT_DW ? (p.N + 63) / 64 : row_tiles_bound(p, 64);
   const long long tiles = (long long)tm_count * tn_count * (KIND == PRODUCT_DW ? p.outs : 1);
   // steps of the whole sum; of a segment's rows in DW
   const int parts = KIND == PRODUCT_DX ? p.parts : 1, per = (KIND == PRODUCT_OUT ? p.K : p.N) + kStep - 1;
@@ -100,6 +100,7 @@ __global__ __launch_bounds__(512) void k_product(ProductProblem p) {
       rows = min(64, p.N - row0);
     } else {
       const RowTile rt = find_row_tile(p, 64, tr);
+      if (rt.n == 0) continue;  // behind the last
       row0 = rt.row0;
       rows = rt.n;
       stream = rt.stream;
@@ -318,7 +319,7 @@ __global__ __launch_bounds__(256) void k_product_join(ProductProblem p) {
 
 // Splits of the sum where tiles are fewer than two for each of the 256 CUs, no shorter than 4 steps each.
 static int splits_of(int kind, long long rows, int K, int N, int parts, int outs, int B, bool merged) {
-  const long long tm = kind == PRODUCT_DW ? (long long)outs * ((N + 63) / 64) : (rows + 63) / 64 + (merged ? 0 : 2 * B - 1);
+  const long long tm = kind == PRODUCT_DW ? (long long)outs * ((N + 63) / 64) : (rows + 63) / 64 + (merged ? 0 : 2 * B - 1);  // row_tiles_bound
   const int bn = kind == PRODUCT_OUT && parts == 2 ? 32 : 64, cols = kind == PRODUCT_OUT ? N : K;
   const long long tiles = std::max(1ll, tm * ((cols + bn - 1) / bn));
   const long long steps = kind == PRODUCT_OUT ? K / kStep : kind == PRODUCT_DX ? (long long)parts * N / kStep : rows / kStep;
@@ -339,7 +340,7 @@ size_t product_part_bytes(bool bf16, int kind, long long rows, int K, int N, int
 template <int TYPE, int KIND, bool GATED>
 static hipError_t run(ProductProblem &p, hipStream_t st) {
   p.splits = splits_of(KIND, p.rows, p.K, p.N, p.parts, p.outs, p.B, p.merged);
-  const long long tm = KIND == PRODUCT_DW ? (long long)p.outs * ((p.N + 63) / 64) : (p.rows + 63) / 64 + (p.merged ? 0 : 2 * p.B - 1);
+  const long long tm = KIND == PRODUCT_DW ? (long long)p.outs * ((p.N + 63) / 64) : row_tiles_bound(p, 64);
   const int cols = KIND == PRODUCT_OUT ? p.N : p.K, bn = KIND == PRODUCT_OUT && GATED ? 32 : 64;
   const long long items = tm * ((cols + bn - 1) / bn) * p.splits;
   if (items <= 0) return hipSuccess;
@@ -413,14 +414,15 @@ static int back_rows(long long rows) { return rows >= 8192 ? 256 : rows >= 2048 
 
 template <bool BF16, bool GATED>
 __global__ __launch_bounds__(256) void k_gate_back(GateBackProblem p) {
-  constexpr int PARTS = GATED ? 2 : 1, TYPE = BF16 ? TYPE_BF16 : TYPE_F32, AHEAD = BF16 ? 4 : 2;
+  constexpr int PARTS = GATED ? 2 : 1, TYPE = BF16 ? TYPE_BF16 : TYPE_F32, AHEAD = 4;
   __shared__ float sums[3][PARTS][8][64];
   const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int tn_count = (p.N + kBackCols - 1) / kBackCols;
-  const long long tiles = (long long)count_row_tiles(p, p.block_rows) * tn_count;
+  const long long tiles = (long long)row_tiles_bound(p, p.block_rows) * tn_count;
   for (long long t = blockIdx.x; t < tiles; t += gridDim.x) {
     const int tr = int(t / tn_count), n = int(t - (long long)tr * tn_count) * kBackCols + 8 * lane;
     const RowTile rt = find_row_tile(p, p.block_rows, tr);
+    if (rt.n == 0) continue;  // behind the last
     float db[PARTS][8];
 #pragma unroll
     for (int q = 0; q < PARTS; ++q)
@@ -535,7 +537,7 @@ size_t gate_back_bytes(long long rows, int N, int parts, int B) {
 template <bool BF16, bool GATED>
 static hipError_t run_gate_back(const GateBackProblem &p, hipStream_t st) {
   if (p.rows > 0 && (GATED || p.part)) {
-    const long long tiles = ((p.rows + p.block_rows - 1) / p.block_rows + (p.merged ? 0 : 2LL * p.B)) * ((p.N + kBackCols - 1) / kBackCols);
+    const long long tiles = (long long)row_tiles_bound(p, p.block_rows) * ((p.N + kBackCols - 1) / kBackCols);
     hipLaunchKernelGGL((k_gate_back<BF16, GATED>), dim3(unsigned(std::min(tiles, 1ll << 20))), dim3(256), 0, st, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;

@@ -86,20 +86,7 @@ HILO_DEV Place place_of(const ProductProblem &p, const Plan &q, int t) {
   } else {
     tile_at(q.R, q.TN, t, r, c);
     z.o = z.part = 0;
-    RowTile rt{0, 0, 0};
-    if (p.merged || p.B > 32) {
-      rt = find_row_tile(p, G::BM, r);
-    } else {  // few samples: by scalar loads, which wait for no load of a tile
-      for (int i = 0; i < 2 * p.B; ++i) {
-        const Segment s = segment(p, i);
-        const int tiles = (s.n + G::BM - 1) / G::BM;
-        if (r < tiles) {
-          rt = RowTile{s.lo + r * G::BM, min(G::BM, s.n - r * G::BM), s.stream};
-          break;
-        }
-        r -= tiles;
-      }
-    }
+    const RowTile rt = find_row_tile(p, G::BM, r);
     z.row0 = rt.row0;
     z.rows = rt.n;
     z.stream = rt.stream;
