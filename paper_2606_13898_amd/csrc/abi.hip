@@ -17,14 +17,14 @@ enum Kind {
   K_SCORE, K_SELECT, K_LAYOUT, K_COMPRESS, K_NORM_ATTN, K_GEMM_QKV, K_ATTN_CORE, K_GEMM_O,
   K_NORM_MLP, K_GEMM_FC1, K_GEMM_FC2, K_DECOMPRESS, K_QUANT_ATTN, K_QUANT_MLP,
   K_ROPE, K_POSITIONS, K_NORM_RESIDUAL, K_NORM_RESIDUAL_BACK, K_QUANT_I8, K_LINEAR_I8,
-  K_LINEAR, K_LINEAR_GATE_BACK, K_LINEAR_DX, K_LINEAR_DW, K_QUANT_BLOCKS, K_LINEAR_FP8, K_COUNT
+  K_LINEAR, K_LINEAR_GATE_BACK, K_LINEAR_BACK, K_QUANT_BLOCKS, K_LINEAR_FP8, K_COUNT
 };
 const char *kKindNames[K_COUNT] = {"score", "select", "layout", "compress", "rownorm_attn",
                                    "gemm_qkv", "attention_core", "gemm_o", "rownorm_mlp",
                                    "gemm_fc1", "gemm_fc2", "decompress", "quantize_attn",
                                    "quantize_mlp", "rope", "token_positions", "norm_residual",
                                    "norm_residual_backward", "quantize_i8", "linear_i8", "linear",
-                                   "linear_gate_backward", "linear_dx", "linear_dw", "quantize_blocks", "linear_fp8"};
+                                   "linear_gate_backward", "linear_backward", "quantize_blocks", "linear_fp8"};
 
 struct ProfRec {
   int kind;
@@ -1027,7 +1027,7 @@ hilo_status check_gate(const void *const gate[2], int streams, int32_t act, bool
 
 // Backward workspace: dpre (with a gate), the rows' sums, partial products.
 struct BackwardLayout {
-  size_t sums, part, total;
+  size_t sums, part, part_dw, total;
 };
 BackwardLayout backward_layout(bool bf16, int64_t rows, int K, int N, int batch, bool gated) {
   const int parts = gated ? 2 : 1;
@@ -1036,7 +1036,8 @@ BackwardLayout backward_layout(bool bf16, int64_t rows, int K, int N, int batch,
   l.part = l.sums + align256(gate_back_bytes(rows, N, parts, batch));
   const size_t dx = product_part_bytes(bf16, PRODUCT_DX, rows, K, N, parts);
   const size_t dw = product_part_bytes(bf16, PRODUCT_DW, rows, K, N, parts);
-  l.total = l.part + align256(dx > dw ? dx : dw);
+  l.part_dw = l.part + (bf16 ? 0 : align256(dx));  // float32: both are formed in one launch
+  l.total = l.part_dw + align256(bf16 && dx > dw ? dx : dw);
   return l;
 }
 
@@ -1164,8 +1165,6 @@ hilo_status hilo_linear_backward(int32_t dtype, const hilo_linear_w w[2], const 
   for (int k = 0; k < 2; ++k)
     for (int q = 0; q < 2; ++q) b.db[k][q] = db[k][q];
   b.part = any_db ? reinterpret_cast<float *>(ws + l.sums) : nullptr;
-  hipError_t he = timed(K_LINEAR_GATE_BACK, st, [&] { return launch_gate_back(bf16, b, st); });
-  if (he != hipSuccess) return HILO_E_DEVICE;
 
   ProductProblem p{};
   p.cu = cu_seqlens;
@@ -1182,25 +1181,35 @@ hilo_status hilo_linear_backward(int32_t dtype, const hilo_linear_w w[2], const 
     p.w[k][1] = v.w;
   }
   p.part = reinterpret_cast<float *>(ws + l.part);
-  if (dx && rows > 0) {
-    p.merged = streams == 1 || (p.w[0][0] == p.w[1][0] && p.w[0][1] == p.w[1][1]);
-    he = timed(K_LINEAR_DX, st, [&] { return launch_product(PRODUCT_DX, p, st); });
-    if (he != hipSuccess) return HILO_E_DEVICE;
-  }
+  p.merged = streams == 1 || (p.w[0][0] == p.w[1][0] && p.w[0][1] == p.w[1][1]);
   // gradients that both streams share run over all rows; those of one stream over its own
+  ProductProblem g[2] = {p, p};
   for (int both = 0; both < 2; ++both) {
-    p.merged = both || text_len == 0;
-    p.outs = 0;
+    g[both].part = reinterpret_cast<float *>(ws + l.part_dw);
+    g[both].merged = both || text_len == 0;
     for (int k = 0; k < 2; ++k)
       for (int q = 0; q < parts; ++q) {
         const bool same = dw[0][q] == dw[1][q];
         if (!dw[k][q] || same != (both != 0) || (both && k)) continue;
-        p.out_stream[p.outs] = k;
-        p.out_part[p.outs] = q;
-        p.dw[p.outs++] = dw[k][q];
+        const int o = g[both].outs++;
+        g[both].out_stream[o] = k;
+        g[both].out_part[o] = q;
+        g[both].dw[o] = dw[k][q];
       }
-    if (p.outs == 0) continue;
-    he = timed(K_LINEAR_DW, st, [&] { return launch_product(PRODUCT_DW, p, st); });
+  }
+  const bool form_dx = dx && rows > 0, one = (g[0].outs > 0) != (g[1].outs > 0), together = !bf16 && form_dx && one;
+  b.sums_later = together;
+  hipError_t he = timed(K_LINEAR_GATE_BACK, st, [&] { return launch_gate_back(bf16, b, st); });
+  if (he != hipSuccess) return HILO_E_DEVICE;
+  if (together)
+    return dev_status(timed(K_LINEAR_BACK, st, [&] { return launch_product_back(p, g[g[1].outs > 0], b, st); }));
+  if (form_dx) {
+    he = timed(K_LINEAR_BACK, st, [&] { return launch_product(PRODUCT_DX, p, st); });
+    if (he != hipSuccess) return HILO_E_DEVICE;
+  }
+  for (const ProductProblem &q : g) {
+    if (q.outs == 0) continue;
+    he = timed(K_LINEAR_BACK, st, [&] { return launch_product(PRODUCT_DW, q, st); });
     if (he != hipSuccess) return HILO_E_DEVICE;
   }
   return HILO_OK;

@@ -261,9 +261,13 @@ struct GateBackProblem {
   void *db[2][2];        // [stream][part]: [N]
   float *part;           // gate_back_bytes
   int block_rows;        // set by the launcher
+  int sums_later;        // the sums are launch_product_back's
 };
 size_t gate_back_bytes(long long rows, int N, int parts, int B);
 hipError_t launch_gate_back(bool bf16, GateBackProblem p, hipStream_t st);
+// In float32 the rest of a backward pass with a dx and weight gradients of one kind: both products in a launch, their
+// partial sums and those over the rows in another.
+hipError_t launch_product_back(ProductProblem x, ProductProblem w, GateBackProblem g, hipStream_t st);
 
 // E4M3 codes and E8M0 scales (scale_stride(cols) a row) of x [rows][cols], a scale for each 128 columns of a row, or
 // for block_rows 128 of 128 rows; limit: a device pointer to the number of rows, or null.

@@ -7,6 +7,8 @@
 
 namespace hilo {
 
+constexpr uint32_t kBehind = 0x80000000u;  // an offset behind any buffer's end, also with rows of the tile added
+
 // A run of rows of one stream.  Segment 2 s is sample s's image rows, 2 s + 1 its text rows; merged, all rows are one.
 struct Segment {
   int lo, n, stream;

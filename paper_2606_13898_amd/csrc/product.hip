@@ -73,46 +73,114 @@ HILO_DEV float e8m0(uint8_t b) {
 // values long, so that 16 lanes' 16-byte reads fall on all banks once.  A lane of group lg takes k = 16 s + 4 lg .. + 3.
 constexpr int kStep = 32, kPad = 36, kAhead = 2;
 
+// 8 values of a step of an operand, as a thread loads them and lays them into LDS as [row][k].
+template <int TYPE>
+struct Piece {
+  typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+  typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+  u32x4 u[TYPE == TYPE_F32 ? 2 : 1];  // codes: the first two
+  uint32_t scale;
+  static HILO_DEV int half(int wid) { return (TYPE == TYPE_F32 ? wid >> 1 : wid) & 1; }
+  // With k first 16 lanes have 16 columns of 8 k, so that the 8-byte stores to 16 rows of LDS fall on 32 banks, not on 8.
+  static HILO_DEV int k_first(int tid) { return 8 * (tid >> 6) + 2 * (tid >> 2 & 3); }
+  static HILO_DEV int col_first(int tid) { return 16 * (tid >> 4 & 3) + 4 * (tid & 3); }
+  // From the tile's first value x[at] on, `pitch` values from row to row of memory, of which there are `rows` of `cols`.
+  // K_LAST: a row has consecutive k.  float32: 4 values of two rows 32 apart, codes: 8 of one; PAIRED: rows of 16 columns
+  // of one part and of the other.  Otherwise a row of memory has one k: 4 values of each of two consecutive k.
+  template <bool K_LAST, bool PAIRED = false>
+  HILO_DEV void load(const void *x, size_t at, int pitch, int rows, int cols, int tid) {
+    constexpr int E = TYPE == TYPE_F32 ? 4 : 1;
+    const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(reinterpret_cast<const char *>(x)) + at * E, 0,
+                                                        int(kBehind - 1), 0x00020000);
+    if constexpr (TYPE == TYPE_F32) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        int q = K_LAST ? (tid >> 3) + 32 * j : k_first(tid) + j;
+        if (PAIRED) q = (tid >> 3 & 15) + 16 * j;
+        const int c = K_LAST ? 4 * (tid & 7) : col_first(tid);
+        u[j] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, q < rows && c < cols ? (q * pitch + c) * E : kBehind, 0, 0);
+      }
+    } else {
+      static_assert(K_LAST || TYPE == TYPE_F32, "codes are loaded for the first product alone");
+      int q = tid >> 2;
+      if (PAIRED) q = 16 * (q >> 5) + (q & 15);
+      const int c = 8 * (tid & 3);
+      const u32x2 v = __builtin_amdgcn_raw_buffer_load_b64(rsrc, q < rows && c < cols ? q * pitch + c : kBehind, 0, 0);
+      u[0] = u32x4{v[0], v[1], 0u, 0u};
+    }
+  }
+  HILO_DEV void load_scale(const uint8_t *x, int pitch, int rows, int cols, int tid) {
+    const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(x), 0, int(kBehind - 1), 0x00020000);
+    const int q = tid >> 2;
+    scale = __builtin_amdgcn_raw_buffer_load_b8(rsrc, q < rows && cols > 0 ? q * pitch : kBehind, 0, 0);
+  }
+  template <bool K_LAST>
+  HILO_DEV void store(float (&lds)[64][kPad], int tid) const {
+    if constexpr (TYPE == TYPE_FP8) {
+      const float s = e8m0(uint8_t(scale));
+      f32x4 f[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const auto v = __builtin_amdgcn_cvt_pk_f32_fp8(u[0][h], false), w = __builtin_amdgcn_cvt_pk_f32_fp8(u[0][h], true);
+        f[h] = f32x4{v[0] * s, v[1] * s, w[0] * s, w[1] * s};
+      }
+      f32x4 *to = reinterpret_cast<f32x4 *>(&lds[tid >> 2][8 * (tid & 3)]);
+      to[0] = f[0];
+      to[1] = f[1];
+    } else if constexpr (K_LAST) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j) *reinterpret_cast<u32x4 *>(&lds[(tid >> 3) + 32 * j][4 * (tid & 7)]) = u[j];
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) *reinterpret_cast<u32x2 *>(&lds[col_first(tid) + e][k_first(tid)]) = u32x2{u[0][e], u[1][e]};
+    }
+  }
+};
+
+typedef float ProductLds[2][2][2][64][kPad];  // [group][buffer][operand][row][k]
+
+// The items of workgroup `block` of `blocks`.
 template <int TYPE, int KIND, bool GATED>
-__global__ __launch_bounds__(512) void k_product(ProductProblem p) {
+HILO_DEV void product_items(const ProductProblem &p, int block, int blocks, ProductLds &buffers) {
   constexpr bool AK = KIND != PRODUCT_DW, BK = KIND == PRODUCT_OUT;  // operand's last index is k
   constexpr int BN = GATED && KIND == PRODUCT_OUT ? 32 : 64;         // columns of a tile
-  __shared__ __attribute__((aligned(16))) float buffers[2][2][2][64][kPad];
   const int tid = threadIdx.x & 255, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int group = __builtin_amdgcn_readfirstlane(threadIdx.x >> 8);
   float (&lds)[2][2][64][kPad] = buffers[group];
   const int lr = lane & 15, lg = lane >> 4, wm = wid >> 1, wn = wid & 1;
   const int cols = KIND == PRODUCT_OUT ? p.N : p.K, tn_count = (cols + BN - 1) / BN;
   const int tm_count = KIND == PRODUCT_DW ? (p.N + 63) / 64 : row_tiles_bound(p, 64);
-  const long long tiles = (long long)tm_count * tn_count * (KIND == PRODUCT_DW ? p.outs : 1);
+  const int tr_count = KIND == PRODUCT_DW ? tm_count * p.outs : tm_count;
   // steps of the whole sum; of a segment's rows in DW
-  const int parts = KIND == PRODUCT_DX ? p.parts : 1, per = (KIND == PRODUCT_OUT ? p.K : p.N) + kStep - 1;
-  for (long long item = blockIdx.x; item < tiles * p.splits; item += gridDim.x) {
-    const long long tile = item / p.splits;
-    const int split = int(item - tile * p.splits);
-    const int tn = int(tile % tn_count), tr = int(tile / tn_count), n0 = tn * BN;
+  const int parts = KIND == PRODUCT_DX ? p.parts : 1, per = (KIND == PRODUCT_OUT ? p.K : p.N) + kStep - 1, each = per / kStep;
+  // a workgroup keeps its columns and its split, and goes from row tile to row tile
+  const uint32_t wide = uint32_t(tn_count) * p.splits;
+  const int across = int(uint32_t(block) % wide), tn = int(uint32_t(across) / uint32_t(p.splits)), split = across - tn * p.splits, n0 = tn * BN;
+  for (int tr = int(uint32_t(block) / wide); tr < tr_count; tr += int(uint32_t(blocks) / wide)) {
     int o = 0, stream = 0, part = 0, row0 = 0, rows = 64;
     if constexpr (KIND == PRODUCT_DW) {
-      o = tr / tm_count;
-      row0 = (tr - o * tm_count) * 64;
+      int t = tr;
+      for (; t >= tm_count; t -= tm_count) ++o;
+      row0 = t * 64;
       stream = p.out_stream[o];
       part = p.out_part[o];
       rows = min(64, p.N - row0);
     } else {
       const RowTile rt = find_row_tile(p, 64, tr);
       if (rt.n == 0) continue;  // behind the last
-      row0 = rt.row0;
-      rows = rt.n;
-      stream = rt.stream;
+      row0 = uni(rt.row0);
+      rows = uni(rt.n);
+      stream = uni(rt.stream);
     }
     // ---- where the sum runs: pieces of k, walked from step s0 to s1
     int total = 0;
     if constexpr (KIND == PRODUCT_DW) {
       for (int i = stream; i < segments(p); i += 2) total += (max(segment(p, i).n, 0) + kStep - 1) / kStep;
     } else {
-      total = parts * (per / kStep);
+      total = parts * each;
     }
-    const int s0 = int((long long)total * split / p.splits), s1 = int((long long)total * (split + 1) / p.splits);
+    const int least = int(uint32_t(total) / uint32_t(p.splits)), over = total - least * p.splits;
+    const int s0 = least * split + min(split, over), s1 = s0 + least + (split < over ? 1 : 0);
     int seg = stream, seg_lo = 0, seg_n = 0, seg_s = 0;  // DW: the segment of the step, its first step
     if constexpr (KIND == PRODUCT_DW) {
       if (s0 < s1) {
@@ -126,69 +194,53 @@ __global__ __launch_bounds__(512) void k_product(ProductProblem p) {
         seg_n = g.n;
       }
     }
-    auto load = [&](int s, Chunk<TYPE> &a, Chunk<TYPE> &b) __attribute__((always_inline)) {
-      a.zero();
-      b.zero();
-      int k0, kn;  // first k of the step in its piece, and the piece's length
-      int dpart = part;
+    // A step's operands, of a step behind the last zeros.  No load stands behind a branch, so that a wait knows how many it
+    // leaves on their way.
+    auto load = [&](int s, Piece<TYPE> &a, Piece<TYPE> &b) __attribute__((always_inline)) {
+      const bool more = s < s1;
+      int k0 = 0, kn = 0;  // first k of the step in its piece, and how many there are from there
       if constexpr (KIND == PRODUCT_DW) {
-        while (s - seg_s >= (seg_n + kStep - 1) / kStep) {
-          seg_s += (max(seg_n, 0) + kStep - 1) / kStep;
-          seg += 2;
-          const Segment g = segment(p, seg);
-          seg_lo = g.lo;
-          seg_n = g.n;
+        if (more) {
+          while (s - seg_s >= (seg_n + kStep - 1) / kStep) {
+            seg_s += (max(seg_n, 0) + kStep - 1) / kStep;
+            seg += 2;
+            const Segment g = segment(p, seg);
+            seg_lo = g.lo;
+            seg_n = g.n;
+          }
+          k0 = (s - seg_s) * kStep;
+          kn = seg_n - k0;
         }
-        k0 = (s - seg_s) * kStep;
-        kn = seg_n;
+        const size_t row = size_t(seg_lo) + k0;
+        a.template load<false>(p.d, (row * p.parts + part) * p.N + row0, p.parts * p.N, kn, p.N - row0, tid);
+        b.template load<false>(p.x, row * p.K + n0, p.K, kn, p.K - n0, tid);
       } else {
-        const int each = per / kStep;
-        dpart = s / each;
-        k0 = (s - dpart * each) * kStep;
-        kn = per - kStep + 1;
-      }
-      const int r = tid >> 2, c = 8 * (tid & 3);  // k last: row, k
-      const int q = tid >> 3, m = 8 * (tid & 7);  // k first: k, row
-      if constexpr (KIND == PRODUCT_OUT) {
-        if (r < rows && k0 + c < kn) {
-          a.load(p.x, size_t(row0 + r) * p.K + k0 + c);
-          if constexpr (TYPE == TYPE_FP8) a.scale = e8m0(p.x_scale[size_t(row0 + r) * scale_stride(p.K) + (k0 + c) / 128]);
+        const int dpart = KIND == PRODUCT_DX && more && s >= each ? 1 : 0;
+        if (more) {
+          k0 = (s - dpart * each) * kStep;
+          kn = per - kStep + 1 - k0;
         }
-        const int wp = GATED ? (r >> 4) & 1 : 0, n = n0 + (GATED ? 16 * (r >> 5) + (r & 15) : r);
-        if (n < p.N && k0 + c < kn) {
+        if constexpr (KIND == PRODUCT_DX) {
+          a.template load<true>(p.d, (size_t(row0) * p.parts + dpart) * p.N + k0, p.parts * p.N, rows, kn, tid);
+          const void *w = stream ? (dpart ? p.w[1][1] : p.w[1][0]) : (dpart ? p.w[0][1] : p.w[0][0]);
+          b.template load<false>(w, size_t(k0) * p.K + n0, p.K, kn, p.K - n0, tid);
+        } else {
+          a.template load<true>(p.x, size_t(row0) * p.K + k0, p.K, rows, kn, tid);
+          // with a gate rows of 16 columns of one part and of the other, in turn; a wave's are of one part
+          const int wp = GATED ? Piece<TYPE>::half(wid) : 0;
           const void *w = stream ? (wp ? p.w[1][1] : p.w[1][0]) : (wp ? p.w[0][1] : p.w[0][0]);
-          b.load(w, size_t(n) * p.K + k0 + c);
+          b.template load<true, GATED>(w, size_t(n0) * p.K + k0, p.K, p.N - n0, kn, tid);
           if constexpr (TYPE == TYPE_FP8) {
             const uint8_t *ws = stream ? (wp ? p.w_scale[1][1] : p.w_scale[1][0]) : (wp ? p.w_scale[0][1] : p.w_scale[0][0]);
-            b.scale = e8m0(ws[size_t(n / 128) * scale_stride(p.K) + (k0 + c) / 128]);
+            a.load_scale(p.x_scale + size_t(row0) * scale_stride(p.K) + k0 / 128, scale_stride(p.K), rows, kn, tid);
+            b.load_scale(ws + size_t(n0 / 128) * scale_stride(p.K) + k0 / 128, 0, 64, kn, tid);  // one of all the tile's columns
           }
-        }
-      } else if constexpr (KIND == PRODUCT_DX) {
-        if (r < rows && k0 + c < kn) a.load(p.d, (size_t(row0 + r) * p.parts + dpart) * p.N + k0 + c);
-        const void *w = stream ? (dpart ? p.w[1][1] : p.w[1][0]) : (dpart ? p.w[0][1] : p.w[0][0]);
-        if (k0 + q < kn && n0 + m < p.K) b.load(w, size_t(k0 + q) * p.K + n0 + m);
-      } else {
-        if (k0 + q < kn) {
-          const size_t row = size_t(seg_lo) + k0 + q;
-          if (row0 + m < p.N) a.load(p.d, (row * p.parts + dpart) * p.N + row0 + m);
-          if (n0 + m < p.K) b.load(p.x, row * p.K + n0 + m);
         }
       }
     };
-    auto store = [&](int buf, const Chunk<TYPE> &a, const Chunk<TYPE> &b) __attribute__((always_inline)) {
-      float f[8];
-      a.values(f);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        if constexpr (AK) lds[buf][0][tid >> 2][8 * (tid & 3) + e] = f[e];
-        else lds[buf][0][8 * (tid & 7) + e][tid >> 3] = f[e];
-      }
-      b.values(f);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        if constexpr (BK) lds[buf][1][tid >> 2][8 * (tid & 3) + e] = f[e];
-        else lds[buf][1][8 * (tid & 7) + e][tid >> 3] = f[e];
-      }
+    auto store = [&](int buf, const Piece<TYPE> &a, const Piece<TYPE> &b) __attribute__((always_inline)) {
+      a.template store<AK>(lds[buf][0], tid);
+      b.template store<BK>(lds[buf][1], tid);
     };
     f32x4 acc[2][2];
 #pragma unroll
@@ -196,21 +248,13 @@ __global__ __launch_bounds__(512) void k_product(ProductProblem p) {
 #pragma unroll
       for (int j = 0; j < 2; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     if (s0 < s1) {
-      Chunk<TYPE> a[kAhead], b[kAhead];
-      auto fetch = [&](int s, Chunk<TYPE> &ca, Chunk<TYPE> &cb) __attribute__((always_inline)) {
-        if (s < s1) {
-          load(s, ca, cb);
-        } else {  // the group without a last step
-          ca.zero();
-          cb.zero();
-        }
-      };
+      Piece<TYPE> a[kAhead], b[kAhead];
 #pragma unroll
-      for (int k = 0; k < kAhead; ++k) fetch(s0 + group + 2 * k, a[k], b[k]);
+      for (int k = 0; k < kAhead; ++k) load(s0 + group + 2 * k, a[k], b[k]);
       // step s of the group out of buffer buf
-      auto step = [&](int s, int buf, Chunk<TYPE> &ca, Chunk<TYPE> &cb) __attribute__((always_inline)) {
+      auto step = [&](int s, int buf, Piece<TYPE> &ca, Piece<TYPE> &cb) __attribute__((always_inline)) {
         store(buf, ca, cb);
-        fetch(s + 2 * kAhead, ca, cb);
+        load(s + 2 * kAhead, ca, cb);
         __syncthreads();
 #pragma unroll
         for (int h = 0; h < kStep / 16; ++h) {
@@ -230,9 +274,12 @@ __global__ __launch_bounds__(512) void k_product(ProductProblem p) {
       };
       static_assert(kAhead == 2, "a buffer for every other step");
 #pragma unroll 1
-      for (int s = s0; s < s1; s += 2 * kAhead) {  // both groups the same number of steps
+      for (int s = s0;; s += 2) {  // both groups the same number of steps
         step(s + group, 0, a[0], b[0]);
-        if (s + 2 < s1) step(s + 2 + group, 1, a[1], b[1]);
+        s += 2;
+        if (s >= s1) break;
+        step(s + group, 1, a[1], b[1]);
+        if (s + 2 >= s1) break;
       }
     }
     // ---- group g finishes row block g of every wave's two
@@ -284,19 +331,33 @@ __global__ __launch_bounds__(512) void k_product(ProductProblem p) {
   }
 }
 
-// Sums of the splits, in order, and the last step.  A thread has four columns of a row.
+template <int TYPE, int KIND, bool GATED>
+__global__ __launch_bounds__(512) void k_product(ProductProblem p) {
+  __shared__ __attribute__((aligned(16))) ProductLds buffers;
+  product_items<TYPE, KIND, GATED>(p, blockIdx.x, gridDim.x, buffers);
+}
+
+// Both products of a float32 backward pass in one launch: the first blocks_x workgroups have dx, the others dw.
+__global__ __launch_bounds__(512) void k_product_back(ProductProblem x, ProductProblem w, int blocks_x) {
+  __shared__ __attribute__((aligned(16))) ProductLds buffers;
+  if (int(blockIdx.x) < blocks_x) product_items<TYPE_F32, PRODUCT_DX, false>(x, blockIdx.x, blocks_x, buffers);
+  else product_items<TYPE_F32, PRODUCT_DW, false>(w, blockIdx.x - blocks_x, gridDim.x - blocks_x, buffers);
+}
+
+// Sums of the splits, in order, and the last step, by workgroup `block` of `blocks`.  A thread has four columns of a row.
 template <int KIND, bool GATED>
-__global__ __launch_bounds__(256) void k_product_join(ProductProblem p) {
+HILO_DEV void join_items(const ProductProblem &p, int block, int blocks) {
   const int cols = KIND == PRODUCT_OUT ? p.N : p.K, quads = cols / 4;
   const long long all = KIND == PRODUCT_DW ? (long long)p.outs * p.N : p.rows;
   const long long rows = KIND == PRODUCT_DW ? all : cu_at(p.cu, p.B);
   constexpr int W = KIND == PRODUCT_OUT && GATED ? 2 : 1;
-  for (long long t = blockIdx.x * 256ll + threadIdx.x; t < rows * quads; t += gridDim.x * 256ll) {
+  for (long long t = block * 256ll + threadIdx.x; t < rows * quads; t += blocks * 256ll) {
     const long long row = t / quads;
     const int n = int(t - row * quads) * 4;
     f32x4 v[W];
 #pragma unroll
     for (int w = 0; w < W; ++w) v[w] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
     for (int s = 0; s < p.splits; ++s)
 #pragma unroll
       for (int w = 0; w < W; ++w)
@@ -317,38 +378,57 @@ __global__ __launch_bounds__(256) void k_product_join(ProductProblem p) {
   }
 }
 
-// Splits of the sum where tiles are fewer than two for each of the 256 CUs, no shorter than 4 steps each.
+template <int KIND, bool GATED>
+__global__ __launch_bounds__(256) void k_product_join(ProductProblem p) {
+  join_items<KIND, GATED>(p, blockIdx.x, gridDim.x);
+}
+
+// Splits of the sum, no shorter than 4 steps each, where tiles are fewer than two for each of the 256 CUs; one in a backward
+// pass, whose two products run together.
+constexpr long long kSplitTiles = 512;
+static long long most_splits(int kind, long long rows, int K, int N, int parts) {
+  const long long steps = kind == PRODUCT_OUT ? K / kStep : kind == PRODUCT_DX ? (long long)parts * N / kStep : rows / kStep;
+  return std::max(1ll, steps / 4);
+}
 static int splits_of(int kind, long long rows, int K, int N, int parts, int outs, int B, bool merged) {
   const long long tm = kind == PRODUCT_DW ? (long long)outs * ((N + 63) / 64) : (rows + 63) / 64 + (merged ? 0 : 2 * B - 1);  // row_tiles_bound
   const int bn = kind == PRODUCT_OUT && parts == 2 ? 32 : 64, cols = kind == PRODUCT_OUT ? N : K;
   const long long tiles = std::max(1ll, tm * ((cols + bn - 1) / bn));
-  const long long steps = kind == PRODUCT_OUT ? K / kStep : kind == PRODUCT_DX ? (long long)parts * N / kStep : rows / kStep;
-  return int(std::min(std::max(1ll, 512 / tiles), std::max(1ll, steps / 4)));
+  return int(std::min(std::max(1ll, (kind == PRODUCT_OUT ? kSplitTiles : kSplitTiles / 2) / tiles), most_splits(kind, rows, K, N, parts)));
 }
 
-// Most partial sums of any call: one segment has the fewest tiles, so the most splits.
+// Bounds the partial sums of any call, and grows with the sizes: a tile's are 64 x 64.
 size_t product_part_bytes(bool bf16, int kind, long long rows, int K, int N, int parts) {
   if (bf16) return kind == PRODUCT_OUT && rows <= kProductFewRows ? 0 : product_tiles_part_bytes();
-  size_t most = 0;
-  for (int outs = 1; outs <= (kind == PRODUCT_DW ? 4 : 1); ++outs) {
-    const int s = splits_of(kind, rows, K, N, parts, outs, 1, true);
-    const size_t each = kind == PRODUCT_OUT ? size_t(rows) * parts * N : kind == PRODUCT_DX ? size_t(rows) * K : size_t(outs) * N * K;
-    if (s > 1) most = std::max(most, s * each * sizeof(float));
-  }
-  return most;
+  const long long most = most_splits(kind, rows, K, N, parts);
+  if (most == 1) return 0;
+  const long long each = kind == PRODUCT_OUT ? rows * parts * N : kind == PRODUCT_DX ? rows * K : 4ll * N * K;
+  return size_t(std::min((most * each + 63) / 64, kSplitTiles * 64)) * 64 * sizeof(float);
 }
+
+// Sets the splits; workgroups of the product and of the sums of its splits.
+static int product_blocks(int kind, ProductProblem &p) {
+  p.splits = splits_of(kind, p.rows, p.K, p.N, p.parts, p.outs, p.B, p.merged);
+  const long long tm = kind == PRODUCT_DW ? (long long)p.outs * ((p.N + 63) / 64) : row_tiles_bound(p, 64);
+  const int cols = kind == PRODUCT_OUT ? p.N : p.K, bn = kind == PRODUCT_OUT && p.parts == 2 ? 32 : 64;
+  const int wide = (cols + bn - 1) / bn * p.splits;  // of one row tile
+  return int(std::min(tm, std::max(1ll, (1ll << 20) / wide))) * wide;
+}
+static int join_blocks(int kind, const ProductProblem &p) {
+  if (p.splits == 1) return 0;
+  const long long quads = (kind == PRODUCT_DW ? (long long)p.outs * p.N : p.rows) * ((kind == PRODUCT_OUT ? p.N : p.K) / 4);
+  return int(std::min((quads + 255) / 256, 4096ll));
+}
+
 template <int TYPE, int KIND, bool GATED>
 static hipError_t run(ProductProblem &p, hipStream_t st) {
-  p.splits = splits_of(KIND, p.rows, p.K, p.N, p.parts, p.outs, p.B, p.merged);
-  const long long tm = KIND == PRODUCT_DW ? (long long)p.outs * ((p.N + 63) / 64) : row_tiles_bound(p, 64);
-  const int cols = KIND == PRODUCT_OUT ? p.N : p.K, bn = KIND == PRODUCT_OUT && GATED ? 32 : 64;
-  const long long items = tm * ((cols + bn - 1) / bn) * p.splits;
-  if (items <= 0) return hipSuccess;
-  hipLaunchKernelGGL((k_product<TYPE, KIND, GATED>), dim3(unsigned(std::min(items, 1ll << 20))), dim3(512), 0, st, p);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || p.splits == 1) return e;
-  const long long quads = (KIND == PRODUCT_DW ? (long long)p.outs * p.N : p.rows) * (cols / 4);
-  hipLaunchKernelGGL((k_product_join<KIND, GATED>), dim3(unsigned(std::min((quads + 255) / 256, 4096ll))), dim3(256), 0, st, p);
+  const int blocks = product_blocks(KIND, p);
+  if (blocks <= 0) return hipSuccess;
+  hipLaunchKernelGGL((k_product<TYPE, KIND, GATED>), dim3(blocks), dim3(512), 0, st, p);
+  const hipError_t e = hipGetLastError();
+  const int joins = join_blocks(KIND, p);
+  if (e != hipSuccess || joins == 0) return e;
+  hipLaunchKernelGGL((k_product_join<KIND, GATED>), dim3(joins), dim3(256), 0, st, p);
   return hipGetLastError();
 }
 
@@ -410,7 +490,7 @@ hipError_t launch_product_fp8(ProductProblem p, hipStream_t st) {
 // 512 columns: a wave every fourth row, a lane 8 columns, four rows on their way.  What a column's rows sum to goes to
 // part[row block][parts][N], and k_gate_back_sum adds those of a stream's blocks in their order.
 constexpr int kBackCols = 512;
-static int back_rows(long long rows) { return rows >= 8192 ? 256 : rows >= 2048 ? 64 : 16; }
+static int back_rows(long long rows) { return rows >= 8192 ? 256 : rows >= 2048 ? 64 : rows >= 1024 ? 16 : 4; }
 
 template <bool BF16, bool GATED>
 __global__ __launch_bounds__(256) void k_gate_back(GateBackProblem p) {
@@ -490,16 +570,16 @@ __global__ __launch_bounds__(256) void k_gate_back(GateBackProblem p) {
   }
 }
 
-// A workgroup has 64 columns of one sum, a wave every eighth row block, eight on their way.
-template <bool BF16>
-__global__ __launch_bounds__(512) void k_gate_back_sum(GateBackProblem p) {
-  __shared__ float sums[8][64];
+// A workgroup has 64 columns (block) of one sum, a wave every W-th row block, eight on their way.
+template <bool BF16, int W>
+HILO_DEV void sum_columns(const GateBackProblem &p, int block, int which) {
+  __shared__ float sums[W][64];
   const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int stream = blockIdx.y / p.parts, part = blockIdx.y % p.parts;
+  const int stream = which / p.parts, part = which % p.parts;
   void *db = stream ? p.db[1][part] : p.db[0][part];
   const bool both = p.db[0][part] == p.db[1][part];
   if (!db || (both && stream)) return;
-  const int n = blockIdx.x * 64 + lane;
+  const int n = block * 64 + lane;
   float v = 0.f;
   int t0 = 0;  // blocks before the segment
   for (int i = 0; i < segments(p); ++i) {
@@ -508,12 +588,12 @@ __global__ __launch_bounds__(512) void k_gate_back_sum(GateBackProblem p) {
     if (both || s.stream == stream) {
       const float *from = p.part + (size_t(t0) * p.parts + part) * p.N + min(n, p.N - 1);
 #pragma unroll 1
-      for (int t = wid; t < tiles; t += 64) {
+      for (int t = wid; t < tiles; t += 8 * W) {
         float w[8];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) w[k] = from[size_t(min(t + 8 * k, tiles - 1)) * p.parts * p.N];
+        for (int k = 0; k < 8; ++k) w[k] = from[size_t(min(t + W * k, tiles - 1)) * p.parts * p.N];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v += t + 8 * k < tiles ? w[k] : 0.f;
+        for (int k = 0; k < 8; ++k) v += t + W * k < tiles ? w[k] : 0.f;
       }
     }
     t0 += tiles;
@@ -523,15 +603,32 @@ __global__ __launch_bounds__(512) void k_gate_back_sum(GateBackProblem p) {
   if (wid == 0 && n < p.N) {
     float s = sums[0][lane];
 #pragma unroll
-    for (int k = 1; k < 8; ++k) s += sums[k][lane];
+    for (int k = 1; k < W; ++k) s += sums[k][lane];
     if (BF16) reinterpret_cast<uint16_t *>(db)[n] = f2bf(s);
     else reinterpret_cast<float *>(db)[n] = s;
   }
 }
 
+template <bool BF16>
+__global__ __launch_bounds__(512) void k_gate_back_sum(GateBackProblem p) {
+  sum_columns<BF16, 8>(p, blockIdx.x, blockIdx.y);
+}
+
+// What is left of a float32 backward pass, in one launch: sums of the splits of dx and of dw, and over the rows.
+__global__ __launch_bounds__(256) void k_join_back(ProductProblem x, ProductProblem w, GateBackProblem g, int blocks_x, int blocks_w) {
+  int block = blockIdx.x;
+  if (block < blocks_x) return join_items<PRODUCT_DX, false>(x, block, blocks_x);
+  block -= blocks_x;
+  if (block < blocks_w) return join_items<PRODUCT_DW, false>(w, block, blocks_w);
+  block -= blocks_w;
+  const int cols = (g.N + 63) / 64;
+  sum_columns<false, 4>(g, block % cols, block / cols);
+}
+
+// Bounds any call's blocks (back_rows: 256 of 4 rows, 128 of 16 or of 64, or of 256 rows), and grows with the rows.
 size_t gate_back_bytes(long long rows, int N, int parts, int B) {
-  const int block = back_rows(rows);
-  return (size_t(rows + block - 1) / block + 2 * size_t(B)) * parts * N * sizeof(float);
+  const long long blocks = std::max(std::min((rows + 3) / 4, 256ll), (rows + 255) / 256);
+  return (size_t(blocks) + 2 * size_t(B)) * parts * N * sizeof(float);
 }
 
 template <bool BF16, bool GATED>
@@ -542,7 +639,7 @@ static hipError_t run_gate_back(const GateBackProblem &p, hipStream_t st) {
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  if (!p.part) return hipSuccess;
+  if (!p.part || p.sums_later) return hipSuccess;
   hipLaunchKernelGGL((k_gate_back_sum<BF16>), dim3((p.N + 63) / 64, 2 * p.parts), dim3(512), 0, st, p);
   return hipGetLastError();
 }
@@ -551,6 +648,17 @@ hipError_t launch_gate_back(bool bf16, GateBackProblem p, hipStream_t st) {
   p.block_rows = back_rows(p.rows);
   if (p.parts == 2) return bf16 ? run_gate_back<true, true>(p, st) : run_gate_back<false, true>(p, st);
   return bf16 ? run_gate_back<true, false>(p, st) : run_gate_back<false, false>(p, st);
+}
+
+hipError_t launch_product_back(ProductProblem x, ProductProblem w, GateBackProblem g, hipStream_t st) {
+  g.block_rows = back_rows(g.rows);
+  const int bx = product_blocks(PRODUCT_DX, x), bw = product_blocks(PRODUCT_DW, w);
+  hipLaunchKernelGGL(k_product_back, dim3(bx + bw), dim3(512), 0, st, x, w, bx);
+  const hipError_t e = hipGetLastError();
+  const int jx = join_blocks(PRODUCT_DX, x), jw = join_blocks(PRODUCT_DW, w), sums = g.part ? (g.N + 63) / 64 * 2 * g.parts : 0;
+  if (e != hipSuccess || jx + jw + sums == 0) return e;
+  hipLaunchKernelGGL(k_join_back, dim3(jx + jw + sums), dim3(256), 0, st, x, w, g, jx, jw);
+  return hipGetLastError();
 }
 
 // ----------------------------------------------------------------------------------- quantisation of blocks

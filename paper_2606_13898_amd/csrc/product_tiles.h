@@ -102,7 +102,6 @@ HILO_DEV void buffer_to_lds(const char *base, uint32_t bytes, uint32_t offset, v
       __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(base), 0, int(bytes), 0x00020000),
       (__attribute__((address_space(3))) void *)lds_wave_base, 16, int(offset), 0, 0, 0);
 }
-constexpr uint32_t kBehind = 0x80000000u;  // an offset behind any buffer's end, also with rows of the tile added
 
 template <int N>
 HILO_DEV void wait_vm() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
