@@ -157,6 +157,30 @@ def test_backward(shape, kind):
 
 
 @pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32], ids=case_id)
+@pytest.mark.parametrize("shared", [("w",), ("w_gate", "b"), ("b", "b_gate"), ("w", "b", "b_gate")], ids=str)
+def test_backward_partly_shared(dt, shared):
+    """Two streams' gradients of which some are one tensor: that one has the sum over both, the others their stream's."""
+    g = torch.Generator().manual_seed(len(shared))
+    cu, text, k, n = pack([70, 9, 130], 33), 33, 72, 136
+    x, dout, pre = (torch.randn(cu[-1], *s, generator=g).to(dt) for s in ((k,), (n,), (2, n)))
+    ws = weights(g, 2, n, k, dt, "silu", True)
+    got = [{name: torch.full_like(v, 7.0, device="cuda") for name, v in d.items()} for d in ws]
+    got[1].update({name: got[0][name] for name in shared})
+    dx, cud = torch.zeros(cu[-1], k, dtype=dt, device="cuda"), torch.tensor(cu, dtype=torch.int32, device="cuda")
+    ws_dev = torch.empty(hilo.hilo_linear_backward_workspace_bytes(dt, cu[-1], k, n, 3, gated=True), dtype=torch.uint8, device="cuda")
+    hilo.hilo_linear_backward(hilo.linear_weights(cuda(ws)), x.cuda(), pre.cuda(), dout.cuda(), dx, hilo.linear_grads(got), cud, text,
+                              act=ACTS["silu"], workspace=ws_dev)
+    (wx, bx), want = P.backward(x.to(F64), ws, pre.to(F64), dout.to(F64), "silu", cu, text, HALF[dt], False)
+    near(dx, wx, bx, "dx")
+    for kk in range(2):
+        for name, t in got[kk].items():
+            if name in shared:
+                near(t, *(want[0][name][j] + want[1][name][j] for j in range(2)), name)
+            else:
+                near(t, *want[kk][name], f"{name} of {kk}")
+
+
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32], ids=case_id)
 @pytest.mark.parametrize("rows, cols", [(1, 16), (5, 128), (130, 144), (77, 1040), (300, 512), (3, 4112)])
 @pytest.mark.parametrize("block_rows", [1, 128])
 def test_quantize(dt, rows, cols, block_rows):
