@@ -1197,12 +1197,15 @@ hilo_status hilo_linear_backward(int32_t dtype, const hilo_linear_w w[2], const 
         g[both].dw[o] = dw[k][q];
       }
   }
-  const bool form_dx = dx && rows > 0, one = (g[0].outs > 0) != (g[1].outs > 0), together = !bf16 && form_dx && one;
-  b.sums_later = together;
+  const bool form_dx = dx && rows > 0, together = form_dx && (g[0].outs > 0) != (g[1].outs > 0);
+  b.sums_later = together && !bf16;
   hipError_t he = timed(K_LINEAR_GATE_BACK, st, [&] { return launch_gate_back(bf16, b, st); });
   if (he != hipSuccess) return HILO_E_DEVICE;
   if (together)
-    return dev_status(timed(K_LINEAR_BACK, st, [&] { return launch_product_back(p, g[g[1].outs > 0], b, st); }));
+    return dev_status(timed(K_LINEAR_BACK, st, [&] {
+      const ProductProblem &q = g[g[1].outs > 0];
+      return bf16 ? launch_product_back_tiles(p, q, st) : launch_product_back(p, q, b, st);
+    }));
   if (form_dx) {
     he = timed(K_LINEAR_BACK, st, [&] { return launch_product(PRODUCT_DX, p, st); });
     if (he != hipSuccess) return HILO_E_DEVICE;

@@ -243,6 +243,7 @@ hipError_t launch_product_fp8(ProductProblem p, hipStream_t st);
 // bf16 on large tiles (product_bf16.hip), with partial tiles in p.part.
 size_t product_tiles_part_bytes();
 hipError_t launch_product_tiles(int kind, const ProductProblem &p, hipStream_t st);
+hipError_t launch_product_back_tiles(ProductProblem x, ProductProblem w, hipStream_t st);  // PRODUCT_DX and PRODUCT_DW
 // At most kProductFewRows rows, bf16 or FP8 (product_few.hip): x bf16 or codes, out bf16, or float32 with out_f32.
 constexpr int kProductFewRows = 64;
 hipError_t launch_product_few(const ProductProblem &p, hipStream_t st);

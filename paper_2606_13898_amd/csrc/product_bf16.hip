@@ -533,6 +533,20 @@ __global__ __launch_bounds__(512, 2) void k_product_tiles(ProductProblem p) {
   }
 }
 
+// dx and the weights' gradients in a launch, whole 256 x 256 tiles of the one and then of the others: a workgroup's first of
+// the latter follows the last of the former.
+__global__ __launch_bounds__(512, 2) void k_product_back_tiles(ProductProblem x, ProductProblem w) {
+  using GX = Tile<0, PRODUCT_DX, false>;
+  using GW = Tile<0, PRODUCT_DW, false>;
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[std::max(GX::LDS, GW::LDS)];
+  const int pid = xcd_remap(blockIdx.x, P);
+  const Plan qx = make_plan<GX>(x, count_row_tiles(x, 256), 1, kCost[0]);
+  run<GX>(x, qx, pid, lds);
+  asm volatile("s_barrier" ::: "memory");
+  const Plan qw = make_plan<GW>(w, w.outs * ((w.N + 255) / 256), 1, kCost[0]);
+  run<GW>(w, qw, (pid + P - qx.tail) % P, lds);
+}
+
 template <int KIND, bool GATED>
 __global__ __launch_bounds__(512) void k_product_fix(ProductProblem p) {
   Plan q;
@@ -547,17 +561,56 @@ __global__ __launch_bounds__(512) void k_product_fix(ProductProblem p) {
 
 size_t product_tiles_part_bytes() { return size_t(pt::P) * 256 * 256 * sizeof(float); }
 
+// The plan, and its cost, where all the rows of the buffers are in use.
+template <int KIND, bool GATED>
+static long long plan_rows(ProductProblem p, pt::Plan &q) {
+  const int nk = KIND == PRODUCT_OUT ? (p.K + 63) / 64 : KIND == PRODUCT_DX ? p.parts * ((p.N + 63) / 64) : (p.rows + 63) / 64;
+  p.splits = 1;
+  const int best = pt::choose<KIND, GATED>(
+      p, nk, [&](int bm) { return KIND == PRODUCT_DW ? p.outs * ((p.N + bm - 1) / bm) : (p.rows + bm - 1) / bm; }, q);
+  return pt::plan_cost(q.T, nk, pt::kCost[best], true);
+}
+
 template <int KIND, bool GATED>
 static hipError_t run_tiles(ProductProblem p, hipStream_t st) {
-  const int nk = KIND == PRODUCT_OUT ? (p.K + 63) / 64 : KIND == PRODUCT_DX ? p.parts * ((p.N + 63) / 64) : (p.rows + 63) / 64;
   pt::Plan q;
-  p.splits = 1;
-  pt::choose<KIND, GATED>(p, nk, [&](int bm) { return KIND == PRODUCT_DW ? p.outs * ((p.N + bm - 1) / bm) : (p.rows + bm - 1) / bm; }, q);
+  plan_rows<KIND, GATED>(p, q);
   p.splits = q.s > 1;
   hipLaunchKernelGGL((pt::k_product_tiles<KIND, GATED>), dim3(pt::P), dim3(512), 0, st, p);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || !p.splits) return e;
   hipLaunchKernelGGL((pt::k_product_fix<KIND, GATED>), dim3(pt::P), dim3(512), 0, st, p);
+  return hipGetLastError();
+}
+
+// The longest of the workgroups' shares of whole 256 x 256 tiles, in order: of dx, where `both`, and of the weights' gradients.
+static long long shares(const ProductProblem &x, const ProductProblem &w, bool both) {
+  long long each[pt::P] = {};
+  int at = 0;
+  auto add = [&](int tiles, int nk) {
+    const long long cost = nk * pt::kCost[0].window + pt::kCost[0].tile;
+    for (int k = 0; k < pt::P; ++k) each[(at + k) % pt::P] += (tiles / pt::P + (k < tiles % pt::P)) * cost;
+    at += tiles % pt::P;
+  };
+  const int cols = (x.K + 255) / 256;
+  if (both) add((x.rows + 255) / 256 * cols, x.parts * ((x.N + 63) / 64));
+  for (int o = 0; o < w.outs; ++o) {
+    const long long text = std::min<long long>(x.rows, (long long)x.B * x.L);
+    const long long rows = w.merged ? x.rows : w.out_stream[o] ? text : x.rows - text;
+    add((w.N + 255) / 256 * cols, int((rows + 63) / 64));
+  }
+  return *std::max_element(each, each + pt::P);
+}
+
+hipError_t launch_product_back_tiles(ProductProblem x, ProductProblem w, hipStream_t st) {
+  pt::Plan q;
+  const long long dx = plan_rows<PRODUCT_DX, false>(x, q), dw = plan_rows<PRODUCT_DW, false>(w, q);
+  if (shares(x, w, true) >= dx + (w.merged ? dw : std::min(dw, shares(x, w, false)))) {
+    const hipError_t e = run_tiles<PRODUCT_DX, false>(x, st);
+    return e != hipSuccess ? e : run_tiles<PRODUCT_DW, false>(w, st);
+  }
+  x.splits = w.splits = 0;
+  hipLaunchKernelGGL(pt::k_product_back_tiles, dim3(pt::P), dim3(512), 0, st, x, w);
   return hipGetLastError();
 }
 
