@@ -447,41 +447,43 @@ hipError_t launch_product(int kind, ProductProblem p, hipStream_t st) {
 }
 
 // How an FP8 product is formed: of few rows; on FP8 tiles where bf16 leaves; from widened rows where codes or float32 leave; and
-// where that makes few tiles for a long k, float32 ones cut along it.
+// where that makes few tiles, float32 ones cut along k.  Those run at 0.1 PFLOP/s whatever their number, a widened tile's
+// window of 64 takes 0.7 us alone, as 17 tiles' take there.  Measured, widened and cut (us, float32 out): 16 tiles
+// 400 x 1024 -> 1024 24.5 and 23.4, 32 tiles 1000 x 256 -> 1024 16.7 and 19.6, 2 tiles 209 x 6272 -> 144 83 and 25.  Codes take a
+// launch more there: 8 tiles and a k of 1024 make up for it.
 enum Fp8Way { FP8_FEW, FP8_TILES, FP8_WIDE, FP8_SPLIT };
-static Fp8Way fp8_way(bool bf16, bool coded, long long rows, int N, int parts) {
+constexpr int kSplitCodedTiles = 8;
+static Fp8Way fp8_way(bool bf16, bool coded, long long rows, int K, int N, int parts) {
   if (rows <= kProductFewRows) return FP8_FEW;
-  if (coded) return FP8_WIDE;
-  if (bf16) return FP8_TILES;
+  if (!coded && bf16) return FP8_TILES;
   const int cols = parts == 2 ? 128 : 256;
-  return (rows + 127) / 128 * ((N + cols - 1) / cols) >= 64 ? FP8_WIDE : FP8_SPLIT;
+  const long long tiles = (rows + 127) / 128 * ((N + cols - 1) / cols);
+  return (coded ? tiles <= kSplitCodedTiles && K >= 1024 : tiles <= 16) ? FP8_SPLIT : FP8_WIDE;
 }
+// Partial sums, and float32 rows that codes are formed from (of FP8_SPLIT, behind them)
 size_t product_fp8_part_bytes(long long rows, int K, int N, int parts) {
   if (rows <= kProductFewRows) return size_t(rows) * N * sizeof(float);
-  return std::max(product_tiles_part_bytes(), product_part_bytes(false, PRODUCT_OUT, rows, K, N, parts));
+  const size_t coded = std::min<size_t>(size_t(rows) * N, kSplitCodedTiles * 128 * 128) * sizeof(float);
+  return std::max(product_tiles_part_bytes(), product_part_bytes(false, PRODUCT_OUT, rows, K, N, parts) + coded);
 }
 Fp8Rows product_fp8_rows(const ProductProblem &p) {
-  const Fp8Way way = fp8_way(p.bf16, p.out_scale != nullptr, p.rows, p.N, p.parts);
+  const Fp8Way way = fp8_way(p.bf16, p.out_scale != nullptr, p.rows, p.K, p.N, p.parts);
   if (way == FP8_WIDE) return FP8_ROWS_WIDE;
   return way == FP8_FEW && p.bf16 && p.rows <= 16 ? FP8_ROWS_ANY : FP8_ROWS_CODES;
 }
 hipError_t launch_product_fp8(ProductProblem p, hipStream_t st) {
-  switch (fp8_way(p.bf16, p.out_scale != nullptr, p.rows, p.N, p.parts)) {
-    case FP8_FEW: {
-      p.out_f32 = !p.bf16;
-      if (!p.out_scale) return launch_product_few(p, st);
-      // codes: a scale's 128 columns are eight workgroups', so they are formed from float32 rows in a launch of their own
-      void *codes = p.out;
-      p.out = p.part;
-      p.out_f32 = 1;
-      const hipError_t e = launch_product_few(p, st);
-      if (e != hipSuccess) return e;
-      return launch_quantize_blocks(false, p.out, p.rows, p.N, 1, p.cu + p.B, reinterpret_cast<uint8_t *>(codes), p.out_scale, st);
-    }
-    case FP8_TILES: return launch_product_fp8_tiles(p, st);
-    case FP8_WIDE: return launch_product_fp8_wide(p, st);
-    default: return p.parts == 2 ? run<TYPE_FP8, PRODUCT_OUT, true>(p, st) : run<TYPE_FP8, PRODUCT_OUT, false>(p, st);
-  }
+  const Fp8Way way = fp8_way(p.bf16, p.out_scale != nullptr, p.rows, p.K, p.N, p.parts);
+  if (way == FP8_TILES) return launch_product_fp8_tiles(p, st);
+  if (way == FP8_WIDE) return launch_product_fp8_wide(p, st);
+  // codes: a scale's 128 columns are several workgroups', so they are formed from float32 rows in a launch of their own
+  void *codes = p.out;
+  p.out_f32 = !p.bf16 || p.out_scale;
+  if (p.out_scale) p.out = p.part + (way == FP8_FEW ? 0 : product_part_bytes(false, PRODUCT_OUT, p.rows, p.K, p.N, p.parts) / sizeof(float));
+  const hipError_t e = way == FP8_FEW ? launch_product_few(p, st)
+                       : p.parts == 2 ? run<TYPE_FP8, PRODUCT_OUT, true>(p, st)
+                                      : run<TYPE_FP8, PRODUCT_OUT, false>(p, st);
+  if (e != hipSuccess || !p.out_scale) return e;
+  return launch_quantize_blocks(false, p.out, p.rows, p.N, 1, p.cu + p.B, reinterpret_cast<uint8_t *>(codes), p.out_scale, st);
 }
 
 // ------------------------------------------------------------------------ through the gate, and sums over rows

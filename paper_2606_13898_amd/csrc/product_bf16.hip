@@ -484,7 +484,7 @@ HILO_DEV void fix(const ProductProblem &p, const Plan &q) {
 }
 
 // 256 x 256, 256 x 128, 128 x 128
-constexpr Cost kCost[3] = {{146, 700, 2500}, {80, 500, 2000}, {46, 400, 1500}};
+constexpr Cost kCost[3] = {{146, 700, 500, 50, 7}, {80, 500, 450, 35, 3}, {46, 400, 400, 22, 1}};
 template <int I, int KIND, bool GATED>
 using Tile = Geo<I < 2 ? 256 : 128, I < 1 ? 256 : 128, KIND, GATED>;
 
@@ -495,8 +495,8 @@ HILO_BOTH int choose(const ProductProblem &p, int nk, F &&row_tiles, Plan &q) {
   const Plan a = make_plan<Tile<1, KIND, GATED>>(p, q.R, nk, kCost[1]);
   const Plan b = make_plan<Tile<2, KIND, GATED>>(p, row_tiles(128), nk, kCost[2]);
   int best = 0;
-  long long cost = plan_cost(q.T, nk, kCost[0], p.splits != 0);
-  const long long ca = plan_cost(a.T, nk, kCost[1], p.splits != 0), cb = plan_cost(b.T, nk, kCost[2], p.splits != 0);
+  long long cost = plan_cost(q.T, nk, kCost[0], p.splits);
+  const long long ca = plan_cost(a.T, nk, kCost[1], p.splits), cb = plan_cost(b.T, nk, kCost[2], p.splits);
   if (ca < cost) {
     best = 1;
     cost = ca;
@@ -565,17 +565,17 @@ size_t product_tiles_part_bytes() { return size_t(pt::P) * 256 * 256 * sizeof(fl
 template <int KIND, bool GATED>
 static long long plan_rows(ProductProblem p, pt::Plan &q) {
   const int nk = KIND == PRODUCT_OUT ? (p.K + 63) / 64 : KIND == PRODUCT_DX ? p.parts * ((p.N + 63) / 64) : (p.rows + 63) / 64;
-  p.splits = 1;
+  p.splits = pt::kSearch;
   const int best = pt::choose<KIND, GATED>(
       p, nk, [&](int bm) { return KIND == PRODUCT_DW ? p.outs * ((p.N + bm - 1) / bm) : (p.rows + bm - 1) / bm; }, q);
-  return pt::plan_cost(q.T, nk, pt::kCost[best], true);
+  return pt::plan_cost(q.T, nk, pt::kCost[best], pt::kSearch);
 }
 
 template <int KIND, bool GATED>
 static hipError_t run_tiles(ProductProblem p, hipStream_t st) {
   pt::Plan q;
   plan_rows<KIND, GATED>(p, q);
-  p.splits = q.s > 1;
+  p.splits = q.s > 1 ? q.s : 0;
   hipLaunchKernelGGL((pt::k_product_tiles<KIND, GATED>), dim3(pt::P), dim3(512), 0, st, p);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || !p.splits) return e;

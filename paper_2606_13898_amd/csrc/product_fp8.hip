@@ -126,9 +126,19 @@ HILO_DEV void finish8(const ProductProblem &p, const Place &z, const Bias8<G> &b
   }
 }
 
+// A block of a partial tile, by quads: 64 lanes' 16 bytes side by side.
 template <typename G>
-HILO_DEV size_t part_at8(int slot, int wid, int i, int j, int lane) {
-  return size_t(slot) * G::BM * G::BN + ((size_t(wid) * G::MB * G::NB + i * G::NB + j) * 64 + lane) * 16;
+HILO_DEV float *part_at8(float *part, int slot, int wid, int i, int j, int lane) {
+  return part + size_t(slot) * G::BM * G::BN + (size_t(wid) * G::MB * G::NB + i * G::NB + j) * 1024 + lane * 4;
+}
+HILO_DEV void store_part8(float *to, const f32x16 &v) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    *reinterpret_cast<f32x4 *>(to + 256 * e) = f32x4{v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]};
+}
+HILO_DEV void add_part8(f32x16 &v, const f32x4 (&w)[4]) {
+#pragma unroll
+  for (int e = 0; e < 16; ++e) v[e] += w[e >> 2][e & 3];
 }
 
 // A workgroup's loads, product_bf16.hip's with k last, and a window's scales: windows of its items one after another.
@@ -362,7 +372,7 @@ HILO_DEV void run8(const ProductProblem &p, const Plan &q, int pid, uint8_t *lds
 #pragma unroll
       for (int i = 0; i < MB; ++i)
 #pragma unroll
-        for (int j = 0; j < NB; ++j) *reinterpret_cast<f32x16 *>(p.part + part_at8<G>(it.slot, wid, i, j, lane)) = acc[i][j];
+        for (int j = 0; j < NB; ++j) store_part8(part_at8<G>(p.part, it.slot, wid, i, j, lane), acc[i][j]);
       continue;
     }
     Bias8<G> bias;
@@ -674,16 +684,29 @@ HILO_DEV void fix8(const ProductProblem &p, const Plan &q) {
     f32x16 acc[G::NB];
 #pragma unroll
     for (int j = 0; j < G::NB; ++j) acc[j] = f32x16(0.f);
-#pragma unroll 2
-    for (int pc = 0; pc < q.s; ++pc)
+#pragma unroll 1
+    for (int pc = 0; pc < q.s; pc += 2) {  // two pieces' loads at once
+      f32x4 w[2][G::NB][4];
 #pragma unroll
-      for (int j = 0; j < G::NB; ++j)
-        acc[j] += *reinterpret_cast<const f32x16 *>(p.part + part_at8<G>(pc * q.tail + v, wid, i, j, lane));
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int j = 0; j < G::NB; ++j) {
+          const float *from = part_at8<G>(p.part, min(pc + k, q.s - 1) * q.tail + v, wid, i, j, lane);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) w[k][j][e] = *reinterpret_cast<const f32x4 *>(from + 256 * e);
+        }
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int j = 0; j < G::NB; ++j) {
+        add_part8(acc[j], w[0][j]);
+        if (pc + 1 < q.s) add_part8(acc[j], w[1][j]);
+      }
+    }
     finish8<G>(p, z, bias, wid, i, lane, acc);
   }
 }
 
-constexpr Cost kCost8[2] = {{150, 600, 2500}, {80, 400, 1800}};
+constexpr Cost kCost8[2] = {{150, 600, 500, 80, 7}, {80, 400, 500, 40, 2}};
 
 // 256 x 256 tiles or 128 x 256.
 template <bool GATED, typename F>
@@ -691,7 +714,7 @@ HILO_BOTH bool choose8(const ProductProblem &p, F &&row_tiles, Plan &q) {
   const int nk = (p.K + 127) / 128;
   const Plan a = make_plan<Geo8<256, 256, GATED>>(p, row_tiles(256), nk, kCost8[0]);
   const Plan b = make_plan<Geo8<128, 256, GATED>>(p, row_tiles(128), nk, kCost8[1]);
-  const bool large = plan_cost(a.T, nk, kCost8[0], p.splits != 0) <= plan_cost(b.T, nk, kCost8[1], p.splits != 0);
+  const bool large = plan_cost(a.T, nk, kCost8[0], p.splits) <= plan_cost(b.T, nk, kCost8[1], p.splits);
   q = large ? a : b;
   return large;
 }
@@ -731,9 +754,9 @@ __global__ __launch_bounds__(512, 2) void k_product_fp8_wide(ProductProblem p) {
 template <bool GATED>
 static hipError_t run_tiles8(ProductProblem p, hipStream_t st) {
   pt::Plan q;
-  p.splits = 1;
+  p.splits = pt::kSearch;
   pt::choose8<GATED>(p, [&](int bm) { return (p.rows + bm - 1) / bm; }, q);
-  p.splits = q.s > 1;
+  p.splits = q.s > 1 ? q.s : 0;
   hipLaunchKernelGGL((pt::k_product_fp8<GATED>), dim3(pt::P), dim3(512), 0, st, p);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || !p.splits) return e;

@@ -40,19 +40,28 @@ HILO_DEV Item item_at(const Plan &q, int u) {
   return Item{q.full + v - pc * q.tail, pc, q.s, v, true};
 }
 
-// In units of 10 ns: a window of 64 and a tile's rest, and what pieces of the last turn cost beside their windows.
+// In units of 10 ns: a window and a tile's rest; beside their windows pieces of the last turn cost a launch, and each level
+// of pieces and each piece its share.
 struct Cost {
-  int window, tile, fix;
+  int window, tile, fix, level, piece;
+  __host__ __device__ __forceinline__ int pieces(int s, int tail) const { return fix + s * (level + tail * piece); }
+  // of nk windows; beyond 2^20 of them, 2^20's
+  __host__ __device__ __forceinline__ int windows(int nk) const { return (nk < 1 << 20 ? nk : 1 << 20) * window; }
 };
 #define HILO_BOTH __host__ __device__ __forceinline__
-HILO_BOTH int plan_tail(int tail, int nk, Cost c, bool cuts) {
-  if (tail == 0 || !cuts) return 1;
-  const int s = P / tail < nk / 4 ? P / tail : nk / 4;
-  return s > 1 && nk * c.window > nk * c.window / s + c.fix ? s : 1;
+// Pieces of a tile of the last turn: none (splits 0), at most splits, or on the host (kSearch) as many as are quickest.
+constexpr int kSearch = -1;
+HILO_BOTH int plan_tail(int tail, int nk, Cost c, int splits) {
+  if (tail == 0 || splits == 0) return 1;
+  const int most = P / tail < nk / 4 ? P / tail : nk / 4, all = c.windows(nk);
+  int s = most < splits ? most : splits;
+  if (splits == kSearch)
+    for (s = 1; s < most && all > s * (s + 1) * (c.level + tail * c.piece);) ++s;  // one more saves more than it costs
+  return s > 1 && all - int(unsigned(all) / unsigned(s)) > c.pieces(s, tail) ? s : 1;
 }
-HILO_BOTH long long plan_cost(int T, int nk, Cost c, bool cuts) {
-  const int tail = T % P, s = plan_tail(tail, nk, c, cuts);
-  return (long long)(T / P) * (nk * c.window + c.tile) + (tail ? nk * c.window / s + c.tile + (s > 1 ? c.fix : 0) : 0);
+HILO_BOTH long long plan_cost(int T, int nk, Cost c, int splits) {
+  const int tail = T % P, s = plan_tail(tail, nk, c, splits), all = c.windows(nk);
+  return (long long)(T / P) * (all + c.tile) + (tail ? int(unsigned(all) / unsigned(s)) + c.tile + (s > 1 ? c.pieces(s, tail) : 0) : 0);
 }
 template <typename G>
 HILO_BOTH Plan make_plan(const ProductProblem &p, int R, int nk, Cost c) {
@@ -62,7 +71,7 @@ HILO_BOTH Plan make_plan(const ProductProblem &p, int R, int nk, Cost c) {
   q.T = q.R * q.TN;
   q.tail = q.T % P;
   q.full = q.T - q.tail;
-  q.s = plan_tail(q.tail, nk, c, p.splits != 0);
+  q.s = plan_tail(q.tail, nk, c, p.splits);
   return q;
 }
 

@@ -227,6 +227,7 @@ FP8_SHAPES = [
     ([4, 1], 0, 1168, 640, 1),
     ([600], 0, 1040, 1296, 1),
     ([513, 2, 700], 40, 336, 784, 2),
+    ([150, 3], 9, 2064, 272, 2),
 ]
 
 
