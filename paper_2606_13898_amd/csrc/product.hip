@@ -450,20 +450,20 @@ hipError_t launch_product(int kind, ProductProblem p, hipStream_t st) {
 // where that makes few tiles, float32 ones cut along k.  Those run at 0.1 PFLOP/s whatever their number, a widened tile's
 // window of 64 takes 0.7 us alone, as 17 tiles' take there.  Measured, widened and cut (us, float32 out): 16 tiles
 // 400 x 1024 -> 1024 24.5 and 23.4, 32 tiles 1000 x 256 -> 1024 16.7 and 19.6, 2 tiles 209 x 6272 -> 144 83 and 25.  Codes take a
-// launch more there: 8 tiles and a k of 1024 make up for it.
+// launch more there, 5 us: what 120 such windows of tiles fewer than 17 save (a feed of 209 rows, 6272 wide: 95 and 46).
 enum Fp8Way { FP8_FEW, FP8_TILES, FP8_WIDE, FP8_SPLIT };
-constexpr int kSplitCodedTiles = 8;
+constexpr int kSplitTilesMost = 17;
 static Fp8Way fp8_way(bool bf16, bool coded, long long rows, int K, int N, int parts) {
   if (rows <= kProductFewRows) return FP8_FEW;
   if (!coded && bf16) return FP8_TILES;
   const int cols = parts == 2 ? 128 : 256;
   const long long tiles = (rows + 127) / 128 * ((N + cols - 1) / cols);
-  return (coded ? tiles <= kSplitCodedTiles && K >= 1024 : tiles <= 16) ? FP8_SPLIT : FP8_WIDE;
+  return (kSplitTilesMost - tiles) * K > (coded ? 120 * 64 : 0) ? FP8_SPLIT : FP8_WIDE;
 }
 // Partial sums, and float32 rows that codes are formed from (of FP8_SPLIT, behind them)
 size_t product_fp8_part_bytes(long long rows, int K, int N, int parts) {
   if (rows <= kProductFewRows) return size_t(rows) * N * sizeof(float);
-  const size_t coded = std::min<size_t>(size_t(rows) * N, kSplitCodedTiles * 128 * 128) * sizeof(float);
+  const size_t coded = std::min<size_t>(size_t(rows) * N, kSplitTilesMost * 128 * 128) * sizeof(float);
   return std::max(product_tiles_part_bytes(), product_part_bytes(false, PRODUCT_OUT, rows, K, N, parts) + coded);
 }
 Fp8Rows product_fp8_rows(const ProductProblem &p) {
@@ -492,7 +492,13 @@ hipError_t launch_product_fp8(ProductProblem p, hipStream_t st) {
 // 512 columns: a wave every fourth row, a lane 8 columns, four rows on their way.  What a column's rows sum to goes to
 // part[row block][parts][N], and k_gate_back_sum adds those of a stream's blocks in their order.
 constexpr int kBackCols = 512;
-static int back_rows(long long rows) { return rows >= 8192 ? 256 : rows >= 2048 ? 64 : rows >= 1024 ? 16 : 4; }
+// Rows of a block: the fewest of 4, 16, 64, 256 that leave at most 2048 workgroups (256 CUs have 8 each), or 256.
+constexpr long long kBackItems = 2048;
+static int back_rows(long long rows, int N) {
+  int b = 4;
+  while (b < 256 && (rows + b - 1) / b * ((N + kBackCols - 1) / kBackCols) > kBackItems) b *= 4;
+  return b;
+}
 
 template <bool BF16, bool GATED>
 __global__ __launch_bounds__(256) void k_gate_back(GateBackProblem p) {
@@ -627,9 +633,9 @@ __global__ __launch_bounds__(256) void k_join_back(ProductProblem x, ProductProb
   sum_columns<false, 4>(g, block % cols, block / cols);
 }
 
-// Bounds any call's blocks (back_rows: 256 of 4 rows, 128 of 16 or of 64, or of 256 rows), and grows with the rows.
+// Bounds the blocks, and grows with the rows.
 size_t gate_back_bytes(long long rows, int N, int parts, int B) {
-  const long long blocks = std::max(std::min((rows + 3) / 4, 256ll), (rows + 255) / 256);
+  const long long most = kBackItems / ((N + kBackCols - 1) / kBackCols), blocks = std::max(std::min((rows + 3) / 4, most), (rows + 255) / 256);
   return (size_t(blocks) + 2 * size_t(B)) * parts * N * sizeof(float);
 }
 
@@ -647,13 +653,13 @@ static hipError_t run_gate_back(const GateBackProblem &p, hipStream_t st) {
 }
 
 hipError_t launch_gate_back(bool bf16, GateBackProblem p, hipStream_t st) {
-  p.block_rows = back_rows(p.rows);
+  p.block_rows = back_rows(p.rows, p.N);
   if (p.parts == 2) return bf16 ? run_gate_back<true, true>(p, st) : run_gate_back<false, true>(p, st);
   return bf16 ? run_gate_back<true, false>(p, st) : run_gate_back<false, false>(p, st);
 }
 
 hipError_t launch_product_back(ProductProblem x, ProductProblem w, GateBackProblem g, hipStream_t st) {
-  g.block_rows = back_rows(g.rows);
+  g.block_rows = back_rows(g.rows, g.N);
   const int bx = product_blocks(PRODUCT_DX, x), bw = product_blocks(PRODUCT_DW, w);
   hipLaunchKernelGGL(k_product_back, dim3(bx + bw), dim3(512), 0, st, x, w, bx);
   const hipError_t e = hipGetLastError();

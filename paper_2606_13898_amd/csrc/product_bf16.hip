@@ -484,19 +484,21 @@ HILO_DEV void fix(const ProductProblem &p, const Plan &q) {
 }
 
 // 256 x 256, 256 x 128, 128 x 128
-constexpr Cost kCost[3] = {{146, 700, 500, 50, 7}, {80, 500, 450, 35, 3}, {46, 400, 400, 22, 1}};
+constexpr Cost kCost[3][3] = {{{146, 700, 700, 50, 7}, {84, 500, 650, 35, 3}, {50, 400, 600, 22, 1}},   // by kind of product
+                              {{160, 700, 700, 50, 7}, {100, 500, 650, 35, 3}, {65, 400, 600, 22, 1}},
+                              {{155, 700, 700, 50, 7}, {90, 500, 650, 35, 3}, {55, 400, 600, 22, 1}}};
 template <int I, int KIND, bool GATED>
 using Tile = Geo<I < 2 ? 256 : 128, I < 1 ? 256 : 128, KIND, GATED>;
 
 // Row tiles of outputs (DW) or as the caller counts them, for each tile the plan and its cost: which is quickest.
 template <int KIND, bool GATED, typename F>
 HILO_BOTH int choose(const ProductProblem &p, int nk, F &&row_tiles, Plan &q) {
-  q = make_plan<Tile<0, KIND, GATED>>(p, row_tiles(256), nk, kCost[0]);
-  const Plan a = make_plan<Tile<1, KIND, GATED>>(p, q.R, nk, kCost[1]);
-  const Plan b = make_plan<Tile<2, KIND, GATED>>(p, row_tiles(128), nk, kCost[2]);
+  q = make_plan<Tile<0, KIND, GATED>>(p, row_tiles(256), nk, kCost[KIND][0]);
+  const Plan a = make_plan<Tile<1, KIND, GATED>>(p, q.R, nk, kCost[KIND][1]);
+  const Plan b = make_plan<Tile<2, KIND, GATED>>(p, row_tiles(128), nk, kCost[KIND][2]);
   int best = 0;
-  long long cost = plan_cost(q.T, nk, kCost[0], p.splits);
-  const long long ca = plan_cost(a.T, nk, kCost[1], p.splits), cb = plan_cost(b.T, nk, kCost[2], p.splits);
+  long long cost = plan_cost(q.T, nk, kCost[KIND][0], p.splits);
+  const long long ca = plan_cost(a.T, nk, kCost[KIND][1], p.splits), cb = plan_cost(b.T, nk, kCost[KIND][2], p.splits);
   if (ca < cost) {
     best = 1;
     cost = ca;
@@ -540,10 +542,10 @@ __global__ __launch_bounds__(512, 2) void k_product_back_tiles(ProductProblem x,
   using GW = Tile<0, PRODUCT_DW, false>;
   __shared__ __attribute__((aligned(1024))) uint8_t lds[std::max(GX::LDS, GW::LDS)];
   const int pid = xcd_remap(blockIdx.x, P);
-  const Plan qx = make_plan<GX>(x, count_row_tiles(x, 256), 1, kCost[0]);
+  const Plan qx = make_plan<GX>(x, count_row_tiles(x, 256), 1, kCost[PRODUCT_DX][0]);
   run<GX>(x, qx, pid, lds);
   asm volatile("s_barrier" ::: "memory");
-  const Plan qw = make_plan<GW>(w, w.outs * ((w.N + 255) / 256), 1, kCost[0]);
+  const Plan qw = make_plan<GW>(w, w.outs * ((w.N + 255) / 256), 1, kCost[PRODUCT_DW][0]);
   run<GW>(w, qw, (pid + P - qx.tail) % P, lds);
 }
 
@@ -568,7 +570,7 @@ static long long plan_rows(ProductProblem p, pt::Plan &q) {
   p.splits = pt::kSearch;
   const int best = pt::choose<KIND, GATED>(
       p, nk, [&](int bm) { return KIND == PRODUCT_DW ? p.outs * ((p.N + bm - 1) / bm) : (p.rows + bm - 1) / bm; }, q);
-  return pt::plan_cost(q.T, nk, pt::kCost[best], pt::kSearch);
+  return pt::plan_cost(q.T, nk, pt::kCost[KIND][best], pt::kSearch);
 }
 
 template <int KIND, bool GATED>
@@ -587,17 +589,17 @@ static hipError_t run_tiles(ProductProblem p, hipStream_t st) {
 static long long shares(const ProductProblem &x, const ProductProblem &w, bool both) {
   long long each[pt::P] = {};
   int at = 0;
-  auto add = [&](int tiles, int nk) {
-    const long long cost = nk * pt::kCost[0].window + pt::kCost[0].tile;
+  auto add = [&](int kind, int tiles, int nk) {
+    const long long cost = pt::kCost[kind][0].windows(nk) + pt::kCost[kind][0].tile;
     for (int k = 0; k < pt::P; ++k) each[(at + k) % pt::P] += (tiles / pt::P + (k < tiles % pt::P)) * cost;
     at += tiles % pt::P;
   };
   const int cols = (x.K + 255) / 256;
-  if (both) add((x.rows + 255) / 256 * cols, x.parts * ((x.N + 63) / 64));
+  if (both) add(PRODUCT_DX, (x.rows + 255) / 256 * cols, x.parts * ((x.N + 63) / 64));
   for (int o = 0; o < w.outs; ++o) {
     const long long text = std::min<long long>(x.rows, (long long)x.B * x.L);
     const long long rows = w.merged ? x.rows : w.out_stream[o] ? text : x.rows - text;
-    add((w.N + 255) / 256 * cols, int((rows + 63) / 64));
+    add(PRODUCT_DW, (w.N + 255) / 256 * cols, int((rows + 63) / 64));
   }
   return *std::max_element(each, each + pt::P);
 }

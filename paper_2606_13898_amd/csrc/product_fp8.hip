@@ -706,7 +706,7 @@ HILO_DEV void fix8(const ProductProblem &p, const Plan &q) {
   }
 }
 
-constexpr Cost kCost8[2] = {{150, 600, 500, 80, 7}, {80, 400, 500, 40, 2}};
+constexpr Cost kCost8[2] = {{150, 600, 600, 80, 7}, {80, 400, 600, 40, 2}};
 
 // 256 x 256 tiles or 128 x 256.
 template <bool GATED, typename F>
