@@ -220,8 +220,8 @@ struct ProductProblem {
   int outs;              // weight gradients to form, in the order of:
   int out_stream[4], out_part[4];
   void *dw[4];           // [N][K]
-  float *part;           // partial sums, `splits` times what the product leaves
-  int splits;            // how many; on large tiles whether the last turn's tiles may be cut
+  float *part;           // partial sums: `splits` times what the product leaves, or on large tiles the pieces of the last turn's
+  int splits;            // how many; on large tiles into how many pieces at most a tile is cut (0: none)
   // FP8: x holds codes, w codes
   const uint8_t *x_scale;        // [rows][scale_stride(K)] E8M0 bytes
   const uint8_t *w_scale[2][2];  // [ceil(N / 128)][scale_stride(K)]

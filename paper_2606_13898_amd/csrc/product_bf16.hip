@@ -11,6 +11,13 @@
 //            rows of 16 columns and each gets a column's four values; 32-byte chunk c of row k at c ^ f(k), f(k) = k % 4 + 4
 //            (k / 8 % 2), so that the rows that 32 lanes read at once lie in eight groups of banks
 // What lies behind the last row, column or k is never read: the loads' buffer ends there, and they leave zeros.
+//
+// Bound by the matrix cores at the power limit, and by what feeds them: a window of 256 x 256 takes 1.46 to 1.67 us on all CUs
+// (1.25 to 1.35 PFLOP/s; the library's large product reaches 1.30), 1.07 on few.  The rest: a tile's epilogue, 7 us, which
+// does not run beside the next tile's products (128 of a lane's 256 registers are accumulators, so there are no second ones),
+// and turns that are not full.  2766 x 3072 -> 8192 with a gate 270 us, 1.03 PFLOP/s; 4708 x 4096 -> 1536 63; 22560 x
+// 3072 -> 8192, gradients of both parts, 4.0 ms, 1.14.  The next tile's first windows are loaded before a tile's stores and
+// not waited for behind them.
 #include <algorithm>
 
 #include "product_tiles.h"
@@ -483,7 +490,8 @@ HILO_DEV void fix(const ProductProblem &p, const Plan &q) {
   }
 }
 
-// 256 x 256, 256 x 128, 128 x 128
+// 256 x 256, 256 x 128, 128 x 128: the larger one loads less for a product, the smaller one leaves fewer CUs idle.  Each is best
+// somewhere (us): 18900 x 296 -> 3392 68, 79, 93; 4700 x 4096 -> 1536 78, 62, 73; 1000 x 4096 -> 4096 56, 47, 40.
 constexpr Cost kCost[3][3] = {{{146, 700, 700, 50, 7}, {84, 500, 650, 35, 3}, {50, 400, 600, 22, 1}},   // by kind of product
                               {{160, 700, 700, 50, 7}, {100, 500, 650, 35, 3}, {65, 400, 600, 22, 1}},
                               {{155, 700, 700, 50, 7}, {90, 500, 650, 35, 3}, {55, 400, 600, 22, 1}}};
@@ -536,7 +544,8 @@ __global__ __launch_bounds__(512, 2) void k_product_tiles(ProductProblem p) {
 }
 
 // dx and the weights' gradients in a launch, whole 256 x 256 tiles of the one and then of the others: a workgroup's first of
-// the latter follows the last of the former.
+// the latter follows the last of the former, and the two have one last turn between them.  2766 x 8192 -> 3072: 264 us, in
+// launches of their own 303.
 __global__ __launch_bounds__(512, 2) void k_product_back_tiles(ProductProblem x, ProductProblem w) {
   using GX = Tile<0, PRODUCT_DX, false>;
   using GW = Tile<0, PRODUCT_DW, false>;
