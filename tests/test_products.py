@@ -4,6 +4,7 @@ import ctypes
 import math
 import os
 
+import product_schedule
 import pytest
 import torch
 
@@ -305,3 +306,16 @@ def test_oracle_activations(act):
     want = torch.nn.functional.silu(g) if act == "silu" else torch.nn.functional.gelu(g, approximate="tanh")
     torch.testing.assert_close(P.act_slope(act, g)[0], want, rtol=1e-12, atol=1e-14)
     assert P.act_slope(act, g)[1].abs().max() <= 1.13
+
+
+# ------------------------------------------------------------------------------------------ plans
+
+@pytest.mark.parametrize("kind, images, text, k, n, streams, parts, plan", product_schedule.SHAPES, ids=str)
+def test_plan_of_shape(kind, images, text, k, n, streams, parts, plan):
+    assert product_schedule.describe(kind, images, text, k, n, streams, parts, 3) == plan
+
+
+def test_shapes_reach_every_plan():
+    got = {(kind, parts, plan[0], plan[2] > 1) for kind, *_, parts, plan in product_schedule.SHAPES}
+    assert got == {(kind, parts, tile, cut) for kind in range(4) for parts in (1, 2) for tile in product_schedule.TILES[kind] for cut in (False, True)}
+    assert all(product_schedule.together(*shape, 3) for shape in product_schedule.TOGETHER)

@@ -5,6 +5,7 @@ where additions cut instead of rounding (the bf16 and FP8 matrix instructions); 
 oracle.hilo_products.cut's, for outputs of bf16 and codes (float32 outputs are formed without it).  What the activation
 adds, and how errors of g and u reach the output, is oracle.hilo_products'; the last rounding is half a step: 2^-8 (bf16)
 or 2^-24 of the value, of codes 2^-4 and half the least step, 2^-10 of the scale."""
+import product_schedule
 import pytest
 import torch
 
@@ -48,7 +49,7 @@ def rows_like(t, behind):
 
 
 def near(got, want, bound, what):
-    got = got.cpu().to(F64)
+    got = got.to(want.device).to(F64)
     off = (got - want).abs()
     bad = ~(off <= bound + 1e-30)
     assert not bad.any(), (what, int(bad.sum()), float((off / (bound + 1e-30)).nan_to_num(1e9).max()),
@@ -294,3 +295,84 @@ def test_fp8(shape, kind, coded):
     assert ((kk >= P.block_exponent(lo)) & (kk <= P.block_exponent(hi))).all()
     scale = torch.exp2(kk).repeat_interleave(128, 1)[:, :n]
     near(P.decode(h[:cu[-1]].cpu(), hs[:cu[-1]].cpu(), 1), want, off + 2.0 ** -4 * (want.abs() + off) + 2.0 ** -10 * scale, "codes")
+
+
+# ------------------------------------------------------------------------- each plan of the large tiles, against float64 here
+
+def on_device(shape, seed):
+    """Rows, what they are to be multiplied with and their boundaries, on the device; NaN behind the last row."""
+    images, text, k, n, streams, parts = shape
+    cu, g = pack(images, text), torch.Generator(device="cuda").manual_seed(seed)
+    randn = lambda *s: torch.randn(*s, device="cuda", generator=g)  # noqa: E731
+    ws = [{f"{v}{part}": randn(*s).mul_(c).to(torch.bfloat16) for part in ("", "_gate")[:parts] for v, s, c in (("w", (n, k), k ** -0.5), ("b", (n,), 0.3))}
+          for _ in range(streams)]
+    return cu, torch.tensor(cu, dtype=torch.int32, device="cuda"), randn, ws
+
+
+def padded(t):
+    return torch.cat([t, torch.full((BEHIND, *t.shape[1:]), float("nan"), dtype=t.dtype, device="cuda")])
+
+
+def scratch(nbytes):
+    return torch.empty(max(nbytes, 1), dtype=torch.uint8, device="cuda").fill_(0xff)
+
+
+def backward_bits(shape, seed, form_dx, form_dw):
+    """A bf16 backward pass of a shape against float64; biases' sums as well."""
+    images, text, k, n, streams, parts = shape
+    cu, cud, randn, ws = on_device(shape, seed)
+    act, dt = "silu" if parts == 2 else None, torch.bfloat16
+    x, dout = randn(cu[-1], k).to(dt), randn(cu[-1], n).to(dt)
+    pre = randn(cu[-1], 2, n).to(dt) if act else None
+    dx = torch.full((cu[-1] + BEHIND, k), 7.0, dtype=dt, device="cuda") if form_dx else None
+    got = [{name: torch.full_like(v, 7.0) for name, v in d.items()} for d in ws] if form_dw else None
+    need = hilo.hilo_linear_backward_workspace_bytes(dt, cu[-1] + BEHIND, k, n, len(images), gated=parts == 2)
+    hilo.hilo_linear_backward(hilo.linear_weights(ws), padded(x), None if pre is None else padded(pre), padded(dout), dx,
+                              hilo.linear_grads(got) if got else None, cud, text, act=ACTS[act], workspace=scratch(need))
+    with torch.device("cuda"):
+        (wx, bx), want = P.backward(x.to(F64), ws, None if pre is None else pre.to(F64), dout.to(F64), act, cu, text, HALF[dt], streams == 1)
+    if form_dx:
+        assert (dx[cu[-1]:] == 7.0).all()
+        near(dx[:cu[-1]], wx, bx, "dx")
+    for kk, d in enumerate(got or []):
+        for name, t in d.items():
+            near(t, *want[kk][name], f"{name} of {kk}")
+
+
+@pytest.mark.parametrize("kind, images, text, k, n, streams, parts, plan", product_schedule.SHAPES, ids=str)
+def test_plan(kind, images, text, k, n, streams, parts, plan):
+    shape, dt = (images, text, k, n, streams, parts), torch.bfloat16
+    if kind in (product_schedule.DX, product_schedule.DW):
+        return backward_bits(shape, k + n, kind == product_schedule.DX, kind == product_schedule.DW)
+    act = "silu" if parts == 2 else None
+    cu, cud, randn, ws = on_device(shape, k + n)
+    x, out = randn(cu[-1], k).to(dt), torch.full((cu[-1] + BEHIND, n), 7.0, dtype=dt, device="cuda")
+    if kind == product_schedule.OUT:
+        need = hilo.hilo_linear_workspace_bytes(dt, cu[-1] + BEHIND, k, n, len(images), gated=parts == 2)
+        hilo.hilo_linear(hilo.linear_weights(ws), padded(x), out, cud, text, act=ACTS[act], workspace=scratch(need))
+        xv, values = x.to(F64), ws
+    else:
+        codes, scales = torch.empty_like(x, dtype=torch.uint8), torch.empty(cu[-1], hilo.scale_stride(k), dtype=torch.uint8, device="cuda")
+        hilo.hilo_quantize_blocks(x, codes, scales)
+        plans = [hilo.quantize_block_weights(d["w"], d["b"], d.get("w_gate"), d.get("b_gate")) for d in ws]
+        need = hilo.hilo_linear_fp8_workspace_bytes(cu[-1] + BEHIND, k, n, gated=parts == 2)
+        hilo.hilo_linear_fp8(hilo.linear_weights_fp8(plans), padded(x), out, cud, text, act=ACTS[act], workspace=scratch(need))
+        xv = P.decode(codes, scales, 1)
+        kx = scales[:, :-(-k // 128)].to(F64) - 127
+        values = [{**d, **{"w" + p: P.decode(q["w" + p], q["s" + p], 128) for p in ("", "_gate")[:parts]}} for d, q in zip(ws, plans)]
+        kws = [{"w" + p: q["s" + p][:, :-(-k // 128)].to(F64) - 127 for p in ("", "_gate")[:parts]} for q in plans]
+    assert (out[cu[-1]:] == 7.0).all()
+    v, e = {}, {}
+    with torch.device("cuda"):
+        for p in ("", "_gate")[:parts]:
+            v[p], s = P.affine(xv, values, p, cu, text)
+            e[p] = (k + 2) * 2.0 ** -23 * s
+            if kind == product_schedule.FP8:
+                e[p] += P.cut(xv, kx, values, kws, p, cu, text)
+        want, off = P.gated(act, v["_gate"], v[""], e["_gate"], e[""], True) if act else (v[""], e[""])
+    near(out[:cu[-1]], want, off + HALF[dt] * (want.abs() + off), "out")
+
+
+@pytest.mark.parametrize("shape", product_schedule.TOGETHER, ids=str)
+def test_gradients_together(shape):
+    backward_bits(shape, sum(shape[0]), True, True)
