@@ -393,20 +393,22 @@ __global__ __launch_bounds__(256) void k_product_join(ProductProblem p) {
 
 // Splits of the sum, no shorter than 4 steps each, where tiles are fewer than two for each of the 256 CUs; one in a backward
 // pass, whose two products run together.  They do not depend on what else a call forms, so that an output alone has
-// the same bits.  (512 x 256 -> 1024: 11.2 us on 128 tiles in 4 splits, their sums included)
+// the same bits: the weights' gradients are cut as if the call formed all of them, one for each part, or by stream for each
+// part of either.  (512 x 256 -> 1024: 11.2 us on 128 tiles in 4 splits, their sums included)
 constexpr long long kSplitTiles = 512;
 static long long most_splits(int kind, long long rows, int K, int N, int parts) {
   const long long steps = kind == PRODUCT_OUT ? K / kStep : kind == PRODUCT_DX ? (long long)parts * N / kStep : rows / kStep;
   return std::max(1ll, steps / 4);
 }
-static int splits_of(int kind, long long rows, int K, int N, int parts, int outs, int B, bool merged) {
-  const long long tm = kind == PRODUCT_DW ? (long long)outs * ((N + 63) / 64) : (rows + 63) / 64 + (merged ? 0 : 2 * B - 1);  // row_tiles_bound
+static int splits_of(int kind, long long rows, int K, int N, int parts, int B, bool merged) {
+  const long long tm = kind == PRODUCT_DW ? (long long)parts * (merged ? 1 : 2) * ((N + 63) / 64) : (rows + 63) / 64 + (merged ? 0 : 2 * B - 1);  // row_tiles_bound
   const int bn = kind == PRODUCT_OUT && parts == 2 ? 32 : 64, cols = kind == PRODUCT_OUT ? N : K;
   const long long tiles = std::max(1ll, tm * ((cols + bn - 1) / bn));
   return int(std::min(std::max(1ll, (kind == PRODUCT_OUT ? kSplitTiles : kSplitTiles / 2) / tiles), most_splits(kind, rows, K, N, parts)));
 }
 
-// Bounds the partial sums of any call, and grows with the sizes: a tile's are 64 x 64.
+// Bounds the partial sums of any call, and grows with the sizes: a tile's are 64 x 64.  Weights' gradients without text may
+// be twice as many as they are cut for (stream 1's are zeros), of at most half as many tiles as other sums.
 size_t product_part_bytes(bool bf16, int kind, long long rows, int K, int N, int parts) {
   if (bf16) return kind == PRODUCT_OUT && rows <= kProductFewRows ? 0 : product_tiles_part_bytes();
   const long long most = most_splits(kind, rows, K, N, parts);
@@ -417,7 +419,7 @@ size_t product_part_bytes(bool bf16, int kind, long long rows, int K, int N, int
 
 // Sets the splits; workgroups of the product and of the sums of its splits.
 static int product_blocks(int kind, ProductProblem &p) {
-  p.splits = splits_of(kind, p.rows, p.K, p.N, p.parts, p.outs, p.B, p.merged);
+  p.splits = splits_of(kind, p.rows, p.K, p.N, p.parts, p.B, p.merged);
   const long long tm = kind == PRODUCT_DW ? (long long)p.outs * ((p.N + 63) / 64) : row_tiles_bound(p, 64);
   const int cols = kind == PRODUCT_OUT ? p.N : p.K, bn = kind == PRODUCT_OUT && p.parts == 2 ? 32 : 64;
   const int wide = (cols + bn - 1) / bn * p.splits;  // of one row tile
@@ -592,17 +594,23 @@ __global__ __launch_bounds__(256) void k_gate_back(GateBackProblem p) {
   }
 }
 
-// A workgroup has 64 columns (block) of one sum, a wave every W-th row block, eight on their way.
+// A workgroup of W waves has 64 columns (block) of one sum.  Its row blocks go to kBackSums partial sums in turn, whatever W is, so
+// that a call's other gradients do not change a bias's bits; a wave has every W-th partial sum, eight row blocks of each on
+// their way.
+constexpr int kBackSums = 8;
 template <bool BF16, int W>
 HILO_DEV void sum_columns(const GateBackProblem &p, int block, int which) {
-  __shared__ float sums[W][64];
+  constexpr int V = kBackSums / W;
+  __shared__ float sums[kBackSums][64];
   const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int stream = which / p.parts, part = which % p.parts;
   void *db = stream ? p.db[1][part] : p.db[0][part];
   const bool both = p.db[0][part] == p.db[1][part];
   if (!db || (both && stream)) return;
   const int n = block * 64 + lane;
-  float v = 0.f;
+  float v[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) v[j] = 0.f;
   int t0 = 0;  // blocks before the segment
   for (int i = 0; i < segments(p); ++i) {
     const Segment s = segment(p, i);
@@ -610,22 +618,27 @@ HILO_DEV void sum_columns(const GateBackProblem &p, int block, int which) {
     if (both || s.stream == stream) {
       const float *from = p.part + (size_t(t0) * p.parts + part) * p.N + min(n, p.N - 1);
 #pragma unroll 1
-      for (int t = wid; t < tiles; t += 8 * W) {
-        float w[8];
+      for (int t = wid; t < tiles; t += 8 * kBackSums) {
+        float w[V][8];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) w[k] = from[size_t(min(t + W * k, tiles - 1)) * p.parts * p.N];
+        for (int j = 0; j < V; ++j)
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v += t + W * k < tiles ? w[k] : 0.f;
+          for (int k = 0; k < 8; ++k) w[j][k] = from[size_t(min(t + W * j + kBackSums * k, tiles - 1)) * p.parts * p.N];
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+#pragma unroll
+          for (int k = 0; k < 8; ++k) v[j] += t + W * j + kBackSums * k < tiles ? w[j][k] : 0.f;
       }
     }
     t0 += tiles;
   }
-  sums[wid][lane] = v;
+#pragma unroll
+  for (int j = 0; j < V; ++j) sums[wid + W * j][lane] = v[j];
   __syncthreads();
   if (wid == 0 && n < p.N) {
     float s = sums[0][lane];
 #pragma unroll
-    for (int k = 1; k < W; ++k) s += sums[k][lane];
+    for (int k = 1; k < kBackSums; ++k) s += sums[k][lane];
     if (BF16) reinterpret_cast<uint16_t *>(db)[n] = f2bf(s);
     else reinterpret_cast<float *>(db)[n] = s;
   }

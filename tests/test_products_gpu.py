@@ -376,3 +376,39 @@ def test_plan(kind, images, text, k, n, streams, parts, plan):
 @pytest.mark.parametrize("shape", product_schedule.TOGETHER, ids=str)
 def test_gradients_together(shape):
     backward_bits(shape, sum(shape[0]), True, True)
+
+
+# ------------------------------------------------------------------------------------ which gradients a call forms
+
+def backward_call(shape, dt, act, seed):
+    """A backward pass of a shape on the device: form(dx, grads), and the shapes of all gradients."""
+    images, text, k, n, streams, parts = shape
+    cu, cud, randn, ws = on_device(shape, seed)
+    ws = [{name: t.to(dt) for name, t in d.items()} for d in ws]
+    x, dout, pre = randn(cu[-1], k).to(dt), randn(cu[-1], n).to(dt), randn(cu[-1], 2, n).to(dt) if act else None
+    work = scratch(hilo.hilo_linear_backward_workspace_bytes(dt, cu[-1], k, n, len(images), gated=parts == 2))
+    plan = hilo.linear_weights(ws)
+
+    def form(dx, grads):
+        hilo.hilo_linear_backward(plan, x, pre, dout, dx, hilo.linear_grads(grads) if grads else None, cud, text, act=ACTS[act], workspace=work)
+
+    return form, torch.empty_like(x), ws
+
+
+@pytest.mark.parametrize("shape", [([551], 0, 256, 1024, 1, 2), ([551], 0, 256, 1024, 1, 1), ([300, 70], 30, 256, 512, 2, 2), ([2000], 0, 64, 128, 1, 2),
+                                   ([90, 7, 260], 11, 40, 72, 2, 1), ([1], 0, 8, 8, 1, 2)], ids=str)
+def test_float32_gradients_alone(shape):
+    """In float32 each gradient has the same bits whichever others a call forms."""
+    form, dx, ws = backward_call(shape, torch.float32, "silu" if shape[-1] == 2 else None, 3)
+    got = [{name: torch.empty_like(t) for name, t in d.items()} for d in ws]
+    form(dx, got)
+    alone = torch.empty_like(dx)
+    form(alone, None)
+    assert torch.equal(alone, dx), "dx"
+    for kk, d in enumerate(got):
+        for name, t in d.items():
+            for with_dx in (False, True):
+                one = [{name: torch.empty_like(t)} if j == kk else {} for j in range(len(got))]
+                form(alone if with_dx else None, one)
+                assert torch.equal(one[kk][name], t), (name, kk, with_dx)
+                assert torch.equal(alone, dx), "dx"
