@@ -412,3 +412,22 @@ def test_float32_gradients_alone(shape):
                 form(alone if with_dx else None, one)
                 assert torch.equal(one[kk][name], t), (name, kk, with_dx)
                 assert torch.equal(alone, dx), "dx"
+
+
+# dx alone is cut along k there, beside the weights' gradients it is not
+@pytest.mark.parametrize("shape", [([2450], 0, 7112, 472, 1, 2), ([2450], 0, 7112, 1032, 1, 1), ([2000], 0, 2056, 2056, 1, 2)], ids=str)
+def test_equal_calls_give_equal_bits(shape):
+    """bf16 gradients together and each kind alone: against float64, and twice the same."""
+    parts = shape[-1]
+    assert product_schedule.together(*shape) and product_schedule.describe(product_schedule.DX, *shape)[2] > 1
+    for form_dx, form_dw in ((True, True), (True, False), (False, True)):
+        backward_bits(shape, 5, form_dx, form_dw)
+    form, dx, ws = backward_call(shape, torch.bfloat16, "silu" if parts == 2 else None, 4)
+    for with_dx, with_dw in ((True, True), (True, False), (False, True)):
+        runs = []
+        for _ in range(2):
+            one = [{name: torch.full_like(t, 7.0) for name, t in d.items()} for d in ws] if with_dw else None
+            out = torch.full_like(dx, 7.0)
+            form(out if with_dx else None, one)
+            runs.append([out] + [t for d in one or [] for t in d.values()])
+        assert all(torch.equal(a, b) for a, b in zip(*runs))
