@@ -396,11 +396,13 @@ HILO_DEV void run8(const ProductProblem &p, const Plan &q, int pid, uint8_t *lds
 // W is loaded for two windows at once, whole lines.  An MFMA of half h of a window multiplies values 16 g + 8 h .. + 7 of
 // lane group g.  4096 cubed 135 us, 1.02 PFLOP/s; a window takes 0.7 us alone, 0.9 on all CUs, of which its MFMAs and
 // conversions are 0.58.  4708 x 1536 -> 4096 with a gate into codes 138 us: 4.6 turns of tiles in 5, each 24 windows and 8 us
-// of activations, maxima, codes.
-template <bool GATED_>
+// of activations, maxima, codes.  Of a float32 call the activations are as exact as finish_out's, so that its codes are of
+// the values that it leaves without out_scale: 10 us more there.
+template <bool GATED_, bool EXACT_>
 struct GeoW {
   static constexpr int BM = 128, BN = 256, KIND = PRODUCT_OUT;
   static constexpr bool GATED = GATED_;
+  static constexpr bool EXACT = EXACT_;  // the gate of float32 calls
   static constexpr int MB = 4, NB = 4;  // blocks of 16 x 16 of a wave, 2 x 4 waves
   static constexpr int COLS = GATED ? BN / 2 : BN;
   static constexpr int XB = BM * 128, XSLOTS = 4, WB = BN * 128;  // a window of x, two of W in two slots
@@ -630,7 +632,7 @@ HILO_DEV void run_wide(const ProductProblem &p, const Plan &q, int pid, uint8_t 
         for (int j = 0; j < 2; ++j)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const float h = gate_act<false>(acc[i][j][e] + bias[j][e], p.silu) * (acc[i][2 + j][e] + bias[2 + j][e]);
+            const float h = gate_act<G::EXACT>(acc[i][j][e] + bias[j][e], p.silu) * (acc[i][2 + j][e] + bias[2 + j][e]);
             acc[i][j][e] = h;
             top = n + 16 * j < p.N ? max(top, abs_bits(h)) : top;
           }
@@ -747,9 +749,9 @@ __global__ __launch_bounds__(512) void k_product_fp8_fix(ProductProblem p) {
   else fix8<Geo8<128, 256, GATED>>(p, q);
 }
 
-template <bool GATED>
+template <bool GATED, bool EXACT>
 __global__ __launch_bounds__(512, 2) void k_product_fp8_wide(ProductProblem p) {
-  using G = GeoW<GATED>;
+  using G = GeoW<GATED, EXACT>;
   __shared__ __attribute__((aligned(1024))) uint8_t lds[G::LDS];
   const Plan q = make_plan<G>(p, count_row_tiles(p, G::BM), 1, kCost8[1]);
   run_wide<G>(p, q, xcd_remap(blockIdx.x, P), lds);
@@ -772,8 +774,9 @@ static hipError_t run_tiles8(ProductProblem p, hipStream_t st) {
 
 hipError_t launch_product_fp8_wide(ProductProblem p, hipStream_t st) {
   p.splits = 0;  // whole tiles
-  if (p.parts == 2) hipLaunchKernelGGL(pt::k_product_fp8_wide<true>, dim3(pt::P), dim3(512), 0, st, p);
-  else hipLaunchKernelGGL(pt::k_product_fp8_wide<false>, dim3(pt::P), dim3(512), 0, st, p);
+  if (p.parts == 1) hipLaunchKernelGGL((pt::k_product_fp8_wide<false, false>), dim3(pt::P), dim3(512), 0, st, p);
+  else if (p.bf16) hipLaunchKernelGGL((pt::k_product_fp8_wide<true, false>), dim3(pt::P), dim3(512), 0, st, p);
+  else hipLaunchKernelGGL((pt::k_product_fp8_wide<true, true>), dim3(pt::P), dim3(512), 0, st, p);
   return hipGetLastError();
 }
 

@@ -431,3 +431,21 @@ def test_equal_calls_give_equal_bits(shape):
             form(out if with_dx else None, one)
             runs.append([out] + [t for d in one or [] for t in d.values()])
         assert all(torch.equal(a, b) for a, b in zip(*runs))
+
+
+@pytest.mark.parametrize("T,K,N", [(2000, 128, 4112), (1300, 272, 2064), (40, 144, 4112), (300, 1040, 144)], ids=case_id)
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+def test_codes_are_of_the_float32_values(T, K, N, act):
+    """Codes out of a float32 call are those of the rows that it leaves without out_scale, bit for bit."""
+    g = torch.Generator(device="cuda").manual_seed(T)
+    x, cud = torch.randn(T, K, device="cuda", generator=g), torch.tensor([0, T], dtype=torch.int32, device="cuda")
+    d = {"w" + p: torch.randn(N, K, device="cuda", generator=g) * K ** -0.5 for p in ("", "_gate")}
+    d.update({"b" + p: torch.randn(N, device="cuda", generator=g) for p in ("", "_gate")})
+    plan, work = hilo.linear_weights_fp8([hilo.quantize_block_weights(**d)]), scratch(hilo.hilo_linear_fp8_workspace_bytes(T, K, N, True))
+    out, (codes, want) = torch.empty(T, N, device="cuda"), torch.empty(2, T, N, dtype=torch.uint8, device="cuda")
+    scales, ks = torch.empty(2, T, hilo.scale_stride(N), dtype=torch.uint8, device="cuda")
+    hilo.hilo_linear_fp8(plan, x, out, cud, act=ACTS[act], workspace=work)
+    hilo.hilo_quantize_blocks(out, want, ks)
+    hilo.hilo_linear_fp8(plan, x, codes, cud, act=ACTS[act], out_scale=scales, workspace=work)
+    assert torch.equal(scales, ks)
+    assert int((codes != want).sum()) == 0
