@@ -449,3 +449,96 @@ def test_codes_are_of_the_float32_values(T, K, N, act):
     hilo.hilo_linear_fp8(plan, x, codes, cud, act=ACTS[act], out_scale=scales, workspace=work)
     assert torch.equal(scales, ks)
     assert int((codes != want).sum()) == 0
+
+
+# ------------------------------------------------------------------------ FP8: many tiles, many samples, large buffers
+
+def codes_near(codes, scales, want, off, what):
+    """Codes and scales of values `want` that are off by `off`: the scale of a largest value in that range, a code's rounding."""
+    k = scales[:, :-(-want.shape[1] // 128)].to(F64) - 127
+    lo, hi = (torch.stack([b.amax(1) for b in t.split(128, 1)], 1) for t in ((want.abs() - off).clamp(min=0), want.abs() + off))
+    assert ((k >= P.block_exponent(lo)) & (k <= P.block_exponent(hi))).all(), what
+    scale = torch.exp2(k).repeat_interleave(128, 1)[:, :want.shape[1]]
+    near(P.decode(codes, scales, 1), want, off + 2.0 ** -4 * (want.abs() + off) + 2.0 ** -10 * scale, what)
+
+
+def fp8_bits(shape, dt, coded, seed):
+    """An FP8 product of a shape against float64."""
+    images, text, k, n, streams, parts = shape
+    act = "silu" if parts == 2 else None
+    cu, cud, randn, ws = on_device(shape, seed)
+    T = cu[-1] + BEHIND
+    x, ws = randn(cu[-1], k).to(dt), [{name: t.to(dt) for name, t in d.items()} for d in ws]
+    plans = [hilo.quantize_block_weights(d["w"], d["b"], d.get("w_gate"), d.get("b_gate")) for d in ws]
+    out = torch.full((T, n), 7, dtype=torch.uint8 if coded else dt, device="cuda")
+    os = torch.full((T, hilo.scale_stride(n)), 7, dtype=torch.uint8, device="cuda") if coded else None
+    hilo.hilo_linear_fp8(hilo.linear_weights_fp8(plans), padded(x), out, cud, text, act=ACTS[act], out_scale=os,
+                         workspace=scratch(hilo.hilo_linear_fp8_workspace_bytes(T, k, n, gated=parts == 2)))
+    codes, scales = torch.empty_like(x, dtype=torch.uint8), torch.empty(cu[-1], hilo.scale_stride(k), dtype=torch.uint8, device="cuda")
+    hilo.hilo_quantize_blocks(x, codes, scales)
+    xv, kx = P.decode(codes, scales, 1), scales[:, :-(-k // 128)].to(F64) - 127
+    names = ("", "_gate")[:parts]
+    values = [{**d, **{"w" + p: P.decode(q["w" + p], q["s" + p], 128) for p in names}} for d, q in zip(ws, plans)]
+    kws = [{"w" + p: q["s" + p][:, :-(-k // 128)].to(F64) - 127 for p in names} for q in plans]
+    v, e = {}, {}
+    with torch.device("cuda"):
+        for p in names:
+            v[p], s = P.affine(xv, values, p, cu, text)
+            e[p] = (k + 2) * 2.0 ** -23 * s
+            if dt is torch.bfloat16 and not coded:
+                e[p] += P.cut(xv, kx, values, kws, p, cu, text)
+        want, off = P.gated(act, v["_gate"], v[""], e["_gate"], e[""], True) if act else (v[""], e[""])
+        assert (out[cu[-1]:] == 7).all()
+        if not coded:
+            return near(out[:cu[-1]], want, off + HALF[dt] * (want.abs() + off), "out")
+        assert (os[cu[-1]:] == 7).all() and not os[:cu[-1], -(-n // 128):].any()
+        codes_near(out[:cu[-1]], os[:cu[-1]], want, off, "codes")
+
+
+# more tiles than workgroups and than two each, of one window pair and of several, odd and even, of one segment and of many
+MANY = [24, 0, 61, 130, 7, 300, 1, 90] * 5
+TILED = [([2000], 0, 16, 4112, 1), ([2000], 0, 128, 4112, 1), ([1900], 9, 272, 4112, 2), ([4100], 0, 512, 4112, 1), (MANY, 5, 16, 4112, 2), (MANY, 5, 400, 1040, 2),
+         ([40] * 33, 0, 144, 2064, 1), ([3, 0, 66] * 12, 13, 1040, 144, 2), ([3, 0, 6] * 13, 3, 1040, 144, 2), ([1, 0] * 20, 1, 272, 528, 2)]
+LEAVES = [(torch.float32, 1, False), (torch.float32, 2, False), (torch.float32, 2, True), (torch.bfloat16, 2, True), (torch.bfloat16, 1, False), (torch.bfloat16, 2, False)]
+
+
+@pytest.mark.parametrize("dt,parts,coded", LEAVES, ids=case_id)
+@pytest.mark.parametrize("shape", TILED, ids=lambda s: f"{len(s[0])}x{sum(s[0])}-{s[1:]}".replace(" ", ""))
+def test_fp8_tiles(shape, dt, parts, coded):
+    fp8_bits((*shape, parts), dt, coded, len(shape[0]) + shape[2])
+
+
+@pytest.mark.parametrize("T,K,N,dt,parts,coded", [(530000, 16, 4112, torch.bfloat16, 1, False), (530000, 16, 4112, torch.bfloat16, 2, False),
+                                                  (270000, 16, 4112, torch.float32, 1, False), (1050000, 16, 4112, torch.float32, 2, True),
+                                                  (1050000, 4112, 16, torch.bfloat16, 1, False), (530000, 4112, 16, torch.float32, 1, False)], ids=case_id)
+def test_fp8_past_32_bits(T, K, N, dt, parts, coded):
+    """Rows, codes or outputs of more than 2^32 bytes: rows at both ends and in the middle against float64."""
+    act = "silu" if parts == 2 else None
+    g = torch.Generator(device="cuda").manual_seed(T)
+    x = torch.empty(T, K, dtype=dt, device="cuda").normal_(generator=g)
+    d = {"w" + p: torch.empty(N, K, device="cuda").normal_(generator=g).mul_(K ** -0.5) for p in ("", "_gate")[:parts]}
+    q = hilo.quantize_block_weights(d["w"], None, d.get("w_gate"))
+    codes, scales = torch.empty(T, K, dtype=torch.uint8, device="cuda"), torch.empty(T, hilo.scale_stride(K), dtype=torch.uint8, device="cuda")
+    hilo.hilo_quantize_blocks(x, codes, scales)
+    del x
+    out = torch.empty(T, N, dtype=torch.uint8 if coded else dt, device="cuda")
+    os = torch.empty(T, hilo.scale_stride(N), dtype=torch.uint8, device="cuda") if coded else None
+    assert max(t.numel() * t.element_size() for t in (codes, out)) > 1 << 32 or T * K * 2 > 1 << 32  # the last of the widened rows
+    cud = torch.tensor([0, T], dtype=torch.int32, device="cuda")
+    hilo.hilo_linear_fp8(hilo.linear_weights_fp8([q]), codes, out, cud, x_scale=scales, out_scale=os, act=ACTS[act],
+                         workspace=scratch(hilo.hilo_linear_fp8_workspace_bytes(T, K, N, gated=parts == 2)))
+    values = [{"w" + p: P.decode(q["w" + p], q["s" + p], 128) for p in ("", "_gate")[:parts]}]
+    kws = [{"w" + p: q["s" + p][:, :-(-K // 128)].to(F64) - 127 for p in ("", "_gate")[:parts]}]
+    for a in (0, T // 2, T - 60):
+        xv, kx, v, e = P.decode(codes[a:a + 60], scales[a:a + 60], 1), scales[a:a + 60, :-(-K // 128)].to(F64) - 127, {}, {}
+        with torch.device("cuda"):
+            for p in ("", "_gate")[:parts]:
+                v[p], s = P.affine(xv, values, p, [0, 60], 0)
+                e[p] = (K + 2) * 2.0 ** -23 * s
+                if dt is torch.bfloat16 and not coded:
+                    e[p] += P.cut(xv, kx, values, kws, p, [0, 60], 0)
+            want, off = P.gated(act, v["_gate"], v[""], e["_gate"], e[""], True) if act else (v[""], e[""])
+            if coded:
+                codes_near(out[a:a + 60], os[a:a + 60], want, off, a)
+            else:
+                near(out[a:a + 60], want, off + HALF[dt] * (want.abs() + off), a)
