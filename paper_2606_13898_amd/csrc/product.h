@@ -107,7 +107,8 @@ HILO_DEV void gate_slope(float g, bool silu, float &act, float &slope) {
   slope = q == 0.f ? p : p + g * q * (silu ? 1.0f : c * (1.0f + 3.0f * 0.044715f * g * g));
 }
 
-// 8 E4M3 codes times their scale as bf16, exact; scale: the bits of a float32 whose exponent is the E8M0 byte.
+// 8 E4M3 codes times their scale as bf16, exact; scale: the bits of a float32 whose exponent is the E8M0 byte.  The conversion
+// takes that exponent alone: 0 is 2^-127, and 255 makes every value NaN, a zero's too.
 HILO_DEV bf16x8 wide_codes(uint32_t x, uint32_t y, uint32_t scale) {
   typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
   const float s = __uint_as_float(scale);

@@ -183,7 +183,7 @@ __global__ __launch_bounds__(64 * kWaves) void k_product_few(ProductProblem p) {
             xc[2 * h] = int(fp8x4(f[h][0] * inv, f[h][1] * inv, f[h][2] * inv, f[h][3] * inv));
             xc[2 * h + 1] = int(fp8x4(f[h][4] * inv, f[h][5] * inv, f[h][6] * inv, f[h][7] * inv));
           }
-          sx = finite ? 127 + k : 255;
+          sx = finite ? 127 + k : 255;  // NaN, whatever the codes are
         }
 #pragma unroll
         for (int m = 0; m < 4; ++m) {

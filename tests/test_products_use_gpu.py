@@ -338,3 +338,62 @@ def test_far_gates(act, dt):
     dout, db = torch.ones(T, N, dtype=dt, device="cuda"), [{"b": empty(N, dtype=dt), "b_gate": empty(N, dtype=dt)}]
     hilo.hilo_linear_backward(plan, x, pre, dout, None, hilo.linear_grads(db), cud, act=ACTS[act], workspace=ws)
     assert torch.equal(db[0]["b_gate"].float(), 2.0 * (g > 0)) and torch.equal(db[0]["b"].float(), torch.where(g > 0, g, torch.zeros_like(g)))
+
+
+# T, N and whether codes leave, for each form of an FP8 product: few rows with and without quantisation in the product, FP8 tiles,
+# widened rows, float32 tiles cut along k
+FORMS = [(BF, 1, 144, False), (BF, 4, 144, False), (BF, 4, 144, True), (BF, 16, 144, False), (BF, 40, 144, False), (F32, 4, 144, False), (F32, 40, 144, True),
+         (BF, 300, 144, False), (F32, 300, 1552, False), (BF, 300, 784, True), (F32, 300, 784, True), (F32, 300, 144, False), (BF, 100, 144, True)]
+
+
+def gate_and_up(dt, N, K, **kw):
+    d = hilo.quantize_block_weights(empty(N, K).normal_(), empty(N, dtype=dt).normal_(), empty(N, K).normal_(), empty(N, dtype=dt).normal_())
+    return dict(d, **kw)
+
+
+def gated_rows(plan, x, dt, T, K, N, coded, **kw):
+    """Outputs of a product with a gate in float64, of codes what they stand for."""
+    out, scale = empty(T, N, dtype=U8 if coded else dt), empty(T, hilo.scale_stride(N), dtype=U8) if coded else None
+    hilo.hilo_linear_fp8(plan, x, out, cu_of(T), act=hilo.ACT_SILU, out_scale=scale, workspace=bytes_of(hilo.hilo_linear_fp8_workspace_bytes(T, K, N, True)), **kw)
+    return P.decode(out.cpu(), scale.cpu(), 1) if coded else out.cpu().to(F64)
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("dt,T,N,coded", FORMS, ids=case_id)
+def test_blocks_that_are_not_finite(dt, T, N, coded, bad):
+    """A block of x that holds NaN or an infinity has NaN for codes and scale: the row's outputs are NaN in every form."""
+    K, row = 272, T // 2
+    x = empty(T, K, dtype=dt).normal_()
+    x[row, 128:256] = 0
+    x[row, 200] = bad
+    v = gated_rows(hilo.linear_weights_fp8([gate_and_up(dt, N, K)]), x, dt, T, K, N, coded)
+    others = [i for i in range(T) if i != row]
+    assert v[row].isnan().all() and v[others].isfinite().all()
+
+
+@pytest.mark.parametrize("dt,T,N,coded", FORMS, ids=case_id)
+def test_scales_of_nan(dt, T, N, coded):
+    """A scale of 255 makes its block NaN whatever its codes are, zeros too: of a row its outputs, of W those of its 128 columns."""
+    K = 272
+    codes, scales = empty(T, K, dtype=U8), empty(T, hilo.scale_stride(K), dtype=U8)
+    hilo.hilo_quantize_blocks(empty(T, K, dtype=dt).normal_(), codes, scales)
+    d = gate_and_up(dt, N, K)
+    good = gated_rows(hilo.linear_weights_fp8([d]), codes, dt, T, K, N, coded, x_scale=scales)
+    assert good.isfinite().all()
+    for zero in (False, True):
+        c, s, row = codes.clone(), scales.clone(), T // 2
+        s[row, 1] = 255
+        if zero:
+            c[row, 128:256] = 0
+        v = gated_rows(hilo.linear_weights_fp8([d]), c, dt, T, K, N, coded, x_scale=s)
+        others = [i for i in range(T) if i != row]
+        assert v[row].isnan().all(), ("x", zero)
+        assert torch.equal(v[others], good[others])
+        for part in ("", "_gate"):
+            e = dict(d, **{k + part: d[k + part].clone() for k in ("w", "s")})
+            e["s" + part][0, 2] = 255  # of the last block, 16 wide
+            if zero:
+                e["w" + part][:128, 256:] = 0
+            v = gated_rows(hilo.linear_weights_fp8([e]), codes, dt, T, K, N, coded, x_scale=scales)
+            assert v[:, :128].isnan().all(), ("w" + part, zero)
+            assert torch.equal(v[:, 128:], good[:, 128:])
