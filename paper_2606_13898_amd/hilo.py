@@ -760,7 +760,7 @@ def _workspace(workspace, dev: int):
 def _gated_pointers(struct, ds: Sequence[dict], dtype):
     """Two of `struct` from dicts of tensors (one dict: for both streams): weights of one shape [out][in], biases [out] of one
     type; dtype the weights' type, or None: float32 or bfloat16, that of the biases too.  Any may be missing."""
-    ds = list(ds)
+    ds = [dict(d) for d in ds]  # kept below, whatever the caller does with theirs
     if not 1 <= len(ds) <= 2:
         raise ValueError("of one or two streams")
     arr = (struct * 2)()

@@ -1,8 +1,10 @@
 """The products of a feed-forward on the host: what the library and the binding refuse before anything is enqueued, and the
 float64 oracle against other ways to the same values (CPU only)."""
 import ctypes
+import gc
 import math
 import os
+import weakref
 
 import product_schedule
 import pytest
@@ -235,6 +237,20 @@ def test_fp8_weights_refuse():
     for codes, scales in ((OnDevice(U8, 8, 16), OnDevice(U8, 8, 4)), (OnDevice(U8, 8, 32), OnDevice(U8, 8, 1)), (OnDevice(torch.int8, 8, 32), OnDevice(U8, 8, 4))):
         with pytest.raises(ValueError):
             hilo.hilo_quantize_blocks(OnDevice(BF, 8, 32), codes, scales)
+
+
+@built
+@pytest.mark.parametrize("of,d", [(hilo.linear_weights, weights), (hilo.linear_grads, weights),
+                                  (hilo.linear_weights_fp8, lambda: weights(dt=U8, b=OnDevice(BF, 16), b_gate=None, s=OnDevice(U8, 1, 4), s_gate=OnDevice(U8, 1, 4)))])
+def test_tensors_are_kept(of, d):
+    """Weights and gradients keep their tensors, not the caller's dicts, which may change afterwards."""
+    ds = [d(), d()]
+    kept = [weakref.ref(t) for e in ds for t in e.values() if t is not None]
+    arr = of(ds)
+    ds[0].clear()
+    ds[1].update(w=None, b=OnDevice(BF, 16))
+    gc.collect()
+    assert all(r() is not None for r in kept) and arr is not None
 
 
 @built
