@@ -553,7 +553,7 @@ def hilo_token_positions(shape, fine_idx, pool_idx, counts, cu_seqlens, seg_off,
 def _vectors(h, vectors: dict, gains: dict):
     """Fills the pointers of a hilo_norms or hilo_norm_grads; keeps the tensors and what they are on it."""
     h.batch = h.dim = h.dev = None
-    h.kept = [vectors, gains]
+    h.kept = [vectors]
     for name, v in vectors.items():
         if v is None:
             continue
@@ -578,6 +578,7 @@ def _vectors(h, vectors: dict, gains: dict):
                 raise ValueError(f"{name}: expected float32 [dim] for the image and the text stream")
             h.dim = g.numel()
             _same_device(h, g, name)
+            h.kept.append(g)
             getattr(h, name)[k] = g.data_ptr()
     h.fits = (h.dim, h.batch, h.dev)
     return h
@@ -695,7 +696,7 @@ def quantize_i8_weights(w, b=None, stream=None) -> dict:
 def linear_weights_i8(ws: Sequence[dict]):
     """Weights of hilo_linear_i8: {"w": int8 [out][in], "s": float32 [out], "b": [out] or None} of the image and the text
     stream (one dict: of both).  Keeps the tensors alive."""
-    ws = list(ws)
+    ws = [dict(w) for w in ws]  # kept below, whatever the caller does with theirs
     if not 1 <= len(ws) <= 2:
         raise ValueError("weights of one or two streams")
     arr = (hilo_linear_w_i8 * 2)()

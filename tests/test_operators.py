@@ -1,8 +1,10 @@
 """The rotary, sandwich-norm and int8 operators on the host: what the library and the binding refuse before anything is
 enqueued, and the float64 oracle against other ways to the same values (CPU only)."""
 import ctypes
+import gc
 import os
 import re
+import weakref
 
 import numpy as np
 import pytest
@@ -432,3 +434,17 @@ def test_linear_plans_with_gelu():
              for p in (linear_schedule.describe(*shape, True) for shape, _ in linear_schedule.SHAPES)}
     assert kinds == {("small", False, False), (128, False, False), (192, False, False), (256, False, False), (192, True, False),
                      (192, True, True), (256, True, True)}
+
+
+@built
+def test_tensors_are_kept():
+    """int8 weights and norms' gains keep their tensors, not the caller's dicts and lists, which may change afterwards."""
+    w = [dict(w=OnDevice(torch.int8, 16, 32), s=OnDevice(torch.float32, 16), b=OnDevice(torch.float32, 16)) for _ in range(2)]
+    gains, slopes = [[OnDevice(torch.float32, 32), OnDevice(torch.float32, 32)] for _ in range(2)]
+    kept = [weakref.ref(t) for d in w for t in d.values()] + [weakref.ref(t) for t in gains + slopes]
+    made = hilo.linear_weights_i8(w), hilo.norms(post_gain=gains), hilo.norm_grads(pre_gain=slopes)
+    w[0].clear()
+    w[1].update(b=None)
+    gains[:] = slopes[:] = [None, None]
+    gc.collect()
+    assert all(r() is not None for r in kept) and made
