@@ -613,10 +613,15 @@ static long long shares(const ProductProblem &x, const ProductProblem &w, bool b
   return *std::max_element(each, each + pt::P);
 }
 
-hipError_t launch_product_back_tiles(ProductProblem x, ProductProblem w, hipStream_t st) {
+// Whether both products in one launch are quicker than each with a plan of its own.
+static bool one_launch(const ProductProblem &x, const ProductProblem &w) {
   pt::Plan q;
   const long long dx = plan_rows<PRODUCT_DX, false>(x, q), dw = plan_rows<PRODUCT_DW, false>(w, q);
-  if (shares(x, w, true) >= dx + (w.merged ? dw : std::min(dw, shares(x, w, false)))) {
+  return shares(x, w, true) < dx + (w.merged ? dw : std::min(dw, shares(x, w, false)));
+}
+
+hipError_t launch_product_back_tiles(ProductProblem x, ProductProblem w, hipStream_t st) {
+  if (!one_launch(x, w)) {
     const hipError_t e = run_tiles<PRODUCT_DX, false>(x, st);
     return e != hipSuccess ? e : run_tiles<PRODUCT_DW, false>(w, st);
   }

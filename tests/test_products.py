@@ -4,6 +4,8 @@ import ctypes
 import gc
 import math
 import os
+import random
+import subprocess
 import weakref
 
 import product_schedule
@@ -11,7 +13,7 @@ import pytest
 import torch
 
 from oracle import hilo_products as P
-from paper_2606_13898_amd import hilo
+from paper_2606_13898_amd import build, hilo
 from test_operators import DEVICE, DTYPE, F, NULL, PARAM, SHAPE, WORKSPACE, OnDevice, built, no_gpu
 
 F64 = torch.float64
@@ -335,3 +337,53 @@ def test_shapes_reach_every_plan():
     got = {(kind, parts, plan[0], plan[2] > 1) for kind, *_, parts, plan in product_schedule.SHAPES}
     assert got == {(kind, parts, tile, cut) for kind in range(4) for parts in (1, 2) for tile in product_schedule.TILES[kind] for cut in (False, True)}
     assert all(product_schedule.together(*shape, 3) for shape in product_schedule.TOGETHER)
+
+
+@pytest.fixture(scope="module")
+def library_plans(tmp_path_factory):
+    """The library's plans of calls, by its own sources compiled for the host."""
+    try:
+        hipcc = build.hipcc()
+    except RuntimeError:
+        pytest.skip("no hipcc")
+    exe = str(tmp_path_factory.mktemp("plans") / "plans")
+    # the kernels stay without device code, which nothing here launches
+    subprocess.run([hipcc, f"--offload-arch={build.ARCH}", "--offload-host-only", "-O1", "-std=c++17", "-w", "-I", build.CSRC, "-I", os.path.join(build.ROOT, "include"),
+                    os.path.join(os.path.dirname(__file__), "product_plans.hip"), "-o", exe, "-Wl,--unresolved-symbols=ignore-all"], check=True, timeout=300)
+
+    def plans(calls):
+        """calls: (kind, image rows, text rows, in, out, streams, parts), 3 rows more in the buffers; kind 4: one launch for all gradients."""
+        lines = []
+        for kind, images, text, k, n, streams, parts in calls:
+            segments, rows = product_schedule.segments(images, text, streams == 1), sum(images) + text * len(images) + 3
+            if kind == 4:
+                seen = len(images), text, 0
+            else:
+                nk = {product_schedule.OUT: -(-k // 64), product_schedule.DX: parts * -(-n // 64), product_schedule.FP8: -(-k // 128),
+                      product_schedule.DW: max(sum(-(-m // 64) for m, s in segments if s == t) for t in range(streams))}[kind]
+                seen = nk, *(sum(-(-m // bm) for m, _ in segments) for bm in (256, 128))
+            lines.append(" ".join(map(str, (kind, rows, k, n, parts, streams, *seen))))
+        out = subprocess.run([exe], input="\n".join(lines), capture_output=True, text=True, check=True, timeout=60).stdout.splitlines()
+        assert len(out) == len(calls)
+        return [tuple(map(int, line.split())) for line in out]
+
+    return plans
+
+
+def random_call(rng, kind):
+    size = lambda lo, hi: int(lo * (hi / lo) ** rng.random())  # noqa: E731
+    step, text = 16 if kind == product_schedule.FP8 else 8, rng.choice((0, size(1, 300)))
+    images = [size(1, 9000) for _ in range(rng.randint(1, 4))]
+    images[0] += 64
+    return kind, images, text, step * size(1, 16384 // step), step * size(1, 16384 // step), 2 if text else 1, rng.randint(1, 2)
+
+
+def test_model_is_the_library(library_plans):
+    """product_schedule.py's plans are the library's: of its shapes, and of calls all over the range."""
+    rng = random.Random(7)
+    calls = [call[:7] for call in product_schedule.SHAPES] + [random_call(rng, i % 4) for i in range(2000)]
+    for call, (tile, tiles, pieces) in zip(calls, library_plans(calls)):
+        assert product_schedule.describe(*call, 3) == (product_schedule.TILES[call[0]][tile], tiles, pieces), call
+    calls = [(4, *shape) for shape in product_schedule.TOGETHER] + [random_call(rng, 4) for _ in range(1000)]
+    for call, (one,) in zip(calls, library_plans(calls)):
+        assert product_schedule.together(*call[1:], 3) == bool(one), call
