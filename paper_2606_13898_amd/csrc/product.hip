@@ -74,10 +74,10 @@ HILO_DEV float e8m0(uint8_t b) {
 // the groups' sums meet in LDS.  Both operands lie in LDS as [row][k], whichever index is last in memory; rows are kPad
 // values long, so that 16 lanes' 16-byte reads fall on all banks once.  A lane of group lg takes k = 16 s + 4 lg .. + 3.
 //
-// Bound by the float32 MFMA: 2048 x 4096 -> 4096 in 550 us, 125 TFLOP/s (the library's product reaches 131), its dx 680, its dw
-// 910, whose operands both are transposed on their way to LDS.  Small ones by a launch, two loads on their way and the
+// Bound by the float32 MFMA: 2048 x 4096 -> 4096 in 558 us, 123 TFLOP/s (the library's product reaches 131), its dx alone 587, its
+// dw 646, whose operands both are transposed on their way to LDS.  Small ones by a launch, two loads on their way and the
 // tiles' number: 551 x 256 -> 1024 with a gate, 288 tiles for 256 CUs, 15.2 us, of which 6.6 do not grow with K.  Both
-// products of its gradients in a launch, and what is left in another: 34.4 us; in launches of their own 48.4.  Transposing
+// products of its gradients in a launch, and what is left in another: 33.9 us; in launches of their own 48.4.  Transposing
 // with four lanes' stores on a bank: 39.3.
 constexpr int kStep = 32, kPad = 36, kAhead = 2;
 
@@ -508,7 +508,7 @@ hipError_t launch_product_fp8(ProductProblem p, hipStream_t st) {
 // blocks in their order.  22560 x 8192 bf16: 373 us for 1.85 GB, 5.0 TB/s (a copy reaches 5.2), and 13 for the sums.
 constexpr int kBackCols = 512;
 // Rows of a block: the fewest of 4, 16, 64, 256 that leave at most 2048 workgroups (256 CUs have 8 each), or 256.  1005 x 8208
-// in blocks of 16: 17.7 us and 7.7 for the sums, of 4 23.6 and 10.2; 551 x 1024 of 4 9, of 16 11.7.
+// bf16 in blocks of 16: 17.9 us and 4.4 for the sums, of 4 20.2 and 5.6; 551 x 1024 float32 of 4 6.2 and 4.1, of 16 8.2 and 3.2.
 constexpr long long kBackItems = 2048;
 static int back_rows(long long rows, int N) {
   int b = 4;
@@ -721,8 +721,8 @@ HILO_DEV uint32_t top16(const float (&f)[8]) {
 
 // x is rounded to codes here, the one loss of an FP8 product: x 2^-k with the block's largest in (224, 448], exact but for the
 // rounding to 4 bits.  Bound by memory.
-// Rows: 16 lanes have the 128 columns of a scale, 8 a lane; a wave 512 columns of a row at a time.  2766 x 3072 bf16: 7.6 us,
-// 25.7 MB at 3.4 TB/s, ramp and tail.
+// Rows: 16 lanes have the 128 columns of a scale, 8 a lane; a wave 512 columns of a row at a time.  2766 x 3072 bf16: 8.0 us,
+// 25.5 MB at 3.2 TB/s, ramp and tail; 22560 x 3072 40.9, 5.1 TB/s.
 template <bool BF16>
 __global__ __launch_bounds__(256) void k_quantize_blocks(const void *__restrict__ x, int rows, int cols, const int *__restrict__ limit,
                                                          uint8_t *__restrict__ codes, uint8_t *__restrict__ scale) {
@@ -780,7 +780,8 @@ hipError_t launch_widen_rows(bool bf16, const void *x, const uint8_t *scale, int
   return hipGetLastError();
 }
 
-// Blocks of 128 x 128: a workgroup each, a thread 8 rows of 8 columns, held while the largest is found.
+// Blocks of 128 x 128: a workgroup each, a thread 8 rows of 8 columns, held while the largest is found.  Bound by memory: 8192 x
+// 3072 bf16 17.0 us, 75.5 MB at 4.5 TB/s, float32 24.8 at 5.1; 1024 x 1024, 64 workgroups, 5.6.
 template <bool BF16>
 __global__ __launch_bounds__(256) void k_quantize_tiles(const void *__restrict__ x, int rows, int cols, const int *__restrict__ limit,
                                                         uint8_t *__restrict__ codes, uint8_t *__restrict__ scale) {

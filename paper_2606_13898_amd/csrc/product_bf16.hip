@@ -15,8 +15,8 @@
 // Bound by the matrix cores at the power limit, and by what feeds them: a window of 256 x 256 takes 1.46 to 1.67 us on all CUs
 // (1.25 to 1.35 PFLOP/s; the library's large product reaches 1.30), 1.07 on few.  The rest: a tile's epilogue, 7 us, which
 // does not run beside the next tile's products (128 of a lane's 256 registers are accumulators, so there are no second ones),
-// and turns that are not full.  2766 x 3072 -> 8192 with a gate 270 us, 1.03 PFLOP/s; 4708 x 4096 -> 1536 63; 22560 x
-// 3072 -> 8192, gradients of both parts, 4.0 ms, 1.14.  The next tile's first windows are loaded before a tile's stores and
+// and turns that are not full.  2766 x 3072 -> 8192 with a gate 270 to 276 us, 1.02 PFLOP/s; 4708 x 4096 -> 1536 64;
+// 22560 x 3072 -> 8192, gradients of both parts, 4.1 ms, 1.11.  The next tile's first windows are loaded before a tile's stores and
 // not waited for behind them.
 #include <algorithm>
 

@@ -5,9 +5,10 @@
 // and four steps are on their way while four are multiplied.  The waves' sums meet in LDS.  Rows of a stream need not
 // lie side by side: each is looked up.
 //
-// One row 3072 -> 8192 with a gate: 24.7 us, 101 MB at 4.1 TB/s; FP8 codes 20.7 us, 50 MB.  At 64 rows it is level with the tiles for
-// the widest weights and ahead elsewhere (us, this and tiles): 3072 -> 8192 with a gate 1 row 25.7 and 36.3, 64 rows 41.3 and
-// 38.4; 3072 -> 3072 64 rows 16.5 and 20.5; 1024 -> 1024 7.1 and 13.5; FP8 32.5 and 34.5, 14.0 and 26.3, 7.5 and 14.9.
+// Measured (us, this and tiles, from weights in memory): 3072 -> 8192 with a gate 1 row 25.3 (101 MB at 4.0 TB/s) and 35.9, 64 rows
+// 41.2 and 37.5; 3072 -> 3072 64 rows 17.2 and 21.3; 1024 -> 1024 7.6 and 13.3; of FP8 codes 64 rows 29.7 and 32.4, 11.5 and
+// 25.3, 7.5 and 12.7.  So 64 rows stay here, although the widest bf16 weights would gain a tenth on tiles.  Four rows of FP8
+// 3072 -> 8192 with a gate, 50 MB: 17.7 us of codes, 21.9 of bf16 rows.
 //
 // FP8: up to 16 float rows are quantised where they are read, by every workgroup anew: a row's block of 128 is in four lanes, so
 // its largest value takes two exchanges, and a launch less is worth more than the arithmetic.  Codes are multiplied as

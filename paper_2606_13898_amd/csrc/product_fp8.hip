@@ -9,8 +9,8 @@
 // bits below (each group's sum is then added in float32's precision): enough for outputs of bf16, not for float32's or for
 // codes, which go another way (run_wide).
 //
-// Bound by the matrix cores and the loads that feed them: 22560 x 3072 -> 8192 with a gate 986 us (2.3 PFLOP/s; the library's
-// large product reaches 2.57); 2766 x 3072 -> 9216 93, two turns for 1.55 turns' tiles.
+// Bound by the matrix cores and the loads that feed them: 22560 x 3072 -> 8192 with a gate from codes 976 us (2.3 PFLOP/s; the
+// library's large product reaches 2.57); 2766 x 3072 -> 9216 96, two turns for 1.55 turns' tiles.
 //
 // A wave's 128 x 64 are 32 x 32 blocks: lane l holds row l % 32 and, W's rows being read in the order perm, columns
 // 16 (l / 32) .. + 15 of a block in register order.  With a gate the two blocks of columns are the gate's and the other's.
@@ -394,10 +394,10 @@ HILO_DEV void run8(const ProductProblem &p, const Plan &q, int pid, uint8_t *lds
 // scale exactly, at half the rate.  x comes as such bf16 rows (k_widen_rows); W's codes are widened behind LDS, 16 of a row by
 // a lane, which takes about as long as the MFMAs they feed (16 cycles for two values).  Tiles of 128 x 256, windows of 64 values;
 // W is loaded for two windows at once, whole lines.  An MFMA of half h of a window multiplies values 16 g + 8 h .. + 7 of
-// lane group g.  4096 cubed 135 us, 1.02 PFLOP/s; a window takes 0.7 us alone, 0.9 on all CUs, of which its MFMAs and
-// conversions are 0.58.  4708 x 1536 -> 4096 with a gate into codes 138 us: 4.6 turns of tiles in 5, each 24 windows and 8 us
-// of activations, maxima, codes.  Of a float32 call the activations are as exact as finish_out's, so that its codes are of
-// the values that it leaves without out_scale: 10 us more there.
+// lane group g.  4096 cubed 132 us, 1.04 PFLOP/s; a window takes 0.7 us alone, 0.9 on all CUs, of which its MFMAs and
+// conversions are 0.58.  4708 x 1536 -> 4096 with a gate into codes 129 us, 7 of them k_widen_rows: 4.6 turns of tiles in 5, each
+// 24 windows and 8 us of activations, maxima, codes.  Of a float32 call the activations are as exact as finish_out's, so that
+// its codes are of the values that it leaves without out_scale: 10 us more there.
 template <bool GATED_, bool EXACT_>
 struct GeoW {
   static constexpr int BM = 128, BN = 256, KIND = PRODUCT_OUT;
