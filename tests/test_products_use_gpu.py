@@ -397,3 +397,52 @@ def test_scales_of_nan(dt, T, N, coded):
             v = gated_rows(hilo.linear_weights_fp8([e]), codes, dt, T, K, N, coded, x_scale=scales)
             assert v[:, :128].isnan().all(), ("w" + part, zero)
             assert torch.equal(v[:, 128:], good[:, 128:])
+
+
+@pytest.mark.parametrize("rows,K,N", [(3000, 1040, 272), (5000, 144, 2064), (300, 4112, 528)], ids=case_id)
+@pytest.mark.parametrize("dt", [BF, F32], ids=case_id)
+def test_few_rows_of_large_buffers(dt, rows, K, N):
+    """Buffers of many rows of which few are in use, as where only the device knows how many a selection left: the plans go by
+    the buffers, the sums by the rows, and what lies behind is left alone."""
+    g = torch.Generator().manual_seed(rows)
+    cu, text = pack([30, 0, 24], 5), 5
+    T, cud, ulp = cu[-1], cu_of(*cu[1:]), 2.0 ** -23
+    tail = lambda t, v: torch.cat([t, torch.full((rows - T, *t.shape[1:]), v, dtype=t.dtype)]).cuda()  # noqa: E731
+    ws, nan = weights(g, 2, N, K, dt, True, True), float("nan")
+    x, dout, pre = (torch.randn(T, *s, generator=g).to(dt) for s in ((K,), (N,), (2, N)))
+    plan, out, dx, got = hilo.linear_weights(cuda(ws)), empty(rows, N, dtype=dt).fill_(7), empty(rows, K, dtype=dt).fill_(7), cuda(ws)
+    work = bytes_of(max(f(dt, rows, K, N, 3, True) for f in (hilo.hilo_linear_workspace_bytes, hilo.hilo_linear_backward_workspace_bytes))).fill_(0xff)
+    hilo.hilo_linear(plan, tail(x, nan), out, cud, text, act=hilo.ACT_SILU, workspace=work)
+    hilo.hilo_linear_backward(plan, tail(x, nan), tail(pre, nan), tail(dout, nan), dx, hilo.linear_grads(got), cud, text, act=hilo.ACT_SILU, workspace=work)
+    (u, su), (v, sv) = (P.affine(x.to(F64), ws, p, cu, text) for p in ("", "_gate"))
+    want, off = P.gated("silu", v, u, (K + 2) * ulp * sv, (K + 2) * ulp * su, dt is BF)
+    near(out[:T], want, off + HALF[dt] * (want.abs() + off), "out")
+    (wx, bx), grads = P.backward(x.to(F64), ws, pre.to(F64), dout.to(F64), "silu", cu, text, HALF[dt], False)
+    near(dx[:T], wx, bx, "dx")
+    for k in range(2):
+        for name, t in got[k].items():
+            near(t, *grads[k][name], f"{name} of {k}")
+    assert (out[T:] == 7).all() and (dx[T:] == 7).all()
+    # FP8, rows and codes out, against the same rows in buffers that they fill, within the form's float32 sums
+    q = [hilo.quantize_block_weights(d["w"], d["b"], d["w_gate"], d["b_gate"]) for d in cuda([{k: t.to(F32 if k[0] == "w" else dt) for k, t in d.items()} for d in ws])]
+    w8 = hilo.linear_weights_fp8(q)
+    xq, kx = P.quantize(x.to(F64), 1)
+    exact, kw = [{} for _ in ws], [{} for _ in ws]
+    for k in range(2):
+        for p in ("", "_gate"):
+            exact[k]["w" + p], kw[k]["w" + p] = P.quantize(ws[k]["w" + p].to(F64), 128)
+            exact[k]["b" + p] = ws[k]["b" + p]
+    v, e = {}, {}
+    for p in ("", "_gate"):
+        v[p], s = P.affine(xq, exact, p, cu, text)
+        e[p] = (K + 2) * ulp * s + (P.cut(xq, kx, exact, kw, p, cu, text) if dt is BF else 0)
+    want, off = P.gated("silu", v["_gate"], v[""], e["_gate"], e[""], True)
+    work = bytes_of(hilo.hilo_linear_fp8_workspace_bytes(rows, K, N, True)).fill_(0xff)
+    out.fill_(7)
+    hilo.hilo_linear_fp8(w8, tail(x, nan), out, cud, text, act=hilo.ACT_SILU, workspace=work)
+    near(out[:T], want, off + HALF[dt] * (want.abs() + off), "FP8 out")
+    h, hs = empty(rows, N, dtype=U8).fill_(9), empty(rows, hilo.scale_stride(N), dtype=U8).fill_(9)
+    hilo.hilo_linear_fp8(w8, tail(x, nan), h, cud, text, act=hilo.ACT_SILU, out_scale=hs, workspace=work)
+    scale = torch.exp2(hs[:T, :-(-N // 128)].cpu().to(F64) - 127).repeat_interleave(128, 1)[:, :N]
+    near(P.decode(h[:T].cpu(), hs[:T].cpu(), 1), want, off + 2.0 ** -4 * (want.abs() + off) + 2.0 ** -10 * scale, "codes")
+    assert (out[T:] == 7).all() and (h[T:] == 9).all() and (hs[T:] == 9).all()
