@@ -446,3 +446,20 @@ def test_few_rows_of_large_buffers(dt, rows, K, N):
     scale = torch.exp2(hs[:T, :-(-N // 128)].cpu().to(F64) - 127).repeat_interleave(128, 1)[:, :N]
     near(P.decode(h[:T].cpu(), hs[:T].cpu(), 1), want, off + 2.0 ** -4 * (want.abs() + off) + 2.0 ** -10 * scale, "codes")
     assert (out[T:] == 7).all() and (h[T:] == 9).all() and (hs[T:] == 9).all()
+
+
+@pytest.mark.parametrize("dt,T,N,whole", [(BF, 4, 16, False), (BF, 40, 16, False), (F32, 40, 16, False), (F32, 300, 16, False), (F32, 300, 4112, False), (BF, 300, 16, True)],
+                         ids=case_id)
+def test_values_that_float32_does_not_hold(dt, T, N, whole):
+    """Codes of 2^127, 2^128 and 2^135 times 2^-100: bf16 out above 64 rows multiplies them as they are, others as infinities."""
+    K = 128
+    codes, scales = empty(T, K, dtype=U8).fill_(0), empty(T, 4, dtype=U8).fill_(127)
+    codes[:, 0] = 0x38  # 1
+    for row, (code, scale) in enumerate(((0x70, 247), (0x78, 247), (0x78, 254))):  # 128 and 256
+        codes[row, 0], scales[row, 0] = code, scale
+    w = {"w": empty(N, K, dtype=U8).fill_(0x38), "s": empty(-(-N // 128), 4, dtype=U8).fill_(27)}
+    out = empty(T, N, dtype=dt)
+    hilo.hilo_linear_fp8(hilo.linear_weights_fp8([w]), codes, out, cu_of(T), x_scale=scales, workspace=bytes_of(hilo.hilo_linear_fp8_workspace_bytes(T, K, N)))
+    inf = float("inf")
+    for row, v in enumerate((2.0 ** 27, 2.0 ** 28 if whole else inf, 2.0 ** 35 if whole else inf, 2.0 ** -100)):
+        assert (out[row] == v).all(), row
