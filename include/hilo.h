@@ -503,9 +503,10 @@ size_t hilo_linear_i8_workspace_bytes(int64_t rows, int32_t in_dim); /* 0 if inv
  * stream 1 is not looked at when text_len is 0.  Where all pointers of both streams are the same, rows are
  * not split by stream, which is faster on many short samples.
  * in_dim and out_dim: multiples of 8, 8 .. 65536 (HILO_E_SHAPE).  Every tensor is aligned to 16 bytes, the
- * workspace to 256 (HILO_E_PARAM).  Outputs do not overlap inputs.  Workspace: device scratch of at least the
- * bytes that the function beside it gives (HILO_E_WORKSPACE; NULL will do where that is 0), contents undefined
- * after; calls that may overlap, two captured graphs among them, need one each.  Sums are taken in a fixed
+ * workspace to 256 (HILO_E_PARAM).  Outputs overlap neither inputs nor each other, but for gradients that both
+ * streams share.  Workspace: device scratch of at least the bytes that the function beside it gives
+ * (HILO_E_WORKSPACE; NULL will do where that is 0), contents undefined after; calls that may overlap, two captured
+ * graphs among them, need one each.  Sums are taken in a fixed
  * order: equal calls give equal bits.  The order goes by the sizes, and for bf16 gradients also by which of them
  * a call forms: dx alone and beside the weights' gradients may differ in their last bits.  In float32 they do not.
  * --------------------------------------------------------------------------------------------- */
