@@ -506,9 +506,9 @@ size_t hilo_linear_i8_workspace_bytes(int64_t rows, int32_t in_dim); /* 0 if inv
  * workspace to 256 (HILO_E_PARAM).  Outputs overlap neither inputs nor each other, but for gradients that both
  * streams share.  Workspace: device scratch of at least the bytes that the function beside it gives
  * (HILO_E_WORKSPACE; NULL will do where that is 0), contents undefined after; calls that may overlap, two captured
- * graphs among them, need one each.  Sums are taken in a fixed
- * order: equal calls give equal bits.  The order goes by the sizes, and for bf16 gradients also by which of them
- * a call forms: dx alone and beside the weights' gradients may differ in their last bits.  In float32 they do not.
+ * graphs among them, need one each.  Sums are taken in a fixed order: equal calls give equal bits.  The order goes
+ * by the sizes, and for bf16 gradients also by which of them a call forms: one alone may differ in its last bits
+ * from the same beside others.  In float32 it does not.
  * --------------------------------------------------------------------------------------------- */
 typedef struct {
   const void *w;      /* [out_dim][in_dim] dtype */
